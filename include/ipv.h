@@ -342,6 +342,123 @@ ipv_status ipv_device_error(uint32_t* err_out);
  * IPV_EINVAL (negative), IPV_ENOINIT. */
 ipv_status ipv_set_wait_limit(int64_t polls);
 
+/* ------------------------------------------------------------------------
+ * Paged cache: rows held in pages (bf16, or 8- or 4-bit codes), and attention
+ * over them. What a decoder does with a cache next to compressing it. These
+ * entry points need no ipv_init, allocate nothing, keep no state between calls
+ * and run on the current device; each call only enqueues kernels on its
+ * stream. Calls on different streams may overlap as long as they share no
+ * buffer that one of them writes (the workspace of ipv_attend is written).
+ *
+ * A pool holds n_pages pages of page_size rows for each of n_kv_heads heads.
+ * Row r of head h of page g is row number
+ *     g * page_stride + h * head_stride + r * row_stride
+ * of the arrays k and v (rows of head_dim elements or codes, contiguous) and,
+ * with codes, of k_par and v_par (head_dim/64 pairs). A half of the ping-pong
+ * cache is such a pool: one page per layer of one stream, page_size =
+ * token_capacity, head_stride = token_capacity, row_stride = 1.
+ *
+ * Codes. 64 neighbouring channels of a row form a group with two fp16 numbers,
+ * its step s and its minimum m (stored in that order): a code u stands for
+ * u*s + m. Writing x (bf16) with L = 255 (8 bits) or 15 (4 bits):
+ *     m = min x rounded down to fp16,  s = (max x - m)/L rounded up to fp16,
+ *     u = (x - m)/s rounded to the nearest integer (ties to even), 0..L
+ * (all u = 0 if s = 0). A group that holds a NaN, an infinity or a magnitude
+ * above 32768 gets s = m = NaN: all of it reads as NaN. A group's 4-byte words
+ * hold 4 (8 bits) or 8 (4 bits, lowest bits first) neighbouring channels; the
+ * word of channels 4(t+4w).. or 8(t+4w).., t = 0..3, is stored in place
+ * 4t + w or 2t + w of the group (the order in which the attention's threads
+ * read them). */
+typedef enum { IPV_PAGES_BF16 = 0, IPV_PAGES_U8 = 1, IPV_PAGES_U4 = 2 } ipv_pages_format;
+
+typedef struct {
+  ipv_pages_format format;
+  int n_kv_heads;
+  int head_dim;         /* <= 128; bf16: a multiple of 8; codes: 64 or 128 */
+  int page_size;        /* rows of a page: a power of two >= 16, or any size if
+                           the batch has max_pages = 1 */
+  int64_t n_pages;      /* < 2^31 */
+  int64_t page_stride, head_stride, row_stride; /* in rows, see above */
+  void* k;
+  void* v;              /* 16-byte aligned */
+  void* k_par;
+  void* v_par;          /* codes only: 4*(head_dim/64)-byte aligned */
+} ipv_pages;
+
+/* A batch of sequences (without sequences or rows a call does nothing, and its
+ * other tensors may be NULL): sequence b holds kv_len[b] rows, of which the last
+ * n = row_start[b+1] - row_start[b] are its new ones; the new rows of all
+ * sequences lie packed in the call's other tensors, sequence b's at rows
+ * row_start[b]... Its rows j = 0, 1, ... lie in row j % page_size of page
+ * table[b * table_stride + j / page_size].
+ * Device-side values that do not fit are made to: kv_len is cut to max_kv and
+ * to max_pages * page_size, n to max_rows, and a sequence whose rows do not
+ * lie in 0..total_rows-1 counts as one without new rows. Rows of a page number
+ * outside 0..n_pages-1 read as zero and are not written. */
+typedef struct {
+  int n_seqs;               /* 0 (nothing to do) .. 65535 */
+  int max_pages;            /* pages per sequence in the table */
+  const int32_t* table;     /* device; NULL (max_pages = 1): page b */
+  int64_t table_stride;     /* >= max_pages */
+  const int32_t* row_start; /* device [n_seqs + 1], ascending */
+  const int32_t* kv_len;    /* device [n_seqs], new rows included */
+  int64_t total_rows;       /* packed new rows: >= row_start[n_seqs] */
+  int max_rows;             /* >= every sequence's new rows */
+  int max_kv;               /* >= every kv_len */
+} ipv_batch;
+
+/* Writes the batch's new rows into the pages (quantising them if the pages
+ * hold codes). k_new, v_new: device bf16, row i of head h at element
+ * i * row_stride + h * head_stride (multiples of 8), 16-byte aligned. New rows
+ * before position 0 (more new rows than kv_len) are dropped. Two sequences must
+ * not write the same page row. Errors: IPV_EINVAL (before anything is
+ * enqueued), IPV_ECUDA. */
+ipv_status ipv_pages_write(const ipv_pages* pages, const ipv_batch* batch, const void* k_new,
+                           const void* v_new, int64_t row_stride, int64_t head_stride, void* stream);
+
+/* The inverse: reads the batch's new rows back from the pages into k_out and
+ * v_out (device bf16, laid out as k_new), each value u*s + m (in fp32) rounded
+ * once to bf16. With row_start = the sums of kv_len it reads whole sequences.
+ * Rows before position 0 are written as zero. Errors: as ipv_pages_write. */
+ipv_status ipv_pages_read(const ipv_pages* pages, const ipv_batch* batch, void* k_out, void* v_out,
+                          int64_t row_stride, int64_t head_stride, void* stream);
+
+/* Attention of the batch's new rows (queries) over their sequences' cached
+ * rows, new ones included: write them first. Query row i of sequence b is at
+ * position p = kv_len[b] - n + i; query head h reads KV head
+ * h / (n_q_heads / n_kv_heads). It sees row j if
+ *     j <= p  and  (window = 0  or  j > p - window  or  j < sinks)
+ * (every row of its sequence if causal = 0). With S_j = scale * q . k_j over
+ * the rows it sees: out = sum_j exp(S_j) v_j / sum_j exp(S_j) and
+ * lse = log sum_j exp(S_j); a query that sees none gets 0 and -inf. Rows past
+ * kv_len never matter, whatever they hold. A non-finite number in a cached
+ * row can reach every query of its sequence, as can a marked group.
+ * Sums and softmax statistics are fp32; q . k_j is summed in fp32 from exact
+ * products; the softmax weights are rounded to bf16 (bf16 pages) or fp16. */
+typedef struct {
+  const void* q;            /* device bf16 [total_rows][n_q_heads][head_dim] by strides */
+  void* out;                /* device bf16, likewise; may not overlap q */
+  float* lse;               /* device fp32 [total_rows][n_q_heads], or NULL */
+  int64_t q_row_stride, q_head_stride;     /* elements, multiples of 8 */
+  int64_t out_row_stride, out_head_stride; /* elements, multiples of 8 */
+  int n_q_heads;            /* a multiple of n_kv_heads */
+  float scale;              /* finite */
+  int causal;               /* 0 or 1 */
+  int window;               /* 0: none; else > 0, needs causal */
+  int sinks;                /* first rows that a window leaves visible, >= 0 */
+  void* workspace;          /* 256-byte aligned, may be NULL if none is needed */
+  int64_t workspace_bytes;  /* >= ipv_attend_workspace */
+} ipv_attend_args;
+
+/* Bytes of workspace the call needs (0 if none); reads the sizes only, not the
+ * device memory, and is the same for the same sizes on one device. Working
+ * memory only: nothing is kept in it between calls and it needs no clearing. */
+ipv_status ipv_attend_workspace(const ipv_pages* pages, const ipv_batch* batch,
+                                const ipv_attend_args* args, int64_t* bytes_out);
+
+ipv_status ipv_attend(const ipv_pages* pages, const ipv_batch* batch, const ipv_attend_args* args,
+                      void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,730 @@
+// Attention of a few query rows over a paged cache (single tokens, short
+// chunks, any head width), and the join of keys that were split over blocks.
+//
+// HBM-bound: each cached K and V row is read once per row tile, 8 or 16 query
+// rows (the query heads that share a KV head, times the new tokens) use it.
+// A block is 4 warps on one (sequence, KV head, row tile, split of the keys).
+// Each warp takes steps of 32 keys of its own: it copies them into its own
+// ring of shared-memory stages (cp.async, no block barrier anywhere in the
+// loop) and keeps its own softmax state; the warps join at the end.
+//
+// Keys are the matrix instructions' long side, S^T = K Q^T and O^T = V^T P^T
+// (mma.m16n8k16 with 16 keys or channels by 8 query rows), so 7 or 8 query
+// rows fill a tile that row-major scores would leave half empty. A thread's
+// accumulators of S^T and O^T belong to the same two query rows, so the running
+// maximum rescales in place, and S^T becomes the second product's operand by
+// one 8x8 transpose (movmatrix).
+//
+// Codes go into the fp16 matrix instruction as they are: a code u masked into a
+// 16-bit lane is the subnormal fp16 u * 2^-24 (or 16u * 2^-24), exact. The
+// K side's steps and minima are applied to the sums: q . k = sum over groups
+// of s_g (q_g . u_g) + m_g sum(q_g). Query rows are scaled by a power of two
+// into fp16's range. V is widened to u*s + m in fp16 (11 bits).
+#include <cuda_fp16.h>
+
+#include "paged.cuh"
+
+namespace ipv {
+namespace {
+
+constexpr int kThreads = 32 * kRowsWarps;
+constexpr float kNegInf = -INFINITY;
+
+template <int FMT, int DP>
+struct Ring {
+  static constexpr int kRowB = FMT == kBf16 ? DP * 2 : FMT == kU8 ? DP : DP / 2;  // bytes of a row
+  static constexpr int kTile = kRowsStep * kRowB;
+  static constexpr int kG = DP / kGroup;
+  static constexpr int kPar = FMT == kBf16 ? 0 : kRowsStep * kG * 4;
+  static constexpr int kStage = 2 * kTile + 2 * kPar;
+  static constexpr int kStages = FMT == kBf16 ? 3 : 4;
+  static constexpr int kWarp = kStage * kStages;
+  static constexpr int kBytes = kWarp * kRowsWarps;
+};
+
+// Where 16-byte chunk c of key row r lies in its row: the rows that a quarter
+// or half warp reads at once come to lie in different banks.
+template <int FMT, int RB>
+__device__ __forceinline__ int swizzle(int r, int c) {
+  if (FMT == kBf16) return c ^ (r & 7);
+  if (RB == 128) return c ^ (2 * (r & 3)) ^ (r & 4);
+  if (RB == 64) return c ^ ((((r >> 1) ^ (r >> 2)) & 1) << 1);
+  return c;
+}
+
+// Key of the 16 of a tile that stands at matrix row i. With codes, rows 2t and
+// 2t + 1 are keys t and t + 4, which keeps a half warp's V rows in different
+// banks; with bf16 ldmatrix wants no such thing.
+template <int FMT>
+__device__ __forceinline__ int key_at(int i) {
+  if (FMT == kBf16) return i;
+  return (i & 8) | ((i & 7) >> 1) | ((i & 1) << 2);
+}
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool ok) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void copy_small(uint32_t dst, const void* src, bool ok) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(N), "r"(ok ? N : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+template <bool BF16>
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if (BF16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  if (BF16)
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t at) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<__half2*>(&x); }
+__device__ __forceinline__ uint32_t as_u32(__half2 x) { return *reinterpret_cast<uint32_t*>(&x); }
+__device__ __forceinline__ float par_step(uint32_t p) { return __low2float(as_half2(p)); }
+__device__ __forceinline__ float par_min(uint32_t p) { return __high2float(as_half2(p)); }
+
+// Two 16-bit lanes of codes (masked into the low bits) plus 1024, as fp16.
+__device__ __forceinline__ uint32_t biased(uint32_t x, uint32_t mask) { return (x & mask) | 0x64006400u; }
+
+// Channel of accumulator row (tile ct, half) of the thread in lane group g of
+// the second product: with codes, the channels whose codes the thread reads.
+template <int FMT, int DP>
+__device__ __forceinline__ int out_channel(int ct, int half, int g) {
+  if (FMT == kBf16) return ct * 16 + half * 8 + g;
+  const int gr = DP == 128 ? g >> 2 : 0;
+  if (FMT == kU8) {
+    const int t = DP == 128 ? g & 3 : g >> 1, w = DP == 128 ? ct >> 1 : 2 * (g & 1) + (ct >> 1);
+    return gr * kGroup + 4 * (t + 4 * w) + 2 * (ct & 1) + half;
+  }
+  const int t = DP == 128 ? g & 3 : g >> 1, w = DP == 128 ? ct >> 2 : g & 1;
+  return gr * kGroup + 8 * (t + 4 * w) + 2 * (ct & 3) + half;
+}
+
+template <int FMT, int DP, int NR>
+__global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
+  using R = Ring<FMT, DP>;
+  constexpr bool kB = FMT == kBf16;
+  constexpr int kCh = R::kRowB / 16;     // chunks of a row
+  constexpr int kKs = DP / 16;           // k-steps of the first product
+  constexpr int kCt = DP / 16;           // channel tiles of the second
+  constexpr int kG = kB ? 1 : R::kG;     // accumulators of the first product
+  extern __shared__ __align__(128) unsigned char smem[];
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int b = blockIdx.z, head = blockIdx.y;
+  const int tile = blockIdx.x / a.splits, split = blockIdx.x - tile * a.splits;
+  const Seq seq = sequence(a.p, b);
+  const int rows = seq.n * a.share;
+  const int row0 = tile * (8 * NR);
+  if (row0 >= rows) return;
+  const int row1 = min(row0 + 8 * NR, rows) - 1;
+  const KeyRange kr = key_range(a, seq, row0 / a.share, row1 / a.share);
+  const int ns = splits_of(a, kr);
+  if (split >= ns) return;
+  const int s_begin = split * a.unit, s_end = min(kr.steps, s_begin + a.unit);
+
+  const uint32_t ring = smem_u32(smem) + warp * R::kWarp;
+  const int64_t head_off = head * a.p.head_stride;
+  const int nch = a.p.row_bytes >> 4;
+
+  // ---- copies of one step into one stage (this warp's lanes only)
+  auto issue = [&](int i, int stage) {
+    const uint32_t base = ring + stage * R::kStage;
+    const int j = kr.key0(i, kRowsStep) + lane;
+    int64_t row = -1;
+    if (j < kr.hi_max) {
+      row = pool_row(a.p, b, j);
+      if (row >= 0) row += head_off;
+    }
+    if constexpr (!kB) {
+      constexpr int kN = R::kG * 4;
+      const int64_t at = max(row, int64_t{0}) * R::kG;
+      copy_small<kN>(base + 2 * R::kTile + lane * kN, a.p.k_par + at, row >= 0);
+      copy_small<kN>(base + 2 * R::kTile + R::kPar + lane * kN, a.p.v_par + at, row >= 0);
+    }
+#pragma unroll
+    for (int u = 0; u < kCh; ++u) {
+      const int idx = u * 32 + lane, r = idx / kCh, c = idx % kCh;
+      const int64_t rr = __shfl_sync(0xffffffffu, row, r);
+      const bool ok = rr >= 0 && c < nch;
+      const int64_t at = ok ? rr * a.p.row_bytes + c * 16 : 0;
+      const uint32_t dst = base + r * R::kRowB + swizzle<FMT, R::kRowB>(r, c) * 16;
+      copy16(dst, a.p.k + at, ok);
+      copy16(dst + R::kTile, a.p.v + at, ok);
+    }
+  };
+  const int first = s_begin + warp;
+#pragma unroll
+  for (int i = 0; i < R::kStages - 1; ++i) {
+    if (first + i * kRowsWarps < s_end) issue(first + i * kRowsWarps, i);
+    copy_commit();
+  }
+
+  // ---- the query rows as the first product's second operand
+  uint32_t qb[kKs][NR][2];
+  float c_acc[NR][2], c_min[NR][2][kG];  // codes: factors of a thread's two rows
+#pragma unroll
+  for (int nr = 0; nr < NR; ++nr) {
+    const int r = row0 + nr * 8 + g;
+    const bool in = r <= row1;
+    const int tok = (in ? r : row0) / a.share, hq = (in ? r : row0) - tok * a.share;
+    const uint16_t* qp = a.q + (seq.row0 + static_cast<int64_t>(tok)) * a.q_row + (head * a.share + hq) * a.q_head;
+    if constexpr (kB) {
+#pragma unroll
+      for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int ch = ks * 16 + i * 8 + 2 * t;
+          qb[ks][nr][i] = in && ch < a.p.dim ? *reinterpret_cast<const uint32_t*>(qp + ch) : 0u;
+        }
+    } else {
+      // The row's largest magnitude goes to [2^9, 2^10): its 1/16ths and its
+      // products with subnormal codes keep all their bits. 4 threads share a row.
+      uint32_t top = 0;
+      for (int ch = 8 * t; ch < DP; ch += 32) {
+        const uint4 x = in ? *reinterpret_cast<const uint4*>(qp + ch) : make_uint4(0, 0, 0, 0);
+        const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = max(top, max(xs[i] & 0x7FFFu, (xs[i] >> 16) & 0x7FFFu));
+      }
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const int e = min(max(static_cast<int>(top >> 7) - 127, -100), 126);
+      const float up = __uint_as_float(static_cast<uint32_t>(127 + 9 - e) << 23);
+      const float down = __uint_as_float(static_cast<uint32_t>(127 - 9 + e) << 23);
+      auto load = [&](int ch, float f) {
+        const float x = in ? __uint_as_float(static_cast<uint32_t>(qp[ch]) << 16) : 0.0f;
+        return x * up * f;
+      };
+      float sum[kG];
+#pragma unroll
+      for (int gr = 0; gr < kG; ++gr) sum[gr] = 0.0f;
+#pragma unroll
+      for (int ks = 0; ks < kKs; ++ks) {
+        const int gr = ks >> 2, w = FMT == kU8 ? ks & 3 : (ks >> 1) & 1;
+        const bool hi4 = FMT == kU4 && (ks & 1);  // nibbles 1, 5, 3, 7 stand 4 bits up
+        const float f = hi4 ? 0.0625f : 1.0f;
+        const int c0 = gr * kGroup + (FMT == kU8 ? 4 : 8) * (t + 4 * w) + (hi4 ? 1 : 0);
+        const int d = FMT == kU8 ? 2 : 4, d2 = FMT == kU8 ? 1 : 2;
+        qb[ks][nr][0] = pack2<false>(load(c0, f), load(c0 + d, f));
+        qb[ks][nr][1] = pack2<false>(load(c0 + d2, f), load(c0 + d2 + d, f));
+        const __half2 s2a = as_half2(qb[ks][nr][0]), s2b = as_half2(qb[ks][nr][1]);
+        sum[gr] += (__low2float(s2a) + __high2float(s2a) + __low2float(s2b) + __high2float(s2b)) * (hi4 ? 16.0f : 1.0f);
+      }
+      const float c = a.scale_log2 * down;
+#pragma unroll
+      for (int gr = 0; gr < kG; ++gr) {
+        sum[gr] += __shfl_xor_sync(0xffffffffu, sum[gr], 1);
+        sum[gr] += __shfl_xor_sync(0xffffffffu, sum[gr], 2);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        c_acc[nr][i] = __shfl_sync(0xffffffffu, c * 16777216.0f, 4 * (2 * t + i));
+#pragma unroll
+        for (int gr = 0; gr < kG; ++gr) c_min[nr][i][gr] = __shfl_sync(0xffffffffu, c * sum[gr], 4 * (2 * t + i));
+      }
+    }
+  }
+
+  // ---- what the thread's two rows of each row tile see
+  int hi[NR][2];
+#pragma unroll
+  for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = row0 + nr * 8 + 2 * t + i;
+      hi[nr][i] = r <= row1 ? token_hi(a, seq, r / a.share) : 0;
+    }
+
+  float o[kCt][NR][4];
+  float m[NR][2], l[NR][2];
+#pragma unroll
+  for (int nr = 0; nr < NR; ++nr) {
+    m[nr][0] = m[nr][1] = kNegInf;
+    l[nr][0] = l[nr][1] = 0.0f;
+#pragma unroll
+    for (int ct = 0; ct < kCt; ++ct) o[ct][nr][0] = o[ct][nr][1] = o[ct][nr][2] = o[ct][nr][3] = 0.0f;
+  }
+
+  // ---- the loop over this warp's steps
+  int stage = 0;
+  for (int step = first; step < s_end; step += kRowsWarps) {
+    {
+      const int ahead = step + (R::kStages - 1) * kRowsWarps;
+      const int to = stage == 0 ? R::kStages - 1 : stage - 1;
+      if (ahead < s_end) issue(ahead, to);
+      copy_commit();
+    }
+    copy_wait<R::kStages - 1>();
+    __syncwarp();
+    const uint32_t ks_at = ring + stage * R::kStage, vs_at = ks_at + R::kTile;
+    const uint32_t kp_at = ks_at + 2 * R::kTile, vp_at = kp_at + R::kPar;
+    const int key0 = kr.key0(step, kRowsStep);
+
+    float sc[2][NR][4];
+    // S^T: 2 tiles of 16 keys
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+      if constexpr (kB) {
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr) sc[mt][nr][0] = sc[mt][nr][1] = sc[mt][nr][2] = sc[mt][nr][3] = 0.0f;
+        const int r = mt * 16 + (lane & 15);
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) {
+          uint32_t ka[4];
+          ldsm4(ka, ks_at + r * R::kRowB + swizzle<FMT, R::kRowB>(r, 2 * ks + (lane >> 4)) * 16);
+#pragma unroll
+          for (int nr = 0; nr < NR; ++nr) mma<true>(sc[mt][nr], ka, qb[ks][nr][0], qb[ks][nr][1]);
+        }
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[mt][nr][i] *= a.scale_log2;
+      } else {
+        float part[kG][NR][4];
+#pragma unroll
+        for (int gr = 0; gr < kG; ++gr)
+#pragma unroll
+          for (int nr = 0; nr < NR; ++nr) part[gr][nr][0] = part[gr][nr][1] = part[gr][nr][2] = part[gr][nr][3] = 0.0f;
+        const int r0 = mt * 16 + key_at<FMT>(g), r1 = r0 + 8;
+#pragma unroll
+        for (int gr = 0; gr < kG; ++gr) {
+          if constexpr (FMT == kU8) {
+            const uint4 x = lds128(ks_at + r0 * R::kRowB + swizzle<FMT, R::kRowB>(r0, gr * 4 + t) * 16);
+            const uint4 y = lds128(ks_at + r1 * R::kRowB + swizzle<FMT, R::kRowB>(r1, gr * 4 + t) * 16);
+            const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const uint32_t ka[4] = {xs[w] & 0x00FF00FFu, ys[w] & 0x00FF00FFu, (xs[w] >> 8) & 0x00FF00FFu,
+                                      (ys[w] >> 8) & 0x00FF00FFu};
+#pragma unroll
+              for (int nr = 0; nr < NR; ++nr) mma<false>(part[gr][nr], ka, qb[gr * 4 + w][nr][0], qb[gr * 4 + w][nr][1]);
+            }
+          } else {
+            const int c = gr * 2 + (t >> 1), in = (t & 1) * 8;
+            const uint2 x = lds64(ks_at + r0 * R::kRowB + swizzle<FMT, R::kRowB>(r0, c) * 16 + in);
+            const uint2 y = lds64(ks_at + r1 * R::kRowB + swizzle<FMT, R::kRowB>(r1, c) * 16 + in);
+            const uint32_t xs[2] = {x.x, x.y}, ys[2] = {y.x, y.y};
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+              const uint32_t xh = xs[w] >> 8, yh = ys[w] >> 8;
+              const uint32_t k0[4] = {xs[w] & 0x000F000Fu, ys[w] & 0x000F000Fu, xh & 0x000F000Fu, yh & 0x000F000Fu};
+              const uint32_t k1[4] = {xs[w] & 0x00F000F0u, ys[w] & 0x00F000F0u, xh & 0x00F000F0u, yh & 0x00F000F0u};
+#pragma unroll
+              for (int nr = 0; nr < NR; ++nr) {
+                mma<false>(part[gr][nr], k0, qb[gr * 4 + 2 * w][nr][0], qb[gr * 4 + 2 * w][nr][1]);
+                mma<false>(part[gr][nr], k1, qb[gr * 4 + 2 * w + 1][nr][0], qb[gr * 4 + 2 * w + 1][nr][1]);
+              }
+            }
+          }
+        }
+        uint32_t p0[kG], p1[kG];
+#pragma unroll
+        for (int gr = 0; gr < kG; ++gr) {
+          p0[gr] = lds32(kp_at + (r0 * kG + gr) * 4);
+          p1[gr] = lds32(kp_at + (r1 * kG + gr) * 4);
+        }
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float x = 0.0f, y = 0.0f;
+#pragma unroll
+            for (int gr = 0; gr < kG; ++gr) {
+              const uint32_t pp = i < 2 ? p0[gr] : p1[gr];
+              x = fmaf(par_step(pp), part[gr][nr][i], x);
+              y = fmaf(par_min(pp), c_min[nr][i & 1][gr], y);
+            }
+            sc[mt][nr][i] = fmaf(c_acc[nr][i & 1], x, y);
+          }
+      }
+    }
+    // The mask, only where some row of the tile does not see all 32 keys.
+    if (!(key0 + kRowsStep <= kr.hi_min && (key0 >= kr.lo_max || key0 + kRowsStep <= a.sinks))) {
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = key0 + mt * 16 + key_at<FMT>(g) + (i >> 1) * 8;
+#pragma unroll
+          for (int nr = 0; nr < NR; ++nr) {
+            const int h = hi[nr][i & 1];
+            const bool sees = j < h && (!a.window || j >= h - a.window || j < a.sinks);
+            if (!sees) sc[mt][nr][i] = kNegInf;
+          }
+        }
+    }
+    // Softmax: the rows' new maxima, weights, sums
+    uint32_t pb[2][NR][2], pb2[2][NR][2];
+#pragma unroll
+    for (int nr = 0; nr < NR; ++nr) {
+      float mx[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        mx[i] = fmaxf(fmaxf(sc[0][nr][i], sc[0][nr][i + 2]), fmaxf(sc[1][nr][i], sc[1][nr][i + 2]));
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], d));
+        mx[i] = fmaxf(mx[i], m[nr][i]);
+      }
+      float f[2], base[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        base[i] = mx[i] == kNegInf ? 0.0f : mx[i];
+        f[i] = exp2_fast(m[nr][i] - base[i]);
+        m[nr][i] = mx[i];
+        l[nr][i] *= f[i];
+      }
+      if (__any_sync(0xffffffffu, f[0] != 1.0f || f[1] != 1.0f)) {
+#pragma unroll
+        for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[ct][nr][i] *= f[i & 1];
+      }
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int k8 = 0; k8 < 2; ++k8) {
+          const float p0 = exp2_fast(sc[mt][nr][2 * k8] - base[0]), p1 = exp2_fast(sc[mt][nr][2 * k8 + 1] - base[1]);
+          l[nr][0] += p0;
+          l[nr][1] += p1;
+          const uint32_t pk = pack2<kB>(p0, p1);
+          pb[mt][nr][k8] = transpose8(pk);
+          if constexpr (kB)  // what bf16 leaves of the weight, as a second operand: 16 bits in all
+            pb2[mt][nr][k8] = transpose8(
+                pack2<true>(p0 - __uint_as_float(pk << 16), p1 - __uint_as_float(pk & 0xFFFF0000u)));
+        }
+    }
+    // O^T += V^T P^T
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+      if constexpr (kB) {
+        const int r = mt * 16 + (lane & 7) + ((lane >> 4) << 3);
+#pragma unroll
+        for (int ct = 0; ct < kCt; ++ct) {
+          uint32_t va[4];
+          ldsm4t(va, vs_at + r * R::kRowB + swizzle<FMT, R::kRowB>(r, 2 * ct + ((lane >> 3) & 1)) * 16);
+#pragma unroll
+          for (int nr = 0; nr < NR; ++nr) {
+            mma<true>(o[ct][nr], va, pb[mt][nr][0], pb[mt][nr][1]);
+            mma<true>(o[ct][nr], va, pb2[mt][nr][0], pb2[mt][nr][1]);
+          }
+        }
+      } else {
+        // Keys of matrix columns 2t, 2t+1, 2t+8, 2t+9
+        int kr4[4];
+        uint32_t par[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          kr4[i] = mt * 16 + key_at<FMT>(2 * t + (i & 1)) + (i >> 1) * 8;
+          par[i] = lds32(vp_at + (kr4[i] * kG + (kG == 2 ? g >> 2 : 0)) * 4);
+        }
+        __half2 st[2], mn[2];  // (step, step) and (minimum, minimum) of two keys
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          st[i] = as_half2(__byte_perm(par[2 * i], par[2 * i + 1], 0x5410));
+          mn[i] = as_half2(__byte_perm(par[2 * i], par[2 * i + 1], 0x7632));
+        }
+        constexpr int kW = R::kRowB / 32;  // words of a row a thread reads
+        uint32_t wd[4][kW];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t row = vs_at + kr4[i] * R::kRowB;
+          if constexpr (kW == 4) {
+            const uint4 x = lds128(row + swizzle<FMT, R::kRowB>(kr4[i], g) * 16);
+            wd[i][0] = x.x, wd[i][1 % kW] = x.y, wd[i][2 % kW] = x.z, wd[i][3 % kW] = x.w;
+          } else if constexpr (kW == 2) {
+            const uint2 x = lds64(row + swizzle<FMT, R::kRowB>(kr4[i], g >> 1) * 16 + (g & 1) * 8);
+            wd[i][0] = x.x, wd[i][1 % kW] = x.y;
+          } else {
+            wd[i][0] = lds32(row + swizzle<FMT, R::kRowB>(kr4[i], g >> 2) * 16 + (g & 3) * 4);
+          }
+        }
+        const __half2 k1024 = __float2half2_rn(-1024.0f), k64 = __float2half2_rn(-64.0f),
+                      k16th = __float2half2_rn(0.0625f);
+#pragma unroll
+        for (int w = 0; w < kW; ++w)
+#pragma unroll
+          for (int hl = 0; hl < 2; ++hl) {  // lower and upper 16 bits of the words
+            const uint32_t e0 = __byte_perm(wd[0][w], wd[1][w], hl ? 0x7632 : 0x5410);
+            const uint32_t e1 = __byte_perm(wd[2][w], wd[3][w], hl ? 0x7632 : 0x5410);
+            if constexpr (FMT == kU8) {
+              const int ct = w * 2 + hl;
+              uint32_t va[4];
+#pragma unroll
+              for (int half = 0; half < 2; ++half) {
+                const __half2 u0 = __hadd2(as_half2(biased(e0 >> (8 * half), 0x00FF00FFu)), k1024);
+                const __half2 u1 = __hadd2(as_half2(biased(e1 >> (8 * half), 0x00FF00FFu)), k1024);
+                va[half] = as_u32(__hfma2(u0, st[0], mn[0]));
+                va[half + 2] = as_u32(__hfma2(u1, st[1], mn[1]));
+              }
+#pragma unroll
+              for (int nr = 0; nr < NR; ++nr) mma<false>(o[ct][nr], va, pb[mt][nr][0], pb[mt][nr][1]);
+            } else {
+#pragma unroll
+              for (int q = 0; q < 2; ++q) {  // nibbles 0, 1 and 2, 3 of the 16 bits
+                const int ct = w * 4 + hl * 2 + q;
+                const uint32_t f0 = e0 >> (8 * q), f1 = e1 >> (8 * q);
+                const __half2 a0 = __hadd2(as_half2(biased(f0, 0x000F000Fu)), k1024);
+                const __half2 a1 = __hfma2(as_half2(biased(f0, 0x00F000F0u)), k16th, k64);
+                const __half2 a2 = __hadd2(as_half2(biased(f1, 0x000F000Fu)), k1024);
+                const __half2 a3 = __hfma2(as_half2(biased(f1, 0x00F000F0u)), k16th, k64);
+                const uint32_t va[4] = {as_u32(__hfma2(a0, st[0], mn[0])), as_u32(__hfma2(a1, st[0], mn[0])),
+                                        as_u32(__hfma2(a2, st[1], mn[1])), as_u32(__hfma2(a3, st[1], mn[1]))};
+#pragma unroll
+                for (int nr = 0; nr < NR; ++nr) mma<false>(o[ct][nr], va, pb[mt][nr][0], pb[mt][nr][1]);
+              }
+            }
+          }
+      }
+    }
+    __syncwarp();  // the stage is read before its next copies are issued
+    stage = stage + 1 == R::kStages ? 0 : stage + 1;
+  }
+  copy_wait<0>();
+  __syncthreads();  // the rings are free: they hold the warps' results now
+
+  // ---- join the warps
+  constexpr int kRows = 8 * NR;
+  float* so = reinterpret_cast<float*>(smem);                       // [warps][rows][DP + 4]
+  constexpr int kPitch = DP + 4;
+  float* sm = so + kRowsWarps * kRows * kPitch;                     // [warps][rows] maxima, then sums
+  float* sl = sm + kRowsWarps * kRows;
+#pragma unroll
+  for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float x = l[nr][i];
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+      const int r = nr * 8 + 2 * t + i;
+      if (g == 0) {
+        sm[warp * kRows + r] = m[nr][i];
+        sl[warp * kRows + r] = x;
+      }
+#pragma unroll
+      for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+          so[(warp * kRows + r) * kPitch + out_channel<FMT, DP>(ct, half, g)] = o[ct][nr][half * 2 + i];
+    }
+  pdl_trigger();
+  __syncthreads();
+  constexpr int kQuads = DP / 4;
+  for (int idx = threadIdx.x; idx < kRows * kQuads; idx += kThreads) {
+    const int r = idx / kQuads, c = (idx % kQuads) * 4;
+    if (row0 + r > row1) continue;
+    float top = sm[r];
+#pragma unroll
+    for (int w = 1; w < kRowsWarps; ++w) top = fmaxf(top, sm[w * kRows + r]);
+    const float base = top == kNegInf ? 0.0f : top;
+    float sum = 0.0f;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int w = 0; w < kRowsWarps; ++w) {
+      const float f = exp2_fast(sm[w * kRows + r] - base);
+      sum += f * sl[w * kRows + r];
+      const float4 x = *reinterpret_cast<const float4*>(so + (w * kRows + r) * kPitch + c);
+      acc.x += f * x.x, acc.y += f * x.y, acc.z += f * x.z, acc.w += f * x.w;
+    }
+    const int tok = (row0 + r) / a.share, hq = head * a.share + (row0 + r) - tok * a.share;
+    const int64_t row = seq.row0 + static_cast<int64_t>(tok);
+    if (a.splits > 1) {
+      const int64_t at = (row * a.q_heads + hq) * a.splits + split;
+      if (c < a.p.dim) *reinterpret_cast<float4*>(a.part_o + at * a.p.dim + c) = acc;
+      if (c == 0) a.part_ml[at] = make_float2(top, sum);
+    } else {
+      if (sum == 0.0f) acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // sees nothing
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+      if (c < a.p.dim)
+        *reinterpret_cast<uint2*>(a.out + row * a.out_row + hq * a.out_head + c) =
+            make_uint2(pack2<true>(acc.x * inv, acc.y * inv), pack2<true>(acc.z * inv, acc.w * inv));
+      if (c == 0 && a.lse) a.lse[row * a.q_heads + hq] = sum == 0.0f ? kNegInf : (top + log2f(sum)) * 0.6931471805599453f;
+    }
+  }
+}
+
+// Joins the splits of a query row and head: a warp per (row, head), 4 channels
+// per lane; the splits' (maximum, sum) come first, 32 at a time.
+__global__ void __launch_bounds__(128) attend_combine_kernel(AttendArgs a) {
+  const int lane = threadIdx.x & 31;
+  const int b = blockIdx.y;
+  const Seq seq = sequence(a.p, b);
+  const int item = blockIdx.x * 4 + (threadIdx.x >> 5);
+  const int tok = item / a.q_heads, hq = item - tok * a.q_heads;
+  if (tok >= seq.n) {
+    pdl_wait();  // no block of this kernel ends before the one it joins
+    return;
+  }
+  // The row tile that the row was computed in
+  const int h = hq / a.share, r = tok * a.share + hq - h * a.share;
+  const int row0 = r / a.tile * a.tile, row1 = min(row0 + a.tile, seq.n * a.share) - 1;
+  const int ns = splits_of(a, key_range(a, seq, row0 / a.share, row1 / a.share));
+  const int64_t row = seq.row0 + static_cast<int64_t>(tok);
+  const int64_t at = (row * a.q_heads + hq) * a.splits;
+  pdl_wait();
+  float top = kNegInf, sum = 0.0f;
+  float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  const int c = lane * 4;
+  for (int s0 = 0; s0 < ns; s0 += 32) {
+    const float2 ml = s0 + lane < ns ? a.part_ml[at + s0 + lane] : make_float2(kNegInf, 0.0f);
+    float mx = ml.x;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+    mx = fmaxf(mx, top);
+    const float base = mx == kNegInf ? 0.0f : mx;
+    const float f0 = exp2_fast(top - base), f = exp2_fast(ml.x - base);
+    top = mx;
+    float part = f * ml.y;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
+    sum = sum * f0 + part;
+    acc.x *= f0, acc.y *= f0, acc.z *= f0, acc.w *= f0;
+    const int n = min(32, ns - s0);
+#pragma unroll 4
+    for (int s = 0; s < n; ++s) {
+      const float w = __shfl_sync(0xffffffffu, f, s);
+      if (c < a.p.dim) {
+        const float4 x = *reinterpret_cast<const float4*>(a.part_o + (at + s0 + s) * a.p.dim + c);
+        acc.x += w * x.x, acc.y += w * x.y, acc.z += w * x.z, acc.w += w * x.w;
+      }
+    }
+  }
+  if (sum == 0.0f) acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // sees nothing
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  if (c < a.p.dim)
+    *reinterpret_cast<uint2*>(a.out + row * a.out_row + hq * a.out_head + c) =
+        make_uint2(pack2<true>(acc.x * inv, acc.y * inv), pack2<true>(acc.z * inv, acc.w * inv));
+  if (lane == 0 && a.lse) a.lse[row * a.q_heads + hq] = sum == 0.0f ? kNegInf : (top + log2f(sum)) * 0.6931471805599453f;
+}
+
+template <int FMT, int DP, int NR>
+struct Kernel {
+  // The ring, or the join's buffers where those are larger.
+  static constexpr int kJoin = kRowsWarps * 8 * NR * (DP + 4 + 2) * 4;
+  static constexpr int kSmem = Ring<FMT, DP>::kBytes > kJoin ? Ring<FMT, DP>::kBytes : kJoin;
+  static cudaError_t prepare() {
+    return cudaFuncSetAttribute(attend_rows_kernel<FMT, DP, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  }
+  static cudaError_t launch(const AttendArgs& a, dim3 grid, cudaStream_t st) {
+    attend_rows_kernel<FMT, DP, NR><<<grid, kThreads, kSmem, st>>>(a);
+    return cudaGetLastError();
+  }
+};
+
+template <int FMT>
+cudaError_t prepare_format() {
+  cudaError_t e = Kernel<FMT, 64, 1>::prepare();
+  if (e == cudaSuccess) e = Kernel<FMT, 64, 2>::prepare();
+  if (e == cudaSuccess) e = Kernel<FMT, 128, 1>::prepare();
+  if (e == cudaSuccess) e = Kernel<FMT, 128, 2>::prepare();
+  return e;
+}
+
+template <int FMT>
+cudaError_t launch_format(const AttendArgs& a, dim3 grid, cudaStream_t st) {
+  if (a.p.dim <= 64)
+    return a.tile == 8 ? Kernel<FMT, 64, 1>::launch(a, grid, st) : Kernel<FMT, 64, 2>::launch(a, grid, st);
+  return a.tile == 8 ? Kernel<FMT, 128, 1>::launch(a, grid, st) : Kernel<FMT, 128, 2>::launch(a, grid, st);
+}
+
+template <int FMT>
+int ctas(int dim) {
+  const int bytes = dim <= 64 ? Ring<FMT, 64>::kBytes : Ring<FMT, 128>::kBytes;
+  const int n = (227 << 10) / (bytes + 1024);
+  return n > 4 ? 4 : n;
+}
+
+}  // namespace
+
+int attend_rows_tile(int rows) { return rows <= 8 ? 8 : 16; }
+
+int attend_rows_ctas(int fmt, int dim) {
+  return fmt == kBf16 ? ctas<kBf16>(dim) : fmt == kU8 ? ctas<kU8>(dim) : ctas<kU4>(dim);
+}
+
+cudaError_t attend_rows_prepare() {
+  cudaError_t e = prepare_format<kBf16>();
+  if (e == cudaSuccess) e = prepare_format<kU8>();
+  if (e == cudaSuccess) e = prepare_format<kU4>();
+  return e;
+}
+
+cudaError_t launch_attend_rows(const AttendArgs& a, cudaStream_t st) {
+  const int tiles = static_cast<int>((static_cast<int64_t>(a.p.max_rows) * a.share + a.tile - 1) / a.tile);
+  const dim3 grid(static_cast<unsigned>(a.splits) * tiles, static_cast<unsigned>(a.p.heads),
+                  static_cast<unsigned>(a.p.n_seqs));
+  switch (a.p.fmt) {
+    case kBf16: return launch_format<kBf16>(a, grid, st);
+    case kU8: return launch_format<kU8>(a, grid, st);
+    default: return launch_format<kU4>(a, grid, st);
+  }
+}
+
+cudaError_t launch_attend_combine(const AttendArgs& a, cudaStream_t st) {
+  const int64_t items = static_cast<int64_t>(a.p.max_rows) * a.q_heads;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>((items + 3) / 4), static_cast<unsigned>(a.p.n_seqs));
+  cfg.blockDim = dim3(128);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, attend_combine_kernel, a);
+}
+
+}  // namespace ipv

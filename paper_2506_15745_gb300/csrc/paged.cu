@@ -1,0 +1,295 @@
+// C ABI of the paged cache (declared in include/ipv.h): argument checks, the
+// choice of kernel and of key splits, launches.
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+#include <mutex>
+
+#include "ipv.h"
+#include "paged.cuh"
+
+namespace ipv {
+void record_error(ipv_status s, const char* msg);
+}
+
+namespace {
+
+static_assert(static_cast<int>(ipv::kBf16) == IPV_PAGES_BF16 && static_cast<int>(ipv::kU8) == IPV_PAGES_U8 &&
+                  static_cast<int>(ipv::kU4) == IPV_PAGES_U4,
+              "page formats");
+
+ipv_status reject(ipv_status s, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  std::vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  ipv::record_error(s, buf);
+  return s;
+}
+
+ipv_status cuda_reject(cudaError_t e, const char* what) {
+  return reject(IPV_ECUDA, "%s: %s (%s)", what, cudaGetErrorName(e), cudaGetErrorString(e));
+}
+
+bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+constexpr int kMaxDevices = 64;
+struct DeviceSetup {
+  bool done = false;
+  int num_sms = 0;
+};
+DeviceSetup g_setup[kMaxDevices];
+std::mutex g_setup_mu;
+
+// Once per device, with that device current: kernel limits, SM count.
+ipv_status setup_current_device(int* num_sms) {
+  int dev = -1;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_reject(e, "cudaGetDevice");
+  if (dev < 0 || dev >= kMaxDevices) return reject(IPV_EINVAL, "device ordinal %d not supported", dev);
+  std::lock_guard<std::mutex> lock(g_setup_mu);
+  DeviceSetup& d = g_setup[dev];
+  if (!d.done) {
+    if ((e = ipv::attend_rows_prepare()) != cudaSuccess)
+      return cuda_reject(e, "no usable kernel image for this device (built for sm_103a)");
+    if ((e = cudaDeviceGetAttribute(&d.num_sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess)
+      return cuda_reject(e, "cudaDeviceGetAttribute");
+    d.done = true;
+  }
+  *num_sms = d.num_sms;
+  return IPV_OK;
+}
+
+// Checks the pool and the batch and fills the kernels' view of them.
+ipv_status check(const ipv_pages* p, const ipv_batch* b, ipv::Pages* out) {
+  if (!p || !b) return reject(IPV_EINVAL, "pages and batch must not be NULL");
+  const int fmt = p->format;
+  if (fmt != IPV_PAGES_BF16 && fmt != IPV_PAGES_U8 && fmt != IPV_PAGES_U4)
+    return reject(IPV_EINVAL, "unknown page format %d", fmt);
+  if (p->n_kv_heads < 1 || p->n_kv_heads > 65535) return reject(IPV_EINVAL, "n_kv_heads %d is not in 1..65535", p->n_kv_heads);
+  if (p->head_dim < 1 || p->head_dim > 128) return reject(IPV_EINVAL, "head_dim %d is not in 1..128", p->head_dim);
+  if (fmt == IPV_PAGES_BF16 ? p->head_dim % 8 != 0 : p->head_dim % ipv::kGroup != 0)
+    return reject(IPV_EINVAL, "head_dim %d: bf16 pages need a multiple of 8, codes 64 or 128", p->head_dim);
+  if (p->page_size < 1 || p->n_pages < 1 || p->n_pages > INT32_MAX)
+    return reject(IPV_EINVAL, "page_size %d and n_pages %lld must be positive and below 2^31", p->page_size,
+                  static_cast<long long>(p->n_pages));
+  if (p->page_stride < 0 || p->head_stride < 0 || p->row_stride < 1)
+    return reject(IPV_EINVAL, "page and head strides must not be negative, row_stride must be positive");
+  const double last = static_cast<double>(p->n_pages - 1) * static_cast<double>(p->page_stride) +
+                      static_cast<double>(p->n_kv_heads - 1) * static_cast<double>(p->head_stride) +
+                      static_cast<double>(p->page_size - 1) * static_cast<double>(p->row_stride);
+  if (last >= 9007199254740992.0) return reject(IPV_EINVAL, "row numbers exceed 2^53");
+  if (!p->k || !p->v) return reject(IPV_EINVAL, "k and v pages must not be NULL");
+  if (!aligned(p->k, 16) || !aligned(p->v, 16)) return reject(IPV_EINVAL, "pages must be 16-byte aligned");
+  if (p->k == p->v) return reject(IPV_EINVAL, "k and v pages share one buffer");
+  const int groups = (p->head_dim + ipv::kGroup - 1) / ipv::kGroup;
+  if (fmt != IPV_PAGES_BF16) {
+    if (!p->k_par || !p->v_par) return reject(IPV_EINVAL, "pages of codes need k_par and v_par");
+    if (!aligned(p->k_par, 4 * groups) || !aligned(p->v_par, 4 * groups))
+      return reject(IPV_EINVAL, "k_par and v_par must be %d-byte aligned", 4 * groups);
+    if (p->k_par == p->v_par) return reject(IPV_EINVAL, "k_par and v_par share one buffer");
+  }
+  if (b->n_seqs < 0 || b->n_seqs > 65535) return reject(IPV_EINVAL, "n_seqs %d is not in 0..65535", b->n_seqs);
+  if (b->max_pages < 1) return reject(IPV_EINVAL, "max_pages must be positive");
+  const bool pow2 = (p->page_size & (p->page_size - 1)) == 0;
+  if (b->max_pages > 1 && (!pow2 || p->page_size < 16))
+    return reject(IPV_EINVAL, "page_size %d: several pages per sequence need a power of two of at least 16", p->page_size);
+  if (!b->table && b->max_pages != 1) return reject(IPV_EINVAL, "without a table max_pages must be 1");
+  if (b->table && (!aligned(b->table, 4) || b->table_stride < b->max_pages))
+    return reject(IPV_EINVAL, "table must be 4-byte aligned with table_stride >= max_pages");
+  if (b->total_rows < 0 || b->total_rows > INT32_MAX || b->max_rows < 0 || b->max_kv < 0)
+    return reject(IPV_EINVAL, "total_rows, max_rows and max_kv must not be negative, total_rows below 2^31");
+  if (b->n_seqs > 0) {
+    if (!b->row_start || !b->kv_len) return reject(IPV_EINVAL, "row_start and kv_len must not be NULL");
+    if (!aligned(b->row_start, 4) || !aligned(b->kv_len, 4))
+      return reject(IPV_EINVAL, "row_start and kv_len must be 4-byte aligned");
+  }
+  const int64_t rows = b->max_rows < b->total_rows ? b->max_rows : b->total_rows;
+  if (rows * p->n_kv_heads * groups > INT32_MAX)
+    return reject(IPV_EINVAL, "max_rows * n_kv_heads * groups exceeds 2^31 - 1");
+  ipv::Pages& o = *out;
+  o.fmt = fmt;
+  o.heads = p->n_kv_heads;
+  o.dim = p->head_dim;
+  o.page_size = p->page_size;
+  o.page_shift = 31;
+  if (b->max_pages > 1)
+    for (o.page_shift = 4; (1 << o.page_shift) < p->page_size; ++o.page_shift) {
+    }
+  o.n_pages = static_cast<int>(p->n_pages);
+  o.max_pages = b->max_pages;
+  o.page_stride = p->page_stride;
+  o.head_stride = p->head_stride;
+  o.row_stride = p->row_stride;
+  o.row_bytes = fmt == IPV_PAGES_BF16 ? 2 * p->head_dim : fmt == IPV_PAGES_U8 ? p->head_dim : p->head_dim / 2;
+  o.groups = groups;
+  o.k = static_cast<char*>(p->k);
+  o.v = static_cast<char*>(p->v);
+  o.k_par = static_cast<uint32_t*>(p->k_par);
+  o.v_par = static_cast<uint32_t*>(p->v_par);
+  o.table = b->table;
+  o.table_stride = b->table_stride;
+  o.row_start = b->row_start;
+  o.kv_len = b->kv_len;
+  o.n_seqs = b->n_seqs;
+  o.total_rows = b->total_rows;
+  o.max_rows = static_cast<int>(rows);
+  const int64_t cap = static_cast<int64_t>(b->max_pages) * p->page_size;
+  o.max_kv = static_cast<int>(b->max_kv < cap ? b->max_kv : cap);
+  return IPV_OK;
+}
+
+ipv_status check_packed(const void* x, const char* name, int64_t row, int64_t head) {
+  if (!x) return reject(IPV_EINVAL, "%s must not be NULL", name);
+  if (!aligned(x, 16)) return reject(IPV_EINVAL, "%s must be 16-byte aligned", name);
+  if (row < 0 || head < 0 || row % 8 != 0 || head % 8 != 0)
+    return reject(IPV_EINVAL, "%s: strides must be multiples of 8 elements, not negative", name);
+  return IPV_OK;
+}
+
+ipv_status check_attend(const ipv_pages* p, const ipv_batch* b, const ipv_attend_args* t, ipv::AttendArgs* a) {
+  ipv_status s = check(p, b, &a->p);
+  if (s != IPV_OK) return s;
+  if (!t) return reject(IPV_EINVAL, "args must not be NULL");
+  if (t->n_q_heads < 1 || t->n_q_heads % p->n_kv_heads != 0)
+    return reject(IPV_EINVAL, "n_q_heads %d is not a multiple of n_kv_heads %d", t->n_q_heads, p->n_kv_heads);
+  if (!std::isfinite(t->scale)) return reject(IPV_EINVAL, "scale must be finite");
+  if (t->causal != 0 && t->causal != 1) return reject(IPV_EINVAL, "causal must be 0 or 1");
+  if (t->window < 0 || t->sinks < 0) return reject(IPV_EINVAL, "window and sinks must not be negative");
+  if (t->window > 0 && !t->causal) return reject(IPV_EINVAL, "a window needs causal = 1");
+  if (static_cast<int64_t>(a->p.max_rows) * t->n_q_heads > INT32_MAX)
+    return reject(IPV_EINVAL, "max_rows * n_q_heads exceeds 2^31 - 1");
+  a->q_heads = t->n_q_heads;
+  a->share = t->n_q_heads / p->n_kv_heads;
+  a->scale_log2 = t->scale * 1.4426950408889634f;
+  a->causal = t->causal;
+  a->window = t->window;
+  a->sinks = t->window ? t->sinks : 0;
+  return IPV_OK;
+}
+
+// The kernel's row tile and its split of the keys. Each split costs a partial
+// result, written and read again, so there are as many as fill the device.
+struct Plan {
+  int64_t part_o = 0, part_ml = 0, bytes = 0;
+};
+
+Plan make_plan(ipv::AttendArgs* a, int num_sms) {
+  Plan plan;
+  const int64_t rows = static_cast<int64_t>(a->p.max_rows) * a->share;
+  a->step = ipv::kRowsStep;
+  a->tile = ipv::attend_rows_tile(static_cast<int>(rows));
+  const int64_t tiles = (rows + a->tile - 1) / a->tile;
+  int64_t span = a->p.max_kv;
+  if (a->window) {  // the tile's tokens' windows, the sinks, and a step's slack at each of the three ends
+    const int64_t seen = static_cast<int64_t>(a->window) + a->tile + a->sinks + 3 * a->step;
+    if (seen < span) span = seen;
+  }
+  const int64_t steps = (span + a->step - 1) / a->step;
+  const int64_t blocks = tiles * a->p.heads * a->p.n_seqs;
+  const int64_t slots = static_cast<int64_t>(num_sms) * ipv::attend_rows_ctas(a->p.fmt, a->p.dim) * (a->p.n_seqs > 1 ? 2 : 1);
+  int64_t want = blocks > 0 ? slots / blocks : 1;
+  if (want < 1) want = 1;
+  int64_t unit = (steps + want - 1) / want;
+  unit = (unit + ipv::kRowsWarps - 1) / ipv::kRowsWarps * ipv::kRowsWarps;
+  if (unit < ipv::kRowsWarps) unit = ipv::kRowsWarps;
+  a->unit = static_cast<int>(unit);
+  a->splits = static_cast<int>(steps > 0 ? (steps + unit - 1) / unit : 1);
+  if (a->splits > 1) {
+    const int64_t n = a->p.total_rows * a->q_heads * a->splits;
+    plan.part_o = 0;
+    plan.part_ml = (n * a->p.dim * 4 + 255) & ~int64_t{255};
+    plan.bytes = plan.part_ml + ((n * 8 + 255) & ~int64_t{255});
+  }
+  return plan;
+}
+
+}  // namespace
+
+extern "C" ipv_status ipv_pages_write(const ipv_pages* pages, const ipv_batch* batch, const void* k_new,
+                                      const void* v_new, int64_t row_stride, int64_t head_stride, void* stream) {
+  ipv::RowsArgs a{};
+  ipv_status s = check(pages, batch, &a.p);
+  if (s != IPV_OK) return s;
+  if (a.p.n_seqs == 0 || a.p.max_rows == 0) return IPV_OK;
+  s = check_packed(k_new, "k_new", row_stride, head_stride);
+  if (s == IPV_OK) s = check_packed(v_new, "v_new", row_stride, head_stride);
+  if (s != IPV_OK) return s;
+  a.k_new = static_cast<const uint16_t*>(k_new);
+  a.v_new = static_cast<const uint16_t*>(v_new);
+  a.row = row_stride;
+  a.head = head_stride;
+  const cudaError_t e = ipv::launch_pages_write(a, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? IPV_OK : cuda_reject(e, "page write kernel");
+}
+
+extern "C" ipv_status ipv_pages_read(const ipv_pages* pages, const ipv_batch* batch, void* k_out, void* v_out,
+                                     int64_t row_stride, int64_t head_stride, void* stream) {
+  ipv::RowsArgs a{};
+  ipv_status s = check(pages, batch, &a.p);
+  if (s != IPV_OK) return s;
+  if (a.p.n_seqs == 0 || a.p.max_rows == 0) return IPV_OK;
+  s = check_packed(k_out, "k_out", row_stride, head_stride);
+  if (s == IPV_OK) s = check_packed(v_out, "v_out", row_stride, head_stride);
+  if (s != IPV_OK) return s;
+  if (k_out == v_out) return reject(IPV_EINVAL, "k_out and v_out share one buffer");
+  a.k_out = static_cast<uint16_t*>(k_out);
+  a.v_out = static_cast<uint16_t*>(v_out);
+  a.row = row_stride;
+  a.head = head_stride;
+  const cudaError_t e = ipv::launch_pages_read(a, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? IPV_OK : cuda_reject(e, "page read kernel");
+}
+
+extern "C" ipv_status ipv_attend_workspace(const ipv_pages* pages, const ipv_batch* batch,
+                                           const ipv_attend_args* args, int64_t* bytes_out) {
+  if (!bytes_out) return reject(IPV_EINVAL, "bytes_out must not be NULL");
+  *bytes_out = 0;
+  ipv::AttendArgs a{};
+  ipv_status s = check_attend(pages, batch, args, &a);
+  if (s != IPV_OK) return s;
+  if (a.p.n_seqs == 0 || a.p.max_rows == 0) return IPV_OK;
+  int num_sms = 0;
+  if ((s = setup_current_device(&num_sms)) != IPV_OK) return s;
+  *bytes_out = make_plan(&a, num_sms).bytes;
+  return IPV_OK;
+}
+
+extern "C" ipv_status ipv_attend(const ipv_pages* pages, const ipv_batch* batch, const ipv_attend_args* args,
+                                 void* stream) {
+  ipv::AttendArgs a{};
+  ipv_status s = check_attend(pages, batch, args, &a);
+  if (s != IPV_OK) return s;
+  if (a.p.n_seqs == 0 || a.p.max_rows == 0) return IPV_OK;
+  s = check_packed(args->q, "q", args->q_row_stride, args->q_head_stride);
+  if (s == IPV_OK) s = check_packed(args->out, "out", args->out_row_stride, args->out_head_stride);
+  if (s != IPV_OK) return s;
+  if (args->q == args->out) return reject(IPV_EINVAL, "q and out share one buffer");
+  if (args->lse && !aligned(args->lse, 4)) return reject(IPV_EINVAL, "lse must be 4-byte aligned");
+  int num_sms = 0;
+  if ((s = setup_current_device(&num_sms)) != IPV_OK) return s;
+  const Plan plan = make_plan(&a, num_sms);
+  if (plan.bytes > 0) {
+    if (!args->workspace || args->workspace_bytes < plan.bytes)
+      return reject(IPV_EINVAL, "the workspace has %lld bytes, the call needs %lld",
+                    static_cast<long long>(args->workspace ? args->workspace_bytes : 0),
+                    static_cast<long long>(plan.bytes));
+    if (!aligned(args->workspace, 256)) return reject(IPV_EINVAL, "the workspace must be 256-byte aligned");
+  }
+  a.q = static_cast<const uint16_t*>(args->q);
+  a.out = static_cast<uint16_t*>(args->out);
+  a.lse = args->lse;
+  a.q_row = args->q_row_stride;
+  a.q_head = args->q_head_stride;
+  a.out_row = args->out_row_stride;
+  a.out_head = args->out_head_stride;
+  char* ws = static_cast<char*>(args->workspace);
+  a.part_o = reinterpret_cast<float*>(ws + plan.part_o);
+  a.part_ml = reinterpret_cast<float2*>(ws + plan.part_ml);
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e = ipv::launch_attend_rows(a, st);
+  if (e != cudaSuccess) return cuda_reject(e, "attention kernel");
+  if (a.splits > 1 && (e = ipv::launch_attend_combine(a, st)) != cudaSuccess) return cuda_reject(e, "split join kernel");
+  return IPV_OK;
+}

@@ -1,0 +1,135 @@
+// Internal declarations of the paged cache (paged.cu: C ABI; paged_rows.cu:
+// write and read-back; attend_rows.cu: attention of a few query rows).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "ipv_common.cuh"
+
+namespace ipv {
+
+enum : int { kBf16 = 0, kU8 = 1, kU4 = 2 };  // ipv_pages_format
+
+constexpr int kGroup = 64;            // channels that share a step and a minimum
+constexpr float kLargest = 32768.0f;  // a group with a larger magnitude is marked
+
+// A pool and the sequences in it, as the kernels take them.
+struct Pages {
+  int fmt;
+  int heads, dim;
+  int page_size;
+  int page_shift;      // log2(page_size); 31 with one page per sequence
+  int n_pages, max_pages;
+  int64_t page_stride, head_stride, row_stride;  // rows
+  int row_bytes;       // of codes or elements
+  int groups;          // (dim + 63) / 64
+  char* k;
+  char* v;
+  uint32_t* k_par;     // pairs of fp16 (step, minimum)
+  uint32_t* v_par;
+  const int32_t* table;
+  int64_t table_stride;
+  const int32_t* row_start;
+  const int32_t* kv_len;
+  int n_seqs;
+  int64_t total_rows;
+  int max_rows, max_kv;  // max_kv already cut to max_pages * page_size
+};
+
+// New rows and length of a sequence, made to fit.
+struct Seq {
+  int row0, n, len;
+};
+
+__device__ __forceinline__ Seq sequence(const Pages& p, int b) {
+  Seq s;
+  const int r0 = p.row_start[b], r1 = p.row_start[b + 1];
+  const int len = p.kv_len[b];
+  s.row0 = r0;
+  s.len = min(max(len, 0), p.max_kv);
+  s.n = (r0 < 0 || r1 < r0 || r1 > p.total_rows) ? 0 : min(r1 - r0, p.max_rows);
+  return s;
+}
+
+// Row number in the pool of row j >= 0 of sequence b (head's offset not
+// included), or -1 if its page is not one of the pool's.
+__device__ __forceinline__ int64_t pool_row(const Pages& p, int b, int j) {
+  const int i = j >> p.page_shift;
+  const int g = p.table ? p.table[b * p.table_stride + i] : b;
+  if (static_cast<unsigned>(g) >= static_cast<unsigned>(p.n_pages)) return -1;
+  return g * p.page_stride + (p.page_shift == 31 ? j : j & (p.page_size - 1)) * p.row_stride;
+}
+
+// ------------------------------------------------------------------ attention
+struct AttendArgs {
+  Pages p;
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;
+  int64_t q_row, q_head, out_row, out_head;  // strides in elements
+  int q_heads, share;   // query heads; query heads per KV head
+  float scale_log2;     // scale * log2(e)
+  int causal, window, sinks;
+  // Keys are split: a split is at most `unit` steps of `step` keys.
+  int step, unit, splits;  // splits: most that any row tile has
+  int tile;                // query rows of a row tile
+  float* part_o;    // [total_rows * q_heads][splits][dim] unnormalised sums
+  float2* part_ml;  // [total_rows * q_heads][splits] (running maximum, sum)
+};
+
+// The steps of keys that query rows of tokens tok0..tok1 can see: steps
+// 0..sink_steps-1 of the sequence, then those from first on, `steps` in all.
+struct KeyRange {
+  int sink_steps, first, steps;
+  int hi_min, hi_max;  // keys j < hi of the first and of the last token
+  int lo_max;          // the last token's window starts here
+  __device__ __forceinline__ int key0(int i, int step) const {
+    return (i < sink_steps ? i : i - sink_steps + first) * step;
+  }
+};
+
+__device__ __forceinline__ int token_hi(const AttendArgs& a, const Seq& s, int tok) {
+  return a.causal ? max(0, s.len - s.n + tok + 1) : s.len;
+}
+
+__device__ __forceinline__ KeyRange key_range(const AttendArgs& a, const Seq& s, int tok0, int tok1) {
+  KeyRange r;
+  r.hi_min = token_hi(a, s, tok0);
+  r.hi_max = token_hi(a, s, tok1);
+  const int lo = a.window ? max(0, r.hi_min - a.window) : 0;
+  r.lo_max = a.window ? max(0, r.hi_max - a.window) : 0;
+  r.first = lo / a.step;
+  // (x - 1) / step + 1 rather than (x + step - 1) / step: x may be near 2^31
+  r.sink_steps = a.sinks > 0 ? min(r.first, (a.sinks - 1) / a.step + 1) : 0;
+  const int end = r.hi_max > 0 ? (r.hi_max - 1) / a.step + 1 : 0;
+  r.steps = r.sink_steps + max(0, end - r.first);
+  return r;
+}
+
+__device__ __forceinline__ int splits_of(const AttendArgs& a, const KeyRange& r) {
+  return r.steps > 0 ? (r.steps - 1) / a.unit + 1 : 1;
+}
+
+// ------------------------------------------------------------------ launches
+struct RowsArgs {
+  Pages p;
+  const uint16_t* k_new;
+  const uint16_t* v_new;
+  uint16_t* k_out;
+  uint16_t* v_out;
+  int64_t row, head;  // strides of the packed rows, elements
+  int num_sms;
+};
+cudaError_t launch_pages_write(const RowsArgs& a, cudaStream_t st);
+cudaError_t launch_pages_read(const RowsArgs& a, cudaStream_t st);
+
+int attend_rows_tile(int rows);               // query rows of a row tile
+int attend_rows_ctas(int fmt, int dim);       // resident blocks per SM (smem)
+constexpr int kRowsStep = 32;                 // keys of a step
+constexpr int kRowsWarps = 4;
+cudaError_t attend_rows_prepare();            // once per device
+cudaError_t launch_attend_rows(const AttendArgs& a, cudaStream_t st);
+cudaError_t launch_attend_combine(const AttendArgs& a, cudaStream_t st);
+
+}  // namespace ipv

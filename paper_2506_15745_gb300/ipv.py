@@ -15,6 +15,7 @@ LIB_PATH = os.path.join(_HERE, "libipv.so")
 
 IPV_OK, IPV_EINVAL, IPV_ENOINIT, IPV_ENOMEM, IPV_ECUDA, IPV_ETIMEOUT = range(6)
 IPV_BF16, IPV_F32 = 0, 1
+IPV_PAGES_BF16, IPV_PAGES_U8, IPV_PAGES_U4 = range(3)
 ABLATIONS = {"none": 0, "tar_reverse": 1, "van_reverse": 2, "tar_frame": 3, "uniform": 4}
 NUM_KERNELS = 7
 KERNEL_NAMES = ("recent_mean", "score", "select", "gather", "fused", "pool", "combine")
@@ -52,6 +53,31 @@ class KV(ctypes.Structure):
             kv.frame_id[h] = _ptr(frame_ids[h])
         kv.cur = cur
         return kv
+
+
+class PagesDesc(ctypes.Structure):
+    """ipv_pages: a pool of pages."""
+    _fields_ = [("format", ctypes.c_int), ("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("n_pages", ctypes.c_int64), ("page_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("k_par", ctypes.c_void_p), ("v_par", ctypes.c_void_p)]
+
+
+class Batch(ctypes.Structure):
+    """ipv_batch: sequences in a pool and their new rows."""
+    _fields_ = [("n_seqs", ctypes.c_int), ("max_pages", ctypes.c_int), ("table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("row_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("total_rows", ctypes.c_int64), ("max_rows", ctypes.c_int), ("max_kv", ctypes.c_int)]
+
+
+class AttendArgs(ctypes.Structure):
+    """ipv_attend_args."""
+    _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+                ("q_row_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+                ("out_row_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+                ("n_q_heads", ctypes.c_int), ("scale", ctypes.c_float), ("causal", ctypes.c_int),
+                ("window", ctypes.c_int), ("sinks", ctypes.c_int), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_int64)]
 
 
 _lib = None
@@ -98,10 +124,15 @@ def load():
         lib.ipv_set_wait_limit.argtypes = [I64]
         lib.ipv_append_frames.argtypes = [KVP, KVP, P, P, I32, I32, I32, I64, I32, I32, I32,
                                           ctypes.c_uint32, P]
+        lib.ipv_pages_write.argtypes = [P, P, P, P, I64, I64, P]
+        lib.ipv_pages_read.argtypes = [P, P, P, P, I64, I64, P]
+        lib.ipv_attend_workspace.argtypes = [P, P, P, P]
+        lib.ipv_attend.argtypes = [P, P, P, P]
         for name in ("ipv_init", "ipv_compress", "ipv_score", "ipv_select",
                      "ipv_profile_enable", "ipv_profile_collect", "ipv_device_error",
                      "ipv_compress_static", "ipv_van_pool", "ipv_append_frames",
-                     "ipv_set_wait_limit"):
+                     "ipv_set_wait_limit", "ipv_pages_write", "ipv_pages_read",
+                     "ipv_attend_workspace", "ipv_attend"):
             getattr(lib, name).restype = I32
         _lib = lib
     return _lib
@@ -225,3 +256,23 @@ def profile_collect(timeout_ms: int = 60000):
     n = (ctypes.c_int64 * NUM_KERNELS)()
     _check(load().ipv_profile_collect(ms, n, timeout_ms))
     return {KERNEL_NAMES[i]: (ms[i], n[i]) for i in range(NUM_KERNELS)}
+
+
+def pages_write(pages, batch, k_new, v_new, row_stride: int, head_stride: int, stream=None) -> None:
+    """ipv_pages_write; pages and batch are references to PagesDesc and Batch (see paged.PagedCache)."""
+    _check(load().ipv_pages_write(pages, batch, _ptr(k_new), _ptr(v_new), row_stride, head_stride, _stream(stream)))
+
+
+def pages_read(pages, batch, k_out, v_out, row_stride: int, head_stride: int, stream=None) -> None:
+    _check(load().ipv_pages_read(pages, batch, _ptr(k_out), _ptr(v_out), row_stride, head_stride, _stream(stream)))
+
+
+def attend_workspace(pages, batch, args: AttendArgs) -> int:
+    """Bytes of workspace that ipv_attend needs for these sizes."""
+    out = ctypes.c_int64(0)
+    _check(load().ipv_attend_workspace(pages, batch, ctypes.byref(args), ctypes.byref(out)))
+    return out.value
+
+
+def attend(pages, batch, args: AttendArgs, stream=None) -> None:
+    _check(load().ipv_attend(pages, batch, ctypes.byref(args), _stream(stream)))

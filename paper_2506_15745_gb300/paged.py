@@ -1,0 +1,188 @@
+"""A paged key/value cache and attention over it, on PyTorch tensors.
+
+A PagedCache holds rows in pages of bf16, or of 8-bit or 4-bit codes with a
+step and a minimum for each 64 channels; a PagedBatch says which pages a set of
+sequences uses and which of their rows are new. `write` puts new rows into
+pages, `read` reads them back, `attend` attends with new rows' queries over
+all the rows that their sequences hold. Everything runs in libipv.so's kernels
+(include/ipv.h, ipv_pages_write and on); this module allocates with PyTorch
+and passes pointers. A half of a PingPongCache is a paged cache as it stands:
+`PagedCache.of_layer`.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import ipv
+
+GROUP = 64  # channels that share a step and a minimum
+FORMATS = {"bf16": ipv.IPV_PAGES_BF16, "u8": ipv.IPV_PAGES_U8, "u4": ipv.IPV_PAGES_U4}
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+class PagedBatch:
+    """Sequences and their new rows (ipv_batch).
+
+    table: int32 [n_seqs, max_pages] page numbers, or None (one page per
+    sequence, page b for sequence b). row_start: int32 [n_seqs + 1], the new
+    rows' places in packed tensors. kv_len: int32 [n_seqs], rows held, new ones
+    included. The three are read on the GPU when a call runs and may be
+    updated in place between calls; total_rows, max_rows and max_kv bound
+    them on the host (the packed rows, one sequence's new rows, one sequence's
+    rows)."""
+
+    def __init__(self, table, row_start: torch.Tensor, kv_len: torch.Tensor, *, total_rows: int,
+                 max_rows: int, max_kv: int):
+        for name, t in (("table", table), ("row_start", row_start), ("kv_len", kv_len)):
+            if t is not None:
+                _need(t.dtype == torch.int32 and t.is_cuda, f"{name} must be an int32 CUDA tensor")
+                _need(t.numel() == 0 or t.stride(-1) == 1, f"{name} must be contiguous along its last dimension")
+        _need(kv_len.dim() == 1 and row_start.shape == (kv_len.shape[0] + 1,),
+              "kv_len is [n_seqs], row_start [n_seqs + 1]")
+        n = kv_len.shape[0]
+        _need(table is None or (table.dim() == 2 and table.shape[0] == n and table.shape[1] >= 1),
+              "table is [n_seqs, max_pages]")
+        self.table, self.row_start, self.kv_len = table, row_start, kv_len
+        self.n_seqs, self.total_rows, self.max_rows, self.max_kv = n, total_rows, max_rows, max_kv
+        self.struct = ipv.Batch(n, 1 if table is None else table.shape[1], ipv._ptr(table),
+                                1 if table is None else max(table.stride(0), table.shape[1]), ipv._ptr(row_start),
+                                ipv._ptr(kv_len), total_rows, max_rows, max_kv)
+        self.ref = ctypes.byref(self.struct)
+
+
+class PagedCache:
+    """A pool of pages (ipv_pages): k, v [n_pages, n_kv_heads, page_size,
+    head_dim] bf16, or codes uint8 [..., head_dim (u8) or head_dim / 2 (u4)]
+    with k_par, v_par fp16 [n_pages, n_kv_heads, page_size, head_dim / 64, 2]
+    (step, minimum)."""
+
+    def __init__(self, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, fmt: str = "bf16",
+                 device="cuda"):
+        _need(fmt in FORMATS, f"fmt is one of {sorted(FORMATS)}")
+        shape = (n_pages, n_kv_heads, page_size)
+        if fmt == "bf16":
+            k = torch.zeros(shape + (head_dim,), dtype=torch.bfloat16, device=device)
+            self._set(fmt, k, torch.zeros_like(k), None, None)
+        else:
+            _need(head_dim % GROUP == 0, "codes need head_dim 64 or 128")
+            k = torch.zeros(shape + (head_dim // (1 if fmt == "u8" else 2),), dtype=torch.uint8, device=device)
+            par = torch.zeros(shape + (head_dim // GROUP, 2), dtype=torch.float16, device=device)
+            self._set(fmt, k, torch.zeros_like(k), par, torch.zeros_like(par))
+
+    @classmethod
+    def from_tensors(cls, fmt: str, k, v, k_par=None, v_par=None) -> "PagedCache":
+        """A pool over tensors that the caller keeps. They may be views (a
+        permuted [n_pages, page_size, n_kv_heads, ...] pool, a slice of one) as long
+        as a row is contiguous and all strides are whole rows, the same ones in
+        every tensor."""
+        self = cls.__new__(cls)
+        _need(fmt in FORMATS, f"fmt is one of {sorted(FORMATS)}")
+        self._set(fmt, k, v, k_par, v_par)
+        return self
+
+    @classmethod
+    def of_layer(cls, cache, layer: int, n_layers: int, n_kv_heads: int, n_streams: int = 1) -> "PagedCache":
+        """One layer of a PingPongCache's live half (bf16), without a copy: page b
+        is the layer's rows of stream b (PagedBatch with table=None). Valid
+        until the next compression pass flips the cache or writes this half."""
+        _need(cache.dtype == "bf16", "attention takes bf16 caches")
+        _need(cache.n_slabs == n_streams * n_layers * n_kv_heads and 0 <= layer < n_layers,
+              "the cache's slabs are streams x layers x KV heads")
+        k, v = (t.view(n_streams, n_layers, n_kv_heads, cache.capacity, cache.head_dim)[:, layer]
+                for t in (cache.k_live, cache.v_live))
+        return cls.from_tensors("bf16", k, v)
+
+    def _set(self, fmt, k, v, k_par, v_par):
+        codes = fmt != "bf16"
+        want = torch.uint8 if codes else torch.bfloat16
+        for name, t in (("k", k), ("v", v)):
+            _need(t.dim() == 4 and t.dtype == want and t.is_cuda, f"{name} must be a 4-d {want} CUDA tensor")
+        _need(k.shape == v.shape, "k and v must have one shape")
+        width = k.shape[3]
+        self.fmt, self.k, self.v, self.k_par, self.v_par = fmt, k, v, k_par, v_par
+        self.n_pages, self.n_kv_heads, self.page_size = k.shape[0], k.shape[1], k.shape[2]
+        self.head_dim = width * (2 if fmt == "u4" else 1)
+        rows = self._row_strides(k, width)
+        _need(self._row_strides(v, width) == rows, "k and v must have the same strides")
+        if codes:
+            groups = self.head_dim // GROUP
+            for name, t in (("k_par", k_par), ("v_par", v_par)):
+                _need(t is not None and t.dtype == torch.float16 and t.is_cuda and
+                      t.shape == k.shape[:3] + (groups, 2), f"{name} must be fp16 {tuple(k.shape[:3]) + (groups, 2)}")
+                _need(t.stride(4) == 1 and t.stride(3) == 2, f"{name}: a row's pairs must be contiguous")
+                _need(self._row_strides(t, 2 * groups) == rows, f"{name} must have k's strides, in rows")
+        self.struct = ipv.PagesDesc(FORMATS[fmt], self.n_kv_heads, self.head_dim, self.page_size, self.n_pages, *rows,
+                                    k.data_ptr(), v.data_ptr(), ipv._ptr(k_par), ipv._ptr(v_par))
+        self.ref = ctypes.byref(self.struct)
+        self._workspace = None
+
+    @staticmethod
+    def _row_strides(t, width):
+        _need(t.dim() == 5 or t.stride(3) == 1, "a row must be contiguous")
+        out = []
+        for i in range(3):
+            s = t.stride(i) if t.shape[i] > 1 else width * (1 if i == 2 else t.shape[2])
+            _need(s % width == 0, "strides must be whole rows")
+            out.append(s // width)
+        return tuple(out)
+
+    @staticmethod
+    def _packed(name, t, batch, heads, dim):
+        _need(t.dtype == torch.bfloat16 and t.is_cuda and t.dim() == 3 and t.stride(2) == 1,
+              f"{name} must be a bf16 CUDA tensor [rows, heads, head_dim] with contiguous rows")
+        _need(t.shape[0] >= batch.total_rows and t.shape[1] == heads and t.shape[2] == dim,
+              f"{name} must be [{batch.total_rows}, {heads}, {dim}]")
+
+    def write(self, k_new, v_new, batch: PagedBatch, stream=None) -> None:
+        """ipv_pages_write: k_new, v_new bf16 [total_rows, n_kv_heads, head_dim] into the batch's pages."""
+        for name, t in (("k_new", k_new), ("v_new", v_new)):
+            self._packed(name, t, batch, self.n_kv_heads, self.head_dim)
+        _need(k_new.stride() == v_new.stride(), "k_new and v_new must have the same strides")
+        ipv.pages_write(self.ref, batch.ref, k_new, v_new, k_new.stride(0), k_new.stride(1), stream)
+
+    def read(self, batch: PagedBatch, k_out=None, v_out=None, stream=None):
+        """ipv_pages_read: the batch's new rows, bf16 [total_rows, n_kv_heads, head_dim] each. Packed rows that
+        belong to no sequence are left as they are (new tensors: zero)."""
+        if k_out is None or v_out is None:
+            shape = (batch.total_rows, self.n_kv_heads, self.head_dim)
+            k_out = torch.zeros(shape, dtype=torch.bfloat16, device=self.k.device) if k_out is None else k_out
+            v_out = torch.zeros(shape, dtype=torch.bfloat16, device=self.k.device) if v_out is None else v_out
+        for name, t in (("k_out", k_out), ("v_out", v_out)):
+            self._packed(name, t, batch, self.n_kv_heads, self.head_dim)
+        _need(k_out.stride() == v_out.stride(), "k_out and v_out must have the same strides")
+        ipv.pages_read(self.ref, batch.ref, k_out, v_out, k_out.stride(0), k_out.stride(1), stream)
+        return k_out, v_out
+
+    def attend(self, q, batch: PagedBatch, *, out=None, lse=None, scale: float | None = None, causal: bool = True,
+               window: int = 0, sinks: int = 0, workspace=None, stream=None):
+        """ipv_attend: attention of q, bf16 [total_rows, n_q_heads, head_dim], over the rows that the batch's
+        sequences hold. out: bf16 like q (allocated if None); lse: fp32
+        [total_rows, n_q_heads], filled if given. workspace: a uint8 tensor;
+        without one the cache allocates and keeps one of its own, for calls on one stream at a time."""
+        n_q_heads = q.shape[1]
+        self._packed("q", q, batch, n_q_heads, self.head_dim)
+        if out is None:
+            out = torch.zeros_like(q, memory_format=torch.contiguous_format)
+        self._packed("out", out, batch, n_q_heads, self.head_dim)
+        if lse is not None:
+            _need(lse.dtype == torch.float32 and lse.is_cuda and lse.is_contiguous() and lse.dim() == 2 and
+                  lse.shape[0] >= batch.total_rows and lse.shape[1] == n_q_heads,
+                  "lse must be a contiguous fp32 CUDA tensor [total_rows, n_q_heads]")
+        args = ipv.AttendArgs(q.data_ptr(), out.data_ptr(), ipv._ptr(lse), q.stride(0), q.stride(1), out.stride(0),
+                              out.stride(1), n_q_heads, self.head_dim ** -0.5 if scale is None else scale,
+                              int(causal), window, sinks, None, 0)
+        need = ipv.attend_workspace(self.ref, batch.ref, args)
+        if need:
+            if workspace is None:
+                if self._workspace is None or self._workspace.numel() < need:
+                    self._workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+                workspace = self._workspace
+            args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel()
+        ipv.attend(self.ref, batch.ref, args, stream)
+        return out
