@@ -459,6 +459,18 @@ ipv_status ipv_attend_workspace(const ipv_pages* pages, const ipv_batch* batch,
 ipv_status ipv_attend(const ipv_pages* pages, const ipv_batch* batch, const ipv_attend_args* args,
                       void* stream);
 
+/* Diagnostic: the kernel for many query rows bounds every wait between its
+ * warps by time. When one runs out it sets a bit in a device error word (1: the
+ * copies, 2: the products, 4: the softmax gave up), the block ends without
+ * writing its results, and the device stays usable. Waits for the whole device,
+ * copies the word of the current device to *err_out (0: no wait has run out
+ * since the last read) and clears it. Errors: IPV_EINVAL, IPV_ECUDA. */
+ipv_status ipv_attend_error(uint32_t* err_out);
+
+/* Diagnostic: the longest such wait in nanoseconds (0 restores the default,
+ * 4 s; 1: every wait gives up at once). Takes effect at the next ipv_attend. Errors: IPV_EINVAL (negative). */
+ipv_status ipv_attend_wait_limit(int64_t nanoseconds);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,5 +1,6 @@
 // C ABI of the paged cache (declared in include/ipv.h): argument checks, the
 // choice of kernel and of key splits, launches.
+#include <atomic>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -53,6 +54,7 @@ ipv_status setup_current_device(int* num_sms) {
   if (!d.done) {
     if ((e = ipv::attend_rows_prepare()) != cudaSuccess)
       return cuda_reject(e, "no usable kernel image for this device (built for sm_103a)");
+    if ((e = ipv::attend_tiles_prepare()) != cudaSuccess) return cuda_reject(e, "tiled attention set-up");
     if ((e = cudaDeviceGetAttribute(&d.num_sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess)
       return cuda_reject(e, "cudaDeviceGetAttribute");
     d.done = true;
@@ -169,40 +171,88 @@ ipv_status check_attend(const ipv_pages* p, const ipv_batch* b, const ipv_attend
   return IPV_OK;
 }
 
-// The kernel's row tile and its split of the keys. Each split costs a partial
-// result, written and read again, so there are as many as fill the device.
+// Longest that a wait inside the tiled kernel may take (ipv_attend_wait_limit).
+constexpr int64_t kDefaultLimitNs = 4000000000;
+std::atomic<int64_t> g_limit_ns{kDefaultLimitNs};
+
+// Query rows from which the tiled kernel is the faster one: below, the rows
+// kernel reads K and V once per 16 query rows.
+constexpr int64_t kTilesFrom = 17;
+
+// Which kernel takes the call, its split of the keys, and the workspace. Each
+// split costs a partial result, written and read again, so there are as many
+// as fill the device.
 struct Plan {
-  int64_t part_o = 0, part_ml = 0, bytes = 0;
+  bool tiles = false;
+  ipv::TileMaps maps;  // tiles: made only when launching
+  int64_t k16 = 0, v16 = 0, part_o = 0, part_ml = 0, bytes = 0;  // offsets in the workspace
 };
 
-Plan make_plan(ipv::AttendArgs* a, int num_sms) {
-  Plan plan;
-  const int64_t rows = static_cast<int64_t>(a->p.max_rows) * a->share;
-  a->step = ipv::kRowsStep;
-  a->tile = ipv::attend_rows_tile(static_cast<int>(rows));
+int64_t round256(int64_t x) { return (x + 255) & ~int64_t{255}; }
+
+// a: checked arguments; the plan's tile, step, unit and splits go into it.
+void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
+  const ipv::Pages& p = a->p;
+  const int64_t rows = static_cast<int64_t>(p.max_rows) * a->share;
+  plan->tiles = rows >= kTilesFrom;
+  int64_t slots, least;
+  if (plan->tiles) {
+    a->step = ipv::kTilesStep;
+    a->tile = ipv::kTilesRows;
+    slots = num_sms;
+    least = 2;
+  } else {
+    a->step = ipv::kRowsStep;
+    a->tile = ipv::attend_rows_tile(static_cast<int>(rows));
+    slots = static_cast<int64_t>(num_sms) * ipv::attend_rows_ctas(p.fmt, p.dim) * (p.n_seqs > 1 ? 2 : 1);
+    least = ipv::kRowsWarps;
+  }
   const int64_t tiles = (rows + a->tile - 1) / a->tile;
-  int64_t span = a->p.max_kv;
+  int64_t span = p.max_kv;
   if (a->window) {  // the tile's tokens' windows, the sinks, and a step's slack at each of the three ends
     const int64_t seen = static_cast<int64_t>(a->window) + a->tile + a->sinks + 3 * a->step;
     if (seen < span) span = seen;
   }
   const int64_t steps = (span + a->step - 1) / a->step;
-  const int64_t blocks = tiles * a->p.heads * a->p.n_seqs;
-  const int64_t slots = static_cast<int64_t>(num_sms) * ipv::attend_rows_ctas(a->p.fmt, a->p.dim) * (a->p.n_seqs > 1 ? 2 : 1);
-  int64_t want = blocks > 0 ? slots / blocks : 1;
+  const int64_t blocks = tiles * p.heads * p.n_seqs;
+  int64_t want = slots / blocks;
   if (want < 1) want = 1;
   int64_t unit = (steps + want - 1) / want;
-  unit = (unit + ipv::kRowsWarps - 1) / ipv::kRowsWarps * ipv::kRowsWarps;
-  if (unit < ipv::kRowsWarps) unit = ipv::kRowsWarps;
+  if (!plan->tiles) unit = (unit + ipv::kRowsWarps - 1) / ipv::kRowsWarps * ipv::kRowsWarps;
+  if (unit < least) unit = least;
   a->unit = static_cast<int>(unit);
   a->splits = static_cast<int>(steps > 0 ? (steps + unit - 1) / unit : 1);
-  if (a->splits > 1) {
-    const int64_t n = a->p.total_rows * a->q_heads * a->splits;
-    plan.part_o = 0;
-    plan.part_ml = (n * a->p.dim * 4 + 255) & ~int64_t{255};
-    plan.bytes = plan.part_ml + ((n * 8 + 255) & ~int64_t{255});
+  plan->bytes = 0;
+  if (plan->tiles && p.fmt != ipv::kBf16) {
+    const int64_t one = round256(static_cast<int64_t>(p.n_seqs) * p.heads * p.max_kv * p.dim * 2);
+    plan->k16 = 0;
+    plan->v16 = one;
+    plan->bytes = 2 * one;
   }
-  return plan;
+  if (a->splits > 1) {
+    const int64_t n = p.total_rows * a->q_heads * a->splits;
+    plan->part_o = plan->bytes;
+    plan->part_ml = plan->part_o + round256(n * p.dim * 4);
+    plan->bytes = plan->part_ml + round256(n * 8);
+  }
+}
+
+// The fp16 rows that codes are widened into, as a pool of one page per sequence.
+ipv::Pages widened(const ipv::Pages& p, char* k, char* v) {
+  ipv::Pages w = p;
+  w.fmt = ipv::kBf16;
+  w.page_size = p.max_kv > 0 ? p.max_kv : 1;
+  w.page_shift = 31;
+  w.n_pages = p.n_seqs;
+  w.max_pages = 1;
+  w.row_stride = 1;
+  w.head_stride = w.page_size;
+  w.page_stride = static_cast<int64_t>(w.page_size) * p.heads;
+  w.row_bytes = 2 * p.dim;
+  w.k = k;
+  w.v = v;
+  w.table = nullptr;
+  return w;
 }
 
 }  // namespace
@@ -252,7 +302,9 @@ extern "C" ipv_status ipv_attend_workspace(const ipv_pages* pages, const ipv_bat
   if (a.p.n_seqs == 0 || a.p.max_rows == 0) return IPV_OK;
   int num_sms = 0;
   if ((s = setup_current_device(&num_sms)) != IPV_OK) return s;
-  *bytes_out = make_plan(&a, num_sms).bytes;
+  Plan plan;
+  make_plan(&a, num_sms, &plan);
+  *bytes_out = plan.bytes;
   return IPV_OK;
 }
 
@@ -269,7 +321,8 @@ extern "C" ipv_status ipv_attend(const ipv_pages* pages, const ipv_batch* batch,
   if (args->lse && !aligned(args->lse, 4)) return reject(IPV_EINVAL, "lse must be 4-byte aligned");
   int num_sms = 0;
   if ((s = setup_current_device(&num_sms)) != IPV_OK) return s;
-  const Plan plan = make_plan(&a, num_sms);
+  Plan plan;
+  make_plan(&a, num_sms, &plan);
   if (plan.bytes > 0) {
     if (!args->workspace || args->workspace_bytes < plan.bytes)
       return reject(IPV_EINVAL, "the workspace has %lld bytes, the call needs %lld",
@@ -288,8 +341,42 @@ extern "C" ipv_status ipv_attend(const ipv_pages* pages, const ipv_batch* batch,
   a.part_o = reinterpret_cast<float*>(ws + plan.part_o);
   a.part_ml = reinterpret_cast<float2*>(ws + plan.part_ml);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = ipv::launch_attend_rows(a, st);
+  cudaError_t e;
+  if (plan.tiles) {
+    const bool bf16 = a.p.fmt == ipv::kBf16;
+    if (!bf16) {
+      ipv::ExpandArgs x{};
+      x.p = a.p;
+      x.k_out = reinterpret_cast<uint16_t*>(ws + plan.k16);
+      x.v_out = reinterpret_cast<uint16_t*>(ws + plan.v16);
+      x.causal = a.causal;
+      x.window = a.window;
+      x.sinks = a.sinks;
+      x.step = a.step;
+      if (a.p.max_kv > 0 && (e = ipv::launch_pages_expand(x, st)) != cudaSuccess) return cuda_reject(e, "code widening kernel");
+      a.p = widened(a.p, ws + plan.k16, ws + plan.v16);
+    }
+    if (!ipv::attend_tiles_maps(a, bf16, &plan.maps)) return reject(IPV_ECUDA, "cuTensorMapEncodeTiled refused the pool");
+    e = ipv::launch_attend_tiles(a, bf16, plan.maps, g_limit_ns.load(), st);
+  } else {
+    e = ipv::launch_attend_rows(a, st);
+  }
   if (e != cudaSuccess) return cuda_reject(e, "attention kernel");
   if (a.splits > 1 && (e = ipv::launch_attend_combine(a, st)) != cudaSuccess) return cuda_reject(e, "split join kernel");
+  return IPV_OK;
+}
+
+extern "C" ipv_status ipv_attend_error(uint32_t* err_out) {
+  if (!err_out) return reject(IPV_EINVAL, "err_out must not be NULL");
+  unsigned bits = 0;
+  const cudaError_t e = ipv::attend_tiles_error(&bits);
+  if (e != cudaSuccess) return cuda_reject(e, "reading the attention error word");
+  *err_out = bits;
+  return IPV_OK;
+}
+
+extern "C" ipv_status ipv_attend_wait_limit(int64_t nanoseconds) {
+  if (nanoseconds < 0) return reject(IPV_EINVAL, "the limit must not be negative");
+  g_limit_ns.store(nanoseconds == 0 ? kDefaultLimitNs : nanoseconds - 1);  // 1: no wait at all
   return IPV_OK;
 }

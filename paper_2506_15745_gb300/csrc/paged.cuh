@@ -1,5 +1,6 @@
 // Internal declarations of the paged cache (paged.cu: C ABI; paged_rows.cu:
-// write and read-back; attend_rows.cu: attention of a few query rows).
+// write and read-back; attend_rows.cu: attention of a few query rows;
+// attend_tiles.cu: of many).
 #pragma once
 
 #include <cuda_runtime.h>
@@ -124,6 +125,17 @@ struct RowsArgs {
 cudaError_t launch_pages_write(const RowsArgs& a, cudaStream_t st);
 cudaError_t launch_pages_read(const RowsArgs& a, cudaStream_t st);
 
+// Every row that the new rows of a sequence may read, widened from codes to
+// fp16 [n_seqs][heads][max_kv][dim]; rows that no step of `step` keys reads
+// are left out.
+struct ExpandArgs {
+  Pages p;
+  uint16_t* k_out;
+  uint16_t* v_out;
+  int causal, window, sinks, step;
+};
+cudaError_t launch_pages_expand(const ExpandArgs& a, cudaStream_t st);
+
 int attend_rows_tile(int rows);               // query rows of a row tile
 int attend_rows_ctas(int fmt, int dim);       // resident blocks per SM (smem)
 constexpr int kRowsStep = 32;                 // keys of a step
@@ -131,5 +143,17 @@ constexpr int kRowsWarps = 4;
 cudaError_t attend_rows_prepare();            // once per device
 cudaError_t launch_attend_rows(const AttendArgs& a, cudaStream_t st);
 cudaError_t launch_attend_combine(const AttendArgs& a, cudaStream_t st);
+
+// Many query rows (attend_tiles.cu): the pool's rows are 16-bit elements.
+constexpr int kTilesRows = 256;  // query rows of a block
+constexpr int kTilesStep = 128;  // keys of a step
+struct alignas(128) TileMaps {    // the pool as TMA sees it
+  unsigned char k[128], v[128];
+  int box_rows;                  // rows of a copy
+};
+cudaError_t attend_tiles_prepare();  // once per device
+bool attend_tiles_maps(const AttendArgs& a, bool bf16, TileMaps* maps);
+cudaError_t launch_attend_tiles(const AttendArgs& a, bool bf16, const TileMaps& maps, int64_t limit_ns, cudaStream_t st);
+cudaError_t attend_tiles_error(unsigned* bits);
 
 }  // namespace ipv

@@ -88,8 +88,8 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, uint32_t (&w)[2]) {
   return __half_as_ushort(hs) | (static_cast<uint32_t>(__half_as_ushort(hm)) << 16);
 }
 
-// The inverse, rounded once to bf16.
-template <int FMT>
+// The inverse, rounded once to bf16, or to fp16.
+template <int FMT, bool F16>
 __device__ __forceinline__ uint4 expand(const uint32_t (&w)[2], uint32_t par) {
   const float s = __half2float(__ushort_as_half(static_cast<unsigned short>(par & 0xFFFFu)));
   const float m = __half2float(__ushort_as_half(static_cast<unsigned short>(par >> 16)));
@@ -101,8 +101,12 @@ __device__ __forceinline__ uint4 expand(const uint32_t (&w)[2], uint32_t par) {
   }
   uint32_t o[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[i]) : "f"(f[2 * i + 1]), "f"(f[2 * i]));
+  for (int i = 0; i < 4; ++i) {
+    if (F16)
+      asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(o[i]) : "f"(f[2 * i + 1]), "f"(f[2 * i]));
+    else
+      asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[i]) : "f"(f[2 * i + 1]), "f"(f[2 * i]));
+  }
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
@@ -227,11 +231,60 @@ __global__ void __launch_bounds__(kBlock) read_kernel(RowsArgs a) {
     if (!it[u].in || it[u].g * kGroup + c * 8 >= a.p.dim) continue;
     if (FMT != kBf16) {
       const uint32_t wk[2] = {xk[u].x, xk[u].y}, wv[2] = {xv[u].x, xv[u].y};
-      xk[u] = expand<FMT>(wk, xk[u].z);
-      xv[u] = expand<FMT>(wv, xv[u].z);
+      xk[u] = expand<FMT, false>(wk, xk[u].z);
+      xv[u] = expand<FMT, false>(wv, xv[u].z);
     }
     *reinterpret_cast<uint4*>(a.k_out + it[u].packed + c * 8) = xk[u];
     *reinterpret_cast<uint4*>(a.v_out + it[u].packed + c * 8) = xv[u];
+  }
+}
+
+// Codes widened to fp16 for a kernel that takes 16-bit rows. A team's item is
+// one group of one row of one head, rows innermost, so that the output is
+// written in order.
+template <int FMT, int U>
+__global__ void __launch_bounds__(kBlock) expand_kernel(ExpandArgs a) {
+  const int b = blockIdx.z, h = blockIdx.y;
+  const Seq s = sequence(a.p, b);
+  if (s.n == 0) return;
+  const unsigned groups = a.p.groups, items = static_cast<unsigned>(s.len) * groups;
+  const unsigned base = blockIdx.x * (kTeams * U) + (threadIdx.x >> 3);
+  // Rows skip..lo-1 lie between the sinks and the first new row's window.
+  const int hi = a.causal ? max(0, s.len - s.n + 1) : s.len;
+  const int lo = a.window ? max(0, hi - a.window) / a.step * a.step : 0;
+  const int skip = a.sinks > 0 ? ((a.sinks - 1) / a.step + 1) * a.step : 0;
+  const int c = threadIdx.x & 7;
+  uint32_t wk[U][2], wv[U][2], pk[U], pv[U];
+  int64_t out[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const unsigned item = base + u * kTeams;
+    const int j = static_cast<int>(groups == 2 ? item >> 1 : item), g = groups == 2 ? item & 1 : 0;
+    out[u] = -1;
+    wk[u][0] = wk[u][1] = wv[u][0] = wv[u][1] = pk[u] = pv[u] = 0;
+    if (item >= items || (j >= skip && j < lo)) continue;
+    out[u] = ((static_cast<int64_t>(b) * a.p.heads + h) * a.p.max_kv + j) * a.p.dim + g * kGroup + c * 8;
+    const int64_t r = pool_row(a.p, b, j);
+    if (r < 0) continue;
+    const int64_t row = r + h * a.p.head_stride;
+    const int64_t at = row * a.p.row_bytes + g * (FMT == kU8 ? kGroup : kGroup / 2);
+    const uint32_t* kd = reinterpret_cast<const uint32_t*>(a.p.k + at);
+    const uint32_t* vd = reinterpret_cast<const uint32_t*>(a.p.v + at);
+    if (FMT == kU8) {
+      wk[u][0] = kd[place_u8(2 * c)], wk[u][1] = kd[place_u8(2 * c + 1)];
+      wv[u][0] = vd[place_u8(2 * c)], wv[u][1] = vd[place_u8(2 * c + 1)];
+    } else {
+      wk[u][0] = kd[place_u4(c)];
+      wv[u][0] = vd[place_u4(c)];
+    }
+    pk[u] = a.p.k_par[row * groups + g];
+    pv[u] = a.p.v_par[row * groups + g];
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (out[u] < 0) continue;
+    *reinterpret_cast<uint4*>(a.k_out + out[u]) = expand<FMT, true>(wk[u], pk[u]);
+    *reinterpret_cast<uint4*>(a.v_out + out[u]) = expand<FMT, true>(wv[u], pv[u]);
   }
 }
 
@@ -260,6 +313,18 @@ cudaError_t launch_pages_read(const RowsArgs& a, cudaStream_t st) {
     case kU8: read_kernel<kU8, 2><<<g, kBlock, 0, st>>>(a); break;
     default: read_kernel<kU4, 2><<<g, kBlock, 0, st>>>(a); break;
   }
+  return cudaGetLastError();
+}
+
+cudaError_t launch_pages_expand(const ExpandArgs& a, cudaStream_t st) {
+  constexpr int kU = 2;
+  const int64_t items = static_cast<int64_t>(a.p.max_kv) * a.p.groups;
+  const dim3 g(static_cast<unsigned>((items + kTeams * kU - 1) / (kTeams * kU)), static_cast<unsigned>(a.p.heads),
+               static_cast<unsigned>(a.p.n_seqs));
+  if (a.p.fmt == kU8)
+    expand_kernel<kU8, kU><<<g, kBlock, 0, st>>>(a);
+  else
+    expand_kernel<kU4, kU><<<g, kBlock, 0, st>>>(a);
   return cudaGetLastError();
 }
 

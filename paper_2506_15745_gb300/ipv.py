@@ -128,11 +128,14 @@ def load():
         lib.ipv_pages_read.argtypes = [P, P, P, P, I64, I64, P]
         lib.ipv_attend_workspace.argtypes = [P, P, P, P]
         lib.ipv_attend.argtypes = [P, P, P, P]
+        lib.ipv_attend_error.argtypes = [ctypes.POINTER(ctypes.c_uint32)]
+        lib.ipv_attend_wait_limit.argtypes = [I64]
         for name in ("ipv_init", "ipv_compress", "ipv_score", "ipv_select",
                      "ipv_profile_enable", "ipv_profile_collect", "ipv_device_error",
                      "ipv_compress_static", "ipv_van_pool", "ipv_append_frames",
                      "ipv_set_wait_limit", "ipv_pages_write", "ipv_pages_read",
-                     "ipv_attend_workspace", "ipv_attend"):
+                     "ipv_attend_workspace", "ipv_attend", "ipv_attend_error",
+                     "ipv_attend_wait_limit"):
             getattr(lib, name).restype = I32
         _lib = lib
     return _lib
@@ -276,3 +279,15 @@ def attend_workspace(pages, batch, args: AttendArgs) -> int:
 
 def attend(pages, batch, args: AttendArgs, stream=None) -> None:
     _check(load().ipv_attend(pages, batch, ctypes.byref(args), _stream(stream)))
+
+
+def attend_error() -> int:
+    """Timeout bits of the attention since the last read (waits for the device)."""
+    out = ctypes.c_uint32(0)
+    _check(load().ipv_attend_error(ctypes.byref(out)))
+    return out.value
+
+
+def attend_wait_limit(nanoseconds: int) -> None:
+    """ipv_attend_wait_limit: the longest wait inside the attention's kernel (0: default)."""
+    _check(load().ipv_attend_wait_limit(int(nanoseconds)))

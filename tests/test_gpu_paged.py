@@ -373,6 +373,16 @@ def test_large_and_small_queries():
             check_attend(s, sub, out, lse, scale)
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "u4"])
+@pytest.mark.parametrize("scale", [0.0, -0.1])
+def test_scales_that_are_not_positive(fmt, scale):
+    gen = torch.Generator().manual_seed(75)
+    for n in (1, 20):
+        s = Setup(gen, fmt, 2, 128, 16, [200, 90], [1, n])
+        q, out, lse = run_attend(s, 4, 76, scale=scale, window=50, sinks=3)
+        check_attend(s, q, out, lse, scale, window=50, sinks=3)
+
+
 def test_bits_do_not_change_between_runs_and_streams():
     gen = torch.Generator().manual_seed(81)
     s = Setup(gen, "u8", 2, 128, 64, [3000, 1700], [1, 1])
@@ -464,3 +474,19 @@ def test_refusals_on_the_gpu():
                       total_rows=0, max_rows=0, max_kv=0)
     assert s.cache.attend(q[:0], none).shape == (0, 8, 128)
     s.cache.write(q[:0, :1], q[:0, :1], none)
+
+
+def test_a_wait_that_runs_out_is_reported():
+    """With no time to wait the many-row kernel gives up, says so and leaves the device usable."""
+    gen = torch.Generator().manual_seed(121)
+    s = Setup(gen, "bf16", 1, 128, 64, [900], [100])
+    assert ipv.attend_error() == 0
+    ipv.attend_wait_limit(1)
+    try:
+        run_attend(s, 8, 122)
+        assert ipv.attend_error() != 0
+    finally:
+        ipv.attend_wait_limit(0)
+    q, out, lse = run_attend(s, 8, 122)
+    assert ipv.attend_error() == 0
+    check_attend(s, q, out, lse, 128 ** -0.5)

@@ -77,6 +77,12 @@ def test_null_structures_and_bad_rows(lib):
     assert lib.ipv_pages_read(p, b, 0x80000, 0x80000, 512, 128, None) == ipv.IPV_EINVAL
 
 
+def test_diagnostics(lib):
+    assert lib.ipv_attend_error(None) == ipv.IPV_EINVAL
+    assert lib.ipv_attend_wait_limit(-1) == ipv.IPV_EINVAL
+    assert lib.ipv_attend_wait_limit(0) == ipv.IPV_OK
+
+
 def test_an_empty_batch_is_nothing_to_do(lib):
     for empty in (dict(n_seqs=0, row_start=None, kv_len=None), dict(max_rows=0), dict(total_rows=0)):
         p, b = refs(PAGES, {**BATCH, **empty})
