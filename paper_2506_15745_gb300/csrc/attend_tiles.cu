@@ -1,19 +1,23 @@
 // Attention of many query rows over a paged cache: chunks of new tokens.
 //
 // Bound by the tensor cores (4 * head_dim operations per query row and key it
-// sees) once there are a few hundred query rows. A block owns 256 query rows
-// of one (sequence, KV head): two tiles of 128, in which the query heads that
-// share the KV head lie next to each other, so their K and V are fetched once.
-// It walks over tiles of 128 keys with ten warps:
-//   - one warp copies K and V tiles from their pages by TMA (a box per page),
-//   - one thread issues the matrix instructions (tcgen05.mma): S = Q K^T into
-//     tensor memory and, with the softmax weights P read from tensor memory,
-//     O += P V; while one query tile is in its softmax the other's products run,
-//   - a warpgroup per query tile does the softmax, one thread per query row: it
-//     reads S, takes exp2, stores P in S's place and keeps the running maximum
-//     and sum. O stays in tensor memory and is rescaled only when the maximum
-//     has grown by more than 2^8: weights up to 256 are as exact as weights up
-//     to 1, and hardly any tile needs it.
+// sees) once there are a few hundred query rows. The unit of work is a step:
+// 256 query rows of one (sequence, KV head), as two tiles of 128 in which the
+// query heads that share the KV head lie next to each other, by 128 keys. A
+// block per SM takes an equal share of all steps, in order; where a share ends
+// inside a tile's keys, the block leaves a partial result that a second kernel
+// joins. A block has twelve warps:
+//   - one copies K and V tiles from their pages by TMA (a box per page),
+//   - one for each query tile issues its matrix instructions (tcgen05.mma):
+//     S = Q K^T into tensor memory and, with the softmax weights P read from
+//     tensor memory, O += P V. They take turns, so that one tile's products run
+//     while the other is in its softmax; a warp's waits pass during the other's
+//     turn,
+//   - four for each query tile do its softmax, one thread per query row: it reads
+//     S, takes exp2, stores P in S's place and keeps the running maximum and
+//     sum. O stays in tensor memory and is rescaled only when the maximum has
+//     grown by more than 2^8: weights up to 256 are as exact as weights up to 1,
+//     and hardly any step needs it.
 // Operands are bf16 (bf16 pages) or fp16 (codes, widened into the workspace
 // beforehand); S, O and all statistics are fp32, P is rounded to the operand's
 // type.
@@ -34,12 +38,12 @@ namespace {
 
 constexpr int kRowsCta = kTilesRows;  // query rows of a block
 constexpr int kKeys = kTilesStep;     // keys of a step
-constexpr int kSoftmaxThreads = 256;
-constexpr int kMmaWarp = 8, kLoadWarp = 9;
-constexpr int kThreads = 320;
+constexpr int kMmaWarp = 8, kLoadWarp = 10;  // warps 8, 9: products of query tiles 0, 1
+constexpr int kThreads = 384;                // two softmax warpgroups, one for copies and products
 constexpr int kHalf = 128 * 128;      // bytes of 128 rows x 64 channels
 constexpr float kNegInf = -INFINITY;
 constexpr float kLazy = 8.0f;         // log2 of the growth that rescales O
+constexpr int kAhead = 4;             // pairs between the softmax's pipes
 
 template <int DP>
 struct Layout {
@@ -50,13 +54,13 @@ struct Layout {
   static constexpr int kK = 2 * kTile;
   static constexpr int kV = kK + kStages * kTile;
   static constexpr int kBars = kV + kStages * kTile;
-  static constexpr int kScale = kBars + 256;             // 256 floats
+  static constexpr int kScale = kBars + 512;             // 256 floats
   static constexpr int kBytes = kScale + 1024 + 1024;    // + alignment of the base
 };
 
 // Barriers, 8 bytes each.
-enum : int { kBarKFull = 0, kBarKEmpty = 4, kBarVFull = 8, kBarVEmpty = 12, kBarS = 16, kBarP = 18, kBarO = 20, kBarQ = 21, kBarDrain = 22,
-             kWordTmem = 23 * 8, kWordStop = 24 * 8 };
+enum : int { kBarKFull = 0, kBarKEmpty = 4, kBarVFull = 8, kBarVEmpty = 12, kBarS = 16, kBarP = 18, kBarO = 22, kBarQ = 24,
+             kBarDrain = 26, kBarVTail = 28, kBarTurn = 32, kBars = 34, kWordTmem = 34 * 8, kWordStop = 35 * 8 };
 
 // ------------------------------------------------------------------ PTX
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
@@ -90,25 +94,31 @@ __device__ __forceinline__ uint32_t lds_flag(uint32_t at) {
   return v;
 }
 
-// Waits for a phase of a barrier, at most limit_ns. When the time is up (or
-// another warp's was) the block stops: every wait returns false from then on,
-// `bit` goes to the error word, and the kernel winds up without results.
-__device__ __noinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, uint32_t stop, int64_t limit_ns, unsigned bit) {
+// Waits for a phase of a barrier, at most limit_ns, with the whole warp. When
+// the time is up the block stops: `bit` goes to the error word, every wait
+// returns at once from then on, and the kernel winds up without results.
+__device__ __forceinline__ void bar_wait_slow(uint32_t bar, uint32_t parity, uint32_t stop, int64_t limit_ns, unsigned bit) {
   const uint64_t t0 = now_ns();
+#pragma unroll 1
   for (;;) {
-    if (lds_flag(stop)) return false;
+    if (lds_flag(stop)) return;
     if (static_cast<int64_t>(now_ns() - t0) >= limit_ns) {
       asm volatile("st.volatile.shared.b32 [%0], %1;" ::"r"(stop), "r"(1u) : "memory");
       atomicOr(&g_attend_error, bit);
-      return false;
+      return;
     }
+#pragma unroll 1
     for (int i = 0; i < 8; ++i)
-      if (bar_try(bar, parity)) return true;
+      if (bar_try(bar, parity)) return;
   }
 }
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t stop, int64_t limit_ns, unsigned bit) {
-  if (limit_ns > 0 && bar_try(bar, parity)) return true;
-  return bar_wait_slow(bar, parity, stop, limit_ns, bit);
+// The first try stands in line and the loop out of it: a wait that is over
+// costs 60 clocks that way, and 190 where the try is a loop's.
+__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, uint32_t stop, int64_t limit_ns, unsigned bit) {
+  bool ok = limit_ns > 0;
+  if (ok) ok = bar_try(bar, parity);
+  if (__builtin_expect(!ok, 0)) bar_wait_slow(bar, parity, stop, limit_ns, bit);
+  __syncwarp();
 }
 
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3) {
@@ -118,27 +128,70 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, u
       : "memory");
 }
 
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
+// Shared-memory matrix descriptors, 128-byte swizzle: the low word holds the
+// address (in 16 bytes) and the leading offset, the high word the atoms' stride,
+// the version and the swizzle. Rows of 128 bytes, 8 rows to an atom of 1024
+// bytes. K-major (Q, K): atoms 1024 bytes apart along rows. MN-major (V: a row
+// is a key, its channels are the instruction's N): atoms 1024 bytes apart along
+// keys, 64-channel halves kHalf apart (the leading offset).
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_k(uint32_t at) { return ((at & 0x3FFFF) >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_mn(uint32_t at) { return ((at & 0x3FFFF) >> 4) | (static_cast<uint32_t>(kHalf >> 4) << 16); }
+
+// D (tensor memory) = or += A B, one K = 16 step; OFF: 16-byte units from the
+// operands' descriptors (A in tensor memory: columns) to the step's. The whole
+// warp runs these and one elected thread issues: operands stay in uniform
+// registers, and twice as many instructions wait in the tensor core's queue as
+// when a lane issues from a branch of its own.
+template <int OFF_A, int OFF_B>
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool acc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(acc ? 1u : 0u)
+      "{\n\t.reg .pred p, e;\n\t.reg .b32 x, y;\n\t.reg .b64 da, db;\n\t"
+      "setp.ne.u32 p, %4, 0;\n\t"
+      "add.u32 x, %1, %5;\n\tadd.u32 y, %2, %6;\n\t"
+      "mov.b64 da, {x, %7};\n\tmov.b64 db, {y, %7};\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(acc ? 1u : 0u), "n"(OFF_A), "n"(OFF_B), "r"(kDescHigh)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool acc) {
+template <int OFF_A, int OFF_B>
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool acc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(acc ? 1u : 0u)
+      "{\n\t.reg .pred p, e;\n\t.reg .b32 x, y;\n\t.reg .b64 db;\n\t"
+      "setp.ne.u32 p, %4, 0;\n\t"
+      "add.u32 x, %1, %5;\n\tadd.u32 y, %2, %6;\n\t"
+      "mov.b64 db, {y, %7};\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(acc ? 1u : 0u), "n"(OFF_A), "n"(OFF_B), "r"(kDescHigh)
       : "memory");
 }
-__device__ __forceinline__ void mma_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+// S = Q K^T (KS steps over the channels) and O += P V (KS over the keys).
+template <int KS, int N>
+__device__ __forceinline__ void product_s(uint32_t d, uint32_t q, uint32_t k, uint32_t idesc) {
+  if constexpr (KS < N) {
+    constexpr int kOff = ((KS / 4) * kHalf + (KS % 4) * 32) >> 4;
+    mma_ss<kOff, kOff>(d, q, k, idesc, KS > 0);
+    product_s<KS + 1, N>(d, q, k, idesc);
+  }
+}
+template <int KS, int N>
+__device__ __forceinline__ void product_o(uint32_t d, uint32_t p, uint32_t v, uint32_t idesc, bool acc) {
+  if constexpr (KS < N) {
+    mma_ts<KS * 8, KS * (2048 >> 4)>(d, p, v, idesc, acc || KS > 0);
+    product_o<KS + 1, N>(d, p, v, idesc, acc);
+  }
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {  // by the thread that elect.sync elects
+  asm volatile(
+      "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar)
+      : "memory");
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 #define IPV_R8(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7])
@@ -152,6 +205,12 @@ __device__ __forceinline__ void tm_load(uint32_t* r, uint32_t at) {
       : IPV_R8(r, 0), IPV_R8(r, 8), IPV_R8(r, 16), IPV_R8(r, 24)
       : "r"(at));
 }
+// Waits for the thread's loads from tensor memory; the registers are those of
+// the last one, so that nothing that uses them moves above the wait.
+#define IPV_RW8(r, o) "+r"(r[o]), "+r"(r[o + 1]), "+r"(r[o + 2]), "+r"(r[o + 3]), "+r"(r[o + 4]), "+r"(r[o + 5]), "+r"(r[o + 6]), "+r"(r[o + 7])
+__device__ __forceinline__ void wait_ld(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : IPV_RW8(r, 0), IPV_RW8(r, 8), IPV_RW8(r, 16), IPV_RW8(r, 24)::"memory");
+}
 __device__ __forceinline__ void tm_store32(uint32_t at, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
@@ -159,17 +218,14 @@ __device__ __forceinline__ void tm_store32(uint32_t at, const uint32_t* r) {
       IPV_W8(r, 8), IPV_W8(r, 16), IPV_W8(r, 24), "r"(at)
       : "memory");
 }
-__device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::IPV_W8(r, 0),
-      IPV_W8(r, 8), "r"(at)
-      : "memory");
-}
-
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
 }
 template <bool BF16>
@@ -182,18 +238,6 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return r;
 }
 
-// Shared-memory matrix descriptors, 128-byte swizzle. Rows of 128 bytes, 8 rows
-// to an atom of 1024 bytes. K-major (Q, K): atoms 1024 bytes apart along rows.
-// MN-major (V: a row is a key, its channels are the instruction's N): atoms
-// 1024 bytes apart along keys, 64-channel halves kHalf apart.
-__device__ __forceinline__ uint64_t desc_k(uint32_t at) {
-  return static_cast<uint64_t>((at & 0x3FFFF) >> 4) | (uint64_t{1} << 16) | (uint64_t{1024 >> 4} << 32) | (uint64_t{1} << 46) |
-         (uint64_t{2} << 61);
-}
-__device__ __forceinline__ uint64_t desc_mn(uint32_t at) {
-  return static_cast<uint64_t>((at & 0x3FFFF) >> 4) | (uint64_t{kHalf >> 4} << 16) | (uint64_t{1024 >> 4} << 32) |
-         (uint64_t{1} << 46) | (uint64_t{2} << 61);
-}
 // Instruction descriptor: fp32 accumulator, both operands bf16 or fp16, M = 128.
 template <bool BF16>
 __device__ __forceinline__ constexpr uint32_t instr(int n, bool b_mn) {
@@ -201,29 +245,162 @@ __device__ __forceinline__ constexpr uint32_t instr(int n, bool b_mn) {
          (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(128 >> 4) << 24);
 }
 
+// ------------------------------------------------------------------ work
+// A tile of 256 query rows of a sequence: pair number p = sequence * tiles + tile.
+struct Tile {
+  Seq seq;
+  int b, row0, n_rows, steps;
+  KeyRange kr;
+};
+
+__device__ __forceinline__ void set_tile(const AttendArgs& a, Tile& x, int b, int tile) {
+  x.row0 = tile * kRowsCta;
+  x.n_rows = min(kRowsCta, x.seq.n * a.share - x.row0);
+  x.b = b;
+  x.steps = 0;
+  if (x.n_rows > 0) {
+    x.kr = key_range(a, x.seq, x.row0 / a.share, (x.row0 + x.n_rows - 1) / a.share);
+    x.steps = max(1, x.kr.steps);  // rows that see nothing have their results to write, too
+  }
+}
+__device__ __forceinline__ Tile tile_of(const AttendArgs& a, int tiles, int p) {
+  Tile x;
+  const int b = p / tiles;
+  x.seq = sequence(a.p, b);
+  set_tile(a, x, b, p - b * tiles);
+  return x;
+}
+
+// What a block shares out: a tile's keys for one KV head weigh their steps and
+// kRunCost more, about what loading the queries, filling the pipeline and
+// writing the results take.
+constexpr int kRunCost = 3;
+
+// A block's share: from step s of KV head `head` of pair p, as far as `left`
+// units of weight go. Heads of a pair follow one another, then pairs.
+struct Share {
+  int p, head;
+  int64_t at, left;  // units into the pair's head, units left
+};
+
+// Walks a share, a run of steps of one (pair, head) at a time. A boundary within
+// the first kRunCost units leaves all steps to the block behind it.
+struct Walk {
+  Tile t;
+  int head, s, n;  // steps s .. s + n - 1
+  int64_t left;
+  __device__ __forceinline__ void cut(int64_t at) {
+    const int64_t weight = t.steps + kRunCost, upto = min(weight, at + left);
+    s = static_cast<int>(max(int64_t{0}, at - kRunCost));
+    n = static_cast<int>(max(int64_t{0}, upto - kRunCost)) - s;
+    left -= upto - at;
+  }
+  __device__ __forceinline__ bool begin(const AttendArgs& a, int tiles, const Share& w) {
+    t = tile_of(a, tiles, w.p);
+    head = w.head;
+    left = w.left;
+    cut(w.at);
+    return n > 0 || next(a, tiles);
+  }
+  __device__ __forceinline__ bool next(const AttendArgs& a, int tiles) {
+    if (left <= 0) return false;
+    if (++head == a.p.heads) {
+      head = 0;
+      int tile = t.row0 / kRowsCta, b = t.b;
+      do {
+        if (++tile == tiles) {
+          tile = 0;
+          if (++b == a.p.n_seqs) return false;  // only if the lengths changed under the kernel
+          t.seq = sequence(a.p, b);
+        }
+        set_tile(a, t, b, tile);
+      } while (t.steps == 0);
+    }
+    cut(0);
+    return n > 0;
+  }
+  __device__ __forceinline__ bool starts() const { return s == 0; }
+  __device__ __forceinline__ bool ends() const { return s + n == t.steps; }
+  __device__ __forceinline__ int pair(int tiles) const { return t.b * tiles + t.row0 / kRowsCta; }
+  // Rows of the last V tile from `keep` on lie past the last key.
+  __device__ __forceinline__ int keep() const { return t.kr.hi_max - t.kr.key0(s + n - 1, kKeys); }
+};
+
+// Finds the block's share, with all threads; scratch: 16 64-bit words of shared memory.
+__device__ Share find_share(const AttendArgs& a, int tiles, int64_t* scratch) {
+  const int pairs = a.p.n_seqs * tiles, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  constexpr int kWarps = kThreads / 32;
+  auto weight = [&](int p) {
+    const int steps = p < pairs ? tile_of(a, tiles, p).steps : 0;
+    return steps > 0 ? static_cast<int64_t>(steps + kRunCost) * a.p.heads : int64_t{0};
+  };
+  const int64_t first = weight(threadIdx.x);
+  int64_t sum = first;
+  for (int p = threadIdx.x + kThreads; p < pairs; p += kThreads) sum += weight(p);
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  if (lane == 0) scratch[warp] = sum;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) total += scratch[i];
+  int64_t per = (total + gridDim.x - 1) / gridDim.x;
+  if (per < a.unit + kRunCost) per = a.unit + kRunCost;
+  const int64_t from = per * blockIdx.x;
+  Share w;
+  w.left = min(per, total - from);
+  w.p = w.head = 0;
+  w.at = 0;
+  __syncthreads();
+  if (w.left <= 0) return w;
+  int64_t before = 0;
+  for (int p0 = 0; p0 < pairs; p0 += kThreads) {
+    const int64_t mine = p0 == 0 ? first : weight(p0 + threadIdx.x);
+    int64_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += y;
+    }
+    if (lane == 31) scratch[warp] = upto;
+    __syncthreads();
+    int64_t start = before, all = before;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      if (i < warp) start += scratch[i];
+      all += scratch[i];
+    }
+    start += upto - mine;
+    if (from >= start && from < start + mine) {
+      const int64_t one = mine / a.p.heads;
+      scratch[kWarps] = p0 + threadIdx.x;
+      scratch[kWarps + 1] = (from - start) / one;
+      scratch[kWarps + 2] = (from - start) % one;
+    }
+    __syncthreads();
+    if (from < all) break;
+    before = all;
+  }
+  w.p = static_cast<int>(scratch[kWarps]);
+  w.head = static_cast<int>(scratch[kWarps + 1]);
+  w.at = scratch[kWarps + 2];
+  return w;
+}
+
 // ------------------------------------------------------------------ kernel
 template <bool BF16, int DP>
 __global__ void __launch_bounds__(kThreads, 1)
     attend_tiles_kernel(AttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
-                        int box_rows, int64_t limit_ns) {
+                        int tiles, int box_rows, int64_t limit_ns) {
   using L = Layout<DP>;
   extern __shared__ unsigned char smem_raw[];
-  const int b = blockIdx.z, head = blockIdx.y;
-  const int n_tiles = gridDim.x / a.splits;
-  // Later tokens see more keys: their blocks start first.
-  const int tile = n_tiles - 1 - static_cast<int>(blockIdx.x) / a.splits, split = blockIdx.x % a.splits;
-  const Seq seq = sequence(a.p, b);
-  const int rows = seq.n * a.share;
-  const int row0 = tile * kRowsCta;
-  if (row0 >= rows) return;
-  const int n_rows = min(kRowsCta, rows - row0);
-  const KeyRange kr = key_range(a, seq, row0 / a.share, (row0 + n_rows - 1) / a.share);
-  if (split >= splits_of(a, kr)) return;
-  const int s_begin = split * a.unit, n = min(kr.steps - s_begin, a.unit);  // steps of this block, maybe 0
-  const bool two = n_rows > 128;
-
   const uint32_t base = (smem_u32(smem_raw) + 1023) & ~1023u;
   unsigned char* base_p = smem_raw + (base - smem_u32(smem_raw));
+  const Share share = find_share(a, tiles, reinterpret_cast<int64_t*>(base_p + L::kScale));
+  if (share.left <= 0) {
+    if (threadIdx.x < 2) a.part_rec[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
+    return;
+  }
   const uint32_t bars = base + L::kBars, stop = bars + kWordStop;
   auto bar = [&](int i) { return bars + 8 * i; };
   float* row_scale = reinterpret_cast<float*>(base_p + L::kScale);
@@ -234,11 +411,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 16; ++i) bar_init(bar(i), 1);
-    bar_init(bar(kBarS), 1), bar_init(bar(kBarS + 1), 1);
-    bar_init(bar(kBarP), 128), bar_init(bar(kBarP + 1), 128);
-    bar_init(bar(kBarO), 1), bar_init(bar(kBarDrain), 1);
-    bar_init(bar(kBarQ), kSoftmaxThreads);
+    for (int i = 0; i < kBars; ++i) {
+      const bool tiles2 = (i >= kBarKEmpty && i < kBarVFull) || (i >= kBarVEmpty && i < kBarS);  // both product warps
+      const bool warps4 = (i >= kBarP && i < kBarO) || (i >= kBarQ && i < kBarDrain);            // a warpgroup's warps
+      bar_init(bar(i), tiles2 ? 2 : warps4 ? 4 : 1);
+    }
     asm volatile("st.volatile.shared.b32 [%0], %1;" ::"r"(stop), "r"(0u) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async();
@@ -246,206 +423,303 @@ __global__ void __launch_bounds__(kThreads, 1)
   fence_before();
   __syncthreads();
   fence_after();
-  uint32_t tmem;
-  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(bars + kWordTmem) : "memory");
+  constexpr uint32_t tmem = 0;  // all 512 columns are the block's: they start at 0
+  Walk w = {};
 
-  if (warp == kLoadWarp) {
-    // ---------------------------------------------------------------- copies
-    const int pieces = kKeys / box_rows;
-    const uint32_t piece_bytes = box_rows * 128;
-    int issued_k = 0, issued_v = 0;
-    bool ok = true;
-    for (int i = 0; i < n && ok; ++i) {
-      const int st = i % L::kStages;
-      const uint32_t empty = ((i / L::kStages) & 1) ^ 1;
-      const int key0 = kr.key0(s_begin + i, kKeys);
-      const int j = key0 + lane * box_rows;
-      const bool active = lane < pieces && j < kr.hi_max;
-      int page = 0, row = 0;
-      if (active) {
-        const int at = j >> a.p.page_shift;
-        page = a.p.table ? a.p.table[b * a.p.table_stride + at] : b;
+  // Registers: 384 threads start with 168 each; 256 take 224 (a row's 128 scores
+  // stay in registers), 128 keep 56: the same 64512 in all.
+  if (warp >= kMmaWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp == kLoadWarp) {
+      // -------------------------------------------------------------- copies
+      const int pieces = kKeys / box_rows;
+      const uint32_t piece_bytes = box_rows * 128;
+      int it = 0, k_out = 0, v_out = 0;  // steps; K and V tiles asked for
+      // This lane's piece of step i: its page and the row there, page < 0: none.
+      auto piece = [&](int i, int& page, int& row) {
+        const int j = w.t.kr.key0(w.s + i, kKeys) + lane * box_rows;
+        page = -1;
+        row = 0;
+        if (lane >= pieces || j >= w.t.kr.hi_max) return;
+        page = a.p.table ? a.p.table[w.t.b * a.p.table_stride + (j >> a.p.page_shift)] : w.t.b;
         // A page the pool does not have: past the map's end, which reads as zero.
         if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.p.n_pages)) page = a.p.n_pages;
         row = a.p.page_shift == 31 ? j : j & (a.p.page_size - 1);
-      }
-      const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, active)) * piece_bytes * L::kHalves;
-      for (int kv = 0; kv < 2 && ok; ++kv) {
-        const uint32_t full = bar((kv ? kBarVFull : kBarKFull) + st);
-        ok = bar_wait(bar((kv ? kBarVEmpty : kBarKEmpty) + st), empty, stop, limit_ns, 1u);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        if (lane == 0) bar_expect(full, bytes);
-        __syncwarp();
-        if (active) {
-          const uint32_t dst = base + (kv ? L::kV : L::kK) + st * L::kTile + lane * piece_bytes;
+      };
+      for (bool go = w.begin(a, tiles, share); go; go = w.next(a, tiles)) {
+        int page_next, row_next;
+        piece(0, page_next, row_next);
+        for (int i = 0; i < w.n; ++i, ++it) {
+          const int st = it % L::kStages;
+          const uint32_t empty = ((it / L::kStages) & 1) ^ 1;
+          const int page = page_next, row = row_next;
+          const bool active = page >= 0;
+          const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, active)) * piece_bytes * L::kHalves;
+          if (i + 1 < w.n) piece(i + 1, page_next, row_next);  // the table is read a step ahead
+          for (int kv = 0; kv < 2; ++kv) {
+            const uint32_t full = bar((kv ? kBarVFull : kBarKFull) + st);
+            bar_wait(bar((kv ? kBarVEmpty : kBarKEmpty) + st), empty, stop, limit_ns, 1u);
+            if (__any_sync(0xffffffffu, lds_flag(stop))) break;
+            if (lane == 0) bar_expect(full, bytes);
+            __syncwarp();
+            if (active) {
+              const uint32_t dst = base + (kv ? L::kV : L::kK) + st * L::kTile + lane * piece_bytes;
 #pragma unroll
-          for (int h = 0; h < L::kHalves; ++h) tma_load(dst + h * kHalf, kv ? &v_map : &k_map, full, 64 * h, row, head, page);
+              for (int h = 0; h < L::kHalves; ++h)
+                tma_load(dst + h * kHalf, kv ? &v_map : &k_map, full, 64 * h, row, w.head, page);
+            }
+            (kv ? v_out : k_out) = it + 1;
+            __syncwarp();
+          }
         }
-        (kv ? issued_v : issued_k) = i + 1;
-        __syncwarp();
+        if (w.keep() < kKeys) {
+          // Rows past the last key hold anything; a weight of 0 would not hide a NaN.
+          const int last = it - 1, st = last % L::kStages, keep = w.keep();
+          bar_wait(bar(kBarVFull + st), (last / L::kStages) & 1, stop, limit_ns, 1u);
+          for (int x = lane; x < (kKeys - keep) * 8 * L::kHalves; x += 32) {
+            const int c = x & 7, h = L::kHalves == 2 ? (x >> 3) & 1 : 0, r = keep + x / (8 * L::kHalves);
+            *reinterpret_cast<uint4*>(base_p + L::kV + st * L::kTile + h * kHalf + r * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+          }
+          fence_async();
+          __syncwarp();
+          if (lane == 0) bar_arrive(bar(kBarVTail + st));
+        }
+        if (__any_sync(0xffffffffu, lds_flag(stop))) break;
       }
-    }
-    if (!ok) {
-      // Stopped: the block's memory must outlive the copies in flight.
-      for (int i = max(0, issued_k - L::kStages); i < issued_k; ++i)
-        for (int w = 0; w < 1 << 16 && !bar_try(bar(kBarKFull + i % L::kStages), (i / L::kStages) & 1); ++w) {
-        }
-      for (int i = max(0, issued_v - L::kStages); i < issued_v; ++i)
-        for (int w = 0; w < 1 << 16 && !bar_try(bar(kBarVFull + i % L::kStages), (i / L::kStages) & 1); ++w) {
-        }
-    }
-  } else if (warp == kMmaWarp) {
-    // -------------------------------------------------------------- products
-    const uint32_t idesc_s = instr<BF16>(kKeys, false), idesc_o = instr<BF16>(DP, true);
-    bool ok = true;
-    auto wait = [&](int i, uint32_t parity, unsigned bit) {
-      ok = ok && bar_wait(bar(i), parity, stop, limit_ns, bit);
-      ok = __all_sync(0xffffffffu, ok);
-      if (ok) fence_after();
-      return ok;
-    };
-    auto scores = [&](int t, int st) {
-      if (lane == 0) {
-#pragma unroll
-        for (int ks = 0; ks < DP / 16; ++ks) {
-          const uint32_t off = (ks / 4) * kHalf + (ks % 4) * 32;
-          mma_ss(tmem + t * 128, desc_k(base + L::kQ + t * L::kTile + off), desc_k(base + L::kK + st * L::kTile + off), idesc_s,
-                 ks > 0);
-        }
+      if (__any_sync(0xffffffffu, lds_flag(stop))) {
+        // Stopped: the block's memory must outlive the copies in flight.
+        for (int i = max(0, k_out - L::kStages); i < k_out; ++i)
+          for (int x = 0; x < 1 << 16 && !bar_try(bar(kBarKFull + i % L::kStages), (i / L::kStages) & 1); ++x) {
+          }
+        for (int i = max(0, v_out - L::kStages); i < v_out; ++i)
+          for (int x = 0; x < 1 << 16 && !bar_try(bar(kBarVFull + i % L::kStages), (i / L::kStages) & 1); ++x) {
+          }
+      }
+    } else if (warp < kLoadWarp) {
+      // ------------------------------------------------------------ products
+      const int t = warp - kMmaWarp;
+      constexpr uint32_t idesc_s = instr<BF16>(kKeys, false), idesc_o = instr<BF16>(DP, true);
+      const uint32_t q = desc_k(base + L::kQ + t * L::kTile), k0 = desc_k(base + L::kK), v0 = desc_mn(base + L::kV);
+      const uint32_t s_at = tmem + t * 128, o_at = tmem + 256 + t * DP;
+      auto wait = [&](int i, uint32_t parity) {
+        bar_wait(bar(i), parity, stop, limit_ns, 2u);
+        fence_after();
+      };
+      // Scores of step i into S; K's stage is free when they are done.
+      auto scores = [&](int i) {
+        const int st = i % L::kStages;
+        product_s<0, DP / 16>(s_at, q, k0 + st * (L::kTile >> 4), idesc_s);
         mma_commit(bar(kBarS + t));
-      }
-    };
-    auto output = [&](int t, int st, bool acc) {
-      if (lane == 0) {
-#pragma unroll
-        for (int ks = 0; ks < kKeys / 16; ++ks)
-          mma_ts(tmem + 256 + t * DP, tmem + t * 128 + ks * 8, desc_mn(base + L::kV + st * L::kTile + ks * 2048), idesc_o,
-                 acc || ks > 0);
-      }
-    };
-    if (n > 0) {
-      wait(kBarQ, 0, 2u);
-      if (ok && wait(kBarKFull, 0, 2u)) {
-        scores(0, 0);
-        if (two) scores(1, 0);
-        if (lane == 0) mma_commit(bar(kBarKEmpty));
-      }
-    }
-    for (int i = 0; i < n && ok; ++i) {
-      const int st = i % L::kStages, nx = (i + 1) % L::kStages;
-      const bool more = i + 1 < n;
-      if (!wait(kBarVFull + st, (i / L::kStages) & 1, 2u)) break;
-      const int left = kr.hi_max - kr.key0(s_begin + i, kKeys);
-      if (left < kKeys) {
-        // Rows past the last key hold anything; a weight of 0 would not hide a NaN.
-        for (int x = lane; x < (kKeys - left) * 8 * L::kHalves; x += 32) {
-          const int c = x & 7, h = L::kHalves == 2 ? (x >> 3) & 1 : 0, r = left + x / (8 * L::kHalves);
-          *reinterpret_cast<uint4*>(base_p + L::kV + st * L::kTile + h * kHalf + r * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+        mma_commit(bar(kBarKEmpty + st));
+      };
+      // Turn `it`: tile 0 begins, each tile's end is the other's beginning.
+      auto my_turn = [&](int it) { bar_wait(bar(kBarTurn + t), (it & 1) ^ (t == 0 ? 1 : 0), stop, limit_ns, 2u); };
+      int it = 0, done = 0, runs = 0;  // steps of the block, of this tile; runs of this tile
+      uint32_t tails = 0;              // bit per stage: parity of the tails it has held
+      for (bool go = w.begin(a, tiles, share); go; go = w.next(a, tiles)) {
+        const bool tail = w.keep() < kKeys;
+        if (w.t.n_rows <= 128 * t) {  // no rows in this tile: only lets go of K and V
+          for (int i = 0; i < w.n; ++i, ++it) {
+            const int st = it % L::kStages;
+            wait(kBarKFull + st, (it / L::kStages) & 1);
+            if (lane == 0) bar_arrive(bar(kBarKEmpty + st));
+            wait(kBarVFull + st, (it / L::kStages) & 1);
+            if (lane == 0) bar_arrive(bar(kBarVEmpty + st));
+            my_turn(it);
+            if (lane == 0) bar_arrive(bar(kBarTurn + (t ^ 1)));
+          }
+          if (tail) tails ^= 1u << ((it - 1) % L::kStages);
+          continue;
         }
-        fence_async();
+        wait(kBarQ + t, runs & 1);
+        wait(kBarKFull + it % L::kStages, (it / L::kStages) & 1);
+        scores(it);
+        for (int i = 0; i < w.n; ++i, ++it, ++done) {
+          const int st = it % L::kStages;
+          const bool more = i + 1 < w.n;
+          if (more || !tail)
+            wait(kBarVFull + st, (it / L::kStages) & 1);
+          else
+            wait(kBarVTail + st, (tails >> st) & 1);
+          if (more) wait(kBarKFull + (it + 1) % L::kStages, ((it + 1) / L::kStages) & 1);
+          // The weights come in two halves, as the softmax hands them over.
+          const uint32_t v = v0 + st * (L::kTile >> 4);
+          wait(kBarP + 2 * t, done & 1);
+          my_turn(it);
+          product_o<0, kKeys / 32>(o_at, s_at, v, idesc_o, i > 0);
+          wait(kBarP + 2 * t + 1, done & 1);
+          product_o<kKeys / 32, kKeys / 16>(o_at, s_at, v, idesc_o, true);
+          if (more) scores(it + 1);
+          if (lane == 0) bar_arrive(bar(kBarTurn + (t ^ 1)));
+          mma_commit(bar(kBarVEmpty + st));
+        }
+        mma_commit(bar(kBarO + t));
+        if (tail) tails ^= 1u << ((it - 1) % L::kStages);
+        ++runs;
+      }
+      if (__any_sync(0xffffffffu, lds_flag(stop))) {  // stopped: no product may be in flight when the memory goes
+        mma_commit(bar(kBarDrain + t));
+        for (int x = 0; x < 1 << 16 && !bar_try(bar(kBarDrain + t), 0); ++x) {
+        }
         __syncwarp();
       }
-      if (!wait(kBarP, i & 1, 2u)) break;
-      output(0, st, i > 0);
-      if (more) {
-        if (!wait(kBarKFull + nx, ((i + 1) / L::kStages) & 1, 2u)) break;
-        scores(0, nx);
-      }
-      if (two) {
-        if (!wait(kBarP + 1, i & 1, 2u)) break;
-        output(1, st, i > 0);
-        if (more) scores(1, nx);
-      }
-      if (lane == 0) {
-        mma_commit(bar(kBarVEmpty + st));
-        if (more) mma_commit(bar(kBarKEmpty + nx));
-        if (!more) mma_commit(bar(kBarO));
-      }
-      __syncwarp();
-    }
-    if (!ok) {  // stopped: no product may be in flight when the memory goes
-      if (lane == 0) mma_commit(bar(kBarDrain));
-      for (int w = 0; w < 1 << 16 && !bar_try(bar(kBarDrain), 0); ++w) {
-      }
-      __syncwarp();
     }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
     // --------------------------------------------------------------- softmax
     const int t = warp >> 2, wt = threadIdx.x & 127;  // query tile, thread in its warpgroup
-    // The query tile into shared memory, swizzled; rows that are not there are zero.
-    constexpr int kCh = DP / 8;
-    const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;  // a negative scale turns the queries
-    for (int x = wt; x < 128 * kCh; x += 128) {
-      const int r = x / kCh, c = x % kCh, rr = t * 128 + r;
-      uint4 q = make_uint4(0, 0, 0, 0);
-      if (rr < n_rows && c * 8 < a.p.dim) {
-        const int tok = (row0 + rr) / a.share, hq = row0 + rr - tok * a.share;
-        q = *reinterpret_cast<const uint4*>(a.q + (seq.row0 + static_cast<int64_t>(tok)) * a.q_row +
-                                            (head * a.share + hq) * a.q_head + c * 8);
-      }
-      uint32_t w[4] = {q.x, q.y, q.z, q.w};
-      if (BF16) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] ^= flip;
-      } else {
-        // To fp16: the row's largest magnitude goes to [2^9, 2^10), by a power of two.
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
-#pragma unroll
-        for (int d = 1; d < kCh; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-        const int e = min(max(static_cast<int>(top >> 7) - 127, -100), 126);
-        const float up = __uint_as_float(static_cast<uint32_t>(127 + 9 - e) << 23);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          w[i] ^= flip;
-          w[i] = pack2<false>(__uint_as_float(w[i] << 16) * up, __uint_as_float(w[i] & 0xFFFF0000u) * up);
-        }
-        if (c == 0) row_scale[rr] = fabsf(a.scale_log2) * __uint_as_float(static_cast<uint32_t>(127 - 9 + e) << 23);
-      }
-      *reinterpret_cast<uint4*>(base_p + L::kQ + t * L::kTile + (c / 8) * kHalf + r * 128 + ((c % 8) ^ (r & 7)) * 16) =
-          make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    fence_async();
-    bar_arrive(bar(kBarQ));
-    // row_scale: written by this warpgroup's threads, read by others of it
-    asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");
-
-    const int rr = t * 128 + wt;
-    const bool in = rr < n_rows;
-    const int tok = in ? (row0 + rr) / a.share : 0, hq = in ? head * a.share + row0 + rr - tok * a.share : 0;
-    const int hi = in ? token_hi(a, seq, tok) : 0x7FFFFFFF;  // rows that are not there need no mask
-    const int lo = in && a.window ? max(0, hi - a.window) : 0;
-    // Not 0, which would make a masked score (-inf) NaN.
-    const float scale = fmaxf(BF16 ? fabsf(a.scale_log2) : row_scale[rr], 1.17549435e-38f);
     const uint32_t lane_at = tmem + (static_cast<uint32_t>(warp & 3) << 21);
     const uint32_t s_at = lane_at + t * 128, o_at = lane_at + 256 + t * DP;
-    float m = kNegInf, l = 0.0f;
-    bool ok = true;
-    if (t == 0 || two) {
-      for (int i = 0; i < n; ++i) {
-        ok = __all_sync(0xffffffffu, bar_wait(bar(kBarS + t), i & 1, stop, limit_ns, 4u));
-        if (!ok) break;
-        fence_after();
-        const int key0 = kr.key0(s_begin + i, kKeys);
-        uint32_t s[128];
+    const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;  // a negative scale turns the queries
+    // A run's query tile into shared memory, swizzled; rows that are not there
+    // are zero. A warp loads its own 32 rows. Called when the products that read
+    // the tile before it are over.
+    auto load_queries = [&](const Walk& x) {
+      if (x.t.n_rows <= 128 * t) return;
+      constexpr int kCh = DP / 8, kBatch = 8;
+      const int row0 = x.t.row0 + 128 * t, n_rows = x.t.n_rows - 128 * t;
+      // The lane's first row and channel; the others follow 32 / kCh rows apart.
+      int tok = (row0 + 32 * (warp & 3) + lane / kCh) / a.share;
+      int hq = row0 + 32 * (warp & 3) + lane / kCh - tok * a.share;
+#pragma unroll 1
+      for (int x0 = lane; x0 < 32 * kCh; x0 += 32 * kBatch) {
+        uint4 q[kBatch];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tm_load(s + 32 * c, s_at + 32 * c);
-        wait_ld();
+        for (int i = 0; i < kBatch; ++i) {
+          const int r = 32 * (warp & 3) + (x0 + 32 * i) / kCh, c = (x0 + 32 * i) % kCh;
+          q[i] = make_uint4(0, 0, 0, 0);
+          if (r < n_rows && c * 8 < a.p.dim)
+            q[i] = *reinterpret_cast<const uint4*>(a.q + (x.t.seq.row0 + static_cast<int64_t>(tok)) * a.q_row +
+                                                   (x.head * a.share + hq) * a.q_head + c * 8);
+          for (hq += 32 / kCh; hq >= a.share; hq -= a.share) ++tok;
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const int r = 32 * (warp & 3) + (x0 + 32 * i) / kCh, c = (x0 + 32 * i) % kCh;
+          uint32_t y[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+          if (BF16) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y[k] ^= flip;
+          } else {
+            // To fp16: the row's largest magnitude goes to [2^9, 2^10), by a power of two.
+            uint32_t top = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) top = max(top, max(y[k] & 0x7FFFu, (y[k] >> 16) & 0x7FFFu));
+#pragma unroll
+            for (int d = 1; d < kCh; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const int e = min(max(static_cast<int>(top >> 7) - 127, -100), 126);
+            const float up = __uint_as_float(static_cast<uint32_t>(127 + 9 - e) << 23);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              y[k] ^= flip;
+              y[k] = pack2<false>(__uint_as_float(y[k] << 16) * up, __uint_as_float(y[k] & 0xFFFF0000u) * up);
+            }
+            if (c == 0) row_scale[128 * t + r] = fabsf(a.scale_log2) * __uint_as_float(static_cast<uint32_t>(127 - 9 + e) << 23);
+          }
+          *reinterpret_cast<uint4*>(base_p + L::kQ + t * L::kTile + (c / 8) * kHalf + r * 128 + ((c % 8) ^ (r & 7)) * 16) =
+              make_uint4(y[0], y[1], y[2], y[3]);
+        }
+      }
+      fence_async();
+      __syncwarp();
+      if (lane == 0) bar_arrive(bar(kBarQ + t));
+    };
+    int done = 0, runs = 0, run = 0, slots = 0;  // steps and runs of this tile, of the block; partial results used
+    bool go = w.begin(a, tiles, share);
+    if (go) load_queries(w);
+    while (go) {
+      Walk after = w;
+      const bool partial = !(w.starts() && w.ends());
+      const int slot = 2 * blockIdx.x + (run > 0 ? 1 : 0);
+      ++run;
+      if (partial) {
+        slots |= slot & 1 ? 2 : 1;
+        if (threadIdx.x == 0) a.part_rec[slot] = make_int4(1, w.pair(tiles), w.head, (w.starts() ? 1 : 0) | (w.ends() ? 2 : 0));
+      }
+      if (w.t.n_rows <= 128 * t) {
+        go = after.next(a, tiles);
+        if (go) load_queries(after);
+        w = after;
+        continue;
+      }
+      const Seq seq = w.t.seq;
+      const int row0 = w.t.row0 + 128 * t, n_rows = min(128, w.t.n_rows - 128 * t), head = w.head;
+      const bool in = wt < n_rows;
+      const int tok = in ? (row0 + wt) / a.share : 0, hq = in ? head * a.share + row0 + wt - tok * a.share : 0;
+      const int hi = in ? token_hi(a, seq, tok) : 0x7FFFFFFF;  // rows that are not there need no mask
+      const int lo = in && a.window ? max(0, hi - a.window) : 0;
+      // Not 0, which would make a masked score (-inf) NaN.
+      const float scale = fmaxf(BF16 ? fabsf(a.scale_log2) : row_scale[128 * t + wt], 1.17549435e-38f);
+      const float2 sc2 = make_float2(scale, scale);
+      float m = kNegInf, l = 0.0f;
+      for (int i = 0; i < w.n; ++i, ++done) {
+        bar_wait(bar(kBarS + t), done & 1, stop, limit_ns, 4u);
+        fence_after();
+        const int key0 = w.t.kr.key0(w.s + i, kKeys);
         const bool all = key0 + kKeys <= hi && (key0 >= lo || key0 + kKeys <= a.sinks);
-        if (!__all_sync(0xffffffffu, all)) {
-          const int h = hi - key0, w0 = lo - key0, sk = a.sinks - key0;
+        const bool masked = !__all_sync(0xffffffffu, all);
+        const int h = hi - key0, w0 = lo - key0, sk = a.sinks - key0;
+        // The weights are taken against the maximum known before this step, and
+        // the row's own maximum is found beside them: only if it is more than
+        // 2^8 above (hardly ever after the first step) is the first half done again.
+        uint32_t s[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tm_load(s[c], s_at + 32 * c);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) wait_ld(s[c]);
+        if (masked) {
 #pragma unroll
           for (int c = 0; c < 128; ++c)
-            if (!(c < h && (c >= w0 || c < sk))) s[c] = 0xFF800000u;
+            if (!(c < h && (c >= w0 || c < sk))) s[c >> 5][c & 31] = 0xFF800000u;
         }
-        float mx[4];
+        float2 mb2, sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+        uint32_t p[32];
+        float2 x[2 * kAhead];
+        // A half row, as 32 pairs: the multiply-add runs kAhead pairs ahead of
+        // exp2, the sum and the rounding kAhead behind it, so that no pipe waits.
+        auto half = [&](int first, auto also) {
+          auto scaled = [&](int k) {
+            const uint32_t* y = &s[(first + k) >> 4][2 * ((first + k) & 15)];
+            x[k % (2 * kAhead)] = fma2(make_float2(__uint_as_float(y[0]), __uint_as_float(y[1])), sc2, mb2);
+          };
+          auto weighed = [&](int k) {
+            const float2 y = x[k % (2 * kAhead)];
+            sum[k & 1] = __fadd2_rn(sum[k & 1], y);
+            p[k] = pack2<BF16>(y.x, y.y);
+          };
 #pragma unroll
-        for (int c = 0; c < 4; ++c) mx[c] = __uint_as_float(s[c]);
+          for (int k = 0; k < kAhead; ++k) scaled(k);
 #pragma unroll
-        for (int c = 4; c < 128; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(s[c]));
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+          for (int k = 0; k < 32; ++k) {
+            float2& y = x[k % (2 * kAhead)];
+            y.x = exp2_fast(y.x);
+            y.y = exp2_fast(y.y);
+            also(k);
+            if (k >= kAhead) weighed(k - kAhead);
+            if (k + kAhead < 32) scaled(k + kAhead);
+          }
+#pragma unroll
+          for (int k = 32 - kAhead; k < 32; ++k) weighed(k);
+        };
+        auto hand_over = [&](int which) {
+          tm_store32(s_at + 32 * which, p);  // in the scores' place: they are all read
+          wait_st();
+          fence_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive(bar(kBarP + 2 * t + which));
+        };
+        auto start = [&]() {
+          const float mb = m == kNegInf ? 0.0f : -m;
+          mb2 = make_float2(mb, mb);
+          sum[0] = sum[1] = make_float2(0.0f, 0.0f);
+        };
+        float mx[2] = {kNegInf, kNegInf};
+        start();
+        half(0, [&](int k) {
+          mx[0] = max3(mx[0], __uint_as_float(s[k >> 3][(4 * k) & 31]), __uint_as_float(s[k >> 3][(4 * k + 1) & 31]));
+          mx[1] = max3(mx[1], __uint_as_float(s[k >> 3][(4 * k + 2) & 31]), __uint_as_float(s[k >> 3][(4 * k + 3) & 31]));
+        });
+        const float top = fmaxf(mx[0], mx[1]) * scale;
         if (__any_sync(0xffffffffu, top > m + kLazy)) {
           const float mn = fmaxf(m, top);
           const float f = mn == kNegInf ? 1.0f : exp2_fast(m - mn);
@@ -454,86 +728,130 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (i > 0) {
 #pragma unroll
             for (int c = 0; c < DP / 32; ++c) {
-              uint32_t o[32];
-              tm_load(o, o_at + 32 * c);
-              wait_ld();
+              tm_load(p, o_at + 32 * c);
+              wait_ld(p);
 #pragma unroll
-              for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-              tm_store32(o_at + 32 * c, o);
+              for (int k = 0; k < 32; ++k) p[k] = __float_as_uint(__uint_as_float(p[k]) * f);
+              tm_store32(o_at + 32 * c, p);
             }
           }
+          start();
+          half(0, [](int) {});
         }
-        const float mb = m == kNegInf ? 0.0f : -m;
-        const float2 sc2 = make_float2(scale, scale), mb2 = make_float2(mb, mb);
-        float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t p[16];
-#pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            float2 x = make_float2(__uint_as_float(s[32 * c + 2 * k]), __uint_as_float(s[32 * c + 2 * k + 1]));
-            x = fma2(x, sc2, mb2);
-            x.x = exp2_fast(x.x);
-            x.y = exp2_fast(x.y);
-            sum[k & 1] = __fadd2_rn(sum[k & 1], x);
-            p[k] = pack2<BF16>(x.x, x.y);
-          }
-          tm_store16(s_at + 16 * c, p);
-        }
+        hand_over(0);
+        half(32, [](int) {});
+        hand_over(1);
         l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-        wait_st();
-        fence_before();
-        bar_arrive(bar(kBarP + t));
       }
-      if (ok && n > 0) {
-        ok = __all_sync(0xffffffffu, bar_wait(bar(kBarO), 0, stop, limit_ns, 4u));
-        fence_after();
-      }
-      if (ok) {
-        const int64_t row = seq.row0 + static_cast<int64_t>(tok);
-        const int64_t part = (row * a.q_heads + hq) * a.splits + split;
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+      // The next run's scores are computed while this one's results are written.
+      go = after.next(a, tiles);
+      if (go) load_queries(after);
+      w = after;
+      bar_wait(bar(kBarO + t), runs & 1, stop, limit_ns, 4u);
+      fence_after();
+      ++runs;
+      if (__any_sync(0xffffffffu, lds_flag(stop))) break;
+      const int64_t row = seq.row0 + static_cast<int64_t>(tok);
+      const int64_t part = static_cast<int64_t>(slot) * kRowsCta + 128 * t + wt;
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-        for (int c = 0; c < DP / 32; ++c) {
-          uint32_t o[32];
-          __syncwarp();
-          if (n > 0) {
-            tm_load(o, o_at + 32 * c);
-            wait_ld();
-          }
-          if (l == 0.0f) {  // sees nothing, here or at all
+      for (int c = 0; c < DP / 32; ++c) {
+        uint32_t o[32];
+        __syncwarp();
+        tm_load(o, o_at + 32 * c);
+        wait_ld(o);
+        if (l == 0.0f) {  // sees nothing, here or at all
 #pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] = 0u;
-          }
-          if (in) {
-            if (a.splits > 1) {
+          for (int k = 0; k < 32; ++k) o[k] = 0u;
+        }
+        if (in) {
+          if (partial) {
 #pragma unroll
-              for (int k = 0; k < 32; k += 4)
-                if (32 * c + k < a.p.dim)
-                  *reinterpret_cast<uint4*>(a.part_o + part * a.p.dim + 32 * c + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-            } else {
+            for (int k = 0; k < 32; k += 4)
+              if (32 * c + k < a.p.dim)
+                *reinterpret_cast<uint4*>(a.part_o + part * a.p.dim + 32 * c + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+          } else {
 #pragma unroll
-              for (int k = 0; k < 32; k += 8)
-                if (32 * c + k < a.p.dim) {
-                  uint32_t w[4];
+            for (int k = 0; k < 32; k += 8)
+              if (32 * c + k < a.p.dim) {
+                uint32_t y[4];
 #pragma unroll
-                  for (int x = 0; x < 4; ++x)
-                    w[x] = pack2<true>(__uint_as_float(o[k + 2 * x]) * inv, __uint_as_float(o[k + 2 * x + 1]) * inv);
-                  *reinterpret_cast<uint4*>(a.out + row * a.out_row + hq * a.out_head + 32 * c + k) = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-            }
+                for (int x = 0; x < 4; ++x)
+                  y[x] = pack2<true>(__uint_as_float(o[k + 2 * x]) * inv, __uint_as_float(o[k + 2 * x + 1]) * inv);
+                *reinterpret_cast<uint4*>(a.out + row * a.out_row + hq * a.out_head + 32 * c + k) = make_uint4(y[0], y[1], y[2], y[3]);
+              }
           }
         }
-        __syncwarp();
-        if (in && a.splits > 1) a.part_ml[part] = make_float2(m, l);
-        if (in && a.splits == 1 && a.lse) a.lse[row * a.q_heads + hq] = l == 0.0f ? kNegInf : (m + log2f(l)) * 0.6931471805599453f;
       }
+      __syncwarp();
+      if (in && partial) a.part_ml[part] = make_float2(m, l);
+      if (in && !partial && a.lse) a.lse[row * a.q_heads + hq] = l == 0.0f ? kNegInf : (m + log2f(l)) * 0.6931471805599453f;
+    }
+    if (threadIdx.x == 0) {
+      if (!(slots & 1)) a.part_rec[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
+      if (!(slots & 2)) a.part_rec[2 * blockIdx.x + 1] = make_int4(0, 0, 0, 0);
     }
   }
+  pdl_trigger();
   fence_before();
   __syncthreads();
   fence_after();
   if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+}
+
+// Joins the partial results of the tiles that several blocks shared. The block
+// where a tile starts holds its first part, the following blocks' first runs the
+// others. A warp takes a query row, 4 channels per lane.
+__global__ void __launch_bounds__(128) attend_tiles_join_kernel(AttendArgs a, int tiles, int blocks) {
+  pdl_wait();
+  const int slot = blockIdx.x, lane = threadIdx.x & 31;
+  const int4 rec = a.part_rec[slot];
+  if (!rec.x || !(rec.w & 1)) return;
+  const Tile x = tile_of(a, tiles, rec.y);
+  const int head = rec.z, c = lane * 4;
+  for (int r = blockIdx.y * 4 + (threadIdx.x >> 5); r < x.n_rows; r += gridDim.y * 4) {
+    float top = kNegInf, sum = 0.0f;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    bool more = true;
+    for (int i0 = 0; more; i0 += 32) {  // 32 parts at a time
+      const int i = i0 + lane, blk = (slot >> 1) + i;
+      const int at = i == 0 ? slot : 2 * blk;
+      const bool there = i == 0 || blk < blocks;
+      const uint32_t last = __ballot_sync(0xffffffffu, !there || (a.part_rec[at].w & 2));
+      const int n = last ? __ffs(last) : 32;
+      more = last == 0;
+      const float2 ml = lane < n && there ? a.part_ml[static_cast<int64_t>(at) * kRowsCta + r] : make_float2(kNegInf, 0.0f);
+      float mx = ml.x;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+      mx = fmaxf(mx, top);
+      const float base = mx == kNegInf ? 0.0f : mx;
+      const float f0 = exp2_fast(top - base), f = exp2_fast(ml.x - base);
+      top = mx;
+      float part = f * ml.y;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
+      sum = sum * f0 + part;
+      acc.x *= f0, acc.y *= f0, acc.z *= f0, acc.w *= f0;
+#pragma unroll 4
+      for (int s = 0; s < n; ++s) {
+        const float wgt = __shfl_sync(0xffffffffu, f, s);
+        const int as = __shfl_sync(0xffffffffu, at, s);
+        if (c < a.p.dim) {
+          const float4 y = *reinterpret_cast<const float4*>(a.part_o + (static_cast<int64_t>(as) * kRowsCta + r) * a.p.dim + c);
+          acc.x += wgt * y.x, acc.y += wgt * y.y, acc.z += wgt * y.z, acc.w += wgt * y.w;
+        }
+      }
+    }
+    const int tok = (x.row0 + r) / a.share, hq = head * a.share + x.row0 + r - tok * a.share;
+    const int64_t row = x.seq.row0 + static_cast<int64_t>(tok);
+    if (sum == 0.0f) acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // sees nothing
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    if (c < a.p.dim)
+      *reinterpret_cast<uint2*>(a.out + row * a.out_row + hq * a.out_head + c) =
+          make_uint2(pack2<true>(acc.x * inv, acc.y * inv), pack2<true>(acc.z * inv, acc.w * inv));
+    if (lane == 0 && a.lse) a.lse[row * a.q_heads + hq] = sum == 0.0f ? kNegInf : (top + log2f(sum)) * 0.6931471805599453f;
+  }
 }
 
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -563,9 +881,9 @@ cudaError_t prepare_one() {
 }
 
 template <bool BF16, int DP>
-cudaError_t launch_one(const AttendArgs& a, const CUtensorMap& km, const CUtensorMap& vm, int box_rows, int64_t limit_ns, dim3 grid,
-                       cudaStream_t st) {
-  attend_tiles_kernel<BF16, DP><<<grid, kThreads, Layout<DP>::kBytes, st>>>(a, km, vm, box_rows, limit_ns);
+cudaError_t launch_one(const AttendArgs& a, const CUtensorMap& km, const CUtensorMap& vm, int tiles, int box_rows, int64_t limit_ns,
+                       unsigned grid, cudaStream_t st) {
+  attend_tiles_kernel<BF16, DP><<<grid, kThreads, Layout<DP>::kBytes, st>>>(a, km, vm, tiles, box_rows, limit_ns);
   return cudaGetLastError();
 }
 
@@ -594,16 +912,28 @@ bool attend_tiles_maps(const AttendArgs& a, bool bf16, TileMaps* maps) {
          encode(reinterpret_cast<CUtensorMap*>(maps->v), a.p, a.p.v, bf16, maps->box_rows);
 }
 
-cudaError_t launch_attend_tiles(const AttendArgs& a, bool bf16, const TileMaps& maps, int64_t limit_ns, cudaStream_t st) {
+cudaError_t launch_attend_tiles(const AttendArgs& a, bool bf16, const TileMaps& maps, int blocks, int64_t limit_ns, cudaStream_t st) {
   const int tiles = static_cast<int>((static_cast<int64_t>(a.p.max_rows) * a.share + kRowsCta - 1) / kRowsCta);
-  const dim3 grid(static_cast<unsigned>(a.splits) * tiles, static_cast<unsigned>(a.p.heads), static_cast<unsigned>(a.p.n_seqs));
   const CUtensorMap& km = *reinterpret_cast<const CUtensorMap*>(maps.k);
   const CUtensorMap& vm = *reinterpret_cast<const CUtensorMap*>(maps.v);
+  cudaError_t e;
   if (a.p.dim <= 64)
-    return bf16 ? launch_one<true, 64>(a, km, vm, maps.box_rows, limit_ns, grid, st)
-                : launch_one<false, 64>(a, km, vm, maps.box_rows, limit_ns, grid, st);
-  return bf16 ? launch_one<true, 128>(a, km, vm, maps.box_rows, limit_ns, grid, st)
-              : launch_one<false, 128>(a, km, vm, maps.box_rows, limit_ns, grid, st);
+    e = bf16 ? launch_one<true, 64>(a, km, vm, tiles, maps.box_rows, limit_ns, blocks, st)
+             : launch_one<false, 64>(a, km, vm, tiles, maps.box_rows, limit_ns, blocks, st);
+  else
+    e = bf16 ? launch_one<true, 128>(a, km, vm, tiles, maps.box_rows, limit_ns, blocks, st)
+             : launch_one<false, 128>(a, km, vm, tiles, maps.box_rows, limit_ns, blocks, st);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * static_cast<unsigned>(blocks), 64);
+  cfg.blockDim = dim3(128);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, attend_tiles_join_kernel, a, tiles, blocks);
 }
 
 cudaError_t attend_tiles_error(unsigned* bits) {

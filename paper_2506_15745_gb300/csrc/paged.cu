@@ -162,6 +162,8 @@ ipv_status check_attend(const ipv_pages* p, const ipv_batch* b, const ipv_attend
   if (t->window > 0 && !t->causal) return reject(IPV_EINVAL, "a window needs causal = 1");
   if (static_cast<int64_t>(a->p.max_rows) * t->n_q_heads > INT32_MAX)
     return reject(IPV_EINVAL, "max_rows * n_q_heads exceeds 2^31 - 1");
+  const int64_t tiles = (static_cast<int64_t>(a->p.max_rows) * (t->n_q_heads / p->n_kv_heads) + ipv::kTilesRows - 1) / ipv::kTilesRows;
+  if (tiles * a->p.n_seqs > INT32_MAX) return reject(IPV_EINVAL, "n_seqs times the query tiles of max_rows exceeds 2^31 - 1");
   a->q_heads = t->n_q_heads;
   a->share = t->n_q_heads / p->n_kv_heads;
   a->scale_log2 = t->scale * 1.4426950408889634f;
@@ -179,13 +181,15 @@ std::atomic<int64_t> g_limit_ns{kDefaultLimitNs};
 // kernel reads K and V once per 16 query rows.
 constexpr int64_t kTilesFrom = 17;
 
-// Which kernel takes the call, its split of the keys, and the workspace. Each
-// split costs a partial result, written and read again, so there are as many
-// as fill the device.
+// Fewest steps of a block's share in the tiled kernel.
+constexpr int kTilesLeast = 2;
+
+// Which kernel takes the call, its split of the keys, and the workspace.
 struct Plan {
   bool tiles = false;
-  ipv::TileMaps maps;  // tiles: made only when launching
-  int64_t k16 = 0, v16 = 0, part_o = 0, part_ml = 0, bytes = 0;  // offsets in the workspace
+  int blocks = 0;      // tiled kernel
+  ipv::TileMaps maps;  // tiled kernel: made only when launching
+  int64_t k16 = 0, v16 = 0, part_o = 0, part_ml = 0, part_rec = 0, bytes = 0;  // offsets in the workspace
 };
 
 int64_t round256(int64_t x) { return (x + 255) & ~int64_t{255}; }
@@ -195,45 +199,48 @@ void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
   const ipv::Pages& p = a->p;
   const int64_t rows = static_cast<int64_t>(p.max_rows) * a->share;
   plan->tiles = rows >= kTilesFrom;
-  int64_t slots, least;
+  plan->bytes = 0;
+  int64_t parts = 0;
   if (plan->tiles) {
     a->step = ipv::kTilesStep;
     a->tile = ipv::kTilesRows;
-    slots = num_sms;
-    least = 2;
+    a->unit = kTilesLeast;
+    a->splits = 1;
+    plan->blocks = num_sms;
+    if (p.fmt != ipv::kBf16) {
+      const int64_t one = round256(static_cast<int64_t>(p.n_seqs) * p.heads * p.max_kv * p.dim * 2);
+      plan->k16 = 0;
+      plan->v16 = one;
+      plan->bytes = 2 * one;
+    }
+    parts = static_cast<int64_t>(plan->blocks) * 2 * ipv::kTilesRows;
   } else {
+    // Each split costs a partial result, written and read again: as many as fill the device.
     a->step = ipv::kRowsStep;
     a->tile = ipv::attend_rows_tile(static_cast<int>(rows));
-    slots = static_cast<int64_t>(num_sms) * ipv::attend_rows_ctas(p.fmt, p.dim) * (p.n_seqs > 1 ? 2 : 1);
-    least = ipv::kRowsWarps;
+    const int64_t slots = static_cast<int64_t>(num_sms) * ipv::attend_rows_ctas(p.fmt, p.dim) * (p.n_seqs > 1 ? 2 : 1);
+    const int64_t tiles = (rows + a->tile - 1) / a->tile;
+    int64_t span = p.max_kv;
+    if (a->window) {  // the tile's tokens' windows, the sinks, and a step's slack at each of the three ends
+      const int64_t seen = static_cast<int64_t>(a->window) + a->tile + a->sinks + 3 * a->step;
+      if (seen < span) span = seen;
+    }
+    const int64_t steps = (span + a->step - 1) / a->step;
+    const int64_t blocks = tiles * p.heads * p.n_seqs;
+    int64_t want = slots / blocks;
+    if (want < 1) want = 1;
+    int64_t unit = (steps + want - 1) / want;
+    unit = (unit + ipv::kRowsWarps - 1) / ipv::kRowsWarps * ipv::kRowsWarps;
+    if (unit < ipv::kRowsWarps) unit = ipv::kRowsWarps;
+    a->unit = static_cast<int>(unit);
+    a->splits = static_cast<int>(steps > 0 ? (steps + unit - 1) / unit : 1);
+    if (a->splits > 1) parts = p.total_rows * a->q_heads * a->splits;
   }
-  const int64_t tiles = (rows + a->tile - 1) / a->tile;
-  int64_t span = p.max_kv;
-  if (a->window) {  // the tile's tokens' windows, the sinks, and a step's slack at each of the three ends
-    const int64_t seen = static_cast<int64_t>(a->window) + a->tile + a->sinks + 3 * a->step;
-    if (seen < span) span = seen;
-  }
-  const int64_t steps = (span + a->step - 1) / a->step;
-  const int64_t blocks = tiles * p.heads * p.n_seqs;
-  int64_t want = slots / blocks;
-  if (want < 1) want = 1;
-  int64_t unit = (steps + want - 1) / want;
-  if (!plan->tiles) unit = (unit + ipv::kRowsWarps - 1) / ipv::kRowsWarps * ipv::kRowsWarps;
-  if (unit < least) unit = least;
-  a->unit = static_cast<int>(unit);
-  a->splits = static_cast<int>(steps > 0 ? (steps + unit - 1) / unit : 1);
-  plan->bytes = 0;
-  if (plan->tiles && p.fmt != ipv::kBf16) {
-    const int64_t one = round256(static_cast<int64_t>(p.n_seqs) * p.heads * p.max_kv * p.dim * 2);
-    plan->k16 = 0;
-    plan->v16 = one;
-    plan->bytes = 2 * one;
-  }
-  if (a->splits > 1) {
-    const int64_t n = p.total_rows * a->q_heads * a->splits;
+  if (parts > 0) {
     plan->part_o = plan->bytes;
-    plan->part_ml = plan->part_o + round256(n * p.dim * 4);
-    plan->bytes = plan->part_ml + round256(n * 8);
+    plan->part_ml = plan->part_o + round256(parts * p.dim * 4);
+    plan->part_rec = plan->part_ml + round256(parts * 8);
+    plan->bytes = plan->part_rec + (plan->tiles ? round256(static_cast<int64_t>(plan->blocks) * 2 * 16) : 0);
   }
 }
 
@@ -340,6 +347,7 @@ extern "C" ipv_status ipv_attend(const ipv_pages* pages, const ipv_batch* batch,
   char* ws = static_cast<char*>(args->workspace);
   a.part_o = reinterpret_cast<float*>(ws + plan.part_o);
   a.part_ml = reinterpret_cast<float2*>(ws + plan.part_ml);
+  a.part_rec = reinterpret_cast<int4*>(ws + plan.part_rec);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e;
   if (plan.tiles) {
@@ -357,7 +365,7 @@ extern "C" ipv_status ipv_attend(const ipv_pages* pages, const ipv_batch* batch,
       a.p = widened(a.p, ws + plan.k16, ws + plan.v16);
     }
     if (!ipv::attend_tiles_maps(a, bf16, &plan.maps)) return reject(IPV_ECUDA, "cuTensorMapEncodeTiled refused the pool");
-    e = ipv::launch_attend_tiles(a, bf16, plan.maps, g_limit_ns.load(), st);
+    e = ipv::launch_attend_tiles(a, bf16, plan.maps, plan.blocks, g_limit_ns.load(), st);
   } else {
     e = ipv::launch_attend_rows(a, st);
   }

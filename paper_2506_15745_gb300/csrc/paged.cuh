@@ -72,11 +72,17 @@ struct AttendArgs {
   int q_heads, share;   // query heads; query heads per KV head
   float scale_log2;     // scale * log2(e)
   int causal, window, sinks;
-  // Keys are split: a split is at most `unit` steps of `step` keys.
-  int step, unit, splits;  // splits: most that any row tile has
+  // Keys are split: into at most `unit` steps of `step` keys (rows kernel), or
+  // where a block's share of the steps, at least `unit`, ends (tiled kernel).
+  int step, unit, splits;  // splits: most that any row tile has (rows kernel)
   int tile;                // query rows of a row tile
-  float* part_o;    // [total_rows * q_heads][splits][dim] unnormalised sums
-  float2* part_ml;  // [total_rows * q_heads][splits] (running maximum, sum)
+  // Partial results: unnormalised sums [..][dim] and (running maximum, sum)
+  // [..], of [total_rows * q_heads][splits] (rows kernel) or of
+  // [blocks][2][kTilesRows] with a record each [blocks][2] (tiled kernel):
+  // (1 or 0: none, pair of sequence and tile, KV head, 1: a tile's start + 2: its end).
+  float* part_o;
+  float2* part_ml;
+  int4* part_rec;
 };
 
 // The steps of keys that query rows of tokens tok0..tok1 can see: steps
@@ -145,7 +151,7 @@ cudaError_t launch_attend_rows(const AttendArgs& a, cudaStream_t st);
 cudaError_t launch_attend_combine(const AttendArgs& a, cudaStream_t st);
 
 // Many query rows (attend_tiles.cu): the pool's rows are 16-bit elements.
-constexpr int kTilesRows = 256;  // query rows of a block
+constexpr int kTilesRows = 256;  // query rows of a tile of work
 constexpr int kTilesStep = 128;  // keys of a step
 struct alignas(128) TileMaps {    // the pool as TMA sees it
   unsigned char k[128], v[128];
@@ -153,7 +159,7 @@ struct alignas(128) TileMaps {    // the pool as TMA sees it
 };
 cudaError_t attend_tiles_prepare();  // once per device
 bool attend_tiles_maps(const AttendArgs& a, bool bf16, TileMaps* maps);
-cudaError_t launch_attend_tiles(const AttendArgs& a, bool bf16, const TileMaps& maps, int64_t limit_ns, cudaStream_t st);
+cudaError_t launch_attend_tiles(const AttendArgs& a, bool bf16, const TileMaps& maps, int blocks, int64_t limit_ns, cudaStream_t st);
 cudaError_t attend_tiles_error(unsigned* bits);
 
 }  // namespace ipv
