@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
   const int row0 = tile * (8 * NR);
   if (row0 >= rows) return;
   const int row1 = min(row0 + 8 * NR, rows) - 1;
-  const KeyRange kr = key_range(a, seq, row0 / a.share, row1 / a.share);
+  const KeyRange kr = key_range<kRowsStep>(a, seq, a.by_share(row0), a.by_share(row1));
   const int ns = splits_of(a, kr);
   if (split >= ns) return;
   const int s_begin = split * a.unit, s_end = min(kr.steps, s_begin + a.unit);
@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
   // ---- copies of one step into one stage (this warp's lanes only)
   auto issue = [&](int i, int stage) {
     const uint32_t base = ring + stage * R::kStage;
-    const int j = kr.key0(i, kRowsStep) + lane;
+    const int j = kr.key0<kRowsStep>(i) + lane;
     int64_t row = -1;
     if (j < kr.hi_max) {
       row = pool_row(a.p, b, j);
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
   for (int nr = 0; nr < NR; ++nr) {
     const int r = row0 + nr * 8 + g;
     const bool in = r <= row1;
-    const int tok = (in ? r : row0) / a.share, hq = (in ? r : row0) - tok * a.share;
+    const int tok = a.by_share(in ? r : row0), hq = (in ? r : row0) - tok * a.share;
     const uint16_t* qp = a.q + (seq.row0 + static_cast<int64_t>(tok)) * a.q_row + (head * a.share + hq) * a.q_head;
     if constexpr (kB) {
 #pragma unroll
@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int r = row0 + nr * 8 + 2 * t + i;
-      hi[nr][i] = r <= row1 ? token_hi(a, seq, r / a.share) : 0;
+      hi[nr][i] = r <= row1 ? token_hi(a, seq, a.by_share(r)) : 0;
     }
 
   float o[kCt][NR][4];
@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
     __syncwarp();
     const uint32_t ks_at = ring + stage * R::kStage, vs_at = ks_at + R::kTile;
     const uint32_t kp_at = ks_at + 2 * R::kTile, vp_at = kp_at + R::kPar;
-    const int key0 = kr.key0(step, kRowsStep);
+    const int key0 = kr.key0<kRowsStep>(step);
 
     float sc[2][NR][4];
     // S^T: 2 tiles of 16 keys
@@ -579,7 +579,7 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
       const float4 x = *reinterpret_cast<const float4*>(so + (w * kRows + r) * kPitch + c);
       acc.x += f * x.x, acc.y += f * x.y, acc.z += f * x.z, acc.w += f * x.w;
     }
-    const int tok = (row0 + r) / a.share, hq = head * a.share + (row0 + r) - tok * a.share;
+    const int tok = a.by_share(row0 + r), hq = head * a.share + (row0 + r) - tok * a.share;
     const int64_t row = seq.row0 + static_cast<int64_t>(tok);
     if (a.splits > 1) {
       const int64_t at = (row * a.q_heads + hq) * a.splits + split;
@@ -603,15 +603,15 @@ __global__ void __launch_bounds__(128) attend_combine_kernel(AttendArgs a) {
   const int b = blockIdx.y;
   const Seq seq = sequence(a.p, b);
   const int item = blockIdx.x * 4 + (threadIdx.x >> 5);
-  const int tok = item / a.q_heads, hq = item - tok * a.q_heads;
+  const int tok = a.by_q_heads(item), hq = item - tok * a.q_heads;
   if (tok >= seq.n) {
     pdl_wait();  // no block of this kernel ends before the one it joins
     return;
   }
   // The row tile that the row was computed in
-  const int h = hq / a.share, r = tok * a.share + hq - h * a.share;
-  const int row0 = r / a.tile * a.tile, row1 = min(row0 + a.tile, seq.n * a.share) - 1;
-  const int ns = splits_of(a, key_range(a, seq, row0 / a.share, row1 / a.share));
+  const int h = a.by_share(hq), r = tok * a.share + hq - h * a.share;
+  const int row0 = r & ~(a.tile - 1), row1 = min(row0 + a.tile, seq.n * a.share) - 1;
+  const int ns = splits_of(a, key_range<kRowsStep>(a, seq, a.by_share(row0), a.by_share(row1)));
   const int64_t row = seq.row0 + static_cast<int64_t>(tok);
   const int64_t at = (row * a.q_heads + hq) * a.splits;
   pdl_wait();

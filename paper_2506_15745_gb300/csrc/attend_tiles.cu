@@ -45,6 +45,9 @@ constexpr float kNegInf = -INFINITY;
 constexpr float kLazy = 8.0f;         // log2 of the growth that rescales O
 constexpr int kAhead = 4;             // pairs between the softmax's pipes
 
+// A warp's results: 32 rows of 32 channels, 16 bytes apart from a multiple of 128.
+constexpr int kOutRow = 80, kOutWarp = 32 * kOutRow;
+
 template <int DP>
 struct Layout {
   static constexpr int kHalves = DP / 64;
@@ -55,7 +58,8 @@ struct Layout {
   static constexpr int kV = kK + kStages * kTile;
   static constexpr int kBars = kV + kStages * kTile;
   static constexpr int kScale = kBars + 512;             // 256 floats
-  static constexpr int kBytes = kScale + 1024 + 1024;    // + alignment of the base
+  static constexpr int kOut = kScale + 1024;             // results on their way out
+  static constexpr int kBytes = kOut + 8 * kOutWarp + 1024;  // + alignment of the base
 };
 
 // Barriers, 8 bytes each.
@@ -223,6 +227,14 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ void sts128(uint32_t at, const uint32_t (&v)[4]) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float y;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
@@ -259,13 +271,13 @@ __device__ __forceinline__ void set_tile(const AttendArgs& a, Tile& x, int b, in
   x.b = b;
   x.steps = 0;
   if (x.n_rows > 0) {
-    x.kr = key_range(a, x.seq, x.row0 / a.share, (x.row0 + x.n_rows - 1) / a.share);
+    x.kr = key_range<kKeys>(a, x.seq, a.by_share(x.row0), a.by_share(x.row0 + x.n_rows - 1));
     x.steps = max(1, x.kr.steps);  // rows that see nothing have their results to write, too
   }
 }
 __device__ __forceinline__ Tile tile_of(const AttendArgs& a, int tiles, int p) {
   Tile x;
-  const int b = p / tiles;
+  const int b = a.by_tiles(p);
   x.seq = sequence(a.p, b);
   set_tile(a, x, b, p - b * tiles);
   return x;
@@ -323,8 +335,14 @@ struct Walk {
   __device__ __forceinline__ bool ends() const { return s + n == t.steps; }
   __device__ __forceinline__ int pair(int tiles) const { return t.b * tiles + t.row0 / kRowsCta; }
   // Rows of the last V tile from `keep` on lie past the last key.
-  __device__ __forceinline__ int keep() const { return t.kr.hi_max - t.kr.key0(s + n - 1, kKeys); }
+  __device__ __forceinline__ int keep() const { return t.kr.hi_max - t.kr.key0<kKeys>(s + n - 1); }
 };
+
+// 64-bit numbers that mostly fit 32 bits.
+__device__ __forceinline__ int64_t divide(int64_t x, int64_t d) {
+  if (static_cast<uint64_t>(x | d) >> 32 == 0) return static_cast<uint32_t>(x) / static_cast<uint32_t>(d);
+  return x / d;
+}
 
 // Finds the block's share, with all threads; scratch: 16 64-bit words of shared memory.
 __device__ Share find_share(const AttendArgs& a, int tiles, int64_t* scratch) {
@@ -344,7 +362,7 @@ __device__ Share find_share(const AttendArgs& a, int tiles, int64_t* scratch) {
   int64_t total = 0;
 #pragma unroll
   for (int i = 0; i < kWarps; ++i) total += scratch[i];
-  int64_t per = (total + gridDim.x - 1) / gridDim.x;
+  int64_t per = divide(total + gridDim.x - 1, gridDim.x);
   if (per < a.unit + kRunCost) per = a.unit + kRunCost;
   const int64_t from = per * blockIdx.x;
   Share w;
@@ -372,10 +390,10 @@ __device__ Share find_share(const AttendArgs& a, int tiles, int64_t* scratch) {
     }
     start += upto - mine;
     if (from >= start && from < start + mine) {
-      const int64_t one = mine / a.p.heads;
+      const int64_t one = divide(mine, a.p.heads), head = divide(from - start, one);
       scratch[kWarps] = p0 + threadIdx.x;
-      scratch[kWarps + 1] = (from - start) / one;
-      scratch[kWarps + 2] = (from - start) % one;
+      scratch[kWarps + 1] = head;
+      scratch[kWarps + 2] = from - start - head * one;
     }
     __syncthreads();
     if (from < all) break;
@@ -437,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       int it = 0, k_out = 0, v_out = 0;  // steps; K and V tiles asked for
       // This lane's piece of step i: its page and the row there, page < 0: none.
       auto piece = [&](int i, int& page, int& row) {
-        const int j = w.t.kr.key0(w.s + i, kKeys) + lane * box_rows;
+        const int j = w.t.kr.key0<kKeys>(w.s + i) + lane * box_rows;
         page = -1;
         row = 0;
         if (lane >= pieces || j >= w.t.kr.hi_max) return;
@@ -579,7 +597,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       constexpr int kCh = DP / 8, kBatch = 8;
       const int row0 = x.t.row0 + 128 * t, n_rows = x.t.n_rows - 128 * t;
       // The lane's first row and channel; the others follow 32 / kCh rows apart.
-      int tok = (row0 + 32 * (warp & 3) + lane / kCh) / a.share;
+      int tok = a.by_share(row0 + 32 * (warp & 3) + lane / kCh);
       int hq = row0 + 32 * (warp & 3) + lane / kCh - tok * a.share;
 #pragma unroll 1
       for (int x0 = lane; x0 < 32 * kCh; x0 += 32 * kBatch) {
@@ -642,11 +660,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         w = after;
         continue;
       }
-      const Seq seq = w.t.seq;
       const int row0 = w.t.row0 + 128 * t, n_rows = min(128, w.t.n_rows - 128 * t), head = w.head;
       const bool in = wt < n_rows;
-      const int tok = in ? (row0 + wt) / a.share : 0, hq = in ? head * a.share + row0 + wt - tok * a.share : 0;
-      const int hi = in ? token_hi(a, seq, tok) : 0x7FFFFFFF;  // rows that are not there need no mask
+      const int hi = in ? token_hi(a, w.t.seq, a.by_share(row0 + wt)) : 0x7FFFFFFF;  // rows that are not there need no mask
       const int lo = in && a.window ? max(0, hi - a.window) : 0;
       // Not 0, which would make a masked score (-inf) NaN.
       const float scale = fmaxf(BF16 ? fabsf(a.scale_log2) : row_scale[128 * t + wt], 1.17549435e-38f);
@@ -655,7 +671,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int i = 0; i < w.n; ++i, ++done) {
         bar_wait(bar(kBarS + t), done & 1, stop, limit_ns, 4u);
         fence_after();
-        const int key0 = w.t.kr.key0(w.s + i, kKeys);
+        const int key0 = w.t.kr.key0<kKeys>(w.s + i);
         const bool all = key0 + kKeys <= hi && (key0 >= lo || key0 + kKeys <= a.sinks);
         const bool masked = !__all_sync(0xffffffffu, all);
         const int h = hi - key0, w0 = lo - key0, sk = a.sinks - key0;
@@ -743,6 +759,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         hand_over(1);
         l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       }
+      const int tok = in ? a.by_share(row0 + wt) : 0, hq = in ? head * a.share + row0 + wt - tok * a.share : 0;
+      const int64_t row = w.t.seq.row0 + static_cast<int64_t>(tok);
       // The next run's scores are computed while this one's results are written.
       go = after.next(a, tiles);
       if (go) load_queries(after);
@@ -751,36 +769,46 @@ __global__ void __launch_bounds__(kThreads, 1)
       fence_after();
       ++runs;
       if (__any_sync(0xffffffffu, lds_flag(stop))) break;
-      const int64_t row = seq.row0 + static_cast<int64_t>(tok);
-      const int64_t part = static_cast<int64_t>(slot) * kRowsCta + 128 * t + wt;
+      const int64_t part = static_cast<int64_t>(slot) * kRowsCta + 128 * t + wt, out_at = row * a.out_row + hq * a.out_head;
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
       for (int c = 0; c < DP / 32; ++c) {
         uint32_t o[32];
-        __syncwarp();
         tm_load(o, o_at + 32 * c);
         wait_ld(o);
         if (l == 0.0f) {  // sees nothing, here or at all
 #pragma unroll
           for (int k = 0; k < 32; ++k) o[k] = 0u;
         }
-        if (in) {
-          if (partial) {
+        if (partial) {
+          // 4 channels of the warp's 32 rows lie next to each other.
+          if (in) {
 #pragma unroll
             for (int k = 0; k < 32; k += 4)
               if (32 * c + k < a.p.dim)
-                *reinterpret_cast<uint4*>(a.part_o + part * a.p.dim + 32 * c + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-          } else {
-#pragma unroll
-            for (int k = 0; k < 32; k += 8)
-              if (32 * c + k < a.p.dim) {
-                uint32_t y[4];
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-                  y[x] = pack2<true>(__uint_as_float(o[k + 2 * x]) * inv, __uint_as_float(o[k + 2 * x + 1]) * inv);
-                *reinterpret_cast<uint4*>(a.out + row * a.out_row + hq * a.out_head + 32 * c + k) = make_uint4(y[0], y[1], y[2], y[3]);
-              }
+                *reinterpret_cast<uint4*>(a.part_o + ((static_cast<int64_t>(slot) * (a.p.dim / 4) + 8 * c + k / 4) * kRowsCta + 128 * t + wt) * 4) =
+                    make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
           }
+        } else {
+          // Through shared memory, so that 4 lanes store 64 bytes of a row.
+          const uint32_t row_at = base + L::kOut + warp * kOutWarp;
+#pragma unroll
+          for (int k = 0; k < 32; k += 8) {
+            uint32_t y[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              y[x] = pack2<true>(__uint_as_float(o[k + 2 * x]) * inv, __uint_as_float(o[k + 2 * x + 1]) * inv);
+            sts128(row_at + lane * kOutRow + k * 2, y);
+          }
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int r = 8 * k + (lane >> 2), ch = 32 * c + 8 * (lane & 3);
+            const uint4 y = lds128(row_at + r * kOutRow + (lane & 3) * 16);
+            const int64_t at = __shfl_sync(0xffffffffu, out_at, r);
+            if (32 * (warp & 3) + r < n_rows && ch < a.p.dim) *reinterpret_cast<uint4*>(a.out + at + ch) = y;
+          }
+          __syncwarp();
         }
       }
       __syncwarp();
@@ -801,56 +829,65 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // Joins the partial results of the tiles that several blocks shared. The block
 // where a tile starts holds its first part, the following blocks' first runs the
-// others. A warp takes a query row, 4 channels per lane.
+// others. A block takes 32 query rows, one per lane; each of its 4 warps takes 32
+// channels of them.
 __global__ void __launch_bounds__(128) attend_tiles_join_kernel(AttendArgs a, int tiles, int blocks) {
+  __shared__ __align__(16) uint2 rows[32][34];
   pdl_wait();
-  const int slot = blockIdx.x, lane = threadIdx.x & 31;
+  const int slot = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int4 rec = a.part_rec[slot];
   if (!rec.x || !(rec.w & 1)) return;
   const Tile x = tile_of(a, tiles, rec.y);
-  const int head = rec.z, c = lane * 4;
-  for (int r = blockIdx.y * 4 + (threadIdx.x >> 5); r < x.n_rows; r += gridDim.y * 4) {
-    float top = kNegInf, sum = 0.0f;
-    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    bool more = true;
-    for (int i0 = 0; more; i0 += 32) {  // 32 parts at a time
-      const int i = i0 + lane, blk = (slot >> 1) + i;
-      const int at = i == 0 ? slot : 2 * blk;
-      const bool there = i == 0 || blk < blocks;
-      const uint32_t last = __ballot_sync(0xffffffffu, !there || (a.part_rec[at].w & 2));
-      const int n = last ? __ffs(last) : 32;
-      more = last == 0;
-      const float2 ml = lane < n && there ? a.part_ml[static_cast<int64_t>(at) * kRowsCta + r] : make_float2(kNegInf, 0.0f);
-      float mx = ml.x;
+  const int r0 = blockIdx.y * 32, r = r0 + lane, n_rows = x.n_rows - r0;
+  if (n_rows <= 0) return;
+  const int quads = a.p.dim / 4;
+  float top = kNegInf, sum = 0.0f;
+  float4 acc[8];
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-      mx = fmaxf(mx, top);
-      const float base = mx == kNegInf ? 0.0f : mx;
-      const float f0 = exp2_fast(top - base), f = exp2_fast(ml.x - base);
-      top = mx;
-      float part = f * ml.y;
+  for (int c = 0; c < 8; ++c) acc[c] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  bool more = true;
+  for (int i0 = 0; more; i0 += 32) {  // 32 parts at a time
+    const int blk = (slot >> 1) + i0 + lane, at = i0 + lane == 0 ? slot : 2 * blk;
+    const bool there = i0 + lane == 0 || blk < blocks;
+    const uint32_t last = __ballot_sync(0xffffffffu, !there || (a.part_rec[at].w & 2));
+    const int n = last ? __ffs(last) : 32;
+    more = last == 0;
+    float mx = top;
+    for (int s = 0; s < n; ++s) mx = fmaxf(mx, a.part_ml[static_cast<int64_t>(__shfl_sync(0xffffffffu, at, s)) * kRowsCta + r].x);
+    const float base = mx == kNegInf ? 0.0f : mx, f0 = exp2_fast(top - base);
+    top = mx;
+    sum *= f0;
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
-      sum = sum * f0 + part;
-      acc.x *= f0, acc.y *= f0, acc.z *= f0, acc.w *= f0;
-#pragma unroll 4
-      for (int s = 0; s < n; ++s) {
-        const float wgt = __shfl_sync(0xffffffffu, f, s);
-        const int as = __shfl_sync(0xffffffffu, at, s);
-        if (c < a.p.dim) {
-          const float4 y = *reinterpret_cast<const float4*>(a.part_o + (static_cast<int64_t>(as) * kRowsCta + r) * a.p.dim + c);
-          acc.x += wgt * y.x, acc.y += wgt * y.y, acc.z += wgt * y.z, acc.w += wgt * y.w;
+    for (int c = 0; c < 8; ++c) acc[c].x *= f0, acc[c].y *= f0, acc[c].z *= f0, acc[c].w *= f0;
+    for (int s = 0; s < n; ++s) {
+      const int64_t as = __shfl_sync(0xffffffffu, at, s);
+      const float2 ml = a.part_ml[as * kRowsCta + r];
+      const float f = exp2_fast(ml.x - base);
+      sum += f * ml.y;
+      const float4* o = reinterpret_cast<const float4*>(a.part_o) + (as * quads + 8 * warp) * kRowsCta + r;
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        if (8 * warp + c < quads && lane < n_rows) {
+          const float4 y = o[c * kRowsCta];
+          acc[c].x += f * y.x, acc[c].y += f * y.y, acc[c].z += f * y.z, acc[c].w += f * y.w;
         }
-      }
     }
-    const int tok = (x.row0 + r) / a.share, hq = head * a.share + x.row0 + r - tok * a.share;
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    if (sum == 0.0f) acc[c] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // sees nothing
+    rows[lane][8 * warp + c] = make_uint2(pack2<true>(acc[c].x * inv, acc[c].y * inv), pack2<true>(acc[c].z * inv, acc[c].w * inv));
+  }
+  __syncthreads();
+  for (int i = warp; i < min(32, n_rows); i += 4) {  // a warp stores a row
+    const int tok = a.by_share(x.row0 + r0 + i), hq = rec.z * a.share + x.row0 + r0 + i - tok * a.share;
     const int64_t row = x.seq.row0 + static_cast<int64_t>(tok);
-    if (sum == 0.0f) acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // sees nothing
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    if (c < a.p.dim)
-      *reinterpret_cast<uint2*>(a.out + row * a.out_row + hq * a.out_head + c) =
-          make_uint2(pack2<true>(acc.x * inv, acc.y * inv), pack2<true>(acc.z * inv, acc.w * inv));
-    if (lane == 0 && a.lse) a.lse[row * a.q_heads + hq] = sum == 0.0f ? kNegInf : (top + log2f(sum)) * 0.6931471805599453f;
+    if (lane < quads) *reinterpret_cast<uint2*>(a.out + row * a.out_row + hq * a.out_head + 4 * lane) = rows[i][lane];
+  }
+  if (warp == 0 && a.lse && lane < n_rows) {
+    const int tok = a.by_share(x.row0 + r), hq = rec.z * a.share + x.row0 + r - tok * a.share;
+    a.lse[(x.seq.row0 + static_cast<int64_t>(tok)) * a.q_heads + hq] = sum == 0.0f ? kNegInf : (top + log2f(sum)) * 0.6931471805599453f;
   }
 }
 
@@ -925,7 +962,7 @@ cudaError_t launch_attend_tiles(const AttendArgs& a, bool bf16, const TileMaps& 
              : launch_one<false, 128>(a, km, vm, tiles, maps.box_rows, limit_ns, blocks, st);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(2 * static_cast<unsigned>(blocks), 64);
+  cfg.gridDim = dim3(2 * static_cast<unsigned>(blocks), kRowsCta / 32);
   cfg.blockDim = dim3(128);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];

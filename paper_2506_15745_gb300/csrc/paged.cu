@@ -166,6 +166,9 @@ ipv_status check_attend(const ipv_pages* p, const ipv_batch* b, const ipv_attend
   if (tiles * a->p.n_seqs > INT32_MAX) return reject(IPV_EINVAL, "n_seqs times the query tiles of max_rows exceeds 2^31 - 1");
   a->q_heads = t->n_q_heads;
   a->share = t->n_q_heads / p->n_kv_heads;
+  a->by_share = ipv::Divide(a->share);
+  a->by_q_heads = ipv::Divide(a->q_heads);
+  a->by_tiles = ipv::Divide(tiles > 0 ? static_cast<int>(tiles) : 1);
   a->scale_log2 = t->scale * 1.4426950408889634f;
   a->causal = t->causal;
   a->window = t->window;
@@ -202,7 +205,6 @@ void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
   plan->bytes = 0;
   int64_t parts = 0;
   if (plan->tiles) {
-    a->step = ipv::kTilesStep;
     a->tile = ipv::kTilesRows;
     a->unit = kTilesLeast;
     a->splits = 1;
@@ -216,16 +218,15 @@ void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
     parts = static_cast<int64_t>(plan->blocks) * 2 * ipv::kTilesRows;
   } else {
     // Each split costs a partial result, written and read again: as many as fill the device.
-    a->step = ipv::kRowsStep;
     a->tile = ipv::attend_rows_tile(static_cast<int>(rows));
     const int64_t slots = static_cast<int64_t>(num_sms) * ipv::attend_rows_ctas(p.fmt, p.dim) * (p.n_seqs > 1 ? 2 : 1);
     const int64_t tiles = (rows + a->tile - 1) / a->tile;
     int64_t span = p.max_kv;
     if (a->window) {  // the tile's tokens' windows, the sinks, and a step's slack at each of the three ends
-      const int64_t seen = static_cast<int64_t>(a->window) + a->tile + a->sinks + 3 * a->step;
+      const int64_t seen = static_cast<int64_t>(a->window) + a->tile + a->sinks + 3 * ipv::kRowsStep;
       if (seen < span) span = seen;
     }
-    const int64_t steps = (span + a->step - 1) / a->step;
+    const int64_t steps = (span + ipv::kRowsStep - 1) / ipv::kRowsStep;
     const int64_t blocks = tiles * p.heads * p.n_seqs;
     int64_t want = slots / blocks;
     if (want < 1) want = 1;
@@ -360,7 +361,7 @@ extern "C" ipv_status ipv_attend(const ipv_pages* pages, const ipv_batch* batch,
       x.causal = a.causal;
       x.window = a.window;
       x.sinks = a.sinks;
-      x.step = a.step;
+      x.step = ipv::kTilesStep;
       if (a.p.max_kv > 0 && (e = ipv::launch_pages_expand(x, st)) != cudaSuccess) return cuda_reject(e, "code widening kernel");
       a.p = widened(a.p, ws + plan.k16, ws + plan.v16);
     }

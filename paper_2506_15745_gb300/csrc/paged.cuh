@@ -62,6 +62,22 @@ __device__ __forceinline__ int64_t pool_row(const Pages& p, int b, int j) {
   return g * p.page_stride + (p.page_shift == 31 ? j : j & (p.page_size - 1)) * p.row_stride;
 }
 
+// Division of 0 <= x < 2^31 by a fixed 1 <= d < 2^31 as a multiplication:
+// x / d = x * m >> 31 + s with s = ceil(log2 d), m = ceil(2^(31 + s) / d); m is
+// too large by less than 2^s / 2^(31 + s) of itself, which x cannot make a unit.
+struct Divide {
+  uint32_t m = 0;
+  int s = 0, d = 1;
+  Divide() = default;
+  explicit Divide(int by) : d(by) {
+    while ((int64_t{1} << s) < by) ++s;
+    m = static_cast<uint32_t>(((uint64_t{1} << (31 + s)) + by - 1) / by);
+  }
+  __device__ __forceinline__ int operator()(int x) const {
+    return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(x)) * m) >> (31 + s));
+  }
+};
+
 // ------------------------------------------------------------------ attention
 struct AttendArgs {
   Pages p;
@@ -70,16 +86,18 @@ struct AttendArgs {
   float* lse;
   int64_t q_row, q_head, out_row, out_head;  // strides in elements
   int q_heads, share;   // query heads; query heads per KV head
+  Divide by_share, by_q_heads, by_tiles;  // tiles: row tiles of max_rows (tiled kernel)
   float scale_log2;     // scale * log2(e)
   int causal, window, sinks;
-  // Keys are split: into at most `unit` steps of `step` keys (rows kernel), or
+  // Keys are split: into at most `unit` steps (rows kernel), or
   // where a block's share of the steps, at least `unit`, ends (tiled kernel).
-  int step, unit, splits;  // splits: most that any row tile has (rows kernel)
+  int unit, splits;  // splits: most that any row tile has (rows kernel)
   int tile;                // query rows of a row tile
-  // Partial results: unnormalised sums [..][dim] and (running maximum, sum)
-  // [..], of [total_rows * q_heads][splits] (rows kernel) or of
-  // [blocks][2][kTilesRows] with a record each [blocks][2] (tiled kernel):
-  // (1 or 0: none, pair of sequence and tile, KV head, 1: a tile's start + 2: its end).
+  // Partial results: unnormalised sums and (running maximum, sum).
+  // Rows kernel: [total_rows * q_heads][splits][dim] and [..][splits].
+  // Tiled kernel: [blocks][2][dim / 4][kTilesRows][4] and [blocks][2][kTilesRows],
+  // with a record [blocks][2]: (1 or 0: none, pair of sequence and tile, KV head,
+  // 1: a tile's start + 2: its end).
   float* part_o;
   float2* part_ml;
   int4* part_rec;
@@ -91,8 +109,9 @@ struct KeyRange {
   int sink_steps, first, steps;
   int hi_min, hi_max;  // keys j < hi of the first and of the last token
   int lo_max;          // the last token's window starts here
-  __device__ __forceinline__ int key0(int i, int step) const {
-    return (i < sink_steps ? i : i - sink_steps + first) * step;
+  template <int STEP>
+  __device__ __forceinline__ int key0(int i) const {
+    return (i < sink_steps ? i : i - sink_steps + first) * STEP;
   }
 };
 
@@ -100,16 +119,17 @@ __device__ __forceinline__ int token_hi(const AttendArgs& a, const Seq& s, int t
   return a.causal ? max(0, s.len - s.n + tok + 1) : s.len;
 }
 
+template <int STEP>
 __device__ __forceinline__ KeyRange key_range(const AttendArgs& a, const Seq& s, int tok0, int tok1) {
   KeyRange r;
   r.hi_min = token_hi(a, s, tok0);
   r.hi_max = token_hi(a, s, tok1);
   const int lo = a.window ? max(0, r.hi_min - a.window) : 0;
   r.lo_max = a.window ? max(0, r.hi_max - a.window) : 0;
-  r.first = lo / a.step;
-  // (x - 1) / step + 1 rather than (x + step - 1) / step: x may be near 2^31
-  r.sink_steps = a.sinks > 0 ? min(r.first, (a.sinks - 1) / a.step + 1) : 0;
-  const int end = r.hi_max > 0 ? (r.hi_max - 1) / a.step + 1 : 0;
+  r.first = lo / STEP;
+  // (x - 1) / STEP + 1 rather than (x + STEP - 1) / STEP: x may be near 2^31
+  r.sink_steps = a.sinks > 0 ? min(r.first, (a.sinks - 1) / STEP + 1) : 0;
+  const int end = r.hi_max > 0 ? (r.hi_max - 1) / STEP + 1 : 0;
   r.steps = r.sink_steps + max(0, end - r.first);
   return r;
 }
