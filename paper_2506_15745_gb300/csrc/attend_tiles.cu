@@ -7,7 +7,8 @@
 // block per SM takes an equal share of all steps, in order; where a share ends
 // inside a tile's keys, the block leaves a partial result that a second kernel
 // joins. A block has twelve warps:
-//   - one copies K and V tiles from their pages by TMA (a box per page),
+//   - one copies K tiles from their pages by TMA (a box per page and 64
+//     channels), one V tiles: small boxes are slow to issue,
 //   - one for each query tile issues its matrix instructions (tcgen05.mma):
 //     S = Q K^T into tensor memory and, with the softmax weights P read from
 //     tensor memory, O += P V. They take turns, so that one tile's products run
@@ -38,7 +39,7 @@ namespace {
 
 constexpr int kRowsCta = kTilesRows;  // query rows of a block
 constexpr int kKeys = kTilesStep;     // keys of a step
-constexpr int kMmaWarp = 8, kLoadWarp = 10;  // warps 8, 9: products of query tiles 0, 1
+constexpr int kMmaWarp = 8, kLoadWarp = 10;  // warps 8, 9: products of query tiles 0, 1; 10, 11: copies of K, V
 constexpr int kThreads = 384;                // two softmax warpgroups, one for copies and products
 constexpr int kHalf = 128 * 128;      // bytes of 128 rows x 64 channels
 constexpr float kNegInf = -INFINITY;
@@ -448,11 +449,15 @@ __global__ void __launch_bounds__(kThreads, 1)
   // stay in registers), 128 keep 56: the same 64512 in all.
   if (warp >= kMmaWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (warp == kLoadWarp) {
+    if (warp >= kLoadWarp) {
       // -------------------------------------------------------------- copies
+      const bool v = warp > kLoadWarp;
+      const CUtensorMap* map = v ? &v_map : &k_map;
+      const int full0 = v ? kBarVFull : kBarKFull, empty0 = v ? kBarVEmpty : kBarKEmpty;
+      const uint32_t tile0 = base + (v ? L::kV : L::kK);
       const int pieces = kKeys / box_rows;
       const uint32_t piece_bytes = box_rows * 128;
-      int it = 0, k_out = 0, v_out = 0;  // steps; K and V tiles asked for
+      int it = 0, out = 0;  // steps; tiles asked for
       // This lane's piece of step i: its page and the row there, page < 0: none.
       auto piece = [&](int i, int& page, int& row) {
         const int j = w.t.kr.key0<kKeys>(w.s + i) + lane * box_rows;
@@ -468,29 +473,24 @@ __global__ void __launch_bounds__(kThreads, 1)
         int page_next, row_next;
         piece(0, page_next, row_next);
         for (int i = 0; i < w.n; ++i, ++it) {
-          const int st = it % L::kStages;
-          const uint32_t empty = ((it / L::kStages) & 1) ^ 1;
-          const int page = page_next, row = row_next;
+          const int st = it % L::kStages, page = page_next, row = row_next;
           const bool active = page >= 0;
           const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, active)) * piece_bytes * L::kHalves;
           if (i + 1 < w.n) piece(i + 1, page_next, row_next);  // the table is read a step ahead
-          for (int kv = 0; kv < 2; ++kv) {
-            const uint32_t full = bar((kv ? kBarVFull : kBarKFull) + st);
-            bar_wait(bar((kv ? kBarVEmpty : kBarKEmpty) + st), empty, stop, limit_ns, 1u);
-            if (__any_sync(0xffffffffu, lds_flag(stop))) break;
-            if (lane == 0) bar_expect(full, bytes);
-            __syncwarp();
-            if (active) {
-              const uint32_t dst = base + (kv ? L::kV : L::kK) + st * L::kTile + lane * piece_bytes;
+          bar_wait(bar(empty0 + st), ((it / L::kStages) & 1) ^ 1, stop, limit_ns, 1u);
+          if (__any_sync(0xffffffffu, lds_flag(stop))) break;
+          if (lane == 0) bar_expect(bar(full0 + st), bytes);
+          __syncwarp();
+          if (active) {
+            const uint32_t dst = tile0 + st * L::kTile + lane * piece_bytes;
 #pragma unroll
-              for (int h = 0; h < L::kHalves; ++h)
-                tma_load(dst + h * kHalf, kv ? &v_map : &k_map, full, 64 * h, row, w.head, page);
-            }
-            (kv ? v_out : k_out) = it + 1;
-            __syncwarp();
+            for (int h = 0; h < L::kHalves; ++h) tma_load(dst + h * kHalf, map, bar(full0 + st), 64 * h, row, w.head, page);
           }
+          out = it + 1;
+          __syncwarp();
         }
-        if (w.keep() < kKeys) {
+        if (__any_sync(0xffffffffu, lds_flag(stop))) break;
+        if (v && w.keep() < kKeys) {
           // Rows past the last key hold anything; a weight of 0 would not hide a NaN.
           const int last = it - 1, st = last % L::kStages, keep = w.keep();
           bar_wait(bar(kBarVFull + st), (last / L::kStages) & 1, stop, limit_ns, 1u);
@@ -502,18 +502,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           if (lane == 0) bar_arrive(bar(kBarVTail + st));
         }
-        if (__any_sync(0xffffffffu, lds_flag(stop))) break;
       }
       if (__any_sync(0xffffffffu, lds_flag(stop))) {
         // Stopped: the block's memory must outlive the copies in flight.
-        for (int i = max(0, k_out - L::kStages); i < k_out; ++i)
-          for (int x = 0; x < 1 << 16 && !bar_try(bar(kBarKFull + i % L::kStages), (i / L::kStages) & 1); ++x) {
-          }
-        for (int i = max(0, v_out - L::kStages); i < v_out; ++i)
-          for (int x = 0; x < 1 << 16 && !bar_try(bar(kBarVFull + i % L::kStages), (i / L::kStages) & 1); ++x) {
+        for (int i = max(0, out - L::kStages); i < out; ++i)
+          for (int x = 0; x < 1 << 16 && !bar_try(bar(full0 + i % L::kStages), (i / L::kStages) & 1); ++x) {
           }
       }
-    } else if (warp < kLoadWarp) {
+    } else {
       // ------------------------------------------------------------ products
       const int t = warp - kMmaWarp;
       constexpr uint32_t idesc_s = instr<BF16>(kKeys, false), idesc_o = instr<BF16>(DP, true);
@@ -684,9 +680,17 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int c = 0; c < 4; ++c) wait_ld(s[c]);
         if (masked) {
+          if (__any_sync(0xffffffffu, h < kKeys)) {
 #pragma unroll
-          for (int c = 0; c < 128; ++c)
-            if (!(c < h && (c >= w0 || c < sk))) s[c >> 5][c & 31] = 0xFF800000u;
+            for (int c = 0; c < 128; ++c)
+              if (c >= h) s[c >> 5][c & 31] = 0xFF800000u;
+          }
+          if (__any_sync(0xffffffffu, w0 > 0 && sk < kKeys)) {
+            const unsigned gap = w0 > sk ? w0 - sk : 0;
+#pragma unroll
+            for (int c = 0; c < 128; ++c)
+              if (static_cast<unsigned>(c - sk) < gap) s[c >> 5][c & 31] = 0xFF800000u;
+          }
         }
         float2 mb2, sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
         uint32_t p[32];
@@ -829,63 +833,74 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // Joins the partial results of the tiles that several blocks shared. The block
 // where a tile starts holds its first part, the following blocks' first runs the
-// others. A block takes 32 query rows, one per lane; each of its 4 warps takes 32
-// channels of them.
+// others. A block takes 32 query rows, one per lane, and 64 channels, 16 for
+// each of its 4 warps; 4 parts at a time are on their way at once.
 __global__ void __launch_bounds__(128) attend_tiles_join_kernel(AttendArgs a, int tiles, int blocks) {
-  __shared__ __align__(16) uint2 rows[32][34];
+  __shared__ __align__(16) uint2 rows[32][17];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x;
+  const int r0 = blockIdx.y * 32, r = r0 + lane, quads = a.p.dim / 4, quad0 = 16 * blockIdx.z + 4 * warp;
   pdl_wait();
-  const int slot = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int4 rec = a.part_rec[slot];
-  if (!rec.x || !(rec.w & 1)) return;
+  const int4 one = a.part_rec[2 * c], two = a.part_rec[2 * c + 1];
+  int n = 0;  // parts: up to the first that ends its tile
+  for (int i0 = 1; n == 0; i0 += 32) {
+    const int blk = c + i0 + lane;
+    const uint32_t last = __ballot_sync(0xffffffffu, blk >= blocks || (a.part_rec[2 * blk].w & 2));
+    if (last) n = i0 + __ffs(last);
+  }
+  const int slot = two.x && two.w == 1 ? 2 * c + 1 : one.x && one.w == 1 ? 2 * c : -1;  // started here, not ended
+  if (slot < 0) return;
+  const int4 rec = slot & 1 ? two : one;
   const Tile x = tile_of(a, tiles, rec.y);
-  const int r0 = blockIdx.y * 32, r = r0 + lane, n_rows = x.n_rows - r0;
+  const int n_rows = min(32, x.n_rows - r0);
   if (n_rows <= 0) return;
-  const int quads = a.p.dim / 4;
   float top = kNegInf, sum = 0.0f;
-  float4 acc[8];
+  float4 acc[4];
 #pragma unroll
-  for (int c = 0; c < 8; ++c) acc[c] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  bool more = true;
-  for (int i0 = 0; more; i0 += 32) {  // 32 parts at a time
-    const int blk = (slot >> 1) + i0 + lane, at = i0 + lane == 0 ? slot : 2 * blk;
-    const bool there = i0 + lane == 0 || blk < blocks;
-    const uint32_t last = __ballot_sync(0xffffffffu, !there || (a.part_rec[at].w & 2));
-    const int n = last ? __ffs(last) : 32;
-    more = last == 0;
+  for (int k = 0; k < 4; ++k) acc[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  constexpr int kAtOnce = 4;
+  for (int i0 = 0; i0 < n; i0 += kAtOnce) {
+    float2 ml[kAtOnce];
+    float4 y[kAtOnce][4];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const bool there = i0 + i < n && lane < n_rows;
+      const int64_t at = i0 + i == 0 ? slot : 2 * (c + i0 + i);
+      ml[i] = there ? a.part_ml[at * kRowsCta + r] : make_float2(kNegInf, 0.0f);
+      const float4* o = reinterpret_cast<const float4*>(a.part_o) + (at * quads + quad0) * kRowsCta + r;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[i][k] = there && quad0 + k < quads ? o[k * kRowsCta] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
     float mx = top;
-    for (int s = 0; s < n; ++s) mx = fmaxf(mx, a.part_ml[static_cast<int64_t>(__shfl_sync(0xffffffffu, at, s)) * kRowsCta + r].x);
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) mx = fmaxf(mx, ml[i].x);
     const float base = mx == kNegInf ? 0.0f : mx, f0 = exp2_fast(top - base);
     top = mx;
     sum *= f0;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) acc[c].x *= f0, acc[c].y *= f0, acc[c].z *= f0, acc[c].w *= f0;
-    for (int s = 0; s < n; ++s) {
-      const int64_t as = __shfl_sync(0xffffffffu, at, s);
-      const float2 ml = a.part_ml[as * kRowsCta + r];
-      const float f = exp2_fast(ml.x - base);
-      sum += f * ml.y;
-      const float4* o = reinterpret_cast<const float4*>(a.part_o) + (as * quads + 8 * warp) * kRowsCta + r;
+    for (int k = 0; k < 4; ++k) acc[k].x *= f0, acc[k].y *= f0, acc[k].z *= f0, acc[k].w *= f0;
 #pragma unroll
-      for (int c = 0; c < 8; ++c)
-        if (8 * warp + c < quads && lane < n_rows) {
-          const float4 y = o[c * kRowsCta];
-          acc[c].x += f * y.x, acc[c].y += f * y.y, acc[c].z += f * y.z, acc[c].w += f * y.w;
-        }
+    for (int i = 0; i < kAtOnce; ++i) {
+      const float f = exp2_fast(ml[i].x - base);
+      sum += f * ml[i].y;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        acc[k].x += f * y[i][k].x, acc[k].y += f * y[i][k].y, acc[k].z += f * y[i][k].z, acc[k].w += f * y[i][k].w;
     }
   }
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    if (sum == 0.0f) acc[c] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // sees nothing
-    rows[lane][8 * warp + c] = make_uint2(pack2<true>(acc[c].x * inv, acc[c].y * inv), pack2<true>(acc[c].z * inv, acc[c].w * inv));
+  for (int k = 0; k < 4; ++k) {
+    if (sum == 0.0f) acc[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // sees nothing
+    rows[lane][4 * warp + k] = make_uint2(pack2<true>(acc[k].x * inv, acc[k].y * inv), pack2<true>(acc[k].z * inv, acc[k].w * inv));
   }
   __syncthreads();
-  for (int i = warp; i < min(32, n_rows); i += 4) {  // a warp stores a row
+  const int q = threadIdx.x & 15;  // 16 lanes store 128 bytes of a row
+  for (int i = threadIdx.x >> 4; i < n_rows; i += 8) {
     const int tok = a.by_share(x.row0 + r0 + i), hq = rec.z * a.share + x.row0 + r0 + i - tok * a.share;
     const int64_t row = x.seq.row0 + static_cast<int64_t>(tok);
-    if (lane < quads) *reinterpret_cast<uint2*>(a.out + row * a.out_row + hq * a.out_head + 4 * lane) = rows[i][lane];
+    if (16 * blockIdx.z + q < quads) *reinterpret_cast<uint2*>(a.out + row * a.out_row + hq * a.out_head + 64 * blockIdx.z + 4 * q) = rows[i][q];
   }
-  if (warp == 0 && a.lse && lane < n_rows) {
+  if (warp == 0 && blockIdx.z == 0 && a.lse && lane < n_rows) {
     const int tok = a.by_share(x.row0 + r), hq = rec.z * a.share + x.row0 + r - tok * a.share;
     a.lse[(x.seq.row0 + static_cast<int64_t>(tok)) * a.q_heads + hq] = sum == 0.0f ? kNegInf : (top + log2f(sum)) * 0.6931471805599453f;
   }
@@ -962,7 +977,7 @@ cudaError_t launch_attend_tiles(const AttendArgs& a, bool bf16, const TileMaps& 
              : launch_one<false, 128>(a, km, vm, tiles, maps.box_rows, limit_ns, blocks, st);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(2 * static_cast<unsigned>(blocks), kRowsCta / 32);
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks), kRowsCta / 32, a.p.dim <= 64 ? 1 : 2);
   cfg.blockDim = dim3(128);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];

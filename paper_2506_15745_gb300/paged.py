@@ -50,7 +50,8 @@ class PagedBatch:
               "table is [n_seqs, max_pages]")
         self.table, self.row_start, self.kv_len = table, row_start, kv_len
         self.n_seqs, self.total_rows, self.max_rows, self.max_kv = n, total_rows, max_rows, max_kv
-        self.struct = ipv.Batch(n, 1 if table is None else table.shape[1], ipv._ptr(table),
+        self.max_pages = 1 if table is None else table.shape[1]
+        self.struct = ipv.Batch(n, self.max_pages, ipv._ptr(table),
                                 1 if table is None else max(table.stride(0), table.shape[1]), ipv._ptr(row_start),
                                 ipv._ptr(kv_len), total_rows, max_rows, max_kv)
         self.ref = ctypes.byref(self.struct)
@@ -120,7 +121,7 @@ class PagedCache:
         self.struct = ipv.PagesDesc(FORMATS[fmt], self.n_kv_heads, self.head_dim, self.page_size, self.n_pages, *rows,
                                     k.data_ptr(), v.data_ptr(), ipv._ptr(k_par), ipv._ptr(v_par))
         self.ref = ctypes.byref(self.struct)
-        self._workspace = None
+        self._workspaces, self._needs = {}, {}
 
     @staticmethod
     def _row_strides(t, width):
@@ -134,17 +135,18 @@ class PagedCache:
 
     @staticmethod
     def _packed(name, t, batch, heads, dim):
-        _need(t.dtype == torch.bfloat16 and t.is_cuda and t.dim() == 3 and t.stride(2) == 1,
-              f"{name} must be a bf16 CUDA tensor [rows, heads, head_dim] with contiguous rows")
-        _need(t.shape[0] >= batch.total_rows and t.shape[1] == heads and t.shape[2] == dim,
-              f"{name} must be [{batch.total_rows}, {heads}, {dim}]")
+        shape, strides = t.shape, t.stride()
+        if (t.dtype is not torch.bfloat16 or not t.is_cuda or len(shape) != 3 or strides[2] != 1 or
+                shape[0] < batch.total_rows or shape[1] != heads or shape[2] != dim):
+            raise ValueError(f"{name} must be a bf16 CUDA tensor [{batch.total_rows}, {heads}, {dim}] with contiguous rows")
+        return strides
 
     def write(self, k_new, v_new, batch: PagedBatch, stream=None) -> None:
         """ipv_pages_write: k_new, v_new bf16 [total_rows, n_kv_heads, head_dim] into the batch's pages."""
-        for name, t in (("k_new", k_new), ("v_new", v_new)):
-            self._packed(name, t, batch, self.n_kv_heads, self.head_dim)
-        _need(k_new.stride() == v_new.stride(), "k_new and v_new must have the same strides")
-        ipv.pages_write(self.ref, batch.ref, k_new, v_new, k_new.stride(0), k_new.stride(1), stream)
+        strides = self._packed("k_new", k_new, batch, self.n_kv_heads, self.head_dim)
+        _need(self._packed("v_new", v_new, batch, self.n_kv_heads, self.head_dim) == strides,
+              "k_new and v_new must have the same strides")
+        ipv.pages_write(self.ref, batch.ref, k_new, v_new, strides[0], strides[1], stream)
 
     def read(self, batch: PagedBatch, k_out=None, v_out=None, stream=None):
         """ipv_pages_read: the batch's new rows, bf16 [total_rows, n_kv_heads, head_dim] each. Packed rows that
@@ -153,36 +155,45 @@ class PagedCache:
             shape = (batch.total_rows, self.n_kv_heads, self.head_dim)
             k_out = torch.zeros(shape, dtype=torch.bfloat16, device=self.k.device) if k_out is None else k_out
             v_out = torch.zeros(shape, dtype=torch.bfloat16, device=self.k.device) if v_out is None else v_out
-        for name, t in (("k_out", k_out), ("v_out", v_out)):
-            self._packed(name, t, batch, self.n_kv_heads, self.head_dim)
-        _need(k_out.stride() == v_out.stride(), "k_out and v_out must have the same strides")
-        ipv.pages_read(self.ref, batch.ref, k_out, v_out, k_out.stride(0), k_out.stride(1), stream)
+        strides = self._packed("k_out", k_out, batch, self.n_kv_heads, self.head_dim)
+        _need(self._packed("v_out", v_out, batch, self.n_kv_heads, self.head_dim) == strides,
+              "k_out and v_out must have the same strides")
+        ipv.pages_read(self.ref, batch.ref, k_out, v_out, strides[0], strides[1], stream)
         return k_out, v_out
 
     def attend(self, q, batch: PagedBatch, *, out=None, lse=None, scale: float | None = None, causal: bool = True,
                window: int = 0, sinks: int = 0, workspace=None, stream=None):
         """ipv_attend: attention of q, bf16 [total_rows, n_q_heads, head_dim], over the rows that the batch's
         sequences hold. out: bf16 like q (allocated if None); lse: fp32
-        [total_rows, n_q_heads], filled if given. workspace: a uint8 tensor;
-        without one the cache allocates and keeps one of its own, for calls on one stream at a time."""
+        [total_rows, n_q_heads], filled if given. workspace: a uint8 tensor
+        that no call on another stream uses at the same time; without one the cache keeps one of its own for
+        each stream that is current in a call."""
         n_q_heads = q.shape[1]
-        self._packed("q", q, batch, n_q_heads, self.head_dim)
+        qs = self._packed("q", q, batch, n_q_heads, self.head_dim)
         if out is None:
             out = torch.zeros_like(q, memory_format=torch.contiguous_format)
-        self._packed("out", out, batch, n_q_heads, self.head_dim)
+        os = self._packed("out", out, batch, n_q_heads, self.head_dim)
         if lse is not None:
-            _need(lse.dtype == torch.float32 and lse.is_cuda and lse.is_contiguous() and lse.dim() == 2 and
+            _need(lse.dtype is torch.float32 and lse.is_cuda and lse.is_contiguous() and lse.dim() == 2 and
                   lse.shape[0] >= batch.total_rows and lse.shape[1] == n_q_heads,
                   "lse must be a contiguous fp32 CUDA tensor [total_rows, n_q_heads]")
-        args = ipv.AttendArgs(q.data_ptr(), out.data_ptr(), ipv._ptr(lse), q.stride(0), q.stride(1), out.stride(0),
-                              out.stride(1), n_q_heads, self.head_dim ** -0.5 if scale is None else scale,
-                              int(causal), window, sinks, None, 0)
-        need = ipv.attend_workspace(self.ref, batch.ref, args)
+        args = ipv.AttendArgs(q.data_ptr(), out.data_ptr(), ipv._ptr(lse), qs[0], qs[1], os[0], os[1], n_q_heads,
+                              self.head_dim ** -0.5 if scale is None else scale, int(causal), window, sinks, None, 0)
+        # The sizes that the need depends on; asked for once per set of them.
+        sizes = (batch.n_seqs, batch.total_rows, batch.max_rows, batch.max_kv, batch.max_pages, n_q_heads, causal, window, sinks)
+        need = self._needs.get(sizes)
+        if need is None:
+            need = ipv.attend_workspace(self.ref, batch.ref, args)
+            if len(self._needs) >= 4096:
+                self._needs.clear()
+            self._needs[sizes] = need
+        at = ipv._stream(stream)
         if need:
             if workspace is None:
-                if self._workspace is None or self._workspace.numel() < need:
-                    self._workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-                workspace = self._workspace
+                _need(stream is None or at == ipv._stream(None), "a stream that is not the current one needs a workspace")
+                workspace = self._workspaces.get(at)
+                if workspace is None or workspace.numel() < need:
+                    workspace = self._workspaces[at] = torch.empty(need, dtype=torch.uint8, device=q.device)
             args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel()
-        ipv.attend(self.ref, batch.ref, args, stream)
+        ipv.attend(self.ref, batch.ref, ctypes.byref(args), at)
         return out
