@@ -19,7 +19,11 @@
 // 16-bit lane is the subnormal fp16 u * 2^-24 (or 16u * 2^-24), exact. The
 // K side's steps and minima are applied to the sums: q . k = sum over groups
 // of s_g (q_g . u_g) + m_g sum(q_g). Query rows are scaled by a power of two
-// into fp16's range. V is widened to u*s + m in fp16 (11 bits).
+// into fp16's range. On the V side the steps go into the weights, one operand
+// for each group: out = sum_j (p_j s_gj) u_j + sum_j p_j m_gj, the second sum a
+// number per query row and group. The products p s are rounded to fp16 (11 bits)
+// after a power of two that keeps the largest step's below 2^15. So a code costs
+// a mask and its share of two byte permutations and a shift, no multiplication.
 #include <cuda_fp16.h>
 
 #include "paged.cuh"
@@ -28,6 +32,7 @@ namespace ipv {
 namespace {
 
 constexpr int kThreads = 32 * kRowsWarps;
+constexpr int kMaxCtas = 4;  // resident blocks that the registers allow
 constexpr float kNegInf = -INFINITY;
 
 template <int FMT, int DP>
@@ -37,7 +42,7 @@ struct Ring {
   static constexpr int kG = DP / kGroup;
   static constexpr int kPar = FMT == kBf16 ? 0 : kRowsStep * kG * 4;
   static constexpr int kStage = 2 * kTile + 2 * kPar;
-  static constexpr int kStages = FMT == kBf16 ? 3 : 4;
+  static constexpr int kStages = FMT == kBf16 ? 3 : 2;
   static constexpr int kWarp = kStage * kStages;
   static constexpr int kBytes = kWarp * kRowsWarps;
 };
@@ -132,25 +137,18 @@ __device__ __forceinline__ uint4 lds128(uint32_t at) {
   return v;
 }
 __device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<__half2*>(&x); }
-__device__ __forceinline__ uint32_t as_u32(__half2 x) { return *reinterpret_cast<uint32_t*>(&x); }
 __device__ __forceinline__ float par_step(uint32_t p) { return __low2float(as_half2(p)); }
 __device__ __forceinline__ float par_min(uint32_t p) { return __high2float(as_half2(p)); }
 
-// Two 16-bit lanes of codes (masked into the low bits) plus 1024, as fp16.
-__device__ __forceinline__ uint32_t biased(uint32_t x, uint32_t mask) { return (x & mask) | 0x64006400u; }
-
 // Channel of accumulator row (tile ct, half) of the thread in lane group g of
-// the second product: with codes, the channels whose codes the thread reads.
-template <int FMT, int DP>
+// the second product: with codes, the channels whose codes the thread reads,
+// four tiles for each group of channels.
+template <int FMT>
 __device__ __forceinline__ int out_channel(int ct, int half, int g) {
   if (FMT == kBf16) return ct * 16 + half * 8 + g;
-  const int gr = DP == 128 ? g >> 2 : 0;
-  if (FMT == kU8) {
-    const int t = DP == 128 ? g & 3 : g >> 1, w = DP == 128 ? ct >> 1 : 2 * (g & 1) + (ct >> 1);
-    return gr * kGroup + 4 * (t + 4 * w) + 2 * (ct & 1) + half;
-  }
-  const int t = DP == 128 ? g & 3 : g >> 1, w = DP == 128 ? ct >> 2 : g & 1;
-  return gr * kGroup + 8 * (t + 4 * w) + 2 * (ct & 3) + half;
+  const int gr = (ct >> 2) * kGroup, t = g >> 1;
+  if (FMT == kU8) return gr + 4 * (t + 4 * (2 * (g & 1) + ((ct >> 1) & 1))) + 2 * (ct & 1) + half;
+  return gr + 8 * (t + 4 * (g & 1)) + 2 * (ct & 3) + half;
 }
 
 template <int FMT, int DP, int NR>
@@ -177,41 +175,54 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
   const int s_begin = split * a.unit, s_end = min(kr.steps, s_begin + a.unit);
 
   const uint32_t ring = smem_u32(smem) + warp * R::kWarp;
-  const int64_t head_off = head * a.p.head_stride;
   const int nch = a.p.row_bytes >> 4;
 
   // ---- copies of one step into one stage (this warp's lanes only)
-  auto issue = [&](int i, int stage) {
+  // A lane's chunks are chunk my_c of keys my_r, my_r + 32 / kCh, ...
+  constexpr int kApart = 32 / kCh;
+  const int my_r = lane / kCh, my_c = lane % kCh;
+  const char* k_at = a.p.k + head * a.p.head_stride * a.p.row_bytes + my_c * 16;
+  const int64_t v_from_k = a.p.v - a.p.k;
+  const int64_t par_head = head * a.p.head_stride * (R::kG * 4);
+  const char* kp_at_g = reinterpret_cast<const char*>(a.p.k_par) + par_head;
+  const char* vp_at_g = reinterpret_cast<const char*>(a.p.v_par) + par_head;
+  const int64_t page_bytes = a.p.page_stride * a.p.row_bytes, next_bytes = a.p.row_stride * a.p.row_bytes;
+  // This lane's key of step i: its offset in the pool, -1: none. The page is read
+  // a step ahead of the copies.
+  auto page_of = [&](int i) {
+    const int j = kr.key0<kRowsStep>(i) + lane;
+    int g = -1;
+    if (i < s_end && j < kr.hi_max) g = a.p.table ? a.p.table[b * a.p.table_stride + (j >> a.p.page_shift)] : b;
+    return static_cast<unsigned>(g) < static_cast<unsigned>(a.p.n_pages) ? g : -1;
+  };
+  auto issue = [&](int i, int g, int stage) {
     const uint32_t base = ring + stage * R::kStage;
     const int j = kr.key0<kRowsStep>(i) + lane;
-    int64_t row = -1;
-    if (j < kr.hi_max) {
-      row = pool_row(a.p, b, j);
-      if (row >= 0) row += head_off;
-    }
+    const int64_t off = g < 0 ? int64_t{-1} : g * page_bytes + (a.p.page_shift == 31 ? j : j & (a.p.page_size - 1)) * next_bytes;
     if constexpr (!kB) {
       constexpr int kN = R::kG * 4;
-      const int64_t at = max(row, int64_t{0}) * R::kG;
-      copy_small<kN>(base + 2 * R::kTile + lane * kN, a.p.k_par + at, row >= 0);
-      copy_small<kN>(base + 2 * R::kTile + R::kPar + lane * kN, a.p.v_par + at, row >= 0);
+      const int64_t at = g < 0 ? 0 : off / (R::kRowB / kN);  // a row of codes is 8 or 16 times its pairs
+      copy_small<kN>(base + 2 * R::kTile + lane * kN, kp_at_g + at, g >= 0);
+      copy_small<kN>(base + 2 * R::kTile + R::kPar + lane * kN, vp_at_g + at, g >= 0);
     }
 #pragma unroll
     for (int u = 0; u < kCh; ++u) {
-      const int idx = u * 32 + lane, r = idx / kCh, c = idx % kCh;
-      const int64_t rr = __shfl_sync(0xffffffffu, row, r);
-      const bool ok = rr >= 0 && c < nch;
-      const int64_t at = ok ? rr * a.p.row_bytes + c * 16 : 0;
-      const uint32_t dst = base + r * R::kRowB + swizzle<FMT, R::kRowB>(r, c) * 16;
-      copy16(dst, a.p.k + at, ok);
-      copy16(dst + R::kTile, a.p.v + at, ok);
+      const int r = u * kApart + my_r;
+      const int64_t at = __shfl_sync(0xffffffffu, off, r);
+      const bool ok = at >= 0 && (!kB || my_c < nch);
+      const char* src = ok ? k_at + at : a.p.k;
+      const uint32_t dst = base + r * R::kRowB + swizzle<FMT, R::kRowB>(r, my_c) * 16;
+      copy16(dst, src, ok);
+      copy16(dst + R::kTile, src + v_from_k, ok);
     }
   };
   const int first = s_begin + warp;
 #pragma unroll
   for (int i = 0; i < R::kStages - 1; ++i) {
-    if (first + i * kRowsWarps < s_end) issue(first + i * kRowsWarps, i);
+    if (first + i * kRowsWarps < s_end) issue(first + i * kRowsWarps, page_of(first + i * kRowsWarps), i);
     copy_commit();
   }
+  int page_next = page_of(first + (R::kStages - 1) * kRowsWarps);
 
   // ---- the query rows as the first product's second operand
   uint32_t qb[kKs][NR][2];
@@ -299,13 +310,23 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
     for (int ct = 0; ct < kCt; ++ct) o[ct][nr][0] = o[ct][nr][1] = o[ct][nr][2] = o[ct][nr][3] = 0.0f;
   }
 
+  // Codes: sums of p m, and the largest step so far, as its fp16 exponent field;
+  // weights times steps are held times 2^(29 - field).
+  float pm[NR][2][kG];
+#pragma unroll
+  for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+    for (int gr = 0; gr < kG; ++gr) pm[nr][0][gr] = pm[nr][1][gr] = 0.0f;
+  uint32_t field = 0;
+
   // ---- the loop over this warp's steps
   int stage = 0;
   for (int step = first; step < s_end; step += kRowsWarps) {
     {
       const int ahead = step + (R::kStages - 1) * kRowsWarps;
       const int to = stage == 0 ? R::kStages - 1 : stage - 1;
-      if (ahead < s_end) issue(ahead, to);
+      if (ahead < s_end) issue(ahead, page_next, to);
+      page_next = page_of(ahead + kRowsWarps);
       copy_commit();
     }
     copy_wait<R::kStages - 1>();
@@ -407,8 +428,44 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
           }
         }
     }
+    // V's steps and minima of this thread's keys, and room for the largest step.
+    float vs[2][2][kG], vm[2][2][kG];
+    if constexpr (!kB) {
+      uint32_t most = 0;
+      uint32_t vp[2][2][kG];
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int k8 = 0; k8 < 2; ++k8)
+#pragma unroll
+          for (int gr = 0; gr < kG; ++gr) {
+            vp[mt][k8][gr] = lds32(vp_at + ((mt * 16 + key_at<FMT>(g) + 8 * k8) * kG + gr) * 4);
+            most = max(most, vp[mt][k8][gr] & 0x7C00u);
+          }
+      most = min(__reduce_max_sync(0xffffffffu, most) >> 10, 30u);
+      if (most > field) {  // rarely: the same for the whole warp
+        const float f = __uint_as_float((127u + field - most) << 23);
+#pragma unroll
+        for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+          for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[ct][nr][i] *= f;
+        field = most;
+      }
+      const float up = __uint_as_float((127u + 29u - field) << 23);
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int k8 = 0; k8 < 2; ++k8)
+#pragma unroll
+          for (int gr = 0; gr < kG; ++gr) {
+            vs[mt][k8][gr] = par_step(vp[mt][k8][gr]) * up;
+            vm[mt][k8][gr] = par_min(vp[mt][k8][gr]);
+          }
+    }
     // Softmax: the rows' new maxima, weights, sums
-    uint32_t pb[2][NR][2], pb2[2][NR][2];
+    uint32_t pb[2][NR][2][kB ? 2 : kG];  // bf16: the weight, and what bf16 leaves of it; codes: times each group's step
 #pragma unroll
     for (int nr = 0; nr < NR; ++nr) {
       float mx[2];
@@ -432,6 +489,8 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
         for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[ct][nr][i] *= f[i & 1];
+#pragma unroll
+        for (int gr = 0; gr < kG; ++gr) pm[nr][0][gr] *= f[0], pm[nr][1][gr] *= f[1];
       }
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
@@ -440,11 +499,19 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
           const float p0 = exp2_fast(sc[mt][nr][2 * k8] - base[0]), p1 = exp2_fast(sc[mt][nr][2 * k8 + 1] - base[1]);
           l[nr][0] += p0;
           l[nr][1] += p1;
-          const uint32_t pk = pack2<kB>(p0, p1);
-          pb[mt][nr][k8] = transpose8(pk);
-          if constexpr (kB)  // what bf16 leaves of the weight, as a second operand: 16 bits in all
-            pb2[mt][nr][k8] = transpose8(
+          if constexpr (kB) {
+            const uint32_t pk = pack2<true>(p0, p1);
+            pb[mt][nr][k8][0] = transpose8(pk);
+            pb[mt][nr][k8][1] = transpose8(
                 pack2<true>(p0 - __uint_as_float(pk << 16), p1 - __uint_as_float(pk & 0xFFFF0000u)));
+          } else {
+#pragma unroll
+            for (int gr = 0; gr < kG; ++gr) {
+              pb[mt][nr][k8][gr] = transpose8(pack2<false>(p0 * vs[mt][k8][gr], p1 * vs[mt][k8][gr]));
+              pm[nr][0][gr] = fmaf(p0, vm[mt][k8][gr], pm[nr][0][gr]);
+              pm[nr][1][gr] = fmaf(p1, vm[mt][k8][gr], pm[nr][1][gr]);
+            }
+          }
         }
     }
     // O^T += V^T P^T
@@ -458,76 +525,55 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
           ldsm4t(va, vs_at + r * R::kRowB + swizzle<FMT, R::kRowB>(r, 2 * ct + ((lane >> 3) & 1)) * 16);
 #pragma unroll
           for (int nr = 0; nr < NR; ++nr) {
-            mma<true>(o[ct][nr], va, pb[mt][nr][0], pb[mt][nr][1]);
-            mma<true>(o[ct][nr], va, pb2[mt][nr][0], pb2[mt][nr][1]);
+            mma<true>(o[ct][nr], va, pb[mt][nr][0][0], pb[mt][nr][1][0]);
+            mma<true>(o[ct][nr], va, pb[mt][nr][0][1], pb[mt][nr][1][1]);
           }
         }
       } else {
         // Keys of matrix columns 2t, 2t+1, 2t+8, 2t+9
-        int kr4[4];
-        uint32_t par[4];
+        uint32_t row[4];
+        int rk[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          kr4[i] = mt * 16 + key_at<FMT>(2 * t + (i & 1)) + (i >> 1) * 8;
-          par[i] = lds32(vp_at + (kr4[i] * kG + (kG == 2 ? g >> 2 : 0)) * 4);
+          rk[i] = mt * 16 + key_at<FMT>(2 * t + (i & 1)) + (i >> 1) * 8;
+          row[i] = vs_at + rk[i] * R::kRowB;
         }
-        __half2 st[2], mn[2];  // (step, step) and (minimum, minimum) of two keys
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          st[i] = as_half2(__byte_perm(par[2 * i], par[2 * i + 1], 0x5410));
-          mn[i] = as_half2(__byte_perm(par[2 * i], par[2 * i + 1], 0x7632));
-        }
-        constexpr int kW = R::kRowB / 32;  // words of a row a thread reads
-        uint32_t wd[4][kW];
+        for (int gr = 0; gr < kG; ++gr) {
+          constexpr int kW = FMT == kU8 ? 2 : 1;  // words of a group a thread reads
+          uint32_t wd[4][kW];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t row = vs_at + kr4[i] * R::kRowB;
-          if constexpr (kW == 4) {
-            const uint4 x = lds128(row + swizzle<FMT, R::kRowB>(kr4[i], g) * 16);
-            wd[i][0] = x.x, wd[i][1 % kW] = x.y, wd[i][2 % kW] = x.z, wd[i][3 % kW] = x.w;
-          } else if constexpr (kW == 2) {
-            const uint2 x = lds64(row + swizzle<FMT, R::kRowB>(kr4[i], g >> 1) * 16 + (g & 1) * 8);
-            wd[i][0] = x.x, wd[i][1 % kW] = x.y;
-          } else {
-            wd[i][0] = lds32(row + swizzle<FMT, R::kRowB>(kr4[i], g >> 2) * 16 + (g & 3) * 4);
-          }
-        }
-        const __half2 k1024 = __float2half2_rn(-1024.0f), k64 = __float2half2_rn(-64.0f),
-                      k16th = __float2half2_rn(0.0625f);
-#pragma unroll
-        for (int w = 0; w < kW; ++w)
-#pragma unroll
-          for (int hl = 0; hl < 2; ++hl) {  // lower and upper 16 bits of the words
-            const uint32_t e0 = __byte_perm(wd[0][w], wd[1][w], hl ? 0x7632 : 0x5410);
-            const uint32_t e1 = __byte_perm(wd[2][w], wd[3][w], hl ? 0x7632 : 0x5410);
+          for (int i = 0; i < 4; ++i) {
             if constexpr (FMT == kU8) {
-              const int ct = w * 2 + hl;
-              uint32_t va[4];
-#pragma unroll
-              for (int half = 0; half < 2; ++half) {
-                const __half2 u0 = __hadd2(as_half2(biased(e0 >> (8 * half), 0x00FF00FFu)), k1024);
-                const __half2 u1 = __hadd2(as_half2(biased(e1 >> (8 * half), 0x00FF00FFu)), k1024);
-                va[half] = as_u32(__hfma2(u0, st[0], mn[0]));
-                va[half + 2] = as_u32(__hfma2(u1, st[1], mn[1]));
-              }
-#pragma unroll
-              for (int nr = 0; nr < NR; ++nr) mma<false>(o[ct][nr], va, pb[mt][nr][0], pb[mt][nr][1]);
+              const uint2 x = lds64(row[i] + swizzle<FMT, R::kRowB>(rk[i], gr * 4 + (g >> 1)) * 16 + (g & 1) * 8);
+              wd[i][0] = x.x, wd[i][1] = x.y;
             } else {
-#pragma unroll
-              for (int q = 0; q < 2; ++q) {  // nibbles 0, 1 and 2, 3 of the 16 bits
-                const int ct = w * 4 + hl * 2 + q;
-                const uint32_t f0 = e0 >> (8 * q), f1 = e1 >> (8 * q);
-                const __half2 a0 = __hadd2(as_half2(biased(f0, 0x000F000Fu)), k1024);
-                const __half2 a1 = __hfma2(as_half2(biased(f0, 0x00F000F0u)), k16th, k64);
-                const __half2 a2 = __hadd2(as_half2(biased(f1, 0x000F000Fu)), k1024);
-                const __half2 a3 = __hfma2(as_half2(biased(f1, 0x00F000F0u)), k16th, k64);
-                const uint32_t va[4] = {as_u32(__hfma2(a0, st[0], mn[0])), as_u32(__hfma2(a1, st[0], mn[0])),
-                                        as_u32(__hfma2(a2, st[1], mn[1])), as_u32(__hfma2(a3, st[1], mn[1]))};
-#pragma unroll
-                for (int nr = 0; nr < NR; ++nr) mma<false>(o[ct][nr], va, pb[mt][nr][0], pb[mt][nr][1]);
-              }
+              wd[i][0] = lds32(row[i] + swizzle<FMT, R::kRowB>(rk[i], gr * 2 + (g >> 2)) * 16 + (g & 3) * 4);
             }
           }
+#pragma unroll
+          for (int w = 0; w < kW; ++w)
+#pragma unroll
+            for (int hl = 0; hl < 2; ++hl) {  // lower and upper 16 bits of the words
+              const uint32_t e0 = __byte_perm(wd[0][w], wd[1][w], hl ? 0x7632 : 0x5410);
+              const uint32_t e1 = __byte_perm(wd[2][w], wd[3][w], hl ? 0x7632 : 0x5410);
+              if constexpr (FMT == kU8) {
+                const int ct = gr * 4 + w * 2 + hl;
+                const uint32_t va[4] = {e0 & 0x00FF00FFu, (e0 >> 8) & 0x00FF00FFu, e1 & 0x00FF00FFu, (e1 >> 8) & 0x00FF00FFu};
+#pragma unroll
+                for (int nr = 0; nr < NR; ++nr) mma<false>(o[ct][nr], va, pb[mt][nr][0][gr], pb[mt][nr][1][gr]);
+              } else {
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {  // nibbles 0, 1 and 2, 3 of the 16 bits
+                  const int ct = gr * 4 + hl * 2 + q;
+                  const uint32_t f0 = e0 >> (8 * q), f1 = e1 >> (8 * q);
+                  const uint32_t va[4] = {f0 & 0x000F000Fu, f0 & 0x00F000F0u, f1 & 0x000F000Fu, f1 & 0x00F000F0u};
+#pragma unroll
+                  for (int nr = 0; nr < NR; ++nr) mma<false>(o[ct][nr], va, pb[mt][nr][0][gr], pb[mt][nr][1][gr]);
+                }
+              }
+            }
+        }
       }
     }
     __syncwarp();  // the stage is read before its next copies are issued
@@ -554,11 +600,26 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
         sm[warp * kRows + r] = m[nr][i];
         sl[warp * kRows + r] = x;
       }
+      float add[kG], times[2] = {1.0f, 1.0f};
+#pragma unroll
+      for (int gr = 0; gr < kG; ++gr) {
+        add[gr] = 0.0f;
+        if constexpr (!kB) {
+          add[gr] = pm[nr][i][gr];
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) add[gr] += __shfl_xor_sync(0xffffffffu, add[gr], d);
+        }
+      }
+      if constexpr (!kB) {  // codes stood for u 2^-24, odd nibbles for 16 u 2^-24
+        times[0] = __uint_as_float((127u + 24u - 29u + field) << 23);
+        times[1] = FMT == kU4 ? times[0] * 0.0625f : times[0];
+      }
 #pragma unroll
       for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
         for (int half = 0; half < 2; ++half)
-          so[(warp * kRows + r) * kPitch + out_channel<FMT, DP>(ct, half, g)] = o[ct][nr][half * 2 + i];
+          so[(warp * kRows + r) * kPitch + out_channel<FMT>(ct, half, g)] =
+              kB ? o[ct][nr][half * 2 + i] : fmaf(o[ct][nr][half * 2 + i], times[half], add[kB ? 0 : ct >> 2]);
     }
   pdl_trigger();
   __syncthreads();
@@ -684,7 +745,7 @@ template <int FMT>
 int ctas(int dim) {
   const int bytes = dim <= 64 ? Ring<FMT, 64>::kBytes : Ring<FMT, 128>::kBytes;
   const int n = (227 << 10) / (bytes + 1024);
-  return n > 4 ? 4 : n;
+  return n > kMaxCtas ? kMaxCtas : n;
 }
 
 }  // namespace

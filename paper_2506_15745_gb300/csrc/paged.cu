@@ -219,7 +219,7 @@ void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
   } else {
     // Each split costs a partial result, written and read again: as many as fill the device.
     a->tile = ipv::attend_rows_tile(static_cast<int>(rows));
-    const int64_t slots = static_cast<int64_t>(num_sms) * ipv::attend_rows_ctas(p.fmt, p.dim) * (p.n_seqs > 1 ? 2 : 1);
+    const int64_t slots = static_cast<int64_t>(num_sms) * ipv::attend_rows_ctas(p.fmt, p.dim) * (p.n_seqs > 1 ? 4 : 1);
     const int64_t tiles = (rows + a->tile - 1) / a->tile;
     int64_t span = p.max_kv;
     if (a->window) {  // the tile's tokens' windows, the sinks, and a step's slack at each of the three ends
