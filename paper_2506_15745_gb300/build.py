@@ -28,7 +28,7 @@ def _stale(out: str, deps: list[str]) -> bool:
 def build(force: bool = False, extra_flags: list[str] | None = None, verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
     headers = [os.path.join(CSRC, "ipv_common.cuh"), os.path.join(CSRC, "pass_device.cuh"),
-               os.path.join(CSRC, "paged.cuh"),
+               os.path.join(CSRC, "paged.cuh"), os.path.join(CSRC, "attend_share.cuh"),
                os.path.join(INCLUDE, "ipv.h")]
     procs, objs = [], []
     for src in SOURCES:

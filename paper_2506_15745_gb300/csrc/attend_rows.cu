@@ -3,10 +3,11 @@
 //
 // HBM-bound: each cached K and V row is read once per row tile, 8 or 16 query
 // rows (the query heads that share a KV head, times the new tokens) use it.
-// A block is 4 warps on one (sequence, KV head, row tile, split of the keys).
-// Each warp takes steps of 32 keys of its own: it copies them into its own
-// ring of shared-memory stages (cp.async, no block barrier anywhere in the
-// loop) and keeps its own softmax state; the warps join at the end.
+// Blocks of 4 warps, as many as fit the device, take equal shares of all steps of
+// 32 keys. Each warp takes steps of its own: it copies them into its own ring of
+// shared-memory stages (cp.async, no block barrier anywhere in the loop) and
+// keeps its own softmax state; the warps join at the end of a row tile's keys, and
+// a second kernel joins the parts where several blocks share a tile.
 //
 // Keys are the matrix instructions' long side, S^T = K Q^T and O^T = V^T P^T
 // (mma.m16n8k16 with 16 keys or channels by 8 query rows), so 7 or 8 query
@@ -26,14 +27,16 @@
 // a mask and its share of two byte permutations and a shift, no multiplication.
 #include <cuda_fp16.h>
 
+#include "attend_share.cuh"
 #include "paged.cuh"
 
 namespace ipv {
 namespace {
 
 constexpr int kThreads = 32 * kRowsWarps;
-constexpr int kMaxCtas = 4;  // resident blocks that the registers allow
+constexpr int kRunCost = 6;  // what a run of steps costs beside them, in steps
 constexpr float kNegInf = -INFINITY;
+constexpr int kOneTile = 1;  // row tiles of a sequence: more rows are the tiled kernel's
 
 template <int FMT, int DP>
 struct Ring {
@@ -151,8 +154,24 @@ __device__ __forceinline__ int out_channel(int ct, int half, int g) {
   return gr + 8 * (t + 4 * (g & 1)) + 2 * (ct & 3) + half;
 }
 
+// Four channels, from c on, of query row r of a sequence's KV head.
+__device__ __forceinline__ void write_row(const AttendArgs& a, const Seq& s, int head, int r, int c, const float4& acc, float top,
+                                          float sum) {
+  const int tok = a.by_share(r), hq = head * a.share + r - tok * a.share;
+  const int64_t row = s.row0 + static_cast<int64_t>(tok);
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  if (c < a.p.dim)
+    *reinterpret_cast<uint2*>(a.out + row * a.out_row + hq * a.out_head + c) =
+        make_uint2(pack2<true>(acc.x * inv, acc.y * inv), pack2<true>(acc.z * inv, acc.w * inv));
+  if (c == 0 && a.lse) a.lse[row * a.q_heads + hq] = sum == 0.0f ? kNegInf : (top + log2f(sum)) * 0.6931471805599453f;
+}
+
+// Resident blocks per SM that registers and shared memory are cut to: bf16 at 128
+// channels has enough bytes in flight with one, codes need warps to widen them.
+constexpr int min_blocks(int fmt, int dp, int nr) { return fmt == kBf16 && dp == 128 ? 1 : nr == 1 ? 3 : 2; }
+
 template <int FMT, int DP, int NR>
-__global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows_kernel(AttendArgs a, int tiles) {
   using R = Ring<FMT, DP>;
   constexpr bool kB = FMT == kBf16;
   constexpr int kCh = R::kRowB / 16;     // chunks of a row
@@ -162,18 +181,17 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int b = blockIdx.z, head = blockIdx.y;
-  const int tile = blockIdx.x / a.splits, split = blockIdx.x - tile * a.splits;
-  const Seq seq = sequence(a.p, b);
-  const int rows = seq.n * a.share;
-  const int row0 = tile * (8 * NR);
-  if (row0 >= rows) return;
-  const int row1 = min(row0 + 8 * NR, rows) - 1;
-  const KeyRange kr = key_range<kRowsStep>(a, seq, a.by_share(row0), a.by_share(row1));
-  const int ns = splits_of(a, kr);
-  if (split >= ns) return;
-  const int s_begin = split * a.unit, s_end = min(kr.steps, s_begin + a.unit);
-
+  constexpr int kTileRows = 8 * NR;
+  pdl_wait();
+  const Share share = find_share<kTileRows, kRowsStep, kRunCost, kThreads>(a, tiles, reinterpret_cast<int64_t*>(smem));
+  int slots = 0;  // partial results used
+  if (share.left <= 0) {
+    if (threadIdx.x < 2) a.part_rec[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
+    return;
+  }
+  __syncthreads();  // the shared memory held find_share's scratch
+  using W = Walk<kTileRows, kRowsStep, kRunCost>;
+  W w = {};
   const uint32_t ring = smem_u32(smem) + warp * R::kWarp;
   const int nch = a.p.row_bytes >> 4;
 
@@ -181,48 +199,60 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
   // A lane's chunks are chunk my_c of keys my_r, my_r + 32 / kCh, ...
   constexpr int kApart = 32 / kCh;
   const int my_r = lane / kCh, my_c = lane % kCh;
-  const char* k_at = a.p.k + head * a.p.head_stride * a.p.row_bytes + my_c * 16;
   const int64_t v_from_k = a.p.v - a.p.k;
-  const int64_t par_head = head * a.p.head_stride * (R::kG * 4);
-  const char* kp_at_g = reinterpret_cast<const char*>(a.p.k_par) + par_head;
-  const char* vp_at_g = reinterpret_cast<const char*>(a.p.v_par) + par_head;
   const int64_t page_bytes = a.p.page_stride * a.p.row_bytes, next_bytes = a.p.row_stride * a.p.row_bytes;
-  // This lane's key of step i: its offset in the pool, -1: none. The page is read
-  // a step ahead of the copies.
-  auto page_of = [&](int i) {
-    const int j = kr.key0<kRowsStep>(i) + lane;
-    int g = -1;
-    if (i < s_end && j < kr.hi_max) g = a.p.table ? a.p.table[b * a.p.table_stride + (j >> a.p.page_shift)] : b;
-    return static_cast<unsigned>(g) < static_cast<unsigned>(a.p.n_pages) ? g : -1;
+  // This lane's key of step i of run x: its page, -1: none. Read a step ahead of
+  // the copies.
+  auto page_of = [&](const W& x, int i) {
+    const int j = x.t.kr.template key0<kRowsStep>(i) + lane;
+    int pg = -1;
+    if (i < x.s + x.n && j < x.t.kr.hi_max) pg = a.p.table ? a.p.table[x.t.b * a.p.table_stride + (j >> a.p.page_shift)] : x.t.b;
+    return static_cast<unsigned>(pg) < static_cast<unsigned>(a.p.n_pages) ? pg : -1;
   };
-  auto issue = [&](int i, int g, int stage) {
+  auto issue = [&](const W& x, int i, int pg, int stage) {
     const uint32_t base = ring + stage * R::kStage;
-    const int j = kr.key0<kRowsStep>(i) + lane;
-    const int64_t off = g < 0 ? int64_t{-1} : g * page_bytes + (a.p.page_shift == 31 ? j : j & (a.p.page_size - 1)) * next_bytes;
+    const int j = x.t.kr.template key0<kRowsStep>(i) + lane;
+    const int64_t head_rows = x.head * a.p.head_stride;
+    const int64_t off = pg < 0 ? int64_t{-1}
+                               : head_rows * a.p.row_bytes + pg * page_bytes +
+                                     (a.p.page_shift == 31 ? j : j & (a.p.page_size - 1)) * next_bytes;
     if constexpr (!kB) {
       constexpr int kN = R::kG * 4;
-      const int64_t at = g < 0 ? 0 : off / (R::kRowB / kN);  // a row of codes is 8 or 16 times its pairs
-      copy_small<kN>(base + 2 * R::kTile + lane * kN, kp_at_g + at, g >= 0);
-      copy_small<kN>(base + 2 * R::kTile + R::kPar + lane * kN, vp_at_g + at, g >= 0);
+      const int64_t at = pg < 0 ? 0 : off / (R::kRowB / kN);  // a row of codes is 8 or 16 times its pairs
+      copy_small<kN>(base + 2 * R::kTile + lane * kN, reinterpret_cast<const char*>(a.p.k_par) + at, pg >= 0);
+      copy_small<kN>(base + 2 * R::kTile + R::kPar + lane * kN, reinterpret_cast<const char*>(a.p.v_par) + at, pg >= 0);
     }
 #pragma unroll
     for (int u = 0; u < kCh; ++u) {
       const int r = u * kApart + my_r;
       const int64_t at = __shfl_sync(0xffffffffu, off, r);
       const bool ok = at >= 0 && (!kB || my_c < nch);
-      const char* src = ok ? k_at + at : a.p.k;
+      const char* src = ok ? a.p.k + my_c * 16 + at : a.p.k;
       const uint32_t dst = base + r * R::kRowB + swizzle<FMT, R::kRowB>(r, my_c) * 16;
       copy16(dst, src, ok);
       copy16(dst + R::kTile, src + v_from_k, ok);
     }
   };
-  const int first = s_begin + warp;
+  // The first steps of a run, and the page of the one after them.
+  int page_next = -1;
+  auto fill = [&](const W& x) {
 #pragma unroll
-  for (int i = 0; i < R::kStages - 1; ++i) {
-    if (first + i * kRowsWarps < s_end) issue(first + i * kRowsWarps, page_of(first + i * kRowsWarps), i);
-    copy_commit();
-  }
-  int page_next = page_of(first + (R::kStages - 1) * kRowsWarps);
+    for (int i = 0; i < R::kStages - 1; ++i) {
+      const int step = x.s + warp + i * kRowsWarps;
+      if (step < x.s + x.n) issue(x, step, page_of(x, step), i);
+      copy_commit();
+    }
+    page_next = page_of(x, x.s + warp + (R::kStages - 1) * kRowsWarps);
+  };
+
+  bool go = w.begin(a, tiles, share);
+  if (go) fill(w);
+  for (int run = 0; go; ++run) {
+  const Seq seq = w.t.seq;
+  const KeyRange kr = w.t.kr;
+  const int head = w.head;
+  const int row0 = w.t.row0, row1 = row0 + w.t.n_rows - 1;
+  const int first = w.s + warp, s_end = w.s + w.n;
 
   // ---- the query rows as the first product's second operand
   uint32_t qb[kKs][NR][2];
@@ -325,8 +355,8 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
     {
       const int ahead = step + (R::kStages - 1) * kRowsWarps;
       const int to = stage == 0 ? R::kStages - 1 : stage - 1;
-      if (ahead < s_end) issue(ahead, page_next, to);
-      page_next = page_of(ahead + kRowsWarps);
+      if (ahead < s_end) issue(w, ahead, page_next, to);
+      page_next = page_of(w, ahead + kRowsWarps);
       copy_commit();
     }
     copy_wait<R::kStages - 1>();
@@ -579,12 +609,15 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
     __syncwarp();  // the stage is read before its next copies are issued
     stage = stage + 1 == R::kStages ? 0 : stage + 1;
   }
-  copy_wait<0>();
-  __syncthreads();  // the rings are free: they hold the warps' results now
+  // The next run's first steps are on their way while this one's results are joined.
+  const bool partial = !(w.starts() && w.ends());
+  const int pair = w.pair(tiles), ends = (w.starts() ? 1 : 0) | (w.ends() ? 2 : 0);
+  go = w.next(a, tiles);
+  if (go) fill(w);
 
   // ---- join the warps
   constexpr int kRows = 8 * NR;
-  float* so = reinterpret_cast<float*>(smem);                       // [warps][rows][DP + 4]
+  float* so = reinterpret_cast<float*>(smem + R::kBytes);           // [warps][rows][DP + 4]
   constexpr int kPitch = DP + 4;
   float* sm = so + kRowsWarps * kRows * kPitch;                     // [warps][rows] maxima, then sums
   float* sl = sm + kRowsWarps * kRows;
@@ -621,107 +654,120 @@ __global__ void __launch_bounds__(kThreads) attend_rows_kernel(AttendArgs a) {
           so[(warp * kRows + r) * kPitch + out_channel<FMT>(ct, half, g)] =
               kB ? o[ct][nr][half * 2 + i] : fmaf(o[ct][nr][half * 2 + i], times[half], add[kB ? 0 : ct >> 2]);
     }
-  pdl_trigger();
   __syncthreads();
+  const int slot = 2 * blockIdx.x + (run > 0 ? 1 : 0);
+  if (partial) {
+    slots |= run > 0 ? 2 : 1;
+    if (threadIdx.x == 0) a.part_rec[slot] = make_int4(1, pair, head, ends);
+  }
   constexpr int kQuads = DP / 4;
   for (int idx = threadIdx.x; idx < kRows * kQuads; idx += kThreads) {
     const int r = idx / kQuads, c = (idx % kQuads) * 4;
     if (row0 + r > row1) continue;
     float top = sm[r];
 #pragma unroll
-    for (int w = 1; w < kRowsWarps; ++w) top = fmaxf(top, sm[w * kRows + r]);
+    for (int x = 1; x < kRowsWarps; ++x) top = fmaxf(top, sm[x * kRows + r]);
     const float base = top == kNegInf ? 0.0f : top;
     float sum = 0.0f;
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-    for (int w = 0; w < kRowsWarps; ++w) {
-      const float f = exp2_fast(sm[w * kRows + r] - base);
-      sum += f * sl[w * kRows + r];
-      const float4 x = *reinterpret_cast<const float4*>(so + (w * kRows + r) * kPitch + c);
-      acc.x += f * x.x, acc.y += f * x.y, acc.z += f * x.z, acc.w += f * x.w;
+    for (int x = 0; x < kRowsWarps; ++x) {
+      const float f = exp2_fast(sm[x * kRows + r] - base);
+      sum += f * sl[x * kRows + r];
+      const float4 y = *reinterpret_cast<const float4*>(so + (x * kRows + r) * kPitch + c);
+      acc.x += f * y.x, acc.y += f * y.y, acc.z += f * y.z, acc.w += f * y.w;
     }
-    const int tok = a.by_share(row0 + r), hq = head * a.share + (row0 + r) - tok * a.share;
-    const int64_t row = seq.row0 + static_cast<int64_t>(tok);
-    if (a.splits > 1) {
-      const int64_t at = (row * a.q_heads + hq) * a.splits + split;
+    if (sum == 0.0f) acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // sees nothing, here or at all
+    if (partial) {
+      const int64_t at = static_cast<int64_t>(slot) * kRows + r;
       if (c < a.p.dim) *reinterpret_cast<float4*>(a.part_o + at * a.p.dim + c) = acc;
       if (c == 0) a.part_ml[at] = make_float2(top, sum);
     } else {
-      if (sum == 0.0f) acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // sees nothing
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-      if (c < a.p.dim)
-        *reinterpret_cast<uint2*>(a.out + row * a.out_row + hq * a.out_head + c) =
-            make_uint2(pack2<true>(acc.x * inv, acc.y * inv), pack2<true>(acc.z * inv, acc.w * inv));
-      if (c == 0 && a.lse) a.lse[row * a.q_heads + hq] = sum == 0.0f ? kNegInf : (top + log2f(sum)) * 0.6931471805599453f;
+      write_row(a, seq, head, row0 + r, c, acc, top, sum);
     }
+  }
+  __syncthreads();  // the results are read before the next run's are written
+  }
+  pdl_trigger();
+  if (threadIdx.x == 0) {
+    if (!(slots & 1)) a.part_rec[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
+    if (!(slots & 2)) a.part_rec[2 * blockIdx.x + 1] = make_int4(0, 0, 0, 0);
   }
 }
 
-// Joins the splits of a query row and head: a warp per (row, head), 4 channels
-// per lane; the splits' (maximum, sum) come first, 32 at a time.
-__global__ void __launch_bounds__(128) attend_combine_kernel(AttendArgs a) {
-  const int lane = threadIdx.x & 31;
-  const int b = blockIdx.y;
-  const Seq seq = sequence(a.p, b);
-  const int item = blockIdx.x * 4 + (threadIdx.x >> 5);
-  const int tok = a.by_q_heads(item), hq = item - tok * a.q_heads;
-  if (tok >= seq.n) {
-    pdl_wait();  // no block of this kernel ends before the one it joins
-    return;
-  }
-  // The row tile that the row was computed in
-  const int h = a.by_share(hq), r = tok * a.share + hq - h * a.share;
-  const int row0 = r & ~(a.tile - 1), row1 = min(row0 + a.tile, seq.n * a.share) - 1;
-  const int ns = splits_of(a, key_range<kRowsStep>(a, seq, a.by_share(row0), a.by_share(row1)));
-  const int64_t row = seq.row0 + static_cast<int64_t>(tok);
-  const int64_t at = (row * a.q_heads + hq) * a.splits;
+// Joins the parts of a row tile whose keys several blocks shared: a block for
+// each block that may start one and each row; a warp takes every fourth part,
+// 4 channels per lane, 4 parts at once.
+template <int ROWS>
+__global__ void __launch_bounds__(kThreads) attend_rows_join_kernel(AttendArgs a, int tiles, int blocks) {
+  __shared__ float2 stat[kRowsWarps];
+  __shared__ float4 sums[kRowsWarps][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = blockIdx.x, r = blockIdx.y, c = lane * 4;
+  pdl_trigger();
   pdl_wait();
+  int slot;
+  int4 rec;
+  const int n = parts_from(a, first, blocks, slot, rec);
+  if (n == 0) return;
+  const Tile x = tile_of<ROWS, kRowsStep>(a, tiles, rec.y);
+  if (r >= x.n_rows) return;
   float top = kNegInf, sum = 0.0f;
   float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  const int c = lane * 4;
-  for (int s0 = 0; s0 < ns; s0 += 32) {
-    const float2 ml = s0 + lane < ns ? a.part_ml[at + s0 + lane] : make_float2(kNegInf, 0.0f);
-    float mx = ml.x;
+  constexpr int kAtOnce = 4;
+  for (int i0 = warp; i0 < n; i0 += kRowsWarps * kAtOnce) {
+    float2 ml[kAtOnce];
+    float4 y[kAtOnce];
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-    mx = fmaxf(mx, top);
-    const float base = mx == kNegInf ? 0.0f : mx;
-    const float f0 = exp2_fast(top - base), f = exp2_fast(ml.x - base);
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int i = i0 + k * kRowsWarps;
+      const int64_t at = (i == 0 ? slot : 2 * (first + i)) * static_cast<int64_t>(ROWS) + r;
+      ml[k] = i < n ? a.part_ml[at] : make_float2(kNegInf, 0.0f);
+      y[k] = i < n && c < a.p.dim ? *reinterpret_cast<const float4*>(a.part_o + at * a.p.dim + c) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    float mx = top;
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) mx = fmaxf(mx, ml[k].x);
+    const float base = mx == kNegInf ? 0.0f : mx, f0 = exp2_fast(top - base);
     top = mx;
-    float part = f * ml.y;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
-    sum = sum * f0 + part;
+    sum *= f0;
     acc.x *= f0, acc.y *= f0, acc.z *= f0, acc.w *= f0;
-    const int n = min(32, ns - s0);
-#pragma unroll 4
-    for (int s = 0; s < n; ++s) {
-      const float w = __shfl_sync(0xffffffffu, f, s);
-      if (c < a.p.dim) {
-        const float4 x = *reinterpret_cast<const float4*>(a.part_o + (at + s0 + s) * a.p.dim + c);
-        acc.x += w * x.x, acc.y += w * x.y, acc.z += w * x.z, acc.w += w * x.w;
-      }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const float f = exp2_fast(ml[k].x - base);
+      sum += f * ml[k].y;
+      acc.x += f * y[k].x, acc.y += f * y[k].y, acc.z += f * y[k].z, acc.w += f * y[k].w;
     }
   }
+  if (lane == 0) stat[warp] = make_float2(top, sum);
+  sums[warp][lane] = acc;
+  __syncthreads();
+  if (warp != 0) return;
+#pragma unroll
+  for (int k = 1; k < kRowsWarps; ++k) {
+    const float2 ml = stat[k];
+    const float mx = fmaxf(top, ml.x), base = mx == kNegInf ? 0.0f : mx, f0 = exp2_fast(top - base), f = exp2_fast(ml.x - base);
+    const float4 y = sums[k][lane];
+    top = mx;
+    sum = sum * f0 + f * ml.y;
+    acc.x = acc.x * f0 + f * y.x, acc.y = acc.y * f0 + f * y.y, acc.z = acc.z * f0 + f * y.z, acc.w = acc.w * f0 + f * y.w;
+  }
   if (sum == 0.0f) acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // sees nothing
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  if (c < a.p.dim)
-    *reinterpret_cast<uint2*>(a.out + row * a.out_row + hq * a.out_head + c) =
-        make_uint2(pack2<true>(acc.x * inv, acc.y * inv), pack2<true>(acc.z * inv, acc.w * inv));
-  if (lane == 0 && a.lse) a.lse[row * a.q_heads + hq] = sum == 0.0f ? kNegInf : (top + log2f(sum)) * 0.6931471805599453f;
+  write_row(a, x.seq, rec.z, x.row0 + r, c, acc, top, sum);
 }
 
 template <int FMT, int DP, int NR>
 struct Kernel {
-  // The ring, or the join's buffers where those are larger.
-  static constexpr int kJoin = kRowsWarps * 8 * NR * (DP + 4 + 2) * 4;
-  static constexpr int kSmem = Ring<FMT, DP>::kBytes > kJoin ? Ring<FMT, DP>::kBytes : kJoin;
+  static constexpr int kSmem = Ring<FMT, DP>::kBytes + kRowsWarps * 8 * NR * (DP + 4 + 2) * 4;  // the rings, the warps' results
+  inline static int resident = 0;  // blocks per SM
   static cudaError_t prepare() {
-    return cudaFuncSetAttribute(attend_rows_kernel<FMT, DP, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    const cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<FMT, DP, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return e;
+    return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, attend_rows_kernel<FMT, DP, NR>, kThreads, kSmem);
   }
-  static cudaError_t launch(const AttendArgs& a, dim3 grid, cudaStream_t st) {
-    attend_rows_kernel<FMT, DP, NR><<<grid, kThreads, kSmem, st>>>(a);
-    return cudaGetLastError();
+  static cudaError_t launch(const AttendArgs& a, int blocks, cudaStream_t st) {
+    const cudaError_t e = launch_next(attend_rows_kernel<FMT, DP, NR>, dim3(blocks), kThreads, kSmem, st, a, kOneTile);
+    if (e != cudaSuccess) return e;
+    return launch_next(attend_rows_join_kernel<8 * NR>, dim3(blocks, 8 * NR), kThreads, 0, st, a, kOneTile, blocks);
   }
 };
 
@@ -735,25 +781,24 @@ cudaError_t prepare_format() {
 }
 
 template <int FMT>
-cudaError_t launch_format(const AttendArgs& a, dim3 grid, cudaStream_t st) {
+cudaError_t launch_format(const AttendArgs& a, int blocks, cudaStream_t st) {
   if (a.p.dim <= 64)
-    return a.tile == 8 ? Kernel<FMT, 64, 1>::launch(a, grid, st) : Kernel<FMT, 64, 2>::launch(a, grid, st);
-  return a.tile == 8 ? Kernel<FMT, 128, 1>::launch(a, grid, st) : Kernel<FMT, 128, 2>::launch(a, grid, st);
+    return a.tile == 8 ? Kernel<FMT, 64, 1>::launch(a, blocks, st) : Kernel<FMT, 64, 2>::launch(a, blocks, st);
+  return a.tile == 8 ? Kernel<FMT, 128, 1>::launch(a, blocks, st) : Kernel<FMT, 128, 2>::launch(a, blocks, st);
 }
 
 template <int FMT>
-int ctas(int dim) {
-  const int bytes = dim <= 64 ? Ring<FMT, 64>::kBytes : Ring<FMT, 128>::kBytes;
-  const int n = (227 << 10) / (bytes + 1024);
-  return n > kMaxCtas ? kMaxCtas : n;
+int resident(int dim, int tile) {
+  if (dim <= 64) return tile == 8 ? Kernel<FMT, 64, 1>::resident : Kernel<FMT, 64, 2>::resident;
+  return tile == 8 ? Kernel<FMT, 128, 1>::resident : Kernel<FMT, 128, 2>::resident;
 }
 
 }  // namespace
 
 int attend_rows_tile(int rows) { return rows <= 8 ? 8 : 16; }
 
-int attend_rows_ctas(int fmt, int dim) {
-  return fmt == kBf16 ? ctas<kBf16>(dim) : fmt == kU8 ? ctas<kU8>(dim) : ctas<kU4>(dim);
+int attend_rows_resident(int fmt, int dim, int tile) {
+  return fmt == kBf16 ? resident<kBf16>(dim, tile) : fmt == kU8 ? resident<kU8>(dim, tile) : resident<kU4>(dim, tile);
 }
 
 cudaError_t attend_rows_prepare() {
@@ -763,29 +808,12 @@ cudaError_t attend_rows_prepare() {
   return e;
 }
 
-cudaError_t launch_attend_rows(const AttendArgs& a, cudaStream_t st) {
-  const int tiles = static_cast<int>((static_cast<int64_t>(a.p.max_rows) * a.share + a.tile - 1) / a.tile);
-  const dim3 grid(static_cast<unsigned>(a.splits) * tiles, static_cast<unsigned>(a.p.heads),
-                  static_cast<unsigned>(a.p.n_seqs));
+cudaError_t launch_attend_rows(const AttendArgs& a, int blocks, cudaStream_t st) {
   switch (a.p.fmt) {
-    case kBf16: return launch_format<kBf16>(a, grid, st);
-    case kU8: return launch_format<kU8>(a, grid, st);
-    default: return launch_format<kU4>(a, grid, st);
+    case kBf16: return launch_format<kBf16>(a, blocks, st);
+    case kU8: return launch_format<kU8>(a, blocks, st);
+    default: return launch_format<kU4>(a, blocks, st);
   }
-}
-
-cudaError_t launch_attend_combine(const AttendArgs& a, cudaStream_t st) {
-  const int64_t items = static_cast<int64_t>(a.p.max_rows) * a.q_heads;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>((items + 3) / 4), static_cast<unsigned>(a.p.n_seqs));
-  cfg.blockDim = dim3(128);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, attend_combine_kernel, a);
 }
 
 }  // namespace ipv

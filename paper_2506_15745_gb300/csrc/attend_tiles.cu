@@ -27,6 +27,7 @@
 #include <cuda.h>
 #include <cuda_fp16.h>
 
+#include "attend_share.cuh"
 #include "paged.cuh"
 
 namespace ipv {
@@ -37,8 +38,9 @@ __device__ unsigned g_attend_error;
 
 namespace {
 
-constexpr int kRowsCta = kTilesRows;  // query rows of a block
+constexpr int kRowsCta = kTilesRows;  // query rows of a tile of work
 constexpr int kKeys = kTilesStep;     // keys of a step
+constexpr int kRunCost = 3;           // what a run of steps costs beside them, in steps
 constexpr int kMmaWarp = 8, kLoadWarp = 10;  // warps 8, 9: products of query tiles 0, 1; 10, 11: copies of K, V
 constexpr int kThreads = 384;                // two softmax warpgroups, one for copies and products
 constexpr int kHalf = 128 * 128;      // bytes of 128 rows x 64 channels
@@ -258,154 +260,6 @@ __device__ __forceinline__ constexpr uint32_t instr(int n, bool b_mn) {
          (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(128 >> 4) << 24);
 }
 
-// ------------------------------------------------------------------ work
-// A tile of 256 query rows of a sequence: pair number p = sequence * tiles + tile.
-struct Tile {
-  Seq seq;
-  int b, row0, n_rows, steps;
-  KeyRange kr;
-};
-
-__device__ __forceinline__ void set_tile(const AttendArgs& a, Tile& x, int b, int tile) {
-  x.row0 = tile * kRowsCta;
-  x.n_rows = min(kRowsCta, x.seq.n * a.share - x.row0);
-  x.b = b;
-  x.steps = 0;
-  if (x.n_rows > 0) {
-    x.kr = key_range<kKeys>(a, x.seq, a.by_share(x.row0), a.by_share(x.row0 + x.n_rows - 1));
-    x.steps = max(1, x.kr.steps);  // rows that see nothing have their results to write, too
-  }
-}
-__device__ __forceinline__ Tile tile_of(const AttendArgs& a, int tiles, int p) {
-  Tile x;
-  const int b = a.by_tiles(p);
-  x.seq = sequence(a.p, b);
-  set_tile(a, x, b, p - b * tiles);
-  return x;
-}
-
-// What a block shares out: a tile's keys for one KV head weigh their steps and
-// kRunCost more, about what loading the queries, filling the pipeline and
-// writing the results take.
-constexpr int kRunCost = 3;
-
-// A block's share: from step s of KV head `head` of pair p, as far as `left`
-// units of weight go. Heads of a pair follow one another, then pairs.
-struct Share {
-  int p, head;
-  int64_t at, left;  // units into the pair's head, units left
-};
-
-// Walks a share, a run of steps of one (pair, head) at a time. A boundary within
-// the first kRunCost units leaves all steps to the block behind it.
-struct Walk {
-  Tile t;
-  int head, s, n;  // steps s .. s + n - 1
-  int64_t left;
-  __device__ __forceinline__ void cut(int64_t at) {
-    const int64_t weight = t.steps + kRunCost, upto = min(weight, at + left);
-    s = static_cast<int>(max(int64_t{0}, at - kRunCost));
-    n = static_cast<int>(max(int64_t{0}, upto - kRunCost)) - s;
-    left -= upto - at;
-  }
-  __device__ __forceinline__ bool begin(const AttendArgs& a, int tiles, const Share& w) {
-    t = tile_of(a, tiles, w.p);
-    head = w.head;
-    left = w.left;
-    cut(w.at);
-    return n > 0 || next(a, tiles);
-  }
-  __device__ __forceinline__ bool next(const AttendArgs& a, int tiles) {
-    if (left <= 0) return false;
-    if (++head == a.p.heads) {
-      head = 0;
-      int tile = t.row0 / kRowsCta, b = t.b;
-      do {
-        if (++tile == tiles) {
-          tile = 0;
-          if (++b == a.p.n_seqs) return false;  // only if the lengths changed under the kernel
-          t.seq = sequence(a.p, b);
-        }
-        set_tile(a, t, b, tile);
-      } while (t.steps == 0);
-    }
-    cut(0);
-    return n > 0;
-  }
-  __device__ __forceinline__ bool starts() const { return s == 0; }
-  __device__ __forceinline__ bool ends() const { return s + n == t.steps; }
-  __device__ __forceinline__ int pair(int tiles) const { return t.b * tiles + t.row0 / kRowsCta; }
-  // Rows of the last V tile from `keep` on lie past the last key.
-  __device__ __forceinline__ int keep() const { return t.kr.hi_max - t.kr.key0<kKeys>(s + n - 1); }
-};
-
-// 64-bit numbers that mostly fit 32 bits.
-__device__ __forceinline__ int64_t divide(int64_t x, int64_t d) {
-  if (static_cast<uint64_t>(x | d) >> 32 == 0) return static_cast<uint32_t>(x) / static_cast<uint32_t>(d);
-  return x / d;
-}
-
-// Finds the block's share, with all threads; scratch: 16 64-bit words of shared memory.
-__device__ Share find_share(const AttendArgs& a, int tiles, int64_t* scratch) {
-  const int pairs = a.p.n_seqs * tiles, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  constexpr int kWarps = kThreads / 32;
-  auto weight = [&](int p) {
-    const int steps = p < pairs ? tile_of(a, tiles, p).steps : 0;
-    return steps > 0 ? static_cast<int64_t>(steps + kRunCost) * a.p.heads : int64_t{0};
-  };
-  const int64_t first = weight(threadIdx.x);
-  int64_t sum = first;
-  for (int p = threadIdx.x + kThreads; p < pairs; p += kThreads) sum += weight(p);
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-  if (lane == 0) scratch[warp] = sum;
-  __syncthreads();
-  int64_t total = 0;
-#pragma unroll
-  for (int i = 0; i < kWarps; ++i) total += scratch[i];
-  int64_t per = divide(total + gridDim.x - 1, gridDim.x);
-  if (per < a.unit + kRunCost) per = a.unit + kRunCost;
-  const int64_t from = per * blockIdx.x;
-  Share w;
-  w.left = min(per, total - from);
-  w.p = w.head = 0;
-  w.at = 0;
-  __syncthreads();
-  if (w.left <= 0) return w;
-  int64_t before = 0;
-  for (int p0 = 0; p0 < pairs; p0 += kThreads) {
-    const int64_t mine = p0 == 0 ? first : weight(p0 + threadIdx.x);
-    int64_t upto = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int64_t y = __shfl_up_sync(0xffffffffu, upto, d);
-      if (lane >= d) upto += y;
-    }
-    if (lane == 31) scratch[warp] = upto;
-    __syncthreads();
-    int64_t start = before, all = before;
-#pragma unroll
-    for (int i = 0; i < kWarps; ++i) {
-      if (i < warp) start += scratch[i];
-      all += scratch[i];
-    }
-    start += upto - mine;
-    if (from >= start && from < start + mine) {
-      const int64_t one = divide(mine, a.p.heads), head = divide(from - start, one);
-      scratch[kWarps] = p0 + threadIdx.x;
-      scratch[kWarps + 1] = head;
-      scratch[kWarps + 2] = from - start - head * one;
-    }
-    __syncthreads();
-    if (from < all) break;
-    before = all;
-  }
-  w.p = static_cast<int>(scratch[kWarps]);
-  w.head = static_cast<int>(scratch[kWarps + 1]);
-  w.at = scratch[kWarps + 2];
-  return w;
-}
-
 // ------------------------------------------------------------------ kernel
 template <bool BF16, int DP>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -415,7 +269,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023) & ~1023u;
   unsigned char* base_p = smem_raw + (base - smem_u32(smem_raw));
-  const Share share = find_share(a, tiles, reinterpret_cast<int64_t*>(base_p + L::kScale));
+  pdl_wait();
+  const Share share = find_share<kRowsCta, kKeys, kRunCost, kThreads>(a, tiles, reinterpret_cast<int64_t*>(base_p + L::kScale));
   if (share.left <= 0) {
     if (threadIdx.x < 2) a.part_rec[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
     return;
@@ -443,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   fence_after();
   constexpr uint32_t tmem = 0;  // all 512 columns are the block's: they start at 0
-  Walk w = {};
+  Walk<kRowsCta, kKeys, kRunCost> w = {};
 
   // Registers: 384 threads start with 168 each; 256 take 224 (a row's 128 scores
   // stay in registers), 128 keep 56: the same 64512 in all.
@@ -588,7 +443,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // A run's query tile into shared memory, swizzled; rows that are not there
     // are zero. A warp loads its own 32 rows. Called when the products that read
     // the tile before it are over.
-    auto load_queries = [&](const Walk& x) {
+    auto load_queries = [&](const Walk<kRowsCta, kKeys, kRunCost>& x) {
       if (x.t.n_rows <= 128 * t) return;
       constexpr int kCh = DP / 8, kBatch = 8;
       const int row0 = x.t.row0 + 128 * t, n_rows = x.t.n_rows - 128 * t;
@@ -642,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool go = w.begin(a, tiles, share);
     if (go) load_queries(w);
     while (go) {
-      Walk after = w;
+      Walk<kRowsCta, kKeys, kRunCost> after = w;
       const bool partial = !(w.starts() && w.ends());
       const int slot = 2 * blockIdx.x + (run > 0 ? 1 : 0);
       ++run;
@@ -839,18 +694,13 @@ __global__ void __launch_bounds__(128) attend_tiles_join_kernel(AttendArgs a, in
   __shared__ __align__(16) uint2 rows[32][17];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x;
   const int r0 = blockIdx.y * 32, r = r0 + lane, quads = a.p.dim / 4, quad0 = 16 * blockIdx.z + 4 * warp;
+  pdl_trigger();
   pdl_wait();
-  const int4 one = a.part_rec[2 * c], two = a.part_rec[2 * c + 1];
-  int n = 0;  // parts: up to the first that ends its tile
-  for (int i0 = 1; n == 0; i0 += 32) {
-    const int blk = c + i0 + lane;
-    const uint32_t last = __ballot_sync(0xffffffffu, blk >= blocks || (a.part_rec[2 * blk].w & 2));
-    if (last) n = i0 + __ffs(last);
-  }
-  const int slot = two.x && two.w == 1 ? 2 * c + 1 : one.x && one.w == 1 ? 2 * c : -1;  // started here, not ended
-  if (slot < 0) return;
-  const int4 rec = slot & 1 ? two : one;
-  const Tile x = tile_of(a, tiles, rec.y);
+  int slot;
+  int4 rec;
+  const int n = parts_from(a, c, blocks, slot, rec);
+  if (n == 0) return;
+  const Tile x = tile_of<kRowsCta, kKeys>(a, tiles, rec.y);
   const int n_rows = min(32, x.n_rows - r0);
   if (n_rows <= 0) return;
   float top = kNegInf, sum = 0.0f;
@@ -935,8 +785,7 @@ cudaError_t prepare_one() {
 template <bool BF16, int DP>
 cudaError_t launch_one(const AttendArgs& a, const CUtensorMap& km, const CUtensorMap& vm, int tiles, int box_rows, int64_t limit_ns,
                        unsigned grid, cudaStream_t st) {
-  attend_tiles_kernel<BF16, DP><<<grid, kThreads, Layout<DP>::kBytes, st>>>(a, km, vm, tiles, box_rows, limit_ns);
-  return cudaGetLastError();
+  return launch_next(attend_tiles_kernel<BF16, DP>, dim3(grid), kThreads, Layout<DP>::kBytes, st, a, km, vm, tiles, box_rows, limit_ns);
 }
 
 }  // namespace
@@ -976,16 +825,7 @@ cudaError_t launch_attend_tiles(const AttendArgs& a, bool bf16, const TileMaps& 
     e = bf16 ? launch_one<true, 128>(a, km, vm, tiles, maps.box_rows, limit_ns, blocks, st)
              : launch_one<false, 128>(a, km, vm, tiles, maps.box_rows, limit_ns, blocks, st);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(blocks), kRowsCta / 32, a.p.dim <= 64 ? 1 : 2);
-  cfg.blockDim = dim3(128);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, attend_tiles_join_kernel, a, tiles, blocks);
+  return launch_next(attend_tiles_join_kernel, dim3(blocks, kRowsCta / 32, a.p.dim <= 64 ? 1 : 2), 128, 0, st, a, tiles, blocks);
 }
 
 cudaError_t attend_tiles_error(unsigned* bits) {

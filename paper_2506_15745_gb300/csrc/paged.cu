@@ -167,7 +167,6 @@ ipv_status check_attend(const ipv_pages* p, const ipv_batch* b, const ipv_attend
   a->q_heads = t->n_q_heads;
   a->share = t->n_q_heads / p->n_kv_heads;
   a->by_share = ipv::Divide(a->share);
-  a->by_q_heads = ipv::Divide(a->q_heads);
   a->by_tiles = ipv::Divide(tiles > 0 ? static_cast<int>(tiles) : 1);
   a->scale_log2 = t->scale * 1.4426950408889634f;
   a->causal = t->causal;
@@ -184,30 +183,29 @@ std::atomic<int64_t> g_limit_ns{kDefaultLimitNs};
 // kernel reads K and V once per 16 query rows.
 constexpr int64_t kTilesFrom = 17;
 
-// Fewest steps of a block's share in the tiled kernel.
-constexpr int kTilesLeast = 2;
+// Fewest steps of a block's share: below, joining parts costs more than the
+// other blocks save.
+constexpr int kTilesLeast = 2, kRowsLeast = 8;
 
-// Which kernel takes the call, its split of the keys, and the workspace.
+// Which kernel takes the call, on how many blocks, and the workspace.
 struct Plan {
   bool tiles = false;
-  int blocks = 0;      // tiled kernel
+  int blocks = 0;
   ipv::TileMaps maps;  // tiled kernel: made only when launching
   int64_t k16 = 0, v16 = 0, part_o = 0, part_ml = 0, part_rec = 0, bytes = 0;  // offsets in the workspace
 };
 
 int64_t round256(int64_t x) { return (x + 255) & ~int64_t{255}; }
 
-// a: checked arguments; the plan's tile, step, unit and splits go into it.
+// a: checked arguments; the plan's tile and unit go into it.
 void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
   const ipv::Pages& p = a->p;
   const int64_t rows = static_cast<int64_t>(p.max_rows) * a->share;
   plan->tiles = rows >= kTilesFrom;
   plan->bytes = 0;
-  int64_t parts = 0;
   if (plan->tiles) {
     a->tile = ipv::kTilesRows;
     a->unit = kTilesLeast;
-    a->splits = 1;
     plan->blocks = num_sms;
     if (p.fmt != ipv::kBf16) {
       const int64_t one = round256(static_cast<int64_t>(p.n_seqs) * p.heads * p.max_kv * p.dim * 2);
@@ -215,34 +213,16 @@ void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
       plan->v16 = one;
       plan->bytes = 2 * one;
     }
-    parts = static_cast<int64_t>(plan->blocks) * 2 * ipv::kTilesRows;
   } else {
-    // Each split costs a partial result, written and read again: as many as fill the device.
     a->tile = ipv::attend_rows_tile(static_cast<int>(rows));
-    const int64_t slots = static_cast<int64_t>(num_sms) * ipv::attend_rows_ctas(p.fmt, p.dim) * (p.n_seqs > 1 ? 4 : 1);
-    const int64_t tiles = (rows + a->tile - 1) / a->tile;
-    int64_t span = p.max_kv;
-    if (a->window) {  // the tile's tokens' windows, the sinks, and a step's slack at each of the three ends
-      const int64_t seen = static_cast<int64_t>(a->window) + a->tile + a->sinks + 3 * ipv::kRowsStep;
-      if (seen < span) span = seen;
-    }
-    const int64_t steps = (span + ipv::kRowsStep - 1) / ipv::kRowsStep;
-    const int64_t blocks = tiles * p.heads * p.n_seqs;
-    int64_t want = slots / blocks;
-    if (want < 1) want = 1;
-    int64_t unit = (steps + want - 1) / want;
-    unit = (unit + ipv::kRowsWarps - 1) / ipv::kRowsWarps * ipv::kRowsWarps;
-    if (unit < ipv::kRowsWarps) unit = ipv::kRowsWarps;
-    a->unit = static_cast<int>(unit);
-    a->splits = static_cast<int>(steps > 0 ? (steps + unit - 1) / unit : 1);
-    if (a->splits > 1) parts = p.total_rows * a->q_heads * a->splits;
+    a->unit = kRowsLeast;
+    plan->blocks = num_sms * ipv::attend_rows_resident(p.fmt, p.dim, a->tile);
   }
-  if (parts > 0) {
-    plan->part_o = plan->bytes;
-    plan->part_ml = plan->part_o + round256(parts * p.dim * 4);
-    plan->part_rec = plan->part_ml + round256(parts * 8);
-    plan->bytes = plan->part_rec + (plan->tiles ? round256(static_cast<int64_t>(plan->blocks) * 2 * 16) : 0);
-  }
+  const int64_t parts = static_cast<int64_t>(plan->blocks) * 2 * a->tile;
+  plan->part_o = plan->bytes;
+  plan->part_ml = plan->part_o + round256(parts * p.dim * 4);
+  plan->part_rec = plan->part_ml + round256(parts * 8);
+  plan->bytes = plan->part_rec + round256(static_cast<int64_t>(plan->blocks) * 2 * 16);
 }
 
 // The fp16 rows that codes are widened into, as a pool of one page per sequence.
@@ -368,10 +348,9 @@ extern "C" ipv_status ipv_attend(const ipv_pages* pages, const ipv_batch* batch,
     if (!ipv::attend_tiles_maps(a, bf16, &plan.maps)) return reject(IPV_ECUDA, "cuTensorMapEncodeTiled refused the pool");
     e = ipv::launch_attend_tiles(a, bf16, plan.maps, plan.blocks, g_limit_ns.load(), st);
   } else {
-    e = ipv::launch_attend_rows(a, st);
+    e = ipv::launch_attend_rows(a, plan.blocks, st);
   }
   if (e != cudaSuccess) return cuda_reject(e, "attention kernel");
-  if (a.splits > 1 && (e = ipv::launch_attend_combine(a, st)) != cudaSuccess) return cuda_reject(e, "split join kernel");
   return IPV_OK;
 }
 

@@ -62,6 +62,24 @@ __device__ __forceinline__ int64_t pool_row(const Pages& p, int b, int j) {
   return g * p.page_stride + (p.page_shift == 31 ? j : j & (p.page_size - 1)) * p.row_stride;
 }
 
+// Every kernel of the paged cache is launched to overlap its predecessor's end: it
+// waits with pdl_wait() before it reads or writes anything, and lets its own
+// successor be launched with pdl_trigger().
+template <typename... Params, typename... Args>
+cudaError_t launch_next(void (*kernel)(Params...), dim3 grid, unsigned block, size_t smem, cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // Division of 0 <= x < 2^31 by a fixed 1 <= d < 2^31 as a multiplication:
 // x / d = x * m >> 31 + s with s = ceil(log2 d), m = ceil(2^(31 + s) / d); m is
 // too large by less than 2^s / 2^(31 + s) of itself, which x cannot make a unit.
@@ -86,18 +104,15 @@ struct AttendArgs {
   float* lse;
   int64_t q_row, q_head, out_row, out_head;  // strides in elements
   int q_heads, share;   // query heads; query heads per KV head
-  Divide by_share, by_q_heads, by_tiles;  // tiles: row tiles of max_rows (tiled kernel)
+  Divide by_share, by_tiles;  // tiles: 256-row tiles of max_rows
   float scale_log2;     // scale * log2(e)
   int causal, window, sinks;
-  // Keys are split: into at most `unit` steps (rows kernel), or
-  // where a block's share of the steps, at least `unit`, ends (tiled kernel).
-  int unit, splits;  // splits: most that any row tile has (rows kernel)
-  int tile;                // query rows of a row tile
-  // Partial results: unnormalised sums and (running maximum, sum).
-  // Rows kernel: [total_rows * q_heads][splits][dim] and [..][splits].
-  // Tiled kernel: [blocks][2][dim / 4][kTilesRows][4] and [blocks][2][kTilesRows],
-  // with a record [blocks][2]: (1 or 0: none, pair of sequence and tile, KV head,
-  // 1: a tile's start + 2: its end).
+  int unit;  // fewest steps of a block's share
+  int tile;  // query rows of a row tile
+  // Partial results, for each block's first and last run: unnormalised sums
+  // (rows kernel: [blocks][2][tile][dim], tiled kernel: [blocks][2][dim / 4][tile][4]),
+  // (running maximum, sum) [blocks][2][tile], and a record [blocks][2]: (1, or 0:
+  // none, pair of sequence and tile, KV head, 1: a tile's start + 2: its end).
   float* part_o;
   float2* part_ml;
   int4* part_rec;
@@ -134,10 +149,6 @@ __device__ __forceinline__ KeyRange key_range(const AttendArgs& a, const Seq& s,
   return r;
 }
 
-__device__ __forceinline__ int splits_of(const AttendArgs& a, const KeyRange& r) {
-  return r.steps > 0 ? (r.steps - 1) / a.unit + 1 : 1;
-}
-
 // ------------------------------------------------------------------ launches
 struct RowsArgs {
   Pages p;
@@ -162,13 +173,12 @@ struct ExpandArgs {
 };
 cudaError_t launch_pages_expand(const ExpandArgs& a, cudaStream_t st);
 
-int attend_rows_tile(int rows);               // query rows of a row tile
-int attend_rows_ctas(int fmt, int dim);       // resident blocks per SM (smem)
+int attend_rows_tile(int rows);               // query rows of a row tile, for at most 16
+int attend_rows_resident(int fmt, int dim, int tile);  // blocks per SM, after attend_rows_prepare
 constexpr int kRowsStep = 32;                 // keys of a step
 constexpr int kRowsWarps = 4;
 cudaError_t attend_rows_prepare();            // once per device
-cudaError_t launch_attend_rows(const AttendArgs& a, cudaStream_t st);
-cudaError_t launch_attend_combine(const AttendArgs& a, cudaStream_t st);
+cudaError_t launch_attend_rows(const AttendArgs& a, int blocks, cudaStream_t st);
 
 // Many query rows (attend_tiles.cu): the pool's rows are 16-bit elements.
 constexpr int kTilesRows = 256;  // query rows of a tile of work

@@ -138,6 +138,8 @@ __device__ __forceinline__ Item item_of(const RowsArgs& a, const Seq& s, int b, 
 
 template <int FMT, int U>
 __global__ void __launch_bounds__(kBlock) write_kernel(RowsArgs a) {
+  pdl_trigger();
+  pdl_wait();
   const int b = blockIdx.y;
   const Seq s = sequence(a.p, b);
   const unsigned items = static_cast<unsigned>(s.n) * a.p.heads * a.p.groups;
@@ -191,6 +193,8 @@ __global__ void __launch_bounds__(kBlock) write_kernel(RowsArgs a) {
 
 template <int FMT, int U>
 __global__ void __launch_bounds__(kBlock) read_kernel(RowsArgs a) {
+  pdl_trigger();
+  pdl_wait();
   const int b = blockIdx.y;
   const Seq s = sequence(a.p, b);
   const unsigned items = static_cast<unsigned>(s.n) * a.p.heads * a.p.groups;
@@ -244,6 +248,8 @@ __global__ void __launch_bounds__(kBlock) read_kernel(RowsArgs a) {
 // written in order.
 template <int FMT, int U>
 __global__ void __launch_bounds__(kBlock) expand_kernel(ExpandArgs a) {
+  pdl_trigger();
+  pdl_wait();
   const int b = blockIdx.z, h = blockIdx.y;
   const Seq s = sequence(a.p, b);
   if (s.n == 0) return;
@@ -299,21 +305,19 @@ dim3 grid_of(const RowsArgs& a) {
 cudaError_t launch_pages_write(const RowsArgs& a, cudaStream_t st) {
   const dim3 g = grid_of<2>(a);
   switch (a.p.fmt) {
-    case kBf16: write_kernel<kBf16, 2><<<g, kBlock, 0, st>>>(a); break;
-    case kU8: write_kernel<kU8, 2><<<g, kBlock, 0, st>>>(a); break;
-    default: write_kernel<kU4, 2><<<g, kBlock, 0, st>>>(a); break;
+    case kBf16: return launch_next(write_kernel<kBf16, 2>, g, kBlock, 0, st, a);
+    case kU8: return launch_next(write_kernel<kU8, 2>, g, kBlock, 0, st, a);
+    default: return launch_next(write_kernel<kU4, 2>, g, kBlock, 0, st, a);
   }
-  return cudaGetLastError();
 }
 
 cudaError_t launch_pages_read(const RowsArgs& a, cudaStream_t st) {
   const dim3 g = grid_of<2>(a);
   switch (a.p.fmt) {
-    case kBf16: read_kernel<kBf16, 2><<<g, kBlock, 0, st>>>(a); break;
-    case kU8: read_kernel<kU8, 2><<<g, kBlock, 0, st>>>(a); break;
-    default: read_kernel<kU4, 2><<<g, kBlock, 0, st>>>(a); break;
+    case kBf16: return launch_next(read_kernel<kBf16, 2>, g, kBlock, 0, st, a);
+    case kU8: return launch_next(read_kernel<kU8, 2>, g, kBlock, 0, st, a);
+    default: return launch_next(read_kernel<kU4, 2>, g, kBlock, 0, st, a);
   }
-  return cudaGetLastError();
 }
 
 cudaError_t launch_pages_expand(const ExpandArgs& a, cudaStream_t st) {
@@ -322,10 +326,8 @@ cudaError_t launch_pages_expand(const ExpandArgs& a, cudaStream_t st) {
   const dim3 g(static_cast<unsigned>((items + kTeams * kU - 1) / (kTeams * kU)), static_cast<unsigned>(a.p.heads),
                static_cast<unsigned>(a.p.n_seqs));
   if (a.p.fmt == kU8)
-    expand_kernel<kU8, kU><<<g, kBlock, 0, st>>>(a);
-  else
-    expand_kernel<kU4, kU><<<g, kBlock, 0, st>>>(a);
-  return cudaGetLastError();
+    return launch_next(expand_kernel<kU8, kU>, g, kBlock, 0, st, a);
+  return launch_next(expand_kernel<kU4, kU>, g, kBlock, 0, st, a);
 }
 
 }  // namespace ipv
