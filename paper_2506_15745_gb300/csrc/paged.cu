@@ -258,6 +258,7 @@ extern "C" ipv_status ipv_pages_write(const ipv_pages* pages, const ipv_batch* b
   a.v_new = static_cast<const uint16_t*>(v_new);
   a.row = row_stride;
   a.head = head_stride;
+  a.by_heads = ipv::Divide(a.p.heads);
   const cudaError_t e = ipv::launch_pages_write(a, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? IPV_OK : cuda_reject(e, "page write kernel");
 }
@@ -276,6 +277,7 @@ extern "C" ipv_status ipv_pages_read(const ipv_pages* pages, const ipv_batch* ba
   a.v_out = static_cast<uint16_t*>(v_out);
   a.row = row_stride;
   a.head = head_stride;
+  a.by_heads = ipv::Divide(a.p.heads);
   const cudaError_t e = ipv::launch_pages_read(a, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? IPV_OK : cuda_reject(e, "page read kernel");
 }

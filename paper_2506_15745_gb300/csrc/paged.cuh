@@ -10,6 +10,22 @@
 
 namespace ipv {
 
+// Division of 0 <= x < 2^31 by a fixed 1 <= d < 2^31 as a multiplication:
+// x / d = x * m >> 31 + s with s = ceil(log2 d), m = ceil(2^(31 + s) / d); m is
+// too large by less than 2^s / 2^(31 + s) of itself, which x cannot make a unit.
+struct Divide {
+  uint32_t m = 0;
+  int s = 0, d = 1;
+  Divide() = default;
+  explicit Divide(int by) : d(by) {
+    while ((int64_t{1} << s) < by) ++s;
+    m = static_cast<uint32_t>(((uint64_t{1} << (31 + s)) + by - 1) / by);
+  }
+  __device__ __forceinline__ int operator()(int x) const {
+    return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(x)) * m) >> (31 + s));
+  }
+};
+
 enum : int { kBf16 = 0, kU8 = 1, kU4 = 2 };  // ipv_pages_format
 
 constexpr int kGroup = 64;            // channels that share a step and a minimum
@@ -80,22 +96,6 @@ cudaError_t launch_next(void (*kernel)(Params...), dim3 grid, unsigned block, si
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// Division of 0 <= x < 2^31 by a fixed 1 <= d < 2^31 as a multiplication:
-// x / d = x * m >> 31 + s with s = ceil(log2 d), m = ceil(2^(31 + s) / d); m is
-// too large by less than 2^s / 2^(31 + s) of itself, which x cannot make a unit.
-struct Divide {
-  uint32_t m = 0;
-  int s = 0, d = 1;
-  Divide() = default;
-  explicit Divide(int by) : d(by) {
-    while ((int64_t{1} << s) < by) ++s;
-    m = static_cast<uint32_t>(((uint64_t{1} << (31 + s)) + by - 1) / by);
-  }
-  __device__ __forceinline__ int operator()(int x) const {
-    return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(x)) * m) >> (31 + s));
-  }
-};
-
 // ------------------------------------------------------------------ attention
 struct AttendArgs {
   Pages p;
@@ -157,7 +157,7 @@ struct RowsArgs {
   uint16_t* k_out;
   uint16_t* v_out;
   int64_t row, head;  // strides of the packed rows, elements
-  int num_sms;
+  Divide by_heads;
 };
 cudaError_t launch_pages_write(const RowsArgs& a, cudaStream_t st);
 cudaError_t launch_pages_read(const RowsArgs& a, cudaStream_t st);

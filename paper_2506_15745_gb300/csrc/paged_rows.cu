@@ -22,70 +22,77 @@ __device__ __forceinline__ int place_u8(int word) { return 4 * (word & 3) + (wor
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+// 2^23 in fp32: 2^23 + u has the integer u in its low bits.
+constexpr uint32_t kTwo23 = 0x4B000000u;
+
+__device__ __forceinline__ uint32_t min_bf16x2(uint32_t a, uint32_t b) {  // NaN wins
+  uint32_t r;
+  asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
 // Quantises a lane's 8 channels with its team's other 56: codes in w (one word
 // at 4 bits, two at 8), the group's (step, minimum) in the return value.
 template <int FMT>
 __device__ __forceinline__ uint32_t quantise(const uint4& x, uint32_t (&w)[2]) {
   constexpr float kLevels = FMT == kU8 ? 255.0f : 15.0f;
+  constexpr uint32_t kSigns = 0x80008000u;
   const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
-  float f[8];
+  // The group's minimum, and its maximum as the minimum of the negated values, as
+  // two halves of one word.
+  const uint32_t lo2 = min_bf16x2(min_bf16x2(xs[0], xs[1]), min_bf16x2(xs[2], xs[3]));
+  const uint32_t hi2 = min_bf16x2(min_bf16x2(xs[0] ^ kSigns, xs[1] ^ kSigns), min_bf16x2(xs[2] ^ kSigns, xs[3] ^ kSigns));
+  uint32_t ends = min_bf16x2(__byte_perm(lo2, hi2, 0x5410), __byte_perm(lo2, hi2, 0x7632));
 #pragma unroll
-  for (int i = 0; i < 4; ++i) f[2 * i] = lo_f(xs[i]), f[2 * i + 1] = hi_f(xs[i]);
-  float lo = f[0], hi = f[0], far = 0.0f;
-  bool bad = false;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    lo = fminf(lo, f[i]);
-    hi = fmaxf(hi, f[i]);
-    bad |= !(fabsf(f[i]) <= kLargest);  // NaN too
-  }
-#pragma unroll
-  for (int d = 1; d < 8; d <<= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
-  }
-  const uint32_t any = __ballot_sync(0xffffffffu, bad) >> (threadIdx.x & 24);
-  if (any & 0xffu) {
+  for (int d = 1; d < 8; d <<= 1) ends = min_bf16x2(ends, __shfl_xor_sync(0xffffffffu, ends, d));
+  const float lo = lo_f(ends), hi = -hi_f(ends);
+  if (!(lo >= -kLargest && hi <= kLargest)) {  // NaN too
     w[0] = w[1] = 0;
     return 0x7FFF7FFFu;  // (NaN, NaN)
   }
   const __half hm = __float2half_rd(lo);
-  const float m = __half2float(hm);
-  const __half hs = __float2half_ru((hi - m) / kLevels);
-  const float s = __half2float(hs);
-  // u = rint((x - m) / s). The product with 1/s is within 3e-5 of the quotient,
-  // so it rounds to the same integer unless it lies that near a half: only then
-  // is the division done.
-  const float inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
-  float u[8];
+  const float m = __half2float(hm), range = hi - m;
+  // The step: range / levels rounded up to fp16. A nearest neighbour of the
+  // quotient that is below it (its product with the levels is exact) moves up.
+  unsigned short hs = __half_as_ushort(__float2half_rn(range * (1.0f / kLevels)));
+  if (fmaf(__half2float(__ushort_as_half(hs)), kLevels, -range) < 0.0f) ++hs;
+  const float s = __half2float(__ushort_as_half(hs));
+  // u = rint((x - m) / s). The product with about 1/s is within 1e-4 of the
+  // quotient, so it rounds to the same integer unless it lies that near a half:
+  // only then is the division done. Adding 1.5 * 2^23 rounds; the integer is in
+  // the sum's low bits.
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+  inv = s > 0.0f ? inv : 0.0f;
+  constexpr float kRound = 12582912.0f;
+  uint32_t u[8];
+  float far = 0.0f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float q = (f[i] - m) * inv;
-    u[i] = fminf(rintf(q), kLevels);
-    far = fmaxf(far, fabsf(q - u[i]));
+    const float d = ((i & 1) ? hi_f(xs[i >> 1]) : lo_f(xs[i >> 1])) - m;
+    const float r = fmaf(d, inv, kRound);
+    far = fmaxf(far, fabsf(fmaf(d, inv, kRound - r)));
+    u[i] = __float_as_uint(r);
   }
   if (far > 0.4999f) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) u[i] = s > 0.0f ? fminf(rintf((f[i] - m) / s), kLevels) : 0.0f;
+    for (int i = 0; i < 8; ++i)
+      u[i] = __float_as_uint((s > 0.0f ? (((i & 1) ? hi_f(xs[i >> 1]) : lo_f(xs[i >> 1])) - m) / s : 0.0f) + kRound);
   }
+  // Words by multiplication: what stands above the codes is the same every time.
+  constexpr uint32_t kBits = 0x4B400000u;  // of 1.5 * 2^23
   if (FMT == kU8) {
-    // Two codes at a time: u0 + 256 u1 is exact in fp32.
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t a = static_cast<uint32_t>(fmaf(u[4 * i + 1], 256.0f, u[4 * i]));
-      const uint32_t b = static_cast<uint32_t>(fmaf(u[4 * i + 3], 256.0f, u[4 * i + 2]));
-      w[i] = a | (b << 16);
-    }
-  } else {
-    uint32_t h[2];
+    constexpr uint32_t kAbove = kBits * 0x01010101u;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      h[i] = static_cast<uint32_t>(
-          fmaf(fmaf(u[4 * i + 3], 16.0f, u[4 * i + 2]), 256.0f, fmaf(u[4 * i + 1], 16.0f, u[4 * i])));
-    w[0] = h[0] | (h[1] << 16);
+      w[i] = u[4 * i] + u[4 * i + 1] * 0x100u + u[4 * i + 2] * 0x10000u + u[4 * i + 3] * 0x1000000u - kAbove;
+  } else {
+    constexpr uint32_t kAbove = kBits * 0x11111111u;
+    w[0] = u[0] + u[1] * 0x10u + u[2] * 0x100u + u[3] * 0x1000u + u[4] * 0x10000u + u[5] * 0x100000u + u[6] * 0x1000000u +
+           u[7] * 0x10000000u - kAbove;
     w[1] = 0;
   }
-  return __half_as_ushort(hs) | (static_cast<uint32_t>(__half_as_ushort(hm)) << 16);
+  return hs | (static_cast<uint32_t>(__half_as_ushort(hm)) << 16);
 }
 
 // The inverse, rounded once to bf16, or to fp16.
@@ -96,8 +103,14 @@ __device__ __forceinline__ uint4 expand(const uint32_t (&w)[2], uint32_t par) {
   float f[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const uint32_t u = FMT == kU8 ? (w[i >> 2] >> (8 * (i & 3))) & 255u : (w[0] >> (4 * i)) & 15u;
-    f[i] = fmaf(static_cast<float>(u), s, m);
+    if (FMT == kU8) {  // a byte under 2^23's exponent
+      const float u = __uint_as_float(__byte_perm(w[i >> 2], kTwo23, 0x7650 + (i & 3))) - 8388608.0f;
+      f[i] = fmaf(u, s, m);
+    } else {  // nibble k in its place stands for 16^k u; the step is taken 16^-k times
+      const int k = i & 3;
+      const float u = __uint_as_float(((i < 4 ? w[0] : w[0] >> 16) & (15u << (4 * k))) | kTwo23) - 8388608.0f;
+      f[i] = fmaf(u, s * (1.0f / (1 << (4 * k))), m);
+    }
   }
   uint32_t o[4];
 #pragma unroll
@@ -121,11 +134,10 @@ struct Item {
 __device__ __forceinline__ Item item_of(const RowsArgs& a, const Seq& s, int b, unsigned item, unsigned items) {
   Item it;
   it.in = item < items;
-  const unsigned i = it.in ? item : 0;
-  const unsigned groups = a.p.groups, per_row = groups * a.p.heads;
-  const unsigned r = i / per_row, hg = i - r * per_row;
-  const unsigned h = groups == 2 ? hg >> 1 : hg;
-  it.g = groups == 2 ? hg & 1 : 0;
+  const int i = it.in ? static_cast<int>(item) : 0;
+  const bool two = a.p.groups == 2;
+  const int rh = two ? i >> 1 : i, r = a.by_heads(rh), h = rh - r * a.p.heads;
+  it.g = two ? i & 1 : 0;
   it.packed = (s.row0 + static_cast<int64_t>(r)) * a.row + h * a.head + it.g * kGroup;
   const int j = s.len - s.n + static_cast<int>(r);
   it.row = -1;
