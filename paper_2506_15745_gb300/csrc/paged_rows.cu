@@ -1,9 +1,9 @@
 // Rows into and out of a paged cache: a scatter of new rows to their pages,
 // quantising them in 8 or 4 bits on the way, and the gather that reads them
 // back. HBM-bound: every element is read once and written once. A team of 8
-// lanes takes one group of 64 channels (16 bytes of bf16 per lane) of a K row
-// and of the matching V row, so a group's minimum and maximum are three
-// shuffles away and nothing but the row itself is ever held.
+// lanes takes a K row and the matching V row, 16 bytes of bf16 per lane and group
+// of 64 channels, so a group's minimum and maximum are three shuffles away and
+// nothing but the row itself is ever held.
 #include <cuda_fp16.h>
 
 #include "paged.cuh"
@@ -123,23 +123,19 @@ __device__ __forceinline__ uint4 expand(const uint32_t (&w)[2], uint32_t par) {
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-// One group of one new row: where it lies in the packed rows and in the pool.
+// A new row of a head: where it lies in the packed rows and in the pool.
 struct Item {
-  int64_t packed;  // element of the group's first channel in the packed rows
+  int64_t packed;  // element of its first channel in the packed rows
   int64_t row;     // row of the pool (head included), -1: none
-  int g;           // group
   bool in;         // there is such a row
 };
 
-__device__ __forceinline__ Item item_of(const RowsArgs& a, const Seq& s, int b, unsigned item, unsigned items) {
+__device__ __forceinline__ Item item_of(const RowsArgs& a, const Seq& s, int b, int item, int items) {
   Item it;
   it.in = item < items;
-  const int i = it.in ? static_cast<int>(item) : 0;
-  const bool two = a.p.groups == 2;
-  const int rh = two ? i >> 1 : i, r = a.by_heads(rh), h = rh - r * a.p.heads;
-  it.g = two ? i & 1 : 0;
-  it.packed = (s.row0 + static_cast<int64_t>(r)) * a.row + h * a.head + it.g * kGroup;
-  const int j = s.len - s.n + static_cast<int>(r);
+  const int i = it.in ? item : 0, r = a.by_heads(i), h = i - r * a.p.heads;
+  it.packed = (s.row0 + static_cast<int64_t>(r)) * a.row + h * a.head;
+  const int j = s.len - s.n + r;
   it.row = -1;
   if (it.in && j >= 0) {
     it.row = pool_row(a.p, b, j);
@@ -148,43 +144,42 @@ __device__ __forceinline__ Item item_of(const RowsArgs& a, const Seq& s, int b, 
   return it;
 }
 
-template <int FMT, int U>
+// A team takes a row of K and of V, both groups of them.
+constexpr int kGroups = 2;
+
+template <int FMT>
 __global__ void __launch_bounds__(kBlock) write_kernel(RowsArgs a) {
   pdl_trigger();
   pdl_wait();
   const int b = blockIdx.y;
   const Seq s = sequence(a.p, b);
-  const unsigned items = static_cast<unsigned>(s.n) * a.p.heads * a.p.groups;
-  const unsigned base = blockIdx.x * (kTeams * U) + (threadIdx.x >> 3);
-  if (blockIdx.x * (kTeams * U) >= items) return;
+  const int items = s.n * a.p.heads;
+  if (static_cast<int>(blockIdx.x) * kTeams >= items) return;
   const int c = threadIdx.x & 7;
-  Item it[U];
-  uint4 xk[U], xv[U];
+  const Item it = item_of(a, s, b, blockIdx.x * kTeams + (threadIdx.x >> 3), items);
+  uint4 xk[kGroups], xv[kGroups];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    it[u] = item_of(a, s, b, base + u * kTeams, items);
-    const bool ok = it[u].row >= 0 && it[u].g * kGroup + c * 8 < a.p.dim;
-    xk[u] = xv[u] = make_uint4(0, 0, 0, 0);
-    if (ok) {
-      xk[u] = ld_stream(a.k_new + it[u].packed + c * 8);
-      xv[u] = ld_stream(a.v_new + it[u].packed + c * 8);
+  for (int g = 0; g < kGroups; ++g) {
+    xk[g] = xv[g] = make_uint4(0, 0, 0, 0);
+    if (it.row >= 0 && g * kGroup + c * 8 < a.p.dim) {
+      xk[g] = ld_stream(a.k_new + it.packed + g * kGroup + c * 8);
+      xv[g] = ld_stream(a.v_new + it.packed + g * kGroup + c * 8);
     }
   }
+  const int64_t at = it.row * a.p.row_bytes, par = it.row * a.p.groups;
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
+  for (int g = 0; g < kGroups; ++g) {
     if (FMT == kBf16) {
-      if (it[u].row >= 0 && it[u].g * kGroup + c * 8 < a.p.dim) {
-        const int64_t at = it[u].row * a.p.row_bytes + it[u].g * (2 * kGroup) + c * 16;
-        *reinterpret_cast<uint4*>(a.p.k + at) = xk[u];
-        *reinterpret_cast<uint4*>(a.p.v + at) = xv[u];
+      if (it.row >= 0 && g * kGroup + c * 8 < a.p.dim) {
+        *reinterpret_cast<uint4*>(a.p.k + at + g * (2 * kGroup) + c * 16) = xk[g];
+        *reinterpret_cast<uint4*>(a.p.v + at + g * (2 * kGroup) + c * 16) = xv[g];
       }
-    } else {
+    } else if (g < a.p.groups) {  // whole warps
       uint32_t wk[2], wv[2];
-      const uint32_t pk = quantise<FMT>(xk[u], wk), pv = quantise<FMT>(xv[u], wv);  // whole warps
-      if (it[u].row >= 0) {
-        const int64_t at = it[u].row * a.p.row_bytes + it[u].g * (FMT == kU8 ? kGroup : kGroup / 2);
-        uint32_t* kd = reinterpret_cast<uint32_t*>(a.p.k + at);
-        uint32_t* vd = reinterpret_cast<uint32_t*>(a.p.v + at);
+      const uint32_t pk = quantise<FMT>(xk[g], wk), pv = quantise<FMT>(xv[g], wv);
+      if (it.row >= 0) {
+        uint32_t* kd = reinterpret_cast<uint32_t*>(a.p.k + at) + g * (FMT == kU8 ? kGroup / 4 : kGroup / 8);
+        uint32_t* vd = reinterpret_cast<uint32_t*>(a.p.v + at) + g * (FMT == kU8 ? kGroup / 4 : kGroup / 8);
         if (FMT == kU8) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
@@ -195,63 +190,57 @@ __global__ void __launch_bounds__(kBlock) write_kernel(RowsArgs a) {
           kd[place_u4(c)] = wk[0];
           vd[place_u4(c)] = wv[0];
         }
-        const int64_t par = it[u].row * a.p.groups + it[u].g;
-        if (c == 0) a.p.k_par[par] = pk;
-        if (c == 1) a.p.v_par[par] = pv;
+        if (c == 0) a.p.k_par[par + g] = pk;
+        if (c == 1) a.p.v_par[par + g] = pv;
       }
     }
   }
 }
 
-template <int FMT, int U>
+template <int FMT>
 __global__ void __launch_bounds__(kBlock) read_kernel(RowsArgs a) {
   pdl_trigger();
   pdl_wait();
   const int b = blockIdx.y;
   const Seq s = sequence(a.p, b);
-  const unsigned items = static_cast<unsigned>(s.n) * a.p.heads * a.p.groups;
-  const unsigned base = blockIdx.x * (kTeams * U) + (threadIdx.x >> 3);
-  if (blockIdx.x * (kTeams * U) >= items) return;
+  const int items = s.n * a.p.heads;
+  if (static_cast<int>(blockIdx.x) * kTeams >= items) return;
   const int c = threadIdx.x & 7;
-  Item it[U];
-  uint4 xk[U], xv[U];  // bf16: the elements; codes: two words and the pair
+  const Item it = item_of(a, s, b, blockIdx.x * kTeams + (threadIdx.x >> 3), items);
+  const int64_t at = it.row * a.p.row_bytes, par = it.row * a.p.groups;
+  uint4 xk[kGroups], xv[kGroups];  // bf16: the elements; codes: two words and the pair
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    it[u] = item_of(a, s, b, base + u * kTeams, items);
-    xk[u] = xv[u] = make_uint4(0, 0, 0, 0);
-    if (it[u].row < 0) continue;
+  for (int g = 0; g < kGroups; ++g) {
+    xk[g] = xv[g] = make_uint4(0, 0, 0, 0);
+    if (it.row < 0 || g * kGroup + c * 8 >= a.p.dim) continue;
     if (FMT == kBf16) {
-      if (it[u].g * kGroup + c * 8 < a.p.dim) {
-        const int64_t at = it[u].row * a.p.row_bytes + it[u].g * (2 * kGroup) + c * 16;
-        xk[u] = ld_stream(a.p.k + at);
-        xv[u] = ld_stream(a.p.v + at);
-      }
+      xk[g] = ld_stream(a.p.k + at + g * (2 * kGroup) + c * 16);
+      xv[g] = ld_stream(a.p.v + at + g * (2 * kGroup) + c * 16);
     } else {
-      const int64_t at = it[u].row * a.p.row_bytes + it[u].g * (FMT == kU8 ? kGroup : kGroup / 2);
-      const uint32_t* kd = reinterpret_cast<const uint32_t*>(a.p.k + at);
-      const uint32_t* vd = reinterpret_cast<const uint32_t*>(a.p.v + at);
+      const uint32_t* kd = reinterpret_cast<const uint32_t*>(a.p.k + at) + g * (FMT == kU8 ? kGroup / 4 : kGroup / 8);
+      const uint32_t* vd = reinterpret_cast<const uint32_t*>(a.p.v + at) + g * (FMT == kU8 ? kGroup / 4 : kGroup / 8);
       if (FMT == kU8) {
-        xk[u].x = kd[place_u8(2 * c)], xk[u].y = kd[place_u8(2 * c + 1)];
-        xv[u].x = vd[place_u8(2 * c)], xv[u].y = vd[place_u8(2 * c + 1)];
+        xk[g].x = kd[place_u8(2 * c)], xk[g].y = kd[place_u8(2 * c + 1)];
+        xv[g].x = vd[place_u8(2 * c)], xv[g].y = vd[place_u8(2 * c + 1)];
       } else {
-        xk[u].x = kd[place_u4(c)];
-        xv[u].x = vd[place_u4(c)];
+        xk[g].x = kd[place_u4(c)];
+        xv[g].x = vd[place_u4(c)];
       }
-      const int64_t par = it[u].row * a.p.groups + it[u].g;
-      xk[u].z = a.p.k_par[par];
-      xv[u].z = a.p.v_par[par];
+      xk[g].z = a.p.k_par[par + g];
+      xv[g].z = a.p.v_par[par + g];
     }
   }
+  if (!it.in) return;
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (!it[u].in || it[u].g * kGroup + c * 8 >= a.p.dim) continue;
+  for (int g = 0; g < kGroups; ++g) {
+    if (g * kGroup + c * 8 >= a.p.dim) continue;
     if (FMT != kBf16) {
-      const uint32_t wk[2] = {xk[u].x, xk[u].y}, wv[2] = {xv[u].x, xv[u].y};
-      xk[u] = expand<FMT, false>(wk, xk[u].z);
-      xv[u] = expand<FMT, false>(wv, xv[u].z);
+      const uint32_t wk[2] = {xk[g].x, xk[g].y}, wv[2] = {xv[g].x, xv[g].y};
+      xk[g] = expand<FMT, false>(wk, xk[g].z);
+      xv[g] = expand<FMT, false>(wv, xv[g].z);
     }
-    *reinterpret_cast<uint4*>(a.k_out + it[u].packed + c * 8) = xk[u];
-    *reinterpret_cast<uint4*>(a.v_out + it[u].packed + c * 8) = xv[u];
+    *reinterpret_cast<uint4*>(a.k_out + it.packed + g * kGroup + c * 8) = xk[g];
+    *reinterpret_cast<uint4*>(a.v_out + it.packed + g * kGroup + c * 8) = xv[g];
   }
 }
 
@@ -306,29 +295,26 @@ __global__ void __launch_bounds__(kBlock) expand_kernel(ExpandArgs a) {
   }
 }
 
-template <int U>
 dim3 grid_of(const RowsArgs& a) {
-  const int64_t items = static_cast<int64_t>(a.p.max_rows) * a.p.heads * a.p.groups;  // < 2^31, checked
-  return dim3(static_cast<unsigned>((items + kTeams * U - 1) / (kTeams * U)), static_cast<unsigned>(a.p.n_seqs));
+  const int64_t items = static_cast<int64_t>(a.p.max_rows) * a.p.heads;  // < 2^31, checked
+  return dim3(static_cast<unsigned>((items + kTeams - 1) / kTeams), static_cast<unsigned>(a.p.n_seqs));
 }
 
 }  // namespace
 
 cudaError_t launch_pages_write(const RowsArgs& a, cudaStream_t st) {
-  const dim3 g = grid_of<2>(a);
   switch (a.p.fmt) {
-    case kBf16: return launch_next(write_kernel<kBf16, 2>, g, kBlock, 0, st, a);
-    case kU8: return launch_next(write_kernel<kU8, 2>, g, kBlock, 0, st, a);
-    default: return launch_next(write_kernel<kU4, 2>, g, kBlock, 0, st, a);
+    case kBf16: return launch_next(write_kernel<kBf16>, grid_of(a), kBlock, 0, st, a);
+    case kU8: return launch_next(write_kernel<kU8>, grid_of(a), kBlock, 0, st, a);
+    default: return launch_next(write_kernel<kU4>, grid_of(a), kBlock, 0, st, a);
   }
 }
 
 cudaError_t launch_pages_read(const RowsArgs& a, cudaStream_t st) {
-  const dim3 g = grid_of<2>(a);
   switch (a.p.fmt) {
-    case kBf16: return launch_next(read_kernel<kBf16, 2>, g, kBlock, 0, st, a);
-    case kU8: return launch_next(read_kernel<kU8, 2>, g, kBlock, 0, st, a);
-    default: return launch_next(read_kernel<kU4, 2>, g, kBlock, 0, st, a);
+    case kBf16: return launch_next(read_kernel<kBf16>, grid_of(a), kBlock, 0, st, a);
+    case kU8: return launch_next(read_kernel<kU8>, grid_of(a), kBlock, 0, st, a);
+    default: return launch_next(read_kernel<kU4>, grid_of(a), kBlock, 0, st, a);
   }
 }
 
