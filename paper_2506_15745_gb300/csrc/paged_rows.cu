@@ -1,9 +1,9 @@
 // Rows into and out of a paged cache: a scatter of new rows to their pages,
 // quantising them in 8 or 4 bits on the way, and the gather that reads them
-// back. HBM-bound: every element is read once and written once. A team of 8
-// lanes takes a K row and the matching V row, 16 bytes of bf16 per lane and group
-// of 64 channels, so a group's minimum and maximum are three shuffles away and
-// nothing but the row itself is ever held.
+// back. HBM-bound: every element is read once and written once. A team of
+// lanes takes a K row and the matching V row: 4 lanes when writing, so that a
+// group's minimum and maximum are two shuffles away and what a group costs beside
+// its values is shared by 16 of them, 8 lanes when reading.
 #include <cuda_fp16.h>
 
 #include "paged.cuh"
@@ -12,7 +12,8 @@ namespace ipv {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kTeams = kBlock / 8;  // groups in flight per block and round
+constexpr int kTeam = 4;              // lanes that write a row
+constexpr int kTeams = kBlock / 8;    // rows that a block reads
 
 // Where a group's words lie (ipv.h, Codes): lane c of a team holds channels
 // 8c..8c+7: word c at 4 bits, words 2c and 2c+1 at 8 bits.
@@ -31,23 +32,25 @@ __device__ __forceinline__ uint32_t min_bf16x2(uint32_t a, uint32_t b) {  // NaN
   return r;
 }
 
-// Quantises a lane's 8 channels with its team's other 56: codes in w (one word
-// at 4 bits, two at 8), the group's (step, minimum) in the return value.
+// Quantises a lane's 16 channels (chunks c and c + 4 of 8 of the group) with its
+// team's other 48: codes in w (a word for each chunk at 4 bits, two at 8), the
+// group's (step, minimum) in the return value.
 template <int FMT>
-__device__ __forceinline__ uint32_t quantise(const uint4& x, uint32_t (&w)[2]) {
+__device__ __forceinline__ uint32_t quantise(const uint4 (&x)[2], uint32_t (&w)[4]) {
   constexpr float kLevels = FMT == kU8 ? 255.0f : 15.0f;
   constexpr uint32_t kSigns = 0x80008000u;
-  const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+  const uint32_t xs[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
   // The group's minimum, and its maximum as the minimum of the negated values, as
   // two halves of one word.
-  const uint32_t lo2 = min_bf16x2(min_bf16x2(xs[0], xs[1]), min_bf16x2(xs[2], xs[3]));
-  const uint32_t hi2 = min_bf16x2(min_bf16x2(xs[0] ^ kSigns, xs[1] ^ kSigns), min_bf16x2(xs[2] ^ kSigns, xs[3] ^ kSigns));
+  uint32_t lo2 = xs[0], hi2 = xs[0] ^ kSigns;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) lo2 = min_bf16x2(lo2, xs[i]), hi2 = min_bf16x2(hi2, xs[i] ^ kSigns);
   uint32_t ends = min_bf16x2(__byte_perm(lo2, hi2, 0x5410), __byte_perm(lo2, hi2, 0x7632));
 #pragma unroll
-  for (int d = 1; d < 8; d <<= 1) ends = min_bf16x2(ends, __shfl_xor_sync(0xffffffffu, ends, d));
+  for (int d = 1; d < kTeam; d <<= 1) ends = min_bf16x2(ends, __shfl_xor_sync(0xffffffffu, ends, d));
   const float lo = lo_f(ends), hi = -hi_f(ends);
   if (!(lo >= -kLargest && hi <= kLargest)) {  // NaN too
-    w[0] = w[1] = 0;
+    w[0] = w[1] = w[2] = w[3] = 0;
     return 0x7FFF7FFFu;  // (NaN, NaN)
   }
   const __half hm = __float2half_rd(lo);
@@ -57,40 +60,43 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, uint32_t (&w)[2]) {
   unsigned short hs = __half_as_ushort(__float2half_rn(range * (1.0f / kLevels)));
   if (fmaf(__half2float(__ushort_as_half(hs)), kLevels, -range) < 0.0f) ++hs;
   const float s = __half2float(__ushort_as_half(hs));
-  // u = rint((x - m) / s). The product with about 1/s is within 1e-4 of the
-  // quotient, so it rounds to the same integer unless it lies that near a half:
-  // only then is the division done. Adding 1.5 * 2^23 rounds; the integer is in
-  // the sum's low bits.
+  // u = rint((x - m) / s). Products with a little less and a little more than 1/s
+  // (2^-20 of it, more than all roundings) enclose the quotient: where they round
+  // to one integer it is the quotient's, and only where they do not is the
+  // division done. Adding 1.5 * 2^23 rounds; the integer is in the sum's low bits.
   float inv;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
   inv = s > 0.0f ? inv : 0.0f;
+  const float less = inv * (1.0f - 0x1p-20f), more = inv * (1.0f + 0x1p-20f);
   constexpr float kRound = 12582912.0f;
-  uint32_t u[8];
-  float far = 0.0f;
+  uint32_t u[16], apart = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 16; ++i) {
     const float d = ((i & 1) ? hi_f(xs[i >> 1]) : lo_f(xs[i >> 1])) - m;
-    const float r = fmaf(d, inv, kRound);
-    far = fmaxf(far, fabsf(fmaf(d, inv, kRound - r)));
-    u[i] = __float_as_uint(r);
+    u[i] = __float_as_uint(fmaf(d, less, kRound));
+    apart |= u[i] ^ __float_as_uint(fmaf(d, more, kRound));
   }
-  if (far > 0.4999f) {
+  if (apart) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      u[i] = __float_as_uint((s > 0.0f ? (((i & 1) ? hi_f(xs[i >> 1]) : lo_f(xs[i >> 1])) - m) / s : 0.0f) + kRound);
+    for (int i = 0; i < 16; ++i)
+      u[i] = __float_as_uint((((i & 1) ? hi_f(xs[i >> 1]) : lo_f(xs[i >> 1])) - m) / s + kRound);
   }
   // Words by multiplication: what stands above the codes is the same every time.
   constexpr uint32_t kBits = 0x4B400000u;  // of 1.5 * 2^23
   if (FMT == kU8) {
     constexpr uint32_t kAbove = kBits * 0x01010101u;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 4; ++i)
       w[i] = u[4 * i] + u[4 * i + 1] * 0x100u + u[4 * i + 2] * 0x10000u + u[4 * i + 3] * 0x1000000u - kAbove;
   } else {
     constexpr uint32_t kAbove = kBits * 0x11111111u;
-    w[0] = u[0] + u[1] * 0x10u + u[2] * 0x100u + u[3] * 0x1000u + u[4] * 0x10000u + u[5] * 0x100000u + u[6] * 0x1000000u +
-           u[7] * 0x10000000u - kAbove;
-    w[1] = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t* v = u + 8 * i;
+      w[i] = v[0] + v[1] * 0x10u + v[2] * 0x100u + v[3] * 0x1000u + v[4] * 0x10000u + v[5] * 0x100000u + v[6] * 0x1000000u +
+             v[7] * 0x10000000u - kAbove;
+    }
+    w[2] = w[3] = 0;
   }
   return hs | (static_cast<uint32_t>(__half_as_ushort(hm)) << 16);
 }
@@ -154,41 +160,49 @@ __global__ void __launch_bounds__(kBlock) write_kernel(RowsArgs a) {
   const int b = blockIdx.y;
   const Seq s = sequence(a.p, b);
   const int items = s.n * a.p.heads;
-  if (static_cast<int>(blockIdx.x) * kTeams >= items) return;
-  const int c = threadIdx.x & 7;
-  const Item it = item_of(a, s, b, blockIdx.x * kTeams + (threadIdx.x >> 3), items);
-  uint4 xk[kGroups], xv[kGroups];
+  if (static_cast<int>(blockIdx.x) * (kBlock / kTeam) >= items) return;
+  const int c = threadIdx.x & (kTeam - 1);
+  const Item it = item_of(a, s, b, blockIdx.x * (kBlock / kTeam) + threadIdx.x / kTeam, items);
+  uint4 xk[kGroups][2], xv[kGroups][2];
 #pragma unroll
-  for (int g = 0; g < kGroups; ++g) {
-    xk[g] = xv[g] = make_uint4(0, 0, 0, 0);
-    if (it.row >= 0 && g * kGroup + c * 8 < a.p.dim) {
-      xk[g] = ld_stream(a.k_new + it.packed + g * kGroup + c * 8);
-      xv[g] = ld_stream(a.v_new + it.packed + g * kGroup + c * 8);
+  for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int ch = g * kGroup + (c + kTeam * i) * 8;
+      xk[g][i] = xv[g][i] = make_uint4(0, 0, 0, 0);
+      if (it.row >= 0 && ch < a.p.dim) {
+        xk[g][i] = ld_stream(a.k_new + it.packed + ch);
+        xv[g][i] = ld_stream(a.v_new + it.packed + ch);
+      }
     }
-  }
   const int64_t at = it.row * a.p.row_bytes, par = it.row * a.p.groups;
 #pragma unroll
   for (int g = 0; g < kGroups; ++g) {
     if (FMT == kBf16) {
-      if (it.row >= 0 && g * kGroup + c * 8 < a.p.dim) {
-        *reinterpret_cast<uint4*>(a.p.k + at + g * (2 * kGroup) + c * 16) = xk[g];
-        *reinterpret_cast<uint4*>(a.p.v + at + g * (2 * kGroup) + c * 16) = xv[g];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int ch = g * kGroup + (c + kTeam * i) * 8;
+        if (it.row >= 0 && ch < a.p.dim) {
+          *reinterpret_cast<uint4*>(a.p.k + at + 2 * ch) = xk[g][i];
+          *reinterpret_cast<uint4*>(a.p.v + at + 2 * ch) = xv[g][i];
+        }
       }
     } else if (g < a.p.groups) {  // whole warps
-      uint32_t wk[2], wv[2];
+      uint32_t wk[4], wv[4];
       const uint32_t pk = quantise<FMT>(xk[g], wk), pv = quantise<FMT>(xv[g], wv);
       if (it.row >= 0) {
         uint32_t* kd = reinterpret_cast<uint32_t*>(a.p.k + at) + g * (FMT == kU8 ? kGroup / 4 : kGroup / 8);
         uint32_t* vd = reinterpret_cast<uint32_t*>(a.p.v + at) + g * (FMT == kU8 ? kGroup / 4 : kGroup / 8);
         if (FMT == kU8) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            kd[place_u8(2 * c + i)] = wk[i];
-            vd[place_u8(2 * c + i)] = wv[i];
+          for (int i = 0; i < 4; ++i) {
+            const int word = 2 * (c + kTeam * (i >> 1)) + (i & 1);
+            kd[place_u8(word)] = wk[i];
+            vd[place_u8(word)] = wv[i];
           }
-        } else {
-          kd[place_u4(c)] = wk[0];
-          vd[place_u4(c)] = wv[0];
+        } else {  // words c and c + 4 lie side by side
+          *reinterpret_cast<uint2*>(kd + place_u4(c)) = make_uint2(wk[0], wk[1]);
+          *reinterpret_cast<uint2*>(vd + place_u4(c)) = make_uint2(wv[0], wv[1]);
         }
         if (c == 0) a.p.k_par[par + g] = pk;
         if (c == 1) a.p.v_par[par + g] = pv;
@@ -295,26 +309,26 @@ __global__ void __launch_bounds__(kBlock) expand_kernel(ExpandArgs a) {
   }
 }
 
-dim3 grid_of(const RowsArgs& a) {
+dim3 grid_of(const RowsArgs& a, int rows) {  // rows of a block
   const int64_t items = static_cast<int64_t>(a.p.max_rows) * a.p.heads;  // < 2^31, checked
-  return dim3(static_cast<unsigned>((items + kTeams - 1) / kTeams), static_cast<unsigned>(a.p.n_seqs));
+  return dim3(static_cast<unsigned>((items + rows - 1) / rows), static_cast<unsigned>(a.p.n_seqs));
 }
 
 }  // namespace
 
 cudaError_t launch_pages_write(const RowsArgs& a, cudaStream_t st) {
   switch (a.p.fmt) {
-    case kBf16: return launch_next(write_kernel<kBf16>, grid_of(a), kBlock, 0, st, a);
-    case kU8: return launch_next(write_kernel<kU8>, grid_of(a), kBlock, 0, st, a);
-    default: return launch_next(write_kernel<kU4>, grid_of(a), kBlock, 0, st, a);
+    case kBf16: return launch_next(write_kernel<kBf16>, grid_of(a, kBlock / kTeam), kBlock, 0, st, a);
+    case kU8: return launch_next(write_kernel<kU8>, grid_of(a, kBlock / kTeam), kBlock, 0, st, a);
+    default: return launch_next(write_kernel<kU4>, grid_of(a, kBlock / kTeam), kBlock, 0, st, a);
   }
 }
 
 cudaError_t launch_pages_read(const RowsArgs& a, cudaStream_t st) {
   switch (a.p.fmt) {
-    case kBf16: return launch_next(read_kernel<kBf16>, grid_of(a), kBlock, 0, st, a);
-    case kU8: return launch_next(read_kernel<kU8>, grid_of(a), kBlock, 0, st, a);
-    default: return launch_next(read_kernel<kU4>, grid_of(a), kBlock, 0, st, a);
+    case kBf16: return launch_next(read_kernel<kBf16>, grid_of(a, kTeams), kBlock, 0, st, a);
+    case kU8: return launch_next(read_kernel<kU8>, grid_of(a, kTeams), kBlock, 0, st, a);
+    default: return launch_next(read_kernel<kU4>, grid_of(a, kTeams), kBlock, 0, st, a);
   }
 }
 
