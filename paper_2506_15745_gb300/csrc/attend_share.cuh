@@ -102,17 +102,26 @@ __device__ Share find_share(const AttendArgs& a, int tiles, int64_t* scratch) {
     const int steps = p < pairs ? tile_of<ROWS, STEP>(a, tiles, p).steps : 0;
     return steps > 0 ? static_cast<int64_t>(steps + COST) * a.p.heads : int64_t{0};
   };
-  if (pairs == 1) {  // nothing to search
-    const int64_t total = weight(0);
+  if (pairs <= 32) {  // every warp finds it by itself
+    const int64_t mine = weight(lane);
+    int64_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += y;
+    }
+    const int64_t total = __shfl_sync(0xffffffffu, upto, 31);
     const int64_t per = max(divide(total + gridDim.x - 1, gridDim.x), static_cast<int64_t>(a.unit + COST)), from = per * blockIdx.x;
     Share w;
     w.left = min(per, total - from);
     w.p = w.head = 0;
     w.at = 0;
     if (w.left > 0) {
-      const int64_t one = divide(total, a.p.heads);
-      w.head = static_cast<int>(divide(from, one));
-      w.at = from - w.head * one;
+      w.p = __ffs(__ballot_sync(0xffffffffu, from < upto)) - 1;
+      const int64_t one = divide(__shfl_sync(0xffffffffu, mine, w.p), a.p.heads);
+      const int64_t off = from - __shfl_sync(0xffffffffu, upto - mine, w.p);
+      w.head = static_cast<int>(divide(off, one));
+      w.at = off - w.head * one;
     }
     return w;
   }
