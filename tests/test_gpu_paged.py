@@ -490,3 +490,59 @@ def test_a_wait_that_runs_out_is_reported():
     q, out, lse = run_attend(s, 8, 122)
     assert ipv.attend_error() == 0
     check_attend(s, q, out, lse, 128 ** -0.5)
+
+
+SHARED_OUT = [  # fmt, dim, heads, share, page, sequences (rows, kv) as a function of an index, how many, kwargs
+    ("bf16", 64, 1, 2, 16, lambda b: (1, (b * 37) % 190), 500, {}),              # more sequences than a block has threads
+    ("u4", 64, 2, 8, 16, lambda b: (1, (b * 53) % 410), 40, {}),                  # more than a warp has lanes
+    ("u8", 128, 1, 7, 32, lambda b: (b % 3, 60 + (b * 29) % 200), 150, {"window": 40, "sinks": 2}),
+    ("bf16", 64, 1, 4, 16, lambda b: (5 + b % 60, 70 + (b * 31) % 100), 420, {}),  # tiled kernel, more tiles than threads
+    ("bf16", 128, 2, 3, 64, lambda b: (100 * (b % 4), 300 * (b % 4) + 3), 37, {}),
+    ("u4", 128, 1, 4, 64, lambda b: (90, 150 + 20 * b), 12, {"window": 64, "sinks": 10}),
+    ("bf16", 128, 1, 1, 16, lambda b: (1, 40000), 1, {}),                         # one tile over every block
+    ("u8", 64, 1, 3, 16, lambda b: (1, 33000 - 999 * b), 3, {}),
+    ("bf16", 64, 1, 1, 64, lambda b: (24, 40000), 1, {}),
+    ("bf16", 128, 1, 8, 256, lambda b: (700, 5000), 1, {}),                       # many tiles, several to a block
+    ("bf16", 128, 5, 1, 64, lambda b: (2500, 2500), 1, {"window": 300, "sinks": 129}),
+]
+
+
+@pytest.mark.parametrize("case", range(len(SHARED_OUT)))
+def test_work_shared_out_over_blocks(case):
+    """Batches whose tiles, runs and parts fall on the blocks in every way: many small sequences, one long one,
+    tiles that start, continue and end in different blocks."""
+    fmt, dim, heads, share, page, seq, count, kw = SHARED_OUT[case]
+    gen = torch.Generator().manual_seed(1000 + case)
+    seqs = [seq(b) for b in range(count)]
+    s = Setup(gen, fmt, heads, dim, page, [n for _, n in seqs], [min(r, max(n, 1)) for r, n in seqs])
+    q, out, lse = run_attend(s, share, 1100 + case, **kw)
+    check_attend(s, q, out, lse, dim ** -0.5, **kw)
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_bounds_may_be_loose(rows):
+    """max_rows, max_kv and total_rows far above what the sequences have."""
+    gen = torch.Generator().manual_seed(131)
+    s = Setup(gen, "bf16", 2, 128, 16, [300, 0, 77], [rows, 0, min(rows, 30)], max_rows=3 * rows, max_kv=100000)
+    s.batch = PagedBatch(s.batch.table, s.batch.row_start, s.batch.kv_len, total_rows=s.total + 50, max_rows=3 * rows, max_kv=100000)
+    q = (torch.randn((s.total + 50, 6, 128), generator=gen) * 1.5).bfloat16()
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full(q.shape[:2], 7.0, device="cuda")
+    s.cache.attend(q.cuda(), s.batch, out=out, lse=lse)
+    check_attend(s, q, out, lse, 128 ** -0.5)
+    assert (out[s.total:] == 7.0).all() and (lse[s.total:] == 7.0).all()  # rows of no sequence are left alone
+
+
+def test_stream_of_its_own_without_a_workspace_is_refused():
+    gen = torch.Generator().manual_seed(141)
+    s = Setup(gen, "bf16", 1, 128, 16, [4000], [1])
+    q = make_rows(gen, 1, 8, 128).cuda()
+    side = torch.cuda.Stream()
+    with pytest.raises(ValueError, match="workspace"):
+        s.cache.attend(q, s.batch, stream=side)
+    want = s.cache.attend(q, s.batch)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):  # the current stream's own workspace
+        out = s.cache.attend(q, s.batch)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
