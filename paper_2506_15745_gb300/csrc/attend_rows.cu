@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
   const Share share = find_share<kTileRows, kRowsStep, kRunCost, kThreads>(a, tiles, reinterpret_cast<int64_t*>(smem));
   int slots = 0;  // partial results used
   if (share.left <= 0) {
-    if (threadIdx.x < 2) a.part_rec[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
+    if (threadIdx.x < 2 && a.unit > 0) a.part_rec[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
     return;
   }
   __syncthreads();  // the shared memory held find_share's scratch
@@ -689,7 +689,7 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
   __syncthreads();  // the results are read before the next run's are written
   }
   pdl_trigger();
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 0 && a.unit > 0) {
     if (!(slots & 1)) a.part_rec[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
     if (!(slots & 2)) a.part_rec[2 * blockIdx.x + 1] = make_int4(0, 0, 0, 0);
   }
@@ -766,7 +766,7 @@ struct Kernel {
   }
   static cudaError_t launch(const AttendArgs& a, int blocks, cudaStream_t st) {
     const cudaError_t e = launch_next(attend_rows_kernel<FMT, DP, NR>, dim3(blocks), kThreads, kSmem, st, a, kOneTile);
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || a.unit == 0) return e;
     return launch_next(attend_rows_join_kernel<8 * NR>, dim3(blocks, 8 * NR), kThreads, 0, st, a, kOneTile, blocks);
   }
 };

@@ -102,6 +102,15 @@ __device__ Share find_share(const AttendArgs& a, int tiles, int64_t* scratch) {
     const int steps = p < pairs ? tile_of<ROWS, STEP>(a, tiles, p).steps : 0;
     return steps > 0 ? static_cast<int64_t>(steps + COST) * a.p.heads : int64_t{0};
   };
+  if (a.unit == 0) {
+    Share w;
+    w.p = static_cast<int>(blockIdx.x) / a.p.heads;
+    w.head = blockIdx.x - w.p * a.p.heads;
+    w.at = 0;
+    const int steps = tile_of<ROWS, STEP>(a, tiles, w.p).steps;
+    w.left = steps > 0 ? steps + COST : 0;
+    return w;
+  }
   if (pairs <= 32) {  // every warp finds it by itself
     const int64_t mine = weight(lane);
     int64_t upto = mine;

@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   pdl_wait();
   const Share share = find_share<kRowsCta, kKeys, kRunCost, kThreads>(a, tiles, reinterpret_cast<int64_t*>(base_p + L::kScale));
   if (share.left <= 0) {
-    if (threadIdx.x < 2) a.part_rec[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
+    if (threadIdx.x < 2 && a.unit > 0) a.part_rec[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
     return;
   }
   const uint32_t bars = base + L::kBars, stop = bars + kWordStop;
@@ -674,7 +674,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (in && partial) a.part_ml[part] = make_float2(m, l);
       if (in && !partial && a.lse) a.lse[row * a.q_heads + hq] = l == 0.0f ? kNegInf : (m + log2f(l)) * 0.6931471805599453f;
     }
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && a.unit > 0) {
       if (!(slots & 1)) a.part_rec[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
       if (!(slots & 2)) a.part_rec[2 * blockIdx.x + 1] = make_int4(0, 0, 0, 0);
     }
@@ -824,7 +824,7 @@ cudaError_t launch_attend_tiles(const AttendArgs& a, bool bf16, const TileMaps& 
   else
     e = bf16 ? launch_one<true, 128>(a, km, vm, tiles, maps.box_rows, limit_ns, blocks, st)
              : launch_one<false, 128>(a, km, vm, tiles, maps.box_rows, limit_ns, blocks, st);
-  if (e != cudaSuccess) return e;
+  if (e != cudaSuccess || a.unit == 0) return e;
   return launch_next(attend_tiles_join_kernel, dim3(blocks, kRowsCta / 32, a.p.dim <= 64 ? 1 : 2), 128, 0, st, a, tiles, blocks);
 }
 

@@ -186,6 +186,9 @@ constexpr int64_t kTilesFrom = 17;
 // Fewest steps of a block's share: below, joining parts costs more than the
 // other blocks save.
 constexpr int kTilesLeast = 2, kRowsLeast = 8;
+// Keys up to which a block takes a row tile whole, and there is nothing to join:
+// the join and its launch take about as long as a block takes for these.
+constexpr int kWhole = 512;
 
 // Which kernel takes the call, on how many blocks, and the workspace.
 struct Plan {
@@ -217,6 +220,18 @@ void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
     a->tile = ipv::attend_rows_tile(static_cast<int>(rows));
     a->unit = kRowsLeast;
     plan->blocks = num_sms * ipv::attend_rows_resident(p.fmt, p.dim, a->tile);
+  }
+  // Keys that a row tile can see, at most (its windows, the sinks, their steps' ends).
+  int64_t span = p.max_kv;
+  if (a->window) {
+    const int64_t seen = static_cast<int64_t>(a->window) + a->tile + a->sinks + 2 * (plan->tiles ? ipv::kTilesStep : ipv::kRowsStep);
+    if (seen < span) span = seen;
+  }
+  const int64_t items = (rows + a->tile - 1) / a->tile * p.n_seqs * p.heads;
+  if (span <= kWhole && items <= INT32_MAX) {
+    a->unit = 0;
+    plan->blocks = static_cast<int>(items);
+    return;
   }
   const int64_t parts = static_cast<int64_t>(plan->blocks) * 2 * a->tile;
   plan->part_o = plan->bytes;

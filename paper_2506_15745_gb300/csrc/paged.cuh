@@ -107,7 +107,7 @@ struct AttendArgs {
   Divide by_share, by_tiles;  // tiles: 256-row tiles of max_rows
   float scale_log2;     // scale * log2(e)
   int causal, window, sinks;
-  int unit;  // fewest steps of a block's share
+  int unit;  // fewest steps of a block's share; 0: a block takes one KV head of one row tile, whole
   int tile;  // query rows of a row tile
   // Partial results, for each block's first and last run: unnormalised sums
   // (rows kernel: [blocks][2][tile][dim], tiled kernel: [blocks][2][dim / 4][tile][4]),

@@ -55,6 +55,7 @@ class PagedBatch:
                                 1 if table is None else max(table.stride(0), table.shape[1]), ipv._ptr(row_start),
                                 ipv._ptr(kv_len), total_rows, max_rows, max_kv)
         self.ref = ctypes.byref(self.struct)
+        self.sizes = (n, self.max_pages, total_rows, max_rows, max_kv)
 
 
 class PagedCache:
@@ -121,7 +122,7 @@ class PagedCache:
         self.struct = ipv.PagesDesc(FORMATS[fmt], self.n_kv_heads, self.head_dim, self.page_size, self.n_pages, *rows,
                                     k.data_ptr(), v.data_ptr(), ipv._ptr(k_par), ipv._ptr(v_par))
         self.ref = ctypes.byref(self.struct)
-        self._workspaces, self._needs = {}, {}
+        self._workspaces, self._calls = {}, {}
 
     @staticmethod
     def _row_strides(t, width):
@@ -167,7 +168,7 @@ class PagedCache:
         sequences hold. out: bf16 like q (allocated if None); lse: fp32
         [total_rows, n_q_heads], filled if given. workspace: a uint8 tensor
         that no call on another stream uses at the same time; without one the cache keeps one of its own for
-        each stream that is current in a call."""
+        each stream that is current in a call. One host thread at a time uses a cache object."""
         n_q_heads = q.shape[1]
         qs = self._packed("q", q, batch, n_q_heads, self.head_dim)
         if out is None:
@@ -177,16 +178,15 @@ class PagedCache:
             _need(lse.dtype is torch.float32 and lse.is_cuda and lse.is_contiguous() and lse.dim() == 2 and
                   lse.shape[0] >= batch.total_rows and lse.shape[1] == n_q_heads,
                   "lse must be a contiguous fp32 CUDA tensor [total_rows, n_q_heads]")
-        args = ipv.AttendArgs(q.data_ptr(), out.data_ptr(), ipv._ptr(lse), qs[0], qs[1], os[0], os[1], n_q_heads,
-                              self.head_dim ** -0.5 if scale is None else scale, int(causal), window, sinks, None, 0)
-        # The sizes that the need depends on; asked for once per set of them.
-        sizes = (batch.n_seqs, batch.total_rows, batch.max_rows, batch.max_kv, batch.max_pages, n_q_heads, causal, window, sinks)
-        need = self._needs.get(sizes)
-        if need is None:
-            need = ipv.attend_workspace(self.ref, batch.ref, args)
-            if len(self._needs) >= 4096:
-                self._needs.clear()
-            self._needs[sizes] = need
+        # Arguments and workspace need are kept for each set of sizes that they depend on.
+        sizes = (batch.sizes, n_q_heads, causal, window, sinks)
+        kept = self._calls.get(sizes)
+        if kept is None:
+            kept = self._first_call(batch, sizes)
+        args, ref, need = kept
+        args.q, args.out, args.lse = q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr()
+        args.q_row_stride, args.q_head_stride, args.out_row_stride, args.out_head_stride = qs[0], qs[1], os[0], os[1]
+        args.scale = self.head_dim ** -0.5 if scale is None else scale
         at = ipv._stream(stream)
         if need:
             if workspace is None:
@@ -195,5 +195,14 @@ class PagedCache:
                 if workspace is None or workspace.numel() < need:
                     workspace = self._workspaces[at] = torch.empty(need, dtype=torch.uint8, device=q.device)
             args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel()
-        ipv.attend(self.ref, batch.ref, ctypes.byref(args), at)
+        ipv.attend(self.ref, batch.ref, ref, at)
         return out
+
+    def _first_call(self, batch, sizes):
+        _, n_q_heads, causal, window, sinks = sizes
+        args = ipv.AttendArgs(n_q_heads=n_q_heads, scale=1.0, causal=int(causal), window=window, sinks=sinks)
+        kept = args, ctypes.byref(args), ipv.attend_workspace(self.ref, batch.ref, args)
+        if len(self._calls) >= 1024:
+            self._calls.clear()
+        self._calls[sizes] = kept
+        return kept
