@@ -35,6 +35,7 @@ namespace {
 
 constexpr int kThreads = 32 * kRowsWarps;
 constexpr int kRunCost = 6;  // what a run of steps costs beside them, in steps
+constexpr int kCluster = kRowsCluster;
 constexpr float kNegInf = -INFINITY;
 constexpr int kOneTile = 1;  // row tiles of a sequence: more rows are the tiled kernel's
 
@@ -170,6 +171,32 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, const Seq& s, int
 // channels has enough bytes in flight with one, codes need warps to widen them.
 constexpr int min_blocks(int fmt, int dp, int nr) { return fmt == kBf16 && dp == 128 ? 1 : nr == 1 ? 3 : 2; }
 
+// Clusters: a block's rank, the address of a shared-memory word in block r of
+// the cluster, loads from there, and the barrier of all blocks.
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t in_block(uint32_t at, uint32_t r) {
+  uint32_t x;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(x) : "r"(at), "r"(r));
+  return x;
+}
+__device__ __forceinline__ float4 far128(uint32_t at) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ float2 far64(uint32_t at) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
 template <int FMT, int DP, int NR>
 __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows_kernel(AttendArgs a, int tiles) {
   using R = Ring<FMT, DP>;
@@ -185,7 +212,8 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
   pdl_wait();
   const Share share = find_share<kTileRows, kRowsStep, kRunCost, kThreads>(a, tiles, reinterpret_cast<int64_t*>(smem));
   int slots = 0;  // partial results used
-  if (share.left <= 0) {
+  const bool clustered = a.unit == 0 && a.cluster > 1;
+  if (share.left <= 0 && !clustered) {
     if (threadIdx.x < 2 && a.unit > 0) a.part_rec[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
     return;
   }
@@ -236,16 +264,23 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
   // The first steps of a run, and the page of the one after them.
   int page_next = -1;
   auto fill = [&](const W& x) {
+    int pages[R::kStages];  // all on their way at once
+#pragma unroll
+    for (int i = 0; i < R::kStages; ++i) pages[i] = page_of(x, x.s + warp + i * kRowsWarps);
 #pragma unroll
     for (int i = 0; i < R::kStages - 1; ++i) {
       const int step = x.s + warp + i * kRowsWarps;
-      if (step < x.s + x.n) issue(x, step, page_of(x, step), i);
+      if (step < x.s + x.n) issue(x, step, pages[i], i);
       copy_commit();
     }
-    page_next = page_of(x, x.s + warp + (R::kStages - 1) * kRowsWarps);
+    page_next = pages[R::kStages - 1];
   };
 
-  bool go = w.begin(a, tiles, share);
+  // A cluster's part: [rows][DP sums, maximum, sum] in the rings, which one run leaves free.
+  constexpr int kPartPitch = DP + 4;
+  float* part_rows = reinterpret_cast<float*>(smem);
+
+  bool go = share.left > 0 && w.begin(a, tiles, share);
   if (go) fill(w);
   for (int run = 0; go; ++run) {
   const Seq seq = w.t.seq;
@@ -656,7 +691,7 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
     }
   __syncthreads();
   const int slot = 2 * blockIdx.x + (run > 0 ? 1 : 0);
-  if (partial) {
+  if (partial && !clustered) {
     slots |= run > 0 ? 2 : 1;
     if (threadIdx.x == 0) a.part_rec[slot] = make_int4(1, pair, head, ends);
   }
@@ -678,7 +713,11 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
       acc.x += f * y.x, acc.y += f * y.y, acc.z += f * y.z, acc.w += f * y.w;
     }
     if (sum == 0.0f) acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // sees nothing, here or at all
-    if (partial) {
+    if (clustered) {
+      float* row = part_rows + r * kPartPitch;
+      *reinterpret_cast<float4*>(row + c) = acc;
+      if (c == 0) *reinterpret_cast<float2*>(row + DP) = make_float2(top, sum);
+    } else if (partial) {
       const int64_t at = static_cast<int64_t>(slot) * kRows + r;
       if (c < a.p.dim) *reinterpret_cast<float4*>(a.part_o + at * a.p.dim + c) = acc;
       if (c == 0) a.part_ml[at] = make_float2(top, sum);
@@ -687,6 +726,42 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
     }
   }
   __syncthreads();  // the results are read before the next run's are written
+  }
+  if (clustered) {
+    // The cluster's blocks hold a part each, in the place of their rings: every
+    // block joins its share of the rows' channels from all of them.
+    const Tile x = tile_of<kTileRows, kRowsStep>(a, tiles, share.p);
+    if (share.left <= 0)
+      for (int r = threadIdx.x; r < kTileRows; r += kThreads) *reinterpret_cast<float2*>(part_rows + r * kPartPitch + DP) = make_float2(kNegInf, 0.0f);
+    cluster_barrier();
+    constexpr int kQuads = DP / 4;
+    for (int idx = cluster_rank() * kThreads + threadIdx.x; idx < kTileRows * kQuads; idx += a.cluster * kThreads) {
+      const int r = idx / kQuads, c = (idx % kQuads) * 4;
+      if (r >= x.n_rows) continue;
+      const uint32_t row_at = smem_u32(part_rows + r * kPartPitch);
+      float2 ml[kCluster];
+      float4 y[kCluster];
+#pragma unroll
+      for (int k = 0; k < kCluster; ++k) ml[k] = far64(in_block(row_at + DP * 4, k));
+#pragma unroll
+      for (int k = 0; k < kCluster; ++k)  // a block without steps has left no sums
+        y[k] = ml[k].y == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : far128(in_block(row_at + c * 4, k));
+      float top = ml[0].x;
+#pragma unroll
+      for (int k = 1; k < kCluster; ++k) top = fmaxf(top, ml[k].x);
+      const float base = top == kNegInf ? 0.0f : top;
+      float sum = 0.0f;
+      float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int k = 0; k < kCluster; ++k) {
+        const float f = exp2_fast(ml[k].x - base);
+        sum += f * ml[k].y;
+        acc.x += f * y[k].x, acc.y += f * y[k].y, acc.z += f * y[k].z, acc.w += f * y[k].w;
+      }
+      if (sum == 0.0f) acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // sees nothing
+      write_row(a, x.seq, share.head, x.row0 + r, c, acc, top, sum);
+    }
+    cluster_barrier();  // a block's shared memory stays until all have read it
   }
   pdl_trigger();
   if (threadIdx.x == 0 && a.unit > 0) {
@@ -765,7 +840,7 @@ struct Kernel {
     return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, attend_rows_kernel<FMT, DP, NR>, kThreads, kSmem);
   }
   static cudaError_t launch(const AttendArgs& a, int blocks, cudaStream_t st) {
-    const cudaError_t e = launch_next(attend_rows_kernel<FMT, DP, NR>, dim3(blocks), kThreads, kSmem, st, a, kOneTile);
+    const cudaError_t e = launch_clusters(a.unit == 0 ? a.cluster : 1, attend_rows_kernel<FMT, DP, NR>, dim3(blocks), kThreads, kSmem, st, a, kOneTile);
     if (e != cudaSuccess || a.unit == 0) return e;
     return launch_next(attend_rows_join_kernel<8 * NR>, dim3(blocks, 8 * NR), kThreads, 0, st, a, kOneTile, blocks);
   }

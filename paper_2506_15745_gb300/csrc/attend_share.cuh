@@ -103,12 +103,14 @@ __device__ Share find_share(const AttendArgs& a, int tiles, int64_t* scratch) {
     return steps > 0 ? static_cast<int64_t>(steps + COST) * a.p.heads : int64_t{0};
   };
   if (a.unit == 0) {
+    const int item = static_cast<int>(blockIdx.x) / a.cluster, rank = static_cast<int>(blockIdx.x) - item * a.cluster;
     Share w;
-    w.p = static_cast<int>(blockIdx.x) / a.p.heads;
-    w.head = blockIdx.x - w.p * a.p.heads;
-    w.at = 0;
+    w.p = item / a.p.heads;
+    w.head = item - w.p * a.p.heads;
     const int steps = tile_of<ROWS, STEP>(a, tiles, w.p).steps;
-    w.left = steps > 0 ? steps + COST : 0;
+    const int64_t from = static_cast<int64_t>(steps) * rank / a.cluster, to = static_cast<int64_t>(steps) * (rank + 1) / a.cluster;
+    w.at = from > 0 ? from + COST : 0;
+    w.left = to > from ? to + COST - w.at : 0;
     return w;
   }
   if (pairs <= 32) {  // every warp finds it by itself
@@ -193,13 +195,15 @@ __device__ Share find_share(const AttendArgs& a, int tiles, int64_t* scratch) {
 __device__ __forceinline__ int parts_from(const AttendArgs& a, int c, int blocks, int& slot, int4& rec) {
   const int lane = threadIdx.x & 31;
   const int4 one = a.part_rec[2 * c], two = a.part_rec[2 * c + 1];
+  int ends = c + 1 + lane >= blocks ? 2 : a.part_rec[2 * (c + 1 + lane)].w;  // the first 32 with the records
   slot = two.x && two.w == 1 ? 2 * c + 1 : one.x && one.w == 1 ? 2 * c : -1;
   if (slot < 0) return 0;
   rec = slot & 1 ? two : one;
   for (int i0 = 1;; i0 += 32) {
-    const int blk = c + i0 + lane;
-    const uint32_t last = __ballot_sync(0xffffffffu, blk >= blocks || (a.part_rec[2 * blk].w & 2));
+    const uint32_t last = __ballot_sync(0xffffffffu, ends & 2);
     if (last) return i0 + __ffs(last);
+    const int blk = c + i0 + 32 + lane;
+    ends = blk >= blocks ? 2 : a.part_rec[2 * blk].w;
   }
 }
 

@@ -82,18 +82,26 @@ __device__ __forceinline__ int64_t pool_row(const Pages& p, int b, int j) {
 // waits with pdl_wait() before it reads or writes anything, and lets its own
 // successor be launched with pdl_trigger().
 template <typename... Params, typename... Args>
-cudaError_t launch_next(void (*kernel)(Params...), dim3 grid, unsigned block, size_t smem, cudaStream_t st, const Args&... args) {
+cudaError_t launch_clusters(int cluster, void (*kernel)(Params...), dim3 grid, unsigned block, size_t smem, cudaStream_t st,
+                            const Args&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(block);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+template <typename... Params, typename... Args>
+cudaError_t launch_next(void (*kernel)(Params...), dim3 grid, unsigned block, size_t smem, cudaStream_t st, const Args&... args) {
+  return launch_clusters(1, kernel, grid, block, smem, st, args...);
 }
 
 // ------------------------------------------------------------------ attention
@@ -107,7 +115,9 @@ struct AttendArgs {
   Divide by_share, by_tiles;  // tiles: 256-row tiles of max_rows
   float scale_log2;     // scale * log2(e)
   int causal, window, sinks;
-  int unit;  // fewest steps of a block's share; 0: a block takes one KV head of one row tile, whole
+  // Fewest steps of a block's share; 0: `cluster` blocks (1, or 8 as one cluster,
+  // which joins their parts by itself) take one KV head of one row tile.
+  int unit, cluster;
   int tile;  // query rows of a row tile
   // Partial results, for each block's first and last run: unnormalised sums
   // (rows kernel: [blocks][2][tile][dim], tiled kernel: [blocks][2][dim / 4][tile][4]),
@@ -177,6 +187,7 @@ int attend_rows_tile(int rows);               // query rows of a row tile, for a
 int attend_rows_resident(int fmt, int dim, int tile);  // blocks per SM, after attend_rows_prepare
 constexpr int kRowsStep = 32;                 // keys of a step
 constexpr int kRowsWarps = 4;
+constexpr int kRowsCluster = 8;               // blocks of a cluster
 cudaError_t attend_rows_prepare();            // once per device
 cudaError_t launch_attend_rows(const AttendArgs& a, int blocks, cudaStream_t st);
 

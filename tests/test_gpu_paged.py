@@ -466,7 +466,7 @@ def test_offsets_past_32_bits():
 def test_refusals_on_the_gpu():
     """A workspace that is too small is refused before anything runs; empty batches are accepted."""
     gen = torch.Generator().manual_seed(111)
-    s = Setup(gen, "bf16", 1, 128, 16, [4000], [1])
+    s = Setup(gen, "bf16", 1, 128, 16, [20000], [1])  # long enough to need a workspace
     q = make_rows(gen, 1, 8, 128).cuda()
     with pytest.raises(ipv.IpvError, match="workspace"):
         s.cache.attend(q, s.batch, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
@@ -519,6 +519,23 @@ def test_work_shared_out_over_blocks(case):
     check_attend(s, q, out, lse, dim ** -0.5, **kw)
 
 
+@pytest.mark.parametrize("fmt,dim,heads,share,seqs,kw", [
+    ("bf16", 128, 4, 7, [(1, 600)], {}),
+    ("bf16", 64, 2, 8, [(1, 1500), (1, 3), (0, 40), (2, 4000)], {}),
+    ("bf16", 96, 3, 3, [(5, 900), (1, 0)], {}),
+    ("u8", 128, 2, 7, [(1, 4000), (1, 513)], {}),
+    ("u8", 64, 1, 16, [(1, 8000)], {"causal": False}),
+    ("u4", 128, 4, 5, [(1, 2000), (3, 700), (2, 1)], {"window": 600, "sinks": 33}),
+    ("u4", 64, 8, 8, [(1, 5000)], {}),
+])
+def test_clusters(fmt, dim, heads, share, seqs, kw):
+    """Row tiles that 8 blocks of a cluster share, some with fewer steps than blocks, or none."""
+    gen = torch.Generator().manual_seed(dim + share)
+    s = Setup(gen, fmt, heads, dim, 32, [n for _, n in seqs], [r for r, _ in seqs])
+    q, out, lse = run_attend(s, share, 151, **kw)
+    check_attend(s, q, out, lse, dim ** -0.5, **kw)
+
+
 @pytest.mark.parametrize("rows", [1, 40])
 def test_bounds_may_be_loose(rows):
     """max_rows, max_kv and total_rows far above what the sequences have."""
@@ -535,7 +552,7 @@ def test_bounds_may_be_loose(rows):
 
 def test_stream_of_its_own_without_a_workspace_is_refused():
     gen = torch.Generator().manual_seed(141)
-    s = Setup(gen, "bf16", 1, 128, 16, [4000], [1])
+    s = Setup(gen, "bf16", 1, 128, 16, [20000], [1])  # long enough to need a workspace
     q = make_rows(gen, 1, 8, 128).cuda()
     side = torch.cuda.Stream()
     with pytest.raises(ValueError, match="workspace"):
