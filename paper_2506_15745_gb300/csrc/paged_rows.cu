@@ -129,25 +129,29 @@ __device__ __forceinline__ uint4 expand(const uint32_t (&w)[2], uint32_t par) {
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-// A new row of a head: where it lies in the packed rows and in the pool.
+// A new row of a head: where it lies in the packed rows, and which of its
+// sequence's rows it is.
 struct Item {
   int64_t packed;  // element of its first channel in the packed rows
-  int64_t row;     // row of the pool (head included), -1: none
+  int j, h;
   bool in;         // there is such a row
 };
 
-__device__ __forceinline__ Item item_of(const RowsArgs& a, const Seq& s, int b, int item, int items) {
+__device__ __forceinline__ Item item_of(const RowsArgs& a, const Seq& s, int item, int items) {
   Item it;
   it.in = item < items;
-  const int i = it.in ? item : 0, r = a.by_heads(i), h = i - r * a.p.heads;
-  it.packed = (s.row0 + static_cast<int64_t>(r)) * a.row + h * a.head;
-  const int j = s.len - s.n + r;
-  it.row = -1;
-  if (it.in && j >= 0) {
-    it.row = pool_row(a.p, b, j);
-    if (it.row >= 0) it.row += h * a.p.head_stride;
-  }
+  const int i = it.in ? item : 0, r = a.by_heads(i);
+  it.h = i - r * a.p.heads;
+  it.packed = (s.row0 + static_cast<int64_t>(r)) * a.row + it.h * a.head;
+  it.j = s.len - s.n + r;
   return it;
+}
+
+// Its row of the pool (head included), -1: none.
+__device__ __forceinline__ int64_t row_of(const RowsArgs& a, int b, const Item& it) {
+  if (!it.in || it.j < 0) return -1;
+  const int64_t row = pool_row(a.p, b, it.j);
+  return row < 0 ? row : row + it.h * a.p.head_stride;
 }
 
 // A team takes a row of K and of V, both groups of them.
@@ -162,7 +166,7 @@ __global__ void __launch_bounds__(kBlock) write_kernel(RowsArgs a) {
   const int items = s.n * a.p.heads;
   if (static_cast<int>(blockIdx.x) * (kBlock / kTeam) >= items) return;
   const int c = threadIdx.x & (kTeam - 1);
-  const Item it = item_of(a, s, b, blockIdx.x * (kBlock / kTeam) + threadIdx.x / kTeam, items);
+  const Item it = item_of(a, s, blockIdx.x * (kBlock / kTeam) + threadIdx.x / kTeam, items);
   uint4 xk[kGroups][2], xv[kGroups][2];
 #pragma unroll
   for (int g = 0; g < kGroups; ++g)
@@ -170,19 +174,19 @@ __global__ void __launch_bounds__(kBlock) write_kernel(RowsArgs a) {
     for (int i = 0; i < 2; ++i) {
       const int ch = g * kGroup + (c + kTeam * i) * 8;
       xk[g][i] = xv[g][i] = make_uint4(0, 0, 0, 0);
-      if (it.row >= 0 && ch < a.p.dim) {
+      if (it.in && ch < a.p.dim) {  // on their way while the page is looked up
         xk[g][i] = ld_stream(a.k_new + it.packed + ch);
         xv[g][i] = ld_stream(a.v_new + it.packed + ch);
       }
     }
-  const int64_t at = it.row * a.p.row_bytes, par = it.row * a.p.groups;
+  const int64_t row = row_of(a, b, it), at = row * a.p.row_bytes, par = row * a.p.groups;
 #pragma unroll
   for (int g = 0; g < kGroups; ++g) {
     if (FMT == kBf16) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int ch = g * kGroup + (c + kTeam * i) * 8;
-        if (it.row >= 0 && ch < a.p.dim) {
+        if (row >= 0 && ch < a.p.dim) {
           *reinterpret_cast<uint4*>(a.p.k + at + 2 * ch) = xk[g][i];
           *reinterpret_cast<uint4*>(a.p.v + at + 2 * ch) = xv[g][i];
         }
@@ -190,7 +194,7 @@ __global__ void __launch_bounds__(kBlock) write_kernel(RowsArgs a) {
     } else if (g < a.p.groups) {  // whole warps
       uint32_t wk[4], wv[4];
       const uint32_t pk = quantise<FMT>(xk[g], wk), pv = quantise<FMT>(xv[g], wv);
-      if (it.row >= 0) {
+      if (row >= 0) {
         uint32_t* kd = reinterpret_cast<uint32_t*>(a.p.k + at) + g * (FMT == kU8 ? kGroup / 4 : kGroup / 8);
         uint32_t* vd = reinterpret_cast<uint32_t*>(a.p.v + at) + g * (FMT == kU8 ? kGroup / 4 : kGroup / 8);
         if (FMT == kU8) {
@@ -220,13 +224,13 @@ __global__ void __launch_bounds__(kBlock) read_kernel(RowsArgs a) {
   const int items = s.n * a.p.heads;
   if (static_cast<int>(blockIdx.x) * kTeams >= items) return;
   const int c = threadIdx.x & 7;
-  const Item it = item_of(a, s, b, blockIdx.x * kTeams + (threadIdx.x >> 3), items);
-  const int64_t at = it.row * a.p.row_bytes, par = it.row * a.p.groups;
+  const Item it = item_of(a, s, blockIdx.x * kTeams + (threadIdx.x >> 3), items);
+  const int64_t row = row_of(a, b, it), at = row * a.p.row_bytes, par = row * a.p.groups;
   uint4 xk[kGroups], xv[kGroups];  // bf16: the elements; codes: two words and the pair
 #pragma unroll
   for (int g = 0; g < kGroups; ++g) {
     xk[g] = xv[g] = make_uint4(0, 0, 0, 0);
-    if (it.row < 0 || g * kGroup + c * 8 >= a.p.dim) continue;
+    if (row < 0 || g * kGroup + c * 8 >= a.p.dim) continue;
     if (FMT == kBf16) {
       xk[g] = ld_stream(a.p.k + at + g * (2 * kGroup) + c * 16);
       xv[g] = ld_stream(a.p.v + at + g * (2 * kGroup) + c * 16);

@@ -122,7 +122,7 @@ class PagedCache:
         self.struct = ipv.PagesDesc(FORMATS[fmt], self.n_kv_heads, self.head_dim, self.page_size, self.n_pages, *rows,
                                     k.data_ptr(), v.data_ptr(), ipv._ptr(k_par), ipv._ptr(v_par))
         self.ref = ctypes.byref(self.struct)
-        self._workspaces, self._calls = {}, {}
+        self._workspaces, self._calls, self._lib = {}, {}, ipv.load()
 
     @staticmethod
     def _row_strides(t, width):
@@ -142,12 +142,20 @@ class PagedCache:
             raise ValueError(f"{name} must be a bf16 CUDA tensor [{batch.total_rows}, {heads}, {dim}] with contiguous rows")
         return strides
 
+    def _pair(self, k_name, k, v_name, v, batch):
+        strides = self._packed(k_name, k, batch, self.n_kv_heads, self.head_dim)
+        if v.shape != k.shape or v.dtype is not torch.bfloat16 or not v.is_cuda:
+            self._packed(v_name, v, batch, self.n_kv_heads, self.head_dim)
+        _need(v.stride() == strides, f"{k_name} and {v_name} must have the same strides")
+        return strides
+
     def write(self, k_new, v_new, batch: PagedBatch, stream=None) -> None:
         """ipv_pages_write: k_new, v_new bf16 [total_rows, n_kv_heads, head_dim] into the batch's pages."""
-        strides = self._packed("k_new", k_new, batch, self.n_kv_heads, self.head_dim)
-        _need(self._packed("v_new", v_new, batch, self.n_kv_heads, self.head_dim) == strides,
-              "k_new and v_new must have the same strides")
-        ipv.pages_write(self.ref, batch.ref, k_new, v_new, strides[0], strides[1], stream)
+        strides = self._pair("k_new", k_new, "v_new", v_new, batch)
+        status = self._lib.ipv_pages_write(self.ref, batch.ref, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1],
+                                           ipv._stream(stream))
+        if status:
+            ipv._check(status)
 
     def read(self, batch: PagedBatch, k_out=None, v_out=None, stream=None):
         """ipv_pages_read: the batch's new rows, bf16 [total_rows, n_kv_heads, head_dim] each. Packed rows that
@@ -156,10 +164,11 @@ class PagedCache:
             shape = (batch.total_rows, self.n_kv_heads, self.head_dim)
             k_out = torch.zeros(shape, dtype=torch.bfloat16, device=self.k.device) if k_out is None else k_out
             v_out = torch.zeros(shape, dtype=torch.bfloat16, device=self.k.device) if v_out is None else v_out
-        strides = self._packed("k_out", k_out, batch, self.n_kv_heads, self.head_dim)
-        _need(self._packed("v_out", v_out, batch, self.n_kv_heads, self.head_dim) == strides,
-              "k_out and v_out must have the same strides")
-        ipv.pages_read(self.ref, batch.ref, k_out, v_out, strides[0], strides[1], stream)
+        strides = self._pair("k_out", k_out, "v_out", v_out, batch)
+        status = self._lib.ipv_pages_read(self.ref, batch.ref, k_out.data_ptr(), v_out.data_ptr(), strides[0], strides[1],
+                                          ipv._stream(stream))
+        if status:
+            ipv._check(status)
         return k_out, v_out
 
     def attend(self, q, batch: PagedBatch, *, out=None, lse=None, scale: float | None = None, causal: bool = True,
@@ -195,7 +204,9 @@ class PagedCache:
                 if workspace is None or workspace.numel() < need:
                     workspace = self._workspaces[at] = torch.empty(need, dtype=torch.uint8, device=q.device)
             args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel()
-        ipv.attend(self.ref, batch.ref, ref, at)
+        status = self._lib.ipv_attend(self.ref, batch.ref, ref, at)
+        if status:
+            ipv._check(status)
         return out
 
     def _first_call(self, batch, sizes):
