@@ -1,5 +1,5 @@
 // Attention of a few query rows over a paged cache (single tokens, short
-// chunks, any head width), and the join of keys that were split over blocks.
+// chunks), and the join of keys that were split over blocks.
 //
 // HBM-bound: each cached K and V row is read once per row tile, 8 or 16 query
 // rows (the query heads that share a KV head, times the new tokens) use it.
@@ -37,7 +37,6 @@ constexpr int kThreads = 32 * kRowsWarps;
 constexpr int kRunCost = 6;  // what a run of steps costs beside them, in steps
 constexpr int kCluster = kRowsCluster;
 constexpr float kNegInf = -INFINITY;
-constexpr int kOneTile = 1;  // row tiles of a sequence: more rows are the tiled kernel's
 
 template <int FMT, int DP>
 struct Ring {
@@ -840,9 +839,9 @@ struct Kernel {
     return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, attend_rows_kernel<FMT, DP, NR>, kThreads, kSmem);
   }
   static cudaError_t launch(const AttendArgs& a, int blocks, cudaStream_t st) {
-    const cudaError_t e = launch_clusters(a.unit == 0 ? a.cluster : 1, attend_rows_kernel<FMT, DP, NR>, dim3(blocks), kThreads, kSmem, st, a, kOneTile);
+    const cudaError_t e = launch_clusters(a.unit == 0 ? a.cluster : 1, attend_rows_kernel<FMT, DP, NR>, dim3(blocks), kThreads, kSmem, st, a, a.tiles);
     if (e != cudaSuccess || a.unit == 0) return e;
-    return launch_next(attend_rows_join_kernel<8 * NR>, dim3(blocks, 8 * NR), kThreads, 0, st, a, kOneTile, blocks);
+    return launch_next(attend_rows_join_kernel<8 * NR>, dim3(blocks, 8 * NR), kThreads, 0, st, a, a.tiles, blocks);
   }
 };
 

@@ -814,7 +814,7 @@ bool attend_tiles_maps(const AttendArgs& a, bool bf16, TileMaps* maps) {
 }
 
 cudaError_t launch_attend_tiles(const AttendArgs& a, bool bf16, const TileMaps& maps, int blocks, int64_t limit_ns, cudaStream_t st) {
-  const int tiles = static_cast<int>((static_cast<int64_t>(a.p.max_rows) * a.share + kRowsCta - 1) / kRowsCta);
+  const int tiles = a.tiles;
   const CUtensorMap& km = *reinterpret_cast<const CUtensorMap*>(maps.k);
   const CUtensorMap& vm = *reinterpret_cast<const CUtensorMap*>(maps.v);
   cudaError_t e;

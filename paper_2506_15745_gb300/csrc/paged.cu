@@ -1,5 +1,6 @@
 // C ABI of the paged cache (declared in include/ipv.h): argument checks, the
 // choice of kernel and of key splits, launches.
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstdarg>
@@ -162,12 +163,11 @@ ipv_status check_attend(const ipv_pages* p, const ipv_batch* b, const ipv_attend
   if (t->window > 0 && !t->causal) return reject(IPV_EINVAL, "a window needs causal = 1");
   if (static_cast<int64_t>(a->p.max_rows) * t->n_q_heads > INT32_MAX)
     return reject(IPV_EINVAL, "max_rows * n_q_heads exceeds 2^31 - 1");
-  const int64_t tiles = (static_cast<int64_t>(a->p.max_rows) * (t->n_q_heads / p->n_kv_heads) + ipv::kTilesRows - 1) / ipv::kTilesRows;
+  const int64_t tiles = (static_cast<int64_t>(a->p.max_rows) * (t->n_q_heads / p->n_kv_heads) + 15) / 16;
   if (tiles * a->p.n_seqs > INT32_MAX) return reject(IPV_EINVAL, "n_seqs times the query tiles of max_rows exceeds 2^31 - 1");
   a->q_heads = t->n_q_heads;
   a->share = t->n_q_heads / p->n_kv_heads;
   a->by_share = ipv::Divide(a->share);
-  a->by_tiles = ipv::Divide(tiles > 0 ? static_cast<int>(tiles) : 1);
   a->scale_log2 = t->scale * 1.4426950408889634f;
   a->causal = t->causal;
   a->window = t->window;
@@ -179,9 +179,14 @@ ipv_status check_attend(const ipv_pages* p, const ipv_batch* b, const ipv_attend
 constexpr int64_t kDefaultLimitNs = 4000000000;
 std::atomic<int64_t> g_limit_ns{kDefaultLimitNs};
 
-// Query rows from which the tiled kernel is the faster one: below, the rows
-// kernel reads K and V once per 16 query rows.
-constexpr int64_t kTilesFrom = 17;
+// The rows kernel reads K and V once per 16 query rows, the tiled kernel once per
+// 256, after widening codes and with a longer way in and out. Up to 64 rows (per
+// sequence and KV head) the rows kernel is the faster one for codes (7 query heads,
+// 4 KV heads, 6000 rows, 16 sequences of 4 tokens, u4: 51 against 109 us; of 9 tokens
+// 84 against 110), and for bf16 where it reads little (1 sequence of 8 tokens over 9000
+// rows, 74 MB: 19 against 24 us; 16 of 9 tokens over 600, 78 MB: 25 against 20; 16 of 3
+// tokens over 6000, 393 MB: 65 against 48).
+constexpr int64_t kRowsMost = 64, kRowsBytes = 76 << 20;
 
 // Fewest steps of a block's share: below, joining parts costs more than the
 // other blocks save.
@@ -211,7 +216,9 @@ int64_t round256(int64_t x) { return (x + 255) & ~int64_t{255}; }
 void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
   const ipv::Pages& p = a->p;
   const int64_t rows = static_cast<int64_t>(p.max_rows) * a->share;
-  plan->tiles = rows >= kTilesFrom;
+  const int64_t read = (rows + 15) / 16 * p.n_seqs * p.heads * std::min<int64_t>(p.max_kv, a->window ? int64_t{a->window} + a->sinks + 64 : p.max_kv) * 2 * p.row_bytes;
+  const bool waves = p.max_kv <= kWhole && (rows + 15) / 16 * p.n_seqs * p.heads > num_sms;  // of blocks that take tiles whole
+  plan->tiles = rows > kRowsMost || (rows > 16 && p.fmt == ipv::kBf16 && (read > kRowsBytes || waves));
   plan->bytes = 0;
   if (plan->tiles) {
     a->tile = ipv::kTilesRows;
@@ -228,13 +235,15 @@ void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
     a->unit = kRowsLeast;
     plan->blocks = num_sms * ipv::attend_rows_resident(p.fmt, p.dim, a->tile);
   }
+  a->tiles = static_cast<int>((rows + a->tile - 1) / a->tile);
+  a->by_tiles = ipv::Divide(a->tiles);
   // Keys that a row tile can see, at most (its windows, the sinks, their steps' ends).
   int64_t span = p.max_kv;
   if (a->window) {
     const int64_t seen = static_cast<int64_t>(a->window) + a->tile + a->sinks + 2 * (plan->tiles ? ipv::kTilesStep : ipv::kRowsStep);
     if (seen < span) span = seen;
   }
-  const int64_t items = (rows + a->tile - 1) / a->tile * p.n_seqs * p.heads;
+  const int64_t items = static_cast<int64_t>(a->tiles) * p.n_seqs * p.heads;
   a->cluster = 1;
   if (span <= kWhole && items <= INT32_MAX) {
     a->unit = 0;

@@ -112,7 +112,8 @@ struct AttendArgs {
   float* lse;
   int64_t q_row, q_head, out_row, out_head;  // strides in elements
   int q_heads, share;   // query heads; query heads per KV head
-  Divide by_share, by_tiles;  // tiles: 256-row tiles of max_rows
+  Divide by_share, by_tiles;
+  int tiles;            // row tiles of max_rows
   float scale_log2;     // scale * log2(e)
   int causal, window, sinks;
   // Fewest steps of a block's share; 0: `cluster` blocks (1, or 8 as one cluster,
@@ -183,7 +184,7 @@ struct ExpandArgs {
 };
 cudaError_t launch_pages_expand(const ExpandArgs& a, cudaStream_t st);
 
-int attend_rows_tile(int rows);               // query rows of a row tile, for at most 16
+int attend_rows_tile(int rows);               // query rows of a row tile
 int attend_rows_resident(int fmt, int dim, int tile);  // blocks per SM, after attend_rows_prepare
 constexpr int kRowsStep = 32;                 // keys of a step
 constexpr int kRowsWarps = 4;

@@ -536,6 +536,25 @@ def test_clusters(fmt, dim, heads, share, seqs, kw):
     check_attend(s, q, out, lse, dim ** -0.5, **kw)
 
 
+@pytest.mark.parametrize("fmt,dim,heads,share,seqs,kw", [
+    ("bf16", 128, 2, 7, [(9, 9), (3, 200), (8, 450)], {}),                     # whole contexts, several row tiles
+    ("bf16", 64, 1, 4, [(16, 3000)], {"window": 900, "sinks": 7}),             # clusters
+    ("bf16", 112, 2, 3, [(20, 20000), (1, 5), (0, 9), (13, 777)], {}),         # shares
+    ("u8", 128, 3, 8, [(8, 400), (2, 2)], {}),
+    ("u8", 64, 1, 16, [(4, 2500)], {"causal": False}),
+    ("u8", 128, 2, 7, [(9, 9000), (9, 300), (4, 4000)], {}),
+    ("u4", 64, 2, 1, [(64, 64), (33, 500)], {"window": 20, "sinks": 1}),
+    ("u4", 128, 1, 2, [(17, 1700), (32, 32)], {}),
+    ("u4", 128, 4, 7, [(7, 3000 + 50 * b) for b in range(9)], {}),
+])
+def test_several_row_tiles(fmt, dim, heads, share, seqs, kw):
+    """17 to 64 query rows per KV head: a few row tiles of 16, their last one ragged."""
+    gen = torch.Generator().manual_seed(dim * 7 + share)
+    s = Setup(gen, fmt, heads, dim, 32, [n for _, n in seqs], [r for r, _ in seqs])
+    q, out, lse = run_attend(s, share, 161, **kw)
+    check_attend(s, q, out, lse, dim ** -0.5, **kw)
+
+
 @pytest.mark.parametrize("rows", [1, 40])
 def test_bounds_may_be_loose(rows):
     """max_rows, max_kv and total_rows far above what the sequences have."""
