@@ -122,7 +122,7 @@ __device__ Share find_share(const AttendArgs& a, int tiles, int64_t* scratch) {
       if (lane >= d) upto += y;
     }
     const int64_t total = __shfl_sync(0xffffffffu, upto, 31);
-    const int64_t per = max(divide(total + gridDim.x - 1, gridDim.x), static_cast<int64_t>(a.unit + COST)), from = per * blockIdx.x;
+    const int64_t per = max(divide(total + gridDim.x - 1, gridDim.x), static_cast<int64_t>(a.unit)), from = per * blockIdx.x;
     Share w;
     w.left = min(per, total - from);
     w.p = w.head = 0;
@@ -147,7 +147,7 @@ __device__ Share find_share(const AttendArgs& a, int tiles, int64_t* scratch) {
 #pragma unroll
   for (int i = 0; i < kWarps; ++i) total += scratch[i];
   int64_t per = divide(total + gridDim.x - 1, gridDim.x);
-  if (per < a.unit + COST) per = a.unit + COST;
+  if (per < a.unit) per = a.unit;
   const int64_t from = per * blockIdx.x;
   Share w;
   w.left = min(per, total - from);

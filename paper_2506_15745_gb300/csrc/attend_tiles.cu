@@ -40,7 +40,7 @@ namespace {
 
 constexpr int kRowsCta = kTilesRows;  // query rows of a tile of work
 constexpr int kKeys = kTilesStep;     // keys of a step
-constexpr int kRunCost = 3;           // what a run of steps costs beside them, in steps
+constexpr int kRunCost = 5;           // what a run of steps costs beside them, in steps
 constexpr int kMmaWarp = 8, kLoadWarp = 10;  // warps 8, 9: products of query tiles 0, 1; 10, 11: copies of K, V
 constexpr int kThreads = 384;                // two softmax warpgroups, one for copies and products
 constexpr int kHalf = 128 * 128;      // bytes of 128 rows x 64 channels

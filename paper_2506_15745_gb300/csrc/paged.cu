@@ -188,9 +188,9 @@ std::atomic<int64_t> g_limit_ns{kDefaultLimitNs};
 // tokens over 6000, 393 MB: 65 against 48).
 constexpr int64_t kRowsMost = 64, kRowsBytes = 76 << 20;
 
-// Fewest steps of a block's share: below, joining parts costs more than the
-// other blocks save.
-constexpr int kTilesLeast = 2, kRowsLeast = 8;
+// Least share of a block, in steps and what a run costs beside them: below,
+// joining parts costs more than the other blocks save.
+constexpr int kTilesLeast = 3, kRowsLeast = 14;
 // Keys up to which a block takes a row tile whole, and there is nothing to join:
 // the join and its launch take about as long as a block takes for these.
 constexpr int kWhole = 512;

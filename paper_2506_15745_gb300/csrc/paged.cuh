@@ -116,7 +116,7 @@ struct AttendArgs {
   int tiles;            // row tiles of max_rows
   float scale_log2;     // scale * log2(e)
   int causal, window, sinks;
-  // Fewest steps of a block's share; 0: `cluster` blocks (1, or 8 as one cluster,
+  // Fewest units (steps and runs' costs) of a block's share; 0: `cluster` blocks (1, or 8 as one cluster,
   // which joins their parts by itself) take one KV head of one row tile.
   int unit, cluster;
   int tile;  // query rows of a row tile
