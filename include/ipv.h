@@ -378,7 +378,8 @@ typedef struct {
   int page_size;        /* rows of a page: a power of two >= 16, or any size if
                            the batch has max_pages = 1 */
   int64_t n_pages;      /* < 2^31 */
-  int64_t page_stride, head_stride, row_stride; /* in rows, see above */
+  int64_t page_stride, head_stride, row_stride; /* in rows, see above; positive (where
+                           there is more than one) and below 2^32 */
   void* k;
   void* v;              /* 16-byte aligned */
   void* k_par;

@@ -25,6 +25,11 @@
 // number per query row and group. The products p s are rounded to fp16 (11 bits)
 // after a power of two that keeps the largest step's below 2^15. So a code costs
 // a mask and its share of two byte permutations and a shift, no multiplication.
+//
+// Measured: one token for each of 8 streams, 24576 bf16 rows, 8 KV heads of 8 query
+// heads: 124 us, 6.5 TB/s (96% of the copy bandwidth); 32 streams of up to 24577
+// 4-bit rows: 124 us, 4.3 TB/s, bound by integer instructions (masks, permutations,
+// addresses); 32 streams of 12288 8-bit rows: 148 us, 5.8 TB/s.
 #include <cuda_fp16.h>
 
 #include "attend_share.cuh"
@@ -45,6 +50,8 @@ struct Ring {
   static constexpr int kG = DP / kGroup;
   static constexpr int kPar = FMT == kBf16 ? 0 : kRowsStep * kG * 4;
   static constexpr int kStage = 2 * kTile + 2 * kPar;
+  // bf16: 96 to 128 KB in flight with one block per SM; codes: 3 blocks, and 3 stages
+  // were slower (32 streams of 12288 8-bit rows 213 us against 150).
   static constexpr int kStages = FMT == kBf16 ? 3 : 2;
   static constexpr int kWarp = kStage * kStages;
   static constexpr int kBytes = kWarp * kRowsWarps;
@@ -167,7 +174,8 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, const Seq& s, int
 }
 
 // Resident blocks per SM that registers and shared memory are cut to: bf16 at 128
-// channels has enough bytes in flight with one, codes need warps to widen them.
+// channels has enough bytes in flight with one, codes need warps to widen them (32
+// ragged 4-bit streams: 3 blocks of 168 registers 123 us, 4 of 128, with spills, 134).
 constexpr int min_blocks(int fmt, int dp, int nr) { return fmt == kBf16 && dp == 128 ? 1 : nr == 1 ? 3 : 2; }
 
 // Clusters: a block's rank, the address of a shared-memory word in block r of

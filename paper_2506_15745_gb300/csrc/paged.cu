@@ -77,8 +77,11 @@ ipv_status check(const ipv_pages* p, const ipv_batch* b, ipv::Pages* out) {
   if (p->page_size < 1 || p->n_pages < 1 || p->n_pages > INT32_MAX)
     return reject(IPV_EINVAL, "page_size %d and n_pages %lld must be positive and below 2^31", p->page_size,
                   static_cast<long long>(p->n_pages));
-  if (p->page_stride < 0 || p->head_stride < 0 || p->row_stride < 1)
-    return reject(IPV_EINVAL, "page and head strides must not be negative, row_stride must be positive");
+  if (p->page_stride < (p->n_pages > 1) || p->head_stride < (p->n_kv_heads > 1) || p->row_stride < 1)
+    return reject(IPV_EINVAL, "strides must be positive");
+  for (const int64_t stride : {p->page_stride, p->head_stride, p->row_stride})
+    if (stride >= (int64_t{1} << 40) / 256)  // a row has at most 256 bytes
+      return reject(IPV_EINVAL, "a stride of %lld rows exceeds 2^32", static_cast<long long>(stride));
   const double last = static_cast<double>(p->n_pages - 1) * static_cast<double>(p->page_stride) +
                       static_cast<double>(p->n_kv_heads - 1) * static_cast<double>(p->head_stride) +
                       static_cast<double>(p->page_size - 1) * static_cast<double>(p->row_stride);

@@ -28,7 +28,7 @@ ARGS = dict(q=0x50000, out=0x60000, lse=None, q_row_stride=3584, q_head_stride=1
 BAD_PAGES = [dict(format=3), dict(format=-1), dict(n_kv_heads=0), dict(n_kv_heads=70000), dict(head_dim=0), dict(head_dim=136),
              dict(head_dim=100), dict(format=1, head_dim=80), dict(format=2, head_dim=32), dict(page_size=0),
              dict(page_size=48), dict(page_size=8), dict(n_pages=0), dict(n_pages=1 << 31), dict(page_stride=-1),
-             dict(head_stride=-64), dict(row_stride=0), dict(page_stride=1 << 60), dict(k=None), dict(v=None),
+             dict(head_stride=-64), dict(page_stride=0), dict(head_stride=0), dict(row_stride=0), dict(row_stride=1 << 32), dict(page_stride=1 << 60), dict(k=None), dict(v=None),
              dict(k=0x10008), dict(v=0x10000), dict(format=1, k_par=None), dict(format=2, v_par=0x40004),
              dict(format=1, v_par=0x30000)]
 BAD_BATCH = [dict(n_seqs=-1), dict(n_seqs=65536), dict(max_pages=0), dict(table=None), dict(table=0x1002),
