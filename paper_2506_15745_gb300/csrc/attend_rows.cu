@@ -290,449 +290,449 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
   bool go = share.left > 0 && w.begin(a, tiles, share);
   if (go) fill(w);
   for (int run = 0; go; ++run) {
-  const Seq seq = w.t.seq;
-  const KeyRange kr = w.t.kr;
-  const int head = w.head;
-  const int row0 = w.t.row0, row1 = row0 + w.t.n_rows - 1;
-  const int first = w.s + warp, s_end = w.s + w.n;
+    const Seq seq = w.t.seq;
+    const KeyRange kr = w.t.kr;
+    const int head = w.head;
+    const int row0 = w.t.row0, row1 = row0 + w.t.n_rows - 1;
+    const int first = w.s + warp, s_end = w.s + w.n;
 
-  // ---- the query rows as the first product's second operand
-  uint32_t qb[kKs][NR][2];
-  float c_acc[NR][2], c_min[NR][2][kG];  // codes: factors of a thread's two rows
+    // ---- the query rows as the first product's second operand
+    uint32_t qb[kKs][NR][2];
+    float c_acc[NR][2], c_min[NR][2][kG];  // codes: factors of a thread's two rows
 #pragma unroll
-  for (int nr = 0; nr < NR; ++nr) {
-    const int r = row0 + nr * 8 + g;
-    const bool in = r <= row1;
-    const int tok = a.by_share(in ? r : row0), hq = (in ? r : row0) - tok * a.share;
-    const uint16_t* qp = a.q + (seq.row0 + static_cast<int64_t>(tok)) * a.q_row + (head * a.share + hq) * a.q_head;
-    if constexpr (kB) {
-#pragma unroll
-      for (int ks = 0; ks < kKs; ++ks)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int ch = ks * 16 + i * 8 + 2 * t;
-          qb[ks][nr][i] = in && ch < a.p.dim ? *reinterpret_cast<const uint32_t*>(qp + ch) : 0u;
-        }
-    } else {
-      // The row's largest magnitude goes to [2^9, 2^10): its 1/16ths and its
-      // products with subnormal codes keep all their bits. 4 threads share a row.
-      uint32_t top = 0;
-      for (int ch = 8 * t; ch < DP; ch += 32) {
-        const uint4 x = in ? *reinterpret_cast<const uint4*>(qp + ch) : make_uint4(0, 0, 0, 0);
-        const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top = max(top, max(xs[i] & 0x7FFFu, (xs[i] >> 16) & 0x7FFFu));
-      }
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const int e = min(max(static_cast<int>(top >> 7) - 127, -100), 126);
-      const float up = __uint_as_float(static_cast<uint32_t>(127 + 9 - e) << 23);
-      const float down = __uint_as_float(static_cast<uint32_t>(127 - 9 + e) << 23);
-      auto load = [&](int ch, float f) {
-        const float x = in ? __uint_as_float(static_cast<uint32_t>(qp[ch]) << 16) : 0.0f;
-        return x * up * f;
-      };
-      float sum[kG];
-#pragma unroll
-      for (int gr = 0; gr < kG; ++gr) sum[gr] = 0.0f;
-#pragma unroll
-      for (int ks = 0; ks < kKs; ++ks) {
-        const int gr = ks >> 2, w = FMT == kU8 ? ks & 3 : (ks >> 1) & 1;
-        const bool hi4 = FMT == kU4 && (ks & 1);  // nibbles 1, 5, 3, 7 stand 4 bits up
-        const float f = hi4 ? 0.0625f : 1.0f;
-        const int c0 = gr * kGroup + (FMT == kU8 ? 4 : 8) * (t + 4 * w) + (hi4 ? 1 : 0);
-        const int d = FMT == kU8 ? 2 : 4, d2 = FMT == kU8 ? 1 : 2;
-        qb[ks][nr][0] = pack2<false>(load(c0, f), load(c0 + d, f));
-        qb[ks][nr][1] = pack2<false>(load(c0 + d2, f), load(c0 + d2 + d, f));
-        const __half2 s2a = as_half2(qb[ks][nr][0]), s2b = as_half2(qb[ks][nr][1]);
-        sum[gr] += (__low2float(s2a) + __high2float(s2a) + __low2float(s2b) + __high2float(s2b)) * (hi4 ? 16.0f : 1.0f);
-      }
-      const float c = a.scale_log2 * down;
-#pragma unroll
-      for (int gr = 0; gr < kG; ++gr) {
-        sum[gr] += __shfl_xor_sync(0xffffffffu, sum[gr], 1);
-        sum[gr] += __shfl_xor_sync(0xffffffffu, sum[gr], 2);
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        c_acc[nr][i] = __shfl_sync(0xffffffffu, c * 16777216.0f, 4 * (2 * t + i));
-#pragma unroll
-        for (int gr = 0; gr < kG; ++gr) c_min[nr][i][gr] = __shfl_sync(0xffffffffu, c * sum[gr], 4 * (2 * t + i));
-      }
-    }
-  }
-
-  // ---- what the thread's two rows of each row tile see
-  int hi[NR][2];
-#pragma unroll
-  for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = row0 + nr * 8 + 2 * t + i;
-      hi[nr][i] = r <= row1 ? token_hi(a, seq, a.by_share(r)) : 0;
-    }
-
-  float o[kCt][NR][4];
-  float m[NR][2], l[NR][2];
-#pragma unroll
-  for (int nr = 0; nr < NR; ++nr) {
-    m[nr][0] = m[nr][1] = kNegInf;
-    l[nr][0] = l[nr][1] = 0.0f;
-#pragma unroll
-    for (int ct = 0; ct < kCt; ++ct) o[ct][nr][0] = o[ct][nr][1] = o[ct][nr][2] = o[ct][nr][3] = 0.0f;
-  }
-
-  // Codes: sums of p m, and the largest step so far, as its fp16 exponent field;
-  // weights times steps are held times 2^(29 - field).
-  float pm[NR][2][kG];
-#pragma unroll
-  for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-    for (int gr = 0; gr < kG; ++gr) pm[nr][0][gr] = pm[nr][1][gr] = 0.0f;
-  uint32_t field = 0;
-
-  // ---- the loop over this warp's steps
-  int stage = 0;
-  for (int step = first; step < s_end; step += kRowsWarps) {
-    {
-      const int ahead = step + (R::kStages - 1) * kRowsWarps;
-      const int to = stage == 0 ? R::kStages - 1 : stage - 1;
-      if (ahead < s_end) issue(w, ahead, page_next, to);
-      page_next = page_of(w, ahead + kRowsWarps);
-      copy_commit();
-    }
-    copy_wait<R::kStages - 1>();
-    __syncwarp();
-    const uint32_t ks_at = ring + stage * R::kStage, vs_at = ks_at + R::kTile;
-    const uint32_t kp_at = ks_at + 2 * R::kTile, vp_at = kp_at + R::kPar;
-    const int key0 = kr.key0<kRowsStep>(step);
-
-    float sc[2][NR][4];
-    // S^T: 2 tiles of 16 keys
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
+    for (int nr = 0; nr < NR; ++nr) {
+      const int r = row0 + nr * 8 + g;
+      const bool in = r <= row1;
+      const int tok = a.by_share(in ? r : row0), hq = (in ? r : row0) - tok * a.share;
+      const uint16_t* qp = a.q + (seq.row0 + static_cast<int64_t>(tok)) * a.q_row + (head * a.share + hq) * a.q_head;
       if constexpr (kB) {
 #pragma unroll
-        for (int nr = 0; nr < NR; ++nr) sc[mt][nr][0] = sc[mt][nr][1] = sc[mt][nr][2] = sc[mt][nr][3] = 0.0f;
-        const int r = mt * 16 + (lane & 15);
+        for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int ch = ks * 16 + i * 8 + 2 * t;
+            qb[ks][nr][i] = in && ch < a.p.dim ? *reinterpret_cast<const uint32_t*>(qp + ch) : 0u;
+          }
+      } else {
+        // The row's largest magnitude goes to [2^9, 2^10): its 1/16ths and its
+        // products with subnormal codes keep all their bits. 4 threads share a row.
+        uint32_t top = 0;
+        for (int ch = 8 * t; ch < DP; ch += 32) {
+          const uint4 x = in ? *reinterpret_cast<const uint4*>(qp + ch) : make_uint4(0, 0, 0, 0);
+          const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = max(top, max(xs[i] & 0x7FFFu, (xs[i] >> 16) & 0x7FFFu));
+        }
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int e = min(max(static_cast<int>(top >> 7) - 127, -100), 126);
+        const float up = __uint_as_float(static_cast<uint32_t>(127 + 9 - e) << 23);
+        const float down = __uint_as_float(static_cast<uint32_t>(127 - 9 + e) << 23);
+        auto load = [&](int ch, float f) {
+          const float x = in ? __uint_as_float(static_cast<uint32_t>(qp[ch]) << 16) : 0.0f;
+          return x * up * f;
+        };
+        float sum[kG];
+#pragma unroll
+        for (int gr = 0; gr < kG; ++gr) sum[gr] = 0.0f;
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks) {
-          uint32_t ka[4];
-          ldsm4(ka, ks_at + r * R::kRowB + swizzle<FMT, R::kRowB>(r, 2 * ks + (lane >> 4)) * 16);
-#pragma unroll
-          for (int nr = 0; nr < NR; ++nr) mma<true>(sc[mt][nr], ka, qb[ks][nr][0], qb[ks][nr][1]);
+          const int gr = ks >> 2, w = FMT == kU8 ? ks & 3 : (ks >> 1) & 1;
+          const bool hi4 = FMT == kU4 && (ks & 1);  // nibbles 1, 5, 3, 7 stand 4 bits up
+          const float f = hi4 ? 0.0625f : 1.0f;
+          const int c0 = gr * kGroup + (FMT == kU8 ? 4 : 8) * (t + 4 * w) + (hi4 ? 1 : 0);
+          const int d = FMT == kU8 ? 2 : 4, d2 = FMT == kU8 ? 1 : 2;
+          qb[ks][nr][0] = pack2<false>(load(c0, f), load(c0 + d, f));
+          qb[ks][nr][1] = pack2<false>(load(c0 + d2, f), load(c0 + d2 + d, f));
+          const __half2 s2a = as_half2(qb[ks][nr][0]), s2b = as_half2(qb[ks][nr][1]);
+          sum[gr] += (__low2float(s2a) + __high2float(s2a) + __low2float(s2b) + __high2float(s2b)) * (hi4 ? 16.0f : 1.0f);
         }
-#pragma unroll
-        for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sc[mt][nr][i] *= a.scale_log2;
-      } else {
-        float part[kG][NR][4];
-#pragma unroll
-        for (int gr = 0; gr < kG; ++gr)
-#pragma unroll
-          for (int nr = 0; nr < NR; ++nr) part[gr][nr][0] = part[gr][nr][1] = part[gr][nr][2] = part[gr][nr][3] = 0.0f;
-        const int r0 = mt * 16 + key_at<FMT>(g), r1 = r0 + 8;
+        const float c = a.scale_log2 * down;
 #pragma unroll
         for (int gr = 0; gr < kG; ++gr) {
-          if constexpr (FMT == kU8) {
-            const uint4 x = lds128(ks_at + r0 * R::kRowB + swizzle<FMT, R::kRowB>(r0, gr * 4 + t) * 16);
-            const uint4 y = lds128(ks_at + r1 * R::kRowB + swizzle<FMT, R::kRowB>(r1, gr * 4 + t) * 16);
-            const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              const uint32_t ka[4] = {xs[w] & 0x00FF00FFu, ys[w] & 0x00FF00FFu, (xs[w] >> 8) & 0x00FF00FFu,
-                                      (ys[w] >> 8) & 0x00FF00FFu};
-#pragma unroll
-              for (int nr = 0; nr < NR; ++nr) mma<false>(part[gr][nr], ka, qb[gr * 4 + w][nr][0], qb[gr * 4 + w][nr][1]);
-            }
-          } else {
-            const int c = gr * 2 + (t >> 1), in = (t & 1) * 8;
-            const uint2 x = lds64(ks_at + r0 * R::kRowB + swizzle<FMT, R::kRowB>(r0, c) * 16 + in);
-            const uint2 y = lds64(ks_at + r1 * R::kRowB + swizzle<FMT, R::kRowB>(r1, c) * 16 + in);
-            const uint32_t xs[2] = {x.x, x.y}, ys[2] = {y.x, y.y};
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-              const uint32_t xh = xs[w] >> 8, yh = ys[w] >> 8;
-              const uint32_t k0[4] = {xs[w] & 0x000F000Fu, ys[w] & 0x000F000Fu, xh & 0x000F000Fu, yh & 0x000F000Fu};
-              const uint32_t k1[4] = {xs[w] & 0x00F000F0u, ys[w] & 0x00F000F0u, xh & 0x00F000F0u, yh & 0x00F000F0u};
-#pragma unroll
-              for (int nr = 0; nr < NR; ++nr) {
-                mma<false>(part[gr][nr], k0, qb[gr * 4 + 2 * w][nr][0], qb[gr * 4 + 2 * w][nr][1]);
-                mma<false>(part[gr][nr], k1, qb[gr * 4 + 2 * w + 1][nr][0], qb[gr * 4 + 2 * w + 1][nr][1]);
-              }
-            }
-          }
-        }
-        uint32_t p0[kG], p1[kG];
-#pragma unroll
-        for (int gr = 0; gr < kG; ++gr) {
-          p0[gr] = lds32(kp_at + (r0 * kG + gr) * 4);
-          p1[gr] = lds32(kp_at + (r1 * kG + gr) * 4);
+          sum[gr] += __shfl_xor_sync(0xffffffffu, sum[gr], 1);
+          sum[gr] += __shfl_xor_sync(0xffffffffu, sum[gr], 2);
         }
 #pragma unroll
-        for (int nr = 0; nr < NR; ++nr)
+        for (int i = 0; i < 2; ++i) {
+          c_acc[nr][i] = __shfl_sync(0xffffffffu, c * 16777216.0f, 4 * (2 * t + i));
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float x = 0.0f, y = 0.0f;
-#pragma unroll
-            for (int gr = 0; gr < kG; ++gr) {
-              const uint32_t pp = i < 2 ? p0[gr] : p1[gr];
-              x = fmaf(par_step(pp), part[gr][nr][i], x);
-              y = fmaf(par_min(pp), c_min[nr][i & 1][gr], y);
-            }
-            sc[mt][nr][i] = fmaf(c_acc[nr][i & 1], x, y);
-          }
+          for (int gr = 0; gr < kG; ++gr) c_min[nr][i][gr] = __shfl_sync(0xffffffffu, c * sum[gr], 4 * (2 * t + i));
+        }
       }
     }
-    // The mask, only where some row of the tile does not see all 32 keys.
-    if (!(key0 + kRowsStep <= kr.hi_min && (key0 >= kr.lo_max || key0 + kRowsStep <= a.sinks))) {
+
+    // ---- what the thread's two rows of each row tile see
+    int hi[NR][2];
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
+    for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int j = key0 + mt * 16 + key_at<FMT>(g) + (i >> 1) * 8;
+      for (int i = 0; i < 2; ++i) {
+        const int r = row0 + nr * 8 + 2 * t + i;
+        hi[nr][i] = r <= row1 ? token_hi(a, seq, a.by_share(r)) : 0;
+      }
+
+    float o[kCt][NR][4];
+    float m[NR][2], l[NR][2];
 #pragma unroll
-          for (int nr = 0; nr < NR; ++nr) {
-            const int h = hi[nr][i & 1];
-            const bool sees = j < h && (!a.window || j >= h - a.window || j < a.sinks);
-            if (!sees) sc[mt][nr][i] = kNegInf;
-          }
-        }
+    for (int nr = 0; nr < NR; ++nr) {
+      m[nr][0] = m[nr][1] = kNegInf;
+      l[nr][0] = l[nr][1] = 0.0f;
+#pragma unroll
+      for (int ct = 0; ct < kCt; ++ct) o[ct][nr][0] = o[ct][nr][1] = o[ct][nr][2] = o[ct][nr][3] = 0.0f;
     }
-    // V's steps and minima of this thread's keys, and room for the largest step.
-    float vs[2][2][kG], vm[2][2][kG];
-    if constexpr (!kB) {
-      uint32_t most = 0;
-      uint32_t vp[2][2][kG];
+
+    // Codes: sums of p m, and the largest step so far, as its fp16 exponent field;
+    // weights times steps are held times 2^(29 - field).
+    float pm[NR][2][kG];
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
+    for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-        for (int k8 = 0; k8 < 2; ++k8)
+      for (int gr = 0; gr < kG; ++gr) pm[nr][0][gr] = pm[nr][1][gr] = 0.0f;
+    uint32_t field = 0;
+
+    // ---- the loop over this warp's steps
+    int stage = 0;
+    for (int step = first; step < s_end; step += kRowsWarps) {
+      {
+        const int ahead = step + (R::kStages - 1) * kRowsWarps;
+        const int to = stage == 0 ? R::kStages - 1 : stage - 1;
+        if (ahead < s_end) issue(w, ahead, page_next, to);
+        page_next = page_of(w, ahead + kRowsWarps);
+        copy_commit();
+      }
+      copy_wait<R::kStages - 1>();
+      __syncwarp();
+      const uint32_t ks_at = ring + stage * R::kStage, vs_at = ks_at + R::kTile;
+      const uint32_t kp_at = ks_at + 2 * R::kTile, vp_at = kp_at + R::kPar;
+      const int key0 = kr.key0<kRowsStep>(step);
+
+      float sc[2][NR][4];
+      // S^T: 2 tiles of 16 keys
 #pragma unroll
-          for (int gr = 0; gr < kG; ++gr) {
-            vp[mt][k8][gr] = lds32(vp_at + ((mt * 16 + key_at<FMT>(g) + 8 * k8) * kG + gr) * 4);
-            most = max(most, vp[mt][k8][gr] & 0x7C00u);
+      for (int mt = 0; mt < 2; ++mt) {
+        if constexpr (kB) {
+#pragma unroll
+          for (int nr = 0; nr < NR; ++nr) sc[mt][nr][0] = sc[mt][nr][1] = sc[mt][nr][2] = sc[mt][nr][3] = 0.0f;
+          const int r = mt * 16 + (lane & 15);
+#pragma unroll
+          for (int ks = 0; ks < kKs; ++ks) {
+            uint32_t ka[4];
+            ldsm4(ka, ks_at + r * R::kRowB + swizzle<FMT, R::kRowB>(r, 2 * ks + (lane >> 4)) * 16);
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr) mma<true>(sc[mt][nr], ka, qb[ks][nr][0], qb[ks][nr][1]);
           }
-      most = min(__reduce_max_sync(0xffffffffu, most) >> 10, 30u);
-      if (most > field) {  // rarely: the same for the whole warp
-        const float f = __uint_as_float((127u + field - most) << 23);
-#pragma unroll
-        for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
           for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[ct][nr][i] *= f;
-        field = most;
-      }
-      const float up = __uint_as_float((127u + 29u - field) << 23);
+            for (int i = 0; i < 4; ++i) sc[mt][nr][i] *= a.scale_log2;
+        } else {
+          float part[kG][NR][4];
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
+          for (int gr = 0; gr < kG; ++gr)
 #pragma unroll
-        for (int k8 = 0; k8 < 2; ++k8)
+            for (int nr = 0; nr < NR; ++nr) part[gr][nr][0] = part[gr][nr][1] = part[gr][nr][2] = part[gr][nr][3] = 0.0f;
+          const int r0 = mt * 16 + key_at<FMT>(g), r1 = r0 + 8;
 #pragma unroll
           for (int gr = 0; gr < kG; ++gr) {
-            vs[mt][k8][gr] = par_step(vp[mt][k8][gr]) * up;
-            vm[mt][k8][gr] = par_min(vp[mt][k8][gr]);
-          }
-    }
-    // Softmax: the rows' new maxima, weights, sums
-    uint32_t pb[2][NR][2][kB ? 2 : kG];  // bf16: the weight, and what bf16 leaves of it; codes: times each group's step
-#pragma unroll
-    for (int nr = 0; nr < NR; ++nr) {
-      float mx[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        mx[i] = fmaxf(fmaxf(sc[0][nr][i], sc[0][nr][i + 2]), fmaxf(sc[1][nr][i], sc[1][nr][i + 2]));
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], d));
-        mx[i] = fmaxf(mx[i], m[nr][i]);
-      }
-      float f[2], base[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        base[i] = mx[i] == kNegInf ? 0.0f : mx[i];
-        f[i] = exp2_fast(m[nr][i] - base[i]);
-        m[nr][i] = mx[i];
-        l[nr][i] *= f[i];
-      }
-      if (__any_sync(0xffffffffu, f[0] != 1.0f || f[1] != 1.0f)) {
-#pragma unroll
-        for (int ct = 0; ct < kCt; ++ct)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[ct][nr][i] *= f[i & 1];
-#pragma unroll
-        for (int gr = 0; gr < kG; ++gr) pm[nr][0][gr] *= f[0], pm[nr][1][gr] *= f[1];
-      }
-#pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-        for (int k8 = 0; k8 < 2; ++k8) {
-          const float p0 = exp2_fast(sc[mt][nr][2 * k8] - base[0]), p1 = exp2_fast(sc[mt][nr][2 * k8 + 1] - base[1]);
-          l[nr][0] += p0;
-          l[nr][1] += p1;
-          if constexpr (kB) {
-            const uint32_t pk = pack2<true>(p0, p1);
-            pb[mt][nr][k8][0] = transpose8(pk);
-            pb[mt][nr][k8][1] = transpose8(
-                pack2<true>(p0 - __uint_as_float(pk << 16), p1 - __uint_as_float(pk & 0xFFFF0000u)));
-          } else {
-#pragma unroll
-            for (int gr = 0; gr < kG; ++gr) {
-              pb[mt][nr][k8][gr] = transpose8(pack2<false>(p0 * vs[mt][k8][gr], p1 * vs[mt][k8][gr]));
-              pm[nr][0][gr] = fmaf(p0, vm[mt][k8][gr], pm[nr][0][gr]);
-              pm[nr][1][gr] = fmaf(p1, vm[mt][k8][gr], pm[nr][1][gr]);
-            }
-          }
-        }
-    }
-    // O^T += V^T P^T
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
-      if constexpr (kB) {
-        const int r = mt * 16 + (lane & 7) + ((lane >> 4) << 3);
-#pragma unroll
-        for (int ct = 0; ct < kCt; ++ct) {
-          uint32_t va[4];
-          ldsm4t(va, vs_at + r * R::kRowB + swizzle<FMT, R::kRowB>(r, 2 * ct + ((lane >> 3) & 1)) * 16);
-#pragma unroll
-          for (int nr = 0; nr < NR; ++nr) {
-            mma<true>(o[ct][nr], va, pb[mt][nr][0][0], pb[mt][nr][1][0]);
-            mma<true>(o[ct][nr], va, pb[mt][nr][0][1], pb[mt][nr][1][1]);
-          }
-        }
-      } else {
-        // Keys of matrix columns 2t, 2t+1, 2t+8, 2t+9
-        uint32_t row[4];
-        int rk[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          rk[i] = mt * 16 + key_at<FMT>(2 * t + (i & 1)) + (i >> 1) * 8;
-          row[i] = vs_at + rk[i] * R::kRowB;
-        }
-#pragma unroll
-        for (int gr = 0; gr < kG; ++gr) {
-          constexpr int kW = FMT == kU8 ? 2 : 1;  // words of a group a thread reads
-          uint32_t wd[4][kW];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
             if constexpr (FMT == kU8) {
-              const uint2 x = lds64(row[i] + swizzle<FMT, R::kRowB>(rk[i], gr * 4 + (g >> 1)) * 16 + (g & 1) * 8);
-              wd[i][0] = x.x, wd[i][1] = x.y;
+              const uint4 x = lds128(ks_at + r0 * R::kRowB + swizzle<FMT, R::kRowB>(r0, gr * 4 + t) * 16);
+              const uint4 y = lds128(ks_at + r1 * R::kRowB + swizzle<FMT, R::kRowB>(r1, gr * 4 + t) * 16);
+              const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+              for (int w = 0; w < 4; ++w) {
+                const uint32_t ka[4] = {xs[w] & 0x00FF00FFu, ys[w] & 0x00FF00FFu, (xs[w] >> 8) & 0x00FF00FFu,
+                                        (ys[w] >> 8) & 0x00FF00FFu};
+#pragma unroll
+                for (int nr = 0; nr < NR; ++nr) mma<false>(part[gr][nr], ka, qb[gr * 4 + w][nr][0], qb[gr * 4 + w][nr][1]);
+              }
             } else {
-              wd[i][0] = lds32(row[i] + swizzle<FMT, R::kRowB>(rk[i], gr * 2 + (g >> 2)) * 16 + (g & 3) * 4);
-            }
-          }
+              const int c = gr * 2 + (t >> 1), in = (t & 1) * 8;
+              const uint2 x = lds64(ks_at + r0 * R::kRowB + swizzle<FMT, R::kRowB>(r0, c) * 16 + in);
+              const uint2 y = lds64(ks_at + r1 * R::kRowB + swizzle<FMT, R::kRowB>(r1, c) * 16 + in);
+              const uint32_t xs[2] = {x.x, x.y}, ys[2] = {y.x, y.y};
 #pragma unroll
-          for (int w = 0; w < kW; ++w)
+              for (int w = 0; w < 2; ++w) {
+                const uint32_t xh = xs[w] >> 8, yh = ys[w] >> 8;
+                const uint32_t k0[4] = {xs[w] & 0x000F000Fu, ys[w] & 0x000F000Fu, xh & 0x000F000Fu, yh & 0x000F000Fu};
+                const uint32_t k1[4] = {xs[w] & 0x00F000F0u, ys[w] & 0x00F000F0u, xh & 0x00F000F0u, yh & 0x00F000F0u};
 #pragma unroll
-            for (int hl = 0; hl < 2; ++hl) {  // lower and upper 16 bits of the words
-              const uint32_t e0 = __byte_perm(wd[0][w], wd[1][w], hl ? 0x7632 : 0x5410);
-              const uint32_t e1 = __byte_perm(wd[2][w], wd[3][w], hl ? 0x7632 : 0x5410);
-              if constexpr (FMT == kU8) {
-                const int ct = gr * 4 + w * 2 + hl;
-                const uint32_t va[4] = {e0 & 0x00FF00FFu, (e0 >> 8) & 0x00FF00FFu, e1 & 0x00FF00FFu, (e1 >> 8) & 0x00FF00FFu};
-#pragma unroll
-                for (int nr = 0; nr < NR; ++nr) mma<false>(o[ct][nr], va, pb[mt][nr][0][gr], pb[mt][nr][1][gr]);
-              } else {
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {  // nibbles 0, 1 and 2, 3 of the 16 bits
-                  const int ct = gr * 4 + hl * 2 + q;
-                  const uint32_t f0 = e0 >> (8 * q), f1 = e1 >> (8 * q);
-                  const uint32_t va[4] = {f0 & 0x000F000Fu, f0 & 0x00F000F0u, f1 & 0x000F000Fu, f1 & 0x00F000F0u};
-#pragma unroll
-                  for (int nr = 0; nr < NR; ++nr) mma<false>(o[ct][nr], va, pb[mt][nr][0][gr], pb[mt][nr][1][gr]);
+                for (int nr = 0; nr < NR; ++nr) {
+                  mma<false>(part[gr][nr], k0, qb[gr * 4 + 2 * w][nr][0], qb[gr * 4 + 2 * w][nr][1]);
+                  mma<false>(part[gr][nr], k1, qb[gr * 4 + 2 * w + 1][nr][0], qb[gr * 4 + 2 * w + 1][nr][1]);
                 }
               }
             }
+          }
+          uint32_t p0[kG], p1[kG];
+#pragma unroll
+          for (int gr = 0; gr < kG; ++gr) {
+            p0[gr] = lds32(kp_at + (r0 * kG + gr) * 4);
+            p1[gr] = lds32(kp_at + (r1 * kG + gr) * 4);
+          }
+#pragma unroll
+          for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float x = 0.0f, y = 0.0f;
+#pragma unroll
+              for (int gr = 0; gr < kG; ++gr) {
+                const uint32_t pp = i < 2 ? p0[gr] : p1[gr];
+                x = fmaf(par_step(pp), part[gr][nr][i], x);
+                y = fmaf(par_min(pp), c_min[nr][i & 1][gr], y);
+              }
+              sc[mt][nr][i] = fmaf(c_acc[nr][i & 1], x, y);
+            }
         }
       }
+      // The mask, only where some row of the tile does not see all 32 keys.
+      if (!(key0 + kRowsStep <= kr.hi_min && (key0 >= kr.lo_max || key0 + kRowsStep <= a.sinks))) {
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int j = key0 + mt * 16 + key_at<FMT>(g) + (i >> 1) * 8;
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr) {
+              const int h = hi[nr][i & 1];
+              const bool sees = j < h && (!a.window || j >= h - a.window || j < a.sinks);
+              if (!sees) sc[mt][nr][i] = kNegInf;
+            }
+          }
+      }
+      // V's steps and minima of this thread's keys, and room for the largest step.
+      float vs[2][2][kG], vm[2][2][kG];
+      if constexpr (!kB) {
+        uint32_t most = 0;
+        uint32_t vp[2][2][kG];
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+          for (int k8 = 0; k8 < 2; ++k8)
+#pragma unroll
+            for (int gr = 0; gr < kG; ++gr) {
+              vp[mt][k8][gr] = lds32(vp_at + ((mt * 16 + key_at<FMT>(g) + 8 * k8) * kG + gr) * 4);
+              most = max(most, vp[mt][k8][gr] & 0x7C00u);
+            }
+        most = min(__reduce_max_sync(0xffffffffu, most) >> 10, 30u);
+        if (most > field) {  // rarely: the same for the whole warp
+          const float f = __uint_as_float((127u + field - most) << 23);
+#pragma unroll
+          for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[ct][nr][i] *= f;
+          field = most;
+        }
+        const float up = __uint_as_float((127u + 29u - field) << 23);
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+          for (int k8 = 0; k8 < 2; ++k8)
+#pragma unroll
+            for (int gr = 0; gr < kG; ++gr) {
+              vs[mt][k8][gr] = par_step(vp[mt][k8][gr]) * up;
+              vm[mt][k8][gr] = par_min(vp[mt][k8][gr]);
+            }
+      }
+      // Softmax: the rows' new maxima, weights, sums
+      uint32_t pb[2][NR][2][kB ? 2 : kG];  // bf16: the weight, and what bf16 leaves of it; codes: times each group's step
+#pragma unroll
+      for (int nr = 0; nr < NR; ++nr) {
+        float mx[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          mx[i] = fmaxf(fmaxf(sc[0][nr][i], sc[0][nr][i + 2]), fmaxf(sc[1][nr][i], sc[1][nr][i + 2]));
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], d));
+          mx[i] = fmaxf(mx[i], m[nr][i]);
+        }
+        float f[2], base[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          base[i] = mx[i] == kNegInf ? 0.0f : mx[i];
+          f[i] = exp2_fast(m[nr][i] - base[i]);
+          m[nr][i] = mx[i];
+          l[nr][i] *= f[i];
+        }
+        if (__any_sync(0xffffffffu, f[0] != 1.0f || f[1] != 1.0f)) {
+#pragma unroll
+          for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[ct][nr][i] *= f[i & 1];
+#pragma unroll
+          for (int gr = 0; gr < kG; ++gr) pm[nr][0][gr] *= f[0], pm[nr][1][gr] *= f[1];
+        }
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+          for (int k8 = 0; k8 < 2; ++k8) {
+            const float p0 = exp2_fast(sc[mt][nr][2 * k8] - base[0]), p1 = exp2_fast(sc[mt][nr][2 * k8 + 1] - base[1]);
+            l[nr][0] += p0;
+            l[nr][1] += p1;
+            if constexpr (kB) {
+              const uint32_t pk = pack2<true>(p0, p1);
+              pb[mt][nr][k8][0] = transpose8(pk);
+              pb[mt][nr][k8][1] = transpose8(
+                  pack2<true>(p0 - __uint_as_float(pk << 16), p1 - __uint_as_float(pk & 0xFFFF0000u)));
+            } else {
+#pragma unroll
+              for (int gr = 0; gr < kG; ++gr) {
+                pb[mt][nr][k8][gr] = transpose8(pack2<false>(p0 * vs[mt][k8][gr], p1 * vs[mt][k8][gr]));
+                pm[nr][0][gr] = fmaf(p0, vm[mt][k8][gr], pm[nr][0][gr]);
+                pm[nr][1][gr] = fmaf(p1, vm[mt][k8][gr], pm[nr][1][gr]);
+              }
+            }
+          }
+      }
+      // O^T += V^T P^T
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt) {
+        if constexpr (kB) {
+          const int r = mt * 16 + (lane & 7) + ((lane >> 4) << 3);
+#pragma unroll
+          for (int ct = 0; ct < kCt; ++ct) {
+            uint32_t va[4];
+            ldsm4t(va, vs_at + r * R::kRowB + swizzle<FMT, R::kRowB>(r, 2 * ct + ((lane >> 3) & 1)) * 16);
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr) {
+              mma<true>(o[ct][nr], va, pb[mt][nr][0][0], pb[mt][nr][1][0]);
+              mma<true>(o[ct][nr], va, pb[mt][nr][0][1], pb[mt][nr][1][1]);
+            }
+          }
+        } else {
+          // Keys of matrix columns 2t, 2t+1, 2t+8, 2t+9
+          uint32_t row[4];
+          int rk[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            rk[i] = mt * 16 + key_at<FMT>(2 * t + (i & 1)) + (i >> 1) * 8;
+            row[i] = vs_at + rk[i] * R::kRowB;
+          }
+#pragma unroll
+          for (int gr = 0; gr < kG; ++gr) {
+            constexpr int kW = FMT == kU8 ? 2 : 1;  // words of a group a thread reads
+            uint32_t wd[4][kW];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if constexpr (FMT == kU8) {
+                const uint2 x = lds64(row[i] + swizzle<FMT, R::kRowB>(rk[i], gr * 4 + (g >> 1)) * 16 + (g & 1) * 8);
+                wd[i][0] = x.x, wd[i][1] = x.y;
+              } else {
+                wd[i][0] = lds32(row[i] + swizzle<FMT, R::kRowB>(rk[i], gr * 2 + (g >> 2)) * 16 + (g & 3) * 4);
+              }
+            }
+#pragma unroll
+            for (int w = 0; w < kW; ++w)
+#pragma unroll
+              for (int hl = 0; hl < 2; ++hl) {  // lower and upper 16 bits of the words
+                const uint32_t e0 = __byte_perm(wd[0][w], wd[1][w], hl ? 0x7632 : 0x5410);
+                const uint32_t e1 = __byte_perm(wd[2][w], wd[3][w], hl ? 0x7632 : 0x5410);
+                if constexpr (FMT == kU8) {
+                  const int ct = gr * 4 + w * 2 + hl;
+                  const uint32_t va[4] = {e0 & 0x00FF00FFu, (e0 >> 8) & 0x00FF00FFu, e1 & 0x00FF00FFu, (e1 >> 8) & 0x00FF00FFu};
+#pragma unroll
+                  for (int nr = 0; nr < NR; ++nr) mma<false>(o[ct][nr], va, pb[mt][nr][0][gr], pb[mt][nr][1][gr]);
+                } else {
+#pragma unroll
+                  for (int q = 0; q < 2; ++q) {  // nibbles 0, 1 and 2, 3 of the 16 bits
+                    const int ct = gr * 4 + hl * 2 + q;
+                    const uint32_t f0 = e0 >> (8 * q), f1 = e1 >> (8 * q);
+                    const uint32_t va[4] = {f0 & 0x000F000Fu, f0 & 0x00F000F0u, f1 & 0x000F000Fu, f1 & 0x00F000F0u};
+#pragma unroll
+                    for (int nr = 0; nr < NR; ++nr) mma<false>(o[ct][nr], va, pb[mt][nr][0][gr], pb[mt][nr][1][gr]);
+                  }
+                }
+              }
+          }
+        }
+      }
+      __syncwarp();  // the stage is read before its next copies are issued
+      stage = stage + 1 == R::kStages ? 0 : stage + 1;
     }
-    __syncwarp();  // the stage is read before its next copies are issued
-    stage = stage + 1 == R::kStages ? 0 : stage + 1;
-  }
-  // The next run's first steps are on their way while this one's results are joined.
-  const bool partial = !(w.starts() && w.ends());
-  const int pair = w.pair(tiles), ends = (w.starts() ? 1 : 0) | (w.ends() ? 2 : 0);
-  go = w.next(a, tiles);
-  if (go) fill(w);
+    // The next run's first steps are on their way while this one's results are joined.
+    const bool partial = !(w.starts() && w.ends());
+    const int pair = w.pair(tiles), ends = (w.starts() ? 1 : 0) | (w.ends() ? 2 : 0);
+    go = w.next(a, tiles);
+    if (go) fill(w);
 
-  // ---- join the warps
-  constexpr int kRows = 8 * NR;
-  float* so = reinterpret_cast<float*>(smem + R::kBytes);           // [warps][rows][DP + 4]
-  constexpr int kPitch = DP + 4;
-  float* sm = so + kRowsWarps * kRows * kPitch;                     // [warps][rows] maxima, then sums
-  float* sl = sm + kRowsWarps * kRows;
+    // ---- join the warps
+    constexpr int kRows = 8 * NR;
+    float* so = reinterpret_cast<float*>(smem + R::kBytes);           // [warps][rows][DP + 4]
+    constexpr int kPitch = DP + 4;
+    float* sm = so + kRowsWarps * kRows * kPitch;                     // [warps][rows] maxima, then sums
+    float* sl = sm + kRowsWarps * kRows;
 #pragma unroll
-  for (int nr = 0; nr < NR; ++nr)
+    for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      float x = l[nr][i];
+      for (int i = 0; i < 2; ++i) {
+        float x = l[nr][i];
 #pragma unroll
-      for (int d = 4; d < 32; d <<= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-      const int r = nr * 8 + 2 * t + i;
-      if (g == 0) {
-        sm[warp * kRows + r] = m[nr][i];
-        sl[warp * kRows + r] = x;
-      }
-      float add[kG], times[2] = {1.0f, 1.0f};
-#pragma unroll
-      for (int gr = 0; gr < kG; ++gr) {
-        add[gr] = 0.0f;
-        if constexpr (!kB) {
-          add[gr] = pm[nr][i][gr];
-#pragma unroll
-          for (int d = 4; d < 32; d <<= 1) add[gr] += __shfl_xor_sync(0xffffffffu, add[gr], d);
+        for (int d = 4; d < 32; d <<= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+        const int r = nr * 8 + 2 * t + i;
+        if (g == 0) {
+          sm[warp * kRows + r] = m[nr][i];
+          sl[warp * kRows + r] = x;
         }
+        float add[kG], times[2] = {1.0f, 1.0f};
+#pragma unroll
+        for (int gr = 0; gr < kG; ++gr) {
+          add[gr] = 0.0f;
+          if constexpr (!kB) {
+            add[gr] = pm[nr][i][gr];
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) add[gr] += __shfl_xor_sync(0xffffffffu, add[gr], d);
+          }
+        }
+        if constexpr (!kB) {  // codes stood for u 2^-24, odd nibbles for 16 u 2^-24
+          times[0] = __uint_as_float((127u + 24u - 29u + field) << 23);
+          times[1] = FMT == kU4 ? times[0] * 0.0625f : times[0];
+        }
+#pragma unroll
+        for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+            so[(warp * kRows + r) * kPitch + out_channel<FMT>(ct, half, g)] =
+                kB ? o[ct][nr][half * 2 + i] : fmaf(o[ct][nr][half * 2 + i], times[half], add[kB ? 0 : ct >> 2]);
       }
-      if constexpr (!kB) {  // codes stood for u 2^-24, odd nibbles for 16 u 2^-24
-        times[0] = __uint_as_float((127u + 24u - 29u + field) << 23);
-        times[1] = FMT == kU4 ? times[0] * 0.0625f : times[0];
+    __syncthreads();
+    const int slot = 2 * blockIdx.x + (run > 0 ? 1 : 0);
+    if (partial && !clustered) {
+      slots |= run > 0 ? 2 : 1;
+      if (threadIdx.x == 0) a.part_rec[slot] = make_int4(1, pair, head, ends);
+    }
+    constexpr int kQuads = DP / 4;
+    for (int idx = threadIdx.x; idx < kRows * kQuads; idx += kThreads) {
+      const int r = idx / kQuads, c = (idx % kQuads) * 4;
+      if (row0 + r > row1) continue;
+      float top = sm[r];
+#pragma unroll
+      for (int x = 1; x < kRowsWarps; ++x) top = fmaxf(top, sm[x * kRows + r]);
+      const float base = top == kNegInf ? 0.0f : top;
+      float sum = 0.0f;
+      float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int x = 0; x < kRowsWarps; ++x) {
+        const float f = exp2_fast(sm[x * kRows + r] - base);
+        sum += f * sl[x * kRows + r];
+        const float4 y = *reinterpret_cast<const float4*>(so + (x * kRows + r) * kPitch + c);
+        acc.x += f * y.x, acc.y += f * y.y, acc.z += f * y.z, acc.w += f * y.w;
       }
-#pragma unroll
-      for (int ct = 0; ct < kCt; ++ct)
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-          so[(warp * kRows + r) * kPitch + out_channel<FMT>(ct, half, g)] =
-              kB ? o[ct][nr][half * 2 + i] : fmaf(o[ct][nr][half * 2 + i], times[half], add[kB ? 0 : ct >> 2]);
+      if (sum == 0.0f) acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // sees nothing, here or at all
+      if (clustered) {
+        float* row = part_rows + r * kPartPitch;
+        *reinterpret_cast<float4*>(row + c) = acc;
+        if (c == 0) *reinterpret_cast<float2*>(row + DP) = make_float2(top, sum);
+      } else if (partial) {
+        const int64_t at = static_cast<int64_t>(slot) * kRows + r;
+        if (c < a.p.dim) *reinterpret_cast<float4*>(a.part_o + at * a.p.dim + c) = acc;
+        if (c == 0) a.part_ml[at] = make_float2(top, sum);
+      } else {
+        write_row(a, seq, head, row0 + r, c, acc, top, sum);
+      }
     }
-  __syncthreads();
-  const int slot = 2 * blockIdx.x + (run > 0 ? 1 : 0);
-  if (partial && !clustered) {
-    slots |= run > 0 ? 2 : 1;
-    if (threadIdx.x == 0) a.part_rec[slot] = make_int4(1, pair, head, ends);
-  }
-  constexpr int kQuads = DP / 4;
-  for (int idx = threadIdx.x; idx < kRows * kQuads; idx += kThreads) {
-    const int r = idx / kQuads, c = (idx % kQuads) * 4;
-    if (row0 + r > row1) continue;
-    float top = sm[r];
-#pragma unroll
-    for (int x = 1; x < kRowsWarps; ++x) top = fmaxf(top, sm[x * kRows + r]);
-    const float base = top == kNegInf ? 0.0f : top;
-    float sum = 0.0f;
-    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-    for (int x = 0; x < kRowsWarps; ++x) {
-      const float f = exp2_fast(sm[x * kRows + r] - base);
-      sum += f * sl[x * kRows + r];
-      const float4 y = *reinterpret_cast<const float4*>(so + (x * kRows + r) * kPitch + c);
-      acc.x += f * y.x, acc.y += f * y.y, acc.z += f * y.z, acc.w += f * y.w;
-    }
-    if (sum == 0.0f) acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // sees nothing, here or at all
-    if (clustered) {
-      float* row = part_rows + r * kPartPitch;
-      *reinterpret_cast<float4*>(row + c) = acc;
-      if (c == 0) *reinterpret_cast<float2*>(row + DP) = make_float2(top, sum);
-    } else if (partial) {
-      const int64_t at = static_cast<int64_t>(slot) * kRows + r;
-      if (c < a.p.dim) *reinterpret_cast<float4*>(a.part_o + at * a.p.dim + c) = acc;
-      if (c == 0) a.part_ml[at] = make_float2(top, sum);
-    } else {
-      write_row(a, seq, head, row0 + r, c, acc, top, sum);
-    }
-  }
-  __syncthreads();  // the results are read before the next run's are written
+    __syncthreads();  // the results are read before the next run's are written
   }
   if (clustered) {
     // The cluster's blocks hold a part each, in the place of their rings: every
