@@ -400,7 +400,7 @@ typedef struct {
   int n_seqs;               /* 0 (nothing to do) .. 65535 */
   int max_pages;            /* pages per sequence in the table */
   const int32_t* table;     /* device; NULL (max_pages = 1): page b */
-  int64_t table_stride;     /* >= max_pages */
+  int64_t table_stride;     /* >= max_pages; 0: all sequences read one row of the table */
   const int32_t* row_start; /* device [n_seqs + 1], ascending */
   const int32_t* kv_len;    /* device [n_seqs], new rows included */
   int64_t total_rows;       /* packed new rows: >= row_start[n_seqs] */

@@ -102,8 +102,8 @@ ipv_status check(const ipv_pages* p, const ipv_batch* b, ipv::Pages* out) {
   if (b->max_pages > 1 && (!pow2 || p->page_size < 16))
     return reject(IPV_EINVAL, "page_size %d: several pages per sequence need a power of two of at least 16", p->page_size);
   if (!b->table && b->max_pages != 1) return reject(IPV_EINVAL, "without a table max_pages must be 1");
-  if (b->table && (!aligned(b->table, 4) || b->table_stride < b->max_pages))
-    return reject(IPV_EINVAL, "table must be 4-byte aligned with table_stride >= max_pages");
+  if (b->table && (!aligned(b->table, 4) || (b->table_stride != 0 && b->table_stride < b->max_pages)))
+    return reject(IPV_EINVAL, "table must be 4-byte aligned with table_stride 0 or >= max_pages");
   if (b->total_rows < 0 || b->total_rows > INT32_MAX || b->max_rows < 0 || b->max_kv < 0)
     return reject(IPV_EINVAL, "total_rows, max_rows and max_kv must not be negative, total_rows below 2^31");
   if (b->n_seqs > 0) {

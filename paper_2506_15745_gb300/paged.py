@@ -30,7 +30,8 @@ class PagedBatch:
     """Sequences and their new rows (ipv_batch).
 
     table: int32 [n_seqs, max_pages] page numbers, or None (one page per
-    sequence, page b for sequence b). row_start: int32 [n_seqs + 1], the new
+    sequence, page b for sequence b); a row expanded to n_seqs is one set of
+    pages that all sequences read. row_start: int32 [n_seqs + 1], the new
     rows' places in packed tensors. kv_len: int32 [n_seqs], rows held, new ones
     included. The three are read on the GPU when a call runs and may be
     updated in place between calls; total_rows, max_rows and max_kv bound
@@ -48,11 +49,15 @@ class PagedBatch:
         n = kv_len.shape[0]
         _need(table is None or (table.dim() == 2 and table.shape[0] == n and table.shape[1] >= 1),
               "table is [n_seqs, max_pages]")
+        # 0: an expanded row, all sequences read it. Anything else below a row's length has no meaning; the stride of
+        # a table of one row is never used.
+        table_stride = 1 if table is None else table.stride(0) if n > 1 else table.shape[1]
+        _need(table is None or table_stride == 0 or table_stride >= table.shape[1],
+              "the rows of table overlap; table.contiguous() separates them")
         self.table, self.row_start, self.kv_len = table, row_start, kv_len
         self.n_seqs, self.total_rows, self.max_rows, self.max_kv = n, total_rows, max_rows, max_kv
         self.max_pages = 1 if table is None else table.shape[1]
-        self.struct = ipv.Batch(n, self.max_pages, ipv._ptr(table),
-                                1 if table is None else max(table.stride(0), table.shape[1]), ipv._ptr(row_start),
+        self.struct = ipv.Batch(n, self.max_pages, ipv._ptr(table), table_stride, ipv._ptr(row_start),
                                 ipv._ptr(kv_len), total_rows, max_rows, max_kv)
         self.ref = ctypes.byref(self.struct)
         self.sizes = (n, self.max_pages, total_rows, max_rows, max_kv)

@@ -582,3 +582,19 @@ def test_stream_of_its_own_without_a_workspace_is_refused():
         out = s.cache.attend(q, s.batch)
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("fmt,rows", [("bf16", 1), ("bf16", 40), ("u4", 3), ("u8", 30)])
+def test_sequences_that_share_their_pages(fmt, rows):
+    """A table of one row, expanded: several questions over one cache, each from a length of its own."""
+    gen = torch.Generator().manual_seed(171)
+    s = Setup(gen, fmt, 2, 128, 16, [700], [1])
+    lens = [700, 333, 40]
+    batch = PagedBatch(s.batch.table.expand(3, -1), torch.tensor([0, rows, 2 * rows, 3 * rows], dtype=torch.int32).cuda(),
+                       torch.tensor(lens, dtype=torch.int32).cuda(), total_rows=3 * rows, max_rows=rows, max_kv=700)
+    q = (torch.randn((3 * rows, 8, 128), generator=gen) * 1.5).bfloat16()
+    lse = torch.zeros((3 * rows, 8), device="cuda")
+    out = s.cache.attend(q.cuda(), batch, lse=lse)
+    s.k, s.v = [s.k[0][:n] for n in lens], [s.v[0][:n] for n in lens]
+    s.rows, s.lens, s.start = [rows] * 3, lens, np.arange(4) * rows
+    check_attend(s, q, out, lse, 128 ** -0.5)
