@@ -180,7 +180,7 @@ class PagedCache:
                window: int = 0, sinks: int = 0, workspace=None, stream=None):
         """ipv_attend: attention of q, bf16 [total_rows, n_q_heads, head_dim], over the rows that the batch's
         sequences hold. out: bf16 like q (allocated if None); lse: fp32
-        [total_rows, n_q_heads], filled if given. workspace: a uint8 tensor
+        [total_rows, n_q_heads], filled if given. workspace: a contiguous uint8 tensor
         that no call on another stream uses at the same time; without one the cache keeps one of its own for
         each stream that is current in a call. One host thread at a time uses a cache object."""
         n_q_heads = q.shape[1]
@@ -208,6 +208,8 @@ class PagedCache:
                 workspace = self._workspaces.get(at)
                 if workspace is None or workspace.numel() < need:
                     workspace = self._workspaces[at] = torch.empty(need, dtype=torch.uint8, device=q.device)
+            elif not (workspace.is_cuda and workspace.dtype is torch.uint8 and workspace.is_contiguous()):
+                raise ValueError("workspace must be a contiguous uint8 CUDA tensor")
             args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel()
         status = self._lib.ipv_attend(self.ref, batch.ref, ref, at)
         if status:

@@ -66,3 +66,96 @@ def test_rows_of_a_table_that_overlap_are_refused():
     flat = gpu(torch.arange(16, dtype=torch.int32))
     with pytest.raises(ValueError, match="table"):
         batch_of(flat.as_strided((4, 3), (2, 1)), 4)
+
+
+# ---------------------------------------------------------- the calls that launch
+class Library:
+    """Stands in for libipv.so: notes what it is given."""
+
+    def __init__(self, log):
+        self.log = log
+
+    def ipv_pages_read(self, pages, batch, k, v, row, head, stream):
+        self.log.append(("read", k, v, stream))
+        return 0
+
+    def ipv_attend(self, pages, batch, args, stream):
+        a = args._obj
+        self.log.append(("attend", a.out, a.workspace, a.workspace_bytes, stream))
+        return 0
+
+
+class Streams:
+    """PyTorch's streams as numbers; fills are noted with the stream that is current."""
+
+    def __init__(self, log, monkeypatch):
+        self.log, self.at, self.capturing = log, 0, False
+        monkeypatch.setattr(ipv, "_stream", lambda s: self.at if s is None else s if isinstance(s, int) else s.cuda_stream)
+        monkeypatch.setattr(torch.cuda, "stream", self.enter)
+        monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, *_: Handle(handle))
+        monkeypatch.setattr(torch.cuda, "current_stream", lambda *_: Handle(self.at))
+        monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: self.capturing)
+
+    @contextlib.contextmanager
+    def enter(self, stream):
+        before, self.at = self.at, stream.cuda_stream
+        yield
+        self.at = before
+
+
+class Handle:
+    def __init__(self, cuda_stream):
+        self.cuda_stream = cuda_stream
+
+
+NEED = 4096
+
+
+@pytest.fixture
+def world(monkeypatch):
+    """(cache, batch, q, log, streams); attention needs NEED bytes of workspace until `world.need` says otherwise."""
+    log = []
+
+    class World:
+        need = NEED
+
+    class Traced(OnGpu):
+        @classmethod
+        def __torch_function__(cls, func, types, args=(), kwargs=None):
+            out = super().__torch_function__(func, types, args, kwargs or {})
+            if func.__name__ in ("zeros_like", "new_zeros", "zero_", "fill_"):
+                log.append(("fill", out.data_ptr(), World.streams.at))
+            return out
+
+        def record_stream(self, stream):
+            log.append(("used on", self.data_ptr(), stream.cuda_stream))
+
+    empty = torch.empty
+    monkeypatch.setattr(paged.torch, "empty", lambda *a, **k: empty(*a, **{**k, "device": "cpu"}).as_subclass(Traced))
+    World.streams = Streams(log, monkeypatch)
+    monkeypatch.setattr(ipv, "attend_workspace", lambda *_: World.need)
+    World.tensor = staticmethod(lambda *shape: torch.ones(shape, dtype=torch.bfloat16).as_subclass(Traced))
+    World.cache = PagedCache.from_tensors("bf16", World.tensor(4, 2, 16, 64), World.tensor(4, 2, 16, 64))
+    World.cache._lib = Library(log)
+    World.batch = PagedBatch(ints(0, 1, 2, 3).view(1, 4), ints(0, 3), ints(50), total_rows=3, max_rows=3, max_kv=64)
+    World.q, World.log = World.tensor(3, 4, 64), log
+    return World
+
+
+def aligned(n):
+    t = torch.zeros(n + 256, dtype=torch.uint8)
+    at = -t.data_ptr() % 256
+    return t[at:at + n]
+
+
+def test_a_workspace_is_gpu_memory_that_is_really_there(world):
+    w = gpu(aligned(2 * NEED))
+    world.cache.attend(world.q, world.batch, workspace=w)
+    assert world.log[-1][2:4] == (w.data_ptr(), 2 * NEED)
+    for bad in (aligned(NEED),                                      # host memory
+                gpu(aligned(1)).expand(NEED),                       # one byte that says it is many
+                gpu(aligned(2 * NEED))[::2]):
+        n = len(world.log)
+        with pytest.raises(ValueError, match="workspace"):
+            world.cache.attend(world.q, world.batch, workspace=bad)
+        assert not any(e[0] == "attend" for e in world.log[n:])
