@@ -154,6 +154,19 @@ class PagedCache:
         _need(v.stride() == strides, f"{k_name} and {v_name} must have the same strides")
         return strides
 
+    @staticmethod
+    def _results(like, shapes, stream, at):
+        """New zeroed bf16 tensors for a call on stream `at`. Made on that stream: the fill comes before the kernel, and
+        the memory belongs to it; the current stream may use them as well."""
+        if stream is None or at == ipv._stream(None):
+            return [like.new_zeros(shape, dtype=torch.bfloat16) for shape in shapes]
+        here = torch.cuda.current_stream()
+        with torch.cuda.stream(torch.cuda.ExternalStream(at)):
+            out = [like.new_zeros(shape, dtype=torch.bfloat16) for shape in shapes]
+        for t in out:
+            t.record_stream(here)
+        return out
+
     def write(self, k_new, v_new, batch: PagedBatch, stream=None) -> None:
         """ipv_pages_write: k_new, v_new bf16 [total_rows, n_kv_heads, head_dim] into the batch's pages."""
         strides = self._pair("k_new", k_new, "v_new", v_new, batch)
@@ -164,14 +177,15 @@ class PagedCache:
 
     def read(self, batch: PagedBatch, k_out=None, v_out=None, stream=None):
         """ipv_pages_read: the batch's new rows, bf16 [total_rows, n_kv_heads, head_dim] each. Packed rows that
-        belong to no sequence are left as they are (new tensors: zero)."""
+        belong to no sequence are left as they are (new tensors: zero). New tensors belong to the call's stream."""
+        at = ipv._stream(stream)
         if k_out is None or v_out is None:
             shape = (batch.total_rows, self.n_kv_heads, self.head_dim)
-            k_out = torch.zeros(shape, dtype=torch.bfloat16, device=self.k.device) if k_out is None else k_out
-            v_out = torch.zeros(shape, dtype=torch.bfloat16, device=self.k.device) if v_out is None else v_out
+            new = self._results(self.k, [shape] * ((k_out is None) + (v_out is None)), stream, at)
+            k_out = new.pop(0) if k_out is None else k_out
+            v_out = new.pop(0) if v_out is None else v_out
         strides = self._pair("k_out", k_out, "v_out", v_out, batch)
-        status = self._lib.ipv_pages_read(self.ref, batch.ref, k_out.data_ptr(), v_out.data_ptr(), strides[0], strides[1],
-                                          ipv._stream(stream))
+        status = self._lib.ipv_pages_read(self.ref, batch.ref, k_out.data_ptr(), v_out.data_ptr(), strides[0], strides[1], at)
         if status:
             ipv._check(status)
         return k_out, v_out
@@ -179,14 +193,15 @@ class PagedCache:
     def attend(self, q, batch: PagedBatch, *, out=None, lse=None, scale: float | None = None, causal: bool = True,
                window: int = 0, sinks: int = 0, workspace=None, stream=None):
         """ipv_attend: attention of q, bf16 [total_rows, n_q_heads, head_dim], over the rows that the batch's
-        sequences hold. out: bf16 like q (allocated if None); lse: fp32
+        sequences hold. out: bf16 like q (allocated if None, on the call's stream); lse: fp32
         [total_rows, n_q_heads], filled if given. workspace: a contiguous uint8 tensor
         that no call on another stream uses at the same time; without one the cache keeps one of its own for
         each stream that is current in a call. One host thread at a time uses a cache object."""
         n_q_heads = q.shape[1]
         qs = self._packed("q", q, batch, n_q_heads, self.head_dim)
+        at = ipv._stream(stream)
         if out is None:
-            out = torch.zeros_like(q, memory_format=torch.contiguous_format)
+            out, = self._results(q, [q.shape], stream, at)
         os = self._packed("out", out, batch, n_q_heads, self.head_dim)
         if lse is not None:
             _need(lse.dtype is torch.float32 and lse.is_cuda and lse.is_contiguous() and lse.dim() == 2 and
@@ -201,7 +216,6 @@ class PagedCache:
         args.q, args.out, args.lse = q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr()
         args.q_row_stride, args.q_head_stride, args.out_row_stride, args.out_head_stride = qs[0], qs[1], os[0], os[1]
         args.scale = self.head_dim ** -0.5 if scale is None else scale
-        at = ipv._stream(stream)
         if need:
             if workspace is None:
                 _need(stream is None or at == ipv._stream(None), "a stream that is not the current one needs a workspace")

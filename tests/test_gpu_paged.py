@@ -598,3 +598,25 @@ def test_sequences_that_share_their_pages(fmt, rows):
     s.k, s.v = [s.k[0][:n] for n in lens], [s.v[0][:n] for n in lens]
     s.rows, s.lens, s.start = [rows] * 3, lens, np.arange(4) * rows
     check_attend(s, q, out, lse, 128 ** -0.5)
+
+
+@pytest.mark.parametrize("as_number", [False, True])
+def test_new_results_on_a_named_stream(as_number):
+    """The results of a call on a stream of its own are not touched by the current stream, which is far behind."""
+    gen = torch.Generator().manual_seed(181)
+    s = Setup(gen, "u8", 2, 128, 16, [300, 90], [1, 3])
+    q = make_rows(gen, 4, 8, 128).cuda()
+    want, rows = s.cache.attend(q, s.batch), s.cache.read(s.batch)
+    assert want.abs().sum() > 0
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        torch.cuda._sleep(20_000_000)  # the current stream's work: about 10 ms
+        at = side.cuda_stream if as_number else side
+        out, (k, v) = s.cache.attend(q, s.batch, stream=at), s.cache.read(s.batch, stream=at)
+        side.synchronize()
+        with torch.cuda.stream(side):
+            got = [t.clone() for t in (out, k, v)]
+        torch.cuda.synchronize()
+        for t in got, (out, k, v):
+            assert torch.equal(t[0], want) and torch.equal(t[1], rows[0]) and torch.equal(t[2], rows[1])

@@ -159,3 +159,29 @@ def test_a_workspace_is_gpu_memory_that_is_really_there(world):
         with pytest.raises(ValueError, match="workspace"):
             world.cache.attend(world.q, world.batch, workspace=bad)
         assert not any(e[0] == "attend" for e in world.log[n:])
+
+
+SIDE = 0x5000
+
+
+def test_results_are_made_on_the_stream_that_writes_them(world):
+    """Named streams: the fill of new results precedes the kernel on its stream, and their memory is not handed on
+    while the current stream may still use them."""
+    world.need = 0
+    for call in (lambda: [world.cache.attend(world.q, world.batch, stream=SIDE)],
+                 lambda: world.cache.read(world.batch, stream=SIDE),
+                 lambda: world.cache.read(world.batch, stream=Handle(SIDE))):
+        del world.log[:]
+        made = {t.data_ptr() for t in call()}
+        assert made == {e[1] for e in world.log if e[0] == "fill"}
+        assert all(e[2] == SIDE for e in world.log if e[0] == "fill"), world.log
+        assert made == {e[1] for e in world.log if e[0] == "used on" and e[2] == 0}
+        assert world.log[-1][0] in ("attend", "read") and world.log[-1][-1] == SIDE
+        assert world.streams.at == 0
+
+
+def test_results_on_the_current_stream(world):
+    out = world.cache.attend(world.q, world.batch, stream=0)
+    k, v = world.cache.read(world.batch)
+    assert [e for e in world.log if e[0] == "fill"] == [("fill", t.data_ptr(), 0) for t in (out, k, v)]
+    assert not any(e[0] == "used on" for e in world.log)
