@@ -196,7 +196,9 @@ class PagedCache:
         sequences hold. out: bf16 like q (allocated if None, on the call's stream); lse: fp32
         [total_rows, n_q_heads], filled if given. workspace: a contiguous uint8 tensor
         that no call on another stream uses at the same time; without one the cache keeps one of its own for
-        each stream that is current in a call. One host thread at a time uses a cache object."""
+        each stream that is current in a call. A call that torch.cuda.graph captures takes its workspace from the
+        graph's memory; if one is given, it has to live as long as the graph, and graphs that share it may not be
+        replayed at the same time. One host thread at a time uses a cache object."""
         n_q_heads = q.shape[1]
         qs = self._packed("q", q, batch, n_q_heads, self.head_dim)
         at = ipv._stream(stream)
@@ -219,9 +221,14 @@ class PagedCache:
         if need:
             if workspace is None:
                 _need(stream is None or at == ipv._stream(None), "a stream that is not the current one needs a workspace")
-                workspace = self._workspaces.get(at)
-                if workspace is None or workspace.numel() < need:
-                    workspace = self._workspaces[at] = torch.empty(need, dtype=torch.uint8, device=q.device)
+                if torch.cuda.is_current_stream_capturing():
+                    # From the graph's own memory, which lives as long as the graph: a kept one would be shared with
+                    # other graphs and calls, and freed when a later call needs a larger one.
+                    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+                else:
+                    workspace = self._workspaces.get(at)
+                    if workspace is None or workspace.numel() < need:
+                        workspace = self._workspaces[at] = torch.empty(need, dtype=torch.uint8, device=q.device)
             elif not (workspace.is_cuda and workspace.dtype is torch.uint8 and workspace.is_contiguous()):
                 raise ValueError("workspace must be a contiguous uint8 CUDA tensor")
             args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel()

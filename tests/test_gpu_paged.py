@@ -620,3 +620,75 @@ def test_new_results_on_a_named_stream(as_number):
         torch.cuda.synchronize()
         for t in got, (out, k, v):
             assert torch.equal(t[0], want) and torch.equal(t[1], rows[0]) and torch.equal(t[2], rows[1])
+
+
+def long_cache(gen, fmt="bf16", heads=1, kv=20000):
+    """Single tokens over this need a workspace."""
+    return Setup(gen, fmt, heads, 128, 64, [kv], [1])
+
+
+def workspace_need(cache, batch, n_q_heads, **kw):
+    args = ipv.AttendArgs(n_q_heads=n_q_heads, scale=1.0, causal=int(kw.get("causal", True)), window=kw.get("window", 0),
+                          sinks=kw.get("sinks", 0))
+    return ipv.attend_workspace(cache.ref, batch.ref, args)
+
+
+def test_a_graph_keeps_its_workspace():
+    """A captured step whose plan needs a workspace, replayed after the stream's kept workspace has been replaced by a
+    larger one and the memory of the first one has gone to other tensors."""
+    gen = torch.Generator().manual_seed(191)
+    s = long_cache(gen)
+    need = workspace_need(s.cache, s.batch, 8)
+    chunk = PagedBatch(s.batch.table, torch.tensor([0, 90], dtype=torch.int32).cuda(), s.batch.kv_len, total_rows=90, max_rows=90,
+                       max_kv=20000)
+    assert 0 < need < workspace_need(s.cache, chunk, 8)
+    q, big = make_rows(gen, 1, 8, 128).cuda(), make_rows(gen, 90, 8, 128).cuda()
+    side, out = torch.cuda.Stream(), torch.zeros(1, 8, 128, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        s.cache.attend(q, s.batch, out=out)
+        want = out.clone()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            s.cache.attend(q, s.batch, out=out)
+        after = s.cache.attend(big, chunk)
+        others = [torch.full((need,), 77, dtype=torch.uint8, device="cuda") for _ in range(6)]
+        for _ in range(3):
+            out.zero_()
+            graph.replay()
+            assert torch.equal(out, want)
+        assert all(bool((t == 77).all()) for t in others)
+        assert torch.equal(s.cache.attend(big, chunk), after)
+
+
+def test_two_graphs_and_two_streams_at_once():
+    """Two graphs over one cache, captured one after the other, and eager calls on two more streams, all in flight
+    together: none shares a workspace with another."""
+    gen = torch.Generator().manual_seed(192)
+    s = long_cache(gen, heads=2)
+    assert workspace_need(s.cache, s.batch, 16) > 0
+    q = [make_rows(gen, 1, 16, 128).cuda() for _ in range(4)]
+    want = [s.cache.attend(x, s.batch).clone() for x in q]
+    outs, graphs = [torch.zeros_like(x) for x in q], []
+    torch.cuda.synchronize()
+    for i in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            s.cache.attend(q[i], s.batch, out=outs[i])
+        graphs.append(graph)
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    for _ in range(50):
+        for o in outs:
+            o.fill_(7.0)
+        torch.cuda.synchronize()
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                for _ in range(4):
+                    if i < 2:
+                        graphs[i].replay()
+                    else:
+                        s.cache.attend(q[i], s.batch, out=outs[i])
+        torch.cuda.synchronize()
+        for o, w in zip(outs, want):
+            assert torch.equal(o, w)

@@ -185,3 +185,27 @@ def test_results_on_the_current_stream(world):
     k, v = world.cache.read(world.batch)
     assert [e for e in world.log if e[0] == "fill"] == [("fill", t.data_ptr(), 0) for t in (out, k, v)]
     assert not any(e[0] == "used on" for e in world.log)
+
+
+def last(log, kind):
+    return next(e for e in reversed(log) if e[0] == kind)
+
+
+def test_a_captured_call_does_not_use_the_kept_workspace(world):
+    """A graph's workspace is the graph's: it is not the one that later calls on the stream use, replace and free."""
+    attend = lambda: (world.cache.attend(world.q, world.batch), last(world.log, "attend")[2])[1]  # noqa: E731
+    kept = attend()
+    assert attend() == kept and list(world.cache._workspaces) == [0]
+    held = world.cache._workspaces[0]
+    world.streams.capturing = True
+    assert attend() != kept
+    assert world.cache._workspaces == {0: held}
+    world.streams.at = SIDE
+    attend()
+    assert world.cache._workspaces == {0: held}
+    world.streams.capturing, world.streams.at = False, 0
+    assert attend() == kept
+    world.streams.capturing = True  # a workspace that is given is used
+    w = gpu(aligned(NEED))
+    world.cache.attend(world.q, world.batch, workspace=w)
+    assert last(world.log, "attend")[2] == w.data_ptr()
