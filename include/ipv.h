@@ -463,7 +463,8 @@ ipv_status ipv_attend(const ipv_pages* pages, const ipv_batch* batch, const ipv_
 /* Diagnostic: the kernel for many query rows bounds every wait between its
  * warps by time. When one runs out it sets a bit in a device error word (1: the
  * copies, 2: the products, 4: the softmax gave up), the block ends without
- * writing its results, and the device stays usable. Waits for the whole device,
+ * writing its results, queries that need one of them keep what out and lse held
+ * before the call, and the device stays usable. Waits for the whole device,
  * copies the word of the current device to *err_out (0: no wait has run out
  * since the last read) and clears it. Errors: IPV_EINVAL, IPV_ECUDA. */
 ipv_status ipv_attend_error(uint32_t* err_out);

@@ -692,3 +692,25 @@ def test_two_graphs_and_two_streams_at_once():
         torch.cuda.synchronize()
         for o, w in zip(outs, want):
             assert torch.equal(o, w)
+
+
+@pytest.mark.parametrize("fmt,rows,kv", [("bf16", 100, 900), ("u8", 70, 3000), ("bf16", 90, 300)])
+def test_outputs_are_left_alone_when_a_wait_runs_out(fmt, rows, kv):
+    """A block that gave up has no results: no query gets one made of what the workspace held, here an earlier call's
+    parts of the same tiles (the last case: whole contexts, without parts)."""
+    gen = torch.Generator().manual_seed(201)
+    s = Setup(gen, fmt, 2, 128, 64, [kv], [rows])
+    need = workspace_need(s.cache, s.batch, 16)
+    ws = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
+    q, out, lse = run_attend(s, 8, 202, workspace=ws)
+    check_attend(s, q, out, lse, 128 ** -0.5)
+    assert ipv.attend_error() == 0
+    ipv.attend_wait_limit(1)
+    try:
+        _, held, lse_held = run_attend(s, 8, 202, workspace=ws)
+        assert ipv.attend_error() != 0
+    finally:
+        ipv.attend_wait_limit(0)
+    assert (held == 7.0).all() and (lse_held == 7.0).all()
+    _, again, lse_again = run_attend(s, 8, 202, workspace=ws)
+    assert ipv.attend_error() == 0 and torch.equal(again, out) and torch.equal(lse_again, lse)
