@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(kBlock) expand_kernel(ExpandArgs a) {
   // Rows skip..lo-1 lie between the sinks and the first new row's window.
   const int hi = a.causal ? max(0, s.len - s.n + 1) : s.len;
   const int lo = a.window ? max(0, hi - a.window) / a.step * a.step : 0;
-  const int skip = a.sinks > 0 ? ((a.sinks - 1) / a.step + 1) * a.step : 0;
+  const int skip = a.sinks > 0 ? min(lo / a.step, (a.sinks - 1) / a.step + 1) * a.step : 0;  // sinks may be near 2^31
   const int c = threadIdx.x & 7;
   uint32_t wk[U][2], wv[U][2], pk[U], pv[U];
   int64_t out[U];

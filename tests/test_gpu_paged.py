@@ -714,3 +714,15 @@ def test_outputs_are_left_alone_when_a_wait_runs_out(fmt, rows, kv):
     assert (held == 7.0).all() and (lse_held == 7.0).all()
     _, again, lse_again = run_attend(s, 8, 202, workspace=ws)
     assert ipv.attend_error() == 0 and torch.equal(again, out) and torch.equal(lse_again, lse)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "u8", "u4"])
+@pytest.mark.parametrize("rows", [2, 120])
+@pytest.mark.parametrize("sinks", [2 ** 31 - 1, 2 ** 31 - 128, 700])
+def test_sinks_that_cover_everything(fmt, rows, sinks):
+    """As many first rows as the header takes, and a workspace that is full of NaN."""
+    gen = torch.Generator().manual_seed(211)
+    s = Setup(gen, fmt, 1, 64, 64, [900], [rows])
+    ws = torch.empty(max(256, workspace_need(s.cache, s.batch, 4, window=10, sinks=sinks)), dtype=torch.uint8, device="cuda").fill_(255)
+    q, out, lse = run_attend(s, 4, 212, window=10, sinks=sinks, workspace=ws)
+    check_attend(s, q, out, lse, 64 ** -0.5, window=10, sinks=sinks)
