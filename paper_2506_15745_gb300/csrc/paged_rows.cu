@@ -26,6 +26,14 @@ __device__ __forceinline__ int place_u8(int word) { return 4 * (word & 3) + (wor
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+// 16 bytes that are read once. An ordinary, coherent load: the kernel is there
+// before its predecessor, which may be writing these bytes, has ended.
+__device__ __forceinline__ uint4 ld_once(const void* p) {
+  uint4 r;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p) : "memory");
+  return r;
+}
+
 // 2^23 in fp32: 2^23 + u has the integer u in its low bits.
 constexpr uint32_t kTwo23 = 0x4B000000u;
 
@@ -178,8 +186,8 @@ __global__ void __launch_bounds__(kBlock) write_kernel(RowsArgs a) {
       const int ch = g * kGroup + (c + kTeam * i) * 8;
       xk[g][i] = xv[g][i] = make_uint4(0, 0, 0, 0);
       if (it.in && ch < a.p.dim) {  // on their way while the page is looked up
-        xk[g][i] = ld_stream(a.k_new + it.packed + ch);
-        xv[g][i] = ld_stream(a.v_new + it.packed + ch);
+        xk[g][i] = ld_once(a.k_new + it.packed + ch);
+        xv[g][i] = ld_once(a.v_new + it.packed + ch);
       }
     }
   const int64_t row = row_of(a, b, it), at = row * a.p.row_bytes, par = row * a.p.groups;
@@ -235,8 +243,8 @@ __global__ void __launch_bounds__(kBlock) read_kernel(RowsArgs a) {
     xk[g] = xv[g] = make_uint4(0, 0, 0, 0);
     if (row < 0 || g * kGroup + c * 8 >= a.p.dim) continue;
     if (FMT == kBf16) {
-      xk[g] = ld_stream(a.p.k + at + g * (2 * kGroup) + c * 16);
-      xv[g] = ld_stream(a.p.v + at + g * (2 * kGroup) + c * 16);
+      xk[g] = ld_once(a.p.k + at + g * (2 * kGroup) + c * 16);
+      xv[g] = ld_once(a.p.v + at + g * (2 * kGroup) + c * 16);
     } else {
       const uint32_t* kd = reinterpret_cast<const uint32_t*>(a.p.k + at) + g * (FMT == kU8 ? kGroup / 4 : kGroup / 8);
       const uint32_t* vd = reinterpret_cast<const uint32_t*>(a.p.v + at) + g * (FMT == kU8 ? kGroup / 4 : kGroup / 8);

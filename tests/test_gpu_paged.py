@@ -726,3 +726,23 @@ def test_sinks_that_cover_everything(fmt, rows, sinks):
     ws = torch.empty(max(256, workspace_need(s.cache, s.batch, 4, window=10, sinks=sinks)), dtype=torch.uint8, device="cuda").fill_(255)
     q, out, lse = run_attend(s, 4, 212, window=10, sinks=sinks, workspace=ws)
     check_attend(s, q, out, lse, 64 ** -0.5, window=10, sinks=sinks)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "u8"])
+def test_rows_rewritten_and_read_back_in_one_go(fmt):
+    """Writes and reads of the same rows, launched one behind the other: each read returns what the write before it wrote."""
+    gen = torch.Generator().manual_seed(221)
+    cache = PagedCache(8, 16, 4, 128, fmt)
+    table = torch.randperm(8, generator=gen).to(torch.int32)[None].cuda()
+    batch = PagedBatch(table, torch.tensor([0, 40], dtype=torch.int32).cuda(), torch.tensor([100], dtype=torch.int32).cuda(),
+                       total_rows=40, max_rows=40, max_kv=128)
+    rows = make_rows(gen, 200, 40, 4, 128)
+    x = rows.cuda()
+    outs = torch.zeros((200, 2, 40, 4, 128), dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    for i in range(200):
+        cache.write(x[i], x[199 - i], batch)
+        cache.read(batch, outs[i, 0], outs[i, 1])
+    torch.cuda.synchronize()
+    want = rows if fmt == "bf16" else ref.values(*ref.quantise(rows, fmt)).float().bfloat16()
+    assert torch.equal(outs[:, 0].cpu(), want) and torch.equal(outs[:, 1].cpu(), want.flip(0))

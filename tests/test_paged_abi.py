@@ -1,6 +1,7 @@
 """The paged cache's entry points refuse bad arguments on the host, before a GPU
 is touched; the float64 definitions that the GPU tests use hold on worked cases."""
 import ctypes
+import os
 
 import pytest
 
@@ -148,3 +149,13 @@ def test_attend_worked_case():
     assert torch.equal(out, torch.ones_like(out)) and float(lse) == 4.0
     assert ref.sees(5, 2, True, 2, 1).tolist() == [[True, False, True, True, False], [True, False, False, True, True]]
     assert not ref.sees(3, 5, True, 0, 0)[:2].any()
+
+
+def test_overlapping_kernels_read_coherently():
+    """The paged cache's kernels are launched before their predecessors end, which may still be writing what they are
+    about to read: no loads through the path that is for memory nobody writes while the kernel is there."""
+    for name in ("paged_rows.cu", "attend_rows.cu", "attend_tiles.cu", "attend_share.cuh", "paged.cuh"):
+        with open(os.path.join(ipv_build.CSRC, name)) as f:
+            text = f.read()
+        for banned in ("ld_stream(", "ld.global.nc", "__ldg("):
+            assert banned not in text, (name, banned)
