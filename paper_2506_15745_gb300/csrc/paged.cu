@@ -154,6 +154,15 @@ ipv_status check_packed(const void* x, const char* name, int64_t row, int64_t he
   return IPV_OK;
 }
 
+// The rows kernel reads K and V once per 16 query rows, the tiled kernel once per
+// 256, after widening codes and with a longer way in and out. Up to 64 rows (per
+// sequence and KV head) the rows kernel is the faster one for codes (7 query heads,
+// 4 KV heads, 6000 rows, 16 sequences of 4 tokens, u4: 51 against 109 us; of 9 tokens
+// 84 against 110), and for bf16 where it reads little (1 sequence of 8 tokens over 9000
+// rows, 74 MB: 19 against 24 us; 16 of 9 tokens over 600, 78 MB: 25 against 20; 16 of 3
+// tokens over 6000, 393 MB: 65 against 48).
+constexpr int64_t kRowsMost = 64, kRowsBytes = 76 << 20;
+
 ipv_status check_attend(const ipv_pages* p, const ipv_batch* b, const ipv_attend_args* t, ipv::AttendArgs* a) {
   ipv_status s = check(p, b, &a->p);
   if (s != IPV_OK) return s;
@@ -166,8 +175,11 @@ ipv_status check_attend(const ipv_pages* p, const ipv_batch* b, const ipv_attend
   if (t->window > 0 && !t->causal) return reject(IPV_EINVAL, "a window needs causal = 1");
   if (static_cast<int64_t>(a->p.max_rows) * t->n_q_heads > INT32_MAX)
     return reject(IPV_EINVAL, "max_rows * n_q_heads exceeds 2^31 - 1");
-  const int64_t tiles = (static_cast<int64_t>(a->p.max_rows) * (t->n_q_heads / p->n_kv_heads) + 15) / 16;
-  if (tiles * a->p.n_seqs > INT32_MAX) return reject(IPV_EINVAL, "n_seqs times the query tiles of max_rows exceeds 2^31 - 1");
+  const int64_t rows = static_cast<int64_t>(a->p.max_rows) * (t->n_q_heads / p->n_kv_heads);
+  if ((rows + 15) / 16 * a->p.n_seqs > INT32_MAX) return reject(IPV_EINVAL, "n_seqs times the query tiles of max_rows exceeds 2^31 - 1");
+  if (a->p.fmt != ipv::kBf16 && rows > kRowsMost &&  // widened into the workspace
+      4.0 * a->p.n_seqs * a->p.heads * a->p.max_kv * a->p.dim >= 1152921504606846976.0)
+    return reject(IPV_EINVAL, "n_seqs * n_kv_heads * max_kv * head_dim: the workspace would exceed 2^60 bytes");
   a->q_heads = t->n_q_heads;
   a->share = t->n_q_heads / p->n_kv_heads;
   a->by_share = ipv::Divide(a->share);
@@ -181,15 +193,6 @@ ipv_status check_attend(const ipv_pages* p, const ipv_batch* b, const ipv_attend
 // Longest that a wait inside the tiled kernel may take (ipv_attend_wait_limit).
 constexpr int64_t kDefaultLimitNs = 4000000000;
 std::atomic<int64_t> g_limit_ns{kDefaultLimitNs};
-
-// The rows kernel reads K and V once per 16 query rows, the tiled kernel once per
-// 256, after widening codes and with a longer way in and out. Up to 64 rows (per
-// sequence and KV head) the rows kernel is the faster one for codes (7 query heads,
-// 4 KV heads, 6000 rows, 16 sequences of 4 tokens, u4: 51 against 109 us; of 9 tokens
-// 84 against 110), and for bf16 where it reads little (1 sequence of 8 tokens over 9000
-// rows, 74 MB: 19 against 24 us; 16 of 9 tokens over 600, 78 MB: 25 against 20; 16 of 3
-// tokens over 6000, 393 MB: 65 against 48).
-constexpr int64_t kRowsMost = 64, kRowsBytes = 76 << 20;
 
 // Least share of a block, in steps and what a run costs beside them: below,
 // joining parts costs more than the other blocks save.
@@ -219,7 +222,8 @@ int64_t round256(int64_t x) { return (x + 255) & ~int64_t{255}; }
 void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
   const ipv::Pages& p = a->p;
   const int64_t rows = static_cast<int64_t>(p.max_rows) * a->share;
-  const int64_t read = (rows + 15) / 16 * p.n_seqs * p.heads * std::min<int64_t>(p.max_kv, a->window ? int64_t{a->window} + a->sinks + 64 : p.max_kv) * 2 * p.row_bytes;
+  const int64_t keys = std::min<int64_t>(p.max_kv, a->window ? int64_t{a->window} + a->sinks + 64 : p.max_kv);
+  const double read = static_cast<double>((rows + 15) / 16 * p.n_seqs) * static_cast<double>(keys) * p.heads * 2 * p.row_bytes;  // bytes
   const bool waves = p.max_kv <= kWhole && (rows + 15) / 16 * p.n_seqs * p.heads > num_sms;  // of blocks that take tiles whole
   plan->tiles = rows > kRowsMost || (rows > 16 && p.fmt == ipv::kBf16 && (read > kRowsBytes || waves));
   plan->bytes = 0;

@@ -64,6 +64,18 @@ def test_bad_attend_arguments(lib, bad):
     assert lib.ipv_attend(p, b, ctypes.byref(ipv.AttendArgs(**{**ARGS, **bad})), None) == ipv.IPV_EINVAL
 
 
+@pytest.mark.parametrize("fmt", [ipv.IPV_PAGES_U8, ipv.IPV_PAGES_U4])
+def test_a_workspace_that_no_number_holds_is_refused(lib, fmt):
+    """Codes and many query rows: n_seqs * heads * max_kv rows of 2 * dim bytes, K and V. 2^70 bytes come out as 0 or as
+    anything in 64 bits, and the kernels would write behind a workspace of that size."""
+    p, b = refs({**PAGES, "format": fmt, "n_kv_heads": 65535, "page_size": 1 << 30, "n_pages": 65535, "page_stride": 1, "head_stride": 1},
+                {**BATCH, "n_seqs": 65535, "max_pages": 1, "table": None, "table_stride": 1, "max_kv": 1 << 30, "max_rows": 65, "total_rows": 65})
+    args = ipv.AttendArgs(**{**ARGS, "n_q_heads": 65535})
+    n = ctypes.c_int64(0)
+    assert lib.ipv_attend_workspace(p, b, ctypes.byref(args), ctypes.byref(n)) == ipv.IPV_EINVAL
+    assert lib.ipv_attend(p, b, ctypes.byref(args), None) == ipv.IPV_EINVAL
+
+
 def test_null_structures_and_bad_rows(lib):
     p, b = refs(PAGES, BATCH)
     args, n = ctypes.byref(ipv.AttendArgs(**ARGS)), ctypes.c_int64(0)
