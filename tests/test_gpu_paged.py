@@ -746,3 +746,14 @@ def test_rows_rewritten_and_read_back_in_one_go(fmt):
     torch.cuda.synchronize()
     want = rows if fmt == "bf16" else ref.values(*ref.quantise(rows, fmt)).float().bfloat16()
     assert torch.equal(outs[:, 0].cpu(), want) and torch.equal(outs[:, 1].cpu(), want.flip(0))
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "u8", "u4"])
+@pytest.mark.parametrize("rows", [1, 20, 90])
+def test_nothing_is_cached(fmt, rows):
+    """No sequence holds a row, and the bound says so: 0 and -inf for every query."""
+    gen = torch.Generator().manual_seed(231)
+    s = Setup(gen, fmt, 2, 64, 16, [0, 0], [rows, 3])
+    assert s.batch.max_kv == 0
+    q, out, lse = run_attend(s, 4, 232)
+    assert (out == 0).all() and (lse == -math.inf).all()
