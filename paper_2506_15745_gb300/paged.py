@@ -26,6 +26,12 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
+def _fits(bits: int, **values: int) -> None:
+    """ctypes cuts what a C integer does not hold."""
+    for name, x in values.items():
+        _need(-(1 << (bits - 1)) <= x < 1 << (bits - 1), f"{name} {x} does not fit {bits} bits")
+
+
 class PagedBatch:
     """Sequences and their new rows (ipv_batch).
 
@@ -54,6 +60,8 @@ class PagedBatch:
         table_stride = 1 if table is None else table.stride(0) if n > 1 else table.shape[1]
         _need(table is None or table_stride == 0 or table_stride >= table.shape[1],
               "the rows of table overlap; table.contiguous() separates them")
+        _fits(32, max_rows=max_rows, max_kv=max_kv)
+        _fits(64, total_rows=total_rows)
         self.table, self.row_start, self.kv_len = table, row_start, kv_len
         self.n_seqs, self.total_rows, self.max_rows, self.max_kv = n, total_rows, max_rows, max_kv
         self.max_pages = 1 if table is None else table.shape[1]
@@ -239,6 +247,7 @@ class PagedCache:
 
     def _first_call(self, batch, sizes):
         _, n_q_heads, causal, window, sinks = sizes
+        _fits(32, window=window, sinks=sinks)
         args = ipv.AttendArgs(n_q_heads=n_q_heads, scale=1.0, causal=int(causal), window=window, sinks=sinks)
         kept = args, ctypes.byref(args), ipv.attend_workspace(self.ref, batch.ref, args)
         if len(self._calls) >= 1024:

@@ -209,3 +209,18 @@ def test_a_captured_call_does_not_use_the_kept_workspace(world):
     w = gpu(aligned(NEED))
     world.cache.attend(world.q, world.batch, workspace=w)
     assert last(world.log, "attend")[2] == w.data_ptr()
+
+
+# ------------------------------------------------------------- sizes past 32 bits
+@pytest.mark.parametrize("bad", [dict(max_kv=1 << 32), dict(max_kv=1 << 31), dict(max_rows=(1 << 32) + 1), dict(total_rows=1 << 64),
+                                 dict(max_kv=-(1 << 32) + 9)], ids=str)
+def test_bounds_that_32_bits_do_not_hold_are_refused(bad):
+    sizes = {**dict(total_rows=1, max_rows=1, max_kv=9), **bad}
+    with pytest.raises(ValueError, match=next(iter(bad))):
+        PagedBatch(ints(0, 1).view(1, 2), ints(0, 1), ints(9), **sizes)
+
+
+@pytest.mark.parametrize("bad", [dict(window=1 << 32), dict(window=(1 << 32) + 5), dict(sinks=1 << 32, window=4), dict(window=1 << 31)], ids=str)
+def test_masks_that_32_bits_do_not_hold_are_refused(world, bad):
+    with pytest.raises(ValueError, match=next(iter(bad))):
+        world.cache.attend(world.q, world.batch, workspace=gpu(aligned(NEED)), **bad)
