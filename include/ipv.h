@@ -443,7 +443,7 @@ typedef struct {
   int64_t q_row_stride, q_head_stride;     /* elements, multiples of 8 */
   int64_t out_row_stride, out_head_stride; /* elements, multiples of 8 */
   int n_q_heads;            /* a multiple of n_kv_heads */
-  float scale;              /* finite */
+  float scale;              /* finite, its magnitude below 2^127 */
   int causal;               /* 0 or 1 */
   int window;               /* 0: none; else > 0, needs causal */
   int sinks;                /* first rows that a window leaves visible, >= 0 */

@@ -163,13 +163,15 @@ ipv_status check_packed(const void* x, const char* name, int64_t row, int64_t he
 // tokens over 6000, 393 MB: 65 against 48).
 constexpr int64_t kRowsMost = 64, kRowsBytes = 76 << 20;
 
+constexpr float kLog2e = 1.4426950408889634f;
+
 ipv_status check_attend(const ipv_pages* p, const ipv_batch* b, const ipv_attend_args* t, ipv::AttendArgs* a) {
   ipv_status s = check(p, b, &a->p);
   if (s != IPV_OK) return s;
   if (!t) return reject(IPV_EINVAL, "args must not be NULL");
   if (t->n_q_heads < 1 || t->n_q_heads % p->n_kv_heads != 0)
     return reject(IPV_EINVAL, "n_q_heads %d is not a multiple of n_kv_heads %d", t->n_q_heads, p->n_kv_heads);
-  if (!std::isfinite(t->scale)) return reject(IPV_EINVAL, "scale must be finite");
+  if (!std::isfinite(t->scale * kLog2e)) return reject(IPV_EINVAL, "scale must be finite and below 2^127");
   if (t->causal != 0 && t->causal != 1) return reject(IPV_EINVAL, "causal must be 0 or 1");
   if (t->window < 0 || t->sinks < 0) return reject(IPV_EINVAL, "window and sinks must not be negative");
   if (t->window > 0 && !t->causal) return reject(IPV_EINVAL, "a window needs causal = 1");
@@ -183,7 +185,7 @@ ipv_status check_attend(const ipv_pages* p, const ipv_batch* b, const ipv_attend
   a->q_heads = t->n_q_heads;
   a->share = t->n_q_heads / p->n_kv_heads;
   a->by_share = ipv::Divide(a->share);
-  a->scale_log2 = t->scale * 1.4426950408889634f;
+  a->scale_log2 = t->scale * kLog2e;
   a->causal = t->causal;
   a->window = t->window;
   a->sinks = t->window ? t->sinks : 0;

@@ -64,6 +64,13 @@ def test_bad_attend_arguments(lib, bad):
     assert lib.ipv_attend(p, b, ctypes.byref(ipv.AttendArgs(**{**ARGS, **bad})), None) == ipv.IPV_EINVAL
 
 
+@pytest.mark.parametrize("scale", [2.4e38, -2.4e38, 3.4e38])
+def test_a_scale_that_overflows_in_the_kernels_base_is_refused(lib, scale):
+    """The kernels work with scale * log2(e)."""
+    p, b = refs(PAGES, BATCH)
+    assert lib.ipv_attend(p, b, ctypes.byref(ipv.AttendArgs(**{**ARGS, "scale": scale})), None) == ipv.IPV_EINVAL
+
+
 @pytest.mark.parametrize("fmt", [ipv.IPV_PAGES_U8, ipv.IPV_PAGES_U4])
 def test_a_workspace_that_no_number_holds_is_refused(lib, fmt):
     """Codes and many query rows: n_seqs * heads * max_kv rows of 2 * dim bytes, K and V. 2^70 bytes come out as 0 or as
