@@ -158,10 +158,10 @@ ipv_status check_packed(const void* x, const char* name, int64_t row, int64_t he
 // 256, after widening codes and with a longer way in and out. Up to 64 rows (per
 // sequence and KV head) the rows kernel is the faster one for codes (7 query heads,
 // 4 KV heads, 6000 rows, 16 sequences of 4 tokens, u4: 51 against 109 us; of 9 tokens
-// 84 against 110), and for bf16 where it reads little (1 sequence of 8 tokens over 9000
-// rows, 74 MB: 19 against 24 us; 16 of 9 tokens over 600, 78 MB: 25 against 20; 16 of 3
-// tokens over 6000, 393 MB: 65 against 48).
-constexpr int64_t kRowsMost = 64, kRowsBytes = 76 << 20;
+// 84 against 110), and for bf16 where it reads little, in millions of bytes (1 sequence of
+// 8 tokens over 9000 rows, 73.7: 19 against 26 us; 16 of 9 tokens over 600, 78.6: 25 against
+// 19; 16 of 3 tokens over 6000, 393: 65 against 48).
+constexpr int64_t kRowsMost = 64, kRowsBytes = 76000000;
 
 constexpr float kLog2e = 1.4426950408889634f;
 

@@ -757,3 +757,16 @@ def test_nothing_is_cached(fmt, rows):
     assert s.batch.max_kv == 0
     q, out, lse = run_attend(s, 4, 232)
     assert (out == 0).all() and (lse == -math.inf).all()
+
+
+@pytest.mark.parametrize("seqs,rows,kv,tiled", [(1, 8, 9000, False), (16, 9, 600, True), (16, 3, 6000, True)])
+def test_which_kernel_takes_a_few_rows_over_bf16_pages(seqs, rows, kv, tiled):
+    """The measured cases that the limit between the two kernels was drawn from, 7 query heads for each of 4 KV heads:
+    the workspace of parts is that of 256-row tiles, or of 16-row ones."""
+    cache = PagedCache(1, 64, 4, 128)
+    table = torch.zeros((seqs, -(-kv // 64)), dtype=torch.int32, device="cuda")
+    batch = PagedBatch(table, torch.arange(seqs + 1, dtype=torch.int32, device="cuda") * rows,
+                       torch.full((seqs,), kv, dtype=torch.int32, device="cuda"), total_rows=seqs * rows, max_rows=rows, max_kv=kv)
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    per_sm = workspace_need(cache, batch, 28) / sms
+    assert per_sm >= 2 * 256 * 128 * 4 if tiled else per_sm < 2 * 64 * 128 * 4
