@@ -770,3 +770,80 @@ def test_which_kernel_takes_a_few_rows_over_bf16_pages(seqs, rows, kv, tiled):
     sms = torch.cuda.get_device_properties(0).multi_processor_count
     per_sm = workspace_need(cache, batch, 28) / sms
     assert per_sm >= 2 * 256 * 128 * 4 if tiled else per_sm < 2 * 64 * 128 * 4
+
+
+SHARED_LISTS = [  # fmt, dim, heads, share, page, sequences (rows, kv) as a function of an index, how many, kwargs
+    # rows kernel, more (sequence, tile) pairs than a block's 128 threads
+    ("bf16", 64, 1, 2, 16, lambda b: (1, 900 if b % 97 == 50 else (b * 37) % 190), 500, {}),
+    ("u4", 64, 2, 8, 16, lambda b: (1, 4000 if b == 399 else (b * 53) % 410), 400, {}),
+    ("u8", 128, 1, 7, 32, lambda b: (b % 3, 60 + (b * 29) % 800), 270, {"window": 640, "sinks": 2}),
+    ("bf16", 128, 1, 16, 64, lambda b: (1 if b in (0, 299) else 0, 5000 if b in (0, 299) else 20), 300, {}),
+    # tiled kernel, more pairs than its 384 threads
+    ("bf16", 64, 1, 4, 16, lambda b: (5 + b % 60, 900 if b % 150 == 149 else 70 + (b * 31) % 100), 800, {}),
+    ("u8", 64, 1, 3, 16, lambda b: (b % 31, 1500 if b == 0 else 40 + (b * 17) % 90), 450, {"window": 1000, "sinks": 3}),
+    ("bf16", 128, 1, 1, 32, lambda b: (600 if b == 410 else 65 if b % 40 == 3 else 0, 700 if b == 410 else 66), 411, {}),
+    # one pair more than a warp's lanes, a block's threads
+    ("u4", 128, 2, 5, 64, lambda b: (1, 600 + b), 33, {}),
+    ("bf16", 96, 1, 8, 16, lambda b: (1, 513 + b), 129, {}),
+    ("bf16", 64, 1, 1, 64, lambda b: (65, 513 + b % 50), 385, {}),
+]
+
+
+@pytest.mark.parametrize("case", range(len(SHARED_LISTS)))
+def test_long_lists_shared_out_over_blocks(case):
+    """Batches with more sequences than a block looks at together, too long for whole contexts and too many for clusters:
+    the blocks' shares are found in several passes over the list."""
+    fmt, dim, heads, share, page, seq, count, kw = SHARED_LISTS[case]
+    gen = torch.Generator().manual_seed(3000 + case)
+    seqs = [seq(b) for b in range(count)]
+    s = Setup(gen, fmt, heads, dim, page, [n for _, n in seqs], [min(r, max(n, 1)) for r, n in seqs])
+    widened = 0
+    if fmt != "bf16" and max(s.rows) * share > 64:
+        widened = 2 * (-(-len(seqs) * heads * max(s.lens) * dim * 2 // 256) * 256)
+    assert workspace_need(s.cache, s.batch, heads * share, **kw) > widened  # parts: the work is shared out
+    q, out, lse = run_attend(s, share, 3100 + case, **kw)
+    check_attend(s, q, out, lse, dim ** -0.5, **kw)
+
+
+def test_sixteen_row_tiles_shared_out():
+    """17 to 64 bf16 query rows per KV head in the rows kernel, too long for whole contexts and clusters."""
+    gen = torch.Generator().manual_seed(241)
+    seqs = [(20, 5000), (1, 5), (0, 9), (13, 777)]
+    s = Setup(gen, "bf16", 2, 112, 32, [n for _, n in seqs], [r for r, _ in seqs])
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert 0 < workspace_need(s.cache, s.batch, 6) < sms * 2 * 256 * 112 * 4  # parts of 16 rows, not of 256
+    q, out, lse = run_attend(s, 3, 242)
+    check_attend(s, q, out, lse, 112 ** -0.5)
+
+
+@pytest.mark.parametrize("fmt,dim,heads,share,lens,rows", [
+    ("u8", 128, 2, 7, [9000, 17000], [1, 1]), ("u4", 64, 1, 5, [30000], [2]), ("bf16", 128, 1, 8, [20000], [1]),
+    ("bf16", 128, 1, 7, [3000, 700], [61, 33]), ("u8", 128, 1, 7, [2000, 900], [40, 70])])
+def test_what_a_workspace_held_does_not_matter(fmt, dim, heads, share, lens, rows):
+    """The same bits from a workspace full of NaN and full of zeros, on the current stream and on another."""
+    gen = torch.Generator().manual_seed(251)
+    s = Setup(gen, fmt, heads, dim, 64, lens, rows)
+    need = workspace_need(s.cache, s.batch, heads * share)
+    assert need > 0
+    q = make_rows(gen, s.total, heads * share, dim).cuda()
+    want, side = s.cache.attend(q, s.batch), torch.cuda.Stream()
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    for fill in (255, 0, 255):
+        out = torch.zeros_like(q)
+        ws.fill_(fill)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            s.cache.attend(q, s.batch, out=out, workspace=ws)
+        side.synchronize()
+        assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dim", [8, 40, 56])
+@pytest.mark.parametrize("page,seqs,kw", [
+    (16, [(70, 300), (3, 40), (100, 100)], {}), (128, [(200, 1500)], {"window": 130, "sinks": 9}), (64, [(90, 800)], {"causal": False})])
+def test_narrow_heads_in_the_tiled_kernel(dim, page, seqs, kw):
+    """Rows shorter than the 64 channels of a copy."""
+    gen = torch.Generator().manual_seed(261 + dim)
+    s = Setup(gen, "bf16", 2, dim, page, [n for _, n in seqs], [r for r, _ in seqs])
+    q, out, lse = run_attend(s, 2, 262, **kw)
+    check_attend(s, q, out, lse, dim ** -0.5, **kw)
