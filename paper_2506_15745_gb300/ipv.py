@@ -277,26 +277,11 @@ def profile_collect(timeout_ms: int = 60000):
     return {KERNEL_NAMES[i]: (ms[i], n[i]) for i in range(NUM_KERNELS)}
 
 
-def pages_write(pages, batch, k_new, v_new, row_stride: int, head_stride: int, stream=None) -> None:
-    """ipv_pages_write; pages and batch are references to PagesDesc and Batch (see paged.PagedCache)."""
-    _check(load().ipv_pages_write(pages, batch, _ptr(k_new), _ptr(v_new), row_stride, head_stride, _stream(stream)))
-
-
-def pages_read(pages, batch, k_out, v_out, row_stride: int, head_stride: int, stream=None) -> None:
-    """ipv_pages_read."""
-    _check(load().ipv_pages_read(pages, batch, _ptr(k_out), _ptr(v_out), row_stride, head_stride, _stream(stream)))
-
-
 def attend_workspace(pages, batch, args: AttendArgs) -> int:
     """Bytes of workspace that ipv_attend needs for these sizes."""
     out = ctypes.c_int64(0)
     _check(load().ipv_attend_workspace(pages, batch, ctypes.byref(args), ctypes.byref(out)))
     return out.value
-
-
-def attend(pages, batch, args, stream=None) -> None:
-    """ipv_attend; args: a reference to AttendArgs."""
-    _check(load().ipv_attend(pages, batch, args, _stream(stream)))
 
 
 def attend_error() -> int:
