@@ -653,7 +653,7 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
     }
     // The next run's first steps are on their way while this one's results are joined.
     const bool partial = !(w.starts() && w.ends());
-    const int pair = w.pair(tiles), ends = (w.starts() ? 1 : 0) | (w.ends() ? 2 : 0);
+    const int4 record = part_record(w.pair(tiles), head, w.starts(), w.ends());
     go = w.next(a, tiles);
     if (go) fill(w);
 
@@ -700,7 +700,7 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
     const int slot = 2 * blockIdx.x + (run > 0 ? 1 : 0);
     if (partial && !clustered) {
       slots |= run > 0 ? 2 : 1;
-      if (threadIdx.x == 0) a.part_rec[slot] = make_int4(1, pair, head, ends);
+      if (threadIdx.x == 0) a.part_rec[slot] = record;
     }
     constexpr int kQuads = DP / 4;
     for (int idx = threadIdx.x; idx < kRows * kQuads; idx += kThreads) {

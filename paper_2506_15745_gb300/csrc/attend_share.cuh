@@ -189,29 +189,30 @@ __device__ Share find_share(const AttendArgs& a, int tiles, int64_t* scratch) {
   return w;
 }
 
+// A record of a part: (0, pair of sequence and tile, KV head, these bits); all 0: no part.
+enum : int { kPart = 4, kStarts = 1, kEnds = 2 };
+__device__ __forceinline__ int4 part_record(int pair, int head, bool starts, bool ends) {
+  return make_int4(0, pair, head, kPart | (starts ? kStarts : 0) | (ends ? kEnds : 0));
+}
+
 // The parts of the tile that block c starts and does not end, as whole warps:
-// their number, 0 if there is none or if a part is missing because its block gave up.
+// their number, 0 if there is none or if one is missing because its block gave up.
 // Part 0 is slot `slot` (its record: rec), part i the first slot of block c + i.
 __device__ __forceinline__ int parts_from(const AttendArgs& a, int c, int blocks, int& slot, int4& rec) {
-  constexpr int kGoesOn = 1, kEnds = 2;  // 0: no part of the tile
   const int lane = threadIdx.x & 31;
-  auto part = [&](int block) {
-    if (block >= blocks) return 0;
-    const int4 r = a.part_rec[2 * block];
-    return r.x == 0 || (r.w & 1) ? 0 : r.w & 2 ? kEnds : kGoesOn;
-  };
   const int4 one = a.part_rec[2 * c], two = a.part_rec[2 * c + 1];
-  int next = part(c + 1 + lane);  // the first 32 with the records
-  slot = two.x && two.w == 1 ? 2 * c + 1 : one.x && one.w == 1 ? 2 * c : -1;
+  int next = c + 1 + lane >= blocks ? 0 : a.part_rec[2 * (c + 1 + lane)].w;  // the first 32 with the records
+  slot = two.w == (kPart | kStarts) ? 2 * c + 1 : one.w == (kPart | kStarts) ? 2 * c : -1;
   if (slot < 0) return 0;
   rec = slot & 1 ? two : one;
   for (int i0 = 1;; i0 += 32) {
-    const uint32_t last = __ballot_sync(0xffffffffu, next != kGoesOn);
+    const uint32_t last = __ballot_sync(0xffffffffu, next != kPart);  // does not go on
     if (last) {
       const int at = __ffs(last) - 1;
-      return __shfl_sync(0xffffffffu, next, at) == kEnds ? i0 + at + 1 : 0;
+      return __shfl_sync(0xffffffffu, next, at) == (kPart | kEnds) ? i0 + at + 1 : 0;
     }
-    next = part(c + i0 + 32 + lane);
+    const int block = c + i0 + 32 + lane;
+    next = block >= blocks ? 0 : a.part_rec[2 * block].w;
   }
 }
 

@@ -72,8 +72,7 @@ struct Layout {
 
 // Barriers, 8 bytes each.
 enum : int { kBarKFull = 0, kBarKEmpty = 4, kBarVFull = 8, kBarVEmpty = 12, kBarS = 16, kBarP = 18, kBarO = 22, kBarQ = 24,
-             kBarDrain = 26, kBarVTail = 28, kBarTurn = 32, kBars = 34, kWordTmem = 34 * 8, kWordStop = 35 * 8,
-             kRecords = 36 * 8 };  // two records, 16 bytes each: what the block will say of its parts
+             kBarDrain = 26, kBarVTail = 28, kBarTurn = 32, kBars = 34, kWordTmem = 34 * 8, kWordStop = 35 * 8 };
 
 // ------------------------------------------------------------------ PTX
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
@@ -284,7 +283,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t bars = base + L::kBars, stop = bars + kWordStop;
   auto bar = [&](int i) { return bars + 8 * i; };
   float* row_scale = reinterpret_cast<float*>(base_p + L::kScale);
-  int4* records = reinterpret_cast<int4*>(base_p + L::kBars + kRecords);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (warp == kMmaWarp) {
@@ -298,7 +296,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       bar_init(bar(i), tiles2 ? 2 : warps4 ? 4 : 1);
     }
     asm volatile("st.volatile.shared.b32 [%0], %1;" ::"r"(stop), "r"(0u) : "memory");
-    records[0] = records[1] = make_int4(0, 0, 0, 0);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async();
   }
@@ -501,7 +498,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       if (lane == 0) bar_arrive(bar(kBarQ + t));
     };
-    int done = 0, runs = 0, run = 0;  // steps and runs of this tile, of the block
+    int done = 0, runs = 0, run = 0, slots = 0;  // steps and runs of this tile, of the block; partial results used
     bool go = w.begin(a, tiles, share);
     if (go) load_queries(w);
     while (go) {
@@ -509,7 +506,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool partial = !(w.starts() && w.ends());
       const int slot = 2 * blockIdx.x + (run > 0 ? 1 : 0);
       ++run;
-      if (partial && threadIdx.x == 0) records[slot & 1] = make_int4(1, w.pair(tiles), w.head, (w.starts() ? 1 : 0) | (w.ends() ? 2 : 0));
+      if (partial) {
+        slots |= slot & 1 ? 2 : 1;
+        if (threadIdx.x == 0) a.part_rec[slot] = part_record(w.pair(tiles), w.head, w.starts(), w.ends());
+      }
       if (w.t.n_rows <= 128 * t) {
         go = after.next(a, tiles);
         if (go) load_queries(after);
@@ -679,13 +679,17 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (in && partial) a.part_ml[part] = make_float2(m, l);
       if (in && !partial && a.lse) a.lse[row * a.q_heads + hq] = l == 0.0f ? kNegInf : (m + log2f(l)) * 0.6931471805599453f;
     }
+    if (threadIdx.x == 0 && a.unit > 0) {
+      if (!(slots & 1)) a.part_rec[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
+      if (!(slots & 2)) a.part_rec[2 * blockIdx.x + 1] = make_int4(0, 0, 0, 0);
+    }
   }
   pdl_trigger();
   fence_before();
   __syncthreads();
   fence_after();
-  // The parts are written: the records go out. A block that stopped has none.
-  if (threadIdx.x < 2 && a.unit > 0) a.part_rec[2 * blockIdx.x + threadIdx.x] = lds_flag(stop) ? make_int4(0, 0, 0, 0) : records[threadIdx.x];
+  // A block that stopped has no parts: thread 0 takes back what it said of them.
+  if (threadIdx.x == 0 && a.unit > 0 && lds_flag(stop)) a.part_rec[2 * blockIdx.x] = a.part_rec[2 * blockIdx.x + 1] = make_int4(0, 0, 0, 0);
   if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 

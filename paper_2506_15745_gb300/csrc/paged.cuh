@@ -122,8 +122,7 @@ struct AttendArgs {
   int tile;  // query rows of a row tile
   // Partial results, for each block's first and last run: unnormalised sums
   // (rows kernel: [blocks][2][tile][dim], tiled kernel: [blocks][2][dim / 4][tile][4]),
-  // (running maximum, sum) [blocks][2][tile], and a record [blocks][2]: (1, or 0:
-  // none, pair of sequence and tile, KV head, 1: a tile's start + 2: its end).
+  // (running maximum, sum) [blocks][2][tile], and a record [blocks][2] (part_record).
   float* part_o;
   float2* part_ml;
   int4* part_rec;
