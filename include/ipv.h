@@ -434,8 +434,15 @@ ipv_status ipv_pages_read(const ipv_pages* pages, const ipv_batch* batch, void* 
  * lse = log sum_j exp(S_j); a query that sees none gets 0 and -inf. Rows past
  * kv_len never matter, whatever they hold. A non-finite number in a cached
  * row can reach every query of its sequence, as can a marked group.
- * Sums and softmax statistics are fp32; q . k_j is summed in fp32 from exact
- * products; the softmax weights are rounded to bf16 (bf16 pages) or fp16. */
+ * Sums and softmax statistics are fp32. Two kernels share the calls by their sizes,
+ * so a query's last bits can depend on what else is in the call:
+ *  - few query rows (max_rows * n_q_heads / n_kv_heads up to 16; up to 64 over codes,
+ *    and over bf16 pages where little is read): cached values enter as they are,
+ *    weights with 16 bits (bf16 pages) or, times their group's step, 11 (codes);
+ *  - more: cached values enter as they are (bf16 pages) or rounded to fp16 (codes),
+ *    weights with 8 bits (bf16 pages) or 11 (codes).
+ * Over codes a row of q is scaled by a power of two and taken in fp16, where values
+ * below 2^-22 of its largest magnitude lose bits. */
 typedef struct {
   const void* q;            /* device bf16 [total_rows][n_q_heads][head_dim] by strides */
   void* out;                /* device bf16, likewise; may not overlap q */
@@ -452,8 +459,12 @@ typedef struct {
 } ipv_attend_args;
 
 /* Bytes of workspace the call needs (0 if none); reads the sizes only, not the
- * device memory, and is the same for the same sizes on one device. Working
- * memory only: nothing is kept in it between calls and it needs no clearing. */
+ * device memory, and is the same for the same sizes on one device. Parts of
+ * results take up to some tens of MB. The kernel for many query rows widens codes
+ * first, which takes 4 * n_seqs * n_kv_heads * max_kv * head_dim bytes more (by
+ * max_kv, not by the lengths): more than the codes themselves, so calls that follow
+ * one another should share it. Working memory only: nothing is kept in it between
+ * calls and it needs no clearing. */
 ipv_status ipv_attend_workspace(const ipv_pages* pages, const ipv_batch* batch,
                                 const ipv_attend_args* args, int64_t* bytes_out);
 

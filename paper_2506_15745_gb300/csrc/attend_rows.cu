@@ -28,8 +28,8 @@
 //
 // Measured: one token for each of 8 streams, 24576 bf16 rows, 8 KV heads of 8 query
 // heads: 124 us, 6.5 TB/s (96% of the copy bandwidth); 32 streams of up to 24577
-// 4-bit rows: 124 us, 4.3 TB/s, bound by integer instructions (masks, permutations,
-// addresses); 32 streams of 12288 8-bit rows: 148 us, 5.8 TB/s.
+// 4-bit rows: 124 us, 4.3 TB/s: no unit is busy more than 56% (issue; DRAM 51%, ALU 50%:
+// masks, permutations, addresses), 12 warps per SM wait in a step's chain; 32 streams of 12288 8-bit rows: 148 us, 5.8 TB/s.
 #include <cuda_fp16.h>
 
 #include "attend_share.cuh"

@@ -26,7 +26,8 @@
 // Tensor memory: S (and P in its place) 2 x 128 columns, O 2 x head_dim.
 //
 // Measured: 16 frames (3136 tokens, 28 query heads, 4 KV heads, 128 channels) over
-// 9408 rows 242 us, 1460 TFLOP/s (77% of the measured bf16 rate); one frame over 6468
+// 9408 rows 242 us, 1460 TFLOP/s (77% of the measured bf16 rate; call after call on one
+// set of inputs 226); one frame over 6468
 // rows 30 us (start, 9 steps per block, join); 8191 tokens under a window of 2000, 16
 // query heads of 64 channels, 97 us.
 #include <cuda.h>

@@ -5,8 +5,10 @@
 // group's minimum and maximum are two shuffles away and what a group costs beside
 // its values is shared by 16 of them, 8 lanes when reading.
 //
-// Measured, 6272 rows of 112 heads of 128 channels, K and V, 4 bits: write 118 us
-// (bound by instruction issue: about 16 per value), read 69 us (6.7 TB/s).
+// Measured, 6272 rows of 112 heads of 128 channels, K and V, 4 bits: read 69 us (6.7
+// TB/s); write 118 us for 68 us of bytes: no unit is busy more than 61% (issue, at about
+// 16 instructions per value; ALU 53%, DRAM 35%), 3 blocks per SM (79 registers) wait for
+// their loads and shuffles.
 #include <cuda_fp16.h>
 
 #include "paged.cuh"

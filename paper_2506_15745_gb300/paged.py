@@ -204,7 +204,9 @@ class PagedCache:
         sequences hold. out: bf16 like q (allocated if None, on the call's stream); lse: fp32
         [total_rows, n_q_heads], filled if given. workspace: a contiguous uint8 tensor
         that no call on another stream uses at the same time; without one the cache keeps one of its own for
-        each stream that is current in a call. A call that torch.cuda.graph captures takes its workspace from the
+        each stream that is current in a call. ipv.attend_workspace tells its size; many rows over codes (above 64
+        per sequence and KV head) need 4 * n_seqs * n_kv_heads * max_kv * head_dim bytes for the widened codes, which
+        the layers' caches of a model share if they are given one tensor. A call that torch.cuda.graph captures takes its workspace from the
         graph's memory; if one is given, it has to live as long as the graph, and graphs that share it may not be
         replayed at the same time. One host thread at a time uses a cache object."""
         n_q_heads = q.shape[1]
