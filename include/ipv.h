@@ -484,6 +484,145 @@ ipv_status ipv_attend_error(uint32_t* err_out);
  * 4 s; 1: every wait gives up at once). Takes effect at the next ipv_attend. Errors: IPV_EINVAL (negative). */
 ipv_status ipv_attend_wait_limit(int64_t nanoseconds);
 
+/* ---- New rows rotated on their way in, bounds of pages, attention over chosen
+ * pages, pages moved. All follow the paged cache's rules above: the batch's
+ * sizes are checked on the host, what device memory holds is made to fit. */
+
+/* Position rotation of queries and keys. table: device fp32
+ * [n_positions][rot_dim], 16-byte aligned: the rot_dim / 2 cosines of a position,
+ * then its sines. Frequency f turns channels (f, f + rot_dim / 2), or
+ * (2f, 2f + 1) if interleaved: (x, y) becomes (x cos - y sin, y cos + x sin);
+ * channels from rot_dim on stay. Positions have n_axes axes (time, height and
+ * width of a patch, say): the first sections[0] frequencies go by the first
+ * axis, the next sections[1] by the second, and so on. */
+typedef struct {
+  const float* table;
+  int64_t n_positions;
+  int rot_dim;              /* a multiple of 16, <= head_dim */
+  int interleaved;          /* 0 or 1 */
+  int n_axes;               /* 1..4 */
+  int sections[4];          /* multiples of 8, positive; their sum is rot_dim / 2 */
+} ipv_rotary;
+
+/* Writes the batch's new rows into the pages as ipv_pages_write does, their keys
+ * normalised and rotated first, and their queries, normalised and rotated, to
+ * q_out. With a weight w (bf16 [head_dim], NULL: no norm) a head's row x becomes
+ * x * w / sqrt(mean x^2 + eps). Rotation and norm are fp32, rounded once to bf16;
+ * keys are quantised after that. positions: device int32, row i's place on axis
+ * a at a * positions_stride + i; a place outside the table makes the channels
+ * that it turns NaN. q_out may be q, with q's strides. Queries of rows that
+ * belong to no sequence, and q_out there, are left alone; keys and values of
+ * rows before position 0 are dropped. q: strides and alignment as in ipv_attend; k_new, v_new: as in
+ * ipv_pages_write. Errors: IPV_EINVAL (before anything is enqueued), IPV_ECUDA. */
+typedef struct {
+  const void* q;            /* device bf16 [total_rows][n_q_heads][head_dim] by strides */
+  void* q_out;              /* device bf16, likewise */
+  const void* k_new;        /* device bf16 [total_rows][n_kv_heads][head_dim] by strides */
+  const void* v_new;
+  int64_t q_row_stride, q_head_stride, out_row_stride, out_head_stride; /* elements, multiples of 8 */
+  int64_t row_stride, head_stride;                                      /* of k_new and v_new */
+  int n_q_heads;            /* >= 1 */
+  float eps;                /* finite, >= 0 */
+  const void* q_weight;     /* device bf16 [head_dim], 16-byte aligned, or NULL */
+  const void* k_weight;
+  const int32_t* positions;
+  int64_t positions_stride; /* >= total_rows */
+} ipv_rotate_args;
+
+ipv_status ipv_pages_write_rotated(const ipv_pages* pages, const ipv_batch* batch, const ipv_rotary* rotary,
+                                   const ipv_rotate_args* args, void* stream);
+
+/* Copies whole pages, all heads of K and V with their pairs: page to[i] becomes
+ * page from[i] (device int32 [n]). Pairs with a page number outside the pool are
+ * skipped. No page may be in `to` twice, or in `to` and at another place in `from`.
+ * Errors: IPV_EINVAL, IPV_ECUDA. */
+ipv_status ipv_pages_copy(const ipv_pages* pages, const int32_t* from, const int32_t* to, int64_t n, void* stream);
+
+/* Gathers rows of one cache into another, as they are held: new row i of
+ * sequence b of `batch`, KV head h, becomes row kept[b * kept_seq_stride +
+ * h * kept_head_stride + i] of sequence b in `source` (row i if kept is NULL), of which only
+ * the table and kv_len are read. Formats, n_kv_heads and head_dim are the same in both, and so is
+ * n_seqs. A row that the source sequence does not hold reads as zero. The rows written may not
+ * lie in pages that the call reads. With the kept indices of ipv_select this is the pass's
+ * compaction, of a cache in pages. Errors: IPV_EINVAL, IPV_ECUDA. */
+ipv_status ipv_pages_gather(const ipv_pages* source_pages, const ipv_batch* source, const ipv_pages* pages,
+                            const ipv_batch* batch, const int32_t* kept, int64_t kept_seq_stride,
+                            int64_t kept_head_stride, void* stream);
+
+/* Bounds of the keys of pages. For each page and KV head: lower and upper bounds
+ * lo, hi, 8-bit integers, of every channel, and a step, a power of two, with
+ *     lo * step <= k <= hi * step      for all keys k that the page holds:
+ *     step = 2^e, e the smallest integer >= -40 with max |k| <= 127 * 2^e,
+ *     lo = floor(min k / step), hi = ceil(max k / step).
+ * codes: device int8 [n_pages][n_kv_heads][2][padded], lower bounds first, padded
+ * = 64 (head_dim <= 64) or 128, the padding 0; 16-byte aligned. steps: device fp32
+ * [n_pages][n_kv_heads]. A page that holds a NaN or an infinity has NaN as its
+ * step. Codes' keys are taken as ipv_pages_read gives them. */
+typedef struct {
+  int n_kv_heads;
+  int head_dim;             /* <= 128, a multiple of 8 */
+  int page_size;            /* as in the pages */
+  int64_t n_pages;
+  void* codes;
+  float* steps;
+} ipv_bounds;
+
+/* Brings the bounds of the pages that hold new rows of the batch up to date, from
+ * all the rows that these pages hold (up to the sequence's kv_len). To be called
+ * after the rows were written; with row_start = the sums of kv_len for whole
+ * sequences. Two sequences whose new rows lie in one page must hold as much of it.
+ * Errors: IPV_EINVAL, IPV_ECUDA. */
+ipv_status ipv_bounds_update(const ipv_bounds* bounds, const ipv_pages* pages, const ipv_batch* batch, void* stream);
+
+/* Chooses pages for each new row and KV head by their bounds. The row, at
+ * position p, sees pages 0..p / page_size of its sequence (entries of the
+ * table). If these are at most n_chosen, the list is all of them; else it is the
+ * first `first`, the last `recent` (the row's own page is the last) and those
+ * of the highest scores among the others, n_chosen in all; ties go to the lower
+ * page. The score of a page is the largest over the query heads of the KV head
+ * of 2^e * step * sum over channels of max(c lo, c hi), where c = q / 2^e rounded
+ * to the nearest integer (ties to even) and e is the smallest integer >= -40 with
+ * max |q| <= 127 * 2^e: integers, so the list does not depend on any order of
+ * sums. Magnitudes are to stay below 2^50. A query head that holds a NaN or an
+ * infinity is left out; a page without a score (a step of NaN, a page number
+ * outside the pool, no query head left) ranks lowest. out: device int32
+ * [total_rows][n_kv_heads][n_chosen] by strides, ascending, then -1. Rows that
+ * belong to no sequence are left alone. */
+typedef struct {
+  const void* q;            /* device bf16 [total_rows][n_q_heads][head_dim] by strides */
+  int64_t q_row_stride, q_head_stride; /* elements, multiples of 8 */
+  int n_q_heads;            /* a multiple of n_kv_heads */
+  int n_chosen;             /* >= first + recent */
+  int first, recent;        /* >= 0, >= 1 */
+  int32_t* out;
+  int64_t out_row_stride, out_head_stride; /* elements, >= 0 */
+} ipv_choose_args;
+
+/* max_kv spans at most 32768 pages, and n_q_heads / n_kv_heads is at most 64.
+ * Errors: IPV_EINVAL, IPV_ECUDA. */
+ipv_status ipv_bounds_choose(const ipv_bounds* bounds, const ipv_batch* batch, const ipv_choose_args* args,
+                             void* stream);
+
+/* Attention of each new row over the rows of its chosen pages that it sees, as
+ * ipv_attend with causal = 1 over no other rows: window and sinks must be 0. The
+ * list of row i for KV head h starts at chosen + i * row_stride + h * head_stride
+ * (device int32, n_chosen entries, as ipv_bounds_choose writes them). Of a row
+ * that sees P pages the first min(n_chosen, P) entries are read; an entry outside
+ * 0..P-1 is no page, a page that stands there twice counts twice. Each new row
+ * reads pages of its own, so this is for single tokens and chunks that are short beside
+ * the cache. max_kv is at most 2^30. The results are those of the kernel for few rows (weights
+ * with 16 bits over bf16 pages or, times their group's step, 11 over codes). */
+typedef struct {
+  const int32_t* pages;     /* device */
+  int n_chosen;             /* >= 1 */
+  int64_t row_stride, head_stride; /* elements, >= 0 */
+} ipv_chosen;
+
+ipv_status ipv_attend_chosen_workspace(const ipv_pages* pages, const ipv_batch* batch, const ipv_attend_args* args,
+                                       const ipv_chosen* chosen, int64_t* bytes_out);
+ipv_status ipv_attend_chosen(const ipv_pages* pages, const ipv_batch* batch, const ipv_attend_args* args,
+                             const ipv_chosen* chosen, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -16,7 +16,7 @@ INCLUDE = os.path.join(ROOT, "include")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libipv.so")
 SOURCES = ["api.cu", "score.cu", "select.cu", "gather.cu", "pool.cu", "combine.cu", "append.cu", "window.cu", "noalloc.cu",
-           "paged.cu", "paged_rows.cu", "attend_rows.cu", "attend_tiles.cu"]
+           "paged.cu", "paged_rows.cu", "rotate.cu", "bounds.cu", "move.cu", "attend_rows.cu", "attend_chosen.cu", "attend_tiles.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 
@@ -28,7 +28,8 @@ def _stale(out: str, deps: list[str]) -> bool:
 def build(force: bool = False, extra_flags: list[str] | None = None, verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
     headers = [os.path.join(CSRC, "ipv_common.cuh"), os.path.join(CSRC, "pass_device.cuh"),
-               os.path.join(CSRC, "paged.cuh"), os.path.join(CSRC, "attend_share.cuh"),
+               os.path.join(CSRC, "paged.cuh"), os.path.join(CSRC, "paged_codes.cuh"),
+               os.path.join(CSRC, "attend_share.cuh"), os.path.join(CSRC, "attend_rows.cuh"),
                os.path.join(INCLUDE, "ipv.h")]
     procs, objs = [], []
     for src in SOURCES:

@@ -12,10 +12,25 @@ struct Tile {
   Seq seq;
   int b, row0, n_rows, steps;
   KeyRange kr;
+  int number;  // of the tile in its sequence; CHOSEN only, elsewhere row0 / ROWS
 };
 
-template <int ROWS, int STEP>
+// CHOSEN: a tile is ROWS of the query heads of one new row, over the row's chosen pages.
+template <int ROWS, int STEP, bool CHOSEN = false>
 __device__ __forceinline__ void set_tile(const AttendArgs& a, Tile& x, int b, int tile) {
+  if constexpr (CHOSEN) {
+    const int tok = a.by_per_row(tile), head0 = (tile - tok * a.per_row) * ROWS;
+    x.number = tile;
+    x.row0 = tok * a.share + head0;
+    x.n_rows = tok < x.seq.n ? min(ROWS, a.share - head0) : 0;
+    x.b = b;
+    x.steps = 0;
+    if (x.n_rows > 0) {
+      x.kr = chosen_range<STEP>(a, x.seq, tok);
+      x.steps = max(1, x.kr.steps);
+    }
+    return;
+  }
   x.row0 = tile * ROWS;
   x.n_rows = min(ROWS, x.seq.n * a.share - x.row0);
   x.b = b;
@@ -25,12 +40,12 @@ __device__ __forceinline__ void set_tile(const AttendArgs& a, Tile& x, int b, in
     x.steps = max(1, x.kr.steps);  // rows that see nothing have their results to write, too
   }
 }
-template <int ROWS, int STEP>
+template <int ROWS, int STEP, bool CHOSEN = false>
 __device__ __forceinline__ Tile tile_of(const AttendArgs& a, int tiles, int p) {
   Tile x;
   const int b = a.by_tiles(p);
   x.seq = sequence(a.p, b);
-  set_tile<ROWS, STEP>(a, x, b, p - b * tiles);
+  set_tile<ROWS, STEP, CHOSEN>(a, x, b, p - b * tiles);
   return x;
 }
 
@@ -45,7 +60,7 @@ struct Share {
 
 // Walks a share, a run of steps of one (pair, head) at a time. A boundary within
 // the first COST units leaves all steps to the block behind it.
-template <int ROWS, int STEP, int COST>
+template <int ROWS, int STEP, int COST, bool CHOSEN = false>
 struct Walk {
   Tile t;
   int head, s, n;  // steps s .. s + n - 1
@@ -57,7 +72,7 @@ struct Walk {
     left -= upto - at;
   }
   __device__ __forceinline__ bool begin(const AttendArgs& a, int tiles, const Share& w) {
-    t = tile_of<ROWS, STEP>(a, tiles, w.p);
+    t = tile_of<ROWS, STEP, CHOSEN>(a, tiles, w.p);
     head = w.head;
     left = w.left;
     cut(w.at);
@@ -67,14 +82,14 @@ struct Walk {
     if (left <= 0) return false;
     if (++head == a.p.heads) {
       head = 0;
-      int tile = t.row0 / ROWS, b = t.b;
+      int tile = number(), b = t.b;
       do {
         if (++tile == tiles) {
           tile = 0;
           if (++b == a.p.n_seqs) return false;  // only if the lengths changed under the kernel
           t.seq = sequence(a.p, b);
         }
-        set_tile<ROWS, STEP>(a, t, b, tile);
+        set_tile<ROWS, STEP, CHOSEN>(a, t, b, tile);
       } while (t.steps == 0);
     }
     cut(0);
@@ -82,7 +97,8 @@ struct Walk {
   }
   __device__ __forceinline__ bool starts() const { return s == 0; }
   __device__ __forceinline__ bool ends() const { return s + n == t.steps; }
-  __device__ __forceinline__ int pair(int tiles) const { return t.b * tiles + t.row0 / ROWS; }
+  __device__ __forceinline__ int number() const { return CHOSEN ? t.number : t.row0 / ROWS; }
+  __device__ __forceinline__ int pair(int tiles) const { return t.b * tiles + number(); }
   // Rows of the last V tile from `keep` on lie past the last key.
   __device__ __forceinline__ int keep() const { return t.kr.hi_max - t.kr.template key0<STEP>(s + n - 1); }
 };
@@ -94,12 +110,12 @@ __device__ __forceinline__ int64_t divide(int64_t x, int64_t d) {
 }
 
 // Finds the block's share, with all threads; scratch: 16 64-bit words of shared memory.
-template <int ROWS, int STEP, int COST, int THREADS>
+template <int ROWS, int STEP, int COST, int THREADS, bool CHOSEN = false>
 __device__ Share find_share(const AttendArgs& a, int tiles, int64_t* scratch) {
   const int pairs = a.p.n_seqs * tiles, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   constexpr int kWarps = THREADS / 32;
   auto weight = [&](int p) {
-    const int steps = p < pairs ? tile_of<ROWS, STEP>(a, tiles, p).steps : 0;
+    const int steps = p < pairs ? tile_of<ROWS, STEP, CHOSEN>(a, tiles, p).steps : 0;
     return steps > 0 ? static_cast<int64_t>(steps + COST) * a.p.heads : int64_t{0};
   };
   if (a.unit == 0) {
@@ -107,7 +123,7 @@ __device__ Share find_share(const AttendArgs& a, int tiles, int64_t* scratch) {
     Share w;
     w.p = item / a.p.heads;
     w.head = item - w.p * a.p.heads;
-    const int steps = tile_of<ROWS, STEP>(a, tiles, w.p).steps;
+    const int steps = tile_of<ROWS, STEP, CHOSEN>(a, tiles, w.p).steps;
     const int64_t from = static_cast<int64_t>(steps) * rank / a.cluster, to = static_cast<int64_t>(steps) * (rank + 1) / a.cluster;
     w.at = from > 0 ? from + COST : 0;
     w.left = to > from ? to + COST - w.at : 0;

@@ -1,0 +1,427 @@
+// Bounds of the keys of pages, and the pages that a query's bounds on them choose.
+//
+// For each page and KV head, 8-bit integers lo and hi of every channel and one step,
+// a power of two, with lo * step <= key <= hi * step for all the page's keys. A query
+// row rounded to 8-bit integers qc times a power of two has q . k at most about
+// step_q * step * sum over channels of max(qc lo, qc hi), a sum of whole numbers
+// below 2^24: exact in any order, so that the pages that are chosen do not depend on
+// how the work is split. With q's positive and negative parts kept apart it is a dot
+// product, min(qc, 0) . lo + max(qc, 0) . hi, of twice the channels, which the 8-bit
+// integer matrix instruction takes: 16 pages by 8 query heads.
+#include "paged_codes.cuh"
+
+namespace ipv {
+namespace {
+
+constexpr int kLeastExponent = -40;
+
+// The smallest e >= kLeastExponent with m <= 127 * 2^e, m the finite bf16 magnitude
+// with these bits (its mantissa of 127 is 127/64 of a power of two).
+__device__ __forceinline__ int exponent_of(uint32_t bits) {
+  return max(kLeastExponent, static_cast<int>(bits >> 7) - 133 + ((bits & 0x7Fu) == 0x7Fu ? 1 : 0));
+}
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float(static_cast<uint32_t>(127 + e) << 23); }  // -126 <= e <= 127
+
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {  // NaN wins
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// ------------------------------------------------------------------ the bounds
+// A block takes a page of one head: teams of 16 lanes, lane c the 8 channels from 8c on.
+constexpr int kBoundsThreads = 128;
+constexpr int kBoundsTeams = kBoundsThreads / 16;
+
+template <int FMT>
+__global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(BoundsArgs a) {
+  __shared__ uint4 ends[2][kBoundsThreads / 32][16];
+  pdl_trigger();
+  pdl_wait();
+  const int b = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = threadIdx.x & 15;
+  const Seq s = sequence(a.p, b);
+  if (s.n == 0 || s.len == 0) return;
+  const int shift = a.p.page_shift, page0 = max(0, s.len - s.n) >> shift, i = page0 + static_cast<int>(blockIdx.x);
+  if (i > (s.len - 1) >> shift) return;
+  const int g = a.p.table ? a.p.table[b * a.p.table_stride + i] : b;
+  if (static_cast<unsigned>(g) >= static_cast<unsigned>(a.p.n_pages)) return;
+  const int rows = shift == 31 ? s.len : min(a.p.page_size, s.len - (i << shift));
+  const int64_t row0 = g * a.p.page_stride + h * a.p.head_stride;
+  uint32_t lo[4], hi[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) lo[k] = 0x7F807F80u, hi[k] = 0xFF80FF80u;
+  const bool in = 8 * c < a.p.dim;
+  constexpr int kAtOnce = 8;
+  for (int r0 = threadIdx.x >> 4; r0 < rows; r0 += kBoundsTeams * kAtOnce) {
+    uint4 x[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int r = r0 + u * kBoundsTeams;
+      if (!in || r >= rows) continue;
+      const int64_t row = row0 + r * a.p.row_stride;
+      if (FMT == kBf16) {
+        x[u] = ld_once(a.p.k + row * a.p.row_bytes + 16 * c);
+      } else {
+        const uint32_t* kd = reinterpret_cast<const uint32_t*>(a.p.k + row * a.p.row_bytes) + (c >> 3) * (FMT == kU8 ? kGroup / 4 : kGroup / 8);
+        if (FMT == kU8)
+          x[u].x = kd[place_u8(2 * (c & 7))], x[u].y = kd[place_u8(2 * (c & 7) + 1)];
+        else
+          x[u].x = kd[place_u4(c & 7)];
+        x[u].z = a.p.k_par[row * a.p.groups + (c >> 3)];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      if (!in || r0 + u * kBoundsTeams >= rows) continue;
+      if (FMT != kBf16) {
+        const uint32_t w[2] = {x[u].x, x[u].y};
+        x[u] = expand<FMT, false>(w, x[u].z);
+      }
+      const uint32_t xs[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) lo[k] = min_bf16x2(lo[k], xs[k]), hi[k] = max_bf16x2(hi[k], xs[k]);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    lo[k] = min_bf16x2(lo[k], __shfl_xor_sync(0xffffffffu, lo[k], 16));
+    hi[k] = max_bf16x2(hi[k], __shfl_xor_sync(0xffffffffu, hi[k], 16));
+  }
+  if (lane < 16) {
+    ends[0][warp][c] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    ends[1][warp][c] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+  }
+  __syncthreads();
+  if (threadIdx.x >= 16) return;
+#pragma unroll
+  for (int w = 1; w < kBoundsThreads / 32; ++w) {
+    const uint4 x = ends[0][w][c], y = ends[1][w][c];
+    lo[0] = min_bf16x2(lo[0], x.x), lo[1] = min_bf16x2(lo[1], x.y), lo[2] = min_bf16x2(lo[2], x.z), lo[3] = min_bf16x2(lo[3], x.w);
+    hi[0] = max_bf16x2(hi[0], y.x), hi[1] = max_bf16x2(hi[1], y.y), hi[2] = max_bf16x2(hi[2], y.z), hi[3] = max_bf16x2(hi[3], y.w);
+  }
+  uint32_t top = 0;
+  if (in)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      top = max(max(max(top, lo[k] & 0x7FFFu), max((lo[k] >> 16) & 0x7FFFu, hi[k] & 0x7FFFu)), (hi[k] >> 16) & 0x7FFFu);
+#pragma unroll
+  for (int d = 1; d < 16; d <<= 1) top = max(top, __shfl_xor_sync(0xffffu, top, d));
+  const bool finite = top < 0x7F80u;
+  const int e = finite ? exponent_of(top) : 0;
+  const float down = pow2(-e);
+  uint32_t w[2][2] = {};
+  if (in && finite)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float x = k & 1 ? hi_f(lo[k >> 1]) : lo_f(lo[k >> 1]), y = k & 1 ? hi_f(hi[k >> 1]) : lo_f(hi[k >> 1]);
+      // A product too small for fp32 still lies on its side of 0.
+      const int below = min(static_cast<int>(floorf(x * down)), x < 0.0f ? -1 : 127), above = max(static_cast<int>(ceilf(y * down)), y > 0.0f ? 1 : -127);
+      w[0][k >> 2] |= (static_cast<uint32_t>(below) & 0xFFu) << (8 * (k & 3));
+      w[1][k >> 2] |= (static_cast<uint32_t>(above) & 0xFFu) << (8 * (k & 3));
+    }
+  const int64_t at = static_cast<int64_t>(g) * a.p.heads + h;
+  if (8 * c < a.padded) {
+    char* out = a.codes + at * 2 * a.padded + 8 * c;
+    *reinterpret_cast<uint2*>(out) = make_uint2(w[0][0], w[0][1]);
+    *reinterpret_cast<uint2*>(out + a.padded) = make_uint2(w[1][0], w[1][1]);
+  }
+  if (c == 0) a.steps[at] = finite ? pow2(e) : __uint_as_float(0x7FC00000u);
+}
+
+// ------------------------------------------------------------------ the choice
+constexpr int kWarps = kChooseThreads / 32;
+constexpr int kBins = 256;      // of the search for the last page that is chosen
+static_assert(kBins == kChooseThreads, "a thread has a bin, and a candidate");
+
+__device__ __forceinline__ void mma_s8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint4 lds_u4(const unsigned char* p) { return *reinterpret_cast<const uint4*>(p); }
+
+// Scores as unsigned numbers in the same order; NaN is below all of them.
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t b = __float_as_uint(x);
+  return isnan(x) ? 0u : b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+__device__ __forceinline__ uint32_t rank_in_cluster() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void store_in_first(uint32_t at, uint32_t x) {  // into block 0 of the cluster
+  uint32_t far;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(far) : "r"(at));
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(far), "r"(x) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// Sum over the block's threads before this one, and over all; scratch: a word per warp.
+__device__ __forceinline__ int before_me(int x, int* scratch, int& all) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int upto = x;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, upto, d);
+    if (lane >= d) upto += y;
+  }
+  __syncthreads();  // scratch has been read
+  if (lane == 31) scratch[warp] = upto;
+  __syncthreads();
+  int before = upto - x;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    const int y = scratch[w];
+    if (w < warp) before += y;
+    all += y;
+  }
+  return before;
+}
+
+// Of keys[first..end) the `need` largest, ties to the lower index, get the key
+// 0xFFFFFFFF, and the others keep theirs, all below *least. 0 < need < end - first.
+// Rounds of a histogram over equal ranges of keys narrow [lo, hi] to the range in which
+// the last chosen key lies until a block can rank what is in it, or it is one key: every
+// round leaves 1/256 of the range, so there are 4 at most.
+__device__ void mark_largest(uint32_t* keys, int first, int end, int need, int* bins, uint32_t* cand, int* scratch, uint32_t* least) {
+  uint32_t lo = 0xFFFFFFFFu, hi = 0;
+  for (int p = first + threadIdx.x; p < end; p += kChooseThreads) lo = min(lo, keys[p]), hi = max(hi, keys[p]);
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  if ((threadIdx.x & 31) == 0) bins[threadIdx.x >> 5] = static_cast<int>(lo), bins[kWarps + (threadIdx.x >> 5)] = static_cast<int>(hi);
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) lo = min(lo, static_cast<uint32_t>(bins[w])), hi = max(hi, static_cast<uint32_t>(bins[kWarps + w]));
+  int inside = end - first;  // keys in lo..hi; `need` of them are wanted, and all above hi
+  while (inside > kChooseThreads && lo < hi) {
+    int shift = 0;  // bins of 2^shift keys
+    while (((hi - lo) >> shift) >= kBins) ++shift;
+    __syncthreads();
+    bins[threadIdx.x] = 0;
+    __syncthreads();
+    for (int p = first + threadIdx.x; p < end; p += kChooseThreads) {
+      const uint32_t k = keys[p];
+      if (k >= lo && k <= hi) atomicAdd(bins + ((hi - k) >> shift), 1);  // bin 0 has the largest
+    }
+    __syncthreads();
+    const int mine = bins[threadIdx.x];
+    int all;
+    const int above = before_me(mine, scratch, all);
+    if (above < need && above + mine >= need) {
+      const uint32_t top = hi - (static_cast<uint32_t>(threadIdx.x) << shift);
+      cand[0] = top;
+      cand[1] = top - lo < (1u << shift) ? lo : top - ((1u << shift) - 1);
+      cand[2] = static_cast<uint32_t>(need - above);
+      cand[3] = static_cast<uint32_t>(mine);
+    }
+    __syncthreads();
+    hi = cand[0], lo = cand[1], need = static_cast<int>(cand[2]), inside = static_cast<int>(cand[3]);
+    __syncthreads();
+  }
+  if (inside <= kChooseThreads) {  // few keys: each is ranked among them
+    if (threadIdx.x == 0) scratch[kWarps] = 0;
+    __syncthreads();
+    for (int p = first + threadIdx.x; p < end; p += kChooseThreads) {
+      const uint32_t k = keys[p];
+      if (k >= lo && k <= hi) {
+        const int at = atomicAdd(scratch + kWarps, 1);
+        cand[2 * at] = k, cand[2 * at + 1] = static_cast<uint32_t>(p);
+      }
+    }
+    __syncthreads();
+    if (static_cast<int>(threadIdx.x) < inside) {
+      const uint32_t k = cand[2 * threadIdx.x], p = cand[2 * threadIdx.x + 1];
+      int before = 0;
+      for (int i = 0; i < inside; ++i) before += cand[2 * i] > k || (cand[2 * i] == k && cand[2 * i + 1] < p);
+      if (before < need) keys[p] = 0xFFFFFFFFu;
+    }
+  } else {  // more equal keys than threads: the first `need` of them, in order
+    for (int p0 = first; p0 < end && need > 0; p0 += kChooseThreads) {
+      const int p = p0 + static_cast<int>(threadIdx.x);
+      const bool is = p < end && keys[p] == hi;
+      int all;
+      const int at = before_me(is ? 1 : 0, scratch, all);
+      if (is && at < need) keys[p] = 0xFFFFFFFFu;
+      need -= all;
+    }
+  }
+  *least = hi;  // chosen keys are above it
+  __syncthreads();
+}
+
+// A cluster takes one new row and KV head: its blocks score the pages, 16 at a time
+// per warp, into the first block's shared memory; that block chooses.
+template <int DP>
+__global__ void __launch_bounds__(kChooseThreads) choose_kernel(ChooseArgs a) {
+  constexpr int kCodes = 2 * DP;              // bytes of a page's bounds, and of a query head's parts
+  constexpr int kVectors = kCodes / 64;       // 16-byte vectors of a row per thread of a quad
+  extern __shared__ __align__(16) unsigned char smem[];
+  unsigned char* parts = smem;                                              // [head tiles][8][kCodes]
+  float* up = reinterpret_cast<float*>(smem + a.head_tiles * 8 * kCodes);   // [head tiles][8]
+  uint32_t* cand = reinterpret_cast<uint32_t*>(up + a.head_tiles * 8);      // [threads][2]
+  int* bins = reinterpret_cast<int*>(cand + 2 * kChooseThreads);            // [kBins]
+  int* scratch = bins + kBins;                                              // [kWarps + 1], rounded up
+  uint32_t* keys = reinterpret_cast<uint32_t*>(scratch + 16);               // [pages]
+  const int b = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const int token = static_cast<int>(blockIdx.x) / a.cluster, rank = a.cluster > 1 ? static_cast<int>(rank_in_cluster()) : 0;
+  if (a.cluster > 1) cluster_arrive();  // all of them are there before one writes to another
+  pdl_trigger();
+  pdl_wait();
+  const Seq s = sequence(a.p, b);
+  const bool there = token < s.n;
+  const int pos = s.len - s.n + token;
+  const int pages = there && pos >= 0 ? (pos >> a.p.page_shift) + 1 : 0;
+  const int64_t row = s.row0 + static_cast<int64_t>(token);
+  int32_t* out = a.out + row * a.out_row + h * a.out_head;
+  const bool all = pages <= a.n;  // nothing to choose
+  if (!all) {
+    // ---- the query heads, 4 or 2 channels per lane
+    constexpr int kLane = DP / 32;
+    for (int q = warp; q < a.head_tiles * 8; q += kWarps) {
+      uint32_t bits[kLane] = {};
+      if (q < a.share && lane * kLane < a.p.dim) {
+        const uint16_t* x = a.q + row * a.q_row + static_cast<int64_t>(h * a.share + q) * a.q_head + lane * kLane;
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(x);
+        bits[0] = w & 0xFFFFu, bits[1] = w >> 16;
+        if constexpr (kLane == 4) {
+          const uint32_t w2 = *reinterpret_cast<const uint32_t*>(x + 2);
+          bits[2] = w2 & 0xFFFFu, bits[3] = w2 >> 16;
+        }
+      }
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < kLane; ++i) top = max(top, bits[i] & 0x7FFFu);
+      top = __reduce_max_sync(0xffffffffu, top);
+      const bool counts = q < a.share && top < 0x7F80u;
+      const int e = counts ? exponent_of(top) : 0;
+      uint32_t neg = 0, plus = 0;
+#pragma unroll
+      for (int i = 0; i < kLane; ++i) {
+        const int x = counts ? __float2int_rn(__uint_as_float(bits[i] << 16) * pow2(-e)) : 0;
+        neg |= (static_cast<uint32_t>(min(x, 0)) & 0xFFu) << (8 * i);
+        plus |= (static_cast<uint32_t>(max(x, 0)) & 0xFFu) << (8 * i);
+      }
+      unsigned char* to = parts + q * kCodes + lane * kLane;
+      if constexpr (kLane == 4) {
+        *reinterpret_cast<uint32_t*>(to) = neg;
+        *reinterpret_cast<uint32_t*>(to + DP) = plus;
+      } else {
+        *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(neg);
+        *reinterpret_cast<uint16_t*>(to + DP) = static_cast<uint16_t>(plus);
+      }
+      if (lane == 0) up[q] = counts ? pow2(e) : __uint_as_float(0x7FC00000u);
+    }
+  }
+  __syncthreads();
+  if (a.cluster > 1) cluster_wait();
+  if (!all) {
+    // ---- scores: lane (g, t) has 16-byte vectors t, t + 4, .. of pages g and g + 8, which
+    // stand for four k-steps' operands; the query parts are read in the same order.
+    const uint32_t keys_at = smem_u32(keys);
+    for (int p0 = (rank * kWarps + warp) * 16; p0 < pages; p0 += a.cluster * kWarps * 16) {
+      int pg = -1;
+      if (lane < 16 && p0 + lane < pages) pg = a.p.table ? a.p.table[b * a.p.table_stride + p0 + lane] : b;
+      if (static_cast<unsigned>(pg) >= static_cast<unsigned>(a.p.n_pages)) pg = -1;
+      const int pa = __shfl_sync(0xffffffffu, pg, g), pb = __shfl_sync(0xffffffffu, pg, g + 8);
+      uint4 xa[kVectors], xb[kVectors];
+      float sa = __uint_as_float(0x7FC00000u), sb = sa;
+      const char* ca = a.codes + (static_cast<int64_t>(pa) * a.p.heads + h) * kCodes + 16 * t;
+      const char* cb = a.codes + (static_cast<int64_t>(pb) * a.p.heads + h) * kCodes + 16 * t;
+#pragma unroll
+      for (int v = 0; v < kVectors; ++v) {
+        xa[v] = xb[v] = make_uint4(0, 0, 0, 0);
+        if (pa >= 0) xa[v] = ld_once(ca + 64 * v);
+        if (pb >= 0) xb[v] = ld_once(cb + 64 * v);
+      }
+      if (pa >= 0) sa = a.steps[static_cast<int64_t>(pa) * a.p.heads + h];
+      if (pb >= 0) sb = a.steps[static_cast<int64_t>(pb) * a.p.heads + h];
+      float best_a = __uint_as_float(0x7FC00000u), best_b = best_a;
+      for (int ht = 0; ht < a.head_tiles; ++ht) {
+        int c[4] = {0, 0, 0, 0};
+        const unsigned char* at = parts + (ht * 8 + g) * kCodes + 16 * t;
+#pragma unroll
+        for (int v = 0; v < kVectors; ++v) {
+          const uint4 q = lds_u4(at + 64 * v);
+          mma_s8(c, xa[v].x, xb[v].x, xa[v].y, xb[v].y, q.x, q.y);
+          mma_s8(c, xa[v].z, xb[v].z, xa[v].w, xb[v].w, q.z, q.w);
+        }
+        const float2 u = *reinterpret_cast<const float2*>(up + ht * 8 + 2 * t);
+        best_a = fmaxf(best_a, fmaxf(static_cast<float>(c[0]) * u.x * sa, static_cast<float>(c[1]) * u.y * sa));  // NaN loses
+        best_b = fmaxf(best_b, fmaxf(static_cast<float>(c[2]) * u.x * sb, static_cast<float>(c[3]) * u.y * sb));
+      }
+#pragma unroll
+      for (int d = 1; d < 4; d <<= 1) {
+        best_a = fmaxf(best_a, __shfl_xor_sync(0xffffffffu, best_a, d));
+        best_b = fmaxf(best_b, __shfl_xor_sync(0xffffffffu, best_b, d));
+      }
+      const int p = p0 + g + 8 * t;
+      if (t < 2 && p < pages) {
+        const uint32_t k = order_of(t == 0 ? best_a : best_b);
+        if (a.cluster > 1)
+          store_in_first(keys_at + 4 * p, k);
+        else
+          keys[p] = k;
+      }
+    }
+  }
+  if (a.cluster > 1) {
+    cluster_arrive();
+    cluster_wait();
+  }
+  if (!there || rank != 0) return;
+  if (all) {
+    for (int i = threadIdx.x; i < a.n; i += kChooseThreads) out[i] = i < pages ? i : -1;
+    return;
+  }
+  __syncthreads();
+  const int need = a.n - a.first - a.recent, end = pages - a.recent;
+  uint32_t least = 0xFFFFFFFFu;
+  if (need > 0) mark_largest(keys, a.first, end, need, bins, cand, scratch, &least);
+  // ---- the list, in order: a thread has a run of pages
+  const int per = (pages + kChooseThreads - 1) / kChooseThreads, p0 = threadIdx.x * per, p1 = min(pages, p0 + per);
+  auto chosen = [&](int p) { return p < a.first || p >= end || (need > 0 && keys[p] > least); };
+  int count = 0;
+  for (int p = p0; p < p1; ++p) count += chosen(p);
+  int total;
+  int at = before_me(count, scratch, total);
+  for (int p = p0; p < p1; ++p)
+    if (chosen(p)) out[at++] = p;
+}
+
+template <int DP>
+size_t choose_smem(int head_tiles, int pages) {
+  return static_cast<size_t>(head_tiles) * 8 * (2 * DP + 4) + 8 * kChooseThreads + 4 * kBins + 64 + 4 * static_cast<size_t>(pages);
+}
+
+}  // namespace
+
+cudaError_t launch_bounds(const BoundsArgs& a, int pages, cudaStream_t st) {
+  const dim3 g(static_cast<unsigned>(pages), static_cast<unsigned>(a.p.heads), static_cast<unsigned>(a.p.n_seqs));
+  switch (a.p.fmt) {
+    case kBf16: return launch_next(bounds_kernel<kBf16>, g, kBoundsThreads, 0, st, a);
+    case kU8: return launch_next(bounds_kernel<kU8>, g, kBoundsThreads, 0, st, a);
+    default: return launch_next(bounds_kernel<kU4>, g, kBoundsThreads, 0, st, a);
+  }
+}
+
+cudaError_t choose_prepare() {
+  cudaError_t e = cudaFuncSetAttribute(choose_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kChooseSmem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(choose_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kChooseSmem);
+  return e;
+}
+
+int64_t choose_smem_bytes(int padded, int head_tiles, int64_t pages) {
+  return static_cast<int64_t>(padded == 64 ? choose_smem<64>(head_tiles, 0) : choose_smem<128>(head_tiles, 0)) + 4 * pages;
+}
+
+cudaError_t launch_choose(const ChooseArgs& a, int pages, cudaStream_t st) {
+  const dim3 g(static_cast<unsigned>(a.p.max_rows) * a.cluster, static_cast<unsigned>(a.p.heads), static_cast<unsigned>(a.p.n_seqs));
+  if (a.padded == 64) return launch_clusters(a.cluster, choose_kernel<64>, g, kChooseThreads, choose_smem<64>(a.head_tiles, pages), st, a);
+  return launch_clusters(a.cluster, choose_kernel<128>, g, kChooseThreads, choose_smem<128>(a.head_tiles, pages), st, a);
+}
+
+}  // namespace ipv

@@ -56,6 +56,8 @@ ipv_status setup_current_device(int* num_sms) {
     if ((e = ipv::attend_rows_prepare()) != cudaSuccess)
       return cuda_reject(e, "no usable kernel image for this device (built for sm_103a)");
     if ((e = ipv::attend_tiles_prepare()) != cudaSuccess) return cuda_reject(e, "tiled attention set-up");
+    if ((e = ipv::attend_chosen_prepare()) != cudaSuccess) return cuda_reject(e, "chosen pages' attention set-up");
+    if ((e = ipv::choose_prepare()) != cudaSuccess) return cuda_reject(e, "page choice set-up");
     if ((e = cudaDeviceGetAttribute(&d.num_sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess)
       return cuda_reject(e, "cudaDeviceGetAttribute");
     d.done = true;
@@ -64,9 +66,9 @@ ipv_status setup_current_device(int* num_sms) {
   return IPV_OK;
 }
 
-// Checks the pool and the batch and fills the kernels' view of them.
-ipv_status check(const ipv_pages* p, const ipv_batch* b, ipv::Pages* out) {
-  if (!p || !b) return reject(IPV_EINVAL, "pages and batch must not be NULL");
+// Checks the pool.
+ipv_status check_pages(const ipv_pages* p) {
+  if (!p) return reject(IPV_EINVAL, "pages and batch must not be NULL");
   const int fmt = p->format;
   if (fmt != IPV_PAGES_BF16 && fmt != IPV_PAGES_U8 && fmt != IPV_PAGES_U4)
     return reject(IPV_EINVAL, "unknown page format %d", fmt);
@@ -96,11 +98,37 @@ ipv_status check(const ipv_pages* p, const ipv_batch* b, ipv::Pages* out) {
       return reject(IPV_EINVAL, "k_par and v_par must be %d-byte aligned", 4 * groups);
     if (p->k_par == p->v_par) return reject(IPV_EINVAL, "k_par and v_par share one buffer");
   }
+  return IPV_OK;
+}
+
+// The pool as the kernels see it.
+void view_pages(const ipv_pages* p, ipv::Pages* out) {
+  ipv::Pages& o = *out;
+  o.fmt = p->format;
+  o.heads = p->n_kv_heads;
+  o.dim = p->head_dim;
+  o.page_size = p->page_size;
+  o.n_pages = static_cast<int>(p->n_pages);
+  o.page_stride = p->page_stride;
+  o.head_stride = p->head_stride;
+  o.row_stride = p->row_stride;
+  o.row_bytes = p->format == IPV_PAGES_BF16 ? 2 * p->head_dim : p->format == IPV_PAGES_U8 ? p->head_dim : p->head_dim / 2;
+  o.groups = (p->head_dim + ipv::kGroup - 1) / ipv::kGroup;
+  o.k = static_cast<char*>(p->k);
+  o.v = static_cast<char*>(p->v);
+  o.k_par = static_cast<uint32_t*>(p->k_par);
+  o.v_par = static_cast<uint32_t*>(p->v_par);
+}
+
+// Checks a batch over pages of this shape (page_size, heads, groups) and adds it to the kernels' view.
+ipv_status check_batch(const ipv_batch* b, ipv::Pages* out) {
+  if (!b) return reject(IPV_EINVAL, "pages and batch must not be NULL");
+  const int page_size = out->page_size, heads = out->heads, groups = out->groups;
   if (b->n_seqs < 0 || b->n_seqs > 65535) return reject(IPV_EINVAL, "n_seqs %d is not in 0..65535", b->n_seqs);
   if (b->max_pages < 1) return reject(IPV_EINVAL, "max_pages must be positive");
-  const bool pow2 = (p->page_size & (p->page_size - 1)) == 0;
-  if (b->max_pages > 1 && (!pow2 || p->page_size < 16))
-    return reject(IPV_EINVAL, "page_size %d: several pages per sequence need a power of two of at least 16", p->page_size);
+  const bool pow2 = (page_size & (page_size - 1)) == 0;
+  if (b->max_pages > 1 && (!pow2 || page_size < 16))
+    return reject(IPV_EINVAL, "page_size %d: several pages per sequence need a power of two of at least 16", page_size);
   if (!b->table && b->max_pages != 1) return reject(IPV_EINVAL, "without a table max_pages must be 1");
   if (b->table && (!aligned(b->table, 4) || (b->table_stride != 0 && b->table_stride < b->max_pages)))
     return reject(IPV_EINVAL, "table must be 4-byte aligned with table_stride 0 or >= max_pages");
@@ -112,28 +140,14 @@ ipv_status check(const ipv_pages* p, const ipv_batch* b, ipv::Pages* out) {
       return reject(IPV_EINVAL, "row_start and kv_len must be 4-byte aligned");
   }
   const int64_t rows = b->max_rows < b->total_rows ? b->max_rows : b->total_rows;
-  if (rows * p->n_kv_heads * groups > INT32_MAX)
+  if (rows * heads * groups > INT32_MAX)
     return reject(IPV_EINVAL, "max_rows * n_kv_heads * groups exceeds 2^31 - 1");
   ipv::Pages& o = *out;
-  o.fmt = fmt;
-  o.heads = p->n_kv_heads;
-  o.dim = p->head_dim;
-  o.page_size = p->page_size;
   o.page_shift = 31;
   if (b->max_pages > 1)
-    for (o.page_shift = 4; (1 << o.page_shift) < p->page_size; ++o.page_shift) {
+    for (o.page_shift = 4; (1 << o.page_shift) < page_size; ++o.page_shift) {
     }
-  o.n_pages = static_cast<int>(p->n_pages);
   o.max_pages = b->max_pages;
-  o.page_stride = p->page_stride;
-  o.head_stride = p->head_stride;
-  o.row_stride = p->row_stride;
-  o.row_bytes = fmt == IPV_PAGES_BF16 ? 2 * p->head_dim : fmt == IPV_PAGES_U8 ? p->head_dim : p->head_dim / 2;
-  o.groups = groups;
-  o.k = static_cast<char*>(p->k);
-  o.v = static_cast<char*>(p->v);
-  o.k_par = static_cast<uint32_t*>(p->k_par);
-  o.v_par = static_cast<uint32_t*>(p->v_par);
   o.table = b->table;
   o.table_stride = b->table_stride;
   o.row_start = b->row_start;
@@ -141,9 +155,18 @@ ipv_status check(const ipv_pages* p, const ipv_batch* b, ipv::Pages* out) {
   o.n_seqs = b->n_seqs;
   o.total_rows = b->total_rows;
   o.max_rows = static_cast<int>(rows);
-  const int64_t cap = static_cast<int64_t>(b->max_pages) * p->page_size;
+  const int64_t cap = static_cast<int64_t>(b->max_pages) * page_size;
   o.max_kv = static_cast<int>(b->max_kv < cap ? b->max_kv : cap);
   return IPV_OK;
+}
+
+// Checks the pool and the batch and fills the kernels' view of them.
+ipv_status check(const ipv_pages* p, const ipv_batch* b, ipv::Pages* out) {
+  if (!p || !b) return reject(IPV_EINVAL, "pages and batch must not be NULL");
+  const ipv_status s = check_pages(p);
+  if (s != IPV_OK) return s;
+  view_pages(p, out);
+  return check_batch(b, out);
 }
 
 ipv_status check_packed(const void* x, const char* name, int64_t row, int64_t head) {
@@ -165,7 +188,8 @@ constexpr int64_t kRowsMost = 64, kRowsBytes = 76000000;
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-ipv_status check_attend(const ipv_pages* p, const ipv_batch* b, const ipv_attend_args* t, ipv::AttendArgs* a) {
+// chosen: NULL unless the call is for chosen pages.
+ipv_status check_attend(const ipv_pages* p, const ipv_batch* b, const ipv_attend_args* t, const ipv_chosen* chosen, ipv::AttendArgs* a) {
   ipv_status s = check(p, b, &a->p);
   if (s != IPV_OK) return s;
   if (!t) return reject(IPV_EINVAL, "args must not be NULL");
@@ -179,7 +203,19 @@ ipv_status check_attend(const ipv_pages* p, const ipv_batch* b, const ipv_attend
     return reject(IPV_EINVAL, "max_rows * n_q_heads exceeds 2^31 - 1");
   const int64_t rows = static_cast<int64_t>(a->p.max_rows) * (t->n_q_heads / p->n_kv_heads);
   if ((rows + 15) / 16 * a->p.n_seqs > INT32_MAX) return reject(IPV_EINVAL, "n_seqs times the query tiles of max_rows exceeds 2^31 - 1");
-  if (a->p.fmt != ipv::kBf16 && rows > kRowsMost &&  // widened into the workspace
+  if (chosen) {
+    if (!t->causal || t->window > 0 || t->sinks > 0) return reject(IPV_EINVAL, "chosen pages need causal = 1, window = 0 and sinks = 0");
+    if (chosen->n_chosen < 1) return reject(IPV_EINVAL, "n_chosen must be positive");
+    if (chosen->row_stride < 0 || chosen->head_stride < 0) return reject(IPV_EINVAL, "chosen: strides must not be negative");
+    if (a->p.max_kv > 1 << 30) return reject(IPV_EINVAL, "chosen pages: max_kv exceeds 2^30");
+    const int share = t->n_q_heads / p->n_kv_heads, tile = ipv::attend_rows_tile(share);
+    if (static_cast<int64_t>(a->p.max_rows) * ((share + tile - 1) / tile) * a->p.n_seqs > INT32_MAX)
+      return reject(IPV_EINVAL, "n_seqs times the query tiles of max_rows exceeds 2^31 - 1");
+    a->chosen = chosen->pages;
+    a->chosen_row = chosen->row_stride;
+    a->chosen_head = chosen->head_stride;
+    a->n_chosen = chosen->n_chosen;
+  } else if (a->p.fmt != ipv::kBf16 && rows > kRowsMost &&  // widened into the workspace
       4.0 * a->p.n_seqs * a->p.heads * a->p.max_kv * a->p.dim >= 1152921504606846976.0)
     return reject(IPV_EINVAL, "n_seqs * n_kv_heads * max_kv * head_dim: the workspace would exceed 2^60 bytes");
   a->q_heads = t->n_q_heads;
@@ -229,7 +265,12 @@ void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
   const bool waves = p.max_kv <= kWhole && (rows + 15) / 16 * p.n_seqs * p.heads > num_sms;  // of blocks that take tiles whole
   plan->tiles = rows > kRowsMost || (rows > 16 && p.fmt == ipv::kBf16 && (read > kRowsBytes || waves));
   plan->bytes = 0;
-  if (plan->tiles) {
+  if (a->n_chosen > 0) {
+    plan->tiles = false;
+    a->tile = ipv::attend_rows_tile(a->share);
+    a->unit = kRowsLeast;
+    plan->blocks = num_sms * ipv::attend_chosen_resident(p.fmt, p.dim, a->tile);
+  } else if (plan->tiles) {
     a->tile = ipv::kTilesRows;
     a->unit = kTilesLeast;
     plan->blocks = num_sms;
@@ -244,11 +285,15 @@ void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
     a->unit = kRowsLeast;
     plan->blocks = num_sms * ipv::attend_rows_resident(p.fmt, p.dim, a->tile);
   }
-  a->tiles = static_cast<int>((rows + a->tile - 1) / a->tile);
+  a->per_row = (a->share + a->tile - 1) / a->tile;  // chosen pages only, as by_per_row
+  a->by_per_row = ipv::Divide(a->per_row);
+  a->tiles = a->n_chosen > 0 ? p.max_rows * a->per_row : static_cast<int>((rows + a->tile - 1) / a->tile);
   a->by_tiles = ipv::Divide(a->tiles);
   // Keys that a row tile can see, at most (its windows, the sinks, their steps' ends).
   int64_t span = p.max_kv;
-  if (a->window) {
+  if (a->n_chosen > 0) {
+    span = std::min((span + p.page_size - 1) / p.page_size, static_cast<int64_t>(a->n_chosen)) * p.page_size;
+  } else if (a->window) {
     const int64_t seen = static_cast<int64_t>(a->window) + a->tile + a->sinks + 2 * (plan->tiles ? ipv::kTilesStep : ipv::kRowsStep);
     if (seen < span) span = seen;
   }
@@ -330,12 +375,14 @@ extern "C" ipv_status ipv_pages_read(const ipv_pages* pages, const ipv_batch* ba
   return e == cudaSuccess ? IPV_OK : cuda_reject(e, "page read kernel");
 }
 
-extern "C" ipv_status ipv_attend_workspace(const ipv_pages* pages, const ipv_batch* batch,
-                                           const ipv_attend_args* args, int64_t* bytes_out) {
+namespace {
+
+ipv_status attend_workspace(const ipv_pages* pages, const ipv_batch* batch, const ipv_attend_args* args, const ipv_chosen* chosen,
+                            int64_t* bytes_out) {
   if (!bytes_out) return reject(IPV_EINVAL, "bytes_out must not be NULL");
   *bytes_out = 0;
   ipv::AttendArgs a{};
-  ipv_status s = check_attend(pages, batch, args, &a);
+  ipv_status s = check_attend(pages, batch, args, chosen, &a);
   if (s != IPV_OK) return s;
   if (a.p.n_seqs == 0 || a.p.max_rows == 0) return IPV_OK;
   int num_sms = 0;
@@ -346,10 +393,9 @@ extern "C" ipv_status ipv_attend_workspace(const ipv_pages* pages, const ipv_bat
   return IPV_OK;
 }
 
-extern "C" ipv_status ipv_attend(const ipv_pages* pages, const ipv_batch* batch, const ipv_attend_args* args,
-                                 void* stream) {
+ipv_status attend(const ipv_pages* pages, const ipv_batch* batch, const ipv_attend_args* args, const ipv_chosen* chosen, void* stream) {
   ipv::AttendArgs a{};
-  ipv_status s = check_attend(pages, batch, args, &a);
+  ipv_status s = check_attend(pages, batch, args, chosen, &a);
   if (s != IPV_OK) return s;
   if (a.p.n_seqs == 0 || a.p.max_rows == 0) return IPV_OK;
   s = check_packed(args->q, "q", args->q_row_stride, args->q_head_stride);
@@ -357,6 +403,8 @@ extern "C" ipv_status ipv_attend(const ipv_pages* pages, const ipv_batch* batch,
   if (s != IPV_OK) return s;
   if (args->q == args->out) return reject(IPV_EINVAL, "q and out share one buffer");
   if (args->lse && !aligned(args->lse, 4)) return reject(IPV_EINVAL, "lse must be 4-byte aligned");
+  if (chosen && (!chosen->pages || !aligned(chosen->pages, 4)))
+    return reject(IPV_EINVAL, "the chosen pages must not be NULL, and 4-byte aligned");
   int num_sms = 0;
   if ((s = setup_current_device(&num_sms)) != IPV_OK) return s;
   Plan plan;
@@ -398,10 +446,34 @@ extern "C" ipv_status ipv_attend(const ipv_pages* pages, const ipv_batch* batch,
     if (!ipv::attend_tiles_maps(a, bf16, &plan.maps)) return reject(IPV_ECUDA, "cuTensorMapEncodeTiled refused the pool");
     e = ipv::launch_attend_tiles(a, bf16, plan.maps, plan.blocks, g_limit_ns.load(), st);
   } else {
-    e = ipv::launch_attend_rows(a, plan.blocks, st);
+    e = chosen ? ipv::launch_attend_chosen(a, plan.blocks, st) : ipv::launch_attend_rows(a, plan.blocks, st);
   }
   if (e != cudaSuccess) return cuda_reject(e, "attention kernel");
   return IPV_OK;
+}
+
+}  // namespace
+
+extern "C" ipv_status ipv_attend_workspace(const ipv_pages* pages, const ipv_batch* batch,
+                                           const ipv_attend_args* args, int64_t* bytes_out) {
+  return attend_workspace(pages, batch, args, nullptr, bytes_out);
+}
+
+extern "C" ipv_status ipv_attend(const ipv_pages* pages, const ipv_batch* batch, const ipv_attend_args* args,
+                                 void* stream) {
+  return attend(pages, batch, args, nullptr, stream);
+}
+
+extern "C" ipv_status ipv_attend_chosen_workspace(const ipv_pages* pages, const ipv_batch* batch, const ipv_attend_args* args,
+                                                  const ipv_chosen* chosen, int64_t* bytes_out) {
+  if (!chosen) return reject(IPV_EINVAL, "chosen must not be NULL");
+  return attend_workspace(pages, batch, args, chosen, bytes_out);
+}
+
+extern "C" ipv_status ipv_attend_chosen(const ipv_pages* pages, const ipv_batch* batch, const ipv_attend_args* args,
+                                        const ipv_chosen* chosen, void* stream) {
+  if (!chosen) return reject(IPV_EINVAL, "chosen must not be NULL");
+  return attend(pages, batch, args, chosen, stream);
 }
 
 extern "C" ipv_status ipv_attend_error(uint32_t* err_out) {
@@ -417,4 +489,197 @@ extern "C" ipv_status ipv_attend_wait_limit(int64_t nanoseconds) {
   if (nanoseconds < 0) return reject(IPV_EINVAL, "the limit must not be negative");
   g_limit_ns.store(nanoseconds == 0 ? kDefaultLimitNs : nanoseconds - 1);  // 1: no wait at all
   return IPV_OK;
+}
+
+extern "C" ipv_status ipv_pages_write_rotated(const ipv_pages* pages, const ipv_batch* batch, const ipv_rotary* rotary,
+                                              const ipv_rotate_args* t, void* stream) {
+  ipv::RotateArgs a{};
+  ipv_status s = check(pages, batch, &a.p);
+  if (s != IPV_OK) return s;
+  if (!rotary || !t) return reject(IPV_EINVAL, "rotary and args must not be NULL");
+  if (rotary->rot_dim < 16 || rotary->rot_dim % 16 != 0 || rotary->rot_dim > a.p.dim)
+    return reject(IPV_EINVAL, "rot_dim %d is not a multiple of 16 up to head_dim %d", rotary->rot_dim, a.p.dim);
+  if (rotary->n_positions < 1 || rotary->n_positions > INT32_MAX) return reject(IPV_EINVAL, "n_positions must be positive and below 2^31");
+  if (rotary->interleaved != 0 && rotary->interleaved != 1) return reject(IPV_EINVAL, "interleaved must be 0 or 1");
+  if (rotary->n_axes < 1 || rotary->n_axes > 4) return reject(IPV_EINVAL, "n_axes %d is not in 1..4", rotary->n_axes);
+  int64_t end = 0;
+  for (int i = 0; i < rotary->n_axes; ++i) {
+    if (rotary->sections[i] < 8 || rotary->sections[i] % 8 != 0)
+      return reject(IPV_EINVAL, "sections must be positive multiples of 8");
+    end += rotary->sections[i];
+    if (i < 3) a.ends[i] = static_cast<int>(std::min<int64_t>(end, INT32_MAX));
+  }
+  if (end != rotary->rot_dim / 2) return reject(IPV_EINVAL, "the sections' sum is not rot_dim / 2");
+  for (int i = rotary->n_axes - 1; i < 3; ++i) a.ends[i] = INT32_MAX;  // the last axis has no end
+  if (t->n_q_heads < 1 || t->n_q_heads > 65535) return reject(IPV_EINVAL, "n_q_heads %d is not in 1..65535", t->n_q_heads);
+  if (!std::isfinite(t->eps) || t->eps < 0.0f) return reject(IPV_EINVAL, "eps must be finite and not negative");
+  if (!aligned(t->q_weight, 16) || !aligned(t->k_weight, 16)) return reject(IPV_EINVAL, "weights must be 16-byte aligned");
+  if (a.p.n_seqs == 0 || a.p.max_rows == 0) return IPV_OK;
+  s = check_packed(t->q, "q", t->q_row_stride, t->q_head_stride);
+  if (s == IPV_OK) s = check_packed(t->q_out, "q_out", t->out_row_stride, t->out_head_stride);
+  if (s == IPV_OK) s = check_packed(t->k_new, "k_new", t->row_stride, t->head_stride);
+  if (s == IPV_OK) s = check_packed(t->v_new, "v_new", t->row_stride, t->head_stride);
+  if (s != IPV_OK) return s;
+  if (t->q == t->q_out && (t->q_row_stride != t->out_row_stride || t->q_head_stride != t->out_head_stride))
+    return reject(IPV_EINVAL, "q_out may be q only with q's strides");
+  if (!rotary->table || !aligned(rotary->table, 16)) return reject(IPV_EINVAL, "the rotary table must not be NULL, and 16-byte aligned");
+  if (!t->positions || !aligned(t->positions, 4)) return reject(IPV_EINVAL, "positions must not be NULL, and 4-byte aligned");
+  if (t->positions_stride < 0 || (rotary->n_axes > 1 && t->positions_stride < batch->total_rows))
+    return reject(IPV_EINVAL, "positions_stride is below total_rows");
+  a.q = static_cast<const uint16_t*>(t->q);
+  a.q_out = static_cast<uint16_t*>(t->q_out);
+  a.k_new = static_cast<const uint16_t*>(t->k_new);
+  a.v_new = static_cast<const uint16_t*>(t->v_new);
+  a.q_row = t->q_row_stride;
+  a.q_head = t->q_head_stride;
+  a.out_row = t->out_row_stride;
+  a.out_head = t->out_head_stride;
+  a.row = t->row_stride;
+  a.head = t->head_stride;
+  a.q_heads = t->n_q_heads;
+  a.turns = rotary->table;
+  a.n_positions = rotary->n_positions;
+  a.rot = rotary->rot_dim;
+  a.neighbours = rotary->interleaved != 0;
+  a.positions = t->positions;
+  a.positions_stride = t->positions_stride;
+  a.q_weight = static_cast<const uint16_t*>(t->q_weight);
+  a.k_weight = static_cast<const uint16_t*>(t->k_weight);
+  a.eps = t->eps;
+  a.by_dim = 1.0f / static_cast<float>(a.p.dim);
+  const cudaError_t e = ipv::launch_rotate(a, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? IPV_OK : cuda_reject(e, "rotated write kernel");
+}
+
+extern "C" ipv_status ipv_pages_copy(const ipv_pages* pages, const int32_t* from, const int32_t* to, int64_t n, void* stream) {
+  const ipv_status s = check_pages(pages);
+  if (s != IPV_OK) return s;
+  if (n < 0) return reject(IPV_EINVAL, "n must not be negative");
+  if (n == 0) return IPV_OK;
+  if (!from || !to || !aligned(from, 4) || !aligned(to, 4)) return reject(IPV_EINVAL, "from and to must not be NULL, and 4-byte aligned");
+  if (from == to) return reject(IPV_EINVAL, "from and to share one buffer");
+  ipv::CopyArgs a{};
+  view_pages(pages, &a.p);
+  a.from = from;
+  a.to = to;
+  a.row_chunks = a.p.row_bytes / 16;
+  const int64_t chunks = static_cast<int64_t>(a.p.heads) * a.p.page_size * a.row_chunks;
+  if (chunks > INT32_MAX - ipv::pages_copy_part()) return reject(IPV_EINVAL, "a page has 2^31 16-byte pieces or more");
+  a.chunks = static_cast<int>(chunks);
+  a.parts = static_cast<int>((chunks + ipv::pages_copy_part() - 1) / ipv::pages_copy_part());
+  if (n > INT32_MAX / a.parts) return reject(IPV_EINVAL, "n times a page's parts exceeds 2^31 - 1");
+  a.by_row = ipv::Divide(a.row_chunks);
+  a.by_page = ipv::Divide(a.p.page_size);
+  a.by_parts = ipv::Divide(a.parts);
+  const cudaError_t e = ipv::launch_pages_copy(a, n, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? IPV_OK : cuda_reject(e, "page copy kernel");
+}
+
+extern "C" ipv_status ipv_pages_gather(const ipv_pages* source_pages, const ipv_batch* source, const ipv_pages* pages,
+                                       const ipv_batch* batch, const int32_t* kept, int64_t kept_seq_stride,
+                                       int64_t kept_head_stride, void* stream) {
+  ipv::MoveArgs a{};
+  ipv_status s = check(source_pages, source, &a.src);
+  if (s == IPV_OK) s = check(pages, batch, &a.p);
+  if (s != IPV_OK) return s;
+  if (a.src.fmt != a.p.fmt || a.src.heads != a.p.heads || a.src.dim != a.p.dim)
+    return reject(IPV_EINVAL, "the two caches must have one format, n_kv_heads and head_dim");
+  if (a.src.n_seqs != a.p.n_seqs) return reject(IPV_EINVAL, "the two batches must have the same sequences");
+  if (kept && !aligned(kept, 4)) return reject(IPV_EINVAL, "kept must be 4-byte aligned");
+  if (kept_seq_stride < 0 || kept_head_stride < 0) return reject(IPV_EINVAL, "kept: strides must not be negative");
+  if (a.p.n_seqs == 0 || a.p.max_rows == 0) return IPV_OK;
+  a.kept = kept;
+  a.kept_seq = kept_seq_stride;
+  a.kept_head = kept_head_stride;
+  a.row_chunks = a.p.row_bytes / 16;
+  const cudaError_t e = ipv::launch_pages_gather(a, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? IPV_OK : cuda_reject(e, "row gather kernel");
+}
+
+namespace {
+
+ipv_status check_bounds(const ipv_bounds* b) {
+  if (!b) return reject(IPV_EINVAL, "bounds must not be NULL");
+  if (b->n_kv_heads < 1 || b->n_kv_heads > 65535) return reject(IPV_EINVAL, "n_kv_heads %d is not in 1..65535", b->n_kv_heads);
+  if (b->head_dim < 8 || b->head_dim > 128 || b->head_dim % 8 != 0)
+    return reject(IPV_EINVAL, "head_dim %d is not a multiple of 8 up to 128", b->head_dim);
+  if (b->page_size < 1 || b->n_pages < 1 || b->n_pages > INT32_MAX)
+    return reject(IPV_EINVAL, "page_size and n_pages must be positive and below 2^31");
+  if (!b->codes || !b->steps || !aligned(b->codes, 16) || !aligned(b->steps, 4))
+    return reject(IPV_EINVAL, "codes (16-byte aligned) and steps (4-byte aligned) must not be NULL");
+  return IPV_OK;
+}
+
+int padded(int dim) { return dim <= 64 ? 64 : 128; }
+
+constexpr int64_t kChoosePages = 32768;
+constexpr int kChooseShare = 64;
+
+}  // namespace
+
+extern "C" ipv_status ipv_bounds_update(const ipv_bounds* bounds, const ipv_pages* pages, const ipv_batch* batch, void* stream) {
+  ipv::BoundsArgs a{};
+  ipv_status s = check_bounds(bounds);
+  if (s == IPV_OK) s = check(pages, batch, &a.p);
+  if (s != IPV_OK) return s;
+  if (bounds->n_kv_heads != a.p.heads || bounds->head_dim != a.p.dim || bounds->page_size != a.p.page_size || bounds->n_pages != a.p.n_pages)
+    return reject(IPV_EINVAL, "the bounds are of pages of another shape");
+  if (a.p.n_seqs == 0 || a.p.max_rows == 0 || a.p.max_kv == 0) return IPV_OK;
+  a.codes = static_cast<char*>(bounds->codes);
+  a.steps = bounds->steps;
+  a.padded = padded(a.p.dim);
+  const int64_t held = (static_cast<int64_t>(a.p.max_kv) + a.p.page_size - 1) / a.p.page_size;
+  const int64_t touched = (static_cast<int64_t>(a.p.max_rows) + a.p.page_size - 2) / a.p.page_size + 1;
+  const cudaError_t e = ipv::launch_bounds(a, static_cast<int>(std::min(held, touched)), static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? IPV_OK : cuda_reject(e, "page bounds kernel");
+}
+
+extern "C" ipv_status ipv_bounds_choose(const ipv_bounds* bounds, const ipv_batch* batch, const ipv_choose_args* t, void* stream) {
+  ipv_status s = check_bounds(bounds);
+  if (s != IPV_OK) return s;
+  ipv::ChooseArgs a{};
+  a.p.heads = bounds->n_kv_heads;
+  a.p.dim = bounds->head_dim;
+  a.p.page_size = bounds->page_size;
+  a.p.n_pages = static_cast<int>(bounds->n_pages);
+  a.p.groups = 1;
+  s = check_batch(batch, &a.p);
+  if (s != IPV_OK) return s;
+  if (!t) return reject(IPV_EINVAL, "args must not be NULL");
+  if (t->n_q_heads < 1 || t->n_q_heads % a.p.heads != 0)
+    return reject(IPV_EINVAL, "n_q_heads %d is not a multiple of n_kv_heads %d", t->n_q_heads, a.p.heads);
+  a.share = t->n_q_heads / a.p.heads;
+  if (a.share > kChooseShare) return reject(IPV_EINVAL, "%d query heads per KV head: the most is %d", a.share, kChooseShare);
+  if (t->first < 0 || t->recent < 1 || t->n_chosen < 1 || static_cast<int64_t>(t->first) + t->recent > t->n_chosen)
+    return reject(IPV_EINVAL, "n_chosen must be at least first + recent, first at least 0, recent at least 1");
+  if (t->out_row_stride < 0 || t->out_head_stride < 0) return reject(IPV_EINVAL, "out: strides must not be negative");
+  const int64_t pages = (static_cast<int64_t>(a.p.max_kv) + a.p.page_size - 1) / a.p.page_size;
+  if (pages > kChoosePages) return reject(IPV_EINVAL, "max_kv spans %lld pages, the most is %lld", static_cast<long long>(pages),
+                                          static_cast<long long>(kChoosePages));
+  if (a.p.n_seqs == 0 || a.p.max_rows == 0) return IPV_OK;
+  s = check_packed(t->q, "q", t->q_row_stride, t->q_head_stride);
+  if (s != IPV_OK) return s;
+  if (!t->out || !aligned(t->out, 4)) return reject(IPV_EINVAL, "out must not be NULL, and 4-byte aligned");
+  int num_sms = 0;
+  if ((s = setup_current_device(&num_sms)) != IPV_OK) return s;
+  a.codes = static_cast<const char*>(bounds->codes);
+  a.steps = bounds->steps;
+  a.padded = padded(a.p.dim);
+  a.q = static_cast<const uint16_t*>(t->q);
+  a.q_row = t->q_row_stride;
+  a.q_head = t->q_head_stride;
+  a.head_tiles = (a.share + 7) / 8;
+  a.out = t->out;
+  a.out_row = t->out_row_stride;
+  a.out_head = t->out_head_stride;
+  a.n = t->n_chosen;
+  a.first = t->first;
+  a.recent = t->recent;
+  // Blocks for one list: as long as each warp keeps 16 pages and the device has room for them all.
+  const int64_t lists = static_cast<int64_t>(a.p.max_rows) * a.p.n_seqs * a.p.heads;
+  a.cluster = 1;
+  while (a.cluster < 8 && pages > 16 * (ipv::kChooseThreads / 32) * a.cluster && lists * a.cluster * 2 <= num_sms) a.cluster *= 2;
+  if (static_cast<int64_t>(a.p.max_rows) * a.cluster > INT32_MAX) return reject(IPV_EINVAL, "max_rows times a cluster's blocks exceeds 2^31 - 1");
+  const cudaError_t e = ipv::launch_choose(a, static_cast<int>(pages), static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? IPV_OK : cuda_reject(e, "page choice kernel");
 }

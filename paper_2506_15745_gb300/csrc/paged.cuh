@@ -1,5 +1,7 @@
 // Internal declarations of the paged cache (paged.cu: C ABI; paged_rows.cu:
-// write and read-back; attend_rows.cu: attention of a few query rows;
+// write and read-back; rotate.cu: norms and rotation on the way in; bounds.cu:
+// bounds of pages and the choice by them; move.cu: pages and rows moved;
+// attend_rows.cu: attention of a few query rows, over all pages or chosen ones;
 // attend_tiles.cu: of many).
 #pragma once
 
@@ -120,6 +122,14 @@ struct AttendArgs {
   // which joins their parts by itself) take one KV head of one row tile.
   int unit, cluster;
   int tile;  // query rows of a row tile
+  // Chosen pages: a row tile holds one new row's query heads (or `tile` of them), `per_row` tiles a new row; entry
+  // e of chosen[row][KV head] is a page of the row's sequence. Keys count through the row's list: n_chosen pages
+  // at most.
+  const int32_t* chosen;
+  int64_t chosen_row, chosen_head;
+  int n_chosen;
+  Divide by_per_row;
+  int per_row;
   // Partial results, for each block's first and last run: unnormalised sums
   // (rows kernel: [blocks][2][tile][dim], tiled kernel: [blocks][2][dim / 4][tile][4]),
   // (running maximum, sum) [blocks][2][tile], and a record [blocks][2] (part_record).
@@ -142,6 +152,21 @@ struct KeyRange {
 
 __device__ __forceinline__ int token_hi(const AttendArgs& a, const Seq& s, int tok) {
   return a.causal ? max(0, s.len - s.n + tok + 1) : s.len;
+}
+
+// Pages of a sequence that hold rows which token `tok` sees.
+__device__ __forceinline__ int pages_seen(const AttendArgs& a, const Seq& s, int tok) {
+  const int hi = token_hi(a, s, tok);
+  return hi > 0 ? ((hi - 1) >> a.p.page_shift) + 1 : 0;
+}
+
+// The steps over the pages that token `tok` has chosen: keys count through its list.
+template <int STEP>
+__device__ __forceinline__ KeyRange chosen_range(const AttendArgs& a, const Seq& s, int tok) {
+  KeyRange r = {};
+  r.hi_min = r.hi_max = min(a.n_chosen, pages_seen(a, s, tok)) * a.p.page_size;  // <= 2^30 + a page, checked
+  r.steps = r.hi_max > 0 ? (r.hi_max - 1) / STEP + 1 : 0;
+  return r;
 }
 
 template <int STEP>
@@ -172,6 +197,75 @@ struct RowsArgs {
 cudaError_t launch_pages_write(const RowsArgs& a, cudaStream_t st);
 cudaError_t launch_pages_read(const RowsArgs& a, cudaStream_t st);
 
+struct RotateArgs {
+  Pages p;
+  const uint16_t* q;
+  const uint16_t* k_new;
+  const uint16_t* v_new;
+  uint16_t* q_out;
+  int64_t q_row, q_head, out_row, out_head, row, head;  // strides in elements; the last two of k_new and v_new
+  int q_heads;
+  const float* turns;        // [n_positions][rot]: cosines, sines
+  int64_t n_positions;
+  int rot;
+  bool neighbours;           // pairs (2i, 2i + 1)
+  int ends[3];               // where the first axes' frequencies end
+  const int32_t* positions;  // [axes][positions_stride]
+  int64_t positions_stride;
+  const uint16_t* q_weight;  // norms' weights, or NULL
+  const uint16_t* k_weight;
+  float eps, by_dim;
+};
+cudaError_t launch_rotate(const RotateArgs& a, cudaStream_t st);
+
+// Whole pages of one pool: `to[i]` becomes a copy of `from[i]`.
+struct CopyArgs {
+  Pages p;                        // the pool alone
+  const int32_t* from;
+  const int32_t* to;
+  int chunks, row_chunks, parts;  // 16-byte chunks of K in a page and in a row; blocks of a page
+  Divide by_row, by_page, by_parts;
+};
+int pages_copy_part();            // chunks that a block copies
+cudaError_t launch_pages_copy(const CopyArgs& a, int64_t n, cudaStream_t st);
+
+// New row i of sequence b and head h in p becomes row kept[b][h][i] of sequence b in src.
+struct MoveArgs {
+  Pages p, src;
+  const int32_t* kept;            // NULL: row i
+  int64_t kept_seq, kept_head;
+  int row_chunks;
+};
+cudaError_t launch_pages_gather(const MoveArgs& a, cudaStream_t st);
+
+// Bounds of pages: codes [n_pages][heads][2][padded] (lower, upper), steps [n_pages][heads].
+struct BoundsArgs {
+  Pages p;
+  char* codes;
+  float* steps;
+  int padded;
+};
+cudaError_t launch_bounds(const BoundsArgs& a, int pages, cudaStream_t st);  // pages that a sequence's new rows lie in, at most
+
+struct ChooseArgs {
+  Pages p;                        // the batch and the pool's shape; no rows are read
+  const char* codes;
+  const float* steps;
+  int padded;
+  const uint16_t* q;
+  int64_t q_row, q_head;
+  int share, head_tiles;          // query heads per KV head, in tiles of 8
+  int32_t* out;
+  int64_t out_row, out_head;
+  int n, first, recent;
+  int cluster;                    // blocks that score the pages of one row and KV head
+};
+constexpr int kChooseThreads = 256;
+constexpr int kChooseSmem = 227 * 1024;
+cudaError_t choose_prepare();     // once per device
+int64_t choose_smem_bytes(int padded, int head_tiles, int64_t pages);
+cudaError_t launch_choose(const ChooseArgs& a, int pages, cudaStream_t st);
+
 // Every row that the new rows of a sequence may read, widened from codes to
 // fp16 [n_seqs][heads][max_kv][dim]; rows that no step of `step` keys reads
 // are left out.
@@ -190,6 +284,9 @@ constexpr int kRowsWarps = 4;
 constexpr int kRowsCluster = 8;               // blocks of a cluster
 cudaError_t attend_rows_prepare();            // once per device
 cudaError_t launch_attend_rows(const AttendArgs& a, int blocks, cudaStream_t st);
+int attend_chosen_resident(int fmt, int dim, int tile);  // the same for chosen pages
+cudaError_t attend_chosen_prepare();
+cudaError_t launch_attend_chosen(const AttendArgs& a, int blocks, cudaStream_t st);
 
 // Many query rows (attend_tiles.cu): the pool's rows are 16-bit elements.
 constexpr int kTilesRows = 256;  // query rows of a tile of work

@@ -1,0 +1,225 @@
+// New rows on their way into the cache: queries and keys normalised per head and
+// rotated by their positions in one pass, queries to the packed result, keys and
+// values to their pages (quantised as paged_rows.cu does).
+//
+// HBM-bound: a row is read once and written once. 8 lanes take a head of a row,
+// lane c the 16-byte chunks c and c + 8, so that with all of 128 channels rotated in
+// halves a lane has both ends of its pairs; elsewhere the partners come by shuffles.
+// A block takes one row: its lanes fetch their cosines and sines once, and use them
+// for all the heads that they take.
+#include "paged_codes.cuh"
+
+namespace ipv {
+namespace {
+
+constexpr int kBlock = 256;
+constexpr int kTeams = kBlock / 8;
+
+// Pairs of channels: (i, i + 64) of 128, (i, i + rot / 2) of the first rot, (2i, 2i + 1).
+enum : int { kOwn = 0, kHalves = 1, kNeighbours = 2 };
+
+struct Turn {
+  float c[8], s[8];  // kNeighbours: 4 of each
+};
+
+// Cosines and sines from frequency f on, N of them, of one axis.
+template <int N>
+__device__ __forceinline__ void load_turn(const RotateArgs& a, int64_t row, int f, Turn& x) {
+  int axis = 0;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) axis += f >= a.ends[i];
+  const int pos = a.positions[axis * a.positions_stride + row];
+  const bool in = static_cast<unsigned>(pos) < static_cast<unsigned>(a.n_positions);
+  const float4* p = reinterpret_cast<const float4*>(a.turns + static_cast<int64_t>(in ? pos : 0) * a.rot + f);
+  const float bad = __uint_as_float(0x7FC00000u);  // a position that the table has not
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) {
+    const float4 c = in ? p[i] : make_float4(bad, bad, bad, bad), s = in ? p[a.rot / 8 + i] : make_float4(bad, bad, bad, bad);
+    x.c[4 * i] = c.x, x.c[4 * i + 1] = c.y, x.c[4 * i + 2] = c.z, x.c[4 * i + 3] = c.w;
+    x.s[4 * i] = s.x, x.s[4 * i + 1] = s.y, x.s[4 * i + 2] = s.z, x.s[4 * i + 3] = s.w;
+  }
+}
+
+__device__ __forceinline__ void unpack(const uint4& x, float (&y)[8]) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[2 * i] = lo_f(w[i]), y[2 * i + 1] = hi_f(w[i]);
+}
+__device__ __forceinline__ uint4 pack(const float (&y)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(y[2 * i + 1]), "f"(y[2 * i]));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// A head's row, chunks c and c + 8 of it in x: normalised with w (NULL: not), rotated. For whole warps.
+template <int PAIRS>
+__device__ __forceinline__ void rotate(const RotateArgs& a, uint4 (&x)[2], const uint16_t* w, const Turn (&turn)[2], int c) {
+  float y[2][8];
+  unpack(x[0], y[0]);
+  unpack(x[1], y[1]);
+  if (w) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = fmaf(y[g][i], y[g][i], sum);
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    const float inv = rsqrtf(sum * a.by_dim + a.eps);
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      if (8 * (c + 8 * g) >= a.p.dim) continue;
+      float v[8];
+      unpack(*reinterpret_cast<const uint4*>(w + 8 * (c + 8 * g)), v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[g][i] *= inv * v[i];
+    }
+  }
+  if (PAIRS == kOwn) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float lo = y[0][i], hi = y[1][i];
+      y[0][i] = lo * turn[0].c[i] - hi * turn[0].s[i];
+      y[1][i] = hi * turn[0].c[i] + lo * turn[0].s[i];
+    }
+  } else if (PAIRS == kNeighbours) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      if (8 * (c + 8 * g) >= a.rot) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float lo = y[g][2 * i], hi = y[g][2 * i + 1];
+        y[g][2 * i] = lo * turn[g].c[i] - hi * turn[g].s[i];
+        y[g][2 * i + 1] = hi * turn[g].c[i] + lo * turn[g].s[i];
+      }
+    }
+  } else {
+    const int half = a.rot / 16;  // in chunks
+    float z[2][8];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int n = c + 8 * g, other = n < half ? n + half : n - half;  // any lane for a chunk that is not rotated
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float u = __shfl_sync(0xffffffffu, y[0][i], other & 7, 8), v = __shfl_sync(0xffffffffu, y[1][i], other & 7, 8);
+        z[g][i] = other & 8 ? v : u;
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int n = c + 8 * g;
+      if (n >= 2 * half) continue;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        y[g][i] = n < half ? y[g][i] * turn[g].c[i] - z[g][i] * turn[g].s[i] : y[g][i] * turn[g].c[i] + z[g][i] * turn[g].s[i];
+    }
+  }
+  x[0] = pack(y[0]);
+  x[1] = pack(y[1]);
+}
+
+// One chunk of each group of a row of K or V into the pool.
+template <int FMT>
+__device__ __forceinline__ void store(const Pages& p, char* pool, uint32_t* par, int64_t row, const uint4 (&x)[2], int c) {
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    if (FMT == kBf16) {
+      if (row >= 0 && 8 * (c + 8 * g) < p.dim) *reinterpret_cast<uint4*>(pool + row * p.row_bytes + 16 * (c + 8 * g)) = x[g];
+    } else if (g < p.groups) {  // whole warps
+      const uint4 one[1] = {x[g]};
+      uint32_t w[2];
+      const uint32_t pair = quantise<FMT, 1>(one, w);
+      if (row < 0) continue;
+      uint32_t* to = reinterpret_cast<uint32_t*>(pool + row * p.row_bytes) + g * (FMT == kU8 ? kGroup / 4 : kGroup / 8);
+      if (FMT == kU8) {
+        to[place_u8(2 * c)] = w[0];
+        to[place_u8(2 * c + 1)] = w[1];
+      } else {
+        to[place_u4(c)] = w[0];
+      }
+      if (c == 0) par[row * p.groups + g] = pair;
+    }
+  }
+}
+
+template <int FMT, int PAIRS>
+__global__ void __launch_bounds__(kBlock) rotate_kernel(RotateArgs a) {
+  pdl_trigger();
+  pdl_wait();
+  const int b = blockIdx.y, r = blockIdx.x, c = threadIdx.x & 7;
+  const Seq s = sequence(a.p, b);
+  if (r >= s.n) return;
+  const int64_t row = s.row0 + static_cast<int64_t>(r);
+  const int j = s.len - s.n + r, items = a.q_heads + a.p.heads;
+  Turn turn[2];
+  if (PAIRS == kOwn) {
+    load_turn<8>(a, row, 8 * c, turn[0]);
+  } else {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int n = c + 8 * g, half = a.rot / 16;
+      if (n >= 2 * half) continue;
+      if (PAIRS == kNeighbours)
+        load_turn<4>(a, row, 4 * n, turn[g]);
+      else
+        load_turn<8>(a, row, 8 * (n < half ? n : n - half), turn[g]);
+    }
+  }
+  const int64_t page_row = j < 0 ? -1 : pool_row(a.p, b, j);
+  for (int base = (threadIdx.x >> 5) * 4; base < items; base += kTeams) {  // the same for a whole warp
+    const int item = base + ((threadIdx.x & 31) >> 3), h = item - a.q_heads;
+    const bool in = item < items, q = in && h < 0;
+    const uint16_t* from = q ? a.q + row * a.q_row + item * a.q_head : a.k_new + row * a.row + (in ? h : 0) * a.head;
+    uint4 x[2], v[2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int ch = 8 * (c + 8 * g);
+      x[g] = v[g] = make_uint4(0, 0, 0, 0);
+      if (in && ch < a.p.dim) x[g] = ld_once(from + ch);
+      if (in && !q && ch < a.p.dim) v[g] = ld_once(a.v_new + row * a.row + h * a.head + ch);
+    }
+    // Norms are of all heads of a kind or of none; a warp may have both kinds.
+    const uint16_t* w = q ? a.q_weight : a.k_weight;
+    if (a.q_weight && a.k_weight) {
+      rotate<PAIRS>(a, x, w, turn, c);
+    } else if (!a.q_weight && !a.k_weight) {
+      rotate<PAIRS>(a, x, nullptr, turn, c);
+    } else {
+      uint4 y[2] = {x[0], x[1]};
+      rotate<PAIRS>(a, x, a.q_weight ? a.q_weight : a.k_weight, turn, c);
+      rotate<PAIRS>(a, y, nullptr, turn, c);
+      if (!w) x[0] = y[0], x[1] = y[1];
+    }
+    if (q) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+        if (8 * (c + 8 * g) < a.p.dim) *reinterpret_cast<uint4*>(a.q_out + row * a.out_row + item * a.out_head + 8 * (c + 8 * g)) = x[g];
+    }
+    if (base + 4 > a.q_heads) {
+      const int64_t to = in && !q && page_row >= 0 ? page_row + h * a.p.head_stride : -1;
+      store<FMT>(a.p, a.p.k, a.p.k_par, to, x, c);
+      store<FMT>(a.p, a.p.v, a.p.v_par, to, v, c);
+    }
+  }
+}
+
+template <int FMT>
+cudaError_t launch(const RotateArgs& a, cudaStream_t st) {
+  const dim3 g(static_cast<unsigned>(a.p.max_rows), static_cast<unsigned>(a.p.n_seqs));
+  if (a.neighbours) return launch_next(rotate_kernel<FMT, kNeighbours>, g, kBlock, 0, st, a);
+  if (a.rot == 128) return launch_next(rotate_kernel<FMT, kOwn>, g, kBlock, 0, st, a);
+  return launch_next(rotate_kernel<FMT, kHalves>, g, kBlock, 0, st, a);
+}
+
+}  // namespace
+
+cudaError_t launch_rotate(const RotateArgs& a, cudaStream_t st) {
+  switch (a.p.fmt) {
+    case kBf16: return launch<kBf16>(a, st);
+    case kU8: return launch<kU8>(a, st);
+    default: return launch<kU4>(a, st);
+  }
+}
+
+}  // namespace ipv

@@ -80,6 +80,40 @@ class AttendArgs(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_int64)]
 
 
+class RotaryDesc(ctypes.Structure):
+    """ipv_rotary: a table of cosines and sines."""
+    _fields_ = [("table", ctypes.c_void_p), ("n_positions", ctypes.c_int64), ("rot_dim", ctypes.c_int),
+                ("interleaved", ctypes.c_int), ("n_axes", ctypes.c_int), ("sections", ctypes.c_int * 4)]
+
+
+class RotateArgs(ctypes.Structure):
+    """ipv_rotate_args."""
+    _fields_ = [("q", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("k_new", ctypes.c_void_p), ("v_new", ctypes.c_void_p),
+                ("q_row_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64), ("out_row_stride", ctypes.c_int64),
+                ("out_head_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("n_q_heads", ctypes.c_int), ("eps", ctypes.c_float), ("q_weight", ctypes.c_void_p),
+                ("k_weight", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("positions_stride", ctypes.c_int64)]
+
+
+class BoundsDesc(ctypes.Structure):
+    """ipv_bounds: bounds of the keys of pages."""
+    _fields_ = [("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("n_pages", ctypes.c_int64), ("codes", ctypes.c_void_p), ("steps", ctypes.c_void_p)]
+
+
+class ChooseArgs(ctypes.Structure):
+    """ipv_choose_args."""
+    _fields_ = [("q", ctypes.c_void_p), ("q_row_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+                ("n_q_heads", ctypes.c_int), ("n_chosen", ctypes.c_int), ("first", ctypes.c_int), ("recent", ctypes.c_int),
+                ("out", ctypes.c_void_p), ("out_row_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64)]
+
+
+class Chosen(ctypes.Structure):
+    """ipv_chosen: the pages that each new row attends to."""
+    _fields_ = [("pages", ctypes.c_void_p), ("n_chosen", ctypes.c_int), ("row_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -130,12 +164,21 @@ def load():
         lib.ipv_attend.argtypes = [P, P, P, P]
         lib.ipv_attend_error.argtypes = [ctypes.POINTER(ctypes.c_uint32)]
         lib.ipv_attend_wait_limit.argtypes = [I64]
+        lib.ipv_pages_write_rotated.argtypes = [P, P, P, P, P]
+        lib.ipv_pages_copy.argtypes = [P, P, P, I64, P]
+        lib.ipv_pages_gather.argtypes = [P, P, P, P, P, I64, I64, P]
+        lib.ipv_bounds_update.argtypes = [P, P, P, P]
+        lib.ipv_bounds_choose.argtypes = [P, P, P, P]
+        lib.ipv_attend_chosen_workspace.argtypes = [P, P, P, P, P]
+        lib.ipv_attend_chosen.argtypes = [P, P, P, P, P]
         for name in ("ipv_init", "ipv_compress", "ipv_score", "ipv_select",
                      "ipv_profile_enable", "ipv_profile_collect", "ipv_device_error",
                      "ipv_compress_static", "ipv_van_pool", "ipv_append_frames",
                      "ipv_set_wait_limit", "ipv_pages_write", "ipv_pages_read",
                      "ipv_attend_workspace", "ipv_attend", "ipv_attend_error",
-                     "ipv_attend_wait_limit"):
+                     "ipv_attend_wait_limit", "ipv_pages_write_rotated", "ipv_pages_copy",
+                     "ipv_pages_gather", "ipv_bounds_update", "ipv_bounds_choose",
+                     "ipv_attend_chosen_workspace", "ipv_attend_chosen"):
             getattr(lib, name).restype = I32
         _lib = lib
     return _lib
@@ -281,6 +324,13 @@ def attend_workspace(pages, batch, args: AttendArgs) -> int:
     """Bytes of workspace that ipv_attend needs for these sizes."""
     out = ctypes.c_int64(0)
     _check(load().ipv_attend_workspace(pages, batch, ctypes.byref(args), ctypes.byref(out)))
+    return out.value
+
+
+def attend_chosen_workspace(pages, batch, args: AttendArgs, chosen: Chosen) -> int:
+    """Bytes of workspace that ipv_attend_chosen needs for these sizes."""
+    out = ctypes.c_int64(0)
+    _check(load().ipv_attend_chosen_workspace(pages, batch, ctypes.byref(args), ctypes.byref(chosen), ctypes.byref(out)))
     return out.value
 
 

@@ -4,7 +4,12 @@ A PagedCache holds rows in pages of bf16, or of 8-bit or 4-bit codes with a
 step and a minimum for each 64 channels; a PagedBatch says which pages a set of
 sequences uses and which of their rows are new. `write` puts new rows into
 pages, `read` reads them back, `attend` attends with new rows' queries over
-all the rows that their sequences hold. Everything runs in libipv.so's kernels
+all the rows that their sequences hold. `write_rotated` takes rows as a model's
+projections leave them: norms and position rotation (Rotary) on the way.
+PageBounds keeps bounds of each page's keys, by which `choose` picks the pages
+that a query is to see, and `attend_chosen` attends to those alone.
+`copy_pages` and `gather` move pages and rows; sequences.py keeps the books.
+Everything runs in libipv.so's kernels
 (include/ipv.h, ipv_pages_write and on); this module allocates with PyTorch
 and passes pointers. A half of a PingPongCache is a paged cache as it stands:
 `PagedCache.of_layer`.
@@ -69,6 +74,104 @@ class PagedBatch:
                                 ipv._ptr(kv_len), total_rows, max_rows, max_kv)
         self.ref = ctypes.byref(self.struct)
         self.sizes = (n, self.max_pages, total_rows, max_rows, max_kv)
+
+
+class Rotary:
+    """Position rotation (ipv_rotary). table: fp32 [n_positions, rot_dim], a
+    position's rot_dim / 2 cosines and then its sines. Frequency f turns channels
+    f and f + rot_dim / 2, or 2f and 2f + 1 if interleaved. sections: how many
+    frequencies go by each axis of the positions (multiples of 8); one axis if
+    None."""
+
+    def __init__(self, table: torch.Tensor, sections=None, interleaved: bool = False):
+        _need(table.dim() == 2 and table.dtype is torch.float32 and table.is_cuda and table.is_contiguous(),
+              "table must be a contiguous fp32 CUDA tensor [n_positions, rot_dim]")
+        sections = [table.shape[1] // 2] if sections is None else [int(n) for n in sections]
+        _need(1 <= len(sections) <= 4, "positions have 1 to 4 axes")
+        _fits(32, **{f"section {i}": n for i, n in enumerate(sections)})
+        self.table, self.sections, self.interleaved = table, sections, bool(interleaved)
+        self.struct = ipv.RotaryDesc(table.data_ptr(), table.shape[0], table.shape[1], int(self.interleaved), len(sections),
+                                     (ctypes.c_int * 4)(*sections))
+        self.ref = ctypes.byref(self.struct)
+
+    @classmethod
+    def of_base(cls, base: float, n_positions: int, rot_dim: int, sections=None, interleaved: bool = False,
+                device="cuda") -> "Rotary":
+        """Angles position * base^(-2f / rot_dim), taken in 64 bits."""
+        f = torch.arange(rot_dim // 2, dtype=torch.float64, device=device)
+        angle = torch.arange(n_positions, dtype=torch.float64, device=device)[:, None] * base ** (-2.0 * f / rot_dim)
+        return cls(torch.cat([angle.cos(), angle.sin()], 1).float(), sections, interleaved)
+
+
+class PageBounds:
+    """Bounds of the keys of a pool's pages (ipv_bounds): codes int8 [n_pages,
+    n_kv_heads, 2 (lower, upper), 64 or 128], steps fp32 [n_pages, n_kv_heads]. They say
+    nothing of a page before `update` has seen it; copy_pages and gather leave them to the next update."""
+
+    def __init__(self, cache: "PagedCache"):
+        padded = 64 if cache.head_dim <= 64 else 128
+        codes = torch.zeros((cache.n_pages, cache.n_kv_heads, 2, padded), dtype=torch.int8, device=cache.k.device)
+        self._set(codes, torch.zeros((cache.n_pages, cache.n_kv_heads), device=cache.k.device), cache.page_size, cache.head_dim)
+
+    @classmethod
+    def from_tensors(cls, codes: torch.Tensor, steps: torch.Tensor, page_size: int, head_dim: int) -> "PageBounds":
+        """Bounds over contiguous tensors that the caller keeps."""
+        self = cls.__new__(cls)
+        self._set(codes, steps, page_size, head_dim)
+        return self
+
+    def _set(self, codes, steps, page_size, head_dim):
+        padded = 64 if head_dim <= 64 else 128
+        _need(codes.dim() == 4 and codes.shape[2:] == (2, padded) and codes.dtype is torch.int8 and codes.is_cuda and codes.is_contiguous(),
+              f"codes must be a contiguous int8 CUDA tensor [n_pages, n_kv_heads, 2, {padded}]")
+        _need(steps.shape == codes.shape[:2] and steps.dtype is torch.float32 and steps.is_cuda and steps.is_contiguous(),
+              "steps must be a contiguous fp32 CUDA tensor [n_pages, n_kv_heads]")
+        _fits(32, page_size=page_size, head_dim=head_dim)
+        self.codes, self.steps, self.page_size, self.head_dim = codes, steps, page_size, head_dim
+        self.n_pages, self.n_kv_heads = codes.shape[:2]
+        self.struct = ipv.BoundsDesc(self.n_kv_heads, head_dim, page_size, self.n_pages, codes.data_ptr(), steps.data_ptr())
+        self.ref = ctypes.byref(self.struct)
+        self._args, self._lib = ipv.ChooseArgs(), ipv.load()
+        self._args_ref = ctypes.byref(self._args)
+
+    def update(self, cache: "PagedCache", batch: PagedBatch, stream=None) -> None:
+        """ipv_bounds_update: the bounds of the pages that hold the batch's new rows, after these were written."""
+        status = self._lib.ipv_bounds_update(self.ref, cache.ref, batch.ref, ipv._stream(stream))
+        if status:
+            ipv._check(status)
+
+    def choose(self, q, batch: PagedBatch, n_chosen: int, *, first: int = 1, recent: int = 1, out=None, stream=None):
+        """ipv_bounds_choose: for each new row and KV head the n_chosen pages of its sequence (columns of the table)
+        that attend_chosen is to read: the first `first`, the last `recent` and those whose bounds promise the largest
+        products with q, bf16 [total_rows, n_q_heads, head_dim]. int32 [total_rows, n_kv_heads, n_chosen], ascending,
+        then -1; allocated if out is None, with -1 where a row belongs to no sequence. One host thread at a time
+        uses the object."""
+        n_q_heads = q.shape[1] if q.dim() == 3 else 0
+        qs = PagedCache._packed("q", q, batch, n_q_heads, self.head_dim)
+        _fits(32, n_chosen=n_chosen, first=first, recent=recent)
+        at = ipv._stream(stream)
+        if out is None:
+            _need(n_chosen >= 1, "n_chosen must be positive")
+            out, = PagedCache._results(q, [(batch.total_rows, self.n_kv_heads, n_chosen)], stream, at, torch.int32, -1)
+        os = _lists("out", out, batch, self.n_kv_heads, n_chosen)
+        a = self._args
+        a.q, a.q_row_stride, a.q_head_stride, a.n_q_heads = q.data_ptr(), qs[0], qs[1], n_q_heads
+        a.n_chosen, a.first, a.recent = n_chosen, first, recent
+        a.out, a.out_row_stride, a.out_head_stride = out.data_ptr(), os[0], os[1]
+        status = self._lib.ipv_bounds_choose(self.ref, batch.ref, self._args_ref, at)
+        if status:
+            ipv._check(status)
+        return out
+
+
+def _lists(name, t, batch, heads, n=None):
+    """Strides of int32 [total_rows, heads, n] lists."""
+    shape, strides = t.shape, t.stride()
+    if (t.dtype is not torch.int32 or not t.is_cuda or len(shape) != 3 or shape[0] < batch.total_rows or shape[1] != heads or
+            (n is not None and shape[2] != n) or (strides[2] != 1 and shape[2] > 1)):
+        raise ValueError(f"{name} must be an int32 CUDA tensor [{batch.total_rows}, {heads}, {'n' if n is None else n}], contiguous "
+                         "along its last dimension")
+    return strides
 
 
 class PagedCache:
@@ -136,6 +239,8 @@ class PagedCache:
                                     k.data_ptr(), v.data_ptr(), ipv._ptr(k_par), ipv._ptr(v_par))
         self.ref = ctypes.byref(self.struct)
         self._workspaces, self._calls, self._lib = {}, {}, ipv.load()
+        self._rotate_args = ipv.RotateArgs()
+        self._rotate_ref = ctypes.byref(self._rotate_args)
 
     @staticmethod
     def _row_strides(t, width):
@@ -163,14 +268,15 @@ class PagedCache:
         return strides
 
     @staticmethod
-    def _results(like, shapes, stream, at):
-        """New zeroed bf16 tensors for a call on stream `at`. Made on that stream: the fill comes before the kernel, and
+    def _results(like, shapes, stream, at, dtype=torch.bfloat16, fill=0):
+        """New tensors, filled (zeroed), for a call on stream `at`. Made on that stream: the fill comes before the kernel, and
         the memory belongs to it; the current stream may use them as well."""
+        make = lambda shape: like.new_full(shape, fill, dtype=dtype) if fill else like.new_zeros(shape, dtype=dtype)  # noqa: E731
         if stream is None or at == ipv._stream(None):
-            return [like.new_zeros(shape, dtype=torch.bfloat16) for shape in shapes]
+            return [make(shape) for shape in shapes]
         here = torch.cuda.current_stream()
         with torch.cuda.stream(torch.cuda.ExternalStream(at)):
-            out = [like.new_zeros(shape, dtype=torch.bfloat16) for shape in shapes]
+            out = [make(shape) for shape in shapes]
         for t in out:
             t.record_stream(here)
         return out
@@ -216,9 +322,7 @@ class PagedCache:
             out, = self._results(q, [q.shape], stream, at)
         os = self._packed("out", out, batch, n_q_heads, self.head_dim)
         if lse is not None:
-            _need(lse.dtype is torch.float32 and lse.is_cuda and lse.is_contiguous() and lse.dim() == 2 and
-                  lse.shape[0] >= batch.total_rows and lse.shape[1] == n_q_heads,
-                  "lse must be a contiguous fp32 CUDA tensor [total_rows, n_q_heads]")
+            self._check_lse(lse, batch, n_q_heads)
         # Arguments and workspace need are kept for each set of sizes that they depend on.
         sizes = (batch.sizes, n_q_heads, causal, window, sinks)
         kept = self._calls.get(sizes)
@@ -229,30 +333,138 @@ class PagedCache:
         args.q_row_stride, args.q_head_stride, args.out_row_stride, args.out_head_stride = qs[0], qs[1], os[0], os[1]
         args.scale = self.head_dim ** -0.5 if scale is None else scale
         if need:
-            if workspace is None:
-                _need(stream is None or at == ipv._stream(None), "a stream that is not the current one needs a workspace")
-                if torch.cuda.is_current_stream_capturing():
-                    # From the graph's own memory, which lives as long as the graph: a kept one would be shared with
-                    # other graphs and calls, and freed when a later call needs a larger one.
-                    workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-                else:
-                    workspace = self._workspaces.get(at)
-                    if workspace is None or workspace.numel() < need:
-                        workspace = self._workspaces[at] = torch.empty(need, dtype=torch.uint8, device=q.device)
-            elif not (workspace.is_cuda and workspace.dtype is torch.uint8 and workspace.is_contiguous()):
-                raise ValueError("workspace must be a contiguous uint8 CUDA tensor")
-            args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel()
+            self._give_workspace(args, need, workspace, stream, at, q.device)
         status = self._lib.ipv_attend(self.ref, batch.ref, ref, at)
         if status:
             ipv._check(status)
         return out
+
+    def _give_workspace(self, args, need, workspace, stream, at, device):
+        if workspace is None:
+            _need(stream is None or at == ipv._stream(None), "a stream that is not the current one needs a workspace")
+            if torch.cuda.is_current_stream_capturing():
+                # From the graph's own memory, which lives as long as the graph: a kept one would be shared with
+                # other graphs and calls, and freed when a later call needs a larger one.
+                workspace = torch.empty(need, dtype=torch.uint8, device=device)
+            else:
+                workspace = self._workspaces.get(at)
+                if workspace is None or workspace.numel() < need:
+                    workspace = self._workspaces[at] = torch.empty(need, dtype=torch.uint8, device=device)
+        elif not (workspace.is_cuda and workspace.dtype is torch.uint8 and workspace.is_contiguous()):
+            raise ValueError("workspace must be a contiguous uint8 CUDA tensor")
+        args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel()
+
+    def attend_chosen(self, q, batch: PagedBatch, chosen, *, out=None, lse=None, scale: float | None = None, workspace=None, stream=None):
+        """ipv_attend_chosen: attention of each new row over the rows that it sees of its own pages alone. chosen:
+        int32 [total_rows, n_kv_heads, n], columns of the batch's table, as PageBounds.choose gives them (a list
+        shorter than the row's pages; entries that are none of them, -1 say, are skipped). q, out, lse, workspace and
+        captured calls as in attend."""
+        n_q_heads = q.shape[1] if q.dim() == 3 else 0
+        qs = self._packed("q", q, batch, n_q_heads, self.head_dim)
+        cs = _lists("chosen", chosen, batch, self.n_kv_heads)
+        at = ipv._stream(stream)
+        if out is None:
+            out, = self._results(q, [q.shape], stream, at)
+        os = self._packed("out", out, batch, n_q_heads, self.head_dim)
+        if lse is not None:
+            self._check_lse(lse, batch, n_q_heads)
+        sizes = (batch.sizes, n_q_heads, chosen.shape[2])
+        kept = self._calls.get(sizes)
+        if kept is None:
+            _fits(32, n_chosen=chosen.shape[2])
+            args = ipv.AttendArgs(n_q_heads=n_q_heads, scale=1.0, causal=1)
+            lists = ipv.Chosen(n_chosen=chosen.shape[2])
+            kept = args, ctypes.byref(args), lists, ctypes.byref(lists), ipv.attend_chosen_workspace(self.ref, batch.ref, args, lists)
+            self._keep_call(sizes, kept)
+        args, ref, lists, lists_ref, need = kept
+        args.q, args.out, args.lse = q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr()
+        args.q_row_stride, args.q_head_stride, args.out_row_stride, args.out_head_stride = qs[0], qs[1], os[0], os[1]
+        args.scale = self.head_dim ** -0.5 if scale is None else scale
+        lists.pages, lists.row_stride, lists.head_stride = chosen.data_ptr(), cs[0], cs[1]
+        if need:
+            self._give_workspace(args, need, workspace, stream, at, q.device)
+        status = self._lib.ipv_attend_chosen(self.ref, batch.ref, ref, lists_ref, at)
+        if status:
+            ipv._check(status)
+        return out
+
+    @staticmethod
+    def _check_lse(lse, batch, n_q_heads):
+        _need(lse.dtype is torch.float32 and lse.is_cuda and lse.is_contiguous() and lse.dim() == 2 and
+              lse.shape[0] >= batch.total_rows and lse.shape[1] == n_q_heads,
+              "lse must be a contiguous fp32 CUDA tensor [total_rows, n_q_heads]")
+
+    def write_rotated(self, q, k_new, v_new, batch: PagedBatch, rotary: Rotary, positions, *, q_weight=None, k_weight=None,
+                      eps: float = 1e-6, q_out=None, stream=None):
+        """ipv_pages_write_rotated: k_new (normalised with k_weight if given, rotated) and v_new into the batch's pages,
+        and q, bf16 [total_rows, n_q_heads, head_dim], normalised with q_weight if given and rotated, into q_out
+        (allocated if None, on the call's stream; q itself will do), which is returned. positions: int32
+        [total_rows] or [axes, total_rows], places in the rotary's table: a row's place in the stream, which a
+        compacted cache does not tell. weights: bf16 [head_dim]. One host thread at a time uses a cache object."""
+        n_q_heads = q.shape[1] if q.dim() == 3 else 0
+        qs = self._packed("q", q, batch, n_q_heads, self.head_dim)
+        strides = self._pair("k_new", k_new, "v_new", v_new, batch)
+        axes = len(rotary.sections)
+        if positions.dim() == 1 and axes == 1:
+            positions = positions[None]
+        if (positions.dtype is not torch.int32 or not positions.is_cuda or positions.dim() != 2 or positions.shape[0] != axes or
+                positions.shape[1] < batch.total_rows or (positions.stride(1) != 1 and positions.shape[1] > 1)):
+            raise ValueError(f"positions must be an int32 CUDA tensor [{axes}, {batch.total_rows}], contiguous along its last dimension")
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is not None and (w.dtype is not torch.bfloat16 or not w.is_cuda or w.shape != (self.head_dim,) or not w.is_contiguous()):
+                raise ValueError(f"{name} must be a contiguous bf16 CUDA tensor [{self.head_dim}]")
+        at = ipv._stream(stream)
+        if q_out is None:
+            q_out, = self._results(q, [q.shape], stream, at)
+        os = self._packed("q_out", q_out, batch, n_q_heads, self.head_dim)
+        a = self._rotate_args
+        a.q, a.q_out, a.k_new, a.v_new = q.data_ptr(), q_out.data_ptr(), k_new.data_ptr(), v_new.data_ptr()
+        a.q_row_stride, a.q_head_stride, a.out_row_stride, a.out_head_stride = qs[0], qs[1], os[0], os[1]
+        a.row_stride, a.head_stride, a.n_q_heads, a.eps = strides[0], strides[1], n_q_heads, eps
+        a.q_weight, a.k_weight = ipv._ptr(q_weight), ipv._ptr(k_weight)
+        a.positions, a.positions_stride = positions.data_ptr(), positions.stride(0)
+        status = self._lib.ipv_pages_write_rotated(self.ref, batch.ref, rotary.ref, self._rotate_ref, at)
+        if status:
+            ipv._check(status)
+        return q_out
+
+    def copy_pages(self, source, target, stream=None) -> None:
+        """ipv_pages_copy: page target[i] becomes a copy of page source[i], int32 CUDA tensors [n]. No page is in target
+        twice, or in target and at another place in source."""
+        for name, t in (("source", source), ("target", target)):
+            _need(t.dtype is torch.int32 and t.is_cuda and t.dim() == 1 and (t.stride(0) == 1 or t.shape[0] <= 1),
+                  f"{name} must be a contiguous int32 CUDA tensor [n]")
+        _need(source.shape == target.shape, "source and target must have one length")
+        status = self._lib.ipv_pages_copy(self.ref, source.data_ptr(), target.data_ptr(), source.shape[0], ipv._stream(stream))
+        if status:
+            ipv._check(status)
+
+    def gather(self, source: "PagedCache", source_batch: PagedBatch, batch: PagedBatch, kept=None, stream=None) -> None:
+        """ipv_pages_gather: new row i of sequence b of `batch`, for KV head h, becomes row kept[b, h, i] of sequence b of
+        source_batch in the cache `source` (which may be this one), as it is held; row i without kept. kept: int32
+        [n_seqs, n_kv_heads, >= max_rows], indices of ipv.select, say. Pages that are written may not be among those that
+        are read."""
+        kept_strides = (0, 0)
+        if kept is not None:
+            _need(kept.dtype is torch.int32 and kept.is_cuda and kept.dim() == 3 and kept.shape[0] >= batch.n_seqs and
+                  kept.shape[1] == self.n_kv_heads and kept.shape[2] >= min(batch.max_rows, batch.total_rows) and
+                  (kept.stride(2) == 1 or kept.shape[2] <= 1),
+                  "kept must be an int32 CUDA tensor [n_seqs, n_kv_heads, max_rows], contiguous along its last dimension")
+            kept_strides = kept.stride()[:2]
+        status = self._lib.ipv_pages_gather(source.ref, source_batch.ref, self.ref, batch.ref, ipv._ptr(kept), kept_strides[0],
+                                            kept_strides[1], ipv._stream(stream))
+        if status:
+            ipv._check(status)
 
     def _first_call(self, batch, sizes):
         _, n_q_heads, causal, window, sinks = sizes
         _fits(32, window=window, sinks=sinks)
         args = ipv.AttendArgs(n_q_heads=n_q_heads, scale=1.0, causal=int(causal), window=window, sinks=sinks)
         kept = args, ctypes.byref(args), ipv.attend_workspace(self.ref, batch.ref, args)
+        self._keep_call(sizes, kept)
+        return kept
+
+    def _keep_call(self, sizes, kept):
         if len(self._calls) >= 1024:
             self._calls.clear()
         self._calls[sizes] = kept
-        return kept
