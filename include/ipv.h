@@ -541,7 +541,8 @@ ipv_status ipv_pages_copy(const ipv_pages* pages, const int32_t* from, const int
 /* Gathers rows of one cache into another, as they are held: new row i of
  * sequence b of `batch`, KV head h, becomes row kept[b * kept_seq_stride +
  * h * kept_head_stride + i] of sequence b in `source` (row i if kept is NULL), of which only
- * the table and kv_len are read. Formats, n_kv_heads and head_dim are the same in both, and so is
+ * the table and kv_len are read. A list has min(max_rows, total_rows) entries, whatever its
+ * sequence needs of them; an index may come several times. Formats, n_kv_heads and head_dim are the same in both, and so is
  * n_seqs. A row that the source sequence does not hold reads as zero. The rows written may not
  * lie in pages that the call reads. With the kept indices of ipv_select this is the pass's
  * compaction, of a cache in pages. Errors: IPV_EINVAL, IPV_ECUDA. */

@@ -32,9 +32,25 @@ __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {  // NaN
 // A block takes a page of one head: teams of 16 lanes, lane c the 8 channels from 8c on.
 constexpr int kBoundsThreads = 128;
 constexpr int kBoundsTeams = kBoundsThreads / 16;
+constexpr int kBoundsAtOnce = 8;  // rows that a lane has on their way
+
+// 8 channels of a row as they are held: bf16 in x; codes in x.x (and x.y at 8 bits), their pair in x.z.
+template <int FMT>
+__device__ __forceinline__ void load_keys(const Pages& p, int64_t row, int c, uint4& x) {
+  if (FMT == kBf16) {
+    x = ld_once(p.k + row * p.row_bytes + 16 * c);
+  } else {
+    const uint32_t* kd = reinterpret_cast<const uint32_t*>(p.k + row * p.row_bytes) + (c >> 3) * (FMT == kU8 ? kGroup / 4 : kGroup / 8);
+    if (FMT == kU8)
+      x.x = kd[place_u8(2 * (c & 7))], x.y = kd[place_u8(2 * (c & 7) + 1)];
+    else
+      x.x = kd[place_u4(c & 7)];
+    x.z = p.k_par[row * p.groups + (c >> 3)];
+  }
+}
 
 template <int FMT>
-__global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(BoundsArgs a) {
+__global__ void __launch_bounds__(kBoundsThreads, FMT == kBf16 ? 8 : 4) bounds_kernel(BoundsArgs a) {
   __shared__ uint4 ends[2][kBoundsThreads / 32][16];
   pdl_trigger();
   pdl_wait();
@@ -43,44 +59,40 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(BoundsArgs a) {
   if (s.n == 0 || s.len == 0) return;
   const int shift = a.p.page_shift, page0 = max(0, s.len - s.n) >> shift, i = page0 + static_cast<int>(blockIdx.x);
   if (i > (s.len - 1) >> shift) return;
-  const int g = a.p.table ? a.p.table[b * a.p.table_stride + i] : b;
-  if (static_cast<unsigned>(g) >= static_cast<unsigned>(a.p.n_pages)) return;
+  const int pg = a.p.table ? a.p.table[b * a.p.table_stride + i] : b;
+  if (static_cast<unsigned>(pg) >= static_cast<unsigned>(a.p.n_pages)) return;
   const int rows = shift == 31 ? s.len : min(a.p.page_size, s.len - (i << shift));
-  const int64_t row0 = g * a.p.page_stride + h * a.p.head_stride;
+  const int64_t row0 = pg * a.p.page_stride + h * a.p.head_stride;
+  const bool in = 8 * c < a.p.dim;
   uint32_t lo[4], hi[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) lo[k] = 0x7F807F80u, hi[k] = 0xFF80FF80u;
-  const bool in = 8 * c < a.p.dim;
-  constexpr int kAtOnce = 8;
-  for (int r0 = threadIdx.x >> 4; r0 < rows; r0 += kBoundsTeams * kAtOnce) {
-    uint4 x[kAtOnce];
+  uint4 x[kBoundsAtOnce];
+  auto load = [&](int r0) {
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) {
+    for (int u = 0; u < kBoundsAtOnce; ++u) {
       const int r = r0 + u * kBoundsTeams;
-      if (!in || r >= rows) continue;
-      const int64_t row = row0 + r * a.p.row_stride;
-      if (FMT == kBf16) {
-        x[u] = ld_once(a.p.k + row * a.p.row_bytes + 16 * c);
-      } else {
-        const uint32_t* kd = reinterpret_cast<const uint32_t*>(a.p.k + row * a.p.row_bytes) + (c >> 3) * (FMT == kU8 ? kGroup / 4 : kGroup / 8);
-        if (FMT == kU8)
-          x[u].x = kd[place_u8(2 * (c & 7))], x[u].y = kd[place_u8(2 * (c & 7) + 1)];
-        else
-          x[u].x = kd[place_u4(c & 7)];
-        x[u].z = a.p.k_par[row * a.p.groups + (c >> 3)];
-      }
+      if (in && r < rows) load_keys<FMT>(a.p, row0 + r * a.p.row_stride, c, x[u]);
     }
+  };
+  const int team = threadIdx.x >> 4;
+  load(team);
+  for (int r0 = team;; r0 += kBoundsTeams * kBoundsAtOnce) {
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) {
+    for (int u = 0; u < kBoundsAtOnce; ++u) {
       if (!in || r0 + u * kBoundsTeams >= rows) continue;
+      uint4 y = x[u];
       if (FMT != kBf16) {
         const uint32_t w[2] = {x[u].x, x[u].y};
-        x[u] = expand<FMT, false>(w, x[u].z);
+        y = expand<FMT, false>(w, x[u].z);
       }
-      const uint32_t xs[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+      const uint32_t ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) lo[k] = min_bf16x2(lo[k], xs[k]), hi[k] = max_bf16x2(hi[k], xs[k]);
+      for (int k = 0; k < 4; ++k) lo[k] = min_bf16x2(lo[k], ys[k]), hi[k] = max_bf16x2(hi[k], ys[k]);
     }
+    const int more = r0 + kBoundsTeams * kBoundsAtOnce;
+    if (more - team >= rows) break;  // the same for the block
+    load(more);
   }
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -92,20 +104,19 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(BoundsArgs a) {
     ends[1][warp][c] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
   }
   __syncthreads();
-  if (threadIdx.x >= 16) return;
+  if (warp > 0) return;
 #pragma unroll
   for (int w = 1; w < kBoundsThreads / 32; ++w) {
-    const uint4 x = ends[0][w][c], y = ends[1][w][c];
-    lo[0] = min_bf16x2(lo[0], x.x), lo[1] = min_bf16x2(lo[1], x.y), lo[2] = min_bf16x2(lo[2], x.z), lo[3] = min_bf16x2(lo[3], x.w);
-    hi[0] = max_bf16x2(hi[0], y.x), hi[1] = max_bf16x2(hi[1], y.y), hi[2] = max_bf16x2(hi[2], y.z), hi[3] = max_bf16x2(hi[3], y.w);
+    const uint4 y = ends[0][w][c], z = ends[1][w][c];
+    lo[0] = min_bf16x2(lo[0], y.x), lo[1] = min_bf16x2(lo[1], y.y), lo[2] = min_bf16x2(lo[2], y.z), lo[3] = min_bf16x2(lo[3], y.w);
+    hi[0] = max_bf16x2(hi[0], z.x), hi[1] = max_bf16x2(hi[1], z.y), hi[2] = max_bf16x2(hi[2], z.z), hi[3] = max_bf16x2(hi[3], z.w);
   }
   uint32_t top = 0;
   if (in)
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       top = max(max(max(top, lo[k] & 0x7FFFu), max((lo[k] >> 16) & 0x7FFFu, hi[k] & 0x7FFFu)), (hi[k] >> 16) & 0x7FFFu);
-#pragma unroll
-  for (int d = 1; d < 16; d <<= 1) top = max(top, __shfl_xor_sync(0xffffu, top, d));
+  top = __reduce_max_sync(0xffffffffu, top);
   const bool finite = top < 0x7F80u;
   const int e = finite ? exponent_of(top) : 0;
   const float down = pow2(-e);
@@ -113,19 +124,19 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(BoundsArgs a) {
   if (in && finite)
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const float x = k & 1 ? hi_f(lo[k >> 1]) : lo_f(lo[k >> 1]), y = k & 1 ? hi_f(hi[k >> 1]) : lo_f(hi[k >> 1]);
+      const float y = k & 1 ? hi_f(lo[k >> 1]) : lo_f(lo[k >> 1]), z = k & 1 ? hi_f(hi[k >> 1]) : lo_f(hi[k >> 1]);
       // A product too small for fp32 still lies on its side of 0.
-      const int below = min(static_cast<int>(floorf(x * down)), x < 0.0f ? -1 : 127), above = max(static_cast<int>(ceilf(y * down)), y > 0.0f ? 1 : -127);
+      const int below = min(static_cast<int>(floorf(y * down)), y < 0.0f ? -1 : 127), above = max(static_cast<int>(ceilf(z * down)), z > 0.0f ? 1 : -127);
       w[0][k >> 2] |= (static_cast<uint32_t>(below) & 0xFFu) << (8 * (k & 3));
       w[1][k >> 2] |= (static_cast<uint32_t>(above) & 0xFFu) << (8 * (k & 3));
     }
-  const int64_t at = static_cast<int64_t>(g) * a.p.heads + h;
-  if (8 * c < a.padded) {
+  const int64_t at = static_cast<int64_t>(pg) * a.p.heads + h;
+  if (lane < 16 && 8 * c < a.padded) {
     char* out = a.codes + at * 2 * a.padded + 8 * c;
     *reinterpret_cast<uint2*>(out) = make_uint2(w[0][0], w[0][1]);
     *reinterpret_cast<uint2*>(out + a.padded) = make_uint2(w[1][0], w[1][1]);
   }
-  if (c == 0) a.steps[at] = finite ? pow2(e) : __uint_as_float(0x7FC00000u);
+  if (lane == 0) a.steps[at] = finite ? pow2(e) : __uint_as_float(0x7FC00000u);
 }
 
 // ------------------------------------------------------------------ the choice
@@ -182,39 +193,56 @@ __device__ __forceinline__ int before_me(int x, int* scratch, int& all) {
   return before;
 }
 
+// How many of keys[from..upto) are above k; unrolled, for latency.
+__device__ __forceinline__ int count_above(const uint32_t* keys, int from, int upto, uint32_t k) {
+  int n = 0;
+#pragma unroll 8
+  for (int i = from; i < upto; ++i) n += keys[i] > k;
+  return n;
+}
+
 // Of keys[first..end) the `need` largest, ties to the lower index, get the key
-// 0xFFFFFFFF, and the others keep theirs, all below *least. 0 < need < end - first.
-// Rounds of a histogram over equal ranges of keys narrow [lo, hi] to the range in which
-// the last chosen key lies until a block can rank what is in it, or it is one key: every
-// round leaves 1/256 of the range, so there are 4 at most.
-__device__ void mark_largest(uint32_t* keys, int first, int end, int need, int* bins, uint32_t* cand, int* scratch, uint32_t* least) {
+// 0xFFFFFFFF; the others keep theirs. Returns what the chosen keys are above. 0 < need < end - first.
+// Up to a key per thread each is ranked among all. Else rounds of a histogram over equal ranges
+// of keys narrow [lo, hi] to the range in which the last chosen key lies until a thread
+// can rank each that is in it, or it is one key: every round leaves 1/256 of the range, so
+// there are 4 at most.
+__device__ uint32_t mark_largest(uint32_t* keys, int first, int end, int need, int* bins, uint32_t* cand, int* scratch) {
+  int inside = end - first;
+  if (inside <= kChooseThreads) {
+    const int p = first + static_cast<int>(threadIdx.x);
+    const uint32_t k = p < end ? keys[p] : 0u;
+    // Equal keys before p come first: there, above k - 1 (k = 0: all).
+    const int before = p < end ? (k ? count_above(keys, first, p, k - 1) : p - first) + count_above(keys, p + 1, end, k) : need;
+    __syncthreads();
+    if (before < need) keys[p] = 0xFFFFFFFFu;
+    __syncthreads();
+    return 0xFFFFFFFEu;
+  }
   uint32_t lo = 0xFFFFFFFFu, hi = 0;
   for (int p = first + threadIdx.x; p < end; p += kChooseThreads) lo = min(lo, keys[p]), hi = max(hi, keys[p]);
   lo = __reduce_min_sync(0xffffffffu, lo);
   hi = __reduce_max_sync(0xffffffffu, hi);
-  if ((threadIdx.x & 31) == 0) bins[threadIdx.x >> 5] = static_cast<int>(lo), bins[kWarps + (threadIdx.x >> 5)] = static_cast<int>(hi);
+  if ((threadIdx.x & 31) == 0) cand[threadIdx.x >> 5] = lo, cand[kWarps + (threadIdx.x >> 5)] = hi;
+  bins[threadIdx.x] = 0;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) lo = min(lo, static_cast<uint32_t>(bins[w])), hi = max(hi, static_cast<uint32_t>(bins[kWarps + w]));
-  int inside = end - first;  // keys in lo..hi; `need` of them are wanted, and all above hi
-  while (inside > kChooseThreads && lo < hi) {
-    int shift = 0;  // bins of 2^shift keys
-    while (((hi - lo) >> shift) >= kBins) ++shift;
-    __syncthreads();
-    bins[threadIdx.x] = 0;
-    __syncthreads();
+  for (int w = 0; w < kWarps; ++w) lo = min(lo, cand[w]), hi = max(hi, cand[kWarps + w]);
+  while (inside > kChooseThreads && lo < hi) {  // bins are clear; `need` of the `inside` keys in lo..hi are wanted, and all above
+    const int shift = max(0, 24 - __clz(hi - lo));  // bins of 2^shift keys, 256 of them reach
     for (int p = first + threadIdx.x; p < end; p += kChooseThreads) {
       const uint32_t k = keys[p];
       if (k >= lo && k <= hi) atomicAdd(bins + ((hi - k) >> shift), 1);  // bin 0 has the largest
     }
     __syncthreads();
     const int mine = bins[threadIdx.x];
+    bins[threadIdx.x] = 0;
     int all;
     const int above = before_me(mine, scratch, all);
     if (above < need && above + mine >= need) {
-      const uint32_t top = hi - (static_cast<uint32_t>(threadIdx.x) << shift);
+      const uint32_t top = hi - (static_cast<uint32_t>(threadIdx.x) << shift), width = (1u << shift) - 1;
       cand[0] = top;
-      cand[1] = top - lo < (1u << shift) ? lo : top - ((1u << shift) - 1);
+      cand[1] = top - lo < width ? lo : top - width;
       cand[2] = static_cast<uint32_t>(need - above);
       cand[3] = static_cast<uint32_t>(mine);
     }
@@ -222,21 +250,23 @@ __device__ void mark_largest(uint32_t* keys, int first, int end, int need, int* 
     hi = cand[0], lo = cand[1], need = static_cast<int>(cand[2]), inside = static_cast<int>(cand[3]);
     __syncthreads();
   }
-  if (inside <= kChooseThreads) {  // few keys: each is ranked among them
+  if (inside <= kChooseThreads) {
     if (threadIdx.x == 0) scratch[kWarps] = 0;
     __syncthreads();
+    uint32_t* index = cand + kChooseThreads;
     for (int p = first + threadIdx.x; p < end; p += kChooseThreads) {
       const uint32_t k = keys[p];
       if (k >= lo && k <= hi) {
-        const int at = atomicAdd(scratch + kWarps, 1);
-        cand[2 * at] = k, cand[2 * at + 1] = static_cast<uint32_t>(p);
+        const int at = atomicAdd(scratch + kWarps, 1);  // in any order: ranks go by key and index
+        cand[at] = k, index[at] = static_cast<uint32_t>(p);
       }
     }
     __syncthreads();
     if (static_cast<int>(threadIdx.x) < inside) {
-      const uint32_t k = cand[2 * threadIdx.x], p = cand[2 * threadIdx.x + 1];
+      const uint32_t k = cand[threadIdx.x], p = index[threadIdx.x];
       int before = 0;
-      for (int i = 0; i < inside; ++i) before += cand[2 * i] > k || (cand[2 * i] == k && cand[2 * i + 1] < p);
+#pragma unroll 4
+      for (int i = 0; i < inside; ++i) before += cand[i] > k || (cand[i] == k && index[i] < p);
       if (before < need) keys[p] = 0xFFFFFFFFu;
     }
   } else {  // more equal keys than threads: the first `need` of them, in order
@@ -249,14 +279,14 @@ __device__ void mark_largest(uint32_t* keys, int first, int end, int need, int* 
       need -= all;
     }
   }
-  *least = hi;  // chosen keys are above it
   __syncthreads();
+  return hi;
 }
 
 // A cluster takes one new row and KV head: its blocks score the pages, 16 at a time
 // per warp, into the first block's shared memory; that block chooses.
 template <int DP>
-__global__ void __launch_bounds__(kChooseThreads) choose_kernel(ChooseArgs a) {
+__global__ void __launch_bounds__(kChooseThreads, 2) choose_kernel(ChooseArgs a) {
   constexpr int kCodes = 2 * DP;              // bytes of a page's bounds, and of a query head's parts
   constexpr int kVectors = kCodes / 64;       // 16-byte vectors of a row per thread of a quad
   extern __shared__ __align__(16) unsigned char smem[];
@@ -271,6 +301,17 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(ChooseArgs a) {
   if (a.cluster > 1) cluster_arrive();  // all of them are there before one writes to another
   pdl_trigger();
   pdl_wait();
+  // A warp's tiles of 16 pages, and lane i < 16 of it page i's place in the pool: looked up a tile ahead, the first
+  // before the sequence's length is known.
+  const int stride = a.cluster * kWarps * 16;
+  auto look_up = [&](int p0) {
+    const int p = p0 + lane;
+    int pg = -1;
+    if (lane < 16 && p < a.max_pages) pg = a.p.table ? a.p.table[b * a.p.table_stride + p] : b;
+    return static_cast<unsigned>(pg) < static_cast<unsigned>(a.p.n_pages) ? pg : -1;
+  };
+  int p0 = (rank * kWarps + warp) * 16;
+  int pg = look_up(p0);
   const Seq s = sequence(a.p, b);
   const bool there = token < s.n;
   const int pos = s.len - s.n + token;
@@ -278,7 +319,32 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(ChooseArgs a) {
   const int64_t row = s.row0 + static_cast<int64_t>(token);
   int32_t* out = a.out + row * a.out_row + h * a.out_head;
   const bool all = pages <= a.n;  // nothing to choose
+  const float none = __uint_as_float(0x7FC00000u);
+  // Lane (g, t) has the 16-byte vectors t, t + 4, .. of pages g and g + 8 of a tile, which stand for
+  // four k-steps' operands; the query parts are read in the same order.
+  struct Bounds {
+    uint4 a[kVectors], b[kVectors];
+    float step_a, step_b;
+  };
+  auto fetch = [&](Bounds& x, int pg) {
+    const int pa = __shfl_sync(0xffffffffu, pg, g), pb = __shfl_sync(0xffffffffu, pg, g + 8);
+    const char* ca = a.codes + (static_cast<int64_t>(pa) * a.p.heads + h) * kCodes + 16 * t;
+    const char* cb = a.codes + (static_cast<int64_t>(pb) * a.p.heads + h) * kCodes + 16 * t;
+#pragma unroll
+    for (int v = 0; v < kVectors; ++v) {
+      x.a[v] = x.b[v] = make_uint4(0, 0, 0, 0);
+      if (pa >= 0) x.a[v] = ld_once(ca + 64 * v);
+      if (pb >= 0) x.b[v] = ld_once(cb + 64 * v);
+    }
+    x.step_a = pa >= 0 ? a.steps[static_cast<int64_t>(pa) * a.p.heads + h] : none;
+    x.step_b = pb >= 0 ? a.steps[static_cast<int64_t>(pb) * a.p.heads + h] : none;
+  };
+  Bounds now;
   if (!all) {
+    if (p0 < pages) {
+      fetch(now, pg);
+      pg = look_up(p0 + stride);
+    }
     // ---- the query heads, 4 or 2 channels per lane
     constexpr int kLane = DP / 32;
     for (int q = warp; q < a.head_tiles * 8; q += kWarps) {
@@ -313,45 +379,39 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(ChooseArgs a) {
         *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(neg);
         *reinterpret_cast<uint16_t*>(to + DP) = static_cast<uint16_t>(plus);
       }
-      if (lane == 0) up[q] = counts ? pow2(e) : __uint_as_float(0x7FC00000u);
+      if (lane == 0) up[q] = counts ? pow2(e) : none;
     }
   }
   __syncthreads();
   if (a.cluster > 1) cluster_wait();
   if (!all) {
-    // ---- scores: lane (g, t) has 16-byte vectors t, t + 4, .. of pages g and g + 8, which
-    // stand for four k-steps' operands; the query parts are read in the same order.
+    // ---- scores, the next tile's bounds on their way
     const uint32_t keys_at = smem_u32(keys);
-    for (int p0 = (rank * kWarps + warp) * 16; p0 < pages; p0 += a.cluster * kWarps * 16) {
-      int pg = -1;
-      if (lane < 16 && p0 + lane < pages) pg = a.p.table ? a.p.table[b * a.p.table_stride + p0 + lane] : b;
-      if (static_cast<unsigned>(pg) >= static_cast<unsigned>(a.p.n_pages)) pg = -1;
-      const int pa = __shfl_sync(0xffffffffu, pg, g), pb = __shfl_sync(0xffffffffu, pg, g + 8);
-      uint4 xa[kVectors], xb[kVectors];
-      float sa = __uint_as_float(0x7FC00000u), sb = sa;
-      const char* ca = a.codes + (static_cast<int64_t>(pa) * a.p.heads + h) * kCodes + 16 * t;
-      const char* cb = a.codes + (static_cast<int64_t>(pb) * a.p.heads + h) * kCodes + 16 * t;
-#pragma unroll
-      for (int v = 0; v < kVectors; ++v) {
-        xa[v] = xb[v] = make_uint4(0, 0, 0, 0);
-        if (pa >= 0) xa[v] = ld_once(ca + 64 * v);
-        if (pb >= 0) xb[v] = ld_once(cb + 64 * v);
+    for (; p0 < pages; p0 += stride) {
+      Bounds next;
+      if (p0 + stride < pages) {
+        fetch(next, pg);
+        pg = look_up(p0 + 2 * stride);
       }
-      if (pa >= 0) sa = a.steps[static_cast<int64_t>(pa) * a.p.heads + h];
-      if (pb >= 0) sb = a.steps[static_cast<int64_t>(pb) * a.p.heads + h];
-      float best_a = __uint_as_float(0x7FC00000u), best_b = best_a;
+      float best_a = none, best_b = none;
       for (int ht = 0; ht < a.head_tiles; ++ht) {
-        int c[4] = {0, 0, 0, 0};
+        int parts_c[kVectors][4] = {};  // sums apart: a matrix instruction does not wait for the one before
         const unsigned char* at = parts + (ht * 8 + g) * kCodes + 16 * t;
 #pragma unroll
         for (int v = 0; v < kVectors; ++v) {
           const uint4 q = lds_u4(at + 64 * v);
-          mma_s8(c, xa[v].x, xb[v].x, xa[v].y, xb[v].y, q.x, q.y);
-          mma_s8(c, xa[v].z, xb[v].z, xa[v].w, xb[v].w, q.z, q.w);
+          mma_s8(parts_c[v], now.a[v].x, now.b[v].x, now.a[v].y, now.b[v].y, q.x, q.y);
+          mma_s8(parts_c[v], now.a[v].z, now.b[v].z, now.a[v].w, now.b[v].w, q.z, q.w);
+        }
+        int c[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          c[i] = parts_c[0][i] + parts_c[1][i];
+          if constexpr (kVectors == 4) c[i] += parts_c[2][i] + parts_c[3][i];
         }
         const float2 u = *reinterpret_cast<const float2*>(up + ht * 8 + 2 * t);
-        best_a = fmaxf(best_a, fmaxf(static_cast<float>(c[0]) * u.x * sa, static_cast<float>(c[1]) * u.y * sa));  // NaN loses
-        best_b = fmaxf(best_b, fmaxf(static_cast<float>(c[2]) * u.x * sb, static_cast<float>(c[3]) * u.y * sb));
+        best_a = fmaxf(best_a, fmaxf(static_cast<float>(c[0]) * u.x * now.step_a, static_cast<float>(c[1]) * u.y * now.step_a));  // NaN loses
+        best_b = fmaxf(best_b, fmaxf(static_cast<float>(c[2]) * u.x * now.step_b, static_cast<float>(c[3]) * u.y * now.step_b));
       }
 #pragma unroll
       for (int d = 1; d < 4; d <<= 1) {
@@ -366,6 +426,7 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(ChooseArgs a) {
         else
           keys[p] = k;
       }
+      now = next;
     }
   }
   if (a.cluster > 1) {
@@ -379,16 +440,15 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(ChooseArgs a) {
   }
   __syncthreads();
   const int need = a.n - a.first - a.recent, end = pages - a.recent;
-  uint32_t least = 0xFFFFFFFFu;
-  if (need > 0) mark_largest(keys, a.first, end, need, bins, cand, scratch, &least);
+  const uint32_t least = need > 0 ? mark_largest(keys, a.first, end, need, bins, cand, scratch) : 0u;
   // ---- the list, in order: a thread has a run of pages
-  const int per = (pages + kChooseThreads - 1) / kChooseThreads, p0 = threadIdx.x * per, p1 = min(pages, p0 + per);
+  const int per = (pages + kChooseThreads - 1) / kChooseThreads, from = threadIdx.x * per, upto = min(pages, from + per);
   auto chosen = [&](int p) { return p < a.first || p >= end || (need > 0 && keys[p] > least); };
   int count = 0;
-  for (int p = p0; p < p1; ++p) count += chosen(p);
+  for (int p = from; p < upto; ++p) count += chosen(p);
   int total;
   int at = before_me(count, scratch, total);
-  for (int p = p0; p < p1; ++p)
+  for (int p = from; p < upto; ++p)
     if (chosen(p)) out[at++] = p;
 }
 
