@@ -12,7 +12,7 @@
 namespace ipv {
 namespace {
 
-constexpr int kBlock = 256;
+constexpr int kBlock = 128;
 constexpr int kTeams = kBlock / 8;
 
 // Pairs of channels: (i, i + 64) of 128, (i, i + rot / 2) of the first rot, (2i, 2i + 1).
@@ -143,15 +143,42 @@ __device__ __forceinline__ void store(const Pages& p, char* pool, uint32_t* par,
   }
 }
 
+// The sequence whose new rows a packed row lies among: the last that starts at or before it. For whole warps.
+__device__ __forceinline__ int sequence_of(const Pages& p, int64_t row) {
+  const int lane = threadIdx.x & 31;
+  int first = 0, n = p.n_seqs;
+  while (true) {
+    const int step = (n + 31) / 32, b = first + lane * step;
+    const int before = __popc(__ballot_sync(0xffffffffu, b < first + n && p.row_start[b] <= row));
+    first += max(0, before - 1) * step;
+    if (step == 1) return first;
+    n = min(step, p.n_seqs - first);
+  }
+}
+
 template <int FMT, int PAIRS>
-__global__ void __launch_bounds__(kBlock) rotate_kernel(RotateArgs a) {
+__global__ void __launch_bounds__(kBlock, PAIRS == kOwn ? 8 : 4) rotate_kernel(RotateArgs a) {
   pdl_trigger();
   pdl_wait();
-  const int b = blockIdx.y, r = blockIdx.x, c = threadIdx.x & 7;
-  const Seq s = sequence(a.p, b);
-  if (r >= s.n) return;
-  const int64_t row = s.row0 + static_cast<int64_t>(r);
-  const int j = s.len - s.n + r, items = a.q_heads + a.p.heads;
+  const int64_t row = blockIdx.x;
+  const int c = threadIdx.x & 7, items = a.q_heads + a.p.heads;
+  const int first = (threadIdx.x >> 5) * 4, mine = (threadIdx.x & 31) >> 3;  // a warp's items, the team's among them
+  if (first >= items) return;
+  auto load = [&](const uint16_t* from, uint4 (&x)[2], bool in) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int ch = 8 * (c + 8 * g);
+      x[g] = make_uint4(0, 0, 0, 0);
+      if (in && ch < a.p.dim) x[g] = ld_once(from + ch);
+    }
+  };
+  auto load_item = [&](int base, uint4 (&x)[2], uint4 (&v)[2]) {
+    const int item = base + mine, h = item - a.q_heads;
+    load(h < 0 ? a.q + row * a.q_row + item * a.q_head : a.k_new + row * a.row + h * a.head, x, item < items);
+    if (base + 4 > a.q_heads) load(a.v_new + row * a.row + h * a.head, v, h >= 0 && item < items);
+  };
+  uint4 x[2], v[2] = {};
+  load_item(first, x, v);  // on their way while positions, turns, sequence and page are looked up
   Turn turn[2];
   if (PAIRS == kOwn) {
     load_turn<8>(a, row, 8 * c, turn[0]);
@@ -166,18 +193,19 @@ __global__ void __launch_bounds__(kBlock) rotate_kernel(RotateArgs a) {
         load_turn<8>(a, row, 8 * (n < half ? n : n - half), turn[g]);
     }
   }
-  const int64_t page_row = j < 0 ? -1 : pool_row(a.p, b, j);
-  for (int base = (threadIdx.x >> 5) * 4; base < items; base += kTeams) {  // the same for a whole warp
-    const int item = base + ((threadIdx.x & 31) >> 3), h = item - a.q_heads;
+  const int b = sequence_of(a.p, row);
+  const Seq s = sequence(a.p, b);
+  if (row < s.row0 || row >= s.row0 + static_cast<int64_t>(s.n)) return;  // the same for the block
+  const int j = s.len - s.n + static_cast<int>(row - s.row0);
+  for (int base = first; base < items; base += kTeams) {  // the same for a whole warp
+    const int item = base + mine, h = item - a.q_heads;
     const bool in = item < items, q = in && h < 0;
-    const uint16_t* from = q ? a.q + row * a.q_row + item * a.q_head : a.k_new + row * a.row + (in ? h : 0) * a.head;
-    uint4 x[2], v[2];
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const int ch = 8 * (c + 8 * g);
-      x[g] = v[g] = make_uint4(0, 0, 0, 0);
-      if (in && ch < a.p.dim) x[g] = ld_once(from + ch);
-      if (in && !q && ch < a.p.dim) v[g] = ld_once(a.v_new + row * a.row + h * a.head + ch);
+    if (base > first) load_item(base, x, v);
+    int64_t to = -1;
+    if (base + 4 > a.q_heads) {
+      if (in && !q && j >= 0) to = pool_row(a.p, b, j);
+      if (to >= 0) to += h * a.p.head_stride;
+      store<FMT>(a.p, a.p.v, a.p.v_par, to, v, c);
     }
     // Norms are of all heads of a kind or of none; a warp may have both kinds.
     const uint16_t* w = q ? a.q_weight : a.k_weight;
@@ -196,17 +224,13 @@ __global__ void __launch_bounds__(kBlock) rotate_kernel(RotateArgs a) {
       for (int g = 0; g < 2; ++g)
         if (8 * (c + 8 * g) < a.p.dim) *reinterpret_cast<uint4*>(a.q_out + row * a.out_row + item * a.out_head + 8 * (c + 8 * g)) = x[g];
     }
-    if (base + 4 > a.q_heads) {
-      const int64_t to = in && !q && page_row >= 0 ? page_row + h * a.p.head_stride : -1;
-      store<FMT>(a.p, a.p.k, a.p.k_par, to, x, c);
-      store<FMT>(a.p, a.p.v, a.p.v_par, to, v, c);
-    }
+    if (base + 4 > a.q_heads) store<FMT>(a.p, a.p.k, a.p.k_par, to, x, c);
   }
 }
 
 template <int FMT>
 cudaError_t launch(const RotateArgs& a, cudaStream_t st) {
-  const dim3 g(static_cast<unsigned>(a.p.max_rows), static_cast<unsigned>(a.p.n_seqs));
+  const dim3 g(static_cast<unsigned>(a.p.total_rows));
   if (a.neighbours) return launch_next(rotate_kernel<FMT, kNeighbours>, g, kBlock, 0, st, a);
   if (a.rot == 128) return launch_next(rotate_kernel<FMT, kOwn>, g, kBlock, 0, st, a);
   return launch_next(rotate_kernel<FMT, kHalves>, g, kBlock, 0, st, a);
