@@ -57,53 +57,57 @@ __global__ void __launch_bounds__(kBlock) copy_kernel(CopyArgs a) {
 
 // A team of 8 lanes takes a row of K and of V of one head as one list of 16-byte
 // chunks, T of them per lane, and 8 / T rows at once: 8 loads on their way in
-// each lane whatever the format, after one round of look-ups for all the rows.
+// each lane whatever the format. Before that a thread for each row looks up (the kept index,
+// then the pages) where it comes from and goes to.
 constexpr int kTeams = kBlock / 8;
 
 template <int T>
 __global__ void __launch_bounds__(kBlock) move_rows_kernel(MoveArgs a) {
-  constexpr int kRows = 8 / T;
+  constexpr int kRows = 8 / T, kTile = kTeams * kRows;
+  __shared__ longlong2 places[kTile];  // rows of the pools, head included; from: -1 reads as zero, to: -1 is dropped
   pdl_trigger();
   pdl_wait();
-  const int b = blockIdx.z, h = blockIdx.y;
+  const int b = blockIdx.z, h = blockIdx.y, first = blockIdx.x * kTile, lane = threadIdx.x & 7, team = threadIdx.x >> 3;
+  const int i = first + static_cast<int>(threadIdx.x);
+  const bool looks = threadIdx.x < kTile && i < a.p.max_rows;
+  // The index does not wait for the lengths: a list has one for every row that a sequence may have.
+  const int r = !looks ? -1 : a.kept ? a.kept[b * a.kept_seq + h * a.kept_head + i] : i;
   const Seq s = sequence(a.p, b);
-  const int first = blockIdx.x * (kTeams * kRows) + (threadIdx.x >> 3), lane = threadIdx.x & 7;
-  if (static_cast<int>(blockIdx.x) * (kTeams * kRows) >= s.n) return;
-  const int held = min(max(a.src.kv_len[b], 0), a.src.max_kv);
-  const int32_t* kept = a.kept ? a.kept + b * a.kept_seq + h * a.kept_head : nullptr;
-  int64_t from[kRows], to[kRows];  // rows of the pools, head included; from: -1 reads as zero, to: -1 is dropped
-#pragma unroll
-  for (int u = 0; u < kRows; ++u) {
-    const int i = first + u * kTeams, j = s.len - s.n + i;
-    from[u] = to[u] = -1;
-    if (i >= s.n || j < 0) continue;
-    const int r = kept ? kept[i] : i;
-    to[u] = pool_row(a.p, b, j);
-    if (r >= 0 && r < held) from[u] = pool_row(a.src, b, r);
+  if (first >= s.n) return;
+  const int held = min(max(a.src.kv_len[b], 0), a.src.max_kv), j = s.len - s.n + i;
+  if (threadIdx.x < kTile) {
+    longlong2 x = make_longlong2(-1, -1);
+    if (i < s.n && j >= 0) {
+      if (r >= 0 && r < held) x.x = pool_row(a.src, b, r);
+      x.y = pool_row(a.p, b, j);
+      if (x.x >= 0) x.x += h * a.src.head_stride;
+      if (x.y >= 0) x.y += h * a.p.head_stride;
+    }
+    places[threadIdx.x] = x;
   }
+  __syncthreads();
+  const int chunks = a.row_chunks;
   uint4 x[kRows][T];
   uint2 par[kRows];
-  const int chunks = a.row_chunks;
 #pragma unroll
   for (int u = 0; u < kRows; ++u) {
-    const int64_t row = from[u] + h * a.src.head_stride;
+    const int64_t row = places[team + u * kTeams].x;
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       const int c = lane + 8 * t;
       x[u][t] = make_uint4(0, 0, 0, 0);
-      if (from[u] >= 0 && c < 2 * chunks)
-        x[u][t] = ld_once((c < chunks ? a.src.k + c * 16 : a.src.v + (c - chunks) * 16) + row * a.src.row_bytes);
+      if (row >= 0 && c < 2 * chunks) x[u][t] = ld_once((c < chunks ? a.src.k + c * 16 : a.src.v + (c - chunks) * 16) + row * a.src.row_bytes);
     }
     par[u] = make_uint2(0, 0);
-    if (a.p.fmt != kBf16 && from[u] >= 0 && lane < 2) {
+    if (a.p.fmt != kBf16 && row >= 0 && lane < 2) {
       const uint32_t* p = (lane == 0 ? a.src.k_par : a.src.v_par) + row * a.src.groups;
       par[u] = a.src.groups == 2 ? *reinterpret_cast<const uint2*>(p) : make_uint2(*p, 0u);
     }
   }
 #pragma unroll
   for (int u = 0; u < kRows; ++u) {
-    if (to[u] < 0) continue;
-    const int64_t row = to[u] + h * a.p.head_stride;
+    const int64_t row = places[team + u * kTeams].y;
+    if (row < 0) continue;
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       const int c = lane + 8 * t;
@@ -121,8 +125,8 @@ __global__ void __launch_bounds__(kBlock) move_rows_kernel(MoveArgs a) {
 
 template <int T>
 cudaError_t launch_move(const MoveArgs& a, cudaStream_t st) {
-  constexpr int kRows = kTeams * (8 / T);
-  const dim3 g(static_cast<unsigned>((a.p.max_rows + kRows - 1) / kRows), static_cast<unsigned>(a.p.heads), static_cast<unsigned>(a.p.n_seqs));
+  constexpr int kTile = kTeams * (8 / T);
+  const dim3 g(static_cast<unsigned>((a.p.max_rows + kTile - 1) / kTile), static_cast<unsigned>(a.p.heads), static_cast<unsigned>(a.p.n_seqs));
   return launch_next(move_rows_kernel<T>, g, kBlock, 0, st, a);
 }
 
