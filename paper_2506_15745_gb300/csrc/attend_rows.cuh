@@ -40,7 +40,7 @@
 namespace ipv {
 namespace {
 
-constexpr int kThreads = 32 * kRowsWarps;
+constexpr int kThreads = 32 * kRowsWarps;  // of the join, and of most kernels
 constexpr int kRunCost = 6;  // what a run of steps costs beside them, in steps
 constexpr int kCluster = kRowsCluster;
 constexpr float kNegInf = -INFINITY;
@@ -55,14 +55,20 @@ struct Ring {
   // bf16: 96 to 128 KB in flight with one block per SM; codes: 3 blocks, and 3 stages
   // were slower (32 streams of 12288 8-bit rows 213 us against 150).
   static constexpr int kStages = FMT == kBf16 ? 3 : 2;
-  static constexpr int kWarp = kStage * kStages;
-  static constexpr int kBytes = kWarp * kRowsWarps;
 };
 
-// Dynamic shared memory: the rings, the warps' results.
-template <int FMT, int DP, int NR>
-struct Sizes {
-  static constexpr int kBytes = Ring<FMT, DP>::kBytes + kRowsWarps * 8 * NR * (DP + 4 + 2) * 4;
+// How a kernel lays itself out. Chosen bf16 pages of 128 channels are mostly found in L2, where one warp per scheduler
+// waits for its own chain of instructions (0.27 issued per cycle): 8 warps, whose rings hold 3
+// halves of stages, K's or V's each, instead of 4 with 3 stages. A half is refilled as soon as it has been read.
+template <int FMT, int DP, int NR, bool CHOSEN>
+struct Layout {
+  static constexpr bool kHalves = CHOSEN && FMT == kBf16 && DP == 128 && NR == 1;
+  static constexpr int kWarps = kHalves ? 8 : kRowsWarps;
+  static constexpr int kThreads = 32 * kWarps;
+  static constexpr int kRing = kHalves ? 3 * Ring<FMT, DP>::kTile : Ring<FMT, DP>::kStage * Ring<FMT, DP>::kStages;  // of a warp
+  static constexpr int kRings = kRing * kWarps;
+  static constexpr int kResults = kRings + kWarps * 8 * NR * (DP + 4 + 2) * 4;  // and the warps' results
+  static constexpr int kBytes = kResults + (CHOSEN ? kWarps * 3 * 4 : 0);      // and which keys are seen
 };
 
 // Where 16-byte chunk c of key row r lies in its row: the rows that a quarter
@@ -214,8 +220,10 @@ __device__ __forceinline__ void cluster_barrier() {
 
 // CHOSEN: a row tile's keys are those of its new row's chosen pages, one list for each KV head.
 template <int FMT, int DP, int NR, bool CHOSEN>
-__global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows_kernel(AttendArgs a, int tiles) {
+__global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blocks(FMT, DP, NR)) attend_rows_kernel(AttendArgs a, int tiles) {
   using R = Ring<FMT, DP>;
+  using L = Layout<FMT, DP, NR, CHOSEN>;
+  constexpr int kWarps = L::kWarps, kThreads = L::kThreads;
   constexpr bool kB = FMT == kBf16;
   constexpr int kCh = R::kRowB / 16;     // chunks of a row
   constexpr int kKs = DP / 16;           // k-steps of the first product
@@ -236,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
   __syncthreads();  // the shared memory held find_share's scratch
   using W = Walk<kTileRows, kRowsStep, kRunCost, CHOSEN>;
   W w = {};
-  const uint32_t ring = smem_u32(smem) + warp * R::kWarp;
+  const uint32_t ring = smem_u32(smem) + warp * L::kRing;
   const int nch = a.p.row_bytes >> 4;
 
   // ---- copies of one step into one stage (this warp's lanes only)
@@ -246,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
   const int64_t v_from_k = a.p.v - a.p.k;
   const int64_t page_bytes = a.p.page_stride * a.p.row_bytes, next_bytes = a.p.row_stride * a.p.row_bytes;
   // Which keys of a stage's step are seen, a word for each; CHOSEN only.
-  uint32_t* sees = reinterpret_cast<uint32_t*>(smem + Sizes<FMT, DP, NR>::kBytes) + warp * R::kStages;
+  uint32_t* sees = reinterpret_cast<uint32_t*>(smem + L::kResults) + warp * 3;
   // This lane's key of step i of run x: its page, -1: none (CHOSEN, kUnseen: not seen). Read a step ahead of
   // the copies.
   constexpr int kUnseen = -2;
@@ -294,19 +302,56 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
       copy16(dst + R::kTile, src + v_from_k, ok);
     }
   };
+  // Halves: where this lane's key of step i lies (-1: nowhere, reads as zero), and the copies of one step's K or V
+  // into one half, with which of the keys are seen.
+  auto row_at = [&](const W& x, int i, int pg) {
+    if (pg < 0) return int64_t{-1};
+    const int j = x.t.kr.template key0<kRowsStep>(i) + lane;
+    return x.head * a.p.head_stride * a.p.row_bytes + pg * page_bytes + (a.p.page_shift == 31 ? j : j & (a.p.page_size - 1)) * next_bytes;
+  };
+  auto copy_half = [&](const char* from, int64_t off, int half) {
+#pragma unroll
+    for (int u = 0; u < kCh; ++u) {
+      const int r = u * kApart + my_r;
+      const int64_t at = __shfl_sync(0xffffffffu, off, r);
+      const bool ok = at >= 0 && my_c < nch;
+      copy16(ring + half * R::kTile + r * R::kRowB + swizzle<FMT, R::kRowB>(r, my_c) * 16, ok ? from + my_c * 16 + at : from, ok);
+    }
+  };
+  auto note = [&](int pg, int word) {
+    const uint32_t seen = __ballot_sync(0xffffffffu, pg != kUnseen);
+    if (lane == 0) sees[word] = seen;
+  };
+  int64_t v_off = -1;  // of the step whose K was copied last
   // The first steps of a run, and the page of the one after them.
   int page_next = -1;
   auto fill = [&](const W& x) {
-    int pages[R::kStages];  // all on their way at once
-#pragma unroll
-    for (int i = 0; i < R::kStages; ++i) pages[i] = page_of(x, x.s + warp + i * kRowsWarps);
-#pragma unroll
-    for (int i = 0; i < R::kStages - 1; ++i) {
-      const int step = x.s + warp + i * kRowsWarps;
-      if (step < x.s + x.n) issue(x, step, pages[i], i);
+    if constexpr (L::kHalves) {  // K and V of the first step, K of the second
+      const int i0 = x.s + warp, i1 = i0 + kWarps, end = x.s + x.n;
+      const int pg0 = page_of(x, i0), pg1 = page_of(x, i1);
+      page_next = page_of(x, i1 + kWarps);
+      const int64_t off = row_at(x, i0, pg0);
+      v_off = row_at(x, i1, pg1);
+      note(pg0, 0);
+      note(pg1, 1);
+      if (i0 < end) copy_half(a.p.k, off, 0);
       copy_commit();
+      if (i0 < end) copy_half(a.p.v, off, 1);
+      copy_commit();
+      if (i1 < end) copy_half(a.p.k, v_off, 2);
+      copy_commit();
+    } else {
+      int pages[R::kStages];  // all on their way at once
+#pragma unroll
+      for (int i = 0; i < R::kStages; ++i) pages[i] = page_of(x, x.s + warp + i * kWarps);
+#pragma unroll
+      for (int i = 0; i < R::kStages - 1; ++i) {
+        const int step = x.s + warp + i * kWarps;
+        if (step < x.s + x.n) issue(x, step, pages[i], i);
+        copy_commit();
+      }
+      page_next = pages[R::kStages - 1];
     }
-    page_next = pages[R::kStages - 1];
   };
 
   // A cluster's part: [rows][DP sums, maximum, sum] in the rings, which one run leaves free.
@@ -419,17 +464,21 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
 
     // ---- the loop over this warp's steps
     int stage = 0;
-    for (int step = first; step < s_end; step += kRowsWarps) {
-      {
-        const int ahead = step + (R::kStages - 1) * kRowsWarps;
+    int k_half = 0, v_half = 1, next_half = 2, word = 0;  // halves: where K, V and the next step's K are, and the word of sees
+    for (int step = first; step < s_end; step += kWarps) {
+      if constexpr (L::kHalves) {
+        copy_wait<2>();
+      } else {
+        const int ahead = step + (R::kStages - 1) * kWarps;
         const int to = stage == 0 ? R::kStages - 1 : stage - 1;
         if (ahead < s_end) issue(w, ahead, page_next, to);
-        page_next = page_of(w, ahead + kRowsWarps);
+        page_next = page_of(w, ahead + kWarps);
         copy_commit();
+        copy_wait<R::kStages - 1>();
       }
-      copy_wait<R::kStages - 1>();
       __syncwarp();
-      const uint32_t ks_at = ring + stage * R::kStage, vs_at = ks_at + R::kTile;
+      const uint32_t ks_at = ring + (L::kHalves ? k_half * R::kTile : stage * R::kStage);
+      const uint32_t vs_at = L::kHalves ? ring + v_half * R::kTile : ks_at + R::kTile;
       const uint32_t kp_at = ks_at + 2 * R::kTile, vp_at = kp_at + R::kPar;
       const int key0 = kr.key0<kRowsStep>(step);
 
@@ -511,9 +560,14 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
             }
         }
       }
+      if constexpr (L::kHalves) {  // K has been read: the next step's V comes in its place
+        __syncwarp();
+        if (step + kWarps < s_end) copy_half(a.p.v, v_off, k_half);
+        copy_commit();
+      }
       // The mask, only where some row of the tile does not see all 32 keys.
       if constexpr (CHOSEN) {
-        const uint32_t seen = sees[stage];
+        const uint32_t seen = sees[L::kHalves ? word : stage];
         if (seen != 0xffffffffu) {
 #pragma unroll
           for (int mt = 0; mt < 2; ++mt)
@@ -623,6 +677,10 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
             }
           }
       }
+      if constexpr (L::kHalves) {
+        copy_wait<2>();
+        __syncwarp();
+      }
       // O^T += V^T P^T
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt) {
@@ -686,7 +744,19 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
         }
       }
       __syncwarp();  // the stage is read before its next copies are issued
-      stage = stage + 1 == R::kStages ? 0 : stage + 1;
+      if constexpr (L::kHalves) {  // K of the step after the next one in V's place
+        const int ahead = step + 2 * kWarps;
+        v_off = row_at(w, ahead, page_next);
+        word = word == 2 ? 0 : word + 1;
+        note(page_next, word == 2 ? 0 : word + 1);
+        if (ahead < s_end) copy_half(a.p.k, v_off, v_half);
+        copy_commit();
+        page_next = page_of(w, ahead + kWarps);
+        const int free = v_half;
+        v_half = k_half, k_half = next_half, next_half = free;
+      } else {
+        stage = stage + 1 == R::kStages ? 0 : stage + 1;
+      }
     }
     // The next run's first steps are on their way while this one's results are joined.
     const bool partial = !(w.starts() && w.ends());
@@ -696,10 +766,10 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
 
     // ---- join the warps
     constexpr int kRows = 8 * NR;
-    float* so = reinterpret_cast<float*>(smem + R::kBytes);           // [warps][rows][DP + 4]
+    float* so = reinterpret_cast<float*>(smem + L::kRings);           // [warps][rows][DP + 4]
     constexpr int kPitch = DP + 4;
-    float* sm = so + kRowsWarps * kRows * kPitch;                     // [warps][rows] maxima, then sums
-    float* sl = sm + kRowsWarps * kRows;
+    float* sm = so + kWarps * kRows * kPitch;                     // [warps][rows] maxima, then sums
+    float* sl = sm + kWarps * kRows;
 #pragma unroll
     for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
@@ -745,12 +815,12 @@ __global__ void __launch_bounds__(kThreads, min_blocks(FMT, DP, NR)) attend_rows
       if (row0 + r > row1) continue;
       float top = sm[r];
 #pragma unroll
-      for (int x = 1; x < kRowsWarps; ++x) top = fmaxf(top, sm[x * kRows + r]);
+      for (int x = 1; x < kWarps; ++x) top = fmaxf(top, sm[x * kRows + r]);
       const float base = top == kNegInf ? 0.0f : top;
       float sum = 0.0f;
       float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-      for (int x = 0; x < kRowsWarps; ++x) {
+      for (int x = 0; x < kWarps; ++x) {
         const float f = exp2_fast(sm[x * kRows + r] - base);
         sum += f * sl[x * kRows + r];
         const float4 y = *reinterpret_cast<const float4*>(so + (x * kRows + r) * kPitch + c);
@@ -876,17 +946,18 @@ __global__ void __launch_bounds__(kThreads) attend_rows_join_kernel(AttendArgs a
 
 template <int FMT, int DP, int NR, bool CHOSEN>
 struct Kernel {
-  static constexpr int kSmem = Sizes<FMT, DP, NR>::kBytes + (CHOSEN ? kRowsWarps * Ring<FMT, DP>::kStages * 4 : 0);
+  using L = Layout<FMT, DP, NR, CHOSEN>;
+  static constexpr int kSmem = L::kBytes;
   inline static int resident = 0;  // blocks per SM
   static cudaError_t prepare() {
     const cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<FMT, DP, NR, CHOSEN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
-    return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, attend_rows_kernel<FMT, DP, NR, CHOSEN>, kThreads, kSmem);
+    return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, attend_rows_kernel<FMT, DP, NR, CHOSEN>, L::kThreads, kSmem);
   }
   static cudaError_t launch(const AttendArgs& a, int blocks, cudaStream_t st) {
     const cudaError_t e =
-        launch_clusters(a.unit == 0 ? a.cluster : 1, attend_rows_kernel<FMT, DP, NR, CHOSEN>, dim3(blocks), kThreads, kSmem, st, a, a.tiles);
-    if (e != cudaSuccess || a.unit == 0) return e;
+        launch_clusters(a.unit == 0 ? a.cluster : 1, attend_rows_kernel<FMT, DP, NR, CHOSEN>, dim3(blocks), L::kThreads, kSmem, st, a, a.tiles);
+    if (e != cudaSuccess || a.unit <= 0) return e;
     return launch_next(attend_rows_join_kernel<8 * NR, CHOSEN>, dim3(blocks, 8 * NR), kThreads, 0, st, a, a.tiles, blocks);
   }
 };

@@ -64,14 +64,35 @@ template <int ROWS, int STEP, int COST, bool CHOSEN = false>
 struct Walk {
   Tile t;
   int head, s, n;  // steps s .. s + n - 1
-  int64_t left;
+  int64_t left;    // kApart: the number of the tile and head in its sequence, plus what the sequences before it have
   __device__ __forceinline__ void cut(int64_t at) {
     const int64_t weight = t.steps + COST, upto = min(weight, at + left);
     s = static_cast<int>(max(int64_t{0}, at - COST));
     n = static_cast<int>(max(int64_t{0}, upto - COST)) - s;
     left -= upto - at;
   }
+  // kApart: the tile and head `left` places on from sequence b's first. Heads of a sequence follow one another, so that the blocks
+  // that run at the same time read pages of one head or two.
+  __device__ __forceinline__ bool settle(const AttendArgs& a, int b) {
+    for (; b < a.p.n_seqs; ++b) {
+      t.seq = sequence(a.p, b);
+      const int64_t one = static_cast<int64_t>(t.seq.n) * a.per_row, all = one * a.p.heads;
+      if (left < all) {
+        head = static_cast<int>(left / one);
+        set_tile<ROWS, STEP, true>(a, t, b, static_cast<int>(left - head * one));
+        s = 0;
+        n = t.steps;
+        return true;
+      }
+      left -= all;
+    }
+    return false;
+  }
   __device__ __forceinline__ bool begin(const AttendArgs& a, int tiles, const Share& w) {
+    if (CHOSEN && a.unit == kApart) {
+      left = blockIdx.x;
+      return settle(a, 0);
+    }
     t = tile_of<ROWS, STEP, CHOSEN>(a, tiles, w.p);
     head = w.head;
     left = w.left;
@@ -79,6 +100,10 @@ struct Walk {
     return n > 0 || next(a, tiles);
   }
   __device__ __forceinline__ bool next(const AttendArgs& a, int tiles) {
+    if (CHOSEN && a.unit == kApart) {
+      left += gridDim.x;
+      return settle(a, t.b);
+    }
     if (left <= 0) return false;
     if (++head == a.p.heads) {
       head = 0;
@@ -114,6 +139,11 @@ template <int ROWS, int STEP, int COST, int THREADS, bool CHOSEN = false>
 __device__ Share find_share(const AttendArgs& a, int tiles, int64_t* scratch) {
   const int pairs = a.p.n_seqs * tiles, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   constexpr int kWarps = THREADS / 32;
+  if (CHOSEN && a.unit == kApart) {
+    Share w = {};
+    w.left = 1;  // to be walked; there may be nothing
+    return w;
+  }
   auto weight = [&](int p) {
     const int steps = p < pairs ? tile_of<ROWS, STEP, CHOSEN>(a, tiles, p).steps : 0;
     return steps > 0 ? static_cast<int64_t>(steps + COST) * a.p.heads : int64_t{0};

@@ -246,6 +246,10 @@ constexpr int kWhole = 512;
 // 12000 16 against 13; 4 bits: 1500 keys 8.5 against 14.8, 6272 13.0 against 15.1.
 constexpr int64_t kClusterKeys = 8192, kClusterBytes = 1 << 20;
 
+// Chosen pages: from this many row tiles and heads per block on, blocks take them whole and in turn, which keeps the
+// blocks that run at the same time near one another in the cache (and in L2) and leaves nothing to join.
+constexpr int kApartItems = 4;
+
 // Which kernel takes the call, on how many blocks, and the workspace.
 struct Plan {
   bool tiles = false;
@@ -309,6 +313,10 @@ void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
     a->unit = 0;
     a->cluster = ipv::kRowsCluster;
     plan->blocks = static_cast<int>(items) * ipv::kRowsCluster;
+    return;
+  }
+  if (a->n_chosen > 0 && items >= kApartItems * plan->blocks) {
+    a->unit = ipv::kApart;
     return;
   }
   const int64_t parts = static_cast<int64_t>(plan->blocks) * 2 * a->tile;
@@ -675,6 +683,7 @@ extern "C" ipv_status ipv_bounds_choose(const ipv_bounds* bounds, const ipv_batc
   a.n = t->n_chosen;
   a.first = t->first;
   a.recent = t->recent;
+  a.max_pages = static_cast<int>(pages);
   // Blocks for one list: as long as each warp keeps 16 pages and the device has room for them all.
   const int64_t lists = static_cast<int64_t>(a.p.max_rows) * a.p.n_seqs * a.p.heads;
   a.cluster = 1;

@@ -107,6 +107,7 @@ cudaError_t launch_next(void (*kernel)(Params...), dim3 grid, unsigned block, si
 }
 
 // ------------------------------------------------------------------ attention
+constexpr int kApart = -1;  // AttendArgs::unit
 struct AttendArgs {
   Pages p;
   const uint16_t* q;
@@ -119,7 +120,8 @@ struct AttendArgs {
   float scale_log2;     // scale * log2(e)
   int causal, window, sinks;
   // Fewest units (steps and runs' costs) of a block's share; 0: `cluster` blocks (1, or 8 as one cluster,
-  // which joins their parts by itself) take one KV head of one row tile.
+  // which joins their parts by itself) take one KV head of one row tile; kApart (chosen pages): a block takes
+  // tiles whole, every gridDim.x-th one.
   int unit, cluster;
   int tile;  // query rows of a row tile
   // Chosen pages: a row tile holds one new row's query heads (or `tile` of them), `per_row` tiles a new row; entry
@@ -258,6 +260,7 @@ struct ChooseArgs {
   int32_t* out;
   int64_t out_row, out_head;
   int n, first, recent;
+  int max_pages;                  // that a sequence has
   int cluster;                    // blocks that score the pages of one row and KV head
 };
 constexpr int kChooseThreads = 256;
