@@ -17,6 +17,7 @@ and passes pointers. A half of a PingPongCache is a paged cache as it stands:
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import torch
 
@@ -24,6 +25,19 @@ from . import ipv
 
 GROUP = 64  # channels that share a step and a minimum
 FORMATS = {"bf16": ipv.IPV_PAGES_BF16, "u8": ipv.IPV_PAGES_U8, "u4": ipv.IPV_PAGES_U4}
+
+
+# Small calls take as long as the host does, so the ones below check a tensor with few reads of its attributes, spell out what is
+# wrong only then (_packed and its like), and write a structure's fields at once. ctypes lays structures out as these do.
+_ROTATE = struct.Struct("@4P6qi4x3Pq").pack_into  # but eps
+_CHOOSE = struct.Struct("@P2q4iP2q").pack_into
+_ATTEND = struct.Struct("@3P4qi").pack_into  # the fields before scale
+_LISTS = struct.Struct("@Pi2q").pack_into
+
+
+def _fields(structure):
+    """A ctypes structure's memory, for these."""
+    return (ctypes.c_char * ctypes.sizeof(structure)).from_buffer(structure)
 
 
 def _need(ok: bool, what: str) -> None:
@@ -72,7 +86,7 @@ class PagedBatch:
         self.max_pages = 1 if table is None else table.shape[1]
         self.struct = ipv.Batch(n, self.max_pages, ipv._ptr(table), table_stride, ipv._ptr(row_start),
                                 ipv._ptr(kv_len), total_rows, max_rows, max_kv)
-        self.ref = ctypes.byref(self.struct)
+        self.ref, self.at = ctypes.byref(self.struct), ctypes.addressof(self.struct)
         self.sizes = (n, self.max_pages, total_rows, max_rows, max_kv)
 
 
@@ -92,7 +106,7 @@ class Rotary:
         self.table, self.sections, self.interleaved = table, sections, bool(interleaved)
         self.struct = ipv.RotaryDesc(table.data_ptr(), table.shape[0], table.shape[1], int(self.interleaved), len(sections),
                                      (ctypes.c_int * 4)(*sections))
-        self.ref = ctypes.byref(self.struct)
+        self.at = ctypes.addressof(self.struct)
 
     @classmethod
     def of_base(cls, base: float, n_positions: int, rot_dim: int, sections=None, interleaved: bool = False,
@@ -130,13 +144,13 @@ class PageBounds:
         self.codes, self.steps, self.page_size, self.head_dim = codes, steps, page_size, head_dim
         self.n_pages, self.n_kv_heads = codes.shape[:2]
         self.struct = ipv.BoundsDesc(self.n_kv_heads, head_dim, page_size, self.n_pages, codes.data_ptr(), steps.data_ptr())
-        self.ref = ctypes.byref(self.struct)
-        self._args, self._lib = ipv.ChooseArgs(), ipv.load()
-        self._args_ref = ctypes.byref(self._args)
+        self.at, self._lib = ctypes.addressof(self.struct), ipv.load()
+        self._args = ipv.ChooseArgs()
+        self._args_at, self._args_fields = ctypes.addressof(self._args), _fields(self._args)
 
     def update(self, cache: "PagedCache", batch: PagedBatch, stream=None) -> None:
         """ipv_bounds_update: the bounds of the pages that hold the batch's new rows, after these were written."""
-        status = self._lib.ipv_bounds_update(self.ref, cache.ref, batch.ref, ipv._stream(stream))
+        status = self._lib.ipv_bounds_update(self.at, cache.at, batch.at, ipv._stream(stream))
         if status:
             ipv._check(status)
 
@@ -146,19 +160,19 @@ class PageBounds:
         products with q, bf16 [total_rows, n_q_heads, head_dim]. int32 [total_rows, n_kv_heads, n_chosen], ascending,
         then -1; allocated if out is None, with -1 where a row belongs to no sequence. One host thread at a time
         uses the object."""
-        n_q_heads = q.shape[1] if q.dim() == 3 else 0
-        qs = PagedCache._packed("q", q, batch, n_q_heads, self.head_dim)
-        _fits(32, n_chosen=n_chosen, first=first, recent=recent)
+        shape, qs = q.shape, q.stride()
+        if (len(shape) != 3 or shape[0] < batch.total_rows or shape[2] != self.head_dim or q.dtype is not torch.bfloat16 or not q.is_cuda or
+                qs[2] != 1):
+            PagedCache._packed("q", q, batch, shape[1] if len(shape) == 3 else 0, self.head_dim)
+        if not (0 < n_chosen < 1 << 31 and 0 <= first < 1 << 31 and 0 < recent < 1 << 31):
+            raise ValueError(f"n_chosen {n_chosen}, first {first}, recent {recent}: n_chosen and recent must be positive, first at least 0, "
+                             "and fit 32 bits")
         at = ipv._stream(stream)
         if out is None:
-            _need(n_chosen >= 1, "n_chosen must be positive")
             out, = PagedCache._results(q, [(batch.total_rows, self.n_kv_heads, n_chosen)], stream, at, torch.int32, -1)
         os = _lists("out", out, batch, self.n_kv_heads, n_chosen)
-        a = self._args
-        a.q, a.q_row_stride, a.q_head_stride, a.n_q_heads = q.data_ptr(), qs[0], qs[1], n_q_heads
-        a.n_chosen, a.first, a.recent = n_chosen, first, recent
-        a.out, a.out_row_stride, a.out_head_stride = out.data_ptr(), os[0], os[1]
-        status = self._lib.ipv_bounds_choose(self.ref, batch.ref, self._args_ref, at)
+        _CHOOSE(self._args_fields, 0, q.data_ptr(), qs[0], qs[1], shape[1], n_chosen, first, recent, out.data_ptr(), os[0], os[1])
+        status = self._lib.ipv_bounds_choose(self.at, batch.at, self._args_at, at)
         if status:
             ipv._check(status)
         return out
@@ -167,8 +181,8 @@ class PageBounds:
 def _lists(name, t, batch, heads, n=None):
     """Strides of int32 [total_rows, heads, n] lists."""
     shape, strides = t.shape, t.stride()
-    if (t.dtype is not torch.int32 or not t.is_cuda or len(shape) != 3 or shape[0] < batch.total_rows or shape[1] != heads or
-            (n is not None and shape[2] != n) or (strides[2] != 1 and shape[2] > 1)):
+    if (len(shape) != 3 or shape[0] < batch.total_rows or shape[1] != heads or (n is not None and shape[2] != n) or
+            (strides[2] != 1 and shape[2] > 1) or t.dtype is not torch.int32 or not t.is_cuda):
         raise ValueError(f"{name} must be an int32 CUDA tensor [{batch.total_rows}, {heads}, {'n' if n is None else n}], contiguous "
                          "along its last dimension")
     return strides
@@ -237,10 +251,10 @@ class PagedCache:
                 _need(self._row_strides(t, 2 * groups) == rows, f"{name} must have k's strides, in rows")
         self.struct = ipv.PagesDesc(FORMATS[fmt], self.n_kv_heads, self.head_dim, self.page_size, self.n_pages, *rows,
                                     k.data_ptr(), v.data_ptr(), ipv._ptr(k_par), ipv._ptr(v_par))
-        self.ref = ctypes.byref(self.struct)
+        self.ref, self.at = ctypes.byref(self.struct), ctypes.addressof(self.struct)
         self._workspaces, self._calls, self._lib = {}, {}, ipv.load()
         self._rotate_args = ipv.RotateArgs()
-        self._rotate_ref = ctypes.byref(self._rotate_args)
+        self._rotate_at, self._rotate_fields = ctypes.addressof(self._rotate_args), _fields(self._rotate_args)
 
     @staticmethod
     def _row_strides(t, width):
@@ -359,31 +373,35 @@ class PagedCache:
         int32 [total_rows, n_kv_heads, n], columns of the batch's table, as PageBounds.choose gives them (a list
         shorter than the row's pages; entries that are none of them, -1 say, are skipped). q, out, lse, workspace and
         captured calls as in attend."""
-        n_q_heads = q.shape[1] if q.dim() == 3 else 0
-        qs = self._packed("q", q, batch, n_q_heads, self.head_dim)
-        cs = _lists("chosen", chosen, batch, self.n_kv_heads)
+        shape, qs = q.shape, q.stride()
+        n_q_heads = shape[1] if len(shape) == 3 else 0
+        if not n_q_heads or shape[0] < batch.total_rows or shape[2] != self.head_dim or q.dtype is not torch.bfloat16 or not q.is_cuda or qs[2] != 1:
+            self._packed("q", q, batch, n_q_heads, self.head_dim)
+        cs, n_chosen = _lists("chosen", chosen, batch, self.n_kv_heads), chosen.shape[2]
         at = ipv._stream(stream)
         if out is None:
-            out, = self._results(q, [q.shape], stream, at)
-        os = self._packed("out", out, batch, n_q_heads, self.head_dim)
+            out, = self._results(q, [shape], stream, at)
+        os = out.stride()
+        if out.shape != shape or out.dtype is not torch.bfloat16 or not out.is_cuda or os[2] != 1:
+            self._packed("out", out, batch, n_q_heads, self.head_dim)  # may be longer
         if lse is not None:
             self._check_lse(lse, batch, n_q_heads)
-        sizes = (batch.sizes, n_q_heads, chosen.shape[2])
+        sizes = (batch.sizes, n_q_heads, n_chosen)
         kept = self._calls.get(sizes)
         if kept is None:
-            _fits(32, n_chosen=chosen.shape[2])
+            _fits(32, n_chosen=n_chosen)
             args = ipv.AttendArgs(n_q_heads=n_q_heads, scale=1.0, causal=1)
-            lists = ipv.Chosen(n_chosen=chosen.shape[2])
-            kept = args, ctypes.byref(args), lists, ctypes.byref(lists), ipv.attend_chosen_workspace(self.ref, batch.ref, args, lists)
+            lists = ipv.Chosen(n_chosen=n_chosen)
+            need = ipv.attend_chosen_workspace(self.ref, batch.ref, args, lists)
+            kept = args, ctypes.addressof(args), _fields(args), lists, ctypes.addressof(lists), _fields(lists), need
             self._keep_call(sizes, kept)
-        args, ref, lists, lists_ref, need = kept
-        args.q, args.out, args.lse = q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr()
-        args.q_row_stride, args.q_head_stride, args.out_row_stride, args.out_head_stride = qs[0], qs[1], os[0], os[1]
+        args, args_at, args_fields, _, lists_at, lists_fields, need = kept
+        _ATTEND(args_fields, 0, q.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(), qs[0], qs[1], os[0], os[1], n_q_heads)
         args.scale = self.head_dim ** -0.5 if scale is None else scale
-        lists.pages, lists.row_stride, lists.head_stride = chosen.data_ptr(), cs[0], cs[1]
+        _LISTS(lists_fields, 0, chosen.data_ptr(), n_chosen, cs[0], cs[1])
         if need:
             self._give_workspace(args, need, workspace, stream, at, q.device)
-        status = self._lib.ipv_attend_chosen(self.ref, batch.ref, ref, lists_ref, at)
+        status = self._lib.ipv_attend_chosen(self.at, batch.at, args_at, lists_at, at)
         if status:
             ipv._check(status)
         return out
@@ -401,29 +419,35 @@ class PagedCache:
         (allocated if None, on the call's stream; q itself will do), which is returned. positions: int32
         [total_rows] or [axes, total_rows], places in the rotary's table: a row's place in the stream, which a
         compacted cache does not tell. weights: bf16 [head_dim]. One host thread at a time uses a cache object."""
-        n_q_heads = q.shape[1] if q.dim() == 3 else 0
-        qs = self._packed("q", q, batch, n_q_heads, self.head_dim)
-        strides = self._pair("k_new", k_new, "v_new", v_new, batch)
-        axes = len(rotary.sections)
-        if positions.dim() == 1 and axes == 1:
-            positions = positions[None]
-        if (positions.dtype is not torch.int32 or not positions.is_cuda or positions.dim() != 2 or positions.shape[0] != axes or
-                positions.shape[1] < batch.total_rows or (positions.stride(1) != 1 and positions.shape[1] > 1)):
-            raise ValueError(f"positions must be an int32 CUDA tensor [{axes}, {batch.total_rows}], contiguous along its last dimension")
+        rows, heads, dim, bf16 = batch.total_rows, self.n_kv_heads, self.head_dim, torch.bfloat16
+        shape, qs = q.shape, q.stride()
+        n_q_heads = shape[1] if len(shape) == 3 else 0
+        if not n_q_heads or shape[0] < rows or shape[2] != dim or q.dtype is not bf16 or not q.is_cuda or qs[2] != 1:
+            self._packed("q", q, batch, n_q_heads, dim)
+        new, strides = k_new.shape, k_new.stride()
+        if (new != (rows, heads, dim) or k_new.dtype is not bf16 or not k_new.is_cuda or strides[2] != 1 or v_new.shape != new or
+                v_new.dtype is not bf16 or not v_new.is_cuda or v_new.stride() != strides):
+            strides = self._pair("k_new", k_new, "v_new", v_new, batch)  # may be longer
+        at_shape, at_strides, axes = positions.shape, positions.stride(), len(rotary.sections)
+        if len(at_shape) == 1 and axes == 1:
+            at_shape, at_strides = (1, at_shape[0]), (at_shape[0], at_strides[0])
+        if (len(at_shape) != 2 or at_shape[0] != axes or at_shape[1] < rows or (at_strides[1] != 1 and at_shape[1] > 1) or
+                positions.dtype is not torch.int32 or not positions.is_cuda):
+            raise ValueError(f"positions must be an int32 CUDA tensor [{axes}, {rows}], contiguous along its last dimension")
         for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-            if w is not None and (w.dtype is not torch.bfloat16 or not w.is_cuda or w.shape != (self.head_dim,) or not w.is_contiguous()):
-                raise ValueError(f"{name} must be a contiguous bf16 CUDA tensor [{self.head_dim}]")
+            if w is not None and (w.dtype is not bf16 or not w.is_cuda or w.shape != (dim,) or not w.is_contiguous()):
+                raise ValueError(f"{name} must be a contiguous bf16 CUDA tensor [{dim}]")
         at = ipv._stream(stream)
         if q_out is None:
-            q_out, = self._results(q, [q.shape], stream, at)
-        os = self._packed("q_out", q_out, batch, n_q_heads, self.head_dim)
-        a = self._rotate_args
-        a.q, a.q_out, a.k_new, a.v_new = q.data_ptr(), q_out.data_ptr(), k_new.data_ptr(), v_new.data_ptr()
-        a.q_row_stride, a.q_head_stride, a.out_row_stride, a.out_head_stride = qs[0], qs[1], os[0], os[1]
-        a.row_stride, a.head_stride, a.n_q_heads, a.eps = strides[0], strides[1], n_q_heads, eps
-        a.q_weight, a.k_weight = ipv._ptr(q_weight), ipv._ptr(k_weight)
-        a.positions, a.positions_stride = positions.data_ptr(), positions.stride(0)
-        status = self._lib.ipv_pages_write_rotated(self.ref, batch.ref, rotary.ref, self._rotate_ref, at)
+            q_out, = self._results(q, [shape], stream, at)
+        os = q_out.stride()
+        if q_out.shape != shape or q_out.dtype is not bf16 or not q_out.is_cuda or os[2] != 1:
+            self._packed("q_out", q_out, batch, n_q_heads, dim)  # may be longer
+        _ROTATE(self._rotate_fields, 0, q.data_ptr(), q_out.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), qs[0], qs[1], os[0], os[1],
+                strides[0], strides[1], n_q_heads, 0 if q_weight is None else q_weight.data_ptr(),
+                0 if k_weight is None else k_weight.data_ptr(), positions.data_ptr(), at_strides[0])
+        self._rotate_args.eps = eps
+        status = self._lib.ipv_pages_write_rotated(self.at, batch.at, rotary.at, self._rotate_at, at)
         if status:
             ipv._check(status)
         return q_out
@@ -431,11 +455,13 @@ class PagedCache:
     def copy_pages(self, source, target, stream=None) -> None:
         """ipv_pages_copy: page target[i] becomes a copy of page source[i], int32 CUDA tensors [n]. No page is in target
         twice, or in target and at another place in source."""
+        n = source.shape
         for name, t in (("source", source), ("target", target)):
-            _need(t.dtype is torch.int32 and t.is_cuda and t.dim() == 1 and (t.stride(0) == 1 or t.shape[0] <= 1),
-                  f"{name} must be a contiguous int32 CUDA tensor [n]")
-        _need(source.shape == target.shape, "source and target must have one length")
-        status = self._lib.ipv_pages_copy(self.ref, source.data_ptr(), target.data_ptr(), source.shape[0], ipv._stream(stream))
+            if t.dtype is not torch.int32 or not t.is_cuda or len(t.shape) != 1 or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous int32 CUDA tensor [n]")
+        if target.shape != n:
+            raise ValueError("source and target must have one length")
+        status = self._lib.ipv_pages_copy(self.at, source.data_ptr(), target.data_ptr(), n[0], ipv._stream(stream))
         if status:
             ipv._check(status)
 
@@ -446,12 +472,11 @@ class PagedCache:
         are read."""
         kept_strides = (0, 0)
         if kept is not None:
-            _need(kept.dtype is torch.int32 and kept.is_cuda and kept.dim() == 3 and kept.shape[0] >= batch.n_seqs and
-                  kept.shape[1] == self.n_kv_heads and kept.shape[2] >= min(batch.max_rows, batch.total_rows) and
-                  (kept.stride(2) == 1 or kept.shape[2] <= 1),
-                  "kept must be an int32 CUDA tensor [n_seqs, n_kv_heads, max_rows], contiguous along its last dimension")
-            kept_strides = kept.stride()[:2]
-        status = self._lib.ipv_pages_gather(source.ref, source_batch.ref, self.ref, batch.ref, ipv._ptr(kept), kept_strides[0],
+            shape, kept_strides = kept.shape, kept.stride()
+            if (len(shape) != 3 or shape[0] < batch.n_seqs or shape[1] != self.n_kv_heads or shape[2] < min(batch.max_rows, batch.total_rows) or
+                    (kept_strides[2] != 1 and shape[2] > 1) or kept.dtype is not torch.int32 or not kept.is_cuda):
+                raise ValueError("kept must be an int32 CUDA tensor [n_seqs, n_kv_heads, max_rows], contiguous along its last dimension")
+        status = self._lib.ipv_pages_gather(source.at, source_batch.at, self.at, batch.at, ipv._ptr(kept), kept_strides[0],
                                             kept_strides[1], ipv._stream(stream))
         if status:
             ipv._check(status)

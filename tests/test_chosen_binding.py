@@ -1,5 +1,7 @@
 """The binding of rotated writes, page bounds, chosen pages, copies and gathers on the CPU: what it passes to the
 library, and what it refuses before anything is passed. Tensors and streams are stand-ins, as in test_paged_binding.py."""
+import ctypes
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -15,16 +17,26 @@ def built():
     ipv_build.build()
 
 
+PAGES, BATCH = ipv.PagesDesc, ipv.Batch
+STRUCTURES = {  # what a call's first arguments point to
+    "ipv_pages_write_rotated": (PAGES, BATCH, ipv.RotaryDesc, ipv.RotateArgs), "ipv_bounds_update": (ipv.BoundsDesc, PAGES, BATCH),
+    "ipv_bounds_choose": (ipv.BoundsDesc, BATCH, ipv.ChooseArgs), "ipv_attend_chosen": (PAGES, BATCH, ipv.AttendArgs, ipv.Chosen),
+    "ipv_attend": (PAGES, BATCH, ipv.AttendArgs), "ipv_pages_copy": (PAGES,), "ipv_pages_gather": (PAGES, BATCH, PAGES, BATCH)}
+
+
 class Library:
-    """Notes what it is given; structures as dicts."""
+    """Notes what it is given; structures, by reference or address, as dicts."""
 
     def __init__(self, log):
         self.log = log
 
     def __getattr__(self, name):
         def call(*args):
-            read = [{f: getattr(a._obj, f) for f, _ in a._obj._fields_} if hasattr(a, "_obj") else a for a in args]
-            self.log.append((name, *read))
+            read = []
+            for a, cls in zip(args, STRUCTURES[name]):
+                x = a._obj if hasattr(a, "_obj") else cls.from_address(a)
+                read.append({f: getattr(x, f) for f, _ in cls._fields_})
+            self.log.append((name, *read, *args[len(read):]))
             return 0
         return call
 
@@ -67,10 +79,14 @@ def test_what_a_rotated_write_passes(world):
     assert args["q_out"] == out.data_ptr() and args["out_row_stride"] == 256 and out.shape == (3, 4, 64)
     assert (args["k_new"], args["v_new"], args["row_stride"], args["head_stride"]) == (w.k.data_ptr(), w.v.data_ptr(), 128, 64)
     assert (args["q_weight"], args["k_weight"], args["eps"]) == (weight.data_ptr(), None, 0.5)
+    longer = [w.rows(5, 4, 64), w.rows(5, 2, 64), w.rows(5, 2, 64)]  # packed tensors may be longer than the batch
+    w.cache.write_rotated(*longer, w.batch, w.rotary, positions, q_out=w.rows(9, 4, 64))
+    assert w.log[-1][4]["q"] == longer[0].data_ptr() and w.log[-1][4]["eps"] == ctypes.c_float(1e-6).value
     assert args["positions"] == positions.data_ptr() + 8 and args["positions_stride"] == 9
     assert list(rotary["sections"])[:3] == [16, 8, 8] and rotary["n_axes"] == 3 and rotary["n_positions"] == 100 and rotary["rot_dim"] == 64
     assert ("used on", out.data_ptr(), 0) in w.log  # made on the call's stream
-    w.cache.write_rotated(w.q, w.k, w.v, w.batch, Rotary(gpu(torch.zeros(9, 32)), interleaved=True), w.at[0], q_out=w.q)
+    other = Rotary(gpu(torch.zeros(9, 32)), interleaved=True)
+    w.cache.write_rotated(w.q, w.k, w.v, w.batch, other, w.at[0], q_out=w.q)
     _, _, _, rotary, args, stream = w.log[-1]
     assert stream == 0 and args["q_out"] == args["q"] == w.q.data_ptr() and args["q_weight"] is None
     assert list(rotary["sections"])[:1] == [16] and rotary["interleaved"] == 1 and rotary["n_axes"] == 1
