@@ -67,8 +67,7 @@ struct Layout {
   static constexpr int kThreads = 32 * kWarps;
   static constexpr int kRing = kHalves ? 3 * Ring<FMT, DP>::kTile : Ring<FMT, DP>::kStage * Ring<FMT, DP>::kStages;  // of a warp
   static constexpr int kRings = kRing * kWarps;
-  static constexpr int kResults = kRings + kWarps * 8 * NR * (DP + 4 + 2) * 4;  // and the warps' results
-  static constexpr int kBytes = kResults + (CHOSEN ? kWarps * 3 * 4 : 0);      // and which keys are seen
+  static constexpr int kBytes = kRings + kWarps * 8 * NR * (DP + 4 + 2) * 4;  // and the warps' results
 };
 
 // Where 16-byte chunk c of key row r lies in its row: the rows that a quarter
@@ -253,33 +252,15 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
   const int my_r = lane / kCh, my_c = lane % kCh;
   const int64_t v_from_k = a.p.v - a.p.k;
   const int64_t page_bytes = a.p.page_stride * a.p.row_bytes, next_bytes = a.p.row_stride * a.p.row_bytes;
-  // Which keys of a stage's step are seen, a word for each; CHOSEN only.
-  uint32_t* sees = reinterpret_cast<uint32_t*>(smem + L::kResults) + warp * 3;
-  // This lane's key of step i of run x: its page, -1: none (CHOSEN, kUnseen: not seen). Read a step ahead of
-  // the copies.
-  constexpr int kUnseen = -2;
+  // This lane's key of step i of run x: its page, -1: none. Read a step ahead of the copies.
   auto page_of = [&](const W& x, int i) {
     const int j = x.t.kr.template key0<kRowsStep>(i) + lane;
     int pg = -1;
-    if constexpr (CHOSEN) {
-      if (i >= x.s + x.n || j >= x.t.kr.hi_max) return kUnseen;
-      const int tok = a.by_share(x.t.row0), hi = token_hi(a, x.t.seq, tok);
-      const int c = a.chosen[(x.t.seq.row0 + static_cast<int64_t>(tok)) * a.chosen_row + x.head * a.chosen_head + (j >> a.p.page_shift)];
-      if (static_cast<unsigned>(c) >= static_cast<unsigned>(pages_seen(a, x.t.seq, tok))) return kUnseen;
-      if (a.p.page_shift != 31 && (c << a.p.page_shift) + (j & (a.p.page_size - 1)) >= hi) return kUnseen;
-      if (a.p.page_shift == 31 && j >= hi) return kUnseen;
-      pg = a.p.table ? a.p.table[x.t.b * a.p.table_stride + c] : x.t.b;
-      return static_cast<unsigned>(pg) < static_cast<unsigned>(a.p.n_pages) ? pg : -1;
-    }
     if (i < x.s + x.n && j < x.t.kr.hi_max) pg = a.p.table ? a.p.table[x.t.b * a.p.table_stride + (j >> a.p.page_shift)] : x.t.b;
     return static_cast<unsigned>(pg) < static_cast<unsigned>(a.p.n_pages) ? pg : -1;
   };
   auto issue = [&](const W& x, int i, int pg, int stage) {
     const uint32_t base = ring + stage * R::kStage;
-    if constexpr (CHOSEN) {
-      const uint32_t seen = __ballot_sync(0xffffffffu, pg != kUnseen);
-      if (lane == 0) sees[stage] = seen;
-    }
     const int j = x.t.kr.template key0<kRowsStep>(i) + lane;
     const int64_t head_rows = x.head * a.p.head_stride;
     const int64_t off = pg < 0 ? int64_t{-1}
@@ -302,44 +283,93 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
       copy16(dst + R::kTile, src + v_from_k, ok);
     }
   };
-  // Halves: where this lane's key of step i lies (-1: nowhere, reads as zero), and the copies of one step's K or V
-  // into one half, with which of the keys are seen.
-  auto row_at = [&](const W& x, int i, int pg) {
-    if (pg < 0) return int64_t{-1};
-    const int j = x.t.kr.template key0<kRowsStep>(i) + lane;
-    return x.head * a.p.head_stride * a.p.row_bytes + pg * page_bytes + (a.p.page_shift == 31 ? j : j & (a.p.page_size - 1)) * next_bytes;
-  };
-  auto copy_half = [&](const char* from, int64_t off, int half) {
-#pragma unroll
-    for (int u = 0; u < kCh; ++u) {
-      const int r = u * kApart + my_r;
-      const int64_t at = __shfl_sync(0xffffffffu, off, r);
-      const bool ok = at >= 0 && my_c < nch;
-      copy16(ring + half * R::kTile + r * R::kRowB + swizzle<FMT, R::kRowB>(r, my_c) * 16, ok ? from + my_c * 16 + at : from, ok);
+  // Chosen pages: 16 keys of a step lie in one page. Lane l looks up the page (-1: none of the pool, its rows read as zero),
+  // and how many of its keys are seen, of keys (l & 16).. of this warp's step k0 + (l & 15): two dependent loads
+  // for 16 steps, no 64-bit products and few shuffles for each.
+  int page_l = -1, seen_l = 0;
+  auto look_up = [&](const W& x, int k0) {
+    const int i = x.s + warp + (k0 + (lane & 15)) * kWarps, j = x.t.kr.template key0<kRowsStep>(i) + (lane & 16);
+    page_l = -1, seen_l = 0;
+    if (i < x.s + x.n && j < x.t.kr.hi_max) {
+      const int tok = a.by_share(x.t.row0), hi = token_hi(a, x.t.seq, tok);
+      const int c = a.chosen[(x.t.seq.row0 + static_cast<int64_t>(tok)) * a.chosen_row + x.head * a.chosen_head + (j >> a.p.page_shift)];
+      if (static_cast<unsigned>(c) < static_cast<unsigned>(pages_seen(a, x.t.seq, tok))) {
+        const int pg = a.p.table ? a.p.table[x.t.b * a.p.table_stride + c] : x.t.b;
+        if (static_cast<unsigned>(pg) < static_cast<unsigned>(a.p.n_pages)) page_l = pg;
+        seen_l = a.p.page_shift == 31 ? hi : min(hi - (c << a.p.page_shift), a.p.page_size);
+      }
     }
   };
-  auto note = [&](int pg, int word) {
-    const uint32_t seen = __ballot_sync(0xffffffffu, pg != kUnseen);
-    if (lane == 0) sees[word] = seen;
+  // Where the two halves of this warp's step k lie, how many of their 16 rows are to be copied, which keys are seen.
+  struct Halves {
+    int64_t at[2];
+    int n[2];
+    uint32_t seen;
   };
-  int64_t v_off = -1;  // of the step whose K was copied last
+  auto halves = [&](const W& x, int k) {
+    Halves h;
+    h.seen = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int pg = __shfl_sync(0xffffffffu, page_l, (k & 15) + 16 * i), upto = __shfl_sync(0xffffffffu, seen_l, (k & 15) + 16 * i);
+      const int j = x.t.kr.template key0<kRowsStep>(x.s + warp + k * kWarps) + 16 * i;
+      const int in = a.p.page_shift == 31 ? j : j & (a.p.page_size - 1), n = min(max(upto - in, 0), 16);
+      h.n[i] = pg < 0 ? 0 : n;
+      h.at[i] = x.head * a.p.head_stride * a.p.row_bytes + pg * page_bytes + in * next_bytes;
+      h.seen |= ((1u << n) - 1u) << (16 * i);
+    }
+    return h;
+  };
+  const int64_t lane_at = my_r * next_bytes + my_c * 16;
+  const int lane_row = my_c < nch ? my_r : 16;  // 16: never copied
+  auto copy_rows = [&](const char* from, uint32_t to, const Halves& h) {
+#pragma unroll
+    for (int u = 0; u < kCh; ++u) {
+      const int half = u * kApart / 16, r = u * kApart % 16;
+      const bool ok = lane_row + r < h.n[half];
+      copy16(to + (u * kApart + my_r) * R::kRowB + swizzle<FMT, R::kRowB>(u * kApart + my_r, my_c) * 16,
+             ok ? from + (h.at[half] + r * next_bytes + lane_at) : from, ok);
+    }
+  };
+  auto issue_chosen = [&](const Halves& h, int stage) {
+    const uint32_t base = ring + stage * R::kStage;
+    if constexpr (!kB) {
+      constexpr int kN = R::kG * 4;
+      const bool ok = (lane & 15) < (lane < 16 ? h.n[0] : h.n[1]);
+      const int64_t at = ok ? ((lane < 16 ? h.at[0] : h.at[1]) + (lane & 15) * next_bytes) / (R::kRowB / kN) : 0;
+      copy_small<kN>(base + 2 * R::kTile + lane * kN, reinterpret_cast<const char*>(a.p.k_par) + at, ok);
+      copy_small<kN>(base + 2 * R::kTile + R::kPar + lane * kN, reinterpret_cast<const char*>(a.p.v_par) + at, ok);
+    }
+    copy_rows(a.p.k, base, h);
+    copy_rows(a.p.v, base + R::kTile, h);
+  };
+  uint32_t seen_now = 0, seen_next = 0, seen_last = 0;  // keys of the step at hand and of the ones after it
   // The first steps of a run, and the page of the one after them.
   int page_next = -1;
   auto fill = [&](const W& x) {
-    if constexpr (L::kHalves) {  // K and V of the first step, K of the second
-      const int i0 = x.s + warp, i1 = i0 + kWarps, end = x.s + x.n;
-      const int pg0 = page_of(x, i0), pg1 = page_of(x, i1);
-      page_next = page_of(x, i1 + kWarps);
-      const int64_t off = row_at(x, i0, pg0);
-      v_off = row_at(x, i1, pg1);
-      note(pg0, 0);
-      note(pg1, 1);
-      if (i0 < end) copy_half(a.p.k, off, 0);
-      copy_commit();
-      if (i0 < end) copy_half(a.p.v, off, 1);
-      copy_commit();
-      if (i1 < end) copy_half(a.p.k, v_off, 2);
-      copy_commit();
+    if constexpr (CHOSEN) {
+      look_up(x, 0);
+      const int end = x.n - warp;  // steps of the run from this warp's first on
+      const Halves h0 = halves(x, 0);
+      seen_now = h0.seen;
+      if constexpr (L::kHalves) {  // K and V of the first step, K of the second
+        const Halves h1 = halves(x, 1);
+        seen_next = h1.seen;
+        if (end > 0) copy_rows(a.p.k, ring, h0);
+        copy_commit();
+        if (end > 0) copy_rows(a.p.v, ring + R::kTile, h0);
+        copy_commit();
+        if (end > kWarps) copy_rows(a.p.k, ring + 2 * R::kTile, h1);
+        copy_commit();
+      } else {
+#pragma unroll
+        for (int i = 0; i < R::kStages - 1; ++i) {
+          const Halves h = i == 0 ? h0 : halves(x, i);
+          if (i == 1) seen_next = h.seen;
+          if (end > i * kWarps) issue_chosen(h, i);
+          copy_commit();
+        }
+      }
     } else {
       int pages[R::kStages];  // all on their way at once
 #pragma unroll
@@ -464,10 +494,19 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
 
     // ---- the loop over this warp's steps
     int stage = 0;
-    int k_half = 0, v_half = 1, next_half = 2, word = 0;  // halves: where K, V and the next step's K are, and the word of sees
+    int k_half = 0, v_half = 1, next_half = 2;  // halves: where K, V and the next step's K are
+    int k = 0;                                  // chosen pages: which of this warp's steps it is
     for (int step = first; step < s_end; step += kWarps) {
       if constexpr (L::kHalves) {
         copy_wait<2>();
+      } else if constexpr (CHOSEN) {
+        constexpr int kAhead = R::kStages - 1;
+        if ((k + kAhead) % 16 == 0) look_up(w, k + kAhead);
+        const Halves h = halves(w, k + kAhead);
+        if (step + kAhead * kWarps < s_end) issue_chosen(h, stage == 0 ? kAhead : stage - 1);
+        if (kAhead == 1) seen_next = h.seen; else seen_last = h.seen;
+        copy_commit();
+        copy_wait<kAhead>();
       } else {
         const int ahead = step + (R::kStages - 1) * kWarps;
         const int to = stage == 0 ? R::kStages - 1 : stage - 1;
@@ -562,18 +601,17 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
       }
       if constexpr (L::kHalves) {  // K has been read: the next step's V comes in its place
         __syncwarp();
-        if (step + kWarps < s_end) copy_half(a.p.v, v_off, k_half);
+        if (step + kWarps < s_end) copy_rows(a.p.v, ring + k_half * R::kTile, halves(w, k + 1));
         copy_commit();
       }
       // The mask, only where some row of the tile does not see all 32 keys.
       if constexpr (CHOSEN) {
-        const uint32_t seen = sees[L::kHalves ? word : stage];
-        if (seen != 0xffffffffu) {
+        if (seen_now != 0xffffffffu) {
 #pragma unroll
           for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              if (!(seen >> (mt * 16 + key_at<FMT>(g) + (i >> 1) * 8) & 1u))
+              if (!(seen_now >> (mt * 16 + key_at<FMT>(g) + (i >> 1) * 8) & 1u))
 #pragma unroll
                 for (int nr = 0; nr < NR; ++nr) sc[mt][nr][i] = kNegInf;
         }
@@ -745,18 +783,18 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
       }
       __syncwarp();  // the stage is read before its next copies are issued
       if constexpr (L::kHalves) {  // K of the step after the next one in V's place
-        const int ahead = step + 2 * kWarps;
-        v_off = row_at(w, ahead, page_next);
-        word = word == 2 ? 0 : word + 1;
-        note(page_next, word == 2 ? 0 : word + 1);
-        if (ahead < s_end) copy_half(a.p.k, v_off, v_half);
+        if ((k + 2) % 16 == 0) look_up(w, k + 2);
+        const Halves h = halves(w, k + 2);
+        if (step + 2 * kWarps < s_end) copy_rows(a.p.k, ring + v_half * R::kTile, h);
         copy_commit();
-        page_next = page_of(w, ahead + kWarps);
+        seen_now = seen_next, seen_next = h.seen;
         const int free = v_half;
         v_half = k_half, k_half = next_half, next_half = free;
       } else {
         stage = stage + 1 == R::kStages ? 0 : stage + 1;
+        if constexpr (CHOSEN) seen_now = seen_next, seen_next = seen_last;
       }
+      ++k;
     }
     // The next run's first steps are on their way while this one's results are joined.
     const bool partial = !(w.starts() && w.ends());
@@ -856,7 +894,7 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
       float2 ml[kCluster];
       float4 y[kCluster];
 #pragma unroll
-      for (int k = 0; k < kCluster; ++k) ml[k] = far64(in_block(row_at + DP * 4, k));
+      for (int k = 0; k < kCluster; ++k) ml[k] = k < a.cluster ? far64(in_block(row_at + DP * 4, k)) : make_float2(kNegInf, 0.0f);
 #pragma unroll
       for (int k = 0; k < kCluster; ++k)  // a block without steps has left no sums
         y[k] = ml[k].y == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : far128(in_block(row_at + c * 4, k));
