@@ -249,10 +249,10 @@ constexpr int64_t kClusterKeys = 8192, kClusterBytes = 1 << 20;
 // Chosen pages: from this many row tiles and heads per block on, blocks take them whole and in turn, which keeps the
 // blocks that run at the same time near one another in the cache (and in L2) and leaves nothing to join.
 constexpr int kApartItems = 4;
-// Below that, 4 or 2 blocks take a tile each as a cluster where they all have room at once, or one does where that fills three
-// quarters of the room: no parts to write, no second kernel. Lists of 2048 keys, 8 KV heads, 4 bits: 8 streams 13.0 us
-// against 17.2 shared out, 24 streams 24.8 against 28.4 (two blocks each) and 32.5 (one), 48 streams 38.5 (one) against 44.7; bf16:
-// 4 streams 10.6 against 12.4, 16 streams 26.6 (one) against 30.3.
+// Below that, 4 or 2 blocks take a tile each as a cluster where they all have room at once, or one where two have not: no
+// parts to write, no second kernel. Lists of 2048 keys, 8 KV heads, 4 bits: 8 streams 13.0 us against 17.2 shared out, 24
+// streams 24.8 against 28.4 (two blocks each), 32 streams 27.2 against 32.8 (one); bf16: 4 streams 10.6 against 12.4, 12 streams
+// 21.4 against 25.1 (one). More tiles than blocks are shared out.
 
 // Which kernel takes the call, on how many blocks, and the workspace.
 struct Plan {
@@ -326,8 +326,7 @@ void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
     }
     int c = 4;
     while (c > 1 && items * c > plan->blocks) c /= 2;
-    if (items * c <= plan->blocks && (c > 1 ? span <= kClusterKeys && span * p.row_bytes <= kClusterBytes
-                                            : items * 4 >= static_cast<int64_t>(plan->blocks) * 3)) {
+    if (items * c <= plan->blocks && (c == 1 || (span <= kClusterKeys && span * p.row_bytes <= kClusterBytes))) {
       a->unit = 0;
       a->cluster = c;
       plan->blocks = static_cast<int>(items) * c;
