@@ -92,6 +92,9 @@ __device__ __forceinline__ int key_at(int i) {
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool ok) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void copy16_at(uint32_t dst, const char* src, int offset) {  // a constant offset
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src + offset) : "memory");
+}
 template <int N>
 __device__ __forceinline__ void copy_small(uint32_t dst, const void* src, bool ok) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(N), "r"(ok ? N : 0) : "memory");
@@ -322,13 +325,24 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
   };
   const int64_t lane_at = my_r * next_bytes + my_c * 16;
   const int lane_row = my_c < nch ? my_r : 16;  // 16: never copied
+  // Rows without gaps and all there, as most: offsets that are known here, one instruction or two for each copy.
+  const bool dense = next_bytes == R::kRowB && a.p.row_bytes == R::kRowB;
   auto copy_rows = [&](const char* from, uint32_t to, const Halves& h) {
+    if (dense && min(h.n[0], h.n[1]) == 16) {
+      const char* src[2] = {from + h.at[0] + lane_at, from + h.at[1] + lane_at};
 #pragma unroll
+      for (int u = 0; u < kCh; ++u)
+        copy16_at(to + (u * kApart + my_r) * R::kRowB + swizzle<FMT, R::kRowB>(u * kApart + my_r, my_c) * 16, src[u * kApart / 16],
+                  u * kApart % 16 * R::kRowB);
+      return;
+    }
+#pragma unroll 1
     for (int u = 0; u < kCh; ++u) {
-      const int half = u * kApart / 16, r = u * kApart % 16;
-      const bool ok = lane_row + r < h.n[half];
+      const bool up = u * kApart >= 16;
+      const int r = u * kApart - (up ? 16 : 0);
+      const bool ok = lane_row + r < (up ? h.n[1] : h.n[0]);
       copy16(to + (u * kApart + my_r) * R::kRowB + swizzle<FMT, R::kRowB>(u * kApart + my_r, my_c) * 16,
-             ok ? from + (h.at[half] + r * next_bytes + lane_at) : from, ok);
+             ok ? from + ((up ? h.at[1] : h.at[0]) + r * next_bytes + lane_at) : from, ok);
     }
   };
   auto issue_chosen = [&](const Halves& h, int stage) {
