@@ -217,6 +217,7 @@ struct RotateArgs {
   const uint16_t* q_weight;  // norms' weights, or NULL
   const uint16_t* k_weight;
   float eps, by_dim;
+  int row_warps_shift;       // 1, 2 or 4 warps for a row: 0, 1 or 2
 };
 cudaError_t launch_rotate(const RotateArgs& a, cudaStream_t st);
 

@@ -2,18 +2,21 @@
 // rotated by their positions in one pass, queries to the packed result, keys and
 // values to their pages (quantised as paged_rows.cu does).
 //
-// HBM-bound: a row is read once and written once. 8 lanes take a head of a row,
-// lane c the 16-byte chunks c and c + 8, so that with all of 128 channels rotated in
-// halves a lane has both ends of its pairs; elsewhere the partners come by shuffles.
-// A block takes one row: its lanes fetch their cosines and sines once, and use them
-// for all the heads that they take.
+// A row is read once and written once. 8 lanes take a head of a row, lane c the
+// 16-byte chunks c and c + 8, so that with all of 128 channels rotated in halves a
+// lane has both ends of its pairs; elsewhere the partners come by shuffles. 1, 2 or 4
+// warps take a row: their lanes fetch its cosines and sines once and use them for
+// all the heads that they take, the next four heads on their way meanwhile. 16 frames
+// (59 MB, 9 us at the copy rate) take 13.2 us; issue slots, at about 300
+// instructions per four heads, and the look-ups at a row's start (position, then angles;
+// sequence, then page). 80 registers: at 64 it spills (16.3 us).
 #include "paged_codes.cuh"
 
 namespace ipv {
 namespace {
 
 constexpr int kBlock = 128;
-constexpr int kTeams = kBlock / 8;
+constexpr int kBlockWarps = kBlock / 32;
 
 // Pairs of channels: (i, i + 64) of 128, (i, i + rot / 2) of the first rot, (2i, 2i + 1).
 enum : int { kOwn = 0, kHalves = 1, kNeighbours = 2 };
@@ -52,13 +55,14 @@ __device__ __forceinline__ uint4 pack(const float (&y)[8]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// A head's row, chunks c and c + 8 of it in x: normalised with w (NULL: not), rotated. For whole warps.
+// A head's row, chunks c and c + 8 of it in x: normalised with w (NULL: not), rotated. For whole warps, of which some
+// teams may have queries, some keys, and one kind no norm.
 template <int PAIRS>
 __device__ __forceinline__ void rotate(const RotateArgs& a, uint4 (&x)[2], const uint16_t* w, const Turn (&turn)[2], int c) {
   float y[2][8];
   unpack(x[0], y[0]);
   unpack(x[1], y[1]);
-  if (w) {
+  if (a.q_weight || a.k_weight) {
     float sum = 0.0f;
 #pragma unroll
     for (int g = 0; g < 2; ++g)
@@ -69,7 +73,7 @@ __device__ __forceinline__ void rotate(const RotateArgs& a, uint4 (&x)[2], const
     const float inv = rsqrtf(sum * a.by_dim + a.eps);
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      if (8 * (c + 8 * g) >= a.p.dim) continue;
+      if (!w || 8 * (c + 8 * g) >= a.p.dim) continue;
       float v[8];
       unpack(*reinterpret_cast<const uint4*>(w + 8 * (c + 8 * g)), v);
 #pragma unroll
@@ -157,13 +161,14 @@ __device__ __forceinline__ int sequence_of(const Pages& p, int64_t row) {
 }
 
 template <int FMT, int PAIRS>
-__global__ void __launch_bounds__(kBlock, PAIRS == kOwn ? 8 : 4) rotate_kernel(RotateArgs a) {
+__global__ void __launch_bounds__(kBlock, PAIRS == kOwn ? 6 : 4) rotate_kernel(RotateArgs a) {
   pdl_trigger();
   pdl_wait();
-  const int64_t row = blockIdx.x;
+  const int warp = threadIdx.x >> 5, shift = a.row_warps_shift, row_warps = 1 << shift;
+  const int64_t row = blockIdx.x * static_cast<int64_t>(kBlockWarps >> shift) + (warp >> shift);
   const int c = threadIdx.x & 7, items = a.q_heads + a.p.heads;
-  const int first = (threadIdx.x >> 5) * 4, mine = (threadIdx.x & 31) >> 3;  // a warp's items, the team's among them
-  if (first >= items) return;
+  const int first = (warp & (row_warps - 1)) * 4, mine = (threadIdx.x & 31) >> 3;  // a warp's items, the team's among them
+  if (first >= items || row >= a.p.total_rows) return;
   auto load = [&](const uint16_t* from, uint4 (&x)[2], bool in) {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
@@ -195,42 +200,35 @@ __global__ void __launch_bounds__(kBlock, PAIRS == kOwn ? 8 : 4) rotate_kernel(R
   }
   const int b = sequence_of(a.p, row);
   const Seq s = sequence(a.p, b);
-  if (row < s.row0 || row >= s.row0 + static_cast<int64_t>(s.n)) return;  // the same for the block
+  if (row < s.row0 || row >= s.row0 + static_cast<int64_t>(s.n)) return;  // the same for the warp
   const int j = s.len - s.n + static_cast<int>(row - s.row0);
-  for (int base = first; base < items; base += kTeams) {  // the same for a whole warp
+  for (int base = first; base < items; base += 4 * row_warps) {  // the same for a whole warp
     const int item = base + mine, h = item - a.q_heads;
     const bool in = item < items, q = in && h < 0;
-    if (base > first) load_item(base, x, v);
+    uint4 x_next[2] = {}, v_next[2] = {};
+    if (base + 4 * row_warps < items) load_item(base + 4 * row_warps, x_next, v_next);
     int64_t to = -1;
     if (base + 4 > a.q_heads) {
       if (in && !q && j >= 0) to = pool_row(a.p, b, j);
       if (to >= 0) to += h * a.p.head_stride;
       store<FMT>(a.p, a.p.v, a.p.v_par, to, v, c);
     }
-    // Norms are of all heads of a kind or of none; a warp may have both kinds.
-    const uint16_t* w = q ? a.q_weight : a.k_weight;
-    if (a.q_weight && a.k_weight) {
-      rotate<PAIRS>(a, x, w, turn, c);
-    } else if (!a.q_weight && !a.k_weight) {
-      rotate<PAIRS>(a, x, nullptr, turn, c);
-    } else {
-      uint4 y[2] = {x[0], x[1]};
-      rotate<PAIRS>(a, x, a.q_weight ? a.q_weight : a.k_weight, turn, c);
-      rotate<PAIRS>(a, y, nullptr, turn, c);
-      if (!w) x[0] = y[0], x[1] = y[1];
-    }
+    rotate<PAIRS>(a, x, q ? a.q_weight : a.k_weight, turn, c);
     if (q) {
 #pragma unroll
       for (int g = 0; g < 2; ++g)
         if (8 * (c + 8 * g) < a.p.dim) *reinterpret_cast<uint4*>(a.q_out + row * a.out_row + item * a.out_head + 8 * (c + 8 * g)) = x[g];
     }
     if (base + 4 > a.q_heads) store<FMT>(a.p, a.p.k, a.p.k_par, to, x, c);
+#pragma unroll
+    for (int g = 0; g < 2; ++g) x[g] = x_next[g], v[g] = v_next[g];
   }
 }
 
 template <int FMT>
 cudaError_t launch(const RotateArgs& a, cudaStream_t st) {
-  const dim3 g(static_cast<unsigned>(a.p.total_rows));
+  const int rows = kBlockWarps >> a.row_warps_shift;
+  const dim3 g(static_cast<unsigned>((a.p.total_rows + rows - 1) / rows));
   if (a.neighbours) return launch_next(rotate_kernel<FMT, kNeighbours>, g, kBlock, 0, st, a);
   if (a.rot == 128) return launch_next(rotate_kernel<FMT, kOwn>, g, kBlock, 0, st, a);
   return launch_next(rotate_kernel<FMT, kHalves>, g, kBlock, 0, st, a);
