@@ -58,6 +58,12 @@ struct Share {
   int64_t at, left;
 };
 
+// 64-bit numbers that mostly fit 32 bits.
+__device__ __forceinline__ int64_t divide(int64_t x, int64_t d) {
+  if (static_cast<uint64_t>(x | d) >> 32 == 0) return static_cast<uint32_t>(x) / static_cast<uint32_t>(d);
+  return x / d;
+}
+
 // Walks a share, a run of steps of one (pair, head) at a time. A boundary within
 // the first COST units leaves all steps to the block behind it.
 template <int ROWS, int STEP, int COST, bool CHOSEN = false>
@@ -71,20 +77,35 @@ struct Walk {
     n = static_cast<int>(max(int64_t{0}, upto - COST)) - s;
     left -= upto - at;
   }
-  // kApart: the tile and head `left` places on from sequence b's first. Heads of a sequence follow one another, so that the blocks
-  // that run at the same time read pages of one head or two.
+  // kApart: the tile and head `left` places on from the first of sequence b, which is t.seq.
+  __device__ __forceinline__ void place(const AttendArgs& a, int b) {
+    const int64_t one = static_cast<int64_t>(t.seq.n) * a.per_row;
+    head = static_cast<int>(divide(left, one));
+    set_tile<ROWS, STEP, true>(a, t, b, static_cast<int>(left - head * one));
+    s = 0;
+    n = t.steps;
+  }
+  // The same where it may be a later sequence's, 32 sequences at a time. Heads of a sequence follow one
+  // another, so that the blocks that run at the same time read pages of one head or two. For whole warps.
   __device__ __forceinline__ bool settle(const AttendArgs& a, int b) {
-    for (; b < a.p.n_seqs; ++b) {
-      t.seq = sequence(a.p, b);
-      const int64_t one = static_cast<int64_t>(t.seq.n) * a.per_row, all = one * a.p.heads;
-      if (left < all) {
-        head = static_cast<int>(left / one);
-        set_tile<ROWS, STEP, true>(a, t, b, static_cast<int>(left - head * one));
-        s = 0;
-        n = t.steps;
+    const int lane = threadIdx.x & 31;
+    for (; b < a.p.n_seqs; b += 32) {
+      const int64_t mine = b + lane < a.p.n_seqs ? static_cast<int64_t>(sequence(a.p, b + lane).n) * a.per_row * a.p.heads : 0;
+      int64_t upto = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += y;
+      }
+      const uint32_t there = __ballot_sync(0xffffffffu, left < upto);
+      if (there) {
+        const int i = __ffs(there) - 1;
+        left -= __shfl_sync(0xffffffffu, upto - mine, i);
+        t.seq = sequence(a.p, b + i);
+        place(a, b + i);
         return true;
       }
-      left -= all;
+      left -= __shfl_sync(0xffffffffu, upto, 31);
     }
     return false;
   }
@@ -102,7 +123,9 @@ struct Walk {
   __device__ __forceinline__ bool next(const AttendArgs& a, int tiles) {
     if (CHOSEN && a.unit == kApart) {
       left += gridDim.x;
-      return settle(a, t.b);
+      if (left >= static_cast<int64_t>(t.seq.n) * a.per_row * a.p.heads) return settle(a, t.b);
+      place(a, t.b);
+      return true;
     }
     if (left <= 0) return false;
     if (++head == a.p.heads) {
@@ -127,12 +150,6 @@ struct Walk {
   // Rows of the last V tile from `keep` on lie past the last key.
   __device__ __forceinline__ int keep() const { return t.kr.hi_max - t.kr.template key0<STEP>(s + n - 1); }
 };
-
-// 64-bit numbers that mostly fit 32 bits.
-__device__ __forceinline__ int64_t divide(int64_t x, int64_t d) {
-  if (static_cast<uint64_t>(x | d) >> 32 == 0) return static_cast<uint32_t>(x) / static_cast<uint32_t>(d);
-  return x / d;
-}
 
 // Finds the block's share, with all threads; scratch: 16 64-bit words of shared memory.
 template <int ROWS, int STEP, int COST, int THREADS, bool CHOSEN = false>

@@ -373,6 +373,18 @@ CHOSEN = [  # fmt, dim, heads, share, page, [(rows, kv)], n
     ("bf16", 128, 1, 1, 16, [(1, 30000)], 1500),                   # a list of 24000 keys
     ("u4", 64, 1, 2, 16, [(1, 30000), (1, 300)], 1500),
     ("bf16", 128, 1, 2, 16, [(1, 50 + (b * 37) % 300) for b in range(300)], 4),
+    # Longer than a block takes whole, in numbers that go to clusters of 4, of 2, to blocks one by one, to all in shares, to blocks in turn.
+    ("bf16", 128, 2, 7, 16, [(3, 900), (2, 700), (3, 20)], 40),
+    ("bf16", 128, 4, 7, 16, [(4, 900), (1, 700), (2, 30)], 40),
+    ("bf16", 128, 4, 2, 16, [(3, 900), (2, 700), (0, 100), (3, 2), (3, 1000), (3, 640), (3, 641), (3, 639)], 40),
+    ("bf16", 128, 4, 4, 16, [(5, 900 - 80 * b) for b in range(10)], 40),
+    ("bf16", 128, 4, 4, 16, [(20, 700)] * 6 + [(0, 5), (1, 3), (0, 0), (20, 900)], 40),
+    ("u4", 128, 2, 8, 32, [(9, 2000 - 600 * b) for b in range(4)], 30),
+    ("u4", 128, 4, 3, 32, [(9, 2000 - 600 * b) for b in range(4)], 30),
+    ("u8", 128, 4, 3, 32, [(9, 2000 - 300 * b) for b in range(6)], 20),
+    ("u4", 64, 1, 3, 16, [(1, 600 + (b * 29) % 300) for b in range(500)], 40),
+    ("bf16", 64, 1, 2, 16, [(1, 600 + (b * 31) % 300) for b in range(600)], 36),
+    ("bf16", 128, 1, 2, 16, [((b % 5) // 4 + (b % 7 > 0), 600 + (b * 31) % 300) for b in range(800)], 36),
 ]
 
 
