@@ -57,13 +57,14 @@ struct Ring {
   static constexpr int kStages = FMT == kBf16 ? 3 : 2;
 };
 
-// How a kernel lays itself out. Chosen bf16 pages of 128 channels are mostly found in L2, where one warp per scheduler
-// waits for its own chain of instructions (0.27 issued per cycle): 8 warps, whose rings hold 3
-// halves of stages, K's or V's each, instead of 4 with 3 stages. A half is refilled as soon as it has been read.
+// How a kernel lays itself out. Chosen bf16 pages of 128 channels are mostly found in L2, and a tile has few steps: rings
+// of 3 halves of stages, K's or V's each, instead of 3 stages leave room for a second block per SM, which goes on while
+// the first starts a tile or joins its warps (questions of 8 streams 84 us; one block of 8 warps 103, of 4 with stages 126). A
+// half is refilled as soon as it has been read.
 template <int FMT, int DP, int NR, bool CHOSEN>
 struct Layout {
   static constexpr bool kHalves = CHOSEN && FMT == kBf16 && DP == 128 && NR == 1;
-  static constexpr int kWarps = kHalves ? 8 : kRowsWarps;
+  static constexpr int kWarps = kHalves ? 4 : kRowsWarps;
   static constexpr int kThreads = 32 * kWarps;
   static constexpr int kRing = kHalves ? 3 * Ring<FMT, DP>::kTile : Ring<FMT, DP>::kStage * Ring<FMT, DP>::kStages;  // of a warp
   static constexpr int kRings = kRing * kWarps;

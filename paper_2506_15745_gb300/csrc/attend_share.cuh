@@ -70,14 +70,14 @@ template <int ROWS, int STEP, int COST, bool CHOSEN = false>
 struct Walk {
   Tile t;
   int head, s, n;  // steps s .. s + n - 1
-  int64_t left;    // kApart: the number of the tile and head in its sequence, plus what the sequences before it have
+  int64_t left;    // kInTurn: the number of the tile and head in its sequence, plus what the sequences before it have
   __device__ __forceinline__ void cut(int64_t at) {
     const int64_t weight = t.steps + COST, upto = min(weight, at + left);
     s = static_cast<int>(max(int64_t{0}, at - COST));
     n = static_cast<int>(max(int64_t{0}, upto - COST)) - s;
     left -= upto - at;
   }
-  // kApart: the tile and head `left` places on from the first of sequence b, which is t.seq.
+  // kInTurn: the tile and head `left` places on from the first of sequence b, which is t.seq.
   __device__ __forceinline__ void place(const AttendArgs& a, int b) {
     const int64_t one = static_cast<int64_t>(t.seq.n) * a.per_row;
     head = static_cast<int>(divide(left, one));
@@ -110,7 +110,7 @@ struct Walk {
     return false;
   }
   __device__ __forceinline__ bool begin(const AttendArgs& a, int tiles, const Share& w) {
-    if (CHOSEN && a.unit == kApart) {
+    if (CHOSEN && a.unit == kInTurn) {
       left = blockIdx.x;
       return settle(a, 0);
     }
@@ -121,7 +121,7 @@ struct Walk {
     return n > 0 || next(a, tiles);
   }
   __device__ __forceinline__ bool next(const AttendArgs& a, int tiles) {
-    if (CHOSEN && a.unit == kApart) {
+    if (CHOSEN && a.unit == kInTurn) {
       left += gridDim.x;
       if (left >= static_cast<int64_t>(t.seq.n) * a.per_row * a.p.heads) return settle(a, t.b);
       place(a, t.b);
@@ -156,7 +156,7 @@ template <int ROWS, int STEP, int COST, int THREADS, bool CHOSEN = false>
 __device__ Share find_share(const AttendArgs& a, int tiles, int64_t* scratch) {
   const int pairs = a.p.n_seqs * tiles, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   constexpr int kWarps = THREADS / 32;
-  if (CHOSEN && a.unit == kApart) {
+  if (CHOSEN && a.unit == kInTurn) {
     Share w = {};
     w.left = 1;  // to be walked; there may be nothing
     return w;

@@ -246,13 +246,15 @@ constexpr int kWhole = 512;
 // 12000 16 against 13; 4 bits: 1500 keys 8.5 against 14.8, 6272 13.0 against 15.1.
 constexpr int64_t kClusterKeys = 8192, kClusterBytes = 1 << 20;
 
-// Chosen pages: from this many row tiles and heads per block on, blocks take them whole and in turn, which keeps the
-// blocks that run at the same time near one another in the cache (and in L2) and leaves nothing to join.
-constexpr int kApartItems = 4;
-// Below that, 4 or 2 blocks take a tile each as a cluster where they all have room at once, or one where two have not: no
-// parts to write, no second kernel. Lists of 2048 keys, 8 KV heads, 4 bits: 8 streams 13.0 us against 17.2 shared out, 24
-// streams 24.8 against 28.4 (two blocks each), 32 streams 27.2 against 32.8 (one); bf16: 4 streams 10.6 against 12.4, 12 streams
-// 21.4 against 25.1 (one). More tiles than blocks are shared out.
+// Chosen pages: blocks take row tiles and heads whole and in turn where that keeps them busy for this many tenths of their
+// rounds: nothing to join, and the blocks that run at the same time are near one another in the cache (and in L2). Lists of
+// 2048 keys, 8 KV heads, bf16: 8 sequences of 12 tokens 89 us against 123 shared out, of 10 tokens (7 tenths) 87 against 104, 60
+// single tokens 79 against 85; 4 bits: 160 tokens 96 against 103; 8 bits: 80 tokens (7 tenths) 84 against 73, 100 tokens 91
+// against 89.
+constexpr int kInTurnTenths = 7;
+// With less than a round, 4 or 2 blocks take a tile each as a cluster where they all have room at once, or one where two have
+// not: no parts to write, no second kernel. 4 bits: 8 streams 13.0 us against 17.2 shared out, 24 streams 24.8 against 28.4 (two
+// blocks each), 32 streams 27.2 against 32.8 (one); bf16: 4 streams 10.6 against 12.4, 12 streams 21.4 against 25.1 (one).
 
 // Which kernel takes the call, on how many blocks, and the workspace.
 struct Plan {
@@ -320,8 +322,9 @@ void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
     return;
   }
   if (a->n_chosen > 0) {
-    if (items >= kApartItems * plan->blocks) {
-      a->unit = ipv::kApart;
+    const int64_t rounds = (items + plan->blocks - 1) / plan->blocks;
+    if (rounds > 1 && items * 10 >= rounds * plan->blocks * kInTurnTenths) {
+      a->unit = ipv::kInTurn;
       return;
     }
     int c = 4;

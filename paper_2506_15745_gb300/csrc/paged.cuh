@@ -107,7 +107,7 @@ cudaError_t launch_next(void (*kernel)(Params...), dim3 grid, unsigned block, si
 }
 
 // ------------------------------------------------------------------ attention
-constexpr int kApart = -1;  // AttendArgs::unit
+constexpr int kInTurn = -1;  // AttendArgs::unit
 struct AttendArgs {
   Pages p;
   const uint16_t* q;
@@ -120,7 +120,7 @@ struct AttendArgs {
   float scale_log2;     // scale * log2(e)
   int causal, window, sinks;
   // Fewest units (steps and runs' costs) of a block's share; 0: `cluster` blocks (1, or 8 as one cluster,
-  // which joins their parts by itself) take one KV head of one row tile; kApart (chosen pages): a block takes
+  // which joins their parts by itself) take one KV head of one row tile; kInTurn (chosen pages): a block takes
   // tiles whole, every gridDim.x-th one.
   int unit, cluster;
   int tile;  // query rows of a row tile
