@@ -60,13 +60,15 @@ struct Ring {
 // How a kernel lays itself out. Chosen bf16 pages of 128 channels are mostly found in L2, and a tile has few steps: rings
 // of 3 halves of stages, K's or V's each, instead of 3 stages leave room for a second block per SM, which goes on while
 // the first starts a tile or joins its warps (questions of 8 streams 84 us; one block of 8 warps 103, of 4 with stages 126). A
-// half is refilled as soon as it has been read.
+// half is refilled as soon as it has been read. 8-bit codes: a third block instead of two (200 streams' tokens 156 us against
+// 169, questions 95 against 105; 32 streams', a block each, 34 against 32).
 template <int FMT, int DP, int NR, bool CHOSEN>
 struct Layout {
-  static constexpr bool kHalves = CHOSEN && FMT == kBf16 && DP == 128 && NR == 1;
+  static constexpr bool kHalves = CHOSEN && FMT != kU4 && DP == 128 && NR == 1;
+  static constexpr int kHalf = Ring<FMT, DP>::kTile + (FMT == kBf16 ? 0 : Ring<FMT, DP>::kPar);  // of a stage: K's or V's rows, their pairs
   static constexpr int kWarps = kHalves ? 4 : kRowsWarps;
   static constexpr int kThreads = 32 * kWarps;
-  static constexpr int kRing = kHalves ? 3 * Ring<FMT, DP>::kTile : Ring<FMT, DP>::kStage * Ring<FMT, DP>::kStages;  // of a warp
+  static constexpr int kRing = kHalves ? 3 * kHalf : Ring<FMT, DP>::kStage * Ring<FMT, DP>::kStages;  // of a warp
   static constexpr int kRings = kRing * kWarps;
   static constexpr int kBytes = kRings + kWarps * 8 * NR * (DP + 4 + 2) * 4;  // and the warps' results
 };
@@ -346,18 +348,23 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
              ok ? from + ((up ? h.at[1] : h.at[0]) + r * next_bytes + lane_at) : from, ok);
     }
   };
-  auto issue_chosen = [&](const Halves& h, int stage) {
-    const uint32_t base = ring + stage * R::kStage;
+  // K's or V's rows and, of codes, their pairs.
+  auto copy_side = [&](const char* from, const uint32_t* par, uint32_t to, uint32_t par_to, const Halves& h) {
     if constexpr (!kB) {
       constexpr int kN = R::kG * 4;
       const bool ok = (lane & 15) < (lane < 16 ? h.n[0] : h.n[1]);
       const int64_t at = ok ? ((lane < 16 ? h.at[0] : h.at[1]) + (lane & 15) * next_bytes) / (R::kRowB / kN) : 0;
-      copy_small<kN>(base + 2 * R::kTile + lane * kN, reinterpret_cast<const char*>(a.p.k_par) + at, ok);
-      copy_small<kN>(base + 2 * R::kTile + R::kPar + lane * kN, reinterpret_cast<const char*>(a.p.v_par) + at, ok);
+      copy_small<kN>(par_to + lane * kN, reinterpret_cast<const char*>(par) + at, ok);
     }
-    copy_rows(a.p.k, base, h);
-    copy_rows(a.p.v, base + R::kTile, h);
+    copy_rows(from, to, h);
   };
+  auto issue_chosen = [&](const Halves& h, int stage) {
+    const uint32_t base = ring + stage * R::kStage;
+    copy_side(a.p.k, a.p.k_par, base, base + 2 * R::kTile, h);
+    copy_side(a.p.v, a.p.v_par, base + R::kTile, base + 2 * R::kTile + R::kPar, h);
+  };
+  auto copy_k = [&](int half, const Halves& h) { copy_side(a.p.k, a.p.k_par, ring + half * L::kHalf, ring + half * L::kHalf + R::kTile, h); };
+  auto copy_v = [&](int half, const Halves& h) { copy_side(a.p.v, a.p.v_par, ring + half * L::kHalf, ring + half * L::kHalf + R::kTile, h); };
   uint32_t seen_now = 0, seen_next = 0, seen_last = 0;  // keys of the step at hand and of the ones after it
   // The first steps of a run, and the page of the one after them.
   int page_next = -1;
@@ -370,11 +377,11 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
       if constexpr (L::kHalves) {  // K and V of the first step, K of the second
         const Halves h1 = halves(x, 1);
         seen_next = h1.seen;
-        if (end > 0) copy_rows(a.p.k, ring, h0);
+        if (end > 0) copy_k(0, h0);
         copy_commit();
-        if (end > 0) copy_rows(a.p.v, ring + R::kTile, h0);
+        if (end > 0) copy_v(1, h0);
         copy_commit();
-        if (end > kWarps) copy_rows(a.p.k, ring + 2 * R::kTile, h1);
+        if (end > kWarps) copy_k(2, h1);
         copy_commit();
       } else {
 #pragma unroll
@@ -531,9 +538,9 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
         copy_wait<R::kStages - 1>();
       }
       __syncwarp();
-      const uint32_t ks_at = ring + (L::kHalves ? k_half * R::kTile : stage * R::kStage);
-      const uint32_t vs_at = L::kHalves ? ring + v_half * R::kTile : ks_at + R::kTile;
-      const uint32_t kp_at = ks_at + 2 * R::kTile, vp_at = kp_at + R::kPar;
+      const uint32_t ks_at = ring + (L::kHalves ? k_half * L::kHalf : stage * R::kStage);
+      const uint32_t vs_at = L::kHalves ? ring + v_half * L::kHalf : ks_at + R::kTile;
+      const uint32_t kp_at = ks_at + (L::kHalves ? 1 : 2) * R::kTile, vp_at = L::kHalves ? vs_at + R::kTile : kp_at + R::kPar;
       const int key0 = kr.key0<kRowsStep>(step);
 
       float sc[2][NR][4];
@@ -616,8 +623,12 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
       }
       if constexpr (L::kHalves) {  // K has been read: the next step's V comes in its place
         __syncwarp();
-        if (step + kWarps < s_end) copy_rows(a.p.v, ring + k_half * R::kTile, halves(w, k + 1));
+        if (step + kWarps < s_end) copy_v(k_half, halves(w, k + 1));
         copy_commit();
+        if constexpr (!kB) {  // V's pairs come first
+          copy_wait<2>();
+          __syncwarp();
+        }
       }
       // The mask, only where some row of the tile does not see all 32 keys.
       if constexpr (CHOSEN) {
@@ -730,7 +741,7 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
             }
           }
       }
-      if constexpr (L::kHalves) {
+      if constexpr (L::kHalves && kB) {
         copy_wait<2>();
         __syncwarp();
       }
@@ -800,7 +811,7 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
       if constexpr (L::kHalves) {  // K of the step after the next one in V's place
         if ((k + 2) % 16 == 0) look_up(w, k + 2);
         const Halves h = halves(w, k + 2);
-        if (step + 2 * kWarps < s_end) copy_rows(a.p.k, ring + v_half * R::kTile, h);
+        if (step + 2 * kWarps < s_end) copy_k(v_half, h);
         copy_commit();
         seen_now = seen_next, seen_next = h.seen;
         const int free = v_half;
