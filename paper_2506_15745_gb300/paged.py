@@ -278,7 +278,8 @@ class PagedCache:
         strides = self._packed(k_name, k, batch, self.n_kv_heads, self.head_dim)
         if v.shape != k.shape or v.dtype is not torch.bfloat16 or not v.is_cuda:
             self._packed(v_name, v, batch, self.n_kv_heads, self.head_dim)
-        _need(v.stride() == strides, f"{k_name} and {v_name} must have the same strides")
+        if v.stride() != strides:
+            raise ValueError(f"{k_name} and {v_name} must have the same strides")
         return strides
 
     @staticmethod
@@ -298,7 +299,7 @@ class PagedCache:
     def write(self, k_new, v_new, batch: PagedBatch, stream=None) -> None:
         """ipv_pages_write: k_new, v_new bf16 [total_rows, n_kv_heads, head_dim] into the batch's pages."""
         strides = self._pair("k_new", k_new, "v_new", v_new, batch)
-        status = self._lib.ipv_pages_write(self.ref, batch.ref, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1],
+        status = self._lib.ipv_pages_write(self.at, batch.at, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1],
                                            ipv._stream(stream))
         if status:
             ipv._check(status)
@@ -313,7 +314,7 @@ class PagedCache:
             k_out = new.pop(0) if k_out is None else k_out
             v_out = new.pop(0) if v_out is None else v_out
         strides = self._pair("k_out", k_out, "v_out", v_out, batch)
-        status = self._lib.ipv_pages_read(self.ref, batch.ref, k_out.data_ptr(), v_out.data_ptr(), strides[0], strides[1], at)
+        status = self._lib.ipv_pages_read(self.at, batch.at, k_out.data_ptr(), v_out.data_ptr(), strides[0], strides[1], at)
         if status:
             ipv._check(status)
         return k_out, v_out
@@ -384,8 +385,8 @@ class PagedCache:
         os = out.stride()
         if out.shape != shape or out.dtype is not torch.bfloat16 or not out.is_cuda or os[2] != 1:
             self._packed("out", out, batch, n_q_heads, self.head_dim)  # may be longer
-        if lse is not None:
-            self._check_lse(lse, batch, n_q_heads)
+        if lse is not None and (lse.shape != shape[:2] or lse.dtype is not torch.float32 or not lse.is_cuda or not lse.is_contiguous()):
+            self._check_lse(lse, batch, n_q_heads)  # may be longer
         sizes = (batch.sizes, n_q_heads, n_chosen)
         kept = self._calls.get(sizes)
         if kept is None:
