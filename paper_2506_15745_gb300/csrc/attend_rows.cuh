@@ -40,7 +40,7 @@
 namespace ipv {
 namespace {
 
-constexpr int kThreads = 32 * kRowsWarps;  // of the join, and of most kernels
+constexpr int kThreads = 32 * kRowsWarps;
 constexpr int kRunCost = 6;  // what a run of steps costs beside them, in steps
 constexpr int kCluster = kRowsCluster;
 constexpr float kNegInf = -INFINITY;
@@ -57,20 +57,27 @@ struct Ring {
   static constexpr int kStages = FMT == kBf16 ? 3 : 2;
 };
 
-// How a kernel lays itself out. Chosen bf16 pages of 128 channels are mostly found in L2, and a tile has few steps: rings
-// of 3 halves of stages, K's or V's each, instead of 3 stages leave room for a second block per SM, which goes on while
-// the first starts a tile or joins its warps (questions of 8 streams 84 us; one block of 8 warps 103, of 4 with stages 126). A
-// half is refilled as soon as it has been read. 8-bit codes: a third block instead of two (200 streams' tokens 156 us against
-// 169, questions 95 against 105; 32 streams', a block each, 34 against 32).
+// How a kernel lays itself out. Chosen pages of 128 channels are mostly found in L2, and a tile has few steps: what counts is
+// how many warps there are, and that other blocks go on while one starts a tile or joins its warps. bf16: rings of two halves of
+// a stage, K's and V's, each refilled as soon as it has been read, the warps' results in their place at a tile's end, and three
+// blocks per SM (questions of 8 streams 67 us; two blocks with 3 halves and the next tile on its way 84, one of 8 warps 103, of
+// 4 with 3 stages 126). 8-bit codes: 3 halves and the results behind them, three blocks per SM instead of two (200 streams'
+// tokens 156 us against 169, questions 95 against 105; 32 streams', a block each, 34 against 32).
 template <int FMT, int DP, int NR, bool CHOSEN>
 struct Layout {
   static constexpr bool kHalves = CHOSEN && FMT != kU4 && DP == 128 && NR == 1;
-  static constexpr int kHalf = Ring<FMT, DP>::kTile + (FMT == kBf16 ? 0 : Ring<FMT, DP>::kPar);  // of a stage: K's or V's rows, their pairs
-  static constexpr int kWarps = kHalves ? 4 : kRowsWarps;
-  static constexpr int kThreads = 32 * kWarps;
-  static constexpr int kRing = kHalves ? 3 * kHalf : Ring<FMT, DP>::kStage * Ring<FMT, DP>::kStages;  // of a warp
-  static constexpr int kRings = kRing * kWarps;
-  static constexpr int kBytes = kRings + kWarps * 8 * NR * (DP + 4 + 2) * 4;  // and the warps' results
+  static constexpr bool kTwo = kHalves && FMT == kBf16;  // halves; results in their place
+  static constexpr int kBlocks = kHalves ? 3 : FMT == kBf16 && DP == 128 ? 1 : NR == 1 ? 3 : 2;  // per SM
+  static constexpr int kHalf = Ring<FMT, DP>::kTile + (FMT == kBf16 ? 0 : Ring<FMT, DP>::kPar);  // K's or V's rows, their pairs
+  static constexpr int kRing = kHalves ? (kTwo ? 2 : 3) * kHalf : Ring<FMT, DP>::kStage * Ring<FMT, DP>::kStages;  // of a warp
+  static constexpr int kRings = kRing * kRowsWarps;
+  // The warps' results: [rows][kPitch] sums each, maxima and sums of weights; a cluster's part.
+  static constexpr int kPitch = DP + 4, kResult = 8 * NR * kPitch * 4;
+  static constexpr int kResults = kTwo ? 0 : kRings, kResultApart = kTwo ? kRing : kResult;
+  static constexpr int kStats = kTwo ? kRings : kRings + kRowsWarps * kResult;
+  static constexpr int kPart = kTwo ? kHalf : 0;
+  static constexpr int kBytes = kStats + kRowsWarps * 8 * NR * 2 * 4;
+  static_assert(!kTwo || kResult <= kHalf, "a warp's results take the first of its halves, the part the other");
 };
 
 // Where 16-byte chunk c of key row r lies in its row: the rows that a quarter
@@ -195,8 +202,6 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, const Seq& s, int
 // Resident blocks per SM that registers and shared memory are cut to: bf16 at 128
 // channels has enough bytes in flight with one, codes need warps to widen them (32
 // ragged 4-bit streams: 3 blocks of 168 registers 123 us, 4 of 128, with spills, 134).
-constexpr int min_blocks(int fmt, int dp, int nr) { return fmt == kBf16 && dp == 128 ? 1 : nr == 1 ? 3 : 2; }
-
 // Clusters: a block's rank, the address of a shared-memory word in block r of
 // the cluster, loads from there, and the barrier of all blocks.
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -225,10 +230,10 @@ __device__ __forceinline__ void cluster_barrier() {
 
 // CHOSEN: a row tile's keys are those of its new row's chosen pages, one list for each KV head.
 template <int FMT, int DP, int NR, bool CHOSEN>
-__global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blocks(FMT, DP, NR)) attend_rows_kernel(AttendArgs a, int tiles) {
+__global__ void __launch_bounds__(kThreads, (Layout<FMT, DP, NR, CHOSEN>::kBlocks)) attend_rows_kernel(AttendArgs a, int tiles) {
   using R = Ring<FMT, DP>;
   using L = Layout<FMT, DP, NR, CHOSEN>;
-  constexpr int kWarps = L::kWarps, kThreads = L::kThreads;
+  constexpr int kWarps = kRowsWarps;
   constexpr bool kB = FMT == kBf16;
   constexpr int kCh = R::kRowB / 16;     // chunks of a row
   constexpr int kKs = DP / 16;           // k-steps of the first product
@@ -374,7 +379,12 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
       const int end = x.n - warp;  // steps of the run from this warp's first on
       const Halves h0 = halves(x, 0);
       seen_now = h0.seen;
-      if constexpr (L::kHalves) {  // K and V of the first step, K of the second
+      if constexpr (L::kTwo) {
+        if (end > 0) copy_k(0, h0);
+        copy_commit();
+        if (end > 0) copy_v(1, h0);
+        copy_commit();
+      } else if constexpr (L::kHalves) {  // K and V of the first step, K of the second
         const Halves h1 = halves(x, 1);
         seen_next = h1.seen;
         if (end > 0) copy_k(0, h0);
@@ -408,7 +418,7 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
 
   // A cluster's part: [rows][DP sums, maximum, sum] in the rings, which one run leaves free.
   constexpr int kPartPitch = DP + 4;
-  float* part_rows = reinterpret_cast<float*>(smem);
+  float* part_rows = reinterpret_cast<float*>(smem + L::kPart);
 
   bool go = share.left > 0 && w.begin(a, tiles, share);
   if (go) fill(w);
@@ -520,7 +530,7 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
     int k = 0;                                  // chosen pages: which of this warp's steps it is
     for (int step = first; step < s_end; step += kWarps) {
       if constexpr (L::kHalves) {
-        copy_wait<2>();
+        copy_wait<L::kTwo ? 1 : 2>();
       } else if constexpr (CHOSEN) {
         constexpr int kAhead = R::kStages - 1;
         if ((k + kAhead) % 16 == 0) look_up(w, k + kAhead);
@@ -621,7 +631,14 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
             }
         }
       }
-      if constexpr (L::kHalves) {  // K has been read: the next step's V comes in its place
+      Halves ahead;  // the next step
+      if constexpr (L::kTwo) {  // K has been read: the next step's K comes in its place
+        __syncwarp();
+        if ((k + 1) % 16 == 0) look_up(w, k + 1);
+        ahead = halves(w, k + 1);
+        if (step + kWarps < s_end) copy_k(0, ahead);
+        copy_commit();
+      } else if constexpr (L::kHalves) {  // the next step's V comes in its place
         __syncwarp();
         if (step + kWarps < s_end) copy_v(k_half, halves(w, k + 1));
         copy_commit();
@@ -741,8 +758,8 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
             }
           }
       }
-      if constexpr (L::kHalves && kB) {
-        copy_wait<2>();
+      if constexpr (L::kTwo) {
+        copy_wait<1>();
         __syncwarp();
       }
       // O^T += V^T P^T
@@ -808,7 +825,11 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
         }
       }
       __syncwarp();  // the stage is read before its next copies are issued
-      if constexpr (L::kHalves) {  // K of the step after the next one in V's place
+      if constexpr (L::kTwo) {
+        if (step + kWarps < s_end) copy_v(1, ahead);
+        copy_commit();
+        seen_now = ahead.seen;
+      } else if constexpr (L::kHalves) {  // K of the step after the next one in V's place
         if ((k + 2) % 16 == 0) look_up(w, k + 2);
         const Halves h = halves(w, k + 2);
         if (step + 2 * kWarps < s_end) copy_k(v_half, h);
@@ -822,17 +843,18 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
       }
       ++k;
     }
-    // The next run's first steps are on their way while this one's results are joined.
+    // The next run's first steps are on their way while this one's results are joined, where these lie elsewhere.
     const bool partial = !(w.starts() && w.ends());
     const int4 record = part_record(w.pair(tiles), head, w.starts(), w.ends());
     go = w.next(a, tiles);
-    if (go) fill(w);
+    if (go && !L::kTwo) fill(w);
 
     // ---- join the warps
     constexpr int kRows = 8 * NR;
-    float* so = reinterpret_cast<float*>(smem + L::kRings);           // [warps][rows][DP + 4]
-    constexpr int kPitch = DP + 4;
-    float* sm = so + kWarps * kRows * kPitch;                     // [warps][rows] maxima, then sums
+    constexpr int kPitch = L::kPitch;
+    float* so = reinterpret_cast<float*>(smem + L::kResults);         // [warps][rows][kPitch], warps kApartF apart
+    constexpr int kApartF = L::kResultApart / 4;
+    float* sm = reinterpret_cast<float*>(smem + L::kStats);           // [warps][rows] maxima, then sums
     float* sl = sm + kWarps * kRows;
 #pragma unroll
     for (int nr = 0; nr < NR; ++nr)
@@ -864,7 +886,7 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
         for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
           for (int half = 0; half < 2; ++half)
-            so[(warp * kRows + r) * kPitch + out_channel<FMT>(ct, half, g)] =
+            so[warp * kApartF + r * kPitch + out_channel<FMT>(ct, half, g)] =
                 kB ? o[ct][nr][half * 2 + i] : fmaf(o[ct][nr][half * 2 + i], times[half], add[kB ? 0 : ct >> 2]);
       }
     __syncthreads();
@@ -887,7 +909,7 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
       for (int x = 0; x < kWarps; ++x) {
         const float f = exp2_fast(sm[x * kRows + r] - base);
         sum += f * sl[x * kRows + r];
-        const float4 y = *reinterpret_cast<const float4*>(so + (x * kRows + r) * kPitch + c);
+        const float4 y = *reinterpret_cast<const float4*>(so + x * kApartF + r * kPitch + c);
         acc.x += f * y.x, acc.y += f * y.y, acc.z += f * y.z, acc.w += f * y.w;
       }
       if (sum == 0.0f) acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // sees nothing, here or at all
@@ -904,6 +926,7 @@ __global__ void __launch_bounds__(Layout<FMT, DP, NR, CHOSEN>::kThreads, min_blo
       }
     }
     __syncthreads();  // the results are read before the next run's are written
+    if (go && L::kTwo) fill(w);
   }
   if (clustered) {
     // The cluster's blocks hold a part each, in the place of their rings: every
@@ -1016,11 +1039,11 @@ struct Kernel {
   static cudaError_t prepare() {
     const cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<FMT, DP, NR, CHOSEN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
-    return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, attend_rows_kernel<FMT, DP, NR, CHOSEN>, L::kThreads, kSmem);
+    return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, attend_rows_kernel<FMT, DP, NR, CHOSEN>, kThreads, kSmem);
   }
   static cudaError_t launch(const AttendArgs& a, int blocks, cudaStream_t st) {
     const cudaError_t e =
-        launch_clusters(a.unit == 0 ? a.cluster : 1, attend_rows_kernel<FMT, DP, NR, CHOSEN>, dim3(blocks), L::kThreads, kSmem, st, a, a.tiles);
+        launch_clusters(a.unit == 0 ? a.cluster : 1, attend_rows_kernel<FMT, DP, NR, CHOSEN>, dim3(blocks), kThreads, kSmem, st, a, a.tiles);
     if (e != cudaSuccess || a.unit <= 0) return e;
     return launch_next(attend_rows_join_kernel<8 * NR, CHOSEN>, dim3(blocks, 8 * NR), kThreads, 0, st, a, a.tiles, blocks);
   }
