@@ -29,112 +29,129 @@ __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {  // NaN
 }
 
 // ------------------------------------------------------------------ the bounds
-// A block takes a page of one head: teams of 16 lanes, lane c the 8 channels from 8c on.
 constexpr int kBoundsThreads = 128;
-constexpr int kBoundsTeams = kBoundsThreads / 16;
-constexpr int kBoundsAtOnce = 8;  // rows that a lane has on their way
 
-// 8 channels of a row as they are held: bf16 in x; codes in x.x (and x.y at 8 bits), their pair in x.z.
-template <int FMT>
-__device__ __forceinline__ void load_keys(const Pages& p, int64_t row, int c, uint4& x) {
-  if (FMT == kBf16) {
-    x = ld_once(p.k + row * p.row_bytes + 16 * c);
-  } else {
-    const uint32_t* kd = reinterpret_cast<const uint32_t*>(p.k + row * p.row_bytes) + (c >> 3) * (FMT == kU8 ? kGroup / 4 : kGroup / 8);
-    if (FMT == kU8)
-      x.x = kd[place_u8(2 * (c & 7))], x.y = kd[place_u8(2 * (c & 7) + 1)];
-    else
-      x.x = kd[place_u4(c & 7)];
-    x.z = p.k_par[row * p.groups + (c >> 3)];
-  }
+// The first and last page that hold new rows of a sequence; none: last < first.
+__device__ __forceinline__ int2 new_pages(const Pages& p, const Seq& s) {
+  if (s.n == 0 || s.len == 0) return make_int2(0, -1);
+  return make_int2(max(0, s.len - s.n) >> p.page_shift, (s.len - 1) >> p.page_shift);
 }
 
-template <int FMT>
-__global__ void __launch_bounds__(kBoundsThreads, FMT == kBf16 ? 8 : 4) bounds_kernel(BoundsArgs a) {
-  __shared__ uint4 ends[2][kBoundsThreads / 32][16];
+// The 8-bit bounds of a pair of channels, least and greatest values in bf16; down: 2^-e.
+__device__ __forceinline__ uint32_t quantise_pair(uint32_t x, float down, bool upper) {
+  uint32_t r = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float y = i ? hi_f(x) : lo_f(x);
+    // A product too small for fp32 still lies on its side of 0.
+    const int q = upper ? max(static_cast<int>(ceilf(y * down)), y > 0.0f ? 1 : -127) : min(static_cast<int>(floorf(y * down)), y < 0.0f ? -1 : 127);
+    r |= (static_cast<uint32_t>(q) & 0xFFu) << (8 * i);
+  }
+  return r;
+}
+
+// A warp takes a page of one head, or four do where pages are long and few. A lane has 16 bytes of a row (8 channels; of codes 16 or
+// 32 of one group, in the order in which they are held), 32 / kLanes rows are read at once, kAtOnce times. The minima and maxima
+// are taken in bf16 pairs, which codes become first, and then joined by halves: in each round a lane gives away those that
+// its partner keeps. The step follows from the largest magnitude's bits.
+// A compacted cache of 112 heads of 6272 rows: bf16 (180 MB) 29.2 us, 6.2 TB/s, HBM-bound; 8 bits (96 MB) 26 us, 4 bits 29 us, bound
+// by about 5 instructions for each value. A block for each page, lanes with 8 channels: 28.8, 53.7 and 49.2 us, and 10.2 instead
+// of 5.0 over 8 x 1000 bf16 rows in pages of 16. 7 blocks per SM: 5 leave a part of a fourth round (30.2 us), at 8 it spills
+// (32.1). Few pages of 128 rows, 8 x 1000 8-bit rows: 6.6 us with four warps for each, 10.7 with one. A few new tokens' pages
+// are a launch and two dependent loads (2 us in a graph).
+constexpr int kLongPage = 128;        // rows from which four warps may take a page
+constexpr int64_t kFewPages = 4096;   // and the number of pages and heads up to which they do
+
+// G: groups of 64 channels.
+template <int FMT, int G>
+__global__ void __launch_bounds__(kBoundsThreads, FMT == kBf16 ? 7 : 4) bounds_kernel(BoundsArgs a, bool together) {
+  constexpr int kLanes = G * (FMT == kBf16 ? 8 : FMT == kU8 ? 4 : 2), kPairs = FMT == kBf16 ? 4 : FMT == kU8 ? 8 : 16;
+  constexpr int kRows = 32 / kLanes, kAll = kBoundsThreads / 32, kAtOnce = FMT == kBf16 ? 8 : 4;
+  constexpr int kLeft = kPairs * kLanes / 32;  // pairs that a lane has in the end
+  __shared__ uint32_t ends[kAll][2 * kLeft][32];
   pdl_trigger();
   pdl_wait();
-  const int b = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = threadIdx.x & 15;
+  const int b = blockIdx.z, h = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = lane & (kLanes - 1);
   const Seq s = sequence(a.p, b);
-  if (s.n == 0 || s.len == 0) return;
-  const int shift = a.p.page_shift, page0 = max(0, s.len - s.n) >> shift, i = page0 + static_cast<int>(blockIdx.x);
-  if (i > (s.len - 1) >> shift) return;
+  const int2 range = new_pages(a.p, s);
+  const int shift = a.p.page_shift, i = range.x + (together ? static_cast<int>(blockIdx.x) : static_cast<int>(blockIdx.x) * kAll + warp);
+  if (i > range.y) return;  // together: all warps
   const int pg = a.p.table ? a.p.table[b * a.p.table_stride + i] : b;
   if (static_cast<unsigned>(pg) >= static_cast<unsigned>(a.p.n_pages)) return;
-  const int rows = shift == 31 ? s.len : min(a.p.page_size, s.len - (i << shift));
+  const bool in = FMT != kBf16 || 8 * c < a.p.dim;
+  const int rows = !in ? 0 : shift == 31 ? s.len : min(a.p.page_size, s.len - (i << shift));
   const int64_t row0 = pg * a.p.page_stride + h * a.p.head_stride;
-  const bool in = 8 * c < a.p.dim;
-  uint32_t lo[4], hi[4];
+  uint32_t lo[kPairs], hi[kPairs];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) lo[k] = 0x7F807F80u, hi[k] = 0xFF80FF80u;
-  uint4 x[kBoundsAtOnce];
-  auto load = [&](int r0) {
+  for (int k = 0; k < kPairs; ++k) lo[k] = 0x7F807F80u, hi[k] = 0xFF80FF80u;
+  for (int r0 = (together ? warp * kRows : 0) + lane / kLanes; r0 < rows; r0 += kRows * kAtOnce * (together ? kAll : 1)) {
+    uint4 x[kAtOnce];
+    uint32_t par[kAtOnce];
 #pragma unroll
-    for (int u = 0; u < kBoundsAtOnce; ++u) {
-      const int r = r0 + u * kBoundsTeams;
-      if (in && r < rows) load_keys<FMT>(a.p, row0 + r * a.p.row_stride, c, x[u]);
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int r = r0 + u * kRows * (together ? kAll : 1);
+      if (r >= rows) continue;
+      const int64_t row = row0 + r * a.p.row_stride;
+      x[u] = ld_once(a.p.k + row * a.p.row_bytes + 16 * c);
+      if (FMT != kBf16) par[u] = a.p.k_par[row * G + c / (kLanes / G)];
     }
-  };
-  const int team = threadIdx.x >> 4;
-  load(team);
-  for (int r0 = team;; r0 += kBoundsTeams * kBoundsAtOnce) {
 #pragma unroll
-    for (int u = 0; u < kBoundsAtOnce; ++u) {
-      if (!in || r0 + u * kBoundsTeams >= rows) continue;
-      uint4 y = x[u];
-      if (FMT != kBf16) {
-        const uint32_t w[2] = {x[u].x, x[u].y};
-        y = expand<FMT, false>(w, x[u].z);
+    for (int u = 0; u < kAtOnce; ++u) {
+      if (r0 + u * kRows * (together ? kAll : 1) >= rows) continue;
+      const uint32_t ws[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+      for (int j = 0; j < kPairs / 4; ++j) {
+        const uint32_t w[2] = {ws[FMT == kU8 ? 2 * j : j], ws[FMT == kU8 ? 2 * j + 1 : j]};
+        const uint4 y = FMT == kBf16 ? x[u] : expand<FMT == kBf16 ? kU8 : FMT, false>(w, par[u]);
+        const uint32_t ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) lo[4 * j + k] = min_bf16x2(lo[4 * j + k], ys[k]), hi[4 * j + k] = max_bf16x2(hi[4 * j + k], ys[k]);
       }
-      const uint32_t ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) lo[k] = min_bf16x2(lo[k], ys[k]), hi[k] = max_bf16x2(hi[k], ys[k]);
     }
-    const int more = r0 + kBoundsTeams * kBoundsAtOnce;
-    if (more - team >= rows) break;  // the same for the block
-    load(more);
   }
+  int first = 0;  // of the pairs that this lane keeps
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    lo[k] = min_bf16x2(lo[k], __shfl_xor_sync(0xffffffffu, lo[k], 16));
-    hi[k] = max_bf16x2(hi[k], __shfl_xor_sync(0xffffffffu, hi[k], 16));
-  }
-  if (lane < 16) {
-    ends[0][warp][c] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-    ends[1][warp][c] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-  }
-  __syncthreads();
-  if (warp > 0) return;
+  for (int d = 16, half = kPairs / 2; d >= kLanes; d >>= 1, half >>= 1) {
+    const bool upper = lane & d;
+    if (upper) first += half;
 #pragma unroll
-  for (int w = 1; w < kBoundsThreads / 32; ++w) {
-    const uint4 y = ends[0][w][c], z = ends[1][w][c];
-    lo[0] = min_bf16x2(lo[0], y.x), lo[1] = min_bf16x2(lo[1], y.y), lo[2] = min_bf16x2(lo[2], y.z), lo[3] = min_bf16x2(lo[3], y.w);
-    hi[0] = max_bf16x2(hi[0], z.x), hi[1] = max_bf16x2(hi[1], z.y), hi[2] = max_bf16x2(hi[2], z.z), hi[3] = max_bf16x2(hi[3], z.w);
+    for (int k = 0; k < half; ++k) {
+      const uint32_t l = __shfl_xor_sync(0xffffffffu, upper ? lo[k] : lo[k + half], d), g = __shfl_xor_sync(0xffffffffu, upper ? hi[k] : hi[k + half], d);
+      lo[k] = min_bf16x2(upper ? lo[k + half] : lo[k], l);
+      hi[k] = max_bf16x2(upper ? hi[k + half] : hi[k], g);
+    }
+  }
+  if (together) {
+#pragma unroll
+    for (int k = 0; k < kLeft; ++k) ends[warp][2 * k][lane] = lo[k], ends[warp][2 * k + 1][lane] = hi[k];
+    __syncthreads();
+    if (warp > 0) return;
+#pragma unroll
+    for (int w = 1; w < kAll; ++w)
+#pragma unroll
+      for (int k = 0; k < kLeft; ++k) lo[k] = min_bf16x2(lo[k], ends[w][2 * k][lane]), hi[k] = max_bf16x2(hi[k], ends[w][2 * k + 1][lane]);
   }
   uint32_t top = 0;
-  if (in)
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      top = max(max(max(top, lo[k] & 0x7FFFu), max((lo[k] >> 16) & 0x7FFFu, hi[k] & 0x7FFFu)), (hi[k] >> 16) & 0x7FFFu);
+  for (int k = 0; k < kLeft && in; ++k)
+    top = max(max(max(top, lo[k] & 0x7FFFu), max((lo[k] >> 16) & 0x7FFFu, hi[k] & 0x7FFFu)), (hi[k] >> 16) & 0x7FFFu);
   top = __reduce_max_sync(0xffffffffu, top);
   const bool finite = top < 0x7F80u;
   const int e = finite ? exponent_of(top) : 0;
-  const float down = pow2(-e);
-  uint32_t w[2][2] = {};
-  if (in && finite)
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float y = k & 1 ? hi_f(lo[k >> 1]) : lo_f(lo[k >> 1]), z = k & 1 ? hi_f(hi[k >> 1]) : lo_f(hi[k >> 1]);
-      // A product too small for fp32 still lies on its side of 0.
-      const int below = min(static_cast<int>(floorf(y * down)), y < 0.0f ? -1 : 127), above = max(static_cast<int>(ceilf(z * down)), z > 0.0f ? 1 : -127);
-      w[0][k >> 2] |= (static_cast<uint32_t>(below) & 0xFFu) << (8 * (k & 3));
-      w[1][k >> 2] |= (static_cast<uint32_t>(above) & 0xFFu) << (8 * (k & 3));
-    }
   const int64_t at = static_cast<int64_t>(pg) * a.p.heads + h;
-  if (lane < 16 && 8 * c < a.padded) {
-    char* out = a.codes + at * 2 * a.padded + 8 * c;
-    *reinterpret_cast<uint2*>(out) = make_uint2(w[0][0], w[0][1]);
-    *reinterpret_cast<uint2*>(out + a.padded) = make_uint2(w[1][0], w[1][1]);
+  char* out = a.codes + at * 2 * a.padded;
+#pragma unroll
+  for (int k = 0; k < kLeft; ++k) {
+    // Pair n of chunk q of a group. Codes: words g hold 4 (8 bits) or 8 channels from 4 g or 8 g on, and stand in the places that
+    // place_u8 and place_u4 give.
+    const int n = first + k, q = c & (kLanes / G - 1), j = FMT == kU8 ? n >> 1 : n >> 2;
+    const int channel = c / (kLanes / G) * kGroup + (FMT == kBf16 ? 8 * q + 2 * n
+                                                     : FMT == kU8 ? 4 * (q + 4 * j) + 2 * (n & 1)
+                                                                  : 8 * (2 * q + (j >> 1) + 4 * (j & 1)) + 2 * (n & 3));
+    const bool some = finite && in;  // the padding is 0
+    const uint32_t below = some ? quantise_pair(lo[k], pow2(-e), false) : 0u, above = some ? quantise_pair(hi[k], pow2(-e), true) : 0u;
+    *reinterpret_cast<uint16_t*>(out + channel) = static_cast<uint16_t>(below);
+    *reinterpret_cast<uint16_t*>(out + a.padded + channel) = static_cast<uint16_t>(above);
   }
   if (lane == 0) a.steps[at] = finite ? pow2(e) : __uint_as_float(0x7FC00000u);
 }
@@ -284,7 +301,11 @@ __device__ uint32_t mark_largest(uint32_t* keys, int first, int end, int need, i
 }
 
 // A cluster takes one new row and KV head: its blocks score the pages, 16 at a time
-// per warp, into the first block's shared memory; that block chooses.
+// per warp, the next 16 on their way, into the first block's shared memory; that block chooses. Every
+// page's 2 dim + 4 bytes are read once for a row. 32 ragged streams of up to 769 pages, 8 KV heads with 8 query
+// heads each (31 MB): 14.5 us, 2.1 TB/s. The longest streams' blocks set the time: 7 dependent rounds of loads per warp (about
+// 7 us), then the selection with its barriers (2.5 us); without the products 2.4 us less. More warps per list
+// (512 threads: 15.1 us, spills) or four blocks per SM (64 registers: 30 us) were slower. One stream, 98 pages: 4.8 us.
 template <int DP>
 __global__ void __launch_bounds__(kChooseThreads, 2) choose_kernel(ChooseArgs a) {
   constexpr int kCodes = 2 * DP;              // bytes of a page's bounds, and of a query head's parts
@@ -459,12 +480,25 @@ size_t choose_smem(int head_tiles, int pages) {
 
 }  // namespace
 
+namespace {
+
+template <int FMT>
+cudaError_t launch_format(const BoundsArgs& a, int pages, cudaStream_t st) {
+  constexpr int kApart = kBoundsThreads / 32;
+  const bool together = a.p.page_size >= kLongPage && static_cast<int64_t>(pages) * a.p.heads * a.p.n_seqs <= kFewPages;
+  const dim3 g(static_cast<unsigned>(together ? pages : (pages + kApart - 1) / kApart), static_cast<unsigned>(a.p.heads),
+               static_cast<unsigned>(a.p.n_seqs));
+  return a.p.groups == 1 ? launch_next(bounds_kernel<FMT, 1>, g, kBoundsThreads, 0, st, a, together)
+                         : launch_next(bounds_kernel<FMT, 2>, g, kBoundsThreads, 0, st, a, together);
+}
+
+}  // namespace
+
 cudaError_t launch_bounds(const BoundsArgs& a, int pages, cudaStream_t st) {
-  const dim3 g(static_cast<unsigned>(pages), static_cast<unsigned>(a.p.heads), static_cast<unsigned>(a.p.n_seqs));
   switch (a.p.fmt) {
-    case kBf16: return launch_next(bounds_kernel<kBf16>, g, kBoundsThreads, 0, st, a);
-    case kU8: return launch_next(bounds_kernel<kU8>, g, kBoundsThreads, 0, st, a);
-    default: return launch_next(bounds_kernel<kU4>, g, kBoundsThreads, 0, st, a);
+    case kBf16: return launch_format<kBf16>(a, pages, st);
+    case kU8: return launch_format<kU8>(a, pages, st);
+    default: return launch_format<kU4>(a, pages, st);
   }
 }
 
