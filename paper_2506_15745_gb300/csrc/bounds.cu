@@ -57,16 +57,21 @@ __device__ __forceinline__ uint32_t quantise_pair(uint32_t x, float down, bool u
 // A compacted cache of 112 heads of 6272 rows: bf16 (180 MB) 29.2 us, 6.2 TB/s, HBM-bound; 8 bits (96 MB) 26 us, 4 bits 29 us, bound
 // by about 5 instructions for each value. A block for each page, lanes with 8 channels: 28.8, 53.7 and 49.2 us, and 10.2 instead
 // of 5.0 over 8 x 1000 bf16 rows in pages of 16. 7 blocks per SM: 5 leave a part of a fourth round (30.2 us), at 8 it spills
-// (32.1). Few pages of 128 rows, 8 x 1000 8-bit rows: 6.6 us with four warps for each, 10.7 with one. A few new tokens' pages
-// are a launch and two dependent loads (2 us in a graph).
-constexpr int kLongPage = 128;        // rows from which four warps may take a page
-constexpr int64_t kFewPages = 4096;   // and the number of pages and heads up to which they do
+// (32.1). Few pages, of 128 rows, 8 x 1000 8-bit rows: 6.6 us with four warps for each, 10.7 with one. The pages of 8 new
+// tokens are a launch and three dependent loads.
+constexpr int64_t kFewPages = 2048;  // pages and heads up to which four warps take one of more rows than a warp reads at once
+
+// How a lane reads: lanes of a row, rows of a warp, loads at once.
+template <int FMT, int G>
+struct Lanes {
+  static constexpr int kLanes = G * (FMT == kBf16 ? 8 : FMT == kU8 ? 4 : 2), kRows = 32 / kLanes, kAtOnce = FMT == kBf16 ? 8 : 4;
+};
 
 // G: groups of 64 channels.
 template <int FMT, int G>
 __global__ void __launch_bounds__(kBoundsThreads, FMT == kBf16 ? 7 : 4) bounds_kernel(BoundsArgs a, bool together) {
-  constexpr int kLanes = G * (FMT == kBf16 ? 8 : FMT == kU8 ? 4 : 2), kPairs = FMT == kBf16 ? 4 : FMT == kU8 ? 8 : 16;
-  constexpr int kRows = 32 / kLanes, kAll = kBoundsThreads / 32, kAtOnce = FMT == kBf16 ? 8 : 4;
+  constexpr int kLanes = Lanes<FMT, G>::kLanes, kRows = Lanes<FMT, G>::kRows, kAtOnce = Lanes<FMT, G>::kAtOnce;
+  constexpr int kPairs = FMT == kBf16 ? 4 : FMT == kU8 ? 8 : 16, kAll = kBoundsThreads / 32;
   constexpr int kLeft = kPairs * kLanes / 32;  // pairs that a lane has in the end
   __shared__ uint32_t ends[kAll][2 * kLeft][32];
   pdl_trigger();
@@ -482,14 +487,18 @@ size_t choose_smem(int head_tiles, int pages) {
 
 namespace {
 
-template <int FMT>
+template <int FMT, int G>
 cudaError_t launch_format(const BoundsArgs& a, int pages, cudaStream_t st) {
   constexpr int kApart = kBoundsThreads / 32;
-  const bool together = a.p.page_size >= kLongPage && static_cast<int64_t>(pages) * a.p.heads * a.p.n_seqs <= kFewPages;
+  const bool together = a.p.page_size > Lanes<FMT, G>::kRows * Lanes<FMT, G>::kAtOnce && static_cast<int64_t>(pages) * a.p.heads * a.p.n_seqs <= kFewPages;
   const dim3 g(static_cast<unsigned>(together ? pages : (pages + kApart - 1) / kApart), static_cast<unsigned>(a.p.heads),
                static_cast<unsigned>(a.p.n_seqs));
-  return a.p.groups == 1 ? launch_next(bounds_kernel<FMT, 1>, g, kBoundsThreads, 0, st, a, together)
-                         : launch_next(bounds_kernel<FMT, 2>, g, kBoundsThreads, 0, st, a, together);
+  return launch_next(bounds_kernel<FMT, G>, g, kBoundsThreads, 0, st, a, together);
+}
+
+template <int FMT>
+cudaError_t launch_format(const BoundsArgs& a, int pages, cudaStream_t st) {
+  return a.p.groups == 1 ? launch_format<FMT, 1>(a, pages, st) : launch_format<FMT, 2>(a, pages, st);
 }
 
 }  // namespace
