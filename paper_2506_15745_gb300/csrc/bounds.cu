@@ -310,7 +310,8 @@ __device__ uint32_t mark_largest(uint32_t* keys, int first, int end, int need, i
 // page's 2 dim + 4 bytes are read once for a row. 32 ragged streams of up to 769 pages, 8 KV heads with 8 query
 // heads each (31 MB): 14.5 us, 2.1 TB/s. The longest streams' blocks set the time: 7 dependent rounds of loads per warp (about
 // 7 us), then the selection with its barriers (2.5 us); without the products 2.4 us less. More warps per list
-// (512 threads: 15.1 us, spills) or four blocks per SM (64 registers: 30 us) were slower. One stream, 98 pages: 4.8 us.
+// (512 threads: 15.1 us, spills), four blocks per SM (64 registers: 30 us) and rings of 3 tiles in shared memory
+// (asynchronous copies: 14.4 us, of equally long streams 18.2 against 15.8) were slower or no faster. One stream, 98 pages: 4.8 us.
 template <int DP>
 __global__ void __launch_bounds__(kChooseThreads, 2) choose_kernel(ChooseArgs a) {
   constexpr int kCodes = 2 * DP;              // bytes of a page's bounds, and of a query head's parts
@@ -515,10 +516,6 @@ cudaError_t choose_prepare() {
   cudaError_t e = cudaFuncSetAttribute(choose_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kChooseSmem);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(choose_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kChooseSmem);
   return e;
-}
-
-int64_t choose_smem_bytes(int padded, int head_tiles, int64_t pages) {
-  return static_cast<int64_t>(padded == 64 ? choose_smem<64>(head_tiles, 0) : choose_smem<128>(head_tiles, 0)) + 4 * pages;
 }
 
 cudaError_t launch_choose(const ChooseArgs& a, int pages, cudaStream_t st) {

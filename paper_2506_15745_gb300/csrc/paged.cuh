@@ -267,7 +267,6 @@ struct ChooseArgs {
 constexpr int kChooseThreads = 256;
 constexpr int kChooseSmem = 227 * 1024;
 cudaError_t choose_prepare();     // once per device
-int64_t choose_smem_bytes(int padded, int head_tiles, int64_t pages);
 cudaError_t launch_choose(const ChooseArgs& a, int pages, cudaStream_t st);
 
 // Every row that the new rows of a sequence may read, widened from codes to

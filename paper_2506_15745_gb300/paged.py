@@ -103,7 +103,7 @@ class Rotary:
         sections = [table.shape[1] // 2] if sections is None else [int(n) for n in sections]
         _need(1 <= len(sections) <= 4, "positions have 1 to 4 axes")
         _fits(32, **{f"section {i}": n for i, n in enumerate(sections)})
-        self.table, self.sections, self.interleaved = table, sections, bool(interleaved)
+        self.table, self.sections, self.axes, self.interleaved = table, sections, len(sections), bool(interleaved)
         self.struct = ipv.RotaryDesc(table.data_ptr(), table.shape[0], table.shape[1], int(self.interleaved), len(sections),
                                      (ctypes.c_int * 4)(*sections))
         self.at = ctypes.addressof(self.struct)
@@ -413,6 +413,10 @@ class PagedCache:
               lse.shape[0] >= batch.total_rows and lse.shape[1] == n_q_heads,
               "lse must be a contiguous fp32 CUDA tensor [total_rows, n_q_heads]")
 
+    def _check_weight(self, name, w):
+        if w.dtype is not torch.bfloat16 or not w.is_cuda or w.shape != (self.head_dim,) or not w.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous bf16 CUDA tensor [{self.head_dim}]")
+
     def write_rotated(self, q, k_new, v_new, batch: PagedBatch, rotary: Rotary, positions, *, q_weight=None, k_weight=None,
                       eps: float = 1e-6, q_out=None, stream=None):
         """ipv_pages_write_rotated: k_new (normalised with k_weight if given, rotated) and v_new into the batch's pages,
@@ -429,15 +433,16 @@ class PagedCache:
         if (new != (rows, heads, dim) or k_new.dtype is not bf16 or not k_new.is_cuda or strides[2] != 1 or v_new.shape != new or
                 v_new.dtype is not bf16 or not v_new.is_cuda or v_new.stride() != strides):
             strides = self._pair("k_new", k_new, "v_new", v_new, batch)  # may be longer
-        at_shape, at_strides, axes = positions.shape, positions.stride(), len(rotary.sections)
+        at_shape, at_strides, axes = positions.shape, positions.stride(), rotary.axes
         if len(at_shape) == 1 and axes == 1:
             at_shape, at_strides = (1, at_shape[0]), (at_shape[0], at_strides[0])
         if (len(at_shape) != 2 or at_shape[0] != axes or at_shape[1] < rows or (at_strides[1] != 1 and at_shape[1] > 1) or
                 positions.dtype is not torch.int32 or not positions.is_cuda):
             raise ValueError(f"positions must be an int32 CUDA tensor [{axes}, {rows}], contiguous along its last dimension")
-        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-            if w is not None and (w.dtype is not bf16 or not w.is_cuda or w.shape != (dim,) or not w.is_contiguous()):
-                raise ValueError(f"{name} must be a contiguous bf16 CUDA tensor [{dim}]")
+        if q_weight is not None:
+            self._check_weight("q_weight", q_weight)
+        if k_weight is not None:
+            self._check_weight("k_weight", k_weight)
         at = ipv._stream(stream)
         if q_out is None:
             q_out, = self._results(q, [shape], stream, at)
@@ -457,9 +462,9 @@ class PagedCache:
         """ipv_pages_copy: page target[i] becomes a copy of page source[i], int32 CUDA tensors [n]. No page is in target
         twice, or in target and at another place in source."""
         n = source.shape
-        for name, t in (("source", source), ("target", target)):
-            if t.dtype is not torch.int32 or not t.is_cuda or len(t.shape) != 1 or not t.is_contiguous():
-                raise ValueError(f"{name} must be a contiguous int32 CUDA tensor [n]")
+        if (source.dtype is not torch.int32 or target.dtype is not torch.int32 or not source.is_cuda or not target.is_cuda or len(n) != 1 or
+                not source.is_contiguous() or not target.is_contiguous()):
+            raise ValueError("source and target must be contiguous int32 CUDA tensors [n]")
         if target.shape != n:
             raise ValueError("source and target must have one length")
         status = self._lib.ipv_pages_copy(self.at, source.data_ptr(), target.data_ptr(), n[0], ipv._stream(stream))

@@ -433,6 +433,21 @@ def test_lists_by_strides_and_one_for_all_heads():
     check_chosen(s, q, one.cpu(), out, lse, 128 ** -0.5)
 
 
+@pytest.mark.parametrize("rows", [1, 90])  # a cluster or a block for each list; blocks in turn
+def test_rows_of_no_sequence_are_left_alone(rows):
+    gen = torch.Generator().manual_seed(55)
+    s = Setup(gen, "bf16", 4, 128, 16, [700, 60, 800], [rows, 0, rows])
+    chosen = random_lists(gen, s, 40)
+    more = torch.cat([chosen, chosen[:1].expand(9, 4, 40)]).cuda()
+    q = make_rows(gen, s.total + 9, 8, 128)
+    batch = PagedBatch(s.batch.table, s.batch.row_start, s.batch.kv_len, total_rows=s.total + 9, max_rows=rows, max_kv=800)
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full(q.shape[:2], 7.0, device="cuda")
+    s.cache.attend_chosen(q.cuda(), batch, more, out=out, lse=lse)
+    assert (out[s.total:] == 7.0).all() and (lse[s.total:] == 7.0).all()
+    check_chosen(s, q[:s.total], chosen, out[:s.total], lse[:s.total], 128 ** -0.5)
+
+
 def test_one_page_per_sequence():
     gen = torch.Generator().manual_seed(57)
     k, v = make_rows(gen, 3, 2, 300, 128), make_rows(gen, 3, 2, 300, 128)
