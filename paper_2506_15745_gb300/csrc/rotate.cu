@@ -9,7 +9,8 @@
 // all the heads that they take, the next four heads on their way meanwhile. 16 frames
 // (59 MB, 9 us at the copy rate) take 13.2 us; issue slots, at about 300
 // instructions per four heads, and the look-ups at a row's start (position, then angles;
-// sequence, then page). 80 registers: at 64 it spills (16.3 us).
+// sequence, then page). 80 registers: at 64 it spills (16.3 us). Rows of 64 channels have one chunk
+// for a lane (784 rows of 32 + 8 heads 4.8 us; with an empty second chunk 7.1).
 #include "paged_codes.cuh"
 
 namespace ipv {
@@ -55,41 +56,44 @@ __device__ __forceinline__ uint4 pack(const float (&y)[8]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// A head's row, chunks c and c + 8 of it in x: normalised with w (NULL: not), rotated. For whole warps, of which some
+// A head's row, chunk c and, where rows have more than 64 channels (G = 2), chunk c + 8 of it in x: normalised with w (NULL: not), rotated. For whole warps, of which some
 // teams may have queries, some keys, and one kind no norm.
-template <int PAIRS>
-__device__ __forceinline__ void rotate(const RotateArgs& a, uint4 (&x)[2], const uint16_t* w, const Turn (&turn)[2], int c) {
-  float y[2][8];
-  unpack(x[0], y[0]);
-  unpack(x[1], y[1]);
+template <int PAIRS, int G>
+__device__ __forceinline__ void rotate(const RotateArgs& a, uint4 (&x)[G], const uint16_t* w, const Turn (&turn)[G], int c) {
+  float y[G][8];
+#pragma unroll
+  for (int g = 0; g < G; ++g) unpack(x[g], y[g]);
+  auto two = [](float (&z)[8], int i) { return make_float2(z[2 * i], z[2 * i + 1]); };  // packed arithmetic, two channels at once
+  auto put = [](float (&z)[8], int i, float2 v) { z[2 * i] = v.x, z[2 * i + 1] = v.y; };
   if (a.q_weight || a.k_weight) {
-    float sum = 0.0f;
+    float2 sums = make_float2(0.0f, 0.0f);
 #pragma unroll
-    for (int g = 0; g < 2; ++g)
+    for (int g = 0; g < G; ++g)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum = fmaf(y[g][i], y[g][i], sum);
+      for (int i = 0; i < 4; ++i) sums = fma2(two(y[g], i), two(y[g], i), sums);
+    float sum = sums.x + sums.y;
 #pragma unroll
     for (int d = 1; d < 8; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     const float inv = rsqrtf(sum * a.by_dim + a.eps);
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
+    for (int g = 0; g < G; ++g) {
       if (!w || 8 * (c + 8 * g) >= a.p.dim) continue;
       float v[8];
       unpack(*reinterpret_cast<const uint4*>(w + 8 * (c + 8 * g)), v);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[g][i] *= inv * v[i];
+      for (int i = 0; i < 4; ++i) put(y[g], i, __fmul2_rn(two(y[g], i), __fmul2_rn(two(v, i), make_float2(inv, inv))));
     }
   }
-  if (PAIRS == kOwn) {
+  if constexpr (PAIRS == kOwn) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float lo = y[0][i], hi = y[1][i];
       y[0][i] = lo * turn[0].c[i] - hi * turn[0].s[i];
       y[1][i] = hi * turn[0].c[i] + lo * turn[0].s[i];
     }
-  } else if (PAIRS == kNeighbours) {
+  } else if constexpr (PAIRS == kNeighbours) {
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
+    for (int g = 0; g < G; ++g) {
       if (8 * (c + 8 * g) >= a.rot) continue;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -98,11 +102,19 @@ __device__ __forceinline__ void rotate(const RotateArgs& a, uint4 (&x)[2], const
         y[g][2 * i + 1] = hi * turn[g].c[i] + lo * turn[g].s[i];
       }
     }
-  } else {
-    const int half = a.rot / 16;  // in chunks
-    float z[2][8];
+  } else if (G == 1 || a.rot <= 64) {  // all in the first chunks
+    const int half = a.rot / 16, other = c < half ? c + half : c - half;  // any lane for a chunk that is not rotated
+    float z[8];
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
+    for (int i = 0; i < 8; ++i) z[i] = __shfl_sync(0xffffffffu, y[0][i], other & 7, 8);
+    if (c < 2 * half)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[0][i] = y[0][i] * turn[0].c[i] + (c < half ? -z[i] : z[i]) * turn[0].s[i];
+  } else if constexpr (G == 2) {
+    const int half = a.rot / 16;  // in chunks
+    float z[G][8];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
       const int n = c + 8 * g, other = n < half ? n + half : n - half;  // any lane for a chunk that is not rotated
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -111,7 +123,7 @@ __device__ __forceinline__ void rotate(const RotateArgs& a, uint4 (&x)[2], const
       }
     }
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
+    for (int g = 0; g < G; ++g) {
       const int n = c + 8 * g;
       if (n >= 2 * half) continue;
 #pragma unroll
@@ -119,15 +131,15 @@ __device__ __forceinline__ void rotate(const RotateArgs& a, uint4 (&x)[2], const
         y[g][i] = n < half ? y[g][i] * turn[g].c[i] - z[g][i] * turn[g].s[i] : y[g][i] * turn[g].c[i] + z[g][i] * turn[g].s[i];
     }
   }
-  x[0] = pack(y[0]);
-  x[1] = pack(y[1]);
+#pragma unroll
+  for (int g = 0; g < G; ++g) x[g] = pack(y[g]);
 }
 
 // One chunk of each group of a row of K or V into the pool.
-template <int FMT>
-__device__ __forceinline__ void store(const Pages& p, char* pool, uint32_t* par, int64_t row, const uint4 (&x)[2], int c) {
+template <int FMT, int G>
+__device__ __forceinline__ void store(const Pages& p, char* pool, uint32_t* par, int64_t row, const uint4 (&x)[G], int c) {
 #pragma unroll
-  for (int g = 0; g < 2; ++g) {
+  for (int g = 0; g < G; ++g) {
     if (FMT == kBf16) {
       if (row >= 0 && 8 * (c + 8 * g) < p.dim) *reinterpret_cast<uint4*>(pool + row * p.row_bytes + 16 * (c + 8 * g)) = x[g];
     } else if (g < p.groups) {  // whole warps
@@ -160,8 +172,8 @@ __device__ __forceinline__ int sequence_of(const Pages& p, int64_t row) {
   }
 }
 
-template <int FMT, int PAIRS>
-__global__ void __launch_bounds__(kBlock, PAIRS == kOwn ? 6 : 4) rotate_kernel(RotateArgs a) {
+template <int FMT, int PAIRS, int G>
+__global__ void __launch_bounds__(kBlock, PAIRS == kOwn || G == 1 ? 6 : 4) rotate_kernel(RotateArgs a) {
   pdl_trigger();
   pdl_wait();
   const int warp = threadIdx.x >> 5, shift = a.row_warps_shift, row_warps = 1 << shift;
@@ -169,27 +181,27 @@ __global__ void __launch_bounds__(kBlock, PAIRS == kOwn ? 6 : 4) rotate_kernel(R
   const int c = threadIdx.x & 7, items = a.q_heads + a.p.heads;
   const int first = (warp & (row_warps - 1)) * 4, mine = (threadIdx.x & 31) >> 3;  // a warp's items, the team's among them
   if (first >= items || row >= a.p.total_rows) return;
-  auto load = [&](const uint16_t* from, uint4 (&x)[2], bool in) {
+  auto load = [&](const uint16_t* from, uint4 (&x)[G], bool in) {
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
+    for (int g = 0; g < G; ++g) {
       const int ch = 8 * (c + 8 * g);
       x[g] = make_uint4(0, 0, 0, 0);
       if (in && ch < a.p.dim) x[g] = ld_once(from + ch);
     }
   };
-  auto load_item = [&](int base, uint4 (&x)[2], uint4 (&v)[2]) {
+  auto load_item = [&](int base, uint4 (&x)[G], uint4 (&v)[G]) {
     const int item = base + mine, h = item - a.q_heads;
     load(h < 0 ? a.q + row * a.q_row + item * a.q_head : a.k_new + row * a.row + h * a.head, x, item < items);
     if (base + 4 > a.q_heads) load(a.v_new + row * a.row + h * a.head, v, h >= 0 && item < items);
   };
-  uint4 x[2], v[2] = {};
+  uint4 x[G], v[G] = {};
   load_item(first, x, v);  // on their way while positions, turns, sequence and page are looked up
-  Turn turn[2];
+  Turn turn[G];
   if (PAIRS == kOwn) {
     load_turn<8>(a, row, 8 * c, turn[0]);
   } else {
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
+    for (int g = 0; g < G; ++g) {
       const int n = c + 8 * g, half = a.rot / 16;
       if (n >= 2 * half) continue;
       if (PAIRS == kNeighbours)
@@ -205,23 +217,23 @@ __global__ void __launch_bounds__(kBlock, PAIRS == kOwn ? 6 : 4) rotate_kernel(R
   for (int base = first; base < items; base += 4 * row_warps) {  // the same for a whole warp
     const int item = base + mine, h = item - a.q_heads;
     const bool in = item < items, q = in && h < 0;
-    uint4 x_next[2] = {}, v_next[2] = {};
+    uint4 x_next[G] = {}, v_next[G] = {};
     if (base + 4 * row_warps < items) load_item(base + 4 * row_warps, x_next, v_next);
     int64_t to = -1;
     if (base + 4 > a.q_heads) {
       if (in && !q && j >= 0) to = pool_row(a.p, b, j);
       if (to >= 0) to += h * a.p.head_stride;
-      store<FMT>(a.p, a.p.v, a.p.v_par, to, v, c);
+      store<FMT, G>(a.p, a.p.v, a.p.v_par, to, v, c);
     }
-    rotate<PAIRS>(a, x, q ? a.q_weight : a.k_weight, turn, c);
+    rotate<PAIRS, G>(a, x, q ? a.q_weight : a.k_weight, turn, c);
     if (q) {
 #pragma unroll
-      for (int g = 0; g < 2; ++g)
+      for (int g = 0; g < G; ++g)
         if (8 * (c + 8 * g) < a.p.dim) *reinterpret_cast<uint4*>(a.q_out + row * a.out_row + item * a.out_head + 8 * (c + 8 * g)) = x[g];
     }
-    if (base + 4 > a.q_heads) store<FMT>(a.p, a.p.k, a.p.k_par, to, x, c);
+    if (base + 4 > a.q_heads) store<FMT, G>(a.p, a.p.k, a.p.k_par, to, x, c);
 #pragma unroll
-    for (int g = 0; g < 2; ++g) x[g] = x_next[g], v[g] = v_next[g];
+    for (int g = 0; g < G; ++g) x[g] = x_next[g], v[g] = v_next[g];
   }
 }
 
@@ -229,9 +241,11 @@ template <int FMT>
 cudaError_t launch(const RotateArgs& a, cudaStream_t st) {
   const int rows = kBlockWarps >> a.row_warps_shift;
   const dim3 g(static_cast<unsigned>((a.p.total_rows + rows - 1) / rows));
-  if (a.neighbours) return launch_next(rotate_kernel<FMT, kNeighbours>, g, kBlock, 0, st, a);
-  if (a.rot == 128) return launch_next(rotate_kernel<FMT, kOwn>, g, kBlock, 0, st, a);
-  return launch_next(rotate_kernel<FMT, kHalves>, g, kBlock, 0, st, a);
+  if (a.p.dim <= 64)
+    return a.neighbours ? launch_next(rotate_kernel<FMT, kNeighbours, 1>, g, kBlock, 0, st, a) : launch_next(rotate_kernel<FMT, kHalves, 1>, g, kBlock, 0, st, a);
+  if (a.neighbours) return launch_next(rotate_kernel<FMT, kNeighbours, 2>, g, kBlock, 0, st, a);
+  if (a.rot == 128) return launch_next(rotate_kernel<FMT, kOwn, 2>, g, kBlock, 0, st, a);
+  return launch_next(rotate_kernel<FMT, kHalves, 2>, g, kBlock, 0, st, a);
 }
 
 }  // namespace

@@ -274,6 +274,14 @@ class PagedCache:
             raise ValueError(f"{name} must be a bf16 CUDA tensor [{batch.total_rows}, {heads}, {dim}] with contiguous rows")
         return strides
 
+    def _alike(self, k, v, batch):
+        """The strides of K's and V's rows where they are just what most calls give; None: _pair is to look closer."""
+        shape, strides, bf16 = k.shape, k.stride(), torch.bfloat16
+        if (shape == (batch.total_rows, self.n_kv_heads, self.head_dim) and v.shape == shape and strides[2] == 1 and v.stride() == strides and
+                k.dtype is bf16 and v.dtype is bf16 and k.is_cuda and v.is_cuda):
+            return strides
+        return None
+
     def _pair(self, k_name, k, v_name, v, batch):
         strides = self._packed(k_name, k, batch, self.n_kv_heads, self.head_dim)
         if v.shape != k.shape or v.dtype is not torch.bfloat16 or not v.is_cuda:
@@ -298,7 +306,7 @@ class PagedCache:
 
     def write(self, k_new, v_new, batch: PagedBatch, stream=None) -> None:
         """ipv_pages_write: k_new, v_new bf16 [total_rows, n_kv_heads, head_dim] into the batch's pages."""
-        strides = self._pair("k_new", k_new, "v_new", v_new, batch)
+        strides = self._alike(k_new, v_new, batch) or self._pair("k_new", k_new, "v_new", v_new, batch)
         status = self._lib.ipv_pages_write(self.at, batch.at, k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1],
                                            ipv._stream(stream))
         if status:
@@ -313,7 +321,7 @@ class PagedCache:
             new = self._results(self.k, [shape] * ((k_out is None) + (v_out is None)), stream, at)
             k_out = new.pop(0) if k_out is None else k_out
             v_out = new.pop(0) if v_out is None else v_out
-        strides = self._pair("k_out", k_out, "v_out", v_out, batch)
+        strides = self._alike(k_out, v_out, batch) or self._pair("k_out", k_out, "v_out", v_out, batch)
         status = self._lib.ipv_pages_read(self.at, batch.at, k_out.data_ptr(), v_out.data_ptr(), strides[0], strides[1], at)
         if status:
             ipv._check(status)
@@ -424,15 +432,12 @@ class PagedCache:
         (allocated if None, on the call's stream; q itself will do), which is returned. positions: int32
         [total_rows] or [axes, total_rows], places in the rotary's table: a row's place in the stream, which a
         compacted cache does not tell. weights: bf16 [head_dim]. One host thread at a time uses a cache object."""
-        rows, heads, dim, bf16 = batch.total_rows, self.n_kv_heads, self.head_dim, torch.bfloat16
+        rows, dim, bf16 = batch.total_rows, self.head_dim, torch.bfloat16
         shape, qs = q.shape, q.stride()
         n_q_heads = shape[1] if len(shape) == 3 else 0
         if not n_q_heads or shape[0] < rows or shape[2] != dim or q.dtype is not bf16 or not q.is_cuda or qs[2] != 1:
             self._packed("q", q, batch, n_q_heads, dim)
-        new, strides = k_new.shape, k_new.stride()
-        if (new != (rows, heads, dim) or k_new.dtype is not bf16 or not k_new.is_cuda or strides[2] != 1 or v_new.shape != new or
-                v_new.dtype is not bf16 or not v_new.is_cuda or v_new.stride() != strides):
-            strides = self._pair("k_new", k_new, "v_new", v_new, batch)  # may be longer
+        strides = self._alike(k_new, v_new, batch) or self._pair("k_new", k_new, "v_new", v_new, batch)
         at_shape, at_strides, axes = positions.shape, positions.stride(), rotary.axes
         if len(at_shape) == 1 and axes == 1:
             at_shape, at_strides = (1, at_shape[0]), (at_shape[0], at_strides[0])
