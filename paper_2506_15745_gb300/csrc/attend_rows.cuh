@@ -353,23 +353,31 @@ __global__ void __launch_bounds__(kThreads, (Layout<FMT, DP, NR, CHOSEN>::kBlock
              ok ? from + ((up ? h.at[1] : h.at[0]) + r * next_bytes + lane_at) : from, ok);
     }
   };
-  // K's or V's rows and, of codes, their pairs.
-  auto copy_side = [&](const char* from, const uint32_t* par, uint32_t to, uint32_t par_to, const Halves& h) {
-    if constexpr (!kB) {
-      constexpr int kN = R::kG * 4;
-      const bool ok = (lane & 15) < (lane < 16 ? h.n[0] : h.n[1]);
-      const int64_t at = ok ? ((lane < 16 ? h.at[0] : h.at[1]) + (lane & 15) * next_bytes) / (R::kRowB / kN) : 0;
-      copy_small<kN>(par_to + lane * kN, reinterpret_cast<const char*>(par) + at, ok);
-    }
-    copy_rows(from, to, h);
+  // Codes: the pairs of this lane's row, in bytes from a pool's first; -1: not to be copied.
+  constexpr int kPairB = kB ? 4 : R::kG * 4;
+  auto pairs_at = [&](const Halves& h) {
+    const bool ok = (lane & 15) < (lane < 16 ? h.n[0] : h.n[1]);
+    return ok ? ((lane < 16 ? h.at[0] : h.at[1]) + (lane & 15) * next_bytes) / (R::kRowB / kPairB) : int64_t{-1};
+  };
+  auto copy_pairs = [&](const uint32_t* par, uint32_t to, int64_t at) {
+    copy_small<kPairB>(to + lane * kPairB, reinterpret_cast<const char*>(par) + max(at, int64_t{0}), at >= 0);
   };
   auto issue_chosen = [&](const Halves& h, int stage) {
     const uint32_t base = ring + stage * R::kStage;
-    copy_side(a.p.k, a.p.k_par, base, base + 2 * R::kTile, h);
-    copy_side(a.p.v, a.p.v_par, base + R::kTile, base + 2 * R::kTile + R::kPar, h);
+    if constexpr (!kB) {
+      const int64_t at = pairs_at(h);
+      copy_pairs(a.p.k_par, base + 2 * R::kTile, at);
+      copy_pairs(a.p.v_par, base + 2 * R::kTile + R::kPar, at);
+    }
+    copy_rows(a.p.k, base, h);
+    copy_rows(a.p.v, base + R::kTile, h);
   };
-  auto copy_k = [&](int half, const Halves& h) { copy_side(a.p.k, a.p.k_par, ring + half * L::kHalf, ring + half * L::kHalf + R::kTile, h); };
-  auto copy_v = [&](int half, const Halves& h) { copy_side(a.p.v, a.p.v_par, ring + half * L::kHalf, ring + half * L::kHalf + R::kTile, h); };
+  auto copy_half = [&](const char* from, const uint32_t* par, int half, const Halves& h) {
+    if constexpr (!kB) copy_pairs(par, ring + half * L::kHalf + R::kTile, pairs_at(h));
+    copy_rows(from, ring + half * L::kHalf, h);
+  };
+  auto copy_k = [&](int half, const Halves& h) { copy_half(a.p.k, a.p.k_par, half, h); };
+  auto copy_v = [&](int half, const Halves& h) { copy_half(a.p.v, a.p.v_par, half, h); };
   uint32_t seen_now = 0, seen_next = 0, seen_last = 0;  // keys of the step at hand and of the ones after it
   // The first steps of a run, and the page of the one after them.
   int page_next = -1;
