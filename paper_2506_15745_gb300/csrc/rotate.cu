@@ -56,8 +56,8 @@ __device__ __forceinline__ uint4 pack(const float (&y)[8]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// A head's row, chunk c and, where rows have more than 64 channels (G = 2), chunk c + 8 of it in x: normalised with w (NULL: not), rotated. For whole warps, of which some
-// teams may have queries, some keys, and one kind no norm.
+// A head's row, chunk c and, where rows have more than 64 channels (G = 2), chunk c + 8 of it in x: normalised with
+// w (NULL: not), rotated. For whole warps, of which some teams may have queries, some keys, and one kind no norm.
 template <int PAIRS, int G>
 __device__ __forceinline__ void rotate(const RotateArgs& a, uint4 (&x)[G], const uint16_t* w, const Turn (&turn)[G], int c) {
   float y[G][8];
@@ -242,7 +242,8 @@ cudaError_t launch(const RotateArgs& a, cudaStream_t st) {
   const int rows = kBlockWarps >> a.row_warps_shift;
   const dim3 g(static_cast<unsigned>((a.p.total_rows + rows - 1) / rows));
   if (a.p.dim <= 64)
-    return a.neighbours ? launch_next(rotate_kernel<FMT, kNeighbours, 1>, g, kBlock, 0, st, a) : launch_next(rotate_kernel<FMT, kHalves, 1>, g, kBlock, 0, st, a);
+    return a.neighbours ? launch_next(rotate_kernel<FMT, kNeighbours, 1>, g, kBlock, 0, st, a)
+                        : launch_next(rotate_kernel<FMT, kHalves, 1>, g, kBlock, 0, st, a);
   if (a.neighbours) return launch_next(rotate_kernel<FMT, kNeighbours, 2>, g, kBlock, 0, st, a);
   if (a.rot == 128) return launch_next(rotate_kernel<FMT, kOwn, 2>, g, kBlock, 0, st, a);
   return launch_next(rotate_kernel<FMT, kHalves, 2>, g, kBlock, 0, st, a);
