@@ -302,7 +302,8 @@ void make_plan(ipv::AttendArgs* a, int num_sms, Plan* plan) {
   // Keys that a row tile can see, at most (its windows, the sinks, their steps' ends).
   int64_t span = p.max_kv;
   if (a->n_chosen > 0) {
-    span = std::min((span + p.page_size - 1) / p.page_size, static_cast<int64_t>(a->n_chosen)) * p.page_size;
+    const int64_t pages = (span + p.page_size - 1) / p.page_size;
+    if (pages > 1) span = std::min(pages, static_cast<int64_t>(a->n_chosen)) * p.page_size;
   } else if (a->window) {
     const int64_t seen = static_cast<int64_t>(a->window) + a->tile + a->sinks + 2 * (plan->tiles ? ipv::kTilesStep : ipv::kRowsStep);
     if (seen < span) span = seen;

@@ -162,11 +162,14 @@ __device__ __forceinline__ int pages_seen(const AttendArgs& a, const Seq& s, int
   return hi > 0 ? ((hi - 1) >> a.p.page_shift) + 1 : 0;
 }
 
-// The steps over the pages that token `tok` has chosen: keys count through its list.
+// The steps over the pages that token `tok` has chosen: keys count through its list. A row that sees one page ends in it at
+// itself, however long the page is (a cache without a table is one page). At most 2^30 keys: max_kv is checked to be no more,
+// and several pages are powers of two below it.
 template <int STEP>
 __device__ __forceinline__ KeyRange chosen_range(const AttendArgs& a, const Seq& s, int tok) {
   KeyRange r = {};
-  r.hi_min = r.hi_max = min(a.n_chosen, pages_seen(a, s, tok)) * a.p.page_size;  // <= 2^30 + a page, checked
+  const int pages = pages_seen(a, s, tok);
+  r.hi_min = r.hi_max = pages > 1 ? min(a.n_chosen, pages) * a.p.page_size : token_hi(a, s, tok);
   r.steps = r.hi_max > 0 ? (r.hi_max - 1) / STEP + 1 : 0;
   return r;
 }

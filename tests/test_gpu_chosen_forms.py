@@ -1,0 +1,53 @@
+"""Rotated writes, choices and attention over chosen pages in the forms that a call may take beside the usual ones: one long page
+for each sequence."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import chosen_ref as cref  # noqa: E402
+from paper_2506_15745_gb300 import ipv  # noqa: E402
+from paper_2506_15745_gb300.paged import PagedBatch, PagedCache  # noqa: E402
+from test_gpu_chosen import ints, same_bits  # noqa: E402
+from test_gpu_paged import bounds, make_rows  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+def chosen_need(cache, batch, n_q_heads, n_chosen):
+    """Bytes of workspace that attend_chosen takes for these sizes; 0 where no tile is shared out."""
+    return ipv.attend_chosen_workspace(cache.ref, batch.ref, ipv.AttendArgs(n_q_heads=n_q_heads, scale=1.0, causal=1), ipv.Chosen(n_chosen=n_chosen))
+
+
+@pytest.mark.parametrize("fmt,held", [("bf16", 300), ("bf16", 3000), ("u8", 300), ("u4", 1000)])
+def test_a_page_may_be_longer_than_the_sequence(fmt, held):
+    """One page per sequence, as of_layer gives: the work goes by the rows held, not by the page's length, so a longer page is shared
+    out in the same way and gives the same bits."""
+    gen = torch.Generator().manual_seed(held)
+    lens, rows, heads, share, dim = [held, held // 3, 1], [2, 1, 1], 2, 4, 128
+    q = make_rows(gen, 4, heads * share, dim)
+    k, v = (make_rows(gen, sum(lens), heads, dim) for _ in range(2))
+    chosen = torch.zeros((4, heads, 1), dtype=torch.int32, device="cuda")
+    made = []
+    for size in (held, 9408):
+        cache = PagedCache(3, size, heads, dim, fmt)
+        whole = PagedBatch(None, ints(0, lens[0], sum(lens[:2]), sum(lens)), ints(*lens), total_rows=sum(lens), max_rows=held, max_kv=held)
+        cache.write(k.cuda(), v.cuda(), whole)
+        batch = PagedBatch(None, ints(0, 2, 3, 4), ints(*lens), total_rows=4, max_rows=2, max_kv=held)
+        assert chosen_need(cache, batch, heads * share, 1) == 0
+        lse = torch.zeros(4, heads * share, device="cuda")
+        made.append((cache.attend_chosen(q.cuda(), batch, chosen, lse=lse), lse, *cache.read(whole)))
+    assert all(same_bits(a, b) for a, b in zip(*made))
+    out, lse, k_held, v_held = made[0]
+    at, row = 0, 0
+    for n, r in zip(lens, rows):
+        kk, vv = k_held[at:at + n].double().cpu(), v_held[at:at + n].double().cpu()
+        o, l, weight, size = cref.attend(q[row:row + r].double(), kk, vv, chosen[row:row + r].cpu(), 9408, dim ** -0.5)
+        tol = bounds(fmt, weight, size, o, n, float(vv.abs().max()))
+        if fmt != "bf16":  # `read` rounds the codes' values to bf16: scores by 2^-8 of their products, values by 2^-8; a weight times
+            # its group's step is rounded by 2^-11 of itself, which stands before a code of up to (largest - least) / step
+            spread = float((vv.amax(-1) - vv.amin(-1)).max())
+            tol = tol + (2.0 ** -8 + torch.expm1(2.0 * 2.0 ** -8 * size[..., None])) * weight * 1.01 + 2.0 ** -11 * spread * 1.02
+        assert ((out[row:row + r].double().cpu() - o).abs() <= tol).all() and not math.isnan(float(lse.sum()))
+        at, row = at + n, row + r
