@@ -526,7 +526,7 @@ typedef struct {
   const void* q_weight;     /* device bf16 [head_dim], 16-byte aligned, or NULL */
   const void* k_weight;
   const int32_t* positions;
-  int64_t positions_stride; /* >= total_rows */
+  int64_t positions_stride; /* >= total_rows, or 0: one place on all axes */
 } ipv_rotate_args;
 
 ipv_status ipv_pages_write_rotated(const ipv_pages* pages, const ipv_batch* batch, const ipv_rotary* rotary,

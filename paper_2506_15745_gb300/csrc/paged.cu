@@ -554,8 +554,8 @@ extern "C" ipv_status ipv_pages_write_rotated(const ipv_pages* pages, const ipv_
     return reject(IPV_EINVAL, "q_out may be q only with q's strides");
   if (!rotary->table || !aligned(rotary->table, 16)) return reject(IPV_EINVAL, "the rotary table must not be NULL, and 16-byte aligned");
   if (!t->positions || !aligned(t->positions, 4)) return reject(IPV_EINVAL, "positions must not be NULL, and 4-byte aligned");
-  if (t->positions_stride < 0 || (rotary->n_axes > 1 && t->positions_stride < batch->total_rows))
-    return reject(IPV_EINVAL, "positions_stride is below total_rows");
+  if (t->positions_stride < 0 || (rotary->n_axes > 1 && t->positions_stride != 0 && t->positions_stride < batch->total_rows))
+    return reject(IPV_EINVAL, "positions_stride is neither 0 nor at least total_rows");
   a.q = static_cast<const uint16_t*>(t->q);
   a.q_out = static_cast<uint16_t*>(t->q_out);
   a.k_new = static_cast<const uint16_t*>(t->k_new);

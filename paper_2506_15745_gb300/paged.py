@@ -430,8 +430,8 @@ class PagedCache:
         """ipv_pages_write_rotated: k_new (normalised with k_weight if given, rotated) and v_new into the batch's pages,
         and q, bf16 [total_rows, n_q_heads, head_dim], normalised with q_weight if given and rotated, into q_out
         (allocated if None, on the call's stream; q itself will do), which is returned. positions: int32
-        [total_rows] or [axes, total_rows], places in the rotary's table: a row's place in the stream, which a
-        compacted cache does not tell. weights: bf16 [head_dim]. One host thread at a time uses a cache object."""
+        [total_rows] or [axes, total_rows] (one row expanded to all axes will do), places in the rotary's table: a row's place
+        in the stream, which a compacted cache does not tell. weights: bf16 [head_dim]. One host thread at a time uses a cache object."""
         rows, dim, bf16 = batch.total_rows, self.head_dim, torch.bfloat16
         shape, qs = q.shape, q.stride()
         n_q_heads = shape[1] if len(shape) == 3 else 0

@@ -1,5 +1,5 @@
 """Rotated writes, choices and attention over chosen pages in the forms that a call may take beside the usual ones: one long page
-for each sequence."""
+for each sequence, one place on all axes."""
 import math
 
 import pytest
@@ -8,8 +8,8 @@ torch = pytest.importorskip("torch")
 
 import chosen_ref as cref  # noqa: E402
 from paper_2506_15745_gb300 import ipv  # noqa: E402
-from paper_2506_15745_gb300.paged import PagedBatch, PagedCache  # noqa: E402
-from test_gpu_chosen import ints, same_bits  # noqa: E402
+from paper_2506_15745_gb300.paged import PagedBatch, PagedCache, Rotary  # noqa: E402
+from test_gpu_chosen import ints, same_bits, turns  # noqa: E402
 from test_gpu_paged import bounds, make_rows  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -51,3 +51,20 @@ def test_a_page_may_be_longer_than_the_sequence(fmt, held):
             tol = tol + (2.0 ** -8 + torch.expm1(2.0 * 2.0 ** -8 * size[..., None])) * weight * 1.01 + 2.0 ** -11 * spread * 1.02
         assert ((out[row:row + r].double().cpu() - o).abs() <= tol).all() and not math.isnan(float(lse.sum()))
         at, row = at + n, row + r
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_one_place_on_all_axes(interleaved):
+    """A text token has one position on every axis: a row expanded over the axes turns as the same row repeated."""
+    gen = torch.Generator().manual_seed(5)
+    q, k, v = make_rows(gen, 40, 8, 128), make_rows(gen, 40, 2, 128), make_rows(gen, 40, 2, 128)
+    table, at = turns(gen, 60, 128), torch.randint(0, 60, (1, 40), generator=gen, dtype=torch.int32)
+    rotary = Rotary(table.cuda(), [24, 24, 16], interleaved)
+    batch = PagedBatch(ints(2, 0, 1)[None], ints(0, 40), ints(45), total_rows=40, max_rows=40, max_kv=48)
+    made = []
+    for places in (at.cuda().expand(3, 40), at.expand(3, 40).contiguous().cuda()):
+        cache = PagedCache(3, 16, 2, 128)
+        made.append((cache.write_rotated(q.cuda(), k.cuda(), v.cuda(), batch, rotary, places), cache.k, cache.v))
+    assert all(same_bits(a, b) for a, b in zip(*made))
+    want, size = cref.turned(q, None, 0.0, table, at.expand(3, 40), [24, 24, 16], interleaved)
+    assert ((made[0][0].double().cpu() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -16 * size).all()
