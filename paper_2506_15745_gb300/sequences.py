@@ -9,6 +9,8 @@ as long as all calls on the pool go to one stream.
 """
 from __future__ import annotations
 
+from collections import Counter
+
 import torch
 
 from .paged import PagedBatch
@@ -28,6 +30,7 @@ class Sequences:
         self.n_pages, self.page_size = n_pages, page_size
         self._free = list(range(n_pages - 1, -1, -1))  # the last one goes first
         self._holders = [0] * n_pages
+        self._lent = Counter()  # pages that `replace` returned and `release` has not seen, each as often as it was lent
         self._pages, self._rows = {}, {}
         self._next = 0
 
@@ -108,11 +111,18 @@ class Sequences:
         self._count(rows)
         new = self._take(-(-rows // self.page_size))
         old, self._pages[seq], self._rows[seq] = self._pages[seq], new, rows
-        return old
+        self._lent.update(old)
+        return list(old)
 
     def release(self, pages) -> None:
-        """Gives back pages that `replace` returned, after the calls that read them have been enqueued."""
-        for page in pages:
+        """Gives back pages that `replace` returned, after the calls that read them have been enqueued. Each lending is given back
+        once: with any other page nothing is changed."""
+        back = Counter(map(int, pages))
+        for page, times in back.items():
+            if times > self._lent[page]:
+                raise ValueError(f"page {page} is lent to nobody, or was given back already")
+        self._lent -= back
+        for page in back.elements():
             self._drop(page)
 
     def remove(self, seq: int) -> None:
@@ -171,8 +181,6 @@ class Sequences:
         return out
 
     def _drop(self, page):
-        if not self._holders[page]:
-            raise ValueError(f"page {page} is held by nobody")
         self._holders[page] -= 1
         if not self._holders[page]:
             self._free.append(page)

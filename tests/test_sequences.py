@@ -178,3 +178,31 @@ def test_any_order_of_changes(seed):
         except OutOfPages:
             pass
         check(books, live, lent)
+
+
+def test_pages_are_given_back_once():
+    """What replace lent is given back by that lending alone: a second release, or one of pages never lent, takes nobody else's
+    pages away, and one bad page among others changes nothing."""
+    books = Sequences(8, 16)
+    a = books.add(40)
+    b = books.fork(a)
+    old = books.replace(a, 16)
+    with pytest.raises(ValueError, match="lent"):
+        books.release(old + [books.pages(a)[0]])
+    with pytest.raises(ValueError, match="lent"):
+        books.release(old[:1] + old)
+    check(books, [a, b], old)
+    books.release(iter(old))
+    check(books, [a, b])
+    with pytest.raises(ValueError, match="lent"):
+        books.release(old)
+    with pytest.raises(ValueError, match="lent"):
+        books.release(books.pages(b))
+    check(books, [a, b])
+    assert books.pages(b) == old and books.free_pages == 4
+    for bad in (-1, 8):
+        with pytest.raises(ValueError, match="lent"):
+            books.release([bad])
+    c = books.add(64)  # all that is free, and nothing of b
+    assert not set(books.pages(c)) & set(books.pages(b))
+    check(books, [a, b, c])
