@@ -37,30 +37,33 @@ ipv_status cuda_reject(cudaError_t e, const char* what) {
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 constexpr int kMaxDevices = 64;
+enum Kernels : int { kDense, kChosen, kChoice, kKernelSets };  // set up apart: a caller of one does not wait for the others
 struct DeviceSetup {
-  bool done = false;
+  bool done[kKernelSets] = {};
   int num_sms = 0;
 };
 DeviceSetup g_setup[kMaxDevices];
 std::mutex g_setup_mu;
 
-// Once per device, with that device current: kernel limits, SM count.
-ipv_status setup_current_device(int* num_sms) {
+// Once per device and set of kernels, with that device current: kernel limits, SM count.
+ipv_status setup_current_device(Kernels set, int* num_sms) {
   int dev = -1;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return cuda_reject(e, "cudaGetDevice");
   if (dev < 0 || dev >= kMaxDevices) return reject(IPV_EINVAL, "device ordinal %d not supported", dev);
   std::lock_guard<std::mutex> lock(g_setup_mu);
   DeviceSetup& d = g_setup[dev];
-  if (!d.done) {
-    if ((e = ipv::attend_rows_prepare()) != cudaSuccess)
-      return cuda_reject(e, "no usable kernel image for this device (built for sm_103a)");
-    if ((e = ipv::attend_tiles_prepare()) != cudaSuccess) return cuda_reject(e, "tiled attention set-up");
-    if ((e = ipv::attend_chosen_prepare()) != cudaSuccess) return cuda_reject(e, "chosen pages' attention set-up");
-    if ((e = ipv::choose_prepare()) != cudaSuccess) return cuda_reject(e, "page choice set-up");
+  if (!d.done[set]) {
+    const char* what = "no usable kernel image for this device (built for sm_103a)";
+    if (set == kDense) {
+      if ((e = ipv::attend_rows_prepare()) == cudaSuccess && (e = ipv::attend_tiles_prepare()) != cudaSuccess) what = "tiled attention set-up";
+    } else {
+      e = set == kChosen ? ipv::attend_chosen_prepare() : ipv::choose_prepare();
+    }
+    if (e != cudaSuccess) return cuda_reject(e, what);
     if ((e = cudaDeviceGetAttribute(&d.num_sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess)
       return cuda_reject(e, "cudaDeviceGetAttribute");
-    d.done = true;
+    d.done[set] = true;
   }
   *num_sms = d.num_sms;
   return IPV_OK;
@@ -412,7 +415,7 @@ ipv_status attend_workspace(const ipv_pages* pages, const ipv_batch* batch, cons
   if (s != IPV_OK) return s;
   if (a.p.n_seqs == 0 || a.p.max_rows == 0) return IPV_OK;
   int num_sms = 0;
-  if ((s = setup_current_device(&num_sms)) != IPV_OK) return s;
+  if ((s = setup_current_device(chosen ? kChosen : kDense, &num_sms)) != IPV_OK) return s;
   Plan plan;
   make_plan(&a, num_sms, &plan);
   *bytes_out = plan.bytes;
@@ -432,7 +435,7 @@ ipv_status attend(const ipv_pages* pages, const ipv_batch* batch, const ipv_atte
   if (chosen && (!chosen->pages || !aligned(chosen->pages, 4)))
     return reject(IPV_EINVAL, "the chosen pages must not be NULL, and 4-byte aligned");
   int num_sms = 0;
-  if ((s = setup_current_device(&num_sms)) != IPV_OK) return s;
+  if ((s = setup_current_device(chosen ? kChosen : kDense, &num_sms)) != IPV_OK) return s;
   Plan plan;
   make_plan(&a, num_sms, &plan);
   if (plan.bytes > 0) {
@@ -692,7 +695,7 @@ extern "C" ipv_status ipv_bounds_choose(const ipv_bounds* bounds, const ipv_batc
   if (s != IPV_OK) return s;
   if (!t->out || !aligned(t->out, 4)) return reject(IPV_EINVAL, "out must not be NULL, and 4-byte aligned");
   int num_sms = 0;
-  if ((s = setup_current_device(&num_sms)) != IPV_OK) return s;
+  if ((s = setup_current_device(kChoice, &num_sms)) != IPV_OK) return s;
   a.codes = static_cast<const char*>(bounds->codes);
   a.steps = bounds->steps;
   a.padded = padded(a.p.dim);
