@@ -1,0 +1,152 @@
+"""The calls around chosen pages at sizes that take other ways through the kernels than test_gpu_chosen.py's: rows by the
+thousand, whole caches' bounds, more lists than blocks. Against the same float64 definitions, within the same bounds; plain forms of these sizes run on the GPU in float64."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2506_15745_gb300.paged import PageBounds, PagedBatch, PagedCache, Rotary  # noqa: E402
+from test_gpu_chosen import Choice, ints, parts, same_bits, turns  # noqa: E402
+from test_gpu_paged import make_rows  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+def pool_and_batch(gen, fmt, heads, dim, page, seqs, spare_rows=0):
+    """An empty pool and a batch over it of sequences of (rows, kv); spare packed rows behind the last one."""
+    held = [-(-n // page) for _, n in seqs]
+    order, at = torch.randperm(sum(held) + 2, generator=gen).to(torch.int32), 0
+    table = torch.full((len(seqs), max(held)), -1, dtype=torch.int32)
+    for b, n in enumerate(held):
+        table[b, :n] = order[at:at + n]
+        at += n
+    start = [0]
+    for r, _ in seqs:
+        start.append(start[-1] + r)
+    cache = PagedCache(sum(held) + 2, page, heads, dim, fmt)
+    batch = PagedBatch(table.cuda(), ints(*start), ints(*[n for _, n in seqs]), total_rows=start[-1] + spare_rows,
+                       max_rows=max(r for r, _ in seqs), max_kv=max(n for _, n in seqs))
+    return cache, batch, start[-1]
+
+
+# ------------------------------------------------------------------- rotated writes
+def turned(x, weight, eps, table, at, sections, interleaved):
+    """chosen_ref.turned for whole tensors."""
+    x = x.double()
+    rot = table.shape[1]
+    if weight is not None:
+        x = x * weight.double() / torch.sqrt((x * x).mean(-1, keepdim=True) + eps)
+    axis = torch.repeat_interleave(torch.arange(len(sections)), torch.tensor(sections)).to(x.device)
+    f = torch.arange(rot // 2, device=x.device)
+    places = at[axis].long()                                     # [frequencies, rows]
+    c, s = (table.double()[places, f[:, None] + k].t()[:, None] for k in (0, rot // 2))
+    i, j = (2 * f, 2 * f + 1) if interleaved else (f, f + rot // 2)
+    a, b = x[..., i], x[..., j]
+    out, size = x.clone(), x.abs()
+    out[..., i], out[..., j] = a * c - b * s, b * c + a * s
+    size[..., i], size[..., j] = (a * c).abs() + (b * s).abs(), (b * c).abs() + (a * s).abs()
+    return out, size
+
+
+FORMS = [  # dim, heads, share, page, rot, sections, interleaved, norms
+    (128, 4, 7, 64, 128, [32, 16, 16], False, "qk"),
+    (128, 3, 4, 32, 96, [48], False, "k"),
+    (128, 2, 3, 16, 64, [16, 16], False, "qk"),
+    (128, 4, 5, 64, 128, [64], True, "q"),
+    (64, 5, 1, 32, 64, [32], False, "qk"),
+    (64, 2, 8, 64, 32, [8, 8], True, ""),
+]
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "u8", "u4"])
+@pytest.mark.parametrize("rows", [1000, 2800])  # two warps for a row (above 912), one (above 2736)
+@pytest.mark.parametrize("form", range(len(FORMS)))
+def test_many_rotated_rows(form, rows, fmt):
+    dim, heads, share, page, rot, sections, interleaved, norms = FORMS[form]
+    gen = torch.Generator().manual_seed(rows + form)
+    seqs = [(rows - 340, rows), (0, 7), (1, 1), (300, 1000), (39, 100)]
+    cache, batch, total = pool_and_batch(gen, fmt, heads, dim, page, seqs, spare_rows=3)
+    q, k, v = (make_rows(gen, total + 3, h, dim).cuda() for h in (heads * share, heads, heads))
+    w = {x: (1 + 0.3 * torch.randn(dim, generator=gen)).bfloat16().cuda() if x in norms else None for x in "qk"}
+    table, at = turns(gen, 50, rot).cuda(), torch.randint(0, 50, (len(sections), total + 3), generator=gen, dtype=torch.int32).cuda()
+    rotary = Rotary(table, sections, interleaved)
+    before = [t.clone() for t in parts(cache)]
+    out = torch.full_like(q, 5.0)
+    call = lambda c, o: c.write_rotated(q, k, v, batch, rotary, at, q_weight=w["q"], k_weight=w["k"], eps=1e-3, q_out=o)  # noqa: E731
+    call(cache, out)
+    assert (out[total:] == 5.0).all()
+    tol = lambda want, size: 2.0 ** -8 * want.abs() + 2.0 ** -16 * size + 1e-38  # noqa: E731
+    want, size = turned(q, w["q"], 1e-3, table, at, sections, interleaved)
+    assert ((out.double() - want).abs() <= tol(want, size))[:total].all()
+    plain = PagedCache(cache.n_pages, page, heads, dim)
+    call(plain, out)
+    k_back, v_back = plain.read(batch)
+    want, size = turned(k, w["k"], 1e-3, table, at, sections, interleaved)
+    assert ((k_back.double() - want).abs() <= tol(want, size))[:total].all() and same_bits(v_back[:total], v[:total])
+    after = [t.clone() for t in parts(cache)]
+    for t, old in zip(parts(cache), before):
+        t.copy_(old)
+    cache.write(k_back, v_back, batch)
+    assert all(same_bits(a, t) for a, t in zip(after, parts(cache)))  # the whole pool: nothing else was touched
+    again = q.clone()  # in place
+    cache.write_rotated(again, k, v, batch, rotary, at, q_weight=w["q"], k_weight=w["k"], eps=1e-3, q_out=again)
+    assert same_bits(again[:total], out[:total]) and same_bits(again[total:], q[total:])
+
+
+# ------------------------------------------------------------------- bounds of whole caches
+def bounds_of(k):
+    """Keys [..., rows, dim] -> codes [..., 2, dim], steps [...], by chosen_ref's rule."""
+    k = k.double()
+    top = k.abs().amax((-1, -2))
+    m, e = torch.frexp(top)  # top = m 2^e, 1/2 <= m < 1: at most 127 of 2^(e - 7) if m <= 127/128, else of 2^(e - 6)
+    e = torch.where(m * 128.0 <= 127.0, e - 7, e - 6).clamp(min=-40).long()
+    step = (e + 1023 << 52).view(torch.float64)  # 2^e to the bit, which a device's pow does not promise
+    lo, hi = (k.amin(-2) / step[..., None]).floor(), (k.amax(-2) / step[..., None]).ceil()
+    return torch.stack([lo, hi], -2), step
+
+
+@pytest.mark.parametrize("fmt,dim,page", [("bf16", 128, 64), ("bf16", 64, 64), ("bf16", 72, 128), ("u8", 128, 64), ("u8", 64, 64), ("u4", 128, 64),
+                                          ("u4", 64, 128)])
+def test_bounds_of_a_whole_cache(fmt, dim, page):
+    """More than 2048 pages and heads, of more rows than a warp reads at once: a warp for each, several rounds."""
+    gen = torch.Generator().manual_seed(dim)
+    heads, seqs = 16, [(page * 90 + 5,) * 2, (page * 50,) * 2, (page + 1,) * 2]
+    cache, batch, total = pool_and_batch(gen, fmt, heads, dim, page, seqs)
+    k, v = make_rows(gen, total, heads, dim).cuda(), make_rows(gen, total, heads, dim).cuda()
+    if fmt == "bf16":
+        for t in (cache.k, cache.v):
+            t.fill_(math.nan)  # behind the last rows
+    cache.write(k, v, batch)
+    made = PageBounds(cache)
+    made.codes.fill_(77), made.steps.fill_(77.0)
+    made.update(cache, batch)
+    k = cache.read(batch)[0]
+    want_codes, want_steps = torch.full_like(made.codes, 77), torch.full_like(made.steps, 77.0)
+    row = 0
+    for b, (n, _) in enumerate(seqs):
+        for i in range(-(-n // page)):
+            g, rows = int(batch.table[b, i]), min(page, n - i * page)
+            codes, step = bounds_of(k[row:row + rows].transpose(0, 1))
+            want_codes[g] = 0
+            want_codes[g, ..., :dim], want_steps[g] = codes.to(torch.int8), step.float()
+            row += rows
+    assert sum(-(-n // page) for n, _ in seqs) * heads > 2048 and len(set(made.steps.flatten().tolist())) > 2
+    assert torch.equal(made.steps, want_steps) and torch.equal(made.codes, want_codes)
+
+
+# ------------------------------------------------------------------- more lists than blocks
+@pytest.mark.parametrize("levels", [60, 1])
+@pytest.mark.parametrize("dim,heads,share,n,seqs", [
+    (128, 4, 8, 24, [(1, 8000 - 150 * b) for b in range(45)]),             # tokens of ragged streams, up to 500 pages
+    (128, 4, 7, 24, [(61, 6400), (0, 5000), (2, 30)]),                     # a question's rows, each with lists of its own
+    (64, 8, 3, 96, [(1, 16 * 300 + b) for b in range(24)]),
+    (80, 2, 16, 300, [(60, 16 * 700), (60, 16 * 129)]),                    # more chosen than threads
+])
+def test_many_lists_over_many_pages(dim, heads, share, n, seqs, levels):
+    """One block for each list, several rounds of pages for each of its warps."""
+    c = Choice(len(seqs), seqs, heads, share, dim, 16, levels)
+    rows = sorted({0, 1, 2, 30, 59, 60})
+    got, want = c.run(n, 1, 2).cpu(), c.want(n, 1, 2, rows)
+    some = want[:, 0, 0] != -2
+    assert sum(r for r, _ in seqs) * heads > 152 and torch.equal(got[some], want[some])
