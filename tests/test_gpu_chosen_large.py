@@ -1,5 +1,5 @@
 """The calls around chosen pages at sizes that take other ways through the kernels than test_gpu_chosen.py's: rows by the
-thousand, whole caches' bounds, more lists than blocks. Against the same float64 definitions, within the same bounds; plain forms of these sizes run on the GPU in float64."""
+thousand, whole caches' bounds, more lists than blocks, lists of thousands of keys in one block. Against the same float64 definitions, within the same bounds; plain forms of these sizes run on the GPU in float64."""
 import math
 
 import pytest
@@ -7,8 +7,9 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2506_15745_gb300.paged import PageBounds, PagedBatch, PagedCache, Rotary  # noqa: E402
-from test_gpu_chosen import Choice, ints, parts, same_bits, turns  # noqa: E402
-from test_gpu_paged import make_rows  # noqa: E402
+from test_gpu_chosen import Choice, check_chosen, ints, parts, random_lists, run_chosen, same_bits, turns  # noqa: E402
+from test_gpu_chosen_forms import chosen_need  # noqa: E402
+from test_gpu_paged import Setup, make_rows  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -150,3 +151,42 @@ def test_many_lists_over_many_pages(dim, heads, share, n, seqs, levels):
     got, want = c.run(n, 1, 2).cpu(), c.want(n, 1, 2, rows)
     some = want[:, 0, 0] != -2
     assert sum(r for r, _ in seqs) * heads > 152 and torch.equal(got[some], want[some])
+
+
+# ------------------------------------------------------------------- long lists
+LONG = [  # fmt, dim, heads, share, page, [(rows, kv)], n, whether work is shared out with a workspace (three blocks per SM; None: not said)
+    ("bf16", 128, 8, 2, 64, [(50, 5000)], 70, False),                      # a block for each tile: 35 steps for each warp
+    ("bf16", 128, 8, 2, 64, [(70, 5000), (0, 9), (12, 4990)], 70, False),  # blocks in turn
+    ("bf16", 128, 8, 1, 64, [(63, 5000)], 70, True),                       # shared out
+    ("u8", 128, 8, 2, 64, [(50, 5000)], 70, False),
+    ("u8", 128, 8, 2, 64, [(70, 5000), (0, 9), (12, 4990)], 70, False),
+    ("u8", 128, 8, 1, 64, [(63, 5000)], 70, True),
+    ("u8", 128, 8, 3, 16, [(60, 800), (3, 20), (28, 900)], 36, False),     # in turn, ragged, shorter
+    ("u4", 128, 8, 2, 64, [(50, 5000)], 70, False),
+    ("u4", 128, 8, 2, 64, [(70, 5000), (0, 9), (12, 4990)], 70, False),
+    ("u4", 128, 8, 1, 64, [(63, 5000)], 70, True),
+    ("u4", 128, 8, 3, 16, [(60, 800), (3, 20), (28, 900)], 36, False),
+    ("bf16", 64, 8, 2, 64, [(36, 5000)], 70, None),
+    ("bf16", 64, 8, 2, 64, [(70, 5000), (12, 4990)], 70, None),
+    ("u8", 64, 8, 2, 32, [(50, 5000)], 140, None),
+    ("u4", 64, 8, 2, 32, [(90, 5000)], 140, None),
+    ("bf16", 128, 2, 16, 64, [(45, 5000)], 70, None),                      # tiles of 16 query rows
+    ("u8", 128, 2, 16, 64, [(80, 5000)], 70, None),
+    ("u4", 128, 2, 12, 64, [(80, 5000)], 70, None),
+    ("bf16", 128, 1, 1, 16, [(1, 70000), (2, 40000)], 3000, True),         # 48000 keys over all blocks
+    ("u8", 128, 1, 1, 16, [(1, 70000), (2, 40000)], 3000, True),
+]
+
+
+@pytest.mark.parametrize("junk", [False, True])
+@pytest.mark.parametrize("case", range(len(LONG)))
+def test_long_lists(case, junk):
+    """A warp takes more steps than it looks up at once, several times over; rings go on into the next tile."""
+    fmt, dim, heads, share, page, seqs, n, shared = LONG[case]
+    gen = torch.Generator().manual_seed(1500 + case)
+    s = Setup(gen, fmt, heads, dim, page, [k for _, k in seqs], [r for r, _ in seqs])
+    chosen = random_lists(gen, s, n, junk)
+    if shared is not None:
+        assert (chosen_need(s.cache, s.batch, heads * share, n) > 0) == shared
+    q, out, lse = run_chosen(s, share, chosen, 1600 + case)
+    check_chosen(s, q, chosen, out, lse, dim ** -0.5)
