@@ -1,5 +1,6 @@
 """The calls around chosen pages at sizes that take other ways through the kernels than test_gpu_chosen.py's: rows by the
-thousand, whole caches' bounds, more lists than blocks, lists of thousands of keys in one block. Against the same float64 definitions, within the same bounds; plain forms of these sizes run on the GPU in float64."""
+thousand, whole caches' bounds, more lists than blocks, lists of thousands of keys in one block, work that is shared out with a
+workspace. Against the same float64 definitions, within the same bounds; plain forms of these sizes run on the GPU in float64."""
 import math
 
 import pytest
@@ -190,3 +191,61 @@ def test_long_lists(case, junk):
         assert (chosen_need(s.cache, s.batch, heads * share, n) > 0) == shared
     q, out, lse = run_chosen(s, share, chosen, 1600 + case)
     check_chosen(s, q, chosen, out, lse, dim ** -0.5)
+
+
+# ------------------------------------------------------------------- workspaces
+def shared_out(gen, fmt):
+    """Lists that blocks share with a workspace: 19200 keys each."""
+    s = Setup(gen, fmt, 2, 128, 16, [20000, 19500], [2, 1])
+    chosen = random_lists(gen, s, 1200)
+    need = chosen_need(s.cache, s.batch, 14, 1200)
+    assert need > 0
+    return s, chosen, need
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "u8", "u4"])
+def test_what_a_workspace_holds_does_not_matter(fmt):
+    """Bytes of ones and bytes that an earlier call of other sizes left, on another stream; nothing behind its end is touched."""
+    gen = torch.Generator().manual_seed(1700)
+    s, chosen, need = shared_out(gen, fmt)
+    q, want, lse = run_chosen(s, 7, chosen, 1701)
+    check_chosen(s, q, chosen, want, lse, 128 ** -0.5)
+    other = random_lists(gen, s, 900).cuda()
+    assert 0 < chosen_need(s.cache, s.batch, 14, 900) <= need
+    q, chosen = q.cuda(), chosen.cuda()
+    side, ws = torch.cuda.Stream(), torch.empty(need + 4096, dtype=torch.uint8, device="cuda").fill_(255)
+    torch.cuda.synchronize()
+    for k in range(6):
+        if k % 2:
+            s.cache.attend_chosen(q, s.batch, other, workspace=ws[:need], stream=side)
+        out = s.cache.attend_chosen(q, s.batch, chosen, workspace=ws[:need], stream=side)
+        side.synchronize()
+        assert same_bits(out, want)
+    assert (ws[need:] == 255).all()
+
+
+def test_graphs_with_workspaces_of_their_own():
+    """Two captured calls that are shared out, replayed at the same time on two streams, eager calls between and beside them."""
+    gen = torch.Generator().manual_seed(1800)
+    s, chosen, need = shared_out(gen, "bf16")
+    lists = [chosen.cuda(), random_lists(gen, s, 1200).cuda()]
+    q = [make_rows(gen, s.total, 14, 128).cuda() for _ in range(2)]
+    want = [s.cache.attend_chosen(*x) for x in zip(q, (s.batch,) * 2, lists)]
+    outs, graphs, streams = [torch.zeros_like(x) for x in q], [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for i in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=streams[i]):
+            s.cache.attend_chosen(q[i], s.batch, lists[i], out=outs[i])
+        graphs.append(graph)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for t in outs:
+            t.zero_()
+        torch.cuda.synchronize()
+        for g, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                g.replay()
+        again = s.cache.attend_chosen(q[0], s.batch, lists[0])
+        torch.cuda.synchronize()
+        assert same_bits(outs[0], want[0]) and same_bits(outs[1], want[1]) and same_bits(again, want[0])
