@@ -7,6 +7,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
+import chosen_ref as cref  # noqa: E402
 from paper_2506_15745_gb300.paged import PageBounds, PagedBatch, PagedCache, Rotary  # noqa: E402
 from test_gpu_chosen import Choice, check_chosen, ints, parts, random_lists, run_chosen, same_bits, turns  # noqa: E402
 from test_gpu_chosen_forms import chosen_need  # noqa: E402
@@ -249,3 +250,43 @@ def test_graphs_with_workspaces_of_their_own():
         again = s.cache.attend_chosen(q[0], s.batch, lists[0])
         torch.cuda.synchronize()
         assert same_bits(outs[0], want[0]) and same_bits(outs[1], want[1]) and same_bits(again, want[0])
+
+
+# ------------------------------------------------------------------- weights over bf16 pages
+@pytest.mark.parametrize("dim,share,rows,kv,n", [(128, 7, 1, 1000, 70), (64, 7, 1, 1000, 70), (128, 16, 1, 1000, 70), (128, 2, 1, 4000, 250),
+                                                 (128, 1, 82, 1200, 80), (128, 2, 1, 20000, 1250)])
+def test_weights_have_16_bits_over_bf16_pages(dim, share, rows, kv, n):
+    """Weights next to where bf16 rounds one way or the other, under values that cancel: a weight of 8 bits would be off by up to
+    2^-8 sum p |v| in one direction.
+
+    Scores are -log2 of 1, or of 1/2 plus a little less or a little more than half a step of bf16 there, held to 2^-16 by two
+    channels; values are 1 where the weight rounds down and -1 where it rounds up. Of sum p |v| an output may be off by 2^-16 for
+    the two bf16 parts of a weight, by twice the scores' error (2^-16 of their products), and by 2^-16 for fp32 sums: an
+    accumulator takes 4 products for each 32 keys of its warp, 40 at most here, each off by 2^-22 at most."""
+    gen = torch.Generator().manual_seed(1900)
+    heads = 8 if rows > 1 else 2
+    s = Setup(gen, "bf16", heads, dim, 16, [kv], [rows], garbage=False)
+    up = torch.rand(kv, generator=gen) < 0.5
+    x = -torch.log2(torch.where(up, 0.5 + 2.0 ** -9 * 1.05, 0.5 + 2.0 ** -9 * 0.95).double())
+    high = x.bfloat16()
+    k, v = torch.zeros(kv, heads, dim).bfloat16(), torch.where(up, -1.0, 1.0)[:, None, None].expand(kv, heads, dim).bfloat16()
+    k[:, :, 0], k[:, :, 1] = high[:, None], (x - high.double()).bfloat16()[:, None]
+    k[0, :, :2] = 0  # the largest score, weight 1
+    whole = PagedBatch(s.batch.table, ints(0, kv), s.batch.kv_len, total_rows=kv, max_rows=kv, max_kv=kv)
+    s.cache.write(k.cuda(), v.contiguous().cuda(), whole)
+    q = torch.zeros(rows, heads * share, dim).bfloat16()
+    q[..., :2] = -1
+    chosen = torch.full((rows, heads, n), -1, dtype=torch.int32)
+    for i in range(rows):
+        pages = (kv - rows + i) // 16 + 1
+        chosen[i, :, :min(n, pages)] = torch.arange(min(n, pages), dtype=torch.int32)
+    scale = math.log(2.0)
+    out = s.cache.attend_chosen(q.cuda(), s.batch, chosen.cuda(), scale=scale).double().cpu()
+    o, _, weight, size = cref.attend(q.double(), k.double(), v.double(), chosen, 16, scale)
+    tol = 2.0 ** -8 * o.abs() + (2.0 ** -15 + torch.expm1(2.0 * 2.0 ** -16 * size[..., None])) * weight
+    assert ((out - o).abs() <= tol).all(), float(((out - o).abs() / tol).max())
+    # The bound tells: weights rounded once to bf16 are outside of it.
+    p = torch.exp2(-(k[:, 0, 0].double() + k[:, 0, 1].double()))[:16 * n if rows == 1 else kv]
+    once = float((p.bfloat16().double() * v[:len(p), 0, 0].double()).sum() / p.sum())
+    if rows == 1:
+        assert abs(once - float(o[0, 0, 0])) > 4.0 * float(tol.max())
