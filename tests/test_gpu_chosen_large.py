@@ -8,6 +8,8 @@ import pytest
 torch = pytest.importorskip("torch")
 
 import chosen_ref as cref  # noqa: E402
+from paper_2506_15745_gb300 import ipv  # noqa: E402
+from paper_2506_15745_gb300.cache import PingPongCache  # noqa: E402
 from paper_2506_15745_gb300.paged import PageBounds, PagedBatch, PagedCache, Rotary  # noqa: E402
 from test_gpu_chosen import Choice, check_chosen, ints, parts, random_lists, run_chosen, same_bits, turns  # noqa: E402
 from test_gpu_chosen_forms import chosen_need  # noqa: E402
@@ -290,3 +292,30 @@ def test_weights_have_16_bits_over_bf16_pages(dim, share, rows, kv, n):
     once = float((p.bfloat16().double() * v[:len(p), 0, 0].double()).sum() / p.sum())
     if rows == 1:
         assert abs(once - float(o[0, 0, 0])) > 4.0 * float(tol.max())
+
+
+# ------------------------------------------------------------------- the pass's compaction
+def test_a_gather_of_the_kept_rows_is_the_compaction():
+    """The rows that the pass keeps of contiguous slabs, and a gather by ipv_select's indices of the same rows in pages."""
+    layers, heads, dim, grid, frames, budget = 3, 2, 64, 4, 14, 96
+    p, n_slabs, n = grid * grid, layers * heads, grid * grid * frames
+    gen = torch.Generator().manual_seed(2000)
+    ipv.init(device=0, dtype="bf16", max_head_dim=dim, max_frame_tokens=p, max_slabs=n_slabs, token_capacity=n)
+    pp = PingPongCache(n_slabs, n, dim, "bf16")
+    pp.k[0], pp.v[0] = make_rows(gen, n_slabs, n, dim).cuda(), make_rows(gen, n_slabs, n, dim).cuda()
+    pp.n_tokens = n
+    tar, van = torch.empty((n_slabs, n), device="cuda"), torch.empty((n_slabs, n), device="cuda")
+    ipv.score(*pp.structs(False), layers, heads, dim, n, grid, grid, tar, van)
+    kept = torch.empty((n_slabs, budget), dtype=torch.int32, device="cuda")
+    ipv.select(tar, van, n_slabs, n, grid, grid, budget, 0.5, kept)
+    pool = PagedCache(40, 16, n_slabs, dim)
+    pages = torch.randperm(40, generator=gen).to(torch.int32).cuda()
+    source = PagedBatch(pages[None, :14], ints(0, n), ints(n), total_rows=n, max_rows=n, max_kv=n)
+    pool.write(pp.k[0].transpose(0, 1).contiguous(), pp.v[0].transpose(0, 1).contiguous(), source)
+    whole = PagedBatch(pages[None, 14:20], ints(0, budget), ints(budget), total_rows=budget, max_rows=budget, max_kv=budget)
+    pool.gather(pool, source, whole, kept[None])
+    done = torch.empty_like(kept)
+    pp.compress(layers, heads, grid, grid, budget, 0.5, done, pid_valid=False)
+    k, v = pool.read(whole)
+    assert torch.equal(done, kept)
+    assert same_bits(k.transpose(0, 1), pp.k_live[:, :budget]) and same_bits(v.transpose(0, 1), pp.v_live[:, :budget])
