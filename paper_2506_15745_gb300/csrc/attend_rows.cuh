@@ -57,12 +57,14 @@ struct Ring {
   static constexpr int kStages = FMT == kBf16 ? 3 : 2;
 };
 
-// How a kernel lays itself out. Chosen pages of 128 channels are mostly found in L2, and a tile has few steps: what counts is
+// How a kernel lays itself out. Over all pages, blocks per SM: bf16 at 128 channels has enough bytes in flight with one, codes
+// need warps to widen them (32 ragged 4-bit streams: 3 blocks of 168 registers 123 us, 4 of 128, with spills, 134). Chosen pages of 128 channels are mostly found in L2, and a tile has few steps: what counts is
 // how many warps there are, and that other blocks go on while one starts a tile or joins its warps. bf16: rings of two halves of
 // a stage, K's and V's, each refilled as soon as it has been read, the warps' results in their place at a tile's end, and three
-// blocks per SM (questions of 8 streams 67 us; two blocks with 3 halves and the next tile on its way 84, one of 8 warps 103, of
+// blocks per SM (questions of 8 streams 66 us; two blocks with 3 halves and the next tile on its way 84, one of 8 warps 103, of
 // 4 with 3 stages 126). 8-bit codes: 3 halves and the results behind them, three blocks per SM instead of two (200 streams'
-// tokens 156 us against 169, questions 95 against 105; 32 streams', a block each, 34 against 32).
+// tokens 154 us against 169, questions 96 against 105; 32 streams', a block each, 35 against 32). Three blocks leave 168
+// registers, of which the chosen instances for 8 query rows over 8 and 4 bits at 128 channels want a few more (92 and 48 bytes spilled).
 template <int FMT, int DP, int NR, bool CHOSEN>
 struct Layout {
   static constexpr bool kHalves = CHOSEN && FMT != kU4 && DP == 128 && NR == 1;
@@ -199,9 +201,6 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, const Seq& s, int
   if (c == 0 && a.lse) a.lse[row * a.q_heads + hq] = sum == 0.0f ? kNegInf : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
-// Resident blocks per SM that registers and shared memory are cut to: bf16 at 128
-// channels has enough bytes in flight with one, codes need warps to widen them (32
-// ragged 4-bit streams: 3 blocks of 168 registers 123 us, 4 of 128, with spills, 134).
 // Clusters: a block's rank, the address of a shared-memory word in block r of
 // the cluster, loads from there, and the barrier of all blocks.
 __device__ __forceinline__ uint32_t cluster_rank() {

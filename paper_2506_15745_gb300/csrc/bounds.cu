@@ -54,10 +54,11 @@ __device__ __forceinline__ uint32_t quantise_pair(uint32_t x, float down, bool u
 // 32 of one group, in the order in which they are held), 32 / kLanes rows are read at once, kAtOnce times. The minima and maxima
 // are taken in bf16 pairs, which codes become first, and then joined by halves: in each round a lane gives away those that
 // its partner keeps. The step follows from the largest magnitude's bits.
-// A compacted cache of 112 heads of 6272 rows: bf16 (180 MB) 29.2 us, 6.2 TB/s, HBM-bound; 8 bits (96 MB) 26 us, 4 bits 29 us, bound
-// by about 5 instructions for each value. A block for each page, lanes with 8 channels: 28.8, 53.7 and 49.2 us, and 10.2 instead
-// of 5.0 over 8 x 1000 bf16 rows in pages of 16. 7 blocks per SM: 5 leave a part of a fourth round (30.2 us), at 8 it spills
-// (32.1). Few pages, of 128 rows, 8 x 1000 8-bit rows: 6.6 us with four warps for each, 10.7 with one. The pages of 8 new
+// A compacted cache of 112 heads of 6272 rows: bf16 (180 MB) 29.4 us, 6.2 TB/s, HBM-bound; 8 bits (96 MB) 28 us, 4 bits 31 us: 7.6
+// and 8.3 instructions for each value, with the ALU pipe active 61% and 72% of the time and issue 65% and 64%, at 4 blocks of
+// 95 and 124 registers per SM, whose warps wait for their loads between (2.3 and 1.1 of them per issue). A block for each page,
+// lanes with 8 channels: 28.8, 53.7 and 49.2 us, and 10.2 instead of 5.0 over 8 x 1000 bf16 rows in pages of 16. bf16, 7 blocks per
+// SM: 5 leave a part of a fourth round (30.2 us), 8 spill more than the 8 and 20 bytes of 7 (32.1). Few pages, of 128 rows, 8 x 1000 8-bit rows: 6.6 us with four warps for each, 10.7 with one. The pages of 8 new
 // tokens are a launch and three dependent loads.
 constexpr int64_t kFewPages = 2048;  // pages and heads up to which four warps take one of more rows than a warp reads at once
 
@@ -307,11 +308,13 @@ __device__ uint32_t mark_largest(uint32_t* keys, int first, int end, int need, i
 
 // A cluster takes one new row and KV head: its blocks score the pages, 16 at a time
 // per warp, the next 16 on their way, into the first block's shared memory; that block chooses. Every
-// page's 2 dim + 4 bytes are read once for a row. 32 ragged streams of up to 769 pages, 8 KV heads with 8 query
-// heads each (31 MB): 14.5 us, 2.1 TB/s. The longest streams' blocks set the time: 7 dependent rounds of loads per warp (about
-// 7 us), then the selection with its barriers (2.5 us); without the products 2.4 us less. More warps per list
-// (512 threads: 15.1 us, spills), four blocks per SM (64 registers: 30 us) and rings of 3 tiles in shared memory
-// (asynchronous copies: 14.4 us, of equally long streams 18.2 against 15.8) were slower or no faster. One stream, 98 pages: 4.8 us.
+// page's 2 dim + 4 bytes are read once for a row, by the rows of a question each for itself (8 ragged streams of up to 61 rows,
+// 193 pages, 4 KV heads: 30 us for 3.4 MB of bounds and queries). 32 ragged streams of up to 769 pages, 8 KV heads with 8 query
+// heads each (31 MB): 14.5 us, 2.1 TB/s. The longest streams' blocks set the time, one for each list: 7 rounds per warp of loads, products and
+// maxima, one after the other, then the selection with its barriers (2.5 us); without the products 2.4 us less. Issue is active
+// 24%: latency, and not of the loads alone, as rings of 3 tiles in shared memory (asynchronous copies) were no faster (14.4 us, of
+// equally long streams 18.2 against 15.8), nor were more warps per list (512 threads: 15.1 us, spills; at 256 the kernel for 128
+// channels spills 4 bytes) or four blocks per SM (64 registers: 30 us). One stream, 98 pages: 4.8 us.
 template <int DP>
 __global__ void __launch_bounds__(kChooseThreads, 2) choose_kernel(ChooseArgs a) {
   constexpr int kCodes = 2 * DP;              // bytes of a page's bounds, and of a query head's parts

@@ -251,9 +251,9 @@ constexpr int64_t kClusterKeys = 8192, kClusterBytes = 1 << 20;
 
 // Chosen pages: blocks take row tiles and heads whole and in turn where that keeps them busy for this many tenths of their
 // rounds: nothing to join, and the blocks that run at the same time are near one another in the cache (and in L2). Lists of
-// 2048 keys, 8 KV heads, bf16: 8 sequences of 12 tokens 89 us against 123 shared out, of 10 tokens (7 tenths) 87 against 104, 60
-// single tokens 79 against 85; 4 bits: 160 tokens 96 against 103; 8 bits: 80 tokens (7 tenths) 84 against 73, 100 tokens 91
-// against 89.
+// 2048 keys, 8 KV heads, single tokens, in turn against shared out: bf16, 80 tokens (7 tenths) 100 us against 110, 100 tokens 121
+// against 133; 8 bits 75 against 78 and 86 against 91; 4 bits 57 against 62 and 66 against 71. With 72 tokens (6 tenths) shares
+// take 100, 72 and 57 us, no more than two rounds do.
 constexpr int kInTurnTenths = 7;
 // With less than a round, 4 or 2 blocks take a tile each as a cluster where they all have room at once, or one where two have
 // not: no parts to write, no second kernel. 4 bits: 8 streams 13.0 us against 17.2 shared out, 24 streams 24.8 against 28.4 (two
@@ -520,8 +520,12 @@ extern "C" ipv_status ipv_attend_wait_limit(int64_t nanoseconds) {
   return IPV_OK;
 }
 
-// Rows up to which 4 warps take one: as many blocks of 4 warps as 152 SMs hold at once. 2 warps up to three times as many, then
-// one: fewer look-ups per head (28 + 4 heads with norms, 1568 rows: 4 warps 7.7 us, 2 7.1, 1 10.8; 3136 rows: 15.7, 13.4, 13.2).
+// Rows up to which 4 warps take one: as many blocks of 4 warps as 152 SMs hold of 6 each. 2 warps up to three times as many, then
+// one: fewer look-ups per head. 28 + 4 heads with norms, 4, 2 and 1 warps: bf16, 128 channels in halves, 784 rows 7.1, 6.8, 8.4 us (a
+// call is the host's 6.7), 1568 rows 8.0, 7.2, 11.1, 2352 rows 11.3, 11.1, 12.0, 3136 rows 16.1, 13.8, 14.0; into 8 bits 7.2, 8.7, 12.8
+// at 784 rows, 11.0, 9.5, 14.5 at 1568, 21.0, 16.8, 16.2 at 3136; 64 channels as bf16. It is the rule of these instances: interleaved
+// pairs and partial halves of 128 channels have 4 blocks per SM, and would be up to 1.4 times faster with fewer warps between
+// 784 and 2352 rows (bits 8, interleaved: 784 rows 9.1, 7.0, 9.6; 1568 rows 13.0, 11.9, 10.4; 3136 rows 25.2, 19.4, 19.9).
 constexpr int64_t kRotateWave = 152 * 6;
 
 extern "C" ipv_status ipv_pages_write_rotated(const ipv_pages* pages, const ipv_batch* batch, const ipv_rotary* rotary,

@@ -7,9 +7,10 @@
 // lane has both ends of its pairs; elsewhere the partners come by shuffles. 1, 2 or 4
 // warps take a row: their lanes fetch its cosines and sines once and use them for
 // all the heads that they take, the next four heads on their way meanwhile. 16 frames
-// (59 MB, 9 us at the copy rate) take 13.2 us; issue slots, at about 300
+// (59 MB, 9 us at the copy rate) take 13.6 us, 16.0 into 8 and 4 bits; issue slots (66%), at about 320
 // instructions per four heads, and the look-ups at a row's start (position, then angles;
-// sequence, then page). 80 registers: at 64 it spills (16.3 us). Rows of 64 channels have one chunk
+// sequence, then page). The bf16 instance for all of 128 channels in halves has 80 registers and no spills with 6 blocks per SM,
+// at 64 registers it spills (16.3 us); those into codes spill 52 bytes at 80. Rows of 64 channels have one chunk
 // for a lane (784 rows of 32 + 8 heads 4.8 us; with an empty second chunk 7.1).
 #include "paged_codes.cuh"
 
