@@ -1,5 +1,6 @@
 """Rotated writes, choices and attention over chosen pages in the forms that a call may take beside the usual ones: one long page
-for each sequence, one place on all axes, first uses."""
+for each sequence, one place on all axes, queries and results inside
+wider tensors, first uses."""
 import math
 import os
 import subprocess
@@ -11,9 +12,9 @@ torch = pytest.importorskip("torch")
 
 import chosen_ref as cref  # noqa: E402
 from paper_2506_15745_gb300 import ipv  # noqa: E402
-from paper_2506_15745_gb300.paged import PagedBatch, PagedCache, Rotary  # noqa: E402
-from test_gpu_chosen import ints, same_bits, turns  # noqa: E402
-from test_gpu_paged import bounds, make_rows  # noqa: E402
+from paper_2506_15745_gb300.paged import PageBounds, PagedBatch, PagedCache, Rotary  # noqa: E402
+from test_gpu_chosen import ints, random_lists, same_bits, turns  # noqa: E402
+from test_gpu_paged import Setup, bounds, make_rows  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -71,6 +72,43 @@ def test_one_place_on_all_axes(interleaved):
     assert all(same_bits(a, b) for a, b in zip(*made))
     want, size = cref.turned(q, None, 0.0, table, at.expand(3, 40), [24, 24, 16], interleaved)
     assert ((made[0][0].double().cpu() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -16 * size).all()
+
+
+@pytest.mark.parametrize("fmt,dim,rows", [("bf16", 128, 3), ("bf16", 80, 70), ("u8", 128, 70), ("u4", 64, 3)])
+def test_queries_and_results_inside_wider_tensors(fmt, dim, rows):
+    """q a slice of a projection's rows, out one of another tensor's, heads first in one of them: the bits of contiguous ones, and
+    nothing beside them is touched."""
+    gen = torch.Generator().manual_seed(dim + rows)
+    s = Setup(gen, fmt, 2, dim, 16, [700, 90], [rows, 1])
+    made = PageBounds(s.cache)
+    whole = PagedBatch(s.batch.table, ints(0, 700, 790), s.batch.kv_len, total_rows=790, max_rows=700, max_kv=700)
+    made.update(s.cache, whole)
+    q = make_rows(gen, s.total, 8, dim).cuda()
+    wide = torch.full((s.total + 2, 14, dim), math.nan, dtype=torch.bfloat16, device="cuda")
+    wide[:s.total, 3:11] = q
+    inside = wide[:, 3:11]
+    heads_first = torch.full((11, s.total, dim), 7.0, dtype=torch.bfloat16, device="cuda")
+    lists = made.choose(q, s.batch, 9)
+    assert torch.equal(made.choose(inside, s.batch, 9), lists)
+    want = s.cache.attend_chosen(q, s.batch, lists)
+    out = heads_first[1:9].transpose(0, 1)
+    assert s.cache.attend_chosen(inside, s.batch, lists, out=out) is out
+    assert same_bits(out, want) and (heads_first[0] == 7.0).all() and (heads_first[9:] == 7.0).all()
+    chosen = random_lists(gen, s, 44).cuda()  # over 512 keys
+    assert same_bits(s.cache.attend_chosen(inside, s.batch, chosen, out=out), s.cache.attend_chosen(q, s.batch, chosen))
+    assert torch.isnan(wide[:, :3]).all() and torch.isnan(wide[:, 11:]).all()
+
+
+def test_rotated_rows_into_one_page_per_sequence():
+    """Without a table: what the same rows give through pages of 16."""
+    gen = torch.Generator().manual_seed(9)
+    q, k, v = make_rows(gen, 90, 4, 64).cuda(), make_rows(gen, 90, 2, 64).cuda(), make_rows(gen, 90, 2, 64).cuda()
+    rotary, at = Rotary(turns(gen, 200, 64).cuda()), torch.randint(0, 200, (90,), generator=gen, dtype=torch.int32).cuda()
+    made = []
+    for cache, table in ((PagedCache(2, 333, 2, 64), None), (PagedCache(10, 16, 2, 64), ints(*range(9, -1, -1)).view(2, 5))):
+        batch = PagedBatch(table, ints(0, 50, 90), ints(70, 40), total_rows=90, max_rows=50, max_kv=70)
+        made.append((cache.write_rotated(q, k, v, batch, rotary, at), *cache.read(batch)))
+    assert all(same_bits(a, b) for a, b in zip(*made))
 
 
 FIRST_USES = """
