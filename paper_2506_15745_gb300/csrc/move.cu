@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(kBlock) copy_kernel(CopyArgs a) {
 // chunks, T of them per lane, and 8 / T rows at once: 8 loads on their way in
 // each lane whatever the format. Before that a thread for each row looks up (the kept index,
 // then the pages) where it comes from and goes to. 112 heads of 9408 bf16 rows cut to 6272 (722 MB with the indices) 109.9 us,
-// 6.6 TB/s, 97% of the copy rate; 8 streams' 4-bit rows cut to two thirds (233 MB) 41 us, 84%.
+// 6.6 TB/s, 97% of the copy rate; 8 streams' 4-bit rows cut to two thirds (199 MB) 44 us, 66%.
 constexpr int kTeams = kBlock / 8;
 
 template <int T>
